@@ -34,6 +34,13 @@ EXPORTS = ("da_spmm", "da_spmm_ex", "da_spmm_select", "da_spmm_features", "da_cs
            "da_spmm_algo_name", "da_spmm_last_error")
 
 
+# include/da_layers.h; called through the extension module
+DA_F32, DA_BF16 = 0, 1
+DA_ACT_NONE, DA_ACT_RELU, DA_ACT_SILU, DA_ACT_GELU, DA_ACT_SIGMOID = range(5)
+LAYER_EXPORTS = ("da_group_norm_sizes", "da_group_norm", "da_group_norm_backward", "da_distill_workspace", "da_distill",
+                 "da_distill_backward")
+
+
 class da_features(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("nnz", ctypes.c_int64),
                 ("row_nnz_mean", ctypes.c_double), ("row_nnz_std", ctypes.c_double),

@@ -5,14 +5,15 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdaspmm.so")
-SOURCES = ["da_spmm_api.hip", "da_spmm_select.cpp"]
+SOURCES = ["da_spmm_api.hip", "da_layers.hip", "da_spmm_select.cpp"]
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-munsafe-fp-atomics",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
     # packed fp32 arithmetic stays off for all device code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
@@ -27,16 +28,33 @@ def hipcc() -> str:
 
 def build_hip(verbose: bool = False) -> str:
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [hipcc(), *FLAGS, "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-o", tmp,
-           *[os.path.join(CSRC, s) for s in SOURCES]]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
+    objects = [tmp + "." + s + ".o" for s in SOURCES]
+
+    def compile_one(job):
+        source, obj = job
+        return run([hipcc(), *FLAGS, "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-c", os.path.join(CSRC, source), "-o", obj])
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + out)
+        return out
+
+    try:
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            said = list(pool.map(compile_one, zip(SOURCES, objects)))
+        said.append(run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *objects]))
+        if verbose:
+            for out in said:
+                if out.strip():
+                    print(out)
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     os.replace(tmp, LIB)
     build_native(verbose)
     return LIB
@@ -58,7 +76,7 @@ def build_native(verbose: bool = False) -> str:
            "-isystem", os.path.join(rocm, "include"), "-DTORCH_EXTENSION_NAME=_native",
            "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"],
            "-isystem", os.path.join(tdir, "include"), "-isystem", os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
-           os.path.join(CSRC, "native.cpp"), "-o", tmp,
+           os.path.join(CSRC, "native.cpp"), os.path.join(CSRC, "native_layers.cpp"), "-o", tmp,
            "-L" + PKG, "-ldaspmm", "-L" + os.path.join(tdir, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
            "-ltorch_hip", "-lc10", "-lc10_hip", "-lamdhip64", "-L" + os.path.join(rocm, "lib"), "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(tdir, "lib")]
     if verbose:

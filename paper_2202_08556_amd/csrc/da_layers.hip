@@ -1,0 +1,471 @@
+// Host side of include/da_layers.h: argument checks, choice of kernels and launch geometry.
+#include "da_layers.h"
+
+#include "da_internal.h"
+#include "da_norm_kernels.hip"
+#include "da_distill_kernels.hip"
+#include "da_spmm.h"
+
+#include <algorithm>
+#include <numeric>
+
+namespace {
+
+using namespace daspmm;
+
+int fail(int code, const char* text) { return set_error(code, text); }
+
+int launched(const char* where) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? DA_OK : set_hip_error(e, where);
+}
+
+bool known_dtype(int d) { return d == DA_F32 || d == DA_BF16; }
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int pow2_at_least(int64_t x) {
+    int p = 1;
+    while (p < x) p <<= 1;
+    return p;
+}
+
+// ------------------------------------------------------------------------------------------
+// group norm
+// ------------------------------------------------------------------------------------------
+struct NormPlan {
+    int V;                   // numbers of an access: divides a group
+    // each
+    bool each;
+    int P, E;
+    int64_t each_grid;
+    // team
+    int team;                // threads of a team; 0: none
+    int GT;
+    int64_t team_grid, longest;
+    // split
+    bool split;
+    int TX;
+    int64_t per, per_sample, chunks, most_long;
+    bool table;
+    // memory
+    size_t stats, part_bytes, table_at, list_at, forward, means_at, backward;
+    int64_t part_rows;
+};
+
+constexpr int64_t kNormMaxChannels = 1 << 20, kNormMaxGroups = 65535;
+
+int norm_check(int dtype, int64_t rows, int64_t samples, int64_t channels, int64_t groups) {
+    if (!known_dtype(dtype)) return fail(DA_ERR_UNSUPPORTED, "dtype is neither DA_F32 nor DA_BF16");
+    if (rows < 0 || samples < 0 || channels < 0) return fail(DA_ERR_INVALID_ARG, "negative size");
+    if (groups < 1 || channels % groups != 0) return fail(DA_ERR_INVALID_ARG, "channels are no multiple of groups");
+    if (rows > INT32_MAX || samples > INT32_MAX || channels > kNormMaxChannels || groups > kNormMaxGroups)
+        return fail(DA_ERR_UNSUPPORTED, "size too large");
+    return DA_OK;
+}
+
+// Which kernels a shape takes.  train: statistics are kept and the backward pass is planned, too.
+NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_t C, int64_t G, bool train) {
+    NormPlan p{};
+    const int64_t cg = C / G, length = ragged || samples == 0 ? 0 : rows / samples;
+    const int most = dtype == DA_F32 ? 4 : 8;
+    p.V = 1;
+    while (p.V < most && cg % (2 * p.V) == 0) p.V *= 2;
+    const int64_t cgv = cg / p.V, cv = C / p.V, cus = compute_units();
+
+    if (!ragged && length == 1 && cgv * p.V <= 64 * 32) {
+        int E = 1;
+        while (64 * E < cgv) E *= 2;
+        if (E * p.V <= 32) {
+            p.each = true;
+            p.E = E;
+            p.P = pow2_at_least(ceil_div(cgv, E));
+            const int64_t per_block = kNormBlock / p.P, m = G / std::gcd(G, per_block);
+            const int64_t need = ceil_div(rows * G, per_block), cap = std::max<int64_t>(m, cus * 8 / m * m);
+            p.each_grid = std::min(cap, ceil_div(need, m) * m);
+            p.part_rows = p.each_grid;
+        }
+    }
+    if (!p.each) {
+        const int E = p.V >= 8 ? 4 : 8;
+        const double mean = samples ? (double)rows / (double)samples : 0.0;
+        auto tile = [&](int team) { return std::max<int64_t>(1, std::min<int64_t>(team / cgv, G)); };
+        auto held = [&](int team) { return cgv > team ? 0 : (team / (tile(team) * cgv)) * (int64_t)E; };
+        for (int team : {64, 256, 1024}) {
+            if (cgv > team) continue;
+            if (team == 1024 || (ragged ? 2 * mean : mean) <= (double)held(team)) { p.team = team; break; }
+        }
+        // A block takes up to a few times what its registers hold; longer samples are split.
+        p.longest = cgv > 1024 ? 0 : (ragged ? 4 : 2) * held(1024);
+        if (!ragged && length > p.longest) p.team = 0;
+        if (ragged && cgv > 1024) p.team = 0;
+        p.split = ragged ? rows > p.longest : length > p.longest;
+        if (p.team) {
+            p.GT = (int)tile(p.team);
+            const int64_t teams = p.team == 64 ? 4 : 1, cap = train ? cus * (p.team == 1024 ? 2 : 8) : 1 << 20;
+            p.team_grid = std::min(ceil_div(samples, teams), cap);
+            p.part_rows = p.team_grid;
+        }
+        if (p.split) {
+            p.TX = (int)std::min<int64_t>(cv, kNormBlock);
+            const int64_t TY = kNormBlock / p.TX;
+            const int64_t target = std::clamp<int64_t>(rows * C / (cus * 8), 4096, 65536);
+            p.per = std::max<int64_t>(ceil_div(target, C), 1);
+            p.per = ceil_div(p.per, TY) * TY;
+            if (ragged) {
+                p.table = true;
+                p.most_long = std::min(samples, rows / (p.longest + 1));
+                p.chunks = rows / p.per + p.most_long;
+            } else {
+                p.per_sample = ceil_div(length, p.per);
+                p.most_long = samples;
+                p.chunks = samples * p.per_sample;
+            }
+        }
+    }
+    p.stats = train || p.split ? (p.each ? 0 : (size_t)(samples * G * 2)) : 0;
+    // Forward: chunks' statistics; both: table.  Backward: sums of the blocks and chunks, means.
+    const size_t table = p.table ? 64 + round16((size_t)p.chunks * sizeof(int2)) + (size_t)p.most_long * sizeof(int4) : 0;
+    const size_t fpart = p.split ? round16((size_t)(p.chunks * cv) * sizeof(float2)) : 0;
+    p.forward = fpart + table + (train ? 0 : round16(p.stats * sizeof(float)));
+    p.part_bytes = round16((size_t)((p.part_rows + (p.split ? p.chunks : 0)) * 2 * C) * sizeof(float));
+    p.means_at = p.part_bytes + table;
+    p.backward = p.means_at + (p.split ? round16((size_t)(samples * G * 2) * sizeof(float)) : 0);
+    return p;
+}
+
+NormChunks norm_chunks(const NormPlan& p, char* table) {
+    NormChunks ch{};
+    ch.per = p.per;
+    ch.each = p.per_sample;
+    ch.count = p.chunks;
+    if (p.table) {
+        ch.counts = reinterpret_cast<int*>(table);
+        ch.table = reinterpret_cast<int2*>(table + 64);
+        ch.list = reinterpret_cast<int4*>(table + 64 + round16((size_t)p.chunks * sizeof(int2)));
+    }
+    return ch;
+}
+
+void fill_table(const NormPlan& p, const NormShape& sh, const NormChunks& ch, hipStream_t s) {
+    if (!p.table) return;
+    hipLaunchKernelGGL(norm_clear_kernel, dim3(1), dim3(64), 0, s, const_cast<int*>(ch.counts));
+    hipLaunchKernelGGL(norm_long_kernel, dim3((unsigned)ceil_div(sh.samples, 256)), dim3(256), 0, s, sh, p.longest, p.per,
+                       const_cast<int*>(ch.counts), const_cast<int2*>(ch.table), const_cast<int4*>(ch.list));
+}
+
+template <class T, int V, bool BWD>
+void launch_each(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, const T* dy, int64_t ldy, T* out, float* part,
+                 hipStream_t s) {
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)p.each_grid), dim3(kNormBlock), 0, s, sh, p.P, x, (long)ldx, dy, (long)ldy, out,
+                           part);
+    };
+    if (p.E == 1) return go(norm_each_kernel<T, V, 1, BWD>);
+    if (p.E == 2) return go(norm_each_kernel<T, V, 2, BWD>);
+    if (p.E == 4) return go(norm_each_kernel<T, V, 4, BWD>);
+    if constexpr (V <= 4) {
+        if (p.E == 8) return go(norm_each_kernel<T, V, 8, BWD>);
+    }
+    if constexpr (V <= 2) {
+        if (p.E == 16) return go(norm_each_kernel<T, V, 16, BWD>);
+    }
+    if constexpr (V == 1) {
+        if (p.E == 32) return go(norm_each_kernel<T, V, 32, BWD>);
+    }
+}
+
+template <class T, int V, bool BWD>
+void launch_team(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, const T* dy, int64_t ldy, T* out, float* stats,
+                 float* part, hipStream_t s) {
+    auto go = [&](auto kernel, int block) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)p.team_grid, (unsigned)ceil_div(sh.G, p.GT)), dim3(block), 0, s, sh, p.GT,
+                           p.longest, x, (long)ldx, dy, (long)ldy, out, stats, part);
+    };
+    if (p.team == 64) go(norm_team_kernel<T, V, 64, BWD>, 256);
+    else if (p.team == 256) go(norm_team_kernel<T, V, 256, BWD>, 256);
+    else go(norm_team_kernel<T, V, 1024, BWD>, 1024);
+}
+
+template <class T, int V>
+void norm_forward(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, T* y, float* stats, char* ws, hipStream_t s) {
+    if (p.each) return launch_each<T, V, false>(p, sh, x, ldx, nullptr, 0, y, nullptr, s);
+    if (p.team) launch_team<T, V, false>(p, sh, x, ldx, nullptr, 0, y, stats, nullptr, s);
+    if (!p.split) return;
+    const int cv = sh.C / V;
+    const NormChunks ch = norm_chunks(p, ws + round16((size_t)(p.chunks * cv) * sizeof(float2)));
+    fill_table(p, sh, ch, s);
+    const dim3 grid((unsigned)p.chunks, (unsigned)ceil_div(cv, p.TX));
+    float2* part = reinterpret_cast<float2*>(ws);
+    hipLaunchKernelGGL((norm_stats_kernel<T, V>), grid, dim3(kNormBlock), 0, s, sh, ch, p.TX, x, (long)ldx, part);
+    hipLaunchKernelGGL((norm_join_kernel<V>), dim3((unsigned)p.most_long, (unsigned)sh.G), dim3(64), 0, s, sh, ch, part, stats);
+    hipLaunchKernelGGL((norm_apply_kernel<T, V, false>), grid, dim3(kNormBlock), 0, s, sh, ch, p.TX, x, (long)ldx,
+                       static_cast<const T*>(nullptr), 0L, stats, static_cast<const float*>(nullptr), y);
+}
+
+template <class T, int V>
+void norm_backward(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, const T* dy, int64_t ldy, const float* stats,
+                   T* dx, void* dw, void* db, char* ws, hipStream_t s) {
+    float* part = reinterpret_cast<float*>(ws);
+    float* chunk_part = part + p.part_rows * 2 * sh.C;
+    NormChunks ch{};
+    if (p.each) launch_each<T, V, true>(p, sh, x, ldx, dy, ldy, dx, part, s);
+    if (p.team) launch_team<T, V, true>(p, sh, x, ldx, dy, ldy, dx, const_cast<float*>(stats), part, s);
+    if (p.split) {
+        ch = norm_chunks(p, ws + p.part_bytes);
+        float* means = reinterpret_cast<float*>(ws + p.means_at);
+        fill_table(p, sh, ch, s);
+        const dim3 grid((unsigned)p.chunks, (unsigned)ceil_div(sh.C / V, p.TX));
+        hipLaunchKernelGGL((norm_grad_stats_kernel<T, V>), grid, dim3(kNormBlock), 0, s, sh, ch, p.TX, x, (long)ldx, dy, (long)ldy,
+                           stats, chunk_part);
+        hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)p.most_long, (unsigned)sh.G), dim3(256), 0, s, sh, ch, chunk_part,
+                           means);
+        hipLaunchKernelGGL((norm_apply_kernel<T, V, true>), grid, dim3(kNormBlock), 0, s, sh, ch, p.TX, x, (long)ldx, dy, (long)ldy,
+                           stats, means, dx);
+    }
+    if (dw || db)
+        hipLaunchKernelGGL(norm_param_grads_kernel, dim3((unsigned)ceil_div(2 * sh.C, 64)), dim3(1024), 0, s, sh.C, part,
+                           (long)p.part_rows, chunk_part, p.split && !p.table ? (long)p.chunks : 0L,
+                           p.split && p.table ? ch.counts : static_cast<const int*>(nullptr), dw, db, sh.param_dtype);
+}
+
+template <class F> void with_type_and_width(int dtype, int V, F&& f) {
+    if (dtype == DA_F32) {
+        if (V == 4) f(float{}, std::integral_constant<int, 4>{});
+        else if (V == 2) f(float{}, std::integral_constant<int, 2>{});
+        else f(float{}, std::integral_constant<int, 1>{});
+    } else {
+        if (V == 8) f(bf16{}, std::integral_constant<int, 8>{});
+        else if (V == 4) f(bf16{}, std::integral_constant<int, 4>{});
+        else if (V == 2) f(bf16{}, std::integral_constant<int, 2>{});
+        else f(bf16{}, std::integral_constant<int, 1>{});
+    }
+}
+
+int norm_shape(int dtype, int64_t rows, int64_t samples, const int32_t* offsets, int64_t channels, int64_t groups, const void* x,
+               int64_t ldx, const void* w, const void* b, int param_dtype, float eps, int act, NormShape* sh) {
+    const int st = norm_check(dtype, rows, samples, channels, groups);
+    if (st != DA_OK) return st;
+    if (!known_dtype(param_dtype)) return fail(DA_ERR_UNSUPPORTED, "param_dtype is neither DA_F32 nor DA_BF16");
+    if (act < 0 || act >= DA_NUM_ACTS) return fail(DA_ERR_INVALID_ARG, "unknown activation");
+    if (!(eps >= 0.f)) return fail(DA_ERR_INVALID_ARG, "eps is negative or no number");
+    if (ldx < channels) return fail(DA_ERR_INVALID_ARG, "leading dimension smaller than the extent it strides over");
+    if (rows > 0 && samples == 0) return fail(DA_ERR_INVALID_ARG, "rows without a sample");
+    if (!offsets && samples > 0 && rows % samples != 0) return fail(DA_ERR_INVALID_ARG, "rows are no multiple of samples");
+    if (rows > 0 && channels > 0 && !x) return fail(DA_ERR_INVALID_ARG, "null x");
+    *sh = NormShape{rows, samples, offsets, samples ? rows / samples : 0, (int)channels, (int)groups, (int)(channels / groups), eps,
+                    act, param_dtype, w, b};
+    return DA_OK;
+}
+
+int workspace_error() {
+    return fail(DA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than reported");
+}
+
+}  // namespace
+
+extern "C" int da_group_norm_sizes(int dtype, int64_t rows, int64_t samples, int ragged, int64_t channels, int64_t groups, int train,
+                                   size_t* stats_floats, size_t* forward_bytes, size_t* backward_bytes)
+{
+    if (!stats_floats || !forward_bytes || !backward_bytes) return fail(DA_ERR_INVALID_ARG, "null output");
+    const int st = norm_check(dtype, rows, samples, channels, groups);
+    if (st != DA_OK) return st;
+    *stats_floats = *forward_bytes = *backward_bytes = 0;
+    if (channels == 0) return DA_OK;
+    const NormPlan p = norm_plan(dtype, rows, samples, ragged != 0, channels, groups, train != 0);
+    *stats_floats = train ? p.stats : 0;
+    *forward_bytes = p.forward;
+    *backward_bytes = p.backward;
+    return DA_OK;
+}
+
+extern "C" int da_group_norm(int dtype, int64_t rows, int64_t samples, const int32_t* offsets, int64_t channels, int64_t groups,
+                             const void* x, int64_t ldx, const void* w, const void* b, int param_dtype, float eps, int act, void* y,
+                             float* stats, void* workspace, size_t workspace_bytes, void* stream)
+{
+    NormShape sh;
+    const int st = norm_shape(dtype, rows, samples, offsets, channels, groups, x, ldx, w, b, param_dtype, eps, act, &sh);
+    if (st != DA_OK) return st;
+    if (rows == 0 || channels == 0) return DA_OK;
+    if (!y) return fail(DA_ERR_INVALID_ARG, "null y");
+    const NormPlan p = norm_plan(dtype, rows, samples, offsets != nullptr, channels, groups, stats != nullptr);
+    if (p.forward && (!workspace || workspace_bytes < p.forward || !aligned16(workspace))) return workspace_error();
+    if (p.split && p.chunks > INT32_MAX) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    char* ws = static_cast<char*>(workspace);
+    float* kept = stats ? stats : p.stats ? reinterpret_cast<float*>(ws + p.forward - round16(p.stats * sizeof(float))) : nullptr;
+    with_type_and_width(dtype, p.V, [&](auto t, auto v) {
+        using T = decltype(t);
+        norm_forward<T, decltype(v)::value>(p, sh, static_cast<const T*>(x), ldx, static_cast<T*>(y), kept, ws, (hipStream_t)stream);
+    });
+    return launched("da_group_norm launch");
+}
+
+extern "C" int da_group_norm_backward(int dtype, int64_t rows, int64_t samples, const int32_t* offsets, int64_t channels,
+                                      int64_t groups, const void* x, int64_t ldx, const void* dy, int64_t ldy, const void* w,
+                                      const void* b, int param_dtype, float eps, int act, const float* stats, void* dx, void* dw,
+                                      void* db, void* workspace, size_t workspace_bytes, void* stream)
+{
+    NormShape sh;
+    const int st = norm_shape(dtype, rows, samples, offsets, channels, groups, x, ldx, w, b, param_dtype, eps, act, &sh);
+    if (st != DA_OK) return st;
+    if (channels == 0) return DA_OK;
+    if (ldy < channels) return fail(DA_ERR_INVALID_ARG, "leading dimension smaller than the extent it strides over");
+    if (rows > 0 && (!dy || !dx)) return fail(DA_ERR_INVALID_ARG, "null dy or dx");
+    const NormPlan p = rows > 0 ? norm_plan(dtype, rows, samples, offsets != nullptr, channels, groups, true) : NormPlan{1};
+    if (p.stats && !stats) return fail(DA_ERR_INVALID_ARG, "null stats");
+    if (p.backward && (!workspace || workspace_bytes < p.backward || !aligned16(workspace))) return workspace_error();
+    if (p.split && p.chunks > INT32_MAX) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    with_type_and_width(dtype, p.V, [&](auto t, auto v) {
+        using T = decltype(t);
+        norm_backward<T, decltype(v)::value>(p, sh, static_cast<const T*>(x), ldx, static_cast<const T*>(dy), ldy, stats,
+                                             static_cast<T*>(dx), dw, db, static_cast<char*>(workspace), (hipStream_t)stream);
+    });
+    return launched("da_group_norm_backward launch");
+}
+
+// ------------------------------------------------------------------------------------------
+// distillation
+// ------------------------------------------------------------------------------------------
+namespace {
+
+constexpr int64_t kDistillMaxClasses = INT32_MAX - (1 << 16);
+constexpr size_t kNarrowEntriesBytes = 32 << 10;
+
+struct DistillPlan {
+    bool narrow;
+    int P, E;
+    int64_t pieces, piece;
+};
+
+// Rows of up to 2048 classes fit a wave's registers.  Wider ones are cut into pieces where there are too few for the chip.
+DistillPlan distill_plan(int dtype, int64_t rows, int64_t classes, int64_t best) {
+    DistillPlan p{};
+    const int V = dtype == DA_F32 ? 4 : 8;
+    const int64_t vecs = ceil_div(classes, V);
+    int64_t slots = INT64_MAX;
+    for (int E : {1, 2, 3, 4, 8}) {
+        if (E * V > 32) continue;
+        const int P = pow2_at_least(ceil_div(vecs, E));
+        if (P > 64 || (int64_t)P * E >= slots) continue;
+        slots = (int64_t)P * E;
+        p.P = P;
+        p.E = E;
+    }
+    p.narrow = slots != INT64_MAX && (size_t)(kDistillBlock / p.P) * best * sizeof(Entry) <= kNarrowEntriesBytes;
+    const int64_t want = 8 * compute_units();
+    p.pieces = std::clamp<int64_t>(ceil_div(want, std::max<int64_t>(rows, 1)), 1, std::max<int64_t>(1, classes / 8192));
+    const int64_t turn = 4 * kWideBlock * V;
+    p.piece = ceil_div(ceil_div(classes, p.pieces), turn) * turn;
+    p.pieces = std::max<int64_t>(1, ceil_div(classes, p.piece));
+    return p;
+}
+
+int distill_check(int dtype, int64_t rows, int64_t classes, int64_t best, const void* z, int64_t ldz, const void* index,
+                  const void* top, int top_dtype, float temperature) {
+    if (!known_dtype(dtype) || !known_dtype(top_dtype)) return fail(DA_ERR_UNSUPPORTED, "dtype is neither DA_F32 nor DA_BF16");
+    if (rows < 0 || classes < 0 || best < 0) return fail(DA_ERR_INVALID_ARG, "negative size");
+    if (rows > INT32_MAX || classes > kDistillMaxClasses) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    if (best > kDistillMaxBest) return fail(DA_ERR_UNSUPPORTED, "more than 1024 entries to a row");
+    if (!(temperature > 0.f) || !(1.f / temperature > 0.f)) return fail(DA_ERR_INVALID_ARG, "temperature is not positive and finite");
+    if (ldz < classes) return fail(DA_ERR_INVALID_ARG, "leading dimension smaller than the extent it strides over");
+    if (rows > 0 && ((classes > 0 && !z) || (best > 0 && (!index || !top)))) return fail(DA_ERR_INVALID_ARG, "null z, index or top");
+    return DA_OK;
+}
+
+template <class T, int V, bool BWD>
+void launch_narrow(const DistillPlan& p, int64_t rows, const Teacher& te, const T* z, int64_t ldz, float temperature, float* loss,
+                   float* stats, const float* dloss, int64_t dloss_stride, T* dz, hipStream_t s) {
+    const int64_t per_block = kDistillBlock / p.P;
+    const int64_t grid = std::min<int64_t>(ceil_div(rows, per_block), 1 << 20);
+    const size_t lds = BWD ? (size_t)per_block * te.best * sizeof(Entry) : 0;
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kDistillBlock), lds, s, (long)rows, p.P, te, z, (long)ldz, temperature,
+                           loss, stats, dloss, (long)dloss_stride, dz);
+    };
+    if (p.E == 1) return go(distill_narrow_kernel<T, V, 1, BWD>);
+    if (p.E == 2) return go(distill_narrow_kernel<T, V, 2, BWD>);
+    if (p.E == 3) return go(distill_narrow_kernel<T, V, 3, BWD>);
+    if (p.E == 4) return go(distill_narrow_kernel<T, V, 4, BWD>);
+    if constexpr (V == 4) return go(distill_narrow_kernel<T, V, 8, BWD>);
+}
+
+template <class T, int V>
+void distill_forward(const DistillPlan& p, int64_t rows, const Teacher& te, const T* z, int64_t ldz, float temperature, float* loss,
+                     float* stats, float2* part, hipStream_t s) {
+    if (p.narrow)
+        return launch_narrow<T, V, false>(p, rows, te, z, ldz, temperature, loss, stats, nullptr, 0, nullptr, s);
+    hipLaunchKernelGGL((distill_wide_kernel<T, V>), dim3((unsigned)p.pieces, (unsigned)std::min<int64_t>(rows, 65535)),
+                       dim3(kWideBlock), 0, s, (long)rows, (long)p.piece, te, z, (long)ldz, temperature, loss, stats, part);
+    if (p.pieces > 1)
+        hipLaunchKernelGGL((distill_join_kernel<T>), dim3((unsigned)std::min<int64_t>(rows, 65535)), dim3(256), 0, s, (long)rows,
+                           (int)p.pieces, te, z, (long)ldz, temperature, loss, stats, part);
+}
+
+Teacher teacher(int64_t classes, int64_t best, const void* index, int index64, const void* top, int top_dtype, float temperature) {
+    return Teacher{classes, best, index, top, index64, top_dtype, 1.f / temperature};
+}
+
+}  // namespace
+
+extern "C" int da_distill_workspace(int64_t rows, int64_t classes, size_t* bytes)
+{
+    if (!bytes) return fail(DA_ERR_INVALID_ARG, "null bytes");
+    if (rows < 0 || classes < 0) return fail(DA_ERR_INVALID_ARG, "negative size");
+    if (rows > INT32_MAX || classes > kDistillMaxClasses) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    const int64_t pieces = std::max(distill_plan(DA_F32, rows, classes, 0).pieces, distill_plan(DA_BF16, rows, classes, 0).pieces);
+    *bytes = pieces > 1 ? (size_t)(rows * pieces) * sizeof(float2) : 0;
+    return DA_OK;
+}
+
+extern "C" int da_distill(int dtype, int64_t rows, int64_t classes, int64_t best, const void* z, int64_t ldz, const void* index,
+                          int index64, const void* top, int top_dtype, float temperature, float* loss, float* stats,
+                          void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int st = distill_check(dtype, rows, classes, best, z, ldz, index, top, top_dtype, temperature);
+    if (st != DA_OK) return st;
+    if (rows == 0) return DA_OK;
+    if (!loss) return fail(DA_ERR_INVALID_ARG, "null loss");
+    const DistillPlan p = distill_plan(dtype, rows, classes, best);
+    const size_t need = !p.narrow && p.pieces > 1 ? (size_t)(rows * p.pieces) * sizeof(float2) : 0;
+    if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return workspace_error();
+    const Teacher te = teacher(classes, best, index, index64, top, top_dtype, temperature);
+    float2* part = static_cast<float2*>(workspace);
+    if (dtype == DA_F32)
+        distill_forward<float, 4>(p, rows, te, static_cast<const float*>(z), ldz, temperature, loss, stats, part, (hipStream_t)stream);
+    else
+        distill_forward<bf16, 8>(p, rows, te, static_cast<const bf16*>(z), ldz, temperature, loss, stats, part, (hipStream_t)stream);
+    return launched("da_distill launch");
+}
+
+namespace {
+
+template <class T, int V>
+void distill_grad(const DistillPlan& p, int64_t rows, const Teacher& te, const void* z, int64_t ldz, float temperature,
+                  const float* stats, const float* dloss, int64_t dloss_stride, void* dz, hipStream_t s) {
+    const T* zt = static_cast<const T*>(z);
+    T* dt = static_cast<T*>(dz);
+    if (p.narrow)
+        return launch_narrow<T, V, true>(p, rows, te, zt, ldz, temperature, nullptr, const_cast<float*>(stats), dloss, dloss_stride,
+                                         dt, s);
+    hipLaunchKernelGGL((distill_wide_grad_kernel<T, V>), dim3((unsigned)p.pieces, (unsigned)std::min<int64_t>(rows, 65535)),
+                       dim3(kWideBlock), 0, s, (long)rows, (long)p.piece, te, zt, (long)ldz, temperature, stats, dloss,
+                       (long)dloss_stride, dt);
+}
+
+}  // namespace
+
+extern "C" int da_distill_backward(int dtype, int64_t rows, int64_t classes, int64_t best, const void* z, int64_t ldz,
+                                   const void* index, int index64, const void* top, int top_dtype, float temperature,
+                                   const float* stats, const float* dloss, int64_t dloss_stride, void* dz, void* stream)
+{
+    const int st = distill_check(dtype, rows, classes, best, z, ldz, index, top, top_dtype, temperature);
+    if (st != DA_OK) return st;
+    if (dloss_stride < 0) return fail(DA_ERR_INVALID_ARG, "negative stride");
+    if (rows == 0 || classes == 0) return DA_OK;
+    if (!stats || !dloss || !dz) return fail(DA_ERR_INVALID_ARG, "null stats, dloss or dz");
+    const DistillPlan p = distill_plan(dtype, rows, classes, best);
+    const Teacher te = teacher(classes, best, index, index64, top, top_dtype, temperature);
+    if (dtype == DA_F32) distill_grad<float, 4>(p, rows, te, z, ldz, temperature, stats, dloss, dloss_stride, dz, (hipStream_t)stream);
+    else distill_grad<bf16, 8>(p, rows, te, z, ldz, temperature, stats, dloss, dloss_stride, dz, (hipStream_t)stream);
+    return launched("da_distill_backward launch");
+}

@@ -2,6 +2,7 @@
 // algorithm id to a kernel instantiation, the feature-extraction helper and the selector.
 // The C ABI is declared and documented in include/da_spmm.h.
 #include "da_spmm.h"
+#include "da_internal.h"
 #include "da_spmm_kernels.hip"
 #include "da_transpose_kernels.hip"
 #include "da_dense_kernels.hip"
@@ -47,6 +48,16 @@ int cu_count() {
     }
     return c;
 }
+
+}  // namespace
+
+namespace daspmm {
+int set_error(int code, const char* text) noexcept { return fail(code, "%s", text); }
+int set_hip_error(hipError_t e, const char* where) noexcept { return hip_fail(e, where); }
+int compute_units() noexcept { return cu_count(); }
+}  // namespace daspmm
+
+namespace {
 
 int pow2_ceil(long x) {
     int p = 1;

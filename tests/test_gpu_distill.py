@@ -1,0 +1,294 @@
+"""distill_loss (a teacher's best classes) against its formula in 64 bits, forward and backward.
+
+Tolerances, with e = 2^-24.  Logits relative to the row's largest, over T: a = (z - max) / T is off by 2 e |a|, exp(a) by
+(2 |a| + 4) e relative; the largest |a| that matters is where exp(a) still adds something, so sums and their logarithms are
+off by R = e (K + 2 A) with A = max|a| up to 100 and K = 64 for the additions.  The loss T^2 sum p (log p - log q) is off by
+T^2 (sum p |log p - log q| (R_t + R_z) + R_t + R_z + 2 e sum p (|t| + |a|)); the gradient g T (q - p) by
+|g| T (q (R_z + 2 e |a|) + p (R_t + 2 e |t|) + 4 e (q + p)).  bfloat16 gradients are rounded once more (2^-8)."""
+import math
+
+import pytest
+import torch
+
+from paper_2202_08556_amd import layers
+
+pytestmark = pytest.mark.gpu
+E, K = 2.0 ** -24, 64.0
+
+
+def formula(z, index, top, T, dloss):
+    """(loss, its tolerance, dz, its tolerance) in 64 bits, on the CPU."""
+    z, top, g = z.detach().double().cpu() / T, top.detach().double().cpu() / T, dloss.double().cpu()
+    index = index.long().cpu()
+    if index.shape[1] == 0:                                  # no entries: one that is missing
+        index, top = torch.full((z.shape[0], 1), -1), torch.zeros((z.shape[0], 1), dtype=torch.float64)
+    classes = z.shape[1]
+    valid = (index >= 0) & (index < classes) & (top > -math.inf)
+    some = valid.any(1)
+    t = top.masked_fill(~valid, -math.inf).masked_fill(~some[:, None], 0.0)
+    t = t - t.max(1, keepdim=True).values
+    logp = t - t.logsumexp(1, keepdim=True)
+    p = logp.exp() * valid
+    a = z - z.max(1, keepdim=True).values
+    logq = a - a.logsumexp(1, keepdim=True)
+    q = logq.exp()
+    at = index.clamp(0, classes - 1)
+    use = p > 0
+    gap = torch.where(use, logp - logq.gather(1, at), 0.0)
+    loss = T * T * (p * gap).sum(1) * some
+    rz = E * (K + 2 * a.abs().masked_fill(a == -math.inf, 0).max(1).values.clamp(max=100))
+    rt = E * (K + 2 * t.abs().masked_fill(t == -math.inf, 0).max(1).values.clamp(max=100))
+    size = torch.where(use, t.abs() + a.gather(1, at).abs(), 0.0)
+    tol = T * T * ((p * gap.abs()).sum(1) * (rt + rz) + rt + rz + 2 * E * (p * size).sum(1)) + 4 * E * loss.abs()
+    dense = torch.zeros_like(q).scatter_add_(1, at, p)
+    dense_t = torch.zeros_like(q).scatter_add_(1, at, torch.where(use, p * t.abs(), 0.0))
+    scale = (g * T)[:, None]
+    dz = torch.where(some[:, None], scale * (q - dense), 0.0)
+    abs_a = a.abs().masked_fill(a == -math.inf, 0)
+    tol_dz = scale.abs() * (q * (rz[:, None] + 2 * E * abs_a) + dense * rt[:, None] + 2 * E * dense_t + 4 * E * (q + dense))
+    return loss, tol, dz, tol_dz + E * dz.abs() + 2.0 ** -126
+
+
+def run(z, index, top, T=1.0, dloss=None):
+    z = z.detach().requires_grad_(True)
+    if dloss is None:
+        dloss = torch.rand(z.shape[0], device="cuda") + 0.1
+    loss = layers.distill_loss(z, index, top, T, "none")
+    assert loss.shape == z.shape[:1] and loss.dtype == torch.float32
+    dz, = torch.autograd.grad(loss, z, dloss)
+    assert dz.shape == z.shape and dz.dtype == z.dtype
+    torch.cuda.synchronize()
+    want, tol, want_dz, tol_dz = formula(z, index, top, T, dloss)
+    err = (loss.detach().double().cpu() - want).abs()
+    assert ((err <= tol) | (loss.cpu() == want)).all(), f"loss: {float((err / tol).max()):.3g} times the tolerance"
+    if z.dtype == torch.bfloat16:
+        tol_dz = tol_dz + 2.0 ** -8 * want_dz.abs()
+    err = (dz.double().cpu() - want_dz).abs()
+    assert (err <= tol_dz).all(), f"dz: {float((err / tol_dz).max()):.3g} times the tolerance"
+    with torch.no_grad():
+        assert torch.equal(layers.distill_loss(z, index, top, T, "none"), loss)
+    return loss.detach(), dz
+
+
+def inputs(R, V, best, dtype, seed=0, missing=0.2, empty=0.1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = (2 * torch.randn(R, V, generator=g, device="cuda")).to(dtype)
+    index = torch.rand(R, V, generator=g, device="cuda").topk(best, 1).indices if V <= 5000 else \
+        (torch.randint(0, V, (R, 1), generator=g, device="cuda") + torch.arange(best, device="cuda") * (V // best)) % V
+    gone = (torch.rand(R, best, generator=g, device="cuda") < missing) | (torch.rand(R, 1, generator=g, device="cuda") < empty)
+    top = (2 * torch.randn(R, best, generator=g, device="cuda") + 3).to(dtype)
+    return z, torch.where(gone, -1, index).to(torch.int32), top
+
+
+# rows x classes x best: rows in a few lanes' registers, in a wave's, up to the widest of those, walked by a block, cut into
+# pieces; classes that are no multiple of an access
+SIZES = [(1, 1, 1), (3, 2, 1), (61, 41, 5), (700, 41, 8), (5, 4, 4), (100, 7, 3), (40, 100, 100), (9, 255, 17), (9, 256, 40),
+         (33, 1023, 9), (4, 2047, 64), (4, 2048, 64), (3, 2049, 64), (5, 5000, 1000), (2, 4097, 1024), (1, 8193, 5), (1, 131071, 100),
+         (16, 65536, 64), (300, 3000, 3), (1, 50000, 0), (20, 30, 0), (2, 300, 300)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("R,V,best", SIZES)
+def test_sizes(R, V, best, dtype):
+    print(f"distill {R}x{V} best {best} {dtype}", flush=True)
+    z, index, top = inputs(R, V, max(best, 1), dtype, seed=R + V)
+    index, top = index[:, :best], top[:, :best]
+    run(z, index, top, 2.0)
+    run(z, index.long(), top.float(), 0.7)                   # 64-bit classes, float32 teacher
+
+
+@pytest.mark.parametrize("R,V", [(50, 41), (6, 1000), (4, 3001), (1, 90001)])
+def test_rows_at_a_distance_and_odd_addresses(R, V):
+    z, index, top = inputs(R, V, 5, torch.float32, seed=1)
+    want = run(z, index, top, 1.5, torch.ones(R, device="cuda"))
+    wide = torch.full((R, V + 13), float("nan"), device="cuda")
+    wide[:, 3:3 + V] = z
+    for other in (wide[:, 3:3 + V], z.t().contiguous().t()):
+        got = run(other, index, top, 1.5, torch.ones(R, device="cuda"))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    one = torch.ones(1, device="cuda").expand(R)             # one gradient for all rows
+    assert torch.equal(run(z, index, top, 1.5, one)[1], want[1])
+    assert torch.equal(run(z, index, top, 1.5, torch.ones(R, 2, device="cuda")[:, 1])[1], want[1])
+
+
+@pytest.mark.parametrize("V", [41, 700, 3001, 70000])
+def test_masks_and_lowest_values(V):
+    """Classes of the student that are masked by -inf or by the type's lowest value, teachers' entries likewise, entries
+    out of range, rows whose entries are all missing or all -inf."""
+    z, index, top = inputs(12, V, 9, torch.float32, seed=2, missing=0.0, empty=0.0)
+    lowest = torch.finfo(torch.float32).min
+    masked = torch.zeros(12, V, dtype=torch.bool, device="cuda")
+    masked.scatter_(1, index.long(), True)
+    z[0:2] = z[0:2].masked_fill(~masked[0:2], -math.inf)
+    z[2:4] = z[2:4].masked_fill(~masked[2:4], lowest)
+    top[4, 1:] = -math.inf
+    top[5, 2:] = lowest
+    index[6] = -1
+    top[7] = -math.inf
+    index[8, 3:] = V
+    index[9, :5] = 2 ** 31 - 1
+    index[10, 1:] = -2 ** 31
+    loss, dz = run(z, index, top, 1.3)
+    for r in (6, 7):
+        assert loss[r] == 0 and not dz[r].any()
+    # a missing entry's logit is not looked at
+    index[0, 0] = -1
+    a = run(z, index, top, 1.3)
+    top[0, 0] = float("nan")
+    b = layers.distill_loss(z, index, top, 1.3, "none")
+    assert torch.equal(a[0], b)
+
+
+@pytest.mark.parametrize("V", [41, 3001, 90001])
+def test_student_without_a_teachers_class_has_an_infinite_loss(V):
+    z, index, top = inputs(3, V, 4, torch.float32, seed=3, missing=0.0, empty=0.0)
+    z[1, index[1, 2].item()] = -math.inf
+    z.requires_grad_(True)
+    loss = layers.distill_loss(z, index, top, 1.0, "none")
+    dz, = torch.autograd.grad(loss, z, torch.ones_like(loss))
+    assert loss[1] == math.inf and torch.isfinite(loss[[0, 2]]).all() and torch.isfinite(dz).all()
+
+
+@pytest.mark.parametrize("V", [41, 3001, 90001])
+def test_bad_numbers_stay_in_their_row(V):
+    z, index, top = inputs(5, V, 4, torch.float32, seed=4, missing=0.0, empty=0.0)
+    want = run(z, index, top)
+    for bad in (float("nan"), math.inf):
+        other = z.detach().clone()
+        other[2, V // 2] = bad
+        other.requires_grad_(True)
+        loss = layers.distill_loss(other, index, top, 1.0, "none")
+        dz, = torch.autograd.grad(loss, other, torch.ones_like(loss))
+        assert torch.isnan(loss[2]) and torch.isnan(dz[2]).all()
+        keep = [0, 1, 3, 4]
+        assert torch.equal(loss[keep], want[0][keep]) and torch.isfinite(dz[keep]).all()
+
+
+@pytest.mark.parametrize("V", [41, 700, 3001, 90001])
+def test_entries_of_one_class_add(V):
+    z, index, top = inputs(6, V, 12, torch.float32, seed=5, missing=0.1, empty=0.0)
+    index[1] = index[1, 0]
+    index[2, 5:9] = 3
+    index[3, ::2] = V - 1
+    run(z, index, top, 0.9)
+
+
+@pytest.mark.parametrize("V", [41, 3001])
+def test_large_logits(V):
+    """Differences of the logits count, not their size: the same loss and gradient with 30 000 added to every logit."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    z = torch.randint(-40, 41, (7, V), generator=g, device="cuda").float() / 8
+    _, index, top = inputs(7, V, 5, torch.float32, seed=6)
+    a, b = run(z, index, top), run(z + 30000, index, top + 30000 - (top + 30000 - 30000 - top))
+    assert torch.allclose(a[0], b[0], rtol=1e-3)
+    run(z * 1e30, index, top)
+
+
+def test_reductions_and_shapes():
+    z, index, top = inputs(12, 41, 5, torch.float32, seed=7)
+    rows = layers.distill_loss(z, index, top, 2.0, "none")
+    z3, i3, t3 = z.view(3, 4, 41), index.view(3, 4, 5), top.view(3, 4, 5)
+    assert torch.equal(layers.distill_loss(z3, i3, t3, 2.0, "none"), rows.view(3, 4))
+    assert torch.equal(layers.distill_loss(z[0], index[0], top[0], 2.0, "none"), rows[0])
+    for reduction, scale in (("sum", 1.0), ("mean", 1 / 12)):
+        leaf = z.detach().requires_grad_(True)
+        loss = layers.distill_loss(leaf, index, top, 2.0, reduction)
+        assert abs(float(loss) - float(rows.double().sum()) * scale) <= 1e-5 * float(rows.sum()) * scale
+        dz, = torch.autograd.grad(loss, leaf)
+        want, = torch.autograd.grad(layers.distill_loss(leaf, index, top, 2.0, "none"), leaf, torch.full((12,), scale, device="cuda"))
+        assert torch.allclose(dz, want, rtol=1e-6, atol=0)
+    for shape in ((0, 41), (0, 3, 41)):
+        leaf = torch.empty(shape, device="cuda", requires_grad=True)
+        e = torch.empty((*shape[:-1], 5), dtype=torch.int32, device="cuda")
+        loss = layers.distill_loss(leaf, e, e.float(), reduction="sum")
+        loss.backward()
+        assert loss == 0 and leaf.grad.shape == leaf.shape
+
+
+@pytest.mark.parametrize("V", [41, 3001])
+def test_gradient_against_differences(V):
+    """Slope of sum(loss) along a direction by central differences of step h: truncation under h^2 (third derivatives of a
+    log-sum-exp are at most 1 in directions of size 1), rounding K e |loss| / h."""
+    z, index, top = inputs(8, V, 5, torch.float32, seed=8)
+    _, dz = run(z, index, top, 1.5, torch.ones(8, device="cuda"))
+    v = torch.randn(z.shape, generator=torch.Generator(device="cuda").manual_seed(9), device="cuda")
+    v = v / v.abs().max()
+    h = 2.0 ** -5
+    up, down = (layers.distill_loss(z + s * h * v, index, top, 1.5, "none").double() for s in (1, -1))
+    slope, want = ((up - down) / (2 * h)).sum(), (dz.double() * v.double()).sum()
+    assert abs(float(slope - want)) <= 8 * (1.5 * h * h + 4 * K * E * float(up.max()) / h)
+
+
+def test_other_stream_and_graph():
+    cases = [inputs(200, 41, 5, torch.float32, seed=10), inputs(3, 70001, 9, torch.float32, seed=10)]
+    cases = [(z.requires_grad_(True), i, t) for z, i, t in cases]
+
+    def once():
+        out = []
+        for z, index, top in cases:
+            loss = layers.distill_loss(z, index, top, 2.0, "none")
+            out += [loss.detach(), torch.autograd.grad(loss, z, torch.ones_like(loss))[0]]
+        return out
+
+    want = once()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = once()
+    s.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = once()
+    for k in range(4):
+        with torch.no_grad():
+            for z, _, _ in cases:
+                z.mul_(-0.7).add_(0.2 * k)
+        want = once()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), k
+
+
+def test_more_than_2_31_logits():
+    rows, V = 2 ** 15 + 3, 65540
+    z = torch.zeros((rows, V), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(11)
+    z[-4:] = torch.randn(4, V, generator=g, device="cuda").to(torch.bfloat16)
+    index = torch.randint(0, V, (rows, 3), generator=g, device="cuda")
+    index[-1, 0] = V - 1
+    top = torch.randn(rows, 3, generator=g, device="cuda")
+    z.requires_grad_(True)
+    loss = layers.distill_loss(z, index, top, 1.0, "none")
+    dz, = torch.autograd.grad(loss, z, torch.ones_like(loss))
+    # many rows take a block each, few are cut into pieces: sums in another order
+    want, tol, want_dz, tol_dz = formula(z[-4:], index[-4:], top[-4:], 1.0, torch.ones(4))
+    assert ((loss[-4:].detach().double().cpu() - want).abs() <= tol).all()
+    assert ((dz[-4:].double().cpu() - want_dz).abs() <= tol_dz + 2.0 ** -8 * want_dz.abs()).all()
+
+
+def test_refusals():
+    z, index, top = inputs(6, 41, 5, torch.float32)
+    f = layers.distill_loss
+    cases = [
+        (ValueError, lambda: f(z, index, top, 0.0)),
+        (ValueError, lambda: f(z, index, top, float("nan"))),
+        (ValueError, lambda: f(z, index, top, float("inf"))),
+        (ValueError, lambda: f(z, index, top, 1.0, "average")),
+        (ValueError, lambda: f(z, index[:5], top[:5])),
+        (ValueError, lambda: f(z, index, top[:, :4])),
+        (ValueError, lambda: f(z, index.view(-1), top.view(-1))),
+        (ValueError, lambda: f(z, index.cpu(), top)),
+        (ValueError, lambda: f(z.cpu(), index.cpu(), top.cpu())),
+        (TypeError, lambda: f(z, index.short(), top)),
+        (TypeError, lambda: f(z, index, top.half())),
+        (TypeError, lambda: f(z.double(), index, top)),
+        (RuntimeError, lambda: f(z, index[:, :1].expand(6, 1025), top[:, :1].expand(6, 1025))),
+    ]
+    for error, call in cases:
+        with pytest.raises(error):
+            call()
+    z.requires_grad_(True)
+    g, = torch.autograd.grad(f(z, index, top), z, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiated again"):
+        g.sum().backward()

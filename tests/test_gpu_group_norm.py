@@ -1,0 +1,366 @@
+"""group_norm (group norm with an activation, channels last) against its formula in 64 bits, forward and backward, on
+samples of every size and its edge cases.
+
+Tolerances, with e = 2^-24 (half a unit in the last place of 1):
+  a sum of n numbers in float32 takes at most a few hundred additions in a row before they are joined pairwise; their
+  roundings are independent, so its error stays under K e sum|terms| / n per term with K = 64 (three times the square
+  root of 500).  So the mean is off by K e max|x|, r by 8 e (and K e of the variance: half of it) relative, and
+    z is off by   dz_ = e (K |r w| max|x| + (K + 8) |xh w| + 2 |b| + 2 |z|),
+    y by 1.13 dz_ + 8 e (|y| + |z|)      (no activation is steeper than 1.13; exp's argument is rounded: |z| e)
+  dz = dy act'(z) by |dy| (dz_ + 8 e (1 + |z|))  (no second derivative exceeds 1)
+  e_ = dz w likewise; dx = r (e_ - mean e_ - xh mean(e_ xh)) by  r (the error of e_ + K e (max|e_| + |xh| max|e_ xh|)) +
+  (K + 8) e |dx| and what the error of xh adds, and dw, db by the sum of the terms' errors and 16 e sum|terms|.
+bfloat16 results are rounded once more: 2^-8 of their size (half a unit is at most that)."""
+import math
+
+import pytest
+import torch
+
+from paper_2202_08556_amd import layers
+
+pytestmark = pytest.mark.gpu
+E, K = 2.0 ** -24, 64.0
+
+
+def act64(name, z):
+    F = torch.nn.functional
+    return {None: lambda t: t, "relu": torch.relu, "silu": F.silu, "gelu": F.gelu, "sigmoid": torch.sigmoid}[name](z)
+
+
+def slope64(name, z):
+    z = z.detach().requires_grad_(True)
+    return torch.autograd.grad(act64(name, z).sum(), z)[0]
+
+
+def lengths_of(x, offsets):
+    """(flat rows x C, list of (first, last) rows of the samples)"""
+    flat = x.reshape(-1, x.shape[-1])
+    if offsets is not None:
+        o = offsets.tolist()
+        return flat, [(a, b) for a, b in zip(o, o[1:])]
+    n = x.shape[-2]
+    return flat, [(i, i + n) for i in range(0, flat.shape[0], n)]
+
+
+def check(x, groups, w, b, eps, act, offsets, dy, tensors):
+    """Compares y, dx, dw, db in `tensors` with the formula in 64 bits."""
+    y, dx, dw, db = tensors
+    flat, samples = lengths_of(x.detach().double().cpu(), None if offsets is None else offsets.cpu())
+    C = flat.shape[1]
+    w64 = torch.ones(C, dtype=torch.float64) if w is None else w.detach().double().cpu()
+    b64 = torch.zeros(C, dtype=torch.float64) if b is None else b.detach().double().cpu()
+    d64 = dy.double().cpu().reshape(-1, C)
+    half = 2.0 ** -8 if x.dtype == torch.bfloat16 else 0.0
+    got_y, got_dx = y.detach().double().cpu().reshape(-1, C), dx.double().cpu().reshape(-1, C)
+    want_w, want_b = torch.zeros(C, dtype=torch.float64), torch.zeros(C, dtype=torch.float64)
+    tol_w, tol_b = torch.zeros_like(want_w), torch.zeros_like(want_b)
+    for r0, r1 in samples:
+        if r0 == r1:
+            continue
+        v = flat[r0:r1].unflatten(1, (groups, -1))
+        mean = v.mean(dim=(0, 2), keepdim=True)
+        r = 1 / ((v - mean).pow(2).mean(dim=(0, 2), keepdim=True) + eps).sqrt()
+        wv, bv, dv = w64.view(1, groups, -1), b64.view(1, groups, -1), d64[r0:r1].unflatten(1, (groups, -1))
+        xh = (v - mean) * r
+        z = xh * wv + bv
+        big = v.abs().amax(dim=(0, 2), keepdim=True)
+        exh = E * (K * r * big + (K + 8) * xh.abs())
+        ez = wv.abs() * exh + E * (2 * bv.abs() + 2 * z.abs())
+        want = act64(act, z)
+        tol = 1.13 * ez + 8 * E * (want.abs() + z.abs()) + half * want.abs()
+        err = (got_y[r0:r1].unflatten(1, (groups, -1)) - want).abs()
+        assert (err <= tol).all(), f"y: {float((err / tol).max()):.3g} times the tolerance"
+        dz = dv * slope64(act, z)
+        edz = dv.abs() * (ez + 8 * E * (1 + z.abs()))
+        e_, ee = dz * wv, edz * wv.abs() + E * (dz * wv).abs()
+        m1, m2 = e_.mean(dim=(0, 2), keepdim=True), (e_ * xh).mean(dim=(0, 2), keepdim=True)
+        want = r * (e_ - m1 - xh * m2)
+        top, topx = e_.abs().amax(dim=(0, 2), keepdim=True), (e_ * xh).abs().amax(dim=(0, 2), keepdim=True)
+        mean_err = ee.mean(dim=(0, 2), keepdim=True)
+        mean_err_x = (ee * xh.abs() + e_.abs() * exh).mean(dim=(0, 2), keepdim=True)
+        tol = r * (ee + mean_err + K * E * top + xh.abs() * (mean_err_x + K * E * topx) + exh * m2.abs())
+        tol = tol + r * E * 4 * (e_.abs() + m1.abs() + (xh * m2).abs()) + (K + 8) * E * want.abs() + half * want.abs()
+        err = (got_dx[r0:r1].unflatten(1, (groups, -1)) - want).abs()
+        assert (err <= tol).all(), f"dx: {float((err / tol).max()):.3g} times the tolerance"
+        want_w += (dz * xh).sum(0).flatten()
+        want_b += dz.sum(0).flatten()
+        tol_w += (edz * xh.abs() + dz.abs() * exh + 16 * E * (dz * xh).abs()).sum(0).flatten()
+        tol_b += (edz + 16 * E * dz.abs()).sum(0).flatten()
+    for got, want, tol, name in ((dw, want_w, tol_w, "dw"), (db, want_b, tol_b, "db")):
+        if got is None:
+            continue
+        tol = tol + (2.0 ** -8 if got.dtype == torch.bfloat16 else E) * want.abs()
+        err = (got.double().cpu() - want).abs()
+        assert (err <= tol).all(), f"{name}: {float((err / tol).max()):.3g} times the tolerance"
+
+
+def run(x, groups, w, b, act, offsets=None, eps=1e-5, dy=None):
+    leaves = [t for t in (x, w, b) if t is not None]
+    for t in leaves:
+        t.requires_grad_(True)
+    y = layers.group_norm(x, groups, w, b, eps, act, offsets)
+    assert y.shape == x.shape and y.dtype == x.dtype and y.is_contiguous()
+    g = list(torch.autograd.grad(y, leaves, dy))
+    torch.cuda.synchronize()
+    dx = g.pop(0)
+    dw = g.pop(0) if w is not None else None
+    db = g.pop(0) if b is not None else None
+    check(x, groups, w, b, eps, act, offsets, dy, (y, dx, dw, db))
+    with torch.no_grad():                                    # without a gradient: the same y
+        assert torch.equal(layers.group_norm(x, groups, w, b, eps, act, offsets), y)
+    return y, dx, dw, db
+
+
+def inputs(shape, dtype, seed=0, shift=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    C = shape[-1]
+    x = torch.randn(*shape, generator=g, device="cuda") * 1.5 + shift * torch.randn(C, generator=g, device="cuda")
+    w = 1 + 0.2 * torch.randn(C, generator=g, device="cuda")
+    b = 0.2 * torch.randn(C, generator=g, device="cuda")
+    dy = torch.randn(*shape, generator=g, device="cuda")
+    return x.to(dtype), w, b, dy.to(dtype)
+
+
+# samples x rows x channels, groups: one row (a few lanes' registers, several accesses a lane, groups beyond that), a few
+# rows (one wave), some (a block), many (cut into chunks); widths of a group that are no multiple of an access
+SHAPES = [(1, 1, 128, 4), (7, 1, 8, 1), (300, 1, 96, 8), (1000, 1, 602, 7), (65, 1, 33, 3), (33, 1, 2048, 1), (9, 1, 2052, 1),
+          (5, 1, 4096, 2), (3, 1, 5000, 1), (70, 1, 24, 24), (50, 3, 16, 4), (400, 2, 40, 5), (40, 23, 96, 8), (9, 41, 602, 7),
+          (5, 100, 128, 32), (3, 257, 64, 1), (2, 1500, 48, 6), (1, 5000, 33, 3), (1, 3000, 256, 32), (2, 700, 1, 1),
+          (1, 129, 2304, 1), (1, 40000, 8, 2), (3, 2, 4104, 1)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("B,L,C,G", SHAPES)
+def test_equal_samples(B, L, C, G, dtype):
+    x, w, b, dy = inputs((B, L, C), dtype, seed=B + L)
+    print(f"norm {B}x{L}x{C} groups {G} {dtype}", flush=True)
+    run(x, G, w.to(dtype), b.to(dtype), "silu", dy=dy)
+
+
+@pytest.mark.parametrize("act", list(layers.ACTIVATIONS))
+@pytest.mark.parametrize("shape", [(20, 1, 24, 3), (20, 7, 24, 3), (1, 4000, 24, 3)], ids=str)
+def test_activations(act, shape):
+    x, w, b, dy = inputs(shape[:3], torch.float32, seed=5)
+    if act == "relu":                                        # a rounding next to 0 may turn the slope over: away from 0
+        b = b + 20 * torch.where(torch.arange(b.numel(), device="cuda") % 2 == 0, 1.0, -1.0)
+    run(x, shape[3], w, b, act, dy=dy)
+
+
+RAGGED = [[0], [1], [5], [0, 0, 3, 0], [1, 2, 0, 40, 7, 1], [300, 1, 0, 5], [23] * 100 + [0, 9000, 1], [2000, 1, 2500, 0, 1800],
+          [3] * 1000 + [20000], [0] * 70 + [4]]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("C,G", [(96, 8), (6, 2), (602, 7), (2100, 1), (1, 1)])
+@pytest.mark.parametrize("lens", RAGGED, ids=[f"r{i}" for i in range(len(RAGGED))])
+def test_ragged_samples(lens, C, G, dtype):
+    if sum(lens) * C > 6000000:
+        lens = [min(n, 700) for n in lens]
+    offsets = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+    x, w, b, dy = inputs((sum(lens), C), dtype, seed=len(lens))
+    print(f"norm ragged {lens[:8]} x{C} groups {G} {dtype}", flush=True)
+    run(x, G, w, b, "gelu", offsets, dy=dy)                  # float32 parameters beside either type
+
+
+@pytest.mark.parametrize("shape", [(30, 1, 32, 2), (6, 9, 32, 2), (1, 6000, 32, 2)], ids=str)
+def test_parameters_may_be_missing(shape):
+    x, w, b, dy = inputs(shape[:3], torch.float32, seed=2)
+    run(x, shape[3], None, None, None, dy=dy)
+    run(x, shape[3], w, None, "silu", dy=dy)
+    run(x, shape[3], None, b, "silu", dy=dy)
+
+
+@pytest.mark.parametrize("shape", [(30, 1, 32, 2), (6, 9, 32, 2), (1, 6000, 32, 2)], ids=str)
+def test_large_mean(shape):
+    """Variance of 1 beside a mean of 1000: the mean of squares less the square of the mean would have lost it."""
+    x, w, b, dy = inputs(shape[:3], torch.float32, seed=3, shift=0.0)
+    run(x + 1000.0, shape[3], w, b, "silu", dy=dy)
+
+
+@pytest.mark.parametrize("shape", [(4, 1, 32, 2), (4, 9, 32, 2), (1, 6000, 32, 2)], ids=str)
+def test_no_variance(shape):
+    x, w, b, dy = inputs(shape[:3], torch.float32, seed=4)
+    y, dx, _, _ = run(torch.full_like(x, 2.5), shape[3], w, b, None, dy=dy)
+    assert torch.equal(y, b.detach().expand_as(y))
+
+
+@pytest.mark.parametrize("B,L", [(50, 1), (30, 9), (3, 5000)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_bad_numbers_stay_in_their_sample_and_group(B, L, bad):
+    x, w, b, dy = inputs((B, L, 32), torch.float32, seed=6)
+    clean, clean_dx, _, _ = run(x.clone(), 4, w.clone(), b.clone(), "silu", dy=dy)
+    x = x.detach().clone()
+    x[1, L // 2, 9] = bad                                    # group 1
+    x.requires_grad_(True)
+    y = layers.group_norm(x, 4, w, b, activation="silu")
+    dx, = torch.autograd.grad(y, x, dy)
+    for got, want in ((y, clean), (dx, clean_dx)):
+        assert torch.isnan(got[1, :, 8:16]).all()
+        keep = torch.ones_like(got, dtype=torch.bool)
+        keep[1, :, 8:16] = False
+        assert torch.equal(got[keep], want[keep])
+
+
+def test_strided_input_and_gradient():
+    x, w, b, dy = inputs((500, 48), torch.float32, seed=7)
+    wide = torch.full((500, 64), float("nan"), device="cuda")
+    wide[:, 5:53] = x
+    wide_dy = torch.full((500, 50), float("nan"), device="cuda")
+    wide_dy[:, 1:49] = dy
+    want = run(x, 4, w, b, "silu", dy=dy)
+    for other, grad in ((wide[:, 5:53], wide_dy[:, 1:49]), (x.detach().t().contiguous().t(), dy.t().contiguous().t())):
+        assert not other.is_contiguous()
+        got = run(other.detach(), 4, w, b, "silu", dy=grad)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    # a broadcast gradient, and one row for all samples
+    run(x, 4, w, b, "silu", dy=dy[:1].expand(500, 48))
+    run(x.detach()[:1].expand(500, 48), 4, w, b, "silu", dy=dy)
+    # an address that is a multiple of an element's size only
+    odd = torch.empty(500 * 48 + 1, device="cuda")[1:].view(500, 48)
+    odd.copy_(x.detach())
+    got = run(odd, 4, w, b, "silu", dy=dy)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("shape", [(40, 1, 24, 3), (8, 17, 24, 3), (1, 5000, 24, 3)], ids=str)
+def test_gradient_against_differences(shape):
+    """The slope of sum(dy y) along a direction v, by central differences of step h of the kernels' own y: truncation
+    h^2 / 6 times a third derivative (of order |dy| |v| once a sample's numbers are of order 1: 20 h^2 covers silu and the
+    norm), rounding e |y| |dy| / h, both summed as independent errors would."""
+    x, w, b, dy = inputs(shape[:3], torch.float32, seed=8)
+    x = x / 1.5
+    g = torch.Generator(device="cuda").manual_seed(9)
+    h = 2.0 ** -7
+    _, dx, dw, db = run(x, shape[3], w, b, "silu", dy=dy)
+    for which, grad in ((0, dx), (1, dw), (2, db)):
+        v = torch.randn(grad.shape, generator=g, device="cuda")
+        ends = []
+        for sign in (1, -1):
+            args = [x.detach(), w.detach(), b.detach()]
+            args[which] = args[which] + sign * h * v
+            ends.append((layers.group_norm(args[0], shape[3], args[1], args[2], activation="silu").double() * dy.double()).sum())
+        slope = float((ends[0] - ends[1]) / (2 * h))
+        want = float((grad.double() * v.double()).sum())
+        n = math.sqrt(dy.numel())
+        assert abs(slope - want) <= n * (20 * h * h + 16 * E / h) * 4, (which, slope, want)
+
+
+def test_results_do_not_change_from_run_to_run():
+    lens = [23] * 300 + [0, 9000, 1, 30000]
+    offsets = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+    x, w, b, dy = inputs((sum(lens), 40), torch.float32, seed=10)
+    for t in (x, w, b):
+        t.requires_grad_(True)
+
+    def once():
+        y = layers.group_norm(x, 5, w, b, activation="silu", offsets=offsets)
+        return [y.detach(), *torch.autograd.grad(y, (x, w, b), dy)]
+
+    first = once()
+    for _ in range(5):
+        assert all(torch.equal(p, q) for p, q in zip(first, once()))
+
+
+def test_other_stream_and_graph():
+    """On a stream of its own, and in a graph that is replayed between eager work, on inputs that change."""
+    lens = [23] * 50 + [0, 4000]
+    offsets = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+    x, w, b, dy = inputs((sum(lens), 96), torch.float32, seed=11)
+    for t in (x, w, b):
+        t.requires_grad_(True)
+
+    def once():
+        y = layers.group_norm(x, 8, w, b, activation="silu", offsets=offsets)
+        return [y.detach(), *torch.autograd.grad(y, (x, w, b), dy)]
+
+    want = once()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        once()
+        got = once()
+    s.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = once()
+    for k in range(4):
+        with torch.no_grad():
+            x.mul_(-0.5).add_(0.1 * k)
+        want = once()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), k
+
+
+def test_more_than_2_31_numbers():
+    """The last rows of a tensor of 2^31 numbers and a few: each row a sample, and all rows one sample of which the last
+    rows alone are not zero."""
+    rows, C = 2 ** 21 + 77, 1024
+    x = torch.zeros((rows, C), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(12)
+    x[-200:] = torch.randn(200, C, generator=g, device="cuda").to(torch.bfloat16)
+    y = layers.group_norm(x.view(rows, 1, C), 8, activation="silu")
+    assert torch.equal(y[-200:], layers.group_norm(x[-200:].view(200, 1, C), 8, activation="silu"))
+    del y
+    tail = x[-200:].double().unflatten(1, (8, -1))
+    n = rows * 128
+    mean = tail.sum(dim=(0, 2)) / n
+    var = (tail * tail).sum(dim=(0, 2)) / n - mean * mean
+    want = (tail - mean[None, :, None]) / (var + 1e-5).sqrt()[None, :, None]
+    y = layers.group_norm(x, 8)
+    err = (y[-200:].double() - want.flatten(1)).abs()
+    assert (err <= 2.0 ** -8 * want.flatten(1).abs() + 1e-4).all()
+    assert torch.equal(y[0], y[rows - 201])
+
+
+def test_module_and_empty_inputs():
+    m = layers.GroupNorm(4, 32, activation="gelu").cuda()
+    x = torch.randn(10, 32, device="cuda")
+    assert torch.equal(m(x), layers.group_norm(x, 4, m.weight, m.bias, activation="gelu"))
+    for shape, offsets in (((0, 32), None), ((3, 0, 32), None), ((0, 5, 32), None), ((0, 32), [0]), ((0, 32), [0, 0, 0])):
+        x = torch.empty(shape, device="cuda", requires_grad=True)
+        o = None if offsets is None else torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        y = layers.group_norm(x, 4, m.weight, m.bias, offsets=o)
+        dx, dw, db = torch.autograd.grad(y, (x, m.weight, m.bias), torch.empty_like(y))
+        assert y.shape == x.shape and dx.shape == x.shape and not dw.any() and not db.any()
+
+
+def test_offsets_that_are_no_valid_ones_touch_no_other_memory():
+    x, w, b, dy = inputs((100, 16), torch.float32, seed=13)
+    for offsets in ([0, 5, 2000000000], [-7, 50, 20, 100], [90, 10, 100]):
+        o = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        x.requires_grad_(True)
+        y = layers.group_norm(x, 2, w, b, offsets=o)
+        torch.autograd.grad(y, x, dy)
+    torch.cuda.synchronize()
+
+
+def test_refusals():
+    x = torch.randn(6, 4, 12, device="cuda")
+    w = torch.ones(12, device="cuda")
+    cases = [
+        (ValueError, lambda: layers.group_norm(x, 5)),
+        (ValueError, lambda: layers.group_norm(x, 0)),
+        (ValueError, lambda: layers.group_norm(x, 3, activation="tanh")),
+        (ValueError, lambda: layers.group_norm(x, 3, weight=w[:5])),
+        (ValueError, lambda: layers.group_norm(x, 3, weight=w.cpu())),
+        (ValueError, lambda: layers.group_norm(x.cpu(), 3)),
+        (ValueError, lambda: layers.group_norm(x[0, 0], 3)),
+        (TypeError, lambda: layers.group_norm(x.half(), 3)),
+        (TypeError, lambda: layers.group_norm(x.double(), 3)),
+        (TypeError, lambda: layers.group_norm(x, 3, w, w.bfloat16())),
+        (ValueError, lambda: layers.group_norm(x, 3, offsets=torch.zeros(3, dtype=torch.int32, device="cuda"))),
+        (TypeError, lambda: layers.group_norm(x[0], 3, offsets=torch.zeros(3, dtype=torch.int64, device="cuda"))),
+        (ValueError, lambda: layers.group_norm(x[0], 3, offsets=torch.zeros(1, dtype=torch.int32, device="cuda"))),
+        (RuntimeError, lambda: layers.group_norm(x, 3, eps=-1.0)),
+        (ValueError, lambda: layers.GroupNorm(5, 12)),
+    ]
+    for error, call in cases:
+        with pytest.raises(error):
+            call()
+    x.requires_grad_(True)
+    y = layers.group_norm(x, 3, w)
+    g, = torch.autograd.grad(y.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiated again"):
+        g.sum().backward()
