@@ -85,6 +85,34 @@ int da_distill_backward(int dtype, int64_t rows, int64_t classes, int64_t best, 
                         const void *index, int index64, const void *top, int top_dtype, float temperature,
                         const float *stats, const float *dloss, int64_t dloss_stride, void *dz, void *stream);
 
+/*
+ * Gated feed-forward block on the matrix cores:
+ *
+ *   u = x . w_gate,  v = x . w_up,  a = act(u) v,  y = a . w_down
+ *   da = dy . w_down^T,  du = da v act'(u),  dv = da act(u),  dx = du . w_gate^T + dv . w_up^T,
+ *   dw_gate = x^T . du,  dw_up = x^T . dv,  dw_down = a^T . dy
+ *
+ *   x         rows x d, ldx >= d;  w_gate, w_up  d x h;  w_down  h x dout;  y, dy  rows x dout (ldy >= dout), all of dtype,
+ *             row-major, dense where no leading dimension is given
+ *   u, v      float32, rows x h: written forward where not NULL (a backward pass is to follow), read backward.  They stay in
+ *             32 bits for bfloat16, too: rounded, they would add as much to the error of dx as everything else together.
+ *   a         rows x h of dtype, written forward (always), read backward; with bfloat16 it, du and dv are rounded, since they
+ *             are operands of the matrix cores
+ *   dx, dw_*  dense; any of them may be NULL and is then not computed
+ *
+ * Sums are held in 32 bits.  float32 is multiplied as it is (fp32 matrix cores).  All sizes up to 2^30, and fewer than 2^24
+ * tiles of a result (DA_ERR_UNSUPPORTED beyond).
+ */
+int da_gated_workspace(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout, size_t *forward_bytes,
+                       size_t *backward_bytes /* host, out */);
+int da_gated(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout, const void *x, int64_t ldx, const void *w_gate,
+             const void *w_up, const void *w_down, int act, void *y, float *u, float *v, void *a, void *workspace,
+             size_t workspace_bytes, void *stream);
+int da_gated_backward(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout, const void *x, int64_t ldx, const void *dy,
+                      int64_t ldy, const void *w_gate, const void *w_up, const void *w_down, int act, const float *u,
+                      const float *v, const void *a, void *dx, void *dw_gate, void *dw_up, void *dw_down, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,7 +38,7 @@ EXPORTS = ("da_spmm", "da_spmm_ex", "da_spmm_select", "da_spmm_features", "da_cs
 DA_F32, DA_BF16 = 0, 1
 DA_ACT_NONE, DA_ACT_RELU, DA_ACT_SILU, DA_ACT_GELU, DA_ACT_SIGMOID = range(5)
 LAYER_EXPORTS = ("da_group_norm_sizes", "da_group_norm", "da_group_norm_backward", "da_distill_workspace", "da_distill",
-                 "da_distill_backward")
+                 "da_distill_backward", "da_gated_workspace", "da_gated", "da_gated_backward")
 
 
 class da_features(ctypes.Structure):

@@ -11,7 +11,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdaspmm.so")
-SOURCES = ["da_spmm_api.hip", "da_layers.hip", "da_spmm_select.cpp"]
+SOURCES = ["da_spmm_api.hip", "da_layers.hip", "da_gated_f32.hip", "da_gated_bf16.hip", "da_spmm_select.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
     # packed fp32 arithmetic stays off for all device code

@@ -1,0 +1,185 @@
+// Products of the gated feed-forward block: tiles, parts of the sums, launches.  Included by one translation unit for
+// each type.
+#pragma once
+#include "da_gated.h"
+#include "da_gated_kernels.hip"
+#include "da_internal.h"
+
+#include <algorithm>
+
+namespace daspmm {
+namespace {
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+// Tile of a product, and how its sum is cut: a tile of 128 x 128 has the most products for what it reads, fewer rows or
+// columns take one that has no more of them than needed; where the tiles do not fill the chip, the inner axis is cut
+// until two blocks a compute unit work, each on at least four tiles of it.
+struct GemmPlan {
+    int BM, BN;
+    int splits, per;
+};
+
+template <class T> GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi) {
+    GemmPlan p{};
+    const int64_t width = epi == kGate ? 2 * N : N;
+    p.BN = width <= 64 && M > 64 && epi != kGate ? 64 : 128;
+    p.BM = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const int64_t tiles = ceil_div(M, p.BM) * ceil_div(width, p.BN) * batches;
+    const int64_t inner = ceil_div(K, kLineBytes / (int64_t)sizeof(T)) * segments;
+    int64_t splits = 1;
+    if (tiles < compute_units()) splits = std::min(2 * compute_units() / std::max<int64_t>(tiles, 1), ceil_div(inner, 4));
+    p.per = (int)std::max<int64_t>(1, ceil_div(inner, std::max<int64_t>(splits, 1)));
+    p.splits = (int)std::max<int64_t>(1, ceil_div(inner, p.per));
+    return p;
+}
+
+template <class T> size_t part_bytes(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi) {
+    const GemmPlan p = gemm_plan<T>(M, N, K, segments, batches, epi);
+    return p.splits > 1 ? (size_t)batches * p.splits * M * N * (epi == kGate ? 2 : 1) * sizeof(float) : 0;
+}
+
+template <class T, int ALAY, int BLAY, int EPI>
+void gemm(GemmArgs<T> g, int batches, float* part, hipStream_t s) {
+    if (g.M == 0 || g.N == 0) return;
+    const GemmPlan p = gemm_plan<T>(g.M, g.N, g.K, g.segments, batches, EPI);
+    g.splits = p.splits;
+    g.per = p.per;
+    g.part = part;
+    const int64_t width = EPI == kGate ? 2 * (int64_t)g.N : g.N;
+    const dim3 grid((unsigned)(ceil_div(g.M, p.BM) * ceil_div(width, p.BN)), (unsigned)p.splits, (unsigned)batches);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, g); };
+    if constexpr (EPI != kGate) {
+        if (p.BN == 64) go(gated_gemm_kernel<T, 2, 4, 4, 1, ALAY, BLAY, EPI>);
+    }
+    if (p.BN == 128) {
+        if (p.BM == 16) go(gated_gemm_kernel<T, 1, 2, 1, 4, ALAY, BLAY, EPI>);
+        else if (p.BM == 32) go(gated_gemm_kernel<T, 2, 2, 1, 4, ALAY, BLAY, EPI>);
+        else if (p.BM == 64) go(gated_gemm_kernel<T, 4, 2, 1, 4, ALAY, BLAY, EPI>);
+        else go(gated_gemm_kernel<T, 4, 4, 2, 2, ALAY, BLAY, EPI>);
+    }
+    if (p.splits > 1) {
+        const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.M * g.N, 256), 16384);
+        hipLaunchKernelGGL((gated_join_kernel<T, EPI>), dim3((unsigned)blocks, 1, (unsigned)batches), dim3(256), 0, s, g);
+    }
+}
+
+}  // namespace
+
+template <class T> size_t gated_forward_bytes(const GatedShape& s) {
+    return std::max(part_bytes<T>(s.rows, s.h, s.d, 1, 1, kGate), part_bytes<T>(s.rows, s.dout, s.h, 1, 1, kStore));
+}
+
+template <class T> size_t gated_backward_bytes(const GatedShape& s) {
+    size_t part = part_bytes<T>(s.rows, s.h, s.dout, 1, 1, kGateGrad);
+    part = std::max(part, part_bytes<T>(s.rows, s.d, s.h, 2, 1, kStore));
+    part = std::max(part, part_bytes<T>(s.d, s.h, s.rows, 1, 2, kStore));
+    part = std::max(part, part_bytes<T>(s.h, s.dout, s.rows, 1, 1, kStore));
+    return 2 * round16((size_t)(s.rows * s.h) * sizeof(T)) + part;
+}
+
+template <class T> void gated_forward(const GatedCall& c) {
+    const int rows = (int)c.s.rows, d = (int)c.s.d, h = (int)c.s.h, dout = (int)c.s.dout;
+    float* part = reinterpret_cast<float*>(c.workspace);
+    GemmArgs<T> g{};
+    g.A[0] = g.A[1] = static_cast<const T*>(c.x);
+    g.B[0] = static_cast<const T*>(c.wg);
+    g.B[1] = static_cast<const T*>(c.wu);
+    g.lda = c.ldx;
+    g.ldb = h;
+    g.M = rows;
+    g.N = h;
+    g.K = d;
+    g.segments = 1;
+    g.C[0] = static_cast<T*>(c.a);
+    g.U = c.u;
+    g.V = c.v;
+    g.act = c.act;
+    gemm<T, kInner, kOuter, kGate>(g, 1, part, c.stream);
+
+    g = GemmArgs<T>{};
+    g.A[0] = g.A[1] = static_cast<const T*>(c.a);
+    g.B[0] = g.B[1] = static_cast<const T*>(c.wd);
+    g.lda = h;
+    g.ldb = dout;
+    g.M = rows;
+    g.N = dout;
+    g.K = h;
+    g.segments = 1;
+    g.C[0] = static_cast<T*>(c.y);
+    gemm<T, kInner, kOuter, kStore>(g, 1, part, c.stream);
+}
+
+template <class T> void gated_backward(const GatedCall& c) {
+    const int rows = (int)c.s.rows, d = (int)c.s.d, h = (int)c.s.h, dout = (int)c.s.dout;
+    const size_t hidden = round16((size_t)(c.s.rows * c.s.h) * sizeof(T));
+    T* du = reinterpret_cast<T*>(c.workspace);
+    T* dv = reinterpret_cast<T*>(c.workspace + hidden);
+    float* part = reinterpret_cast<float*>(c.workspace + 2 * hidden);
+    GemmArgs<T> g{};
+    if (c.dx || c.dwg || c.dwu) {
+        g.A[0] = g.A[1] = static_cast<const T*>(c.dy);
+        g.B[0] = g.B[1] = static_cast<const T*>(c.wd);
+        g.lda = c.ldy;
+        g.ldb = dout;
+        g.M = rows;
+        g.N = h;
+        g.K = dout;
+        g.segments = 1;
+        g.C[0] = du;
+        g.C[1] = dv;
+        g.U = c.u;
+        g.V = c.v;
+        g.act = c.act;
+        gemm<T, kInner, kInner, kGateGrad>(g, 1, part, c.stream);
+    }
+    if (c.dx) {
+        g = GemmArgs<T>{};
+        g.A[0] = du;
+        g.A[1] = dv;
+        g.B[0] = static_cast<const T*>(c.wg);
+        g.B[1] = static_cast<const T*>(c.wu);
+        g.lda = h;
+        g.ldb = h;
+        g.M = rows;
+        g.N = d;
+        g.K = h;
+        g.segments = 2;
+        g.C[0] = static_cast<T*>(c.dx);
+        gemm<T, kInner, kInner, kStore>(g, 1, part, c.stream);
+    }
+    if (c.dwg || c.dwu) {
+        const int first = c.dwg ? 0 : 1, batches = c.dwg && c.dwu ? 2 : 1;
+        T* const of[2] = {du, dv};
+        void* const to[2] = {c.dwg, c.dwu};
+        g = GemmArgs<T>{};
+        g.A[0] = g.A[1] = static_cast<const T*>(c.x);
+        g.B[0] = of[first];
+        g.B[1] = dv;
+        g.lda = c.ldx;
+        g.ldb = h;
+        g.M = d;
+        g.N = h;
+        g.K = rows;
+        g.segments = 1;
+        g.C[0] = static_cast<T*>(to[first]);
+        g.C[1] = static_cast<T*>(c.dwu);
+        gemm<T, kOuter, kOuter, kStore>(g, batches, part, c.stream);
+    }
+    if (c.dwd) {
+        g = GemmArgs<T>{};
+        g.A[0] = g.A[1] = static_cast<const T*>(c.a);
+        g.B[0] = g.B[1] = static_cast<const T*>(c.dy);
+        g.lda = h;
+        g.ldb = c.ldy;
+        g.M = h;
+        g.N = dout;
+        g.K = rows;
+        g.segments = 1;
+        g.C[0] = static_cast<T*>(c.dwd);
+        gemm<T, kOuter, kOuter, kStore>(g, 1, part, c.stream);
+    }
+}
+
+}  // namespace daspmm

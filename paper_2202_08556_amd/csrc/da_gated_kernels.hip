@@ -1,0 +1,318 @@
+// The gated feed-forward block on the matrix cores:
+//   u = x Wg, v = x Wu, a = act(u) v, y = a Wd
+//   da = dy Wd^T, du = da v act'(u), dv = da act(u), dx = du Wg^T + dv Wu^T, dWg = x^T du, dWu = x^T dv, dWd = a^T dy
+// Every line is one product with the rest in its epilogue: both projections share the tile of x and leave as a; du and
+// dv leave the product of da; dx is one sum over both pairs.
+//
+// Operands stay as they are in memory.  A tile of one is either lines of neighbouring inner positions (x, a, dy
+// everywhere but in the weights' gradients, the weights in products with their transposes) or lines of neighbouring
+// outer ones.  Both are copied to LDS line by line; the second kind is turned around on the way to the registers (for
+// bf16 by the transposing LDS read, for float by reading single numbers).
+#pragma once
+#include "da_layer_common.h"
+
+namespace daspmm {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+enum { kInner = 0, kOuter = 1 };             // what neighbours in memory
+enum { kStore = 0, kGate = 1, kGateGrad = 2 };
+
+// 16 bytes a lane are a fragment: 8 bf16, one instruction of 16 x 16 x 32, or 4 floats, four of 16 x 16 x 4 (element j
+// of all lanes is one instruction: any assignment of inner positions to instructions gives the same sum).
+template <class T> struct Mma;
+template <> struct Mma<bf16> {
+    typedef bf16x8 Frag;
+    typedef Pack<uint16_t, 8>::type Memory;                  // at any address that an element may have
+    static constexpr int VEC = 8;
+    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mma<float> {
+    typedef f32x4 Frag;
+    typedef Pack<float, 4>::type Memory;
+    static constexpr int VEC = 4;
+    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <class T> struct GemmArgs {
+    const T* A[2];
+    const T* B[2];               // kGate: the second half of a tile's columns; otherwise operands of the second segment or batch
+    long lda, ldb;
+    int M, N, K;                 // K of one segment
+    int segments;                // pairs of operands whose products are summed
+    int splits, per;             // parts of the sum and tiles of the inner axis to each
+    T* C[2];                     // kStore: by batch; kGate: a; kGateGrad: du, dv
+    float *U, *V;                // kGate: written where not null; kGateGrad: read; dense M x N
+    float* part;                 // splits > 1: [batch][split][M][N] sums, of u and v side by side for kGate
+    int act;
+};
+
+constexpr int kLineBytes = 128;  // of the inner axis in a tile
+
+// One operand's tile: OUTER outer positions x kLineBytes of the inner axis
+template <class T, int LAY, int OUTER> struct Tile {
+    static constexpr int VEC = Mma<T>::VEC, BK = kLineBytes / (int)sizeof(T);
+    static constexpr int LINES = LAY == kInner ? OUTER : BK;
+    static constexpr int CHUNKS = (LAY == kInner ? BK : OUTER) / VEC;         // of 16 bytes in a line
+    // padding: 8 or 16 lines of a fragment's read lie in different banks
+    static constexpr int PITCH = CHUNKS * 16 + (LAY == kOuter && sizeof(T) == 2 ? 32 : 16);
+    static constexpr int BYTES = LINES * PITCH;
+    static constexpr int PER = (LINES * CHUNKS + 255) / 256;                  // chunks of a thread
+
+    // the fragment of outer positions o .. o + 15 and the step-th half of the inner axis
+    static __device__ __forceinline__ typename Mma<T>::Frag frag(const char* lds, int o, int step) {
+        const int i = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
+        if constexpr (LAY == kInner) {
+            return *reinterpret_cast<const typename Mma<T>::Frag*>(lds + (o + i) * PITCH + step * 64 + h * 16);
+        } else if constexpr (sizeof(T) == 2) {
+            // 16 lanes read 4 lines of 16 numbers and get a number of each line
+            const char* p = lds + (step * 32 + h * 8 + i / 4) * PITCH + (o + (i & 3) * 4) * 2;
+            typedef __attribute__((address_space(3))) s16x4* Lds;
+            union { s16x4 half[2]; bf16x8 all; } f;
+            f.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p);
+            f.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 4 * PITCH));
+            return f.all;
+        } else {
+            const char* p = lds + (step * 16 + h * 4) * PITCH + (o + i) * 4;
+            f32x4 f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const float*>(p + j * PITCH);
+            return f;
+        }
+    }
+};
+
+// 16 bytes at `at` of a line that has `left` elements from there on (none: zeros)
+template <class T> __device__ __forceinline__ uint4 edge_chunk(const T* p, int left) {
+    constexpr int VEC = Mma<T>::VEC;
+    T v[VEC] = {};
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+        if (i < left) v[i] = p[i];
+    uint4 r;
+    __builtin_memcpy(&r, v, 16);
+    return r;
+}
+template <class T> __device__ __forceinline__ uint4 whole_chunk(const T* p) {
+    const auto v = *reinterpret_cast<const typename Mma<T>::Memory*>(p);
+    uint4 r;
+    __builtin_memcpy(&r, &v, 16);
+    return r;
+}
+
+// MT x NT fragments of 16 x 16 to a wave, WM x WN waves to a block of 256 threads
+template <class T, int MT, int NT, int WM, int WN, int ALAY, int BLAY, int EPI>
+__global__ __launch_bounds__(256) void gated_gemm_kernel(GemmArgs<T> g)
+{
+    static_assert(WM * WN == 4, "four waves");
+    constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, HALF = BN / 2;
+    typedef Tile<T, ALAY, BM> TA;
+    typedef Tile<T, BLAY, BN> TB;
+    constexpr int VEC = Mma<T>::VEC, BK = TA::BK;
+    __shared__ __attribute__((aligned(16))) char lds[2][TA::BYTES + TB::BYTES];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / WN, wn = wave % WN;
+    constexpr int WIDTH = EPI == kGate ? HALF : BN;          // columns of the result in a block
+    const int tiles_n = (g.N + WIDTH - 1) / WIDTH;
+    const int bm = blockIdx.x / tiles_n, bn = blockIdx.x % tiles_n;
+    const int m0 = bm * BM, n0 = bn * WIDTH, batch = blockIdx.z;
+    const int tps = (g.K + BK - 1) / BK;                     // tiles of a segment
+    const int t0 = blockIdx.y * g.per, t1 = min(t0 + g.per, tps * g.segments);
+    const bool inside = m0 + BM <= g.M && n0 + WIDTH <= g.N;
+
+    uint4 ra[TA::PER], rb[TB::PER];
+    auto load = [&](int t) {
+        const int seg = t / tps, k0 = (t % tps) * BK;
+        const T* __restrict__ A = seg ? g.A[1] : g.A[0];
+        const T* __restrict__ B = seg + batch ? g.B[1] : g.B[0];
+        const bool whole = inside && k0 + BK <= g.K;
+#pragma unroll
+        for (int i = 0; i < TA::PER; ++i) {
+            const int q = tid + 256 * i, line = q / TA::CHUNKS, at = q % TA::CHUNKS * VEC;
+            if (TA::LINES * TA::CHUNKS % 256 != 0 && line >= TA::LINES) continue;
+            const int outer = m0 + (ALAY == kInner ? line : at), inner = k0 + (ALAY == kInner ? at : line);
+            const T* p = ALAY == kInner ? A + (long)outer * g.lda + inner : A + (long)inner * g.lda + outer;
+            if (whole) ra[i] = whole_chunk(p);
+            else ra[i] = edge_chunk(p, ALAY == kInner ? (outer < g.M ? g.K - inner : 0) : (inner < g.K ? g.M - outer : 0));
+        }
+#pragma unroll
+        for (int i = 0; i < TB::PER; ++i) {
+            const int q = tid + 256 * i, line = q / TB::CHUNKS, at = q % TB::CHUNKS * VEC;
+            if (TB::LINES * TB::CHUNKS % 256 != 0 && line >= TB::LINES) continue;
+            int col = BLAY == kInner ? line : at;
+            const T* W = B;
+            if (EPI == kGate && col >= HALF) { W = g.B[1]; col -= HALF; }
+            const int outer = n0 + col, inner = k0 + (BLAY == kInner ? at : line);
+            const T* p = BLAY == kInner ? W + (long)outer * g.ldb + inner : W + (long)inner * g.ldb + outer;
+            if (whole) rb[i] = whole_chunk(p);
+            else {
+                const int room = EPI == kGate ? min(g.N, n0 + HALF) : g.N;
+                rb[i] = edge_chunk(p, BLAY == kInner ? (outer < g.N ? g.K - inner : 0) : (inner < g.K ? room - outer : 0));
+            }
+        }
+    };
+    auto put = [&](char* buf) {
+#pragma unroll
+        for (int i = 0; i < TA::PER; ++i) {
+            const int q = tid + 256 * i, line = q / TA::CHUNKS;
+            if (TA::LINES * TA::CHUNKS % 256 != 0 && line >= TA::LINES) continue;
+            *reinterpret_cast<uint4*>(buf + line * TA::PITCH + q % TA::CHUNKS * 16) = ra[i];
+        }
+#pragma unroll
+        for (int i = 0; i < TB::PER; ++i) {
+            const int q = tid + 256 * i, line = q / TB::CHUNKS;
+            if (TB::LINES * TB::CHUNKS % 256 != 0 && line >= TB::LINES) continue;
+            *reinterpret_cast<uint4*>(buf + TA::BYTES + line * TB::PITCH + q % TB::CHUNKS * 16) = rb[i];
+        }
+    };
+    // first column of the wave's j-th fragment in the tile; kGate: the first half of them from Wg, the others from Wu
+    auto column = [&](int j) {
+        return EPI == kGate ? (j < NT / 2 ? wn * (NT / 2) * 16 + j * 16 : HALF + wn * (NT / 2) * 16 + (j - NT / 2) * 16)
+                            : wn * NT * 16 + j * 16;
+    };
+
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    if (t0 < t1) {
+        load(t0);
+        put(lds[0]);
+    }
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const char* buf = lds[(t - t0) & 1];
+        if (t + 1 < t1) load(t + 1);
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            typename Mma<T>::Frag a[MT], b[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[i] = TA::frag(buf, wm * MT * 16 + i * 16, step);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[j] = TB::frag(buf + TA::BYTES, column(j), step);
+            // columns as the first operand: a lane's four results are neighbours in a row
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = Mma<T>::mul(b[j], a[i], acc[i][j]);
+        }
+        if (t + 1 < t1) put(lds[(t + 1 - t0) & 1]);
+        __syncthreads();
+    }
+
+    const int i16 = lane & 15, h = lane >> 4;
+    auto store4 = [&](auto* p, int left, const float (&x)[4]) {
+        if (left >= 4) store_floats<4>(p, x);
+        else
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float one[1] = {x[q]};
+                if (q < left) store_floats<1>(p + q, one);
+            }
+    };
+    constexpr int COLS = EPI == kGate ? NT / 2 : NT;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int m = m0 + (wm * MT + i) * 16 + i16;
+        if (m >= g.M) continue;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) {
+            const int n = n0 + column(j) + 4 * h, left = g.N - n;
+            if (left <= 0) continue;
+            const long at = (long)m * g.N + n;
+            float x[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = acc[i][j][q];
+            if (g.splits > 1) {
+                const long width = EPI == kGate ? 2L * g.N : g.N;
+                float* p = g.part + (((long)batch * g.splits + blockIdx.y) * g.M + m) * width + n;
+                store4(p, left, x);
+                if constexpr (EPI == kGate) {
+                    float v[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = acc[i][j + NT / 2][q];
+                    store4(p + g.N, left, v);
+                }
+            } else if constexpr (EPI == kStore) {
+                store4((batch ? g.C[1] : g.C[0]) + at, left, x);
+            } else if constexpr (EPI == kGate) {
+                float v[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = acc[i][j + NT / 2][q];
+                if (g.U) {
+                    store4(g.U + at, left, x);
+                    store4(g.V + at, left, v);
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] = act_value(g.act, x[q]) * v[q];
+                store4(g.C[0] + at, left, x);
+            } else {
+                float du[4], dv[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float value;
+                    const float u = q < left ? g.U[at + q] : 0.f, v = q < left ? g.V[at + q] : 0.f;
+                    const float slope = act_slope(g.act, u, &value);
+                    du[q] = x[q] * v * slope;
+                    dv[q] = x[q] * value;
+                }
+                store4(g.C[0] + at, left, du);
+                store4(g.C[1] + at, left, dv);
+            }
+        }
+    }
+}
+
+// Sums the parts of a product and does what its epilogue would have done; a thread owns one number.
+template <class T, int EPI>
+__global__ __launch_bounds__(256) void gated_join_kernel(GemmArgs<T> g)
+{
+    const long total = (long)g.M * g.N, width = EPI == kGate ? 2L * g.N : g.N;
+    const int batch = blockIdx.z;
+    for (long at = (long)blockIdx.x * 256 + threadIdx.x; at < total; at += (long)gridDim.x * 256) {
+        const long m = at / g.N, n = at % g.N, plane = (long)g.M * width;
+        const float* __restrict__ p = g.part + (long)batch * g.splits * plane + m * width + n;
+        float x = 0.f, v = 0.f;
+        constexpr int U = 4;
+        int s = 0;
+        float ax[U] = {}, av[U] = {};
+        for (; s + U <= g.splits; s += U)
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                ax[k] += p[(s + k) * plane];
+                if constexpr (EPI == kGate) av[k] += p[(s + k) * plane + g.N];
+            }
+        for (; s < g.splits; ++s) {
+            ax[0] += p[s * plane];
+            if constexpr (EPI == kGate) av[0] += p[s * plane + g.N];
+        }
+        x = (ax[0] + ax[1]) + (ax[2] + ax[3]);
+        v = (av[0] + av[1]) + (av[2] + av[3]);
+        if constexpr (EPI == kStore) {
+            const float one[1] = {x};
+            store_floats<1>((batch ? g.C[1] : g.C[0]) + at, one);
+        } else if constexpr (EPI == kGate) {
+            if (g.U) { g.U[at] = x; g.V[at] = v; }
+            const float one[1] = {act_value(g.act, x) * v};
+            store_floats<1>(g.C[0] + at, one);
+        } else {
+            float value;
+            const float slope = act_slope(g.act, g.U[at], &value);
+            const float du[1] = {x * g.V[at] * slope}, dv[1] = {x * value};
+            store_floats<1>(g.C[0] + at, du);
+            store_floats<1>(g.C[1] + at, dv);
+        }
+    }
+}
+
+}  // namespace daspmm

@@ -1,6 +1,7 @@
 // Host side of include/da_layers.h: argument checks, choice of kernels and launch geometry.
 #include "da_layers.h"
 
+#include "da_gated.h"
 #include "da_internal.h"
 #include "da_norm_kernels.hip"
 #include "da_distill_kernels.hip"
@@ -468,4 +469,109 @@ extern "C" int da_distill_backward(int dtype, int64_t rows, int64_t classes, int
     if (dtype == DA_F32) distill_grad<float, 4>(p, rows, te, z, ldz, temperature, stats, dloss, dloss_stride, dz, (hipStream_t)stream);
     else distill_grad<bf16, 8>(p, rows, te, z, ldz, temperature, stats, dloss, dloss_stride, dz, (hipStream_t)stream);
     return launched("da_distill_backward launch");
+}
+
+// ------------------------------------------------------------------------------------------
+// gated feed-forward block
+// ------------------------------------------------------------------------------------------
+namespace {
+
+constexpr int64_t kGatedMax = 1 << 30;                      // the kernels count rows and columns, and those past the end, in 32 bits
+constexpr int64_t kGatedMaxTiles = 1 << 24;                 // of 2^32 threads and more the high bits are lost
+
+int gated_check(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout) {
+    if (!known_dtype(dtype)) return fail(DA_ERR_UNSUPPORTED, "dtype is neither DA_F32 nor DA_BF16");
+    if (rows < 0 || d < 0 || h < 0 || dout < 0) return fail(DA_ERR_INVALID_ARG, "negative size");
+    const int64_t most = std::max({rows, d, h, dout});
+    if (most > kGatedMax) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    const int64_t n = std::max({d, 2 * h, dout});
+    if (ceil_div(std::max(rows, h), 128) * ceil_div(n, 64) >= kGatedMaxTiles || ceil_div(d, 128) * ceil_div(h, 64) >= kGatedMaxTiles)
+        return fail(DA_ERR_UNSUPPORTED, "size too large");
+    return DA_OK;
+}
+
+}  // namespace
+
+extern "C" int da_gated_workspace(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout, size_t* forward_bytes,
+                                  size_t* backward_bytes)
+{
+    if (!forward_bytes || !backward_bytes) return fail(DA_ERR_INVALID_ARG, "null output");
+    const int st = gated_check(dtype, rows, d, h, dout);
+    if (st != DA_OK) return st;
+    const GatedShape s{rows, d, h, dout};
+    *forward_bytes = dtype == DA_F32 ? gated_forward_bytes<float>(s) : gated_forward_bytes<bf16>(s);
+    *backward_bytes = dtype == DA_F32 ? gated_backward_bytes<float>(s) : gated_backward_bytes<bf16>(s);
+    return DA_OK;
+}
+
+extern "C" int da_gated(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout, const void* x, int64_t ldx, const void* w_gate,
+                        const void* w_up, const void* w_down, int act, void* y, float* u, float* v, void* a, void* workspace,
+                        size_t workspace_bytes, void* stream)
+{
+    size_t need = 0, backward = 0;
+    const int st = da_gated_workspace(dtype, rows, d, h, dout, &need, &backward);
+    if (st != DA_OK) return st;
+    if (act < 0 || act >= DA_NUM_ACTS) return fail(DA_ERR_INVALID_ARG, "unknown activation");
+    if (ldx < d) return fail(DA_ERR_INVALID_ARG, "leading dimension smaller than the extent it strides over");
+    if (rows == 0 || (h == 0 && dout == 0)) return DA_OK;
+    if ((d > 0 && (!x || (h > 0 && (!w_gate || !w_up)))) || (h > 0 && (!a || (dout > 0 && !w_down))) || (dout > 0 && !y))
+        return fail(DA_ERR_INVALID_ARG, "null x, weight, a or y");
+    if (!u != !v) return fail(DA_ERR_INVALID_ARG, "one of u and v is null");
+    if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return workspace_error();
+    GatedCall c{};
+    c.s = GatedShape{rows, d, h, dout};
+    c.x = x;
+    c.wg = w_gate;
+    c.wu = w_up;
+    c.wd = w_down;
+    c.ldx = ldx;
+    c.act = act;
+    c.u = u;
+    c.v = v;
+    c.a = a;
+    c.y = y;
+    c.workspace = static_cast<char*>(workspace);
+    c.stream = (hipStream_t)stream;
+    if (dtype == DA_F32) gated_forward<float>(c);
+    else gated_forward<bf16>(c);
+    return launched("da_gated launch");
+}
+
+extern "C" int da_gated_backward(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout, const void* x, int64_t ldx,
+                                 const void* dy, int64_t ldy, const void* w_gate, const void* w_up, const void* w_down, int act,
+                                 const float* u, const float* v, const void* a, void* dx, void* dw_gate, void* dw_up, void* dw_down,
+                                 void* workspace, size_t workspace_bytes, void* stream)
+{
+    size_t forward = 0, need = 0;
+    const int st = da_gated_workspace(dtype, rows, d, h, dout, &forward, &need);
+    if (st != DA_OK) return st;
+    if (act < 0 || act >= DA_NUM_ACTS) return fail(DA_ERR_INVALID_ARG, "unknown activation");
+    if (ldx < d || ldy < dout) return fail(DA_ERR_INVALID_ARG, "leading dimension smaller than the extent it strides over");
+    const bool inner = rows > 0 && h > 0;
+    if ((rows > 0 && ((d > 0 && !x) || (dout > 0 && !dy))) || (inner && (!u || !v || !a)) ||
+        (h > 0 && ((d > 0 && (!w_gate || !w_up)) || (dout > 0 && !w_down))))
+        return fail(DA_ERR_INVALID_ARG, "null x, dy, weight, u, v or a");
+    if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return workspace_error();
+    GatedCall c{};
+    c.s = GatedShape{rows, d, h, dout};
+    c.x = x;
+    c.dy = dy;
+    c.wg = w_gate;
+    c.wu = w_up;
+    c.wd = w_down;
+    c.ldx = ldx;
+    c.ldy = ldy;
+    c.act = act;
+    c.u = const_cast<float*>(u);
+    c.v = const_cast<float*>(v);
+    c.a = const_cast<void*>(a);
+    c.dx = dx;
+    c.dwg = dw_gate;
+    c.dwu = dw_up;
+    c.dwd = dw_down;
+    c.workspace = static_cast<char*>(workspace);
+    c.stream = (hipStream_t)stream;
+    if (dtype == DA_F32) gated_backward<float>(c);
+    else gated_backward<bf16>(c);
+    return launched("da_gated_backward launch");
 }

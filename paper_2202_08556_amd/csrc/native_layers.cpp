@@ -7,6 +7,8 @@
 
 #include <torch/csrc/autograd/functions/basic_ops.h>
 
+#include <array>
+
 #include "da_layers.h"
 
 namespace da_native {
@@ -337,6 +339,157 @@ Tensor distill(const Tensor& z, const Tensor& index, const Tensor& top, double t
     return out.first;
 }
 
+// ------------------------------------------------------------------------------------------
+// gated feed-forward block
+// ------------------------------------------------------------------------------------------
+struct Weights {
+    Tensor gate, up, down;       // contiguous
+};
+
+struct GatedSizes {
+    int64_t rows, d, h, dout;
+};
+
+GatedSizes gated_sizes(const Tensor& x, const Weights& w) {
+    on_gpu(x, "x");
+    dtype_of(x, "x");
+    if (x.dim() < 1) throw py::value_error("x must have a last axis");
+    for (const auto& p : {std::make_pair(&w.gate, "w_gate"), std::make_pair(&w.up, "w_up"), std::make_pair(&w.down, "w_down")}) {
+        on_device_of(x, *p.first, p.second);
+        if (p.first->scalar_type() != x.scalar_type()) throw py::type_error(std::string(p.second) + " must have the type of x");
+        if (p.first->dim() != 2) throw py::value_error(std::string(p.second) + " must be a matrix");
+    }
+    GatedSizes s{1, x.size(-1), w.gate.size(1), w.down.size(1)};
+    for (int64_t i = 0; i + 1 < x.dim(); ++i) s.rows *= x.size(i);
+    if (w.gate.size(0) != s.d || !w.up.sizes().equals(w.gate.sizes()) || w.down.size(0) != s.h)
+        throw py::value_error("sizes do not match: x (..., d), w_gate and w_up (d, h), w_down (h, d_out)");
+    return s;
+}
+
+Weights whole(const Weights& w) {
+    return {w.gate.resolve_neg().contiguous(), w.up.resolve_neg().contiguous(), w.down.resolve_neg().contiguous()};
+}
+
+std::vector<int64_t> with_last(at::IntArrayRef sizes, int64_t last) {
+    std::vector<int64_t> v(sizes.begin(), sizes.end());
+    v.back() = last;
+    return v;
+}
+
+struct GatedKept {
+    Tensor u, v, a;
+};
+
+int64_t gated_pitch(const Tensor& t, const Tensor& m) { return t.dim() == 1 ? t.size(0) : pitch(m); }
+
+Tensor gated_forward(const Tensor& x, const Weights& weights, int act, bool train, GatedKept* kept) {
+    const GatedSizes s = gated_sizes(x, weights);
+    const Weights w = whole(weights);
+    c10::DeviceGuard guard(x.device());
+    const Tensor m = as_rows(x);
+    const int dt = dtype_of(x, "x");
+    Tensor y = at::empty(with_last(x.sizes(), s.dout), x.options());
+    kept->a = at::empty({s.rows, s.h}, x.options());
+    if (train) {
+        kept->u = at::empty({s.rows, s.h}, x.options().dtype(at::kFloat));
+        kept->v = at::empty({s.rows, s.h}, x.options().dtype(at::kFloat));
+    }
+    size_t fwd = 0, bwd = 0;
+    check(da_gated_workspace(dt, s.rows, s.d, s.h, s.dout, &fwd, &bwd));
+    const Tensor ws = scratch(fwd, x);
+    check(da_gated(dt, s.rows, s.d, s.h, s.dout, data<void>(m), gated_pitch(x, m), data<void>(w.gate), data<void>(w.up),
+                   data<void>(w.down), act, data<void>(y), data<float>(kept->u), data<float>(kept->v), data<void>(kept->a),
+                   data<void>(ws), fwd, stream_of(x)));
+    return y;
+}
+
+variable_list gated_backward(const Tensor& dy, const Tensor& x, const Weights& weights, int act, const GatedKept& kept,
+                             const std::array<bool, 4>& need) {
+    const GatedSizes s = gated_sizes(x, weights);
+    const Weights w = whole(weights);
+    if (dy.dim() != x.dim() || dy.scalar_type() != x.scalar_type() || dy.size(-1) != s.dout || dy.numel() != s.rows * s.dout)
+        throw py::value_error("dy must be like y");
+    on_device_of(x, dy, "dy");
+    c10::DeviceGuard guard(x.device());
+    const Tensor m = as_rows(x), d = as_rows(dy);
+    const int dt = dtype_of(x, "x");
+    variable_list out(4);
+    if (need[0]) out[0] = at::empty(x.sizes(), x.options());
+    if (need[1]) out[1] = at::empty(w.gate.sizes(), w.gate.options());
+    if (need[2]) out[2] = at::empty(w.up.sizes(), w.up.options());
+    if (need[3]) out[3] = at::empty(w.down.sizes(), w.down.options());
+    size_t fwd = 0, bwd = 0;
+    check(da_gated_workspace(dt, s.rows, s.d, s.h, s.dout, &fwd, &bwd));
+    const Tensor ws = scratch(bwd, x);
+    check(da_gated_backward(dt, s.rows, s.d, s.h, s.dout, data<void>(m), gated_pitch(x, m), data<void>(d), gated_pitch(dy, d),
+                            data<void>(w.gate), data<void>(w.up), data<void>(w.down), act, data<float>(kept.u),
+                            data<float>(kept.v), data<void>(kept.a), data<void>(out[0]), data<void>(out[1]), data<void>(out[2]),
+                            data<void>(out[3]), data<void>(ws), bwd, stream_of(x)));
+    return out;
+}
+
+struct GatedBackward : torch::autograd::Node {
+    SavedVariable x, gate, up, down;
+    GatedKept kept;
+    int act = 0;
+
+    void release_variables() override {
+        std::lock_guard<std::mutex> lk(mutex_);
+        x.reset_data();
+        gate.reset_data();
+        up.reset_data();
+        down.reset_data();
+        kept = GatedKept{};
+    }
+    variable_list apply(variable_list&& grads) override {
+        return in_backward([&] { return gradients(grads); });
+    }
+    variable_list gradients(const variable_list& grads) {
+        if (!grads[0].defined()) return variable_list(4);
+        Tensor X;
+        Weights w;
+        GatedKept k;
+        {
+            std::lock_guard<std::mutex> lk(mutex_);
+            X = x.unpack();
+            w = Weights{gate.unpack(), up.unpack(), down.unpack()};
+            k = kept;
+        }
+        std::array<bool, 4> need;
+        for (int i = 0; i < 4; ++i) need[i] = task_should_compute_output(i);
+        variable_list result;
+        {
+            at::AutoDispatchBelowADInplaceOrView below;
+            result = gated_backward(grads[0], X, w, act, k, need);
+        }
+        return once(std::move(result), "gated_feed_forward", {grads[0], X, w.gate, w.up, w.down});
+    }
+    std::string name() const override { return "GatedBackward"; }
+};
+
+Tensor gated(const Tensor& x, const Tensor& gate, const Tensor& up, const Tensor& down, int act) {
+    const Weights w{gate, up, down};
+    const bool train = at::GradMode::is_enabled() && (wants_grad(x) || wants_grad(gate) || wants_grad(up) || wants_grad(down));
+    GatedKept kept;
+    Tensor y;
+    {
+        at::AutoDispatchBelowADInplaceOrView below;
+        y = gated_forward(x, w, act, train, &kept);
+    }
+    if (train) {
+        auto node = std::shared_ptr<GatedBackward>(new GatedBackward(), torch::autograd::deleteNode);
+        node->act = act;
+        node->kept = std::move(kept);
+        node->x = SavedVariable(x, false);
+        node->gate = SavedVariable(gate, false);
+        node->up = SavedVariable(up, false);
+        node->down = SavedVariable(down, false);
+        node->set_next_edges(torch::autograd::collect_next_edges(x, gate, up, down));
+        torch::autograd::set_history(y, node);
+    }
+    return y;
+}
+
 }  // namespace
 
 void bind_layers(py::module_& mod) {
@@ -365,6 +518,20 @@ void bind_layers(py::module_& mod) {
                                              norm_args(groups, eps, act, offsets), w.has_value(), b.has_value());
                 auto some = [](const Tensor& t) { return t.defined() ? std::optional<Tensor>(t) : std::nullopt; };
                 return std::make_tuple(g[0], some(g[1]), some(g[2]));
+            }, release());
+    mod.def("gated", &gated, release());
+    mod.def("gated_forward", [](const Tensor& x, const Tensor& gate, const Tensor& up, const Tensor& down, int act) {
+        at::AutoDispatchBelowADInplaceOrView below;
+        GatedKept k;
+        const Tensor y = gated_forward(x, Weights{gate, up, down}, act, true, &k);
+        return std::make_tuple(y, k.u, k.v, k.a);
+    }, release());
+    mod.def("gated_backward",
+            [](const Tensor& dy, const Tensor& x, const Tensor& gate, const Tensor& up, const Tensor& down, int act, const Tensor& u,
+               const Tensor& v, const Tensor& a) {
+                at::AutoDispatchBelowADInplaceOrView below;
+                const auto g = gated_backward(dy, x, Weights{gate, up, down}, act, GatedKept{u, v, a}, {true, true, true, true});
+                return std::make_tuple(g[0], g[1], g[2], g[3]);
             }, release());
     mod.def("distill", &distill, release());
     mod.def("distill_forward", [](const Tensor& z, const Tensor& index, const Tensor& top, double temperature) {

@@ -1,6 +1,6 @@
-"""Layers that stand between the aggregations of a model of node features: group norm with an activation and the
-loss of a distillation from a teacher's best classes, each forward and backward in hand-written kernels
-(include/da_layers.h).
+"""Layers that stand between the aggregations of a model of node features: group norm with an activation, a gated
+feed-forward block and the loss of a distillation from a teacher's best classes, each forward and backward in
+hand-written kernels (include/da_layers.h).
 
 float32 and bfloat16.  Each is one operation forward and one backward, in C++ (csrc/native_layers.cpp); this module
 only checks and marshals arguments, and there is no fallback when the HIP library is missing (importing ``binding``
@@ -74,6 +74,49 @@ class GroupNorm(torch.nn.Module):
 
     def forward(self, x: torch.Tensor, offsets: torch.Tensor | None = None) -> torch.Tensor:
         return group_norm(x, self.groups, self.weight, self.bias, self.eps, self.activation, offsets)
+
+
+class _Gated(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, act):
+        y, *kept = _native.gated_forward(x, w_gate, w_up, w_down, act)
+        ctx.save_for_backward(x, w_gate, w_up, w_down, *kept)
+        ctx.act = act
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, w_gate, w_up, w_down, *kept = ctx.saved_tensors
+        return *_native.gated_backward(dy, x, w_gate, w_up, w_down, ctx.act, *kept), None
+
+
+def gated_feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+                       activation: str | None = "silu") -> torch.Tensor:
+    """(act(x . w_gate) * (x . w_up)) . w_down for x (..., d), w_gate and w_up (d, h), w_down (h, d_out), all float32 or all
+    bfloat16.  activation as for group_norm.  For the backward pass both projections are kept in float32 and their gated
+    product in the type of x."""
+    act = _activation(activation)
+    if _native.layers_take(x, w_gate, w_up, w_down):
+        return _native.gated(x, w_gate, w_up, w_down, act)
+    return _Gated.apply(x, w_gate, w_up, w_down, act)
+
+
+class GatedFeedForward(torch.nn.Module):
+    """gated_feed_forward with its weights, (in, out) like those of GraphConv."""
+
+    def __init__(self, features: int, hidden: int, out_features: int | None = None, activation: str | None = "silu"):
+        super().__init__()
+        _activation(activation)
+        self.activation = activation
+        self.w_gate = torch.nn.Parameter(torch.empty(features, hidden))
+        self.w_up = torch.nn.Parameter(torch.empty(features, hidden))
+        self.w_down = torch.nn.Parameter(torch.empty(hidden, features if out_features is None else out_features))
+        for w in (self.w_gate, self.w_up, self.w_down):
+            torch.nn.init.xavier_uniform_(w)
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        return gated_feed_forward(x, self.w_gate, self.w_up, self.w_down, self.activation)
 
 
 class _Distill(torch.autograd.Function):

@@ -1,0 +1,287 @@
+"""gated_feed_forward against its formula in 64 bits, forward and backward.
+
+Tolerances, with e = 2^-24 and r half a unit in the last place of the type at 1 (2^-24, or 2^-8 for bfloat16).
+Each number: a sum of products is off by at most 8 e sum|terms| (roundings of partial sums are independent and partial sums
+smaller than sum|terms|), an activation by 1.13 times its argument's error and 8 e (1 + |z|) of rounding, its derivative
+by the argument's error (no second derivative exceeds 1) and as much; a, du, dv and the results are rounded to the type
+once (r of their size).  These add up along the formula, signs dropped.
+All together: roundings are independent, so the norm of the error is at most 4 r of the result's (a result sees two
+or three of them), and for float32 that much times the square root of the longest sum."""
+import math
+
+import pytest
+import torch
+
+from paper_2202_08556_amd import layers
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+
+
+def act64(name, z):
+    F = torch.nn.functional
+    return {None: lambda t: t, "relu": torch.relu, "silu": F.silu, "gelu": F.gelu, "sigmoid": torch.sigmoid}[name](z)
+
+
+def formula(x, wg, wu, wd, act, dy):
+    """{name: (value, tolerance)} in 64 bits."""
+    r = 2.0 ** -8 if x.dtype == torch.bfloat16 else E
+    x, wg, wu, wd, dy = (t.detach().double() for t in (x, wg, wu, wd, dy))
+
+    def product(a, ta, b, tb=None):
+        """a . b and its tolerance, of factors with theirs"""
+        t = ta @ b.abs() + 8 * E * (a.abs() @ b.abs())
+        return a @ b, t if tb is None else t + a.abs() @ tb
+
+    zero = torch.zeros_like
+    u, tu = product(x, zero(x), wg)
+    v, tv = product(x, zero(x), wu)
+    with torch.enable_grad():
+        leaf = u.clone().requires_grad_(True)
+        s = act64(act, leaf)
+        slope, = torch.autograd.grad(s.sum(), leaf)
+        s = s.detach()
+    ts, tslope = 1.13 * tu + 8 * E * (1 + u.abs()), tu + 8 * E * (1 + u.abs())
+    a = s * v
+    ta = ts * v.abs() + s.abs() * tv + (r + 2 * E) * a.abs()
+    out = {"y": product(a, ta, wd)}
+    da, tda = product(dy, zero(dy), wd.t())
+    du = da * v * slope
+    tdu = tda * (v * slope).abs() + da.abs() * (tv * slope.abs() + v.abs() * tslope) + (r + 4 * E) * du.abs()
+    dv = da * s
+    tdv = tda * s.abs() + da.abs() * ts + (r + 2 * E) * dv.abs()
+    p, q = product(du, tdu, wg.t()), product(dv, tdv, wu.t())
+    out["dx"] = (p[0] + q[0], p[1] + q[1] + 8 * E * (du.abs() @ wg.t().abs() + dv.abs() @ wu.t().abs()))
+    out["dwg"] = product(x.t(), zero(x.t()), du, tdu)
+    out["dwu"] = product(x.t(), zero(x.t()), dv, tdv)
+    out["dwd"] = product(a.t(), ta.t(), dy)
+    return {k: (w, t + r * w.abs() + 2.0 ** -126) for k, (w, t) in out.items()}
+
+
+def compare(got, want, dtype, longest):
+    r = 2.0 ** -8 if dtype == torch.bfloat16 else E
+    for name, (value, tol) in want.items():
+        if got.get(name) is None:
+            continue
+        g = got[name].double().reshape(value.shape)
+        err = (g - value).abs()
+        assert (err <= tol).all(), f"{name}: {float((err / tol).max()):.3g} times the tolerance"
+        norm = float(value.norm())
+        off = float((g - value).norm())
+        share = 4 * r * (math.sqrt(longest) if dtype == torch.float32 else 1)
+        assert off <= share * norm + 1e-30, f"{name}: off by {off / norm:.3g} of its norm"
+
+
+def inputs(T, d, h, dout, dtype, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def normal(*shape, scale=1.0):
+        return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype)
+
+    return (normal(T, d), normal(d, h, scale=max(d, 1) ** -0.5), normal(d, h, scale=max(d, 1) ** -0.5),
+            normal(h, dout, scale=max(h, 1) ** -0.5), normal(T, dout))
+
+
+def run(x, wg, wu, wd, dy, act="silu"):
+    leaves = [t.detach().requires_grad_(True) for t in (x, wg, wu, wd)]
+    y = layers.gated_feed_forward(*leaves, activation=act)
+    assert y.shape == (*x.shape[:-1], wd.shape[1]) and y.dtype == x.dtype and y.is_contiguous()
+    grads = torch.autograd.grad(y, leaves, dy)
+    torch.cuda.synchronize()
+    got = dict(y=y.detach(), dx=grads[0], dwg=grads[1], dwu=grads[2], dwd=grads[3])
+    compare(got, formula(x.reshape(-1, x.shape[-1]), wg, wu, wd, act, dy.reshape(-1, wd.shape[1])), x.dtype,
+            max(x.numel() // max(x.shape[-1], 1), 2 * wg.shape[1], x.shape[-1], wd.shape[1]))
+    with torch.no_grad():
+        assert torch.equal(layers.gated_feed_forward(x, wg, wu, wd, activation=act), y)
+    return got
+
+
+# rows x d x h x d_out: one row, rows around the tiles of 16, 32, 64 and 128, widths that are no multiple of an access or
+# a tile, sums cut into parts (few tiles) and not, narrow results
+SIZES = [(1, 1, 1, 1), (1, 8, 8, 8), (1, 512, 1024, 512), (1, 1000, 777, 3), (2, 33, 65, 31), (15, 64, 128, 64), (16, 64, 64, 64),
+         (17, 130, 70, 128), (31, 256, 512, 40), (33, 100, 300, 100), (63, 72, 200, 72), (65, 602, 41, 602), (127, 96, 96, 96),
+         (128, 128, 64, 128), (129, 129, 129, 129), (300, 64, 256, 64), (1000, 20, 44, 20), (1531, 602, 1187, 602), (257, 1024, 520, 64),
+         (5000, 7, 13, 5), (100003, 16, 24, 16), (640, 512, 2048, 512), (3, 4096, 640, 4096), (2048, 256, 1024, 256), (1100, 1032, 1608, 1032)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,d,h,dout", SIZES)
+def test_sizes(T, d, h, dout, dtype):
+    print(f"gated {T}x{d}x{h}x{dout} {dtype}", flush=True)
+    run(*inputs(T, d, h, dout, dtype, seed=T + d))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("act", list(layers.ACTIVATIONS))
+@pytest.mark.parametrize("T", [5, 200])
+def test_activations(T, act, dtype):
+    x, wg, wu, wd, dy = inputs(T, 64, 96, 64, dtype, seed=1)
+    if act == "relu":                                        # whole numbers: no sum's rounding turns the slope over
+        x, wg = (x * 2).round(), (wg * 16).round() / 16
+    run(x, wg, wu, wd, dy, act)
+
+
+@pytest.mark.parametrize("shape", [(0, 16, 24, 16), (4, 0, 24, 16), (4, 16, 0, 16), (4, 16, 24, 0)], ids=str)
+def test_empty_sizes(shape):
+    x, wg, wu, wd, dy = inputs(*shape, torch.float32)
+    leaves = [t.requires_grad_(True) for t in (x, wg, wu, wd)]
+    y = layers.gated_feed_forward(*leaves)
+    grads = torch.autograd.grad(y, leaves, dy)
+    assert not y.any() and all(g.shape == t.shape and not g.any() for g, t in zip(grads, leaves))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 40, 700])
+def test_strides_shapes_and_odd_addresses(T, dtype):
+    x, wg, wu, wd, dy = inputs(T, 72, 136, 72, dtype, seed=2)
+    want = run(x, wg, wu, wd, dy)
+    wide = torch.full((T, 80), float("nan"), device="cuda", dtype=dtype)
+    wide[:, 3:75] = x
+    wide_dy = torch.full((T, 75), float("nan"), device="cuda", dtype=dtype)
+    wide_dy[:, 1:73] = dy
+    odd = [torch.empty(t.numel() + 1, device="cuda", dtype=dtype)[1:].view(t.shape).copy_(t) for t in (wg, wu, wd)]
+    turned = [t.t().contiguous().t() for t in (wg, wu, wd)]
+    for a, w, g in ((wide[:, 3:75], (wg, wu, wd), wide_dy[:, 1:73]), (x, odd, dy), (x.t().contiguous().t(), turned, dy)):
+        got = run(a, *w, g)
+        assert all(torch.equal(got[k], want[k]) for k in want)
+    got = run(x.view(T, 1, 72), wg, wu, wd, dy.view(T, 1, 72))
+    assert all(torch.equal(got[k].reshape(want[k].shape), want[k]) for k in want)
+    run(x, wg, wu, wd, dy[:1].expand(T, 72))
+    run(x[:1].expand(T, 72), wg, wu, wd, dy)
+    if T == 1:
+        y = layers.gated_feed_forward(x[0], wg, wu, wd)
+        assert y.shape == (72,) and torch.equal(y, want["y"][0])
+
+
+@pytest.mark.parametrize("T", [3, 300])
+def test_only_the_gradients_that_are_asked_for(T):
+    args = inputs(T, 64, 96, 64, torch.float32, seed=3)
+    want = run(*args)
+    names = ["dx", "dwg", "dwu", "dwd"]
+    for which in ([0], [1], [2], [3], [1, 2], [0, 3], [2, 3]):
+        leaves = [t.detach().requires_grad_(i in which) for i, t in enumerate(args[:4])]
+        y = layers.gated_feed_forward(*leaves)
+        for i, g in zip(which, torch.autograd.grad(y, [leaves[i] for i in which], args[4])):
+            assert torch.equal(g, want[names[i]])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [4, 40, 300])
+def test_bad_numbers_stay_in_their_rows(T, dtype):
+    x, wg, wu, wd, dy = inputs(T, 64, 96, 64, dtype, seed=4)
+    want = run(x, wg, wu, wd, dy)
+    for bad in (float("nan"), math.inf):
+        other = x.clone()
+        other[2, 7] = bad
+        y = layers.gated_feed_forward(other, wg, wu, wd)
+        keep = torch.arange(T, device="cuda") != 2
+        assert torch.equal(y[keep], want["y"][keep]) and not torch.isfinite(y[2]).any()
+
+
+def test_infinite_products_are_infinite():
+    """One infinite number in x and weights of one sign: u and v are infinite, not NaN, and so is y."""
+    x, wg, wu, wd, _ = inputs(5, 64, 96, 64, torch.float32, seed=5)
+    x[3, 9] = math.inf
+    y = layers.gated_feed_forward(x, wg.abs(), wu.abs(), wd.abs())
+    assert (y[3] == math.inf).all() and torch.isfinite(y[[0, 1, 2, 4]]).all()
+
+
+@pytest.mark.parametrize("T", [3, 300])
+def test_gradient_against_differences(T):
+    """Slope of sum(dy y) along a direction by central differences of step h: truncation 20 h^2 (third derivatives of order
+    1 in directions of size 1), rounding 64 e |y| / h, each for independent terms."""
+    x, wg, wu, wd, dy = inputs(T, 48, 80, 48, torch.float32, seed=6)
+    got = run(x, wg, wu, wd, dy)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    h = 2.0 ** -8
+    args = [x, wg, wu, wd]
+    for i, name in enumerate(("dx", "dwg", "dwu", "dwd")):
+        v = torch.randn(args[i].shape, generator=g, device="cuda") * (1.0 if i == 0 else args[i].shape[0] ** -0.5)
+        ends = []
+        for sign in (1, -1):
+            a = list(args)
+            a[i] = a[i] + sign * h * v
+            ends.append((layers.gated_feed_forward(*a).double() * dy.double()).sum())
+        slope, want = float((ends[0] - ends[1]) / (2 * h)), float((got[name].double() * v.double()).sum())
+        assert abs(slope - want) <= math.sqrt(dy.numel()) * (20 * h * h + 64 * E / h) * 4, (name, slope, want)
+
+
+def test_results_do_not_change_from_run_to_run():
+    for T, d, h in ((1, 512, 1024), (20000, 32, 48), (700, 200, 300)):
+        args = inputs(T, d, h, d, torch.bfloat16, seed=8)
+        first = run(*args)
+        for _ in range(3):
+            again = run(*args)
+            assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+def test_other_stream_and_graph():
+    cases = [inputs(1, 256, 512, 256, torch.bfloat16, seed=9), inputs(3000, 40, 72, 40, torch.float32, seed=9)]
+
+    def once(leaves):
+        out = []
+        for (x, wg, wu, wd), c in zip(leaves, cases):
+            y = layers.gated_feed_forward(x, wg, wu, wd)
+            out += [y.detach(), *torch.autograd.grad(y, (x, wg, wu, wd), c[4])]
+        return out
+
+    leaves = [[t.detach().requires_grad_(True) for t in c[:4]] for c in cases]
+    want = once(leaves)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = once(leaves)
+    s.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = once(leaves)
+    for k in range(4):
+        with torch.no_grad():
+            for c in leaves:
+                c[0].mul_(-0.7).add_(0.2 * k)
+        want = once(leaves)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), k
+
+
+def test_more_than_2_31_numbers_in_between():
+    """The last rows of an input whose hidden layer has 2^31 numbers and a few."""
+    T, d, h = 2 ** 20 + 130, 8, 2056
+    x, wg, wu, wd, _ = inputs(T, d, h, d, torch.bfloat16, seed=10)
+    y = layers.gated_feed_forward(x, wg, wu, wd)
+    tail = formula(x[-300:], wg, wu, wd, "silu", x[-300:])["y"]
+    compare({"y": y[-300:]}, {"y": tail}, torch.bfloat16, h)
+
+
+def test_module():
+    m = layers.GatedFeedForward(24, 40, 16, activation="gelu").cuda()
+    x = torch.randn(3, 7, 24, device="cuda")
+    assert torch.equal(m(x), layers.gated_feed_forward(x, m.w_gate, m.w_up, m.w_down, "gelu")) and m(x).shape == (3, 7, 16)
+    assert layers.GatedFeedForward(24, 40).w_down.shape == (40, 24)
+
+
+def test_refusals():
+    x, wg, wu, wd, _ = inputs(4, 16, 24, 16, torch.float32)
+    f = layers.gated_feed_forward
+    cases = [
+        (ValueError, lambda: f(x, wg, wu, wd, "swish")),
+        (ValueError, lambda: f(x[:, :8], wg, wu, wd)),
+        (ValueError, lambda: f(x, wg, wu[:, :8], wd)),
+        (ValueError, lambda: f(x, wg, wu, wd[:8])),
+        (ValueError, lambda: f(x, wg[0], wu, wd)),
+        (ValueError, lambda: f(x, wg.cpu(), wu, wd)),
+        (ValueError, lambda: f(x.cpu(), wg.cpu(), wu.cpu(), wd.cpu())),
+        (TypeError, lambda: f(x, wg.bfloat16(), wu, wd)),
+        (TypeError, lambda: f(x.half(), wg.half(), wu.half(), wd.half())),
+        (TypeError, lambda: f(x.double(), wg.double(), wu.double(), wd.double())),
+        (ValueError, lambda: layers.GatedFeedForward(4, 8, activation="swish")),
+    ]
+    for error, call in cases:
+        with pytest.raises(error):
+            call()
+    x.requires_grad_(True)
+    g, = torch.autograd.grad(f(x, wg, wu, wd).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiated again"):
+        g.sum().backward()
