@@ -253,21 +253,28 @@ __global__ __launch_bounds__(256) void gated_gemm_kernel(GemmArgs<T> g)
                     store4(g.U + at, left, x);
                     store4(g.V + at, left, v);
                 }
+                act_values(g.act, x);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) x[q] = act_value(g.act, x[q]) * v[q];
+                for (int q = 0; q < 4; ++q) x[q] *= v[q];
                 store4(g.C[0] + at, left, x);
             } else {
-                float du[4], dv[4];
+                float u[4] = {}, v[4] = {}, slope[4];
+                if (left >= 4) {
+                    load_floats<4>(g.U + at, u);
+                    load_floats<4>(g.V + at, v);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (q < left) { u[q] = g.U[at + q]; v[q] = g.V[at + q]; }
+                }
+                act_both(g.act, u, slope);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    float value;
-                    const float u = q < left ? g.U[at + q] : 0.f, v = q < left ? g.V[at + q] : 0.f;
-                    const float slope = act_slope(g.act, u, &value);
-                    du[q] = x[q] * v * slope;
-                    dv[q] = x[q] * value;
+                    v[q] *= x[q] * slope[q];
+                    x[q] *= u[q];
                 }
-                store4(g.C[0] + at, left, du);
-                store4(g.C[1] + at, left, dv);
+                store4(g.C[0] + at, left, v);
+                store4(g.C[1] + at, left, x);
             }
         }
     }
@@ -303,12 +310,14 @@ __global__ __launch_bounds__(256) void gated_join_kernel(GemmArgs<T> g)
             store_floats<1>((batch ? g.C[1] : g.C[0]) + at, one);
         } else if constexpr (EPI == kGate) {
             if (g.U) { g.U[at] = x; g.V[at] = v; }
-            const float one[1] = {act_value(g.act, x) * v};
+            float one[1] = {x};
+            act_values(g.act, one);
+            one[0] *= v;
             store_floats<1>(g.C[0] + at, one);
         } else {
-            float value;
-            const float slope = act_slope(g.act, g.U[at], &value);
-            const float du[1] = {x * g.V[at] * slope}, dv[1] = {x * value};
+            float u[1] = {g.U[at]}, slope[1];
+            act_both(g.act, u, slope);
+            const float du[1] = {x * g.V[at] * slope[0]}, dv[1] = {x * u[0]};
             store_floats<1>(g.C[0] + at, du);
             store_floats<1>(g.C[1] + at, dv);
         }

@@ -34,24 +34,24 @@ int pow2_at_least(int64_t x) {
 // ------------------------------------------------------------------------------------------
 // group norm
 // ------------------------------------------------------------------------------------------
+// Blocks of a launch: of 2^32 threads and more the high bits are lost
+constexpr int64_t kMaxBlocks = (1LL << 32) / 1024 - 1;
+
 struct NormPlan {
     int V;                   // numbers of an access: divides a group
-    // each
-    bool each;
+    bool each;               // every row is a sample and a group a few lanes' registers
     int P, E;
     int64_t each_grid;
-    // team
-    int team;                // threads of a team; 0: none
-    int GT;
-    int64_t team_grid, longest;
-    // split
+    int team, held;          // threads of a team (0: none), rows a thread holds
+    TeamPlan tp;
     bool split;
-    int TX;
-    int64_t per, per_sample, chunks, most_long;
-    bool table;
+    SplitPlan sp;
+    int64_t slots;
+    bool fits;               // the chunks are few enough to be counted in 32 bits
     // memory
-    size_t stats, part_bytes, table_at, list_at, forward, means_at, backward;
-    int64_t part_rows;
+    size_t stats;            // floats
+    int64_t col_rows;        // rows of 2 C sums: the first pass's blocks, then the chunks
+    size_t forward, table_at, part_at, means_at, backward;  // forward: part, table, stats; backward: sums, part, means, table
 };
 
 constexpr int64_t kNormMaxChannels = 1 << 20, kNormMaxGroups = 65535;
@@ -68,11 +68,13 @@ int norm_check(int dtype, int64_t rows, int64_t samples, int64_t channels, int64
 // Which kernels a shape takes.  train: statistics are kept and the backward pass is planned, too.
 NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_t C, int64_t G, bool train) {
     NormPlan p{};
+    p.fits = true;
     const int64_t cg = C / G, length = ragged || samples == 0 ? 0 : rows / samples;
     const int most = dtype == DA_F32 ? 4 : 8;
     p.V = 1;
     while (p.V < most && cg % (2 * p.V) == 0) p.V *= 2;
-    const int64_t cgv = cg / p.V, cv = C / p.V, cus = compute_units();
+    const int64_t cgv = cg / p.V, cus = compute_units();
+    int64_t first_rows = 0;
 
     if (!ragged && length == 1 && cgv * p.V <= 64 * 32) {
         int E = 1;
@@ -84,7 +86,7 @@ NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_
             const int64_t per_block = kNormBlock / p.P, m = G / std::gcd(G, per_block);
             const int64_t need = ceil_div(rows * G, per_block), cap = std::max<int64_t>(m, cus * 8 / m * m);
             p.each_grid = std::min(cap, ceil_div(need, m) * m);
-            p.part_rows = p.each_grid;
+            first_rows = p.each_grid;
         }
     }
     if (!p.each) {
@@ -97,62 +99,62 @@ NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_
             if (team == 1024 || (ragged ? 2 * mean : mean) <= (double)held(team)) { p.team = team; break; }
         }
         // A block takes up to a few times what its registers hold; longer samples are split.
-        p.longest = cgv > 1024 ? 0 : (ragged ? 4 : 2) * held(1024);
-        if (!ragged && length > p.longest) p.team = 0;
-        if (ragged && cgv > 1024) p.team = 0;
-        p.split = ragged ? rows > p.longest : length > p.longest;
+        const int64_t longest = (ragged ? 4 : 2) * held(1024);
+        if (!ragged && length > longest) p.team = 0;
+        p.split = ragged ? rows > longest : length > longest;
         if (p.team) {
-            p.GT = (int)tile(p.team);
             const int64_t teams = p.team == 64 ? 4 : 1, cap = train ? cus * (p.team == 1024 ? 2 : 8) : 1 << 20;
-            p.team_grid = std::min(ceil_div(samples, teams), cap);
-            p.part_rows = p.team_grid;
+            p.tp.GT = (int)tile(p.team);
+            // half as many registers where most samples need no more: two more blocks to a compute unit
+            // (and always in blocks of 1024 threads, which have 128 registers a thread)
+            p.held = p.team == 1024 || (ragged ? 1.5 * mean : mean) <= (double)held(p.team) / 2 ? E / 2 : E;
+            p.tp.tiles = (int)ceil_div(G, p.tp.GT);
+            p.tp.longest = longest;
+            p.tp.blocks = std::min(ceil_div(samples, teams), cap);
+            first_rows = p.tp.blocks;
         }
         if (p.split) {
-            p.TX = (int)std::min<int64_t>(cv, kNormBlock);
-            const int64_t TY = kNormBlock / p.TX;
-            const int64_t target = std::clamp<int64_t>(rows * C / (cus * 8), 4096, 65536);
-            p.per = std::max<int64_t>(ceil_div(target, C), 1);
-            p.per = ceil_div(p.per, TY) * TY;
-            if (ragged) {
-                p.table = true;
-                p.most_long = std::min(samples, rows / (p.longest + 1));
-                p.chunks = rows / p.per + p.most_long;
+            p.sp.longest = longest;
+            if (cgv <= kNormBlock) {
+                p.sp.gpt = (int)std::min<int64_t>(kNormBlock / cgv, G);
+                p.sp.pieces = 1;
+                p.sp.TX = (int)(p.sp.gpt * cgv);
+                p.sp.tiles = (int)ceil_div(G, p.sp.gpt);
             } else {
-                p.per_sample = ceil_div(length, p.per);
-                p.most_long = samples;
-                p.chunks = samples * p.per_sample;
+                p.sp.gpt = 1;
+                p.sp.pieces = (int)ceil_div(cgv, kNormBlock);
+                p.sp.TX = kNormBlock;
+                p.sp.tiles = (int)G * p.sp.pieces;
             }
+            const int64_t TY = kNormBlock / p.sp.TX;
+            const int64_t target = std::clamp<int64_t>(rows * C / (cus * 8), ragged ? 32768 : 4096, 65536);
+            p.sp.per = ceil_div(std::max<int64_t>(ceil_div(target, C), 1), TY) * TY;
+            int64_t chunks, each = 0;
+            if (ragged) {
+                p.sp.per = longest == 0 ? 1 : std::min(p.sp.per, longest);
+                chunks = ceil_div(rows, p.sp.per);
+                p.slots = p.sp.per == 1 ? chunks : 2 * chunks;
+            } else {
+                each = ceil_div(length, p.sp.per);
+                chunks = p.slots = samples * each;
+            }
+            p.fits = chunks <= kMaxBlocks;
+            p.sp.each = (int)std::min(each, kMaxBlocks);
+            p.sp.chunks = (int)std::min(chunks, kMaxBlocks);
+            p.sp.slots = p.slots;
         }
     }
-    p.stats = train || p.split ? (p.each ? 0 : (size_t)(samples * G * 2)) : 0;
-    // Forward: chunks' statistics; both: table.  Backward: sums of the blocks and chunks, means.
-    const size_t table = p.table ? 64 + round16((size_t)p.chunks * sizeof(int2)) + (size_t)p.most_long * sizeof(int4) : 0;
-    const size_t fpart = p.split ? round16((size_t)(p.chunks * cv) * sizeof(float2)) : 0;
-    p.forward = fpart + table + (train ? 0 : round16(p.stats * sizeof(float)));
-    p.part_bytes = round16((size_t)((p.part_rows + (p.split ? p.chunks : 0)) * 2 * C) * sizeof(float));
-    p.means_at = p.part_bytes + table;
-    p.backward = p.means_at + (p.split ? round16((size_t)(samples * G * 2) * sizeof(float)) : 0);
+    p.stats = p.each || !(train || p.split) ? 0 : (size_t)(samples * G * 2);
+    const size_t parts = p.split ? round16((size_t)(p.slots * G * p.sp.pieces) * sizeof(float2)) : 0;
+    const size_t table = p.split && ragged ? (size_t)p.sp.chunks * sizeof(ChunkEntry) : 0;
+    p.table_at = parts;
+    p.forward = parts + table + (train ? 0 : p.stats * sizeof(float));
+    p.col_rows = first_rows + p.sp.chunks;
+    p.part_at = round16((size_t)(p.col_rows * 2 * C) * sizeof(float));
+    p.means_at = p.part_at + parts;
+    const size_t means = p.split ? round16((size_t)(samples * G * 2) * sizeof(float)) : 0;
+    p.backward = p.means_at + means + table;
     return p;
-}
-
-NormChunks norm_chunks(const NormPlan& p, char* table) {
-    NormChunks ch{};
-    ch.per = p.per;
-    ch.each = p.per_sample;
-    ch.count = p.chunks;
-    if (p.table) {
-        ch.counts = reinterpret_cast<int*>(table);
-        ch.table = reinterpret_cast<int2*>(table + 64);
-        ch.list = reinterpret_cast<int4*>(table + 64 + round16((size_t)p.chunks * sizeof(int2)));
-    }
-    return ch;
-}
-
-void fill_table(const NormPlan& p, const NormShape& sh, const NormChunks& ch, hipStream_t s) {
-    if (!p.table) return;
-    hipLaunchKernelGGL(norm_clear_kernel, dim3(1), dim3(64), 0, s, const_cast<int*>(ch.counts));
-    hipLaunchKernelGGL(norm_long_kernel, dim3((unsigned)ceil_div(sh.samples, 256)), dim3(256), 0, s, sh, p.longest, p.per,
-                       const_cast<int*>(ch.counts), const_cast<int2*>(ch.table), const_cast<int4*>(ch.list));
 }
 
 template <class T, int V, bool BWD>
@@ -176,58 +178,63 @@ void launch_each(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx
     }
 }
 
+// Teams and chunks in one launch; teams of 1024 threads, whose blocks no chunk has, in one of their own
 template <class T, int V, bool BWD>
-void launch_team(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, const T* dy, int64_t ldy, T* out, float* stats,
-                 float* part, hipStream_t s) {
-    auto go = [&](auto kernel, int block) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)p.team_grid, (unsigned)ceil_div(sh.G, p.GT)), dim3(block), 0, s, sh, p.GT,
-                           p.longest, x, (long)ldx, dy, (long)ldy, out, stats, part);
+void launch_first(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, const T* dy, int64_t ldy, T* out, float* stats,
+                  float* team_cols, ChunkEntry* table, float2* part, float* cols, hipStream_t s) {
+    auto go = [&](auto kernel, int block, const TeamPlan& tp, int64_t chunks) {
+        const int64_t blocks = tp.blocks * tp.tiles + chunks * p.sp.tiles;
+        if (blocks)
+            hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(block), 0, s, sh, tp, p.sp, x, (long)ldx, dy, (long)ldy, out,
+                               stats, team_cols, table, part, cols);
     };
-    if (p.team == 64) go(norm_team_kernel<T, V, 64, BWD>, 256);
-    else if (p.team == 256) go(norm_team_kernel<T, V, 256, BWD>, 256);
-    else go(norm_team_kernel<T, V, 1024, BWD>, 1024);
+    const int64_t chunks = p.split ? p.sp.chunks : 0;
+    constexpr int E = V >= 8 ? 4 : 8;
+    auto held = [&](auto e) {
+        constexpr int H = decltype(e)::value;
+        if (p.team == 64 && chunks) go(norm_first_kernel<T, V, 64, H, true, BWD>, 256, p.tp, chunks);
+        else if (p.team == 64) go(norm_first_kernel<T, V, 64, H, false, BWD>, 256, p.tp, 0);
+        else if (chunks) go(norm_first_kernel<T, V, 256, H, true, BWD>, 256, p.tp, chunks);
+        else go(norm_first_kernel<T, V, 256, H, false, BWD>, 256, p.tp, 0);
+    };
+    if (p.team == 1024) go(norm_first_kernel<T, V, 1024, E / 2, false, BWD>, 1024, p.tp, 0);
+    if (p.team == 1024 || !p.team) go(norm_first_kernel<T, V, 256, 0, true, BWD>, 256, TeamPlan{}, chunks);
+    else if (p.held == E / 2) held(std::integral_constant<int, E / 2>{});
+    else held(std::integral_constant<int, E>{});
 }
 
 template <class T, int V>
 void norm_forward(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, T* y, float* stats, char* ws, hipStream_t s) {
-    if (p.each) return launch_each<T, V, false>(p, sh, x, ldx, nullptr, 0, y, nullptr, s);
-    if (p.team) launch_team<T, V, false>(p, sh, x, ldx, nullptr, 0, y, stats, nullptr, s);
-    if (!p.split) return;
-    const int cv = sh.C / V;
-    const NormChunks ch = norm_chunks(p, ws + round16((size_t)(p.chunks * cv) * sizeof(float2)));
-    fill_table(p, sh, ch, s);
-    const dim3 grid((unsigned)p.chunks, (unsigned)ceil_div(cv, p.TX));
+    const T* none = nullptr;
+    if (p.each) return launch_each<T, V, false>(p, sh, x, ldx, none, 0, y, nullptr, s);
     float2* part = reinterpret_cast<float2*>(ws);
-    hipLaunchKernelGGL((norm_stats_kernel<T, V>), grid, dim3(kNormBlock), 0, s, sh, ch, p.TX, x, (long)ldx, part);
-    hipLaunchKernelGGL((norm_join_kernel<V>), dim3((unsigned)p.most_long, (unsigned)sh.G), dim3(64), 0, s, sh, ch, part, stats);
-    hipLaunchKernelGGL((norm_apply_kernel<T, V, false>), grid, dim3(kNormBlock), 0, s, sh, ch, p.TX, x, (long)ldx,
-                       static_cast<const T*>(nullptr), 0L, stats, static_cast<const float*>(nullptr), y);
+    ChunkEntry* table = reinterpret_cast<ChunkEntry*>(ws + p.table_at);
+    launch_first<T, V, false>(p, sh, x, ldx, none, 0, y, stats, nullptr, table, part, nullptr, s);
+    if (!p.split) return;
+    const int64_t joins = sh.offsets ? p.sp.chunks : sh.samples;
+    hipLaunchKernelGGL((norm_join_kernel<V>), dim3((unsigned)joins, (unsigned)ceil_div(sh.G, kJoinGroups)), dim3(kJoinBlock), 0, s, sh, p.sp,
+                       table, part, stats);
+    hipLaunchKernelGGL((norm_apply_kernel<T, V, false>), dim3((unsigned)p.sp.chunks, (unsigned)p.sp.tiles), dim3(kNormBlock), 0, s, sh,
+                       p.sp, x, (long)ldx, none, 0L, stats, static_cast<const float*>(nullptr), table, y);
 }
 
 template <class T, int V>
 void norm_backward(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, const T* dy, int64_t ldy, const float* stats,
                    T* dx, void* dw, void* db, char* ws, hipStream_t s) {
-    float* part = reinterpret_cast<float*>(ws);
-    float* chunk_part = part + p.part_rows * 2 * sh.C;
-    NormChunks ch{};
-    if (p.each) launch_each<T, V, true>(p, sh, x, ldx, dy, ldy, dx, part, s);
-    if (p.team) launch_team<T, V, true>(p, sh, x, ldx, dy, ldy, dx, const_cast<float*>(stats), part, s);
-    if (p.split) {
-        ch = norm_chunks(p, ws + p.part_bytes);
-        float* means = reinterpret_cast<float*>(ws + p.means_at);
-        fill_table(p, sh, ch, s);
-        const dim3 grid((unsigned)p.chunks, (unsigned)ceil_div(sh.C / V, p.TX));
-        hipLaunchKernelGGL((norm_grad_stats_kernel<T, V>), grid, dim3(kNormBlock), 0, s, sh, ch, p.TX, x, (long)ldx, dy, (long)ldy,
-                           stats, chunk_part);
-        hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)p.most_long, (unsigned)sh.G), dim3(256), 0, s, sh, ch, chunk_part,
-                           means);
-        hipLaunchKernelGGL((norm_apply_kernel<T, V, true>), grid, dim3(kNormBlock), 0, s, sh, ch, p.TX, x, (long)ldx, dy, (long)ldy,
-                           stats, means, dx);
-    }
-    if (dw || db)
-        hipLaunchKernelGGL(norm_param_grads_kernel, dim3((unsigned)ceil_div(2 * sh.C, 64)), dim3(1024), 0, s, sh.C, part,
-                           (long)p.part_rows, chunk_part, p.split && !p.table ? (long)p.chunks : 0L,
-                           p.split && p.table ? ch.counts : static_cast<const int*>(nullptr), dw, db, sh.param_dtype);
+    float* cols = reinterpret_cast<float*>(ws);
+    float2* part = reinterpret_cast<float2*>(ws + p.part_at);
+    float* means = reinterpret_cast<float*>(ws + p.means_at);
+    ChunkEntry* table = reinterpret_cast<ChunkEntry*>(ws + p.backward - (sh.offsets ? p.sp.chunks * sizeof(ChunkEntry) : 0));
+    if (p.each) launch_each<T, V, true>(p, sh, x, ldx, dy, ldy, dx, cols, s);
+    else launch_first<T, V, true>(p, sh, x, ldx, dy, ldy, dx, const_cast<float*>(stats), cols, table, part, cols + p.tp.blocks * 2 * sh.C,
+                                  s);
+    const int64_t joins = !p.split ? 0 : (sh.offsets ? p.sp.chunks : sh.samples) * ceil_div(sh.G, kJoinGroups), sums = dw || db ? ceil_div(2 * sh.C, 16) : 0;
+    if (joins + sums)
+        hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)(joins + sums)), dim3(kJoinBlock), 0, s, sh, p.sp, (int)joins, table, part, means,
+                           cols, (long)p.col_rows, dw, db);
+    if (p.split)
+        hipLaunchKernelGGL((norm_apply_kernel<T, V, true>), dim3((unsigned)p.sp.chunks, (unsigned)p.sp.tiles), dim3(kNormBlock), 0, s,
+                           sh, p.sp, x, (long)ldx, dy, (long)ldy, stats, means, table, dx);
 }
 
 template <class F> void with_type_and_width(int dtype, int V, F&& f) {
@@ -257,6 +264,10 @@ int norm_shape(int dtype, int64_t rows, int64_t samples, const int32_t* offsets,
     *sh = NormShape{rows, samples, offsets, samples ? rows / samples : 0, (int)channels, (int)groups, (int)(channels / groups), eps,
                     act, param_dtype, w, b};
     return DA_OK;
+}
+
+bool norm_fits(const NormPlan& p, int64_t groups) {
+    return p.fits && p.sp.chunks * std::max<int64_t>(groups, p.sp.tiles) <= kMaxBlocks && p.tp.blocks * p.tp.tiles <= kMaxBlocks;
 }
 
 int workspace_error() {
@@ -291,9 +302,9 @@ extern "C" int da_group_norm(int dtype, int64_t rows, int64_t samples, const int
     if (!y) return fail(DA_ERR_INVALID_ARG, "null y");
     const NormPlan p = norm_plan(dtype, rows, samples, offsets != nullptr, channels, groups, stats != nullptr);
     if (p.forward && (!workspace || workspace_bytes < p.forward || !aligned16(workspace))) return workspace_error();
-    if (p.split && p.chunks > INT32_MAX) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    if (!norm_fits(p, groups)) return fail(DA_ERR_UNSUPPORTED, "size too large");
     char* ws = static_cast<char*>(workspace);
-    float* kept = stats ? stats : p.stats ? reinterpret_cast<float*>(ws + p.forward - round16(p.stats * sizeof(float))) : nullptr;
+    float* kept = stats ? stats : p.stats ? reinterpret_cast<float*>(ws + p.forward - p.stats * sizeof(float)) : nullptr;
     with_type_and_width(dtype, p.V, [&](auto t, auto v) {
         using T = decltype(t);
         norm_forward<T, decltype(v)::value>(p, sh, static_cast<const T*>(x), ldx, static_cast<T*>(y), kept, ws, (hipStream_t)stream);
@@ -312,10 +323,13 @@ extern "C" int da_group_norm_backward(int dtype, int64_t rows, int64_t samples, 
     if (channels == 0) return DA_OK;
     if (ldy < channels) return fail(DA_ERR_INVALID_ARG, "leading dimension smaller than the extent it strides over");
     if (rows > 0 && (!dy || !dx)) return fail(DA_ERR_INVALID_ARG, "null dy or dx");
-    const NormPlan p = rows > 0 ? norm_plan(dtype, rows, samples, offsets != nullptr, channels, groups, true) : NormPlan{1};
+    NormPlan p{};
+    p.V = 1;
+    p.fits = true;                                           // no rows: dw and db are sums of nothing
+    if (rows > 0) p = norm_plan(dtype, rows, samples, offsets != nullptr, channels, groups, true);
     if (p.stats && !stats) return fail(DA_ERR_INVALID_ARG, "null stats");
     if (p.backward && (!workspace || workspace_bytes < p.backward || !aligned16(workspace))) return workspace_error();
-    if (p.split && p.chunks > INT32_MAX) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    if (!norm_fits(p, groups)) return fail(DA_ERR_UNSUPPORTED, "size too large");
     with_type_and_width(dtype, p.V, [&](auto t, auto v) {
         using T = decltype(t);
         norm_backward<T, decltype(v)::value>(p, sh, static_cast<const T*>(x), ldx, static_cast<const T*>(dy), ldy, stats,

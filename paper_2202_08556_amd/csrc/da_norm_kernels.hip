@@ -58,6 +58,7 @@ __global__ __launch_bounds__(kNormBlock) void norm_each_kernel(NormShape sh, int
                                                                const T* __restrict__ dy, long ldy, T* __restrict__ out,
                                                                float* __restrict__ part)
 {
+    constexpr int U = E * V <= 8 ? (BWD ? 2 : 4) : E * V <= 16 ? 2 : 1;  // rows whose loads are in flight together
     __shared__ float sums[BWD ? 2 * kNormBlock * V * E : 1];
     const int lane = threadIdx.x & (P - 1), per_block = kNormBlock / P;
     const long first = (long)blockIdx.x * per_block + threadIdx.x / P;
@@ -73,65 +74,117 @@ __global__ __launch_bounds__(kNormBlock) void norm_each_kernel(NormShape sh, int
         on[e] = at < sh.cg;
         sh.params<V>(g * sh.cg + (on[e] ? at : 0), wv[e], bv[e]);
     }
-    for (long row = first / sh.G; row < sh.rows; row += step) {
-        float v[E][V], d[E][V];
-        float s = 0.f;
+    const int col = g * sh.cg + lane * V;
+    for (long row0 = first / sh.G; row0 < sh.rows; row0 += U * step) {
+        float v[U][E][V], d[BWD ? U : 1][E][V], mean[U], r[U];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int col = g * sh.cg + (lane + P * e) * V;
-            if (on[e]) {
-                load_floats<V>(x + row * ldx + col, v[e]);
-                if constexpr (BWD) load_floats<V>(dy + row * ldy + col, d[e]);
+        for (int u = 0; u < U; ++u) {
+            const long row = row0 + u * step;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool in = on[e] && row < sh.rows;
+                if (in) {
+                    load_floats<V>(x + row * ldx + col + P * e * V, v[u][e]);
+                    if constexpr (BWD) load_floats<V>(dy + row * ldy + col + P * e * V, d[u][e]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        v[u][e][i] = 0.f;
+                        if constexpr (BWD) d[u][e][i] = 0.f;
+                    }
+                }
             }
         }
 #pragma unroll
-        for (int e = 0; e < E; ++e)
+        for (int u = 0; u < U; ++u) {
+            float s = 0.f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) s += on[e] ? v[e][i] : 0.f;
-        const float mean = wave_sum(s, P) * inv;
-        s = 0.f;
+            for (int e = 0; e < E; ++e)
 #pragma unroll
-        for (int e = 0; e < E; ++e)
+                for (int i = 0; i < V; ++i) s += v[u][e][i];
+            mean[u] = s;
+        }
+        for (int k = 1; k < P; k <<= 1)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                v[e][i] -= mean;
-                s += on[e] ? v[e][i] * v[e][i] : 0.f;
-            }
-        const float r = 1.f / sqrtf(wave_sum(s, P) * inv + sh.eps);
-        if constexpr (!BWD) {
+            for (int u = 0; u < U; ++u) mean[u] += __shfl_xor(mean[u], k, 64);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (!on[e]) continue;
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[e][i] = act_value(sh.act, v[e][i] * r * wv[e][i] + bv[e][i]);
-                store_floats<V>(out + row * sh.C + g * sh.cg + (lane + P * e) * V, v[e]);
-            }
-        } else {
-            float s1 = 0.f, s2 = 0.f;
+        for (int u = 0; u < U; ++u) {
+            mean[u] *= inv;
+            float s = 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if (!on[e]) continue;
+                const float m = on[e] ? mean[u] : 0.f;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    float value;
-                    const float xh = v[e][i] * r;
-                    const float dz = d[e][i] * act_slope(sh.act, xh * wv[e][i] + bv[e][i], &value);
-                    aw[e][i] += dz * xh;
-                    ab[e][i] += dz;
-                    d[e][i] = dz * wv[e][i];
-                    v[e][i] = xh;
-                    s1 += d[e][i];
-                    s2 += d[e][i] * xh;
+                    v[u][e][i] -= m;
+                    s += v[u][e][i] * v[u][e][i];
                 }
             }
-            s1 = wave_sum(s1, P) * inv;
-            s2 = wave_sum(s2, P) * inv;
+            r[u] = s;
+        }
+        for (int k = 1; k < P; k <<= 1)
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (!on[e]) continue;
+            for (int u = 0; u < U; ++u) r[u] += __shfl_xor(r[u], k, 64);
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[e][i] = r * (d[e][i] - s1 - v[e][i] * s2);
-                store_floats<V>(out + row * sh.C + g * sh.cg + (lane + P * e) * V, v[e]);
+        for (int u = 0; u < U; ++u) r[u] = __builtin_amdgcn_rsqf(r[u] * inv + sh.eps);
+        if constexpr (!BWD) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long row = row0 + u * step;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if (!on[e] || row >= sh.rows) continue;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[u][e][i] = v[u][e][i] * r[u] * wv[e][i] + bv[e][i];
+                    act_values(sh.act, v[u][e]);
+                    store_floats<V>(out + row * sh.C + col + P * e * V, v[u][e]);
+                }
+            }
+        } else {
+            float s1[U], s2[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                s1[u] = s2[u] = 0.f;
+                if (row0 + u * step >= sh.rows) continue;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if (!on[e]) continue;
+                    float z[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        v[u][e][i] *= r[u];
+                        z[i] = v[u][e][i] * wv[e][i] + bv[e][i];
+                    }
+                    act_slopes(sh.act, z);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float xh = v[u][e][i], dz = d[u][e][i] * z[i];
+                        aw[e][i] += dz * xh;
+                        ab[e][i] += dz;
+                        d[u][e][i] = dz * wv[e][i];
+                        s1[u] += d[u][e][i];
+                        s2[u] += d[u][e][i] * xh;
+                    }
+                }
+            }
+            for (int k = 1; k < P; k <<= 1)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    s1[u] += __shfl_xor(s1[u], k, 64);
+                    s2[u] += __shfl_xor(s2[u], k, 64);
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long row = row0 + u * step;
+                s1[u] *= inv;
+                s2[u] *= inv;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if (!on[e] || row >= sh.rows) continue;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[u][e][i] = r[u] * (d[u][e][i] - s1[u] - v[u][e][i] * s2[u]);
+                    store_floats<V>(out + row * sh.C + col + P * e * V, v[u][e]);
+                }
             }
         }
     }
@@ -159,12 +212,13 @@ __global__ __launch_bounds__(kNormBlock) void norm_each_kernel(NormShape sh, int
 }
 
 // ------------------------------------------------------------------------------------------
-// team: TEAM threads own a sample's GT groups (blockIdx.y says which), TX = GT cg / V of them side by side along the
-// columns, the others along the rows, kTeamRows rows a thread in registers; rows beyond that are read again.
+// team: TEAM threads own a sample's GT groups (`tile` says which), TX = GT cg / V of them side by side along the
+// columns, the others along the rows, E rows a thread in registers; rows beyond that are read again.
 // stats: mean and r of every sample and group, written forward and read backward.
 // Samples of more than `longest` rows are left to the split kernels.
 // ------------------------------------------------------------------------------------------
-template <int V> constexpr int team_rows() { return V >= 8 ? 4 : 8; }
+// Sum of squares about the mean from b = sum c^2, a = sum c and a / n; NaN and infinities stay visible.
+__device__ __forceinline__ float variance(float b, float a, float m) { return fmaxf(b - a * m, 0.f) + (b - b); }
 
 template <int TEAM> __device__ __forceinline__ void team_sync() {
     if constexpr (TEAM == 64) {
@@ -176,19 +230,25 @@ template <int TEAM> __device__ __forceinline__ void team_sync() {
     }
 }
 
-template <class T, int V, int TEAM, bool BWD>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_team_kernel(
-    NormShape sh, int GT, long longest, const T* __restrict__ x, long ldx, const T* __restrict__ dy, long ldy,
-    T* __restrict__ out, float* __restrict__ stats, float* __restrict__ part)
+struct TeamPlan {
+    int GT, tiles;               // groups of a tile, tiles of a sample
+    long blocks;                 // blocks of a tile
+    long longest;
+};
+
+template <class T, int V, int TEAM, int E, bool BWD>
+__device__ __forceinline__ void norm_team(const NormShape& sh, const TeamPlan& tp, long block, int tile, const T* __restrict__ x,
+                                          long ldx, const T* __restrict__ dy, long ldy, T* __restrict__ out,
+                                          float* __restrict__ stats, float* __restrict__ part)
 {
-    constexpr int BLOCK = TEAM < 256 ? 256 : TEAM, TEAMS = BLOCK / TEAM, E = team_rows<V>();
+    constexpr int BLOCK = TEAM < 256 ? 256 : TEAM, TEAMS = BLOCK / TEAM;
     __shared__ float red_mem[TEAMS][2][TEAM], tot_mem[TEAMS][2][TEAM];
-    const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM;
+    const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, GT = tp.GT;
     float (&red)[2][TEAM] = red_mem[team];
     float (&tot)[2][TEAM] = tot_mem[team];
     const int cgv = sh.cg / V, TX = GT * cgv, TY = TEAM / TX;
     const int tx = t % TX, ty = t / TX;
-    const int g0 = blockIdx.y * GT, gn = min(GT, sh.G - g0);
+    const int g0 = tile * GT, gn = min(GT, sh.G - g0);
     const bool on = ty < TY && tx < gn * cgv;
     const int col = g0 * sh.cg + tx * V, g = g0 + tx / cgv;
 
@@ -217,10 +277,12 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_team_kernel(
 
     float wv[V], bv[V], aw[V] = {}, ab[V] = {};
     sh.params<V>(on ? col : 0, wv, bv);
-    for (long s = (long)blockIdx.x * TEAMS + team; s < sh.samples; s += (long)gridDim.x * TEAMS) {
-        long r0, r1;
-        sh.range(s, &r0, &r1);
-        const int n = r1 - r0 > longest ? 0 : (int)(r1 - r0);
+    long s = block * TEAMS + team, next0 = 0, next1 = 0;
+    if (s < sh.samples) sh.range(s, &next0, &next1);
+    for (; s < sh.samples; s += tp.blocks * TEAMS) {
+        const long r0 = next0, r1 = next1;
+        if (s + tp.blocks * TEAMS < sh.samples) sh.range(s + tp.blocks * TEAMS, &next0, &next1);     // in flight beside the rows
+        const int n = r1 - r0 > tp.longest ? 0 : (int)(r1 - r0);
         if (n == 0) continue;                                // the whole team's
         const float inv = 1.f / ((float)n * (float)sh.cg);
         const T* __restrict__ xp = x + r0 * ldx + col;
@@ -239,51 +301,39 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_team_kernel(
         }
         const int rest = ty + TY * E;                        // first row that is not in registers
         if constexpr (!BWD) {
-            float a = 0.f, b = 0.f;
+            float a = 0.f, b = 0.f, shift = 0.f;
             if (on) {
+                float first[1];
+                load_floats<1>(x + r0 * ldx + (long)g * sh.cg, first);
+                shift = first[0];
+                auto add = [&](const float (&u)[V]) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) { const float c = u[i] - shift; a += c; b += c * c; }
+                };
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (ty + TY * e < n)
-#pragma unroll
-                        for (int i = 0; i < V; ++i) a += v[e][i];
+                    if (ty + TY * e < n) add(v[e]);
                 for (int row = rest; row < n; row += TY) {
                     float u[V];
                     load_floats<V>(xp + (long)row * ldx, u);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) a += u[i];
+                    add(u);
                 }
             }
             join(a, b);
-            const float mean = a * inv;
-            a = 0.f;
-            if (on) {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (ty + TY * e < n)
-#pragma unroll
-                        for (int i = 0; i < V; ++i) { v[e][i] -= mean; a += v[e][i] * v[e][i]; }
-                for (int row = rest; row < n; row += TY) {
-                    float u[V];
-                    load_floats<V>(xp + (long)row * ldx, u);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) { u[i] -= mean; a += u[i] * u[i]; }
-                }
+            const float m = a * inv, mean = shift + m;
+            const float r = __builtin_amdgcn_rsqf(variance(b, a, m) * inv + sh.eps);
+            if (stats && on && ty == 0 && tx % cgv == 0) {
+                stats[(s * sh.G + g) * 2] = mean;
+                stats[(s * sh.G + g) * 2 + 1] = r;
             }
-            join(a, b);
-            const float r = 1.f / sqrtf(a * inv + sh.eps);
-            if (stats && t < gn) {
-                float q = 0.f;
-                q = tot[0][t];
-                stats[(s * sh.G + g0 + t) * 2 + 1] = 1.f / sqrtf(q * inv + sh.eps);
-            }
-            if (stats && on && ty == 0 && tx % cgv == 0) stats[(s * sh.G + g) * 2] = mean;
             if (on) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const int row = ty + TY * e;
                     if (row < n) {
 #pragma unroll
-                        for (int i = 0; i < V; ++i) v[e][i] = act_value(sh.act, v[e][i] * r * wv[i] + bv[i]);
+                        for (int i = 0; i < V; ++i) v[e][i] = (v[e][i] - mean) * r * wv[i] + bv[i];
+                        act_values(sh.act, v[e]);
                         store_floats<V>(op + (long)row * sh.C, v[e]);
                     }
                 }
@@ -291,19 +341,24 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_team_kernel(
                     float u[V];
                     load_floats<V>(xp + (long)row * ldx, u);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) u[i] = act_value(sh.act, (u[i] - mean) * r * wv[i] + bv[i]);
+                    for (int i = 0; i < V; ++i) u[i] = (u[i] - mean) * r * wv[i] + bv[i];
+                    act_values(sh.act, u);
                     store_floats<V>(op + (long)row * sh.C, u);
                 }
             }
         } else {
             float s1 = 0.f, s2 = 0.f, mean = 0.f, r = 0.f;
             auto step = [&](float (&u)[V], float (&dd)[V]) {     // x and dy become xh and e
+                float z[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    float value;
-                    const float xh = (u[i] - mean) * r;
-                    const float dz = dd[i] * act_slope(sh.act, xh * wv[i] + bv[i], &value);
-                    u[i] = xh;
+                    u[i] = (u[i] - mean) * r;
+                    z[i] = u[i] * wv[i] + bv[i];
+                }
+                act_slopes(sh.act, z);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float xh = u[i], dz = dd[i] * z[i];
                     dd[i] = dz * wv[i];
                     aw[i] += dz * xh;
                     ab[i] += dz;
@@ -340,13 +395,15 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_team_kernel(
                     float u[V], dd[V];
                     load_floats<V>(xp + (long)row * ldx, u);
                     load_floats<V>(dp + (long)row * ldy, dd);
+                    float z[V];
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        float value;
-                        const float xh = (u[i] - mean) * r;
-                        const float e = dd[i] * act_slope(sh.act, xh * wv[i] + bv[i], &value) * wv[i];
-                        u[i] = r * (e - m1 - xh * m2);
+                        u[i] = (u[i] - mean) * r;
+                        z[i] = u[i] * wv[i] + bv[i];
                     }
+                    act_slopes(sh.act, z);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) u[i] = r * (dd[i] * z[i] * wv[i] - m1 - u[i] * m2);
                     store_floats<V>(op + (long)row * sh.C, u);
                 }
             }
@@ -363,334 +420,490 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_team_kernel(
                 float p = 0.f, q = 0.f;
                 for (int m = 0; m < TEAMS; ++m)
                     for (int k = 0; k < TY; ++k) { p += red_mem[m][0][t + k * TX]; q += red_mem[m][1][t + k * TX]; }
-                part[(long)blockIdx.x * 2 * sh.C + col + i] = p;
-                part[(long)blockIdx.x * 2 * sh.C + sh.C + col + i] = q;
+                part[block * 2 * sh.C + col + i] = p;
+                part[block * 2 * sh.C + sh.C + col + i] = q;
             }
         }
     }
 }
 
 // ------------------------------------------------------------------------------------------
-// split: chunks of `per` rows of one sample.  Ragged samples' chunks come from a table that norm_long_kernel fills
-// with the samples of more than `longest` rows (in any order: nothing is summed in the order of the table).
+// split: chunks of `per` rows, one block each (and column tile).  Equal samples are cut one by one.  Ragged ones are cut
+// together, every `per` rows: a chunk has parts of at most two samples of more than `longest` >= per rows, the one that its
+// first row belongs to (slot 2 c) and the one that its last row belongs to (slot 2 c + 1); the others are the teams'.
+// With per == 1 (groups too wide for a team) every sample is split, and a chunk has one slot.
+// A column tile is whole groups, or a piece of one.
 // ------------------------------------------------------------------------------------------
-struct NormChunks {
-    long per, each, count;       // rows of a chunk; chunks of a sample of equal samples; chunks (the most, where ragged)
-    const int2* table;           // ragged: sample and number within the sample of a chunk; null: equal samples
-    const int* counts;           // ragged: chunks, long samples
-    const int4* list;            // ragged: sample, its first chunk, its chunks
+struct SplitPlan {
+    int each, chunks;            // chunks of a sample of equal samples; chunks
+    long slots;                  // parts of a group (piece): part[group or piece][slot], which a joining wave reads side by side
+    long per, longest;           // rows of a chunk
+    int gpt, pieces, tiles;      // groups of a tile, tiles of a group (one of the two is 1), tiles
+    int TX;                      // accesses side by side in a tile
+};
 
-    __device__ bool find(const NormShape& sh, long c, long* s, long* r0, long* r1) const {
-        long i;
-        if (table) {
-            if (c >= counts[0]) return false;
-            const int2 e = table[c];
-            *s = e.x;
-            i = e.y;
-        } else {
-            *s = c / each;
-            i = c % each;
-        }
-        long a, e;
-        sh.range(*s, &a, &e);
-        *r0 = a + i * per;
-        *r1 = min(*r0 + per, e);
-        return true;
+// the k-th V numbers of an array
+template <int V, int N> __device__ __forceinline__ float (&part_of(float (&x)[N], int k))[V] {
+    return *reinterpret_cast<float (*)[V]>(x + k * V);
+}
+
+struct Segment { long s, r0, r1, slot; };
+
+// A chunk of ragged samples: its parts (s < 0: none).  The first pass finds them and the later ones read them.
+struct ChunkEntry { Segment seg[2]; };
+
+struct ColumnTile { int g0, gn, vec0, width; };              // groups; accesses
+
+template <int V> __device__ __forceinline__ ColumnTile column_tile(const NormShape& sh, const SplitPlan& sp, int tile) {
+    const int cgv = sh.cg / V;
+    if (sp.pieces == 1) {
+        const int g0 = tile * sp.gpt, gn = min(sp.gpt, sh.G - g0);
+        return ColumnTile{g0, gn, g0 * cgv, gn * cgv};
     }
-    // the k-th sample's number, first chunk and chunks
-    __device__ bool sample(long k, long* s, long* first, long* n) const {
-        if (table) {
-            if (k >= counts[1]) return false;
-            const int4 e = list[k];
-            *s = e.x;
-            *first = e.y;
-            *n = e.z;
-        } else {
-            *s = k;
-            *first = k * each;
-            *n = each;
-        }
-        return true;
+    const int g = tile / sp.pieces, from = tile % sp.pieces * sp.TX;
+    return ColumnTile{g, 1, g * cgv + from, min(sp.TX, cgv - from)};
+}
+
+// Last sample that begins at `row` or before: a wave looks at 64 offsets at a time (8000 samples take 3 dependent loads,
+// one offset at a time 13).  All lanes of the wave take part.
+__device__ __forceinline__ long sample_of(const NormShape& sh, long row) {
+    long lo = 0, hi = sh.samples - 1;
+    const int lane = threadIdx.x & 63;
+    while (lo < hi) {
+        const long step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step;
+        const bool before = at <= hi && sh.offsets[at] <= row;
+        lo += __popcll(__ballot(before)) * step;
+        hi = min(lo + step - 1, hi);
+    }
+    return lo;
+}
+
+// The parts of a chunk that are to be computed
+__device__ __forceinline__ void segments_of(const NormShape& sh, const SplitPlan& sp, int c, Segment (&out)[2], ChunkEntry* table,
+                                            bool first_pass) {
+    out[0].s = out[1].s = -1;
+    if (!sh.offsets) {
+        const int s = c / sp.each;
+        const long r0 = s * sh.length + c % sp.each * sp.per;
+        out[0] = Segment{s, r0, min(r0 + sp.per, (s + 1) * sh.length), c};
+        return;
+    }
+    if (!first_pass) {
+        out[0] = table[c].seg[0];
+        out[1] = table[c].seg[1];
+        return;
+    }
+    const long a = c * sp.per, e = min(a + sp.per, sh.rows);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        if (q && sp.per == 1) break;
+        const long s = sample_of(sh, q ? e - 1 : a);
+        long r0, r1;
+        sh.range(s, &r0, &r1);
+        if (r1 - r0 > sp.longest && r0 < e && r1 > a && (q ? s != out[0].s : r0 <= a))
+            out[q] = Segment{s, max(r0, a), min(r1, e), sp.per == 1 ? c : 2 * c + q};
+    }
+    if (threadIdx.x == 0) {                                  // by all column tiles alike
+        table[c].seg[0] = out[0];
+        table[c].seg[1] = out[1];
+    }
+}
+
+// A sample's parts, in order: slot and rows of the k-th
+struct Parts {
+    int first, n;                // first chunk, chunks
+    long r0, r1, per;
+    bool ragged, late;           // late: begins inside its first chunk
+
+    __device__ long slot(int k) const { return !ragged || per == 1 ? first + k : 2 * (first + k) + (k == 0 && late ? 1 : 0); }
+    __device__ long rows(int k) const {
+        if (!ragged) return min(per, r1 - r0 - k * per);
+        const long a = (first + k) * per;
+        return min(r1, a + per) - max(r0, a);
     }
 };
 
-__global__ __launch_bounds__(64) void norm_clear_kernel(int* counts) {
-    if (threadIdx.x < 2) counts[threadIdx.x] = 0;
+// The sample that block k of the joining kernels is to join, if any: equal samples by number, a ragged one by the chunk
+// in which it begins (two may begin in one chunk only where the first is no long one).
+__device__ __forceinline__ bool sample_to_join(const NormShape& sh, const SplitPlan& sp, int k, const ChunkEntry* table, long* s,
+                                               Parts* p) {
+    if (!sh.offsets) {
+        *s = k;
+        *p = Parts{k * sp.each, sp.each, k * sh.length, (k + 1) * sh.length, sp.per, false, false};
+        return true;
+    }
+    const long a = k * sp.per;
+    for (int q = 0; q < 2; ++q) {
+        *s = table[k].seg[q].s;
+        if (*s < 0) continue;
+        long r0, r1;
+        sh.range(*s, &r0, &r1);
+        if (r0 < a) continue;
+        *p = Parts{k, (int)((r1 - 1) / sp.per) - k + 1, r0, r1, sp.per, true, r0 > a};
+        return true;
+    }
+    return false;
 }
 
-__global__ __launch_bounds__(256) void norm_long_kernel(NormShape sh, long longest, long per, int* counts, int2* table,
-                                                        int4* list)
-{
-    const long s = (long)blockIdx.x * 256 + threadIdx.x;
-    long r0 = 0, r1 = 0;
-    if (s < sh.samples) sh.range(s, &r0, &r1);
-    const bool is_long = r1 - r0 > longest;
-    int n = 0, first = 0;
-    if (is_long) {
-        n = (int)((r1 - r0 + per - 1) / per);
-        first = atomicAdd(&counts[0], n);
-        list[atomicAdd(&counts[1], 1)] = make_int4((int)s, first, n, 0);
-    }
-    for (unsigned long long left = __ballot(is_long); left; left &= left - 1) {
-        const int who = __ffsll(left) - 1;
-        const int m = __shfl(n, who), f = __shfl(first, who), sample = __shfl((int)s, who);
-        for (int i = threadIdx.x & 63; i < m; i += 64) table[f + i] = make_int2(sample, i);
-    }
-}
-
-// mean and sum of squares about it of a chunk's columns, V columns together
-template <class T, int V>
-__global__ __launch_bounds__(kNormBlock) void norm_stats_kernel(NormShape sh, NormChunks ch, int TX, const T* __restrict__ x,
-                                                                long ldx, float2* __restrict__ part)
-{
-    __shared__ float red[2][kNormBlock];
-    long s, r0, r1;
-    if (!ch.find(sh, blockIdx.x, &s, &r0, &r1)) return;
-    const int TY = kNormBlock / TX, t = threadIdx.x, tx = t % TX, ty = t / TX, cv = sh.C / V;
-    const int vec = blockIdx.y * TX + tx;
-    const bool on = ty < TY && vec < cv;
-    const T* __restrict__ xp = x + (long)vec * V;
-    float a = 0.f, b = 0.f, shift = 0.f;
-    if (on) {
-        float u[V];
-        load_floats<V>(xp + r0 * ldx, u);
-        shift = u[0];
-        constexpr int U = 4;
-        long row = r0 + ty;
-        for (; row + (U - 1) * TY < r1; row += U * TY) {
-            float m[U][V];
-#pragma unroll
-            for (int k = 0; k < U; ++k) load_floats<V>(xp + (row + k * TY) * ldx, m[k]);
-#pragma unroll
-            for (int k = 0; k < U; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) { const float c = m[k][i] - shift; a += c; b += c * c; }
-        }
-        for (; row < r1; row += TY) {
-            load_floats<V>(xp + row * ldx, u);
-#pragma unroll
-            for (int i = 0; i < V; ++i) { const float c = u[i] - shift; a += c; b += c * c; }
-        }
-    }
+// Sums of two numbers over the threads of a block that share a group (gn == 1: over all), left in red[.][group]
+__device__ __forceinline__ void join_groups(float (&red)[2][kNormBlock], float a, float b, int TX, int TY, int cgv, int gn) {
+    const int t = threadIdx.x;
+    __syncthreads();
     red[0][t] = a;
     red[1][t] = b;
     __syncthreads();
-    if (t < TX && vec < cv) {
+    if (t < TX) {
         for (int k = 1; k < TY; ++k) { a += red[0][t + k * TX]; b += red[1][t + k * TX]; }
-        const float n = (float)(r1 - r0) * V, m = a / n;
-        part[(long)blockIdx.x * cv + vec] = make_float2(shift + m, fmaxf(b - a * m, 0.f) + (b - b));   // NaN stays NaN
+        red[0][t] = a;
+        red[1][t] = b;
+    }
+    __syncthreads();
+    const int width = gn == 1 ? TX : cgv;
+    if (gn == 1 && t < 64) {                                 // up to 256 numbers: a wave
+        a = b = 0.f;
+        for (int k = t; k < width; k += 64) { a += red[0][k]; b += red[1][k]; }
+        a = wave_sum(a, 64);
+        b = wave_sum(b, 64);
+    } else if (gn > 1 && t < gn) {
+        a = b = 0.f;
+        for (int k = 0; k < width; ++k) { a += red[0][t * width + k]; b += red[1][t * width + k]; }
+    }
+    __syncthreads();
+    if (t < gn) {
+        red[0][t] = a;
+        red[1][t] = b;
     }
 }
 
-// Joins a sample's parts: one wave for a sample and group
-template <int V>
-__global__ __launch_bounds__(64) void norm_join_kernel(NormShape sh, NormChunks ch, const float2* __restrict__ part,
-                                                       float* __restrict__ stats)
-{
-    long s, first, chunks, r0, r1;
-    if (!ch.sample(blockIdx.x, &s, &first, &chunks)) return;
-    sh.range(s, &r0, &r1);
-    const int g = blockIdx.y, cgv = sh.cg / V, cv = sh.C / V;
-    const long parts = chunks * cgv;
-    const float total = (float)(r1 - r0) * (float)sh.cg;
-    auto at = [&](long k, float* n) {
-        const long c = k / cgv;
-        const long rows = min(ch.per, (r1 - r0) - c * ch.per);
-        *n = (float)rows * V;
-        return part[(first + c) * cv + g * cgv + k % cgv];
-    };
-    float a = 0.f, n;
-    const float origin = at(0, &n).x;
-    for (long k = threadIdx.x; k < parts; k += 64) { const float2 p = at(k, &n); a += (p.x - origin) * n; }
-    const float mean = origin + wave_sum(a, 64) / total;
-    float m2 = 0.f;
-    for (long k = threadIdx.x; k < parts; k += 64) {
-        const float2 p = at(k, &n);
-        m2 += p.y + n * (p.x - mean) * (p.x - mean);
-    }
-    m2 = wave_sum(m2, 64);
-    if (threadIdx.x == 0) {
-        stats[(s * sh.G + g) * 2] = mean;
-        stats[(s * sh.G + g) * 2 + 1] = 1.f / sqrtf(m2 / total + sh.eps);
-    }
-}
-
-// y of a chunk; BWD: dx, with the means of e and e xh of every sample and group in `means`
-template <class T, int V, bool BWD>
-__global__ __launch_bounds__(kNormBlock) void norm_apply_kernel(NormShape sh, NormChunks ch, int TX, const T* __restrict__ x,
-                                                                long ldx, const T* __restrict__ dy, long ldy,
-                                                                const float* __restrict__ stats,
-                                                                const float* __restrict__ means, T* __restrict__ out)
-{
-    long s, r0, r1;
-    if (!ch.find(sh, blockIdx.x, &s, &r0, &r1)) return;
-    const int TY = kNormBlock / TX, tx = threadIdx.x % TX, ty = threadIdx.x / TX;
-    const int vec = blockIdx.y * TX + tx;
-    if (ty >= TY || vec >= sh.C / V) return;
-    const int col = vec * V, g = col / sh.cg;
-    float wv[V], bv[V];
-    sh.params<V>(col, wv, bv);
-    const float mean = stats[(s * sh.G + g) * 2], r = stats[(s * sh.G + g) * 2 + 1];
-    float m1 = 0.f, m2 = 0.f;
-    if constexpr (BWD) {
-        m1 = means[(s * sh.G + g) * 2];
-        m2 = means[(s * sh.G + g) * 2 + 1];
-    }
-    constexpr int U = 2;
-    auto put = [&](long row, float (&u)[V], float (&d)[V]) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float xh = (u[i] - mean) * r, z = xh * wv[i] + bv[i];
-            if constexpr (!BWD) {
-                u[i] = act_value(sh.act, z);
-            } else {
-                float value;
-                u[i] = r * (d[i] * act_slope(sh.act, z, &value) * wv[i] - m1 - xh * m2);
-            }
-        }
-        store_floats<V>(out + row * sh.C + col, u);
-    };
-    long row = r0 + ty;
-    for (; row + (U - 1) * TY < r1; row += U * TY) {
-        float u[U][V], d[U][V];
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            load_floats<V>(x + (row + k * TY) * ldx + col, u[k]);
-            if constexpr (BWD) load_floats<V>(dy + (row + k * TY) * ldy + col, d[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < U; ++k) put(row + k * TY, u[k], d[k]);
-    }
-    for (; row < r1; row += TY) {
-        float u[V], d[V];
-        load_floats<V>(x + row * ldx + col, u);
-        if constexpr (BWD) load_floats<V>(dy + row * ldy + col, d);
-        put(row, u, d);
-    }
-}
-
-// Sums of dz xh and of dz over a chunk's columns
+// Mean and sum of squares about it of a chunk's groups: part[tile's group or piece][slot]
 template <class T, int V>
-__global__ __launch_bounds__(kNormBlock) void norm_grad_stats_kernel(NormShape sh, NormChunks ch, int TX, const T* __restrict__ x,
-                                                                     long ldx, const T* __restrict__ dy, long ldy,
-                                                                     const float* __restrict__ stats, float* __restrict__ part)
+__device__ __forceinline__ void norm_stats(const NormShape& sh, const SplitPlan& sp, int chunk, int tile, const T* __restrict__ x,
+                                           long ldx, ChunkEntry* __restrict__ table, float2* __restrict__ part)
 {
     __shared__ float red[2][kNormBlock];
-    long s, r0, r1;
-    if (!ch.find(sh, blockIdx.x, &s, &r0, &r1)) return;
-    const int TY = kNormBlock / TX, t = threadIdx.x, tx = t % TX, ty = t / TX;
-    const int vec = blockIdx.y * TX + tx, col = vec * V;
-    const bool on = ty < TY && col < sh.C;
-    float aw[V] = {}, ab[V] = {};
-    if (on) {
-        const int g = col / sh.cg;
-        const float mean = stats[(s * sh.G + g) * 2], r = stats[(s * sh.G + g) * 2 + 1];
-        float wv[V], bv[V];
-        sh.params<V>(col, wv, bv);
-        constexpr int U = 2;
-        auto add = [&](float (&u)[V], float (&d)[V]) {
+    Segment seg[2];
+    segments_of(sh, sp, chunk, seg, table, true);
+    const ColumnTile ct = column_tile<V>(sh, sp, tile);
+    const int TX = sp.TX, TY = kNormBlock / TX, t = threadIdx.x, tx = t % TX, ty = t / TX, cgv = sh.cg / V;
+    const bool on = ty < TY && tx < ct.width;
+    const int vec = ct.vec0 + tx;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float value;
-                const float xh = (u[i] - mean) * r;
-                const float dz = d[i] * act_slope(sh.act, xh * wv[i] + bv[i], &value);
-                aw[i] += dz * xh;
-                ab[i] += dz;
+    for (int q = 0; q < 2; ++q) {
+        if (seg[q].s < 0) continue;
+        const long r0 = seg[q].r0, r1 = seg[q].r1;
+        float a = 0.f, b = 0.f, shift = 0.f;
+        if (on) {
+            const T* __restrict__ xp = x + (long)vec * V;
+            const int from = ct.gn == 1 ? ct.vec0 : vec / cgv * cgv;
+            float one[1];
+            load_floats<1>(x + r0 * ldx + (long)from * V, one);
+            shift = one[0];
+            auto add = [&](const float (&u)[V]) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) { const float c = u[i] - shift; a += c; b += c * c; }
+            };
+            constexpr int U = 8;
+            long row = r0 + ty;
+            for (; row + (U - 1) * TY < r1; row += U * TY) {
+                float m[U][V];
+#pragma unroll
+                for (int k = 0; k < U; ++k) load_floats<V>(xp + (row + k * TY) * ldx, m[k]);
+#pragma unroll
+                for (int k = 0; k < U; ++k) add(m[k]);
+            }
+            for (; row < r1; row += TY) {
+                float u[V];
+                load_floats<V>(xp + row * ldx, u);
+                add(u);
+            }
+        }
+        // every group's first number, for its thread
+        const int width = ct.gn == 1 ? ct.width : cgv;
+        join_groups(red, a, b, TX, TY, cgv, ct.gn);
+        if (t < ct.gn) {
+            float one[1];
+            load_floats<1>(x + r0 * ldx + ((long)ct.vec0 + (long)t * cgv) * V, one);
+            const float count = (float)(r1 - r0) * (float)(width * V), m = red[0][t] / count;
+            const long at = sp.pieces == 1 ? ct.g0 + t : tile;
+            part[at * sp.slots + seg[q].slot] = make_float2(one[0] + m, variance(red[1][t], red[0][t], m));
+        }
+    }
+}
+
+constexpr int kJoinBlock = 1024, kJoinGroups = kJoinBlock / 64;
+
+// f(part, piece, chunk) for a wave's share of the parts of a sample and group, U of them on their way at once
+template <class F>
+__device__ __forceinline__ void for_parts(const NormShape& sh, const SplitPlan& sp, const Parts& p, int g,
+                                          const float2* __restrict__ part, F&& f) {
+    constexpr int U = 8;
+    for (int piece = 0; piece < sp.pieces; ++piece) {
+        const float2* __restrict__ from = part + ((long)g * sp.pieces + piece) * sp.slots;
+        for (int c = threadIdx.x & 63; c < p.n; c += U * 64) {
+            float2 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = from[p.slot(min(c + u * 64, p.n - 1))];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c + u * 64 < p.n) f(v[u], piece, c + u * 64);
+        }
+    }
+}
+
+// Joins the parts of a sample and group by the formula for the variance of a union; a wave owns a group
+template <int V>
+__global__ __launch_bounds__(kJoinBlock) void norm_join_kernel(NormShape sh, SplitPlan sp, const ChunkEntry* __restrict__ table,
+                                                               const float2* __restrict__ part, float* __restrict__ stats)
+{
+    long s;
+    Parts p;
+    if (!sample_to_join(sh, sp, blockIdx.x, table, &s, &p)) return;
+    const int g = blockIdx.y * kJoinGroups + (threadIdx.x >> 6), lane = threadIdx.x & 63, pieces = sp.pieces, cgv = sh.cg / V;
+    if (g >= sh.G) return;
+    const float total = (float)(p.r1 - p.r0) * (float)sh.cg;
+    float a = 0.f, b = 0.f;
+    // relative to the first chunk's mean, which the others are near
+    const float origin = part[(long)g * pieces * sp.slots + p.slot(0)].x;
+    for_parts(sh, sp, p, g, part, [&](float2 v, int piece, int c) {
+        const int width = pieces == 1 ? cgv : min(sp.TX, cgv - piece * sp.TX);
+        const float d = v.x - origin, n = (float)p.rows(c) * (float)(width * V);
+        a += d * n;
+        b += v.y + d * d * n;
+    });
+    a = wave_sum(a, 64);
+    b = wave_sum(b, 64);
+    const float m = a / total, mean = origin + m;
+    b = variance(b, a, m);
+    if (lane == 0) {
+        stats[(s * sh.G + g) * 2] = mean;
+        stats[(s * sh.G + g) * 2 + 1] = 1.f / sqrtf(b / total + sh.eps);
+    }
+}
+
+// y of a chunk; BWD: dx, with the means of e and e xh of every sample and group in `means`.  The last chunks first: they
+// are the ones that the pass before has left in the caches.
+template <class T, int V, bool BWD>
+__global__ __launch_bounds__(kNormBlock) void norm_apply_kernel(NormShape sh, SplitPlan sp, const T* __restrict__ x, long ldx,
+                                                                const T* __restrict__ dy, long ldy,
+                                                                const float* __restrict__ stats,
+                                                                const float* __restrict__ means, ChunkEntry* __restrict__ table,
+                                                                T* __restrict__ out)
+{
+    Segment seg[2];
+    segments_of(sh, sp, sp.chunks - 1 - blockIdx.x, seg, table, false);
+    const ColumnTile ct = column_tile<V>(sh, sp, blockIdx.y);
+    const int TX = sp.TX, TY = kNormBlock / TX, tx = threadIdx.x % TX, ty = threadIdx.x / TX;
+    if ((seg[0].s < 0 && seg[1].s < 0) || ty >= TY || tx >= ct.width) return;
+    const int col = (ct.vec0 + tx) * V, g = col / sh.cg;
+    float wv[V], bv[V];
+    sh.params<V>(col, wv, bv);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        if (seg[q].s < 0) continue;
+        const long s = seg[q].s, r0 = seg[q].r0, r1 = seg[q].r1;
+        const float mean = stats[(s * sh.G + g) * 2], r = stats[(s * sh.G + g) * 2 + 1];
+        float m1 = 0.f, m2 = 0.f;
+        if constexpr (BWD) {
+            m1 = means[(s * sh.G + g) * 2];
+            m2 = means[(s * sh.G + g) * 2 + 1];
+        }
+        auto put = [&](auto& u, auto& d) {                   // several rows' numbers, V to a row
+            constexpr int N = sizeof(u) / sizeof(float);
+            float z[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                u[i] = (u[i] - mean) * r;
+                z[i] = u[i] * wv[i % V] + bv[i % V];
+            }
+            if constexpr (!BWD) {
+                act_values(sh.act, z);
+#pragma unroll
+                for (int i = 0; i < N; ++i) u[i] = z[i];
+            } else {
+                act_slopes(sh.act, z);
+#pragma unroll
+                for (int i = 0; i < N; ++i) u[i] = r * (d[i] * z[i] * wv[i % V] - m1 - u[i] * m2);
             }
         };
+        constexpr int U = 4;
         long row = r0 + ty;
         for (; row + (U - 1) * TY < r1; row += U * TY) {
-            float u[U][V], d[U][V];
+            float u[U * V], d[U * V];
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-                load_floats<V>(x + (row + k * TY) * ldx + col, u[k]);
-                load_floats<V>(dy + (row + k * TY) * ldy + col, d[k]);
+                load_floats<V>(x + (row + k * TY) * ldx + col, part_of<V>(u, k));
+                if constexpr (BWD) load_floats<V>(dy + (row + k * TY) * ldy + col, part_of<V>(d, k));
             }
+            put(u, d);
 #pragma unroll
-            for (int k = 0; k < U; ++k) add(u[k], d[k]);
+            for (int k = 0; k < U; ++k) store_floats<V>(out + (row + k * TY) * sh.C + col, part_of<V>(u, k));
         }
         for (; row < r1; row += TY) {
             float u[V], d[V];
             load_floats<V>(x + row * ldx + col, u);
-            load_floats<V>(dy + row * ldy + col, d);
-            add(u, d);
+            if constexpr (BWD) load_floats<V>(dy + row * ldy + col, d);
+            put(u, d);
+            store_floats<V>(out + row * sh.C + col, u);
+        }
+    }
+}
+
+// Of a chunk: sums of dz xh and of dz over its columns (cols), which dw and db are made of, and of e and e xh over its
+// groups (part).  Slots that no sample has are cleared.
+template <class T, int V>
+__device__ __forceinline__ void norm_grad_stats(const NormShape& sh, const SplitPlan& sp, int chunk, int tile,
+                                                const T* __restrict__ x, long ldx, const T* __restrict__ dy, long ldy,
+                                                const float* __restrict__ stats, ChunkEntry* __restrict__ table,
+                                                float2* __restrict__ part, float* __restrict__ cols)
+{
+    __shared__ float red[2][kNormBlock];
+    Segment seg[2];
+    segments_of(sh, sp, chunk, seg, table, true);
+    const ColumnTile ct = column_tile<V>(sh, sp, tile);
+    const int TX = sp.TX, TY = kNormBlock / TX, t = threadIdx.x, tx = t % TX, ty = t / TX, cgv = sh.cg / V;
+    const bool on = ty < TY && tx < ct.width;
+    const int col = (ct.vec0 + tx) * V;
+    float aw[V] = {}, ab[V] = {}, wv[V], bv[V];
+    const bool some = seg[0].s >= 0 || seg[1].s >= 0;
+    if (on && some) sh.params<V>(col, wv, bv);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        if (seg[q].s < 0) continue;
+        float s1 = 0.f, s2 = 0.f;
+        if (on) {
+            const long r0 = seg[q].r0, r1 = seg[q].r1;
+            const int g = col / sh.cg;
+            const float mean = stats[(seg[q].s * sh.G + g) * 2], r = stats[(seg[q].s * sh.G + g) * 2 + 1];
+            auto add = [&](auto& u, auto& d) {
+                constexpr int N = sizeof(u) / sizeof(float);
+                float z[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    u[i] = (u[i] - mean) * r;
+                    z[i] = u[i] * wv[i % V] + bv[i % V];
+                }
+                act_slopes(sh.act, z);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float dz = d[i] * z[i], e = dz * wv[i % V];
+                    aw[i % V] += dz * u[i];
+                    ab[i % V] += dz;
+                    s1 += e;
+                    s2 += e * u[i];
+                }
+            };
+            constexpr int U = 4;
+            long row = r0 + ty;
+            for (; row + (U - 1) * TY < r1; row += U * TY) {
+                float u[U * V], d[U * V];
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    load_floats<V>(x + (row + k * TY) * ldx + col, part_of<V>(u, k));
+                    load_floats<V>(dy + (row + k * TY) * ldy + col, part_of<V>(d, k));
+                }
+                add(u, d);
+            }
+            for (; row < r1; row += TY) {
+                float u[V], d[V];
+                load_floats<V>(x + row * ldx + col, u);
+                load_floats<V>(dy + row * ldy + col, d);
+                add(u, d);
+            }
+        }
+        join_groups(red, s1, s2, TX, TY, cgv, ct.gn);
+        if (t < ct.gn) {
+            const long at = sp.pieces == 1 ? ct.g0 + t : tile;
+            part[at * sp.slots + seg[q].slot] = make_float2(red[0][t], red[1][t]);
         }
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        __syncthreads();
-        red[0][t] = aw[i];
-        red[1][t] = ab[i];
-        __syncthreads();
-        if (t < TX && col < sh.C) {
-            float p = 0.f, q = 0.f;
-            for (int k = 0; k < TY; ++k) { p += red[0][t + k * TX]; q += red[1][t + k * TX]; }
-            part[(long)blockIdx.x * 2 * sh.C + col + i] = p;
-            part[(long)blockIdx.x * 2 * sh.C + sh.C + col + i] = q;
+        float p = aw[i], q = ab[i];
+        if (some) {                                          // the same for all threads
+            __syncthreads();
+            red[0][t] = on ? p : 0.f;
+            red[1][t] = on ? q : 0.f;
+            __syncthreads();
+            if (t < ct.width)
+                for (int k = 1; k < TY; ++k) { p += red[0][t + k * TX]; q += red[1][t + k * TX]; }
+        }
+        if (t < ct.width) {
+            cols[(long)chunk * 2 * sh.C + col + i] = p;
+            cols[(long)chunk * 2 * sh.C + sh.C + col + i] = q;
         }
     }
 }
 
-// Means of e and e xh of a sample and group from the sums of its chunks' columns (e = dz w)
-__global__ __launch_bounds__(256) void norm_grad_join_kernel(NormShape sh, NormChunks ch, const float* __restrict__ part,
-                                                             float* __restrict__ means)
+// First pass: teams in the first blocks of a launch, chunks in the others.  Ragged samples may be of both kinds and only
+// the device knows, so both are one launch then (TEAM threads and chunks): an empty one would take as long as a small
+// sample.  Equal samples are all of one kind; their launches hold registers for that kind only.
+template <class T, int V, int TEAM, int E, bool CHUNKS, bool BWD>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_first_kernel(
+    NormShape sh, TeamPlan tp, SplitPlan sp, const T* __restrict__ x, long ldx, const T* __restrict__ dy, long ldy,
+    T* __restrict__ out, float* __restrict__ stats, float* __restrict__ team_cols, ChunkEntry* __restrict__ table,
+    float2* __restrict__ part, float* __restrict__ cols)
 {
-    __shared__ float red[2][4];
-    long s, first, chunks, r0, r1;
-    if (!ch.sample(blockIdx.x, &s, &first, &chunks)) return;
-    sh.range(s, &r0, &r1);
-    const int g = blockIdx.y;
-    const long n = chunks * sh.cg;
-    float a = 0.f, b = 0.f;
-    for (long k = threadIdx.x; k < n; k += 256) {
-        const int col = g * sh.cg + (int)(k % sh.cg);
-        const float w = sh.w ? load_param(sh.w, sh.param_dtype, col) : 1.f;
-        const float* __restrict__ p = part + (first + k / sh.cg) * 2 * sh.C + col;
-        a += w * p[sh.C];
-        b += w * p[0];
-    }
-    a = wave_sum(a, 64);
-    b = wave_sum(b, 64);
-    if ((threadIdx.x & 63) == 0) { red[0][threadIdx.x >> 6] = a; red[1][threadIdx.x >> 6] = b; }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const float total = (float)(r1 - r0) * (float)sh.cg;
-        means[(s * sh.G + g) * 2] = (red[0][0] + red[0][1] + red[0][2] + red[0][3]) / total;
-        means[(s * sh.G + g) * 2 + 1] = (red[1][0] + red[1][1] + red[1][2] + red[1][3]) / total;
+    const unsigned teams = (unsigned)tp.blocks * tp.tiles;
+    if (E > 0 && (!CHUNKS || blockIdx.x < teams)) {
+        if constexpr (E > 0)
+            norm_team<T, V, TEAM, E, BWD>(sh, tp, blockIdx.x / tp.tiles, blockIdx.x % tp.tiles, x, ldx, dy, ldy, out, stats, team_cols);
+    } else if constexpr (CHUNKS) {
+        const unsigned k = blockIdx.x - teams, chunk = k / sp.tiles, tile = k % sp.tiles;
+        if constexpr (BWD) norm_grad_stats<T, V>(sh, sp, chunk, tile, x, ldx, dy, ldy, stats, table, part, cols);
+        else norm_stats<T, V>(sh, sp, chunk, tile, x, ldx, table, part);
     }
 }
 
-// dw and db from the parts of all blocks: `fixed` rows of 2 C sums, then counts[0] (or `more`) rows at part2
-__global__ __launch_bounds__(1024) void norm_param_grads_kernel(int C, const float* __restrict__ part, long fixed,
-                                                                const float* __restrict__ part2, long more,
-                                                                const int* __restrict__ counts, void* dw, void* db, int dtype)
+// Second pass backward: the means of e and e xh of every split sample and group (first `joins` blocks, kJoinGroups groups
+// to a block), and dw, db from `rows` rows of 2 C sums, 16 columns to a block.
+__global__ __launch_bounds__(kJoinBlock) void norm_grad_join_kernel(NormShape sh, SplitPlan sp, int joins,
+                                                                    const ChunkEntry* __restrict__ table, const float2* __restrict__ part, float* __restrict__ means,
+                                                                    const float* __restrict__ cols, long rows, void* dw, void* db)
 {
-    __shared__ float sh[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = blockIdx.x * 64 + lane;
-    if (counts) more = counts[0];
+    __shared__ float red[kJoinBlock];
+    const int t = threadIdx.x;
+    if (blockIdx.x < joins) {
+        const int blocks = (sh.G + kJoinGroups - 1) / kJoinGroups;
+        long s;
+        Parts p;
+        if (!sample_to_join(sh, sp, blockIdx.x / blocks, table, &s, &p)) return;
+        const int g = (int)(blockIdx.x % blocks) * kJoinGroups + (t >> 6);
+        if (g >= sh.G) return;
+        float a = 0.f, b = 0.f;
+        for_parts(sh, sp, p, g, part, [&](float2 v, int, int) {
+            a += v.x;
+            b += v.y;
+        });
+        a = wave_sum(a, 64);
+        b = wave_sum(b, 64);
+        if ((t & 63) == 0) {
+            const float total = (float)(p.r1 - p.r0) * (float)sh.cg;
+            means[(s * sh.G + g) * 2] = a / total;
+            means[(s * sh.G + g) * 2 + 1] = b / total;
+        }
+        return;
+    }
+    const int c = (int)(blockIdx.x - joins) * 16 + (t & 15);
     float s = 0.f;
-    if (c < 2 * C) {
+    if (c < 2 * sh.C) {
         constexpr int U = 8;
         float a[U] = {};
-        auto sum = [&](const float* __restrict__ p, long n) {
-            long k = wave;
-            for (; k + (U - 1) * 16 < n; k += U * 16)
+        long k = t >> 4;
+        for (; k + (U - 1) * 64 < rows; k += U * 64)
 #pragma unroll
-                for (int u = 0; u < U; ++u) a[u] += p[(k + u * 16) * 2 * C + c];
-            for (; k < n; k += 16) a[0] += p[k * 2 * C + c];
-        };
-        sum(part, fixed);
-        sum(part2, more);
+            for (int u = 0; u < U; ++u) a[u] += cols[(k + u * 64) * 2 * sh.C + c];
+        for (; k < rows; k += 64) a[0] += cols[k * 2 * sh.C + c];
 #pragma unroll
         for (int u = 0; u < U; ++u) s += a[u];
     }
-    sh[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < 2 * C) {
-        for (int k = 1; k < 16; ++k) s += sh[k][lane];
-        if (c < C) { if (dw) store_param(dw, dtype, c, s); }
-        else if (db) store_param(db, dtype, c - C, s);
+    red[t] = s;
+    for (int d = kJoinBlock / 2; d >= 16; d >>= 1) {
+        __syncthreads();
+        if (t < d) red[t] += red[t + d];
+    }
+    if (t < 16 && c < 2 * sh.C) {
+        if (c < sh.C) { if (dw) store_param(dw, sh.param_dtype, c, red[t]); }
+        else if (db) store_param(db, sh.param_dtype, c - sh.C, red[t]);
     }
 }
 

@@ -364,3 +364,21 @@ def test_refusals():
     g, = torch.autograd.grad(y.sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="differentiated again"):
         g.sum().backward()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_ragged_samples_of_very_wide_groups(dtype):
+    """Groups wider than any block of threads: every sample is cut, a row at a time."""
+    lens = [1, 0, 7, 60, 0, 2]
+    offsets = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+    for C, G in ((8200, 1), (4106, 2), (5001, 3)):
+        x, w, b, dy = inputs((sum(lens), C), dtype, seed=C)
+        run(x, G, w, b, "silu", offsets, dy=dy)
+
+
+@pytest.mark.parametrize("lens", [[4000, 1, 4000], [3, 9000, 2, 2, 8000, 5], [1] * 70 + [5000] + [2] * 300 + [7000, 7001]], ids=["a", "b", "c"])
+def test_long_samples_that_share_a_chunk(lens):
+    offsets = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+    for C, G in ((24, 3), (8, 8)):
+        x, w, b, dy = inputs((sum(lens), C), torch.float32, seed=len(lens))
+        run(x, G, w, b, "gelu", offsets, dy=dy)
