@@ -3,9 +3,11 @@
 #pragma once
 #include "da_gated.h"
 #include "da_gated_kernels.hip"
+#include "da_gated_tiles.hip"
 #include "da_internal.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace daspmm {
 namespace {
@@ -40,9 +42,33 @@ template <class T> size_t part_bytes(int64_t M, int64_t N, int64_t K, int segmen
     return p.splits > 1 ? (size_t)batches * p.splits * M * N * (epi == kGate ? 2 : 1) * sizeof(float) : 0;
 }
 
+// Whether the tiles of 256 x 256 take a product: their loads are of 16 bytes at addresses that are multiples of it
+template <int ALAY, int BLAY> bool wide_takes(const GemmArgs<bf16>& g) {
+    auto whole = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+    return g.lda % 8 == 0 && g.ldb % 8 == 0 && g.lda < (1 << 22) && g.ldb < (1 << 22) && whole(g.A[0]) && whole(g.A[1]) &&
+           whole(g.B[0]) && whole(g.B[1]) && (ALAY == kInner || g.M % 8 == 0) && (BLAY == kInner || g.N % 8 == 0);
+}
+
 template <class T, int ALAY, int BLAY, int EPI>
 void gemm(GemmArgs<T> g, int batches, float* part, hipStream_t s) {
     if (g.M == 0 || g.N == 0) return;
+    if constexpr (std::is_same_v<T, bf16>) {
+        constexpr int ROWS = 256, STEP = 64, STAGES = 2;
+        const int64_t width = EPI == kGate ? 2 * (int64_t)g.N : g.N;
+        const int64_t tiles = ceil_div(g.M, ROWS) * ceil_div(width, kWideColumns) * batches;
+        if (tiles >= compute_units() && wide_takes<ALAY, BLAY>(g)) {
+            typedef WideShape<ROWS, STEP, STAGES> S;
+            g.splits = 1;
+            g.per = (int)ceil_div(g.K, STEP) * g.segments;
+            auto kernel = gated_wide_kernel<ROWS, STEP, STAGES, ALAY, BLAY, EPI>;
+            static const hipError_t allowed =
+                hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+            (void)allowed;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(g.M, ROWS) * ceil_div(width, kWideColumns)), 1, (unsigned)batches),
+                               dim3(S::THREADS), S::LDS, s, g);
+            return;
+        }
+    }
     const GemmPlan p = gemm_plan<T>(g.M, g.N, g.K, g.segments, batches, EPI);
     g.splits = p.splits;
     g.per = p.per;

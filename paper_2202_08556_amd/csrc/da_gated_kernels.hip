@@ -108,6 +108,80 @@ template <class T> __device__ __forceinline__ uint4 whole_chunk(const T* p) {
     return r;
 }
 
+// Results of a wave: MT x NT fragments from row m0 on, the j-th at column(j) of the tile that begins at column n0
+template <class T, int MT, int NT, int EPI, class F>
+__device__ __forceinline__ void gated_epilogue(const GemmArgs<T>& g, f32x4 (&acc)[MT][NT], int m0, int n0, int batch, F&& column)
+{
+    const int i16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
+    auto store4 = [&](auto* p, int left, const float (&x)[4]) {
+        if (left >= 4) store_floats<4>(p, x);
+        else
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float one[1] = {x[q]};
+                if (q < left) store_floats<1>(p + q, one);
+            }
+    };
+    constexpr int COLS = EPI == kGate ? NT / 2 : NT;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int m = m0 + i * 16 + i16;
+        if (m >= g.M) continue;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) {
+            const int n = n0 + column(j) + 4 * h, left = g.N - n;
+            if (left <= 0) continue;
+            const long at = (long)m * g.N + n;
+            float x[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = acc[i][j][q];
+            if (g.splits > 1) {
+                const long width = EPI == kGate ? 2L * g.N : g.N;
+                float* p = g.part + (((long)batch * g.splits + blockIdx.y) * g.M + m) * width + n;
+                store4(p, left, x);
+                if constexpr (EPI == kGate) {
+                    float v[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = acc[i][j + NT / 2][q];
+                    store4(p + g.N, left, v);
+                }
+            } else if constexpr (EPI == kStore) {
+                store4((batch ? g.C[1] : g.C[0]) + at, left, x);
+            } else if constexpr (EPI == kGate) {
+                float v[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = acc[i][j + NT / 2][q];
+                if (g.U) {
+                    store4(g.U + at, left, x);
+                    store4(g.V + at, left, v);
+                }
+                act_values(g.act, x);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] *= v[q];
+                store4(g.C[0] + at, left, x);
+            } else {
+                float u[4] = {}, v[4] = {}, slope[4];
+                if (left >= 4) {
+                    load_floats<4>(g.U + at, u);
+                    load_floats<4>(g.V + at, v);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (q < left) { u[q] = g.U[at + q]; v[q] = g.V[at + q]; }
+                }
+                act_both(g.act, u, slope);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v[q] *= x[q] * slope[q];
+                    x[q] *= u[q];
+                }
+                store4(g.C[0] + at, left, v);
+                store4(g.C[1] + at, left, x);
+            }
+        }
+    }
+}
+
 // MT x NT fragments of 16 x 16 to a wave, WM x WN waves to a block of 256 threads
 template <class T, int MT, int NT, int WM, int WN, int ALAY, int BLAY, int EPI>
 __global__ __launch_bounds__(256) void gated_gemm_kernel(GemmArgs<T> g)
@@ -210,74 +284,7 @@ __global__ __launch_bounds__(256) void gated_gemm_kernel(GemmArgs<T> g)
         __syncthreads();
     }
 
-    const int i16 = lane & 15, h = lane >> 4;
-    auto store4 = [&](auto* p, int left, const float (&x)[4]) {
-        if (left >= 4) store_floats<4>(p, x);
-        else
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float one[1] = {x[q]};
-                if (q < left) store_floats<1>(p + q, one);
-            }
-    };
-    constexpr int COLS = EPI == kGate ? NT / 2 : NT;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int m = m0 + (wm * MT + i) * 16 + i16;
-        if (m >= g.M) continue;
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) {
-            const int n = n0 + column(j) + 4 * h, left = g.N - n;
-            if (left <= 0) continue;
-            const long at = (long)m * g.N + n;
-            float x[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = acc[i][j][q];
-            if (g.splits > 1) {
-                const long width = EPI == kGate ? 2L * g.N : g.N;
-                float* p = g.part + (((long)batch * g.splits + blockIdx.y) * g.M + m) * width + n;
-                store4(p, left, x);
-                if constexpr (EPI == kGate) {
-                    float v[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] = acc[i][j + NT / 2][q];
-                    store4(p + g.N, left, v);
-                }
-            } else if constexpr (EPI == kStore) {
-                store4((batch ? g.C[1] : g.C[0]) + at, left, x);
-            } else if constexpr (EPI == kGate) {
-                float v[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = acc[i][j + NT / 2][q];
-                if (g.U) {
-                    store4(g.U + at, left, x);
-                    store4(g.V + at, left, v);
-                }
-                act_values(g.act, x);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) x[q] *= v[q];
-                store4(g.C[0] + at, left, x);
-            } else {
-                float u[4] = {}, v[4] = {}, slope[4];
-                if (left >= 4) {
-                    load_floats<4>(g.U + at, u);
-                    load_floats<4>(g.V + at, v);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (q < left) { u[q] = g.U[at + q]; v[q] = g.V[at + q]; }
-                }
-                act_both(g.act, u, slope);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[q] *= x[q] * slope[q];
-                    x[q] *= u[q];
-                }
-                store4(g.C[0] + at, left, v);
-                store4(g.C[1] + at, left, x);
-            }
-        }
-    }
+    gated_epilogue<T, MT, NT, EPI>(g, acc, m0 + wm * MT * 16, n0, batch, column);
 }
 
 // Sums the parts of a product and does what its epilogue would have done; a thread owns one number.

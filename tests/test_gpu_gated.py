@@ -285,3 +285,10 @@ def test_refusals():
     g, = torch.autograd.grad(f(x, wg, wu, wd).sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="differentiated again"):
         g.sum().backward()
+
+
+# products of so many tiles of 256 x 256 that they take the kernels for these: whole tiles, ends inside a tile on every
+# axis, sums that end inside a step of 32
+@pytest.mark.parametrize("T,d,h", [(4096, 1024, 4096), (4104, 1032, 4104), (4001, 1016, 4360), (8300, 520, 8328)])
+def test_large_products(T, d, h):
+    run(*inputs(T, d, h, d, torch.bfloat16, seed=T))
