@@ -96,8 +96,9 @@ int da_distill_backward(int dtype, int64_t rows, int64_t classes, int64_t best, 
  *             row-major, dense where no leading dimension is given
  *   u, v      float32, rows x h: written forward where not NULL (a backward pass is to follow), read backward.  They stay in
  *             32 bits for bfloat16, too: rounded, they would add as much to the error of dx as everything else together.
- *   a         rows x h of dtype, written forward (always), read backward; with bfloat16 it, du and dv are rounded, since they
- *             are operands of the matrix cores
+ *   a         rows x h of dtype: scratch of the forward call, which leaves act(u) v there where u and v are not NULL; read
+ *             backward.  With bfloat16 a, du and dv are rounded, since they are operands of the matrix cores (up to 8
+ *             rows are multiplied by the vector units forward, with an a of 32 bits).
  *   dx, dw_*  dense; any of them may be NULL and is then not computed
  *
  * Sums are held in 32 bits.  float32 is multiplied as it is (fp32 matrix cores).  All sizes up to 2^30, and fewer than 2^24

@@ -3,6 +3,7 @@
 #pragma once
 #include "da_gated.h"
 #include "da_gated_kernels.hip"
+#include "da_gated_rows.hip"
 #include "da_gated_tiles.hip"
 #include "da_internal.h"
 
@@ -91,9 +92,55 @@ void gemm(GemmArgs<T> g, int batches, float* part, hipStream_t s) {
     }
 }
 
+// Few rows, forward
+struct RowsPlan {
+    int LN, splits, per;
+    int64_t columns;             // blocks along the columns
+};
+
+// Four waves of eight lines each keep a compute unit's share of memory busy: six blocks a unit, no fewer than 32 lines to one.
+template <class T> RowsPlan rows_plan(int64_t N, int64_t K) {
+    RowsPlan p{};
+    const int64_t pieces = ceil_div(N, Mma<T>::VEC);
+    p.LN = 1;
+    while (p.LN < kRowsBlock && p.LN < pieces) p.LN *= 2;
+    if (p.LN > 64) p.LN = 64;                                // a wave a line: 1 KB
+    p.columns = std::max<int64_t>(1, ceil_div(pieces, p.LN));
+    const int64_t lines = 32 * (kRowsBlock / p.LN) / 4;      // as many blocks' worth for each of the threads along the lines
+    int64_t splits = std::min(ceil_div(6 * compute_units(), p.columns), ceil_div(K, std::max<int64_t>(lines, 32)));
+    splits = std::min<int64_t>(std::max<int64_t>(splits, 1), 65535);
+    p.per = (int)std::max<int64_t>(1, ceil_div(K, splits));
+    p.splits = (int)std::max<int64_t>(1, ceil_div(K, p.per));
+    return p;
+}
+
+template <class T> size_t rows_part_bytes(const GatedShape& s) {
+    const RowsPlan a = rows_plan<T>(s.h, s.d), b = rows_plan<T>(s.dout, s.h);
+    const size_t u = a.splits > 1 ? (size_t)(a.splits * s.rows * s.h * 2) : 0, y = b.splits > 1 ? (size_t)(b.splits * s.rows * s.dout) : 0;
+    return round16(std::max(u, y) * sizeof(float));
+}
+
+template <class T, class TX, int EPI> void rows_product(RowsArgs<T> g, const TX* x, int64_t ldx, hipStream_t s) {
+    if (g.N == 0) return;
+    const RowsPlan p = rows_plan<T>(g.N, g.K);
+    g.LN = p.LN;
+    g.splits = p.splits;
+    g.per = p.per;
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)p.columns, (unsigned)p.splits), dim3(kRowsBlock), 0, s, g, x, (long)ldx);
+    };
+    if (g.rows == 1) go(gated_rows_kernel<T, TX, 1, EPI>);
+    else if (g.rows == 2) go(gated_rows_kernel<T, TX, 2, EPI>);
+    else if (g.rows <= 4) go(gated_rows_kernel<T, TX, 4, EPI>);
+    else go(gated_rows_kernel<T, TX, 8, EPI>);
+    if (p.splits > 1)
+        hipLaunchKernelGGL((gated_rows_join_kernel<T, EPI>), dim3((unsigned)ceil_div(g.N, 64), (unsigned)g.rows), dim3(kRowsBlock), 0, s, g);
+}
+
 }  // namespace
 
 template <class T> size_t gated_forward_bytes(const GatedShape& s) {
+    if (s.rows <= kRowsMost) return rows_part_bytes<T>(s) + round16((size_t)(s.rows * s.h) * sizeof(float));
     return std::max(part_bytes<T>(s.rows, s.h, s.d, 1, 1, kGate), part_bytes<T>(s.rows, s.dout, s.h, 1, 1, kStore));
 }
 
@@ -107,6 +154,31 @@ template <class T> size_t gated_backward_bytes(const GatedShape& s) {
 
 template <class T> void gated_forward(const GatedCall& c) {
     const int rows = (int)c.s.rows, d = (int)c.s.d, h = (int)c.s.h, dout = (int)c.s.dout;
+    if (rows <= kRowsMost) {
+        RowsArgs<T> r{};
+        float* a32 = reinterpret_cast<float*>(c.workspace + rows_part_bytes<T>(c.s));
+        r.W0 = static_cast<const T*>(c.wg);
+        r.W1 = static_cast<const T*>(c.wu);
+        r.rows = rows;
+        r.N = h;
+        r.K = d;
+        r.part = reinterpret_cast<float*>(c.workspace);
+        r.A32 = a32;
+        r.C = c.u ? static_cast<T*>(c.a) : nullptr;          // only a backward pass reads it
+        r.U = c.u;
+        r.V = c.v;
+        r.act = c.act;
+        rows_product<T, T, kGate>(r, static_cast<const T*>(c.x), c.ldx, c.stream);
+        r = RowsArgs<T>{};
+        r.W0 = static_cast<const T*>(c.wd);
+        r.rows = rows;
+        r.N = dout;
+        r.K = h;
+        r.part = reinterpret_cast<float*>(c.workspace);
+        r.C = static_cast<T*>(c.y);
+        rows_product<T, float, kStore>(r, a32, h, c.stream);
+        return;
+    }
     float* part = reinterpret_cast<float*>(c.workspace);
     GemmArgs<T> g{};
     g.A[0] = g.A[1] = static_cast<const T*>(c.x);

@@ -292,3 +292,10 @@ def test_refusals():
 @pytest.mark.parametrize("T,d,h", [(4096, 1024, 4096), (4104, 1032, 4104), (4001, 1016, 4360), (8300, 520, 8328)])
 def test_large_products(T, d, h):
     run(*inputs(T, d, h, d, torch.bfloat16, seed=T))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 3, 5, 8, 9])
+@pytest.mark.parametrize("d,h,dout", [(1000, 2049, 77), (64, 100, 5000), (3, 7, 1), (2100, 64, 4096)])
+def test_few_rows(T, d, h, dout, dtype):
+    run(*inputs(T, d, h, dout, dtype, seed=T + d))
