@@ -16,9 +16,10 @@ namespace {
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
 
-// Tile of a product, and how its sum is cut: a tile of 128 x 128 has the most products for what it reads, fewer rows or
-// columns take one that has no more of them than needed; where the tiles do not fill the chip, the inner axis is cut
-// until two blocks a compute unit work, each on at least four tiles of it.
+// Tile of a product, and how its sum is cut.  A tile of 128 x 128 has the most products for what it reads; tiles of 64 x 64
+// are taken where the larger ones would leave most of the chip idle in their last turn (1531 x 602 out of 1187 float32: 60
+// large tiles, 240 small ones), and no more rows or columns than there are.  Where even these are fewer than the units, the
+// inner axis is cut, in parts of at least eight tiles of it (sixteen where it makes two parts at most).
 struct GemmPlan {
     int BM, BN;
     int splits, per;
@@ -26,13 +27,19 @@ struct GemmPlan {
 
 template <class T> GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi) {
     GemmPlan p{};
-    const int64_t width = epi == kGate ? 2 * N : N;
-    p.BN = width <= 64 && M > 64 && epi != kGate ? 64 : 128;
+    const int64_t width = epi == kGate ? 2 * N : N, cus = compute_units();
+    auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(M, bm) * ceil_div(width, bn) * batches; };
     p.BM = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    const int64_t tiles = ceil_div(M, p.BM) * ceil_div(width, p.BN) * batches;
-    const int64_t inner = ceil_div(K, kLineBytes / (int64_t)sizeof(T)) * segments;
+    p.BN = 128;
+    if (p.BM == 128) {
+        if (width <= 64 && epi != kGate) p.BN = 64;
+        else if (4 * ceil_div(tiles(128, 128), cus) > ceil_div(tiles(64, 64), cus)) p.BM = p.BN = 64;
+    } else if (p.BM == 64 && tiles(64, 128) < cus) {
+        p.BN = 64;
+    }
+    const int64_t count = tiles(p.BM, p.BN), inner = ceil_div(K, kLineBytes / (int64_t)sizeof(T)) * segments;
     int64_t splits = 1;
-    if (tiles < compute_units()) splits = std::min(2 * compute_units() / std::max<int64_t>(tiles, 1), ceil_div(inner, 4));
+    if (count <= cus) splits = std::min(2 * cus / std::max<int64_t>(count, 1), std::max<int64_t>(1, inner / (2 * count <= cus ? 8 : 16)));
     p.per = (int)std::max<int64_t>(1, ceil_div(inner, std::max<int64_t>(splits, 1)));
     p.splits = (int)std::max<int64_t>(1, ceil_div(inner, p.per));
     return p;
@@ -76,15 +83,14 @@ void gemm(GemmArgs<T> g, int batches, float* part, hipStream_t s) {
     g.part = part;
     const int64_t width = EPI == kGate ? 2 * (int64_t)g.N : g.N;
     const dim3 grid((unsigned)(ceil_div(g.M, p.BM) * ceil_div(width, p.BN)), (unsigned)p.splits, (unsigned)batches);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, g); };
+    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, g); };
+    if (p.BM == 128 && p.BN == 128) go(gated_gemm_kernel<T, 2, 4, 4, 2, ALAY, BLAY, EPI>, 512);
+    else if (p.BM == 64 && p.BN == 64) go(gated_gemm_kernel<T, 2, 2, 2, 2, ALAY, BLAY, EPI>, 256);
+    else if (p.BM == 16) go(gated_gemm_kernel<T, 1, 2, 1, 4, ALAY, BLAY, EPI>, 256);
+    else if (p.BM == 32) go(gated_gemm_kernel<T, 2, 2, 1, 4, ALAY, BLAY, EPI>, 256);
+    else if (p.BM == 64) go(gated_gemm_kernel<T, 4, 2, 1, 4, ALAY, BLAY, EPI>, 256);
     if constexpr (EPI != kGate) {
-        if (p.BN == 64) go(gated_gemm_kernel<T, 2, 4, 4, 1, ALAY, BLAY, EPI>);
-    }
-    if (p.BN == 128) {
-        if (p.BM == 16) go(gated_gemm_kernel<T, 1, 2, 1, 4, ALAY, BLAY, EPI>);
-        else if (p.BM == 32) go(gated_gemm_kernel<T, 2, 2, 1, 4, ALAY, BLAY, EPI>);
-        else if (p.BM == 64) go(gated_gemm_kernel<T, 4, 2, 1, 4, ALAY, BLAY, EPI>);
-        else go(gated_gemm_kernel<T, 4, 4, 2, 2, ALAY, BLAY, EPI>);
+        if (p.BM == 128 && p.BN == 64) go(gated_gemm_kernel<T, 2, 4, 4, 1, ALAY, BLAY, EPI>, 256);
     }
     if (p.splits > 1) {
         const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.M * g.N, 256), 16384);

@@ -27,7 +27,8 @@ template <> struct Mma<bf16> {
     typedef bf16x8 Frag;
     typedef Pack<uint16_t, 8>::type Memory;                  // at any address that an element may have
     static constexpr int VEC = 8;
-    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
+    static constexpr int TURNS = 1;                          // instructions that a product of fragments takes
+    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c, int = 0) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
 };
@@ -35,10 +36,9 @@ template <> struct Mma<float> {
     typedef f32x4 Frag;
     typedef Pack<float, 4>::type Memory;
     static constexpr int VEC = 4;
-    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
-        return c;
+    static constexpr int TURNS = 4;
+    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c, int turn) {
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(a[turn], b[turn], c, 0, 0, 0);
     }
 };
 
@@ -65,7 +65,6 @@ template <class T, int LAY, int OUTER> struct Tile {
     // padding: 8 or 16 lines of a fragment's read lie in different banks
     static constexpr int PITCH = CHUNKS * 16 + (LAY == kOuter && sizeof(T) == 2 ? 32 : 16);
     static constexpr int BYTES = LINES * PITCH;
-    static constexpr int PER = (LINES * CHUNKS + 255) / 256;                  // chunks of a thread
 
     // the fragment of outer positions o .. o + 15 and the step-th half of the inner axis
     static __device__ __forceinline__ typename Mma<T>::Frag frag(const char* lds, int o, int step) {
@@ -90,21 +89,26 @@ template <class T, int LAY, int OUTER> struct Tile {
     }
 };
 
-// 16 bytes at `at` of a line that has `left` elements from there on (none: zeros)
-template <class T> __device__ __forceinline__ uint4 edge_chunk(const T* p, int left) {
-    constexpr int VEC = Mma<T>::VEC;
-    T v[VEC] = {};
-#pragma unroll
-    for (int i = 0; i < VEC; ++i)
-        if (i < left) v[i] = p[i];
-    uint4 r;
-    __builtin_memcpy(&r, v, 16);
-    return r;
-}
 template <class T> __device__ __forceinline__ uint4 whole_chunk(const T* p) {
     const auto v = *reinterpret_cast<const typename Mma<T>::Memory*>(p);
     uint4 r;
     __builtin_memcpy(&r, &v, 16);
+    return r;
+}
+// 16 bytes from p on, of which `left` elements are there (none or less: zeros).  Most pieces of a tile at an edge are whole or
+// not there at all.
+template <class T> __device__ __forceinline__ uint4 edge_chunk(const T* p, int left) {
+    constexpr int VEC = Mma<T>::VEC;
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (left >= VEC) {
+        r = whole_chunk(p);
+    } else if (left > 0) {
+        T v[VEC] = {};
+#pragma unroll
+        for (int i = 0; i < VEC - 1; ++i)
+            if (i < left) v[i] = p[i];
+        __builtin_memcpy(&r, v, 16);
+    }
     return r;
 }
 
@@ -182,15 +186,17 @@ __device__ __forceinline__ void gated_epilogue(const GemmArgs<T>& g, f32x4 (&acc
     }
 }
 
-// MT x NT fragments of 16 x 16 to a wave, WM x WN waves to a block of 256 threads
+// MT x NT fragments of 16 x 16 to a wave, WM x WN waves to a block
 template <class T, int MT, int NT, int WM, int WN, int ALAY, int BLAY, int EPI>
-__global__ __launch_bounds__(256) void gated_gemm_kernel(GemmArgs<T> g)
+__global__ __launch_bounds__(64 * WM * WN) void gated_gemm_kernel(GemmArgs<T> g)
 {
-    static_assert(WM * WN == 4, "four waves");
+    constexpr int THREADS = 64 * WM * WN;
     constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, HALF = BN / 2;
     typedef Tile<T, ALAY, BM> TA;
     typedef Tile<T, BLAY, BN> TB;
     constexpr int VEC = Mma<T>::VEC, BK = TA::BK;
+    constexpr int ACHUNKS = TA::LINES * TA::CHUNKS, BCHUNKS = TB::LINES * TB::CHUNKS;
+    constexpr int APER = (ACHUNKS + THREADS - 1) / THREADS, BPER = (BCHUNKS + THREADS - 1) / THREADS;   // of a thread
     __shared__ __attribute__((aligned(16))) char lds[2][TA::BYTES + TB::BYTES];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / WN, wn = wave % WN;
@@ -202,49 +208,98 @@ __global__ __launch_bounds__(256) void gated_gemm_kernel(GemmArgs<T> g)
     const int t0 = blockIdx.y * g.per, t1 = min(t0 + g.per, tps * g.segments);
     const bool inside = m0 + BM <= g.M && n0 + WIDTH <= g.N;
 
-    uint4 ra[TA::PER], rb[TB::PER];
+    uint4 ra[APER], rb[BPER];
+    // Tiles at an edge load from the nearest whole pieces, all in flight together; put() shifts what is there into place and
+    // clears what lies past the end of the inner axis.  (Rows and columns past the result's are any: they are not stored.)
+    // Lines shorter than a piece go element by element.
+    const int a_line = ALAY == kInner ? g.K : g.M, b_line = BLAY == kInner ? g.K : g.N;
+    const bool pieces = a_line >= VEC && b_line >= VEC;
+    auto place = [&](int LAY, int q, int chunks, int o0, int k0, int* outer, int* inner) {
+        const int line = q / chunks, at = q % chunks * VEC;
+        *outer = o0 + (LAY == kInner ? line : at);
+        *inner = k0 + (LAY == kInner ? at : line);
+    };
     auto load = [&](int t) {
-        const int seg = t / tps, k0 = (t % tps) * BK;
+        const int seg = t / tps, k0 = (t - seg * tps) * BK;
         const T* __restrict__ A = seg ? g.A[1] : g.A[0];
         const T* __restrict__ B = seg + batch ? g.B[1] : g.B[0];
-        const bool whole = inside && k0 + BK <= g.K;
+        // get(layout, operand, its distance of lines, outer and inner position, outer positions) for all pieces: one branch around
+        // all loads and none between them, where the compiler would wait
+        auto all = [&](auto&& get) {
 #pragma unroll
-        for (int i = 0; i < TA::PER; ++i) {
-            const int q = tid + 256 * i, line = q / TA::CHUNKS, at = q % TA::CHUNKS * VEC;
-            if (TA::LINES * TA::CHUNKS % 256 != 0 && line >= TA::LINES) continue;
-            const int outer = m0 + (ALAY == kInner ? line : at), inner = k0 + (ALAY == kInner ? at : line);
-            const T* p = ALAY == kInner ? A + (long)outer * g.lda + inner : A + (long)inner * g.lda + outer;
-            if (whole) ra[i] = whole_chunk(p);
-            else ra[i] = edge_chunk(p, ALAY == kInner ? (outer < g.M ? g.K - inner : 0) : (inner < g.K ? g.M - outer : 0));
-        }
+            for (int i = 0; i < APER; ++i) {
+                const int q = tid + THREADS * i;
+                if (ACHUNKS % THREADS != 0 && q >= ACHUNKS) continue;
+                int outer, inner;
+                place(ALAY, q, TA::CHUNKS, m0, k0, &outer, &inner);
+                ra[i] = get(ALAY, A, g.lda, outer, inner, g.M);
+            }
 #pragma unroll
-        for (int i = 0; i < TB::PER; ++i) {
-            const int q = tid + 256 * i, line = q / TB::CHUNKS, at = q % TB::CHUNKS * VEC;
-            if (TB::LINES * TB::CHUNKS % 256 != 0 && line >= TB::LINES) continue;
-            int col = BLAY == kInner ? line : at;
-            const T* W = B;
-            if (EPI == kGate && col >= HALF) { W = g.B[1]; col -= HALF; }
-            const int outer = n0 + col, inner = k0 + (BLAY == kInner ? at : line);
-            const T* p = BLAY == kInner ? W + (long)outer * g.ldb + inner : W + (long)inner * g.ldb + outer;
-            if (whole) rb[i] = whole_chunk(p);
-            else {
-                const int room = EPI == kGate ? min(g.N, n0 + HALF) : g.N;
-                rb[i] = edge_chunk(p, BLAY == kInner ? (outer < g.N ? g.K - inner : 0) : (inner < g.K ? room - outer : 0));
+            for (int i = 0; i < BPER; ++i) {
+                const int q = tid + THREADS * i;
+                if (BCHUNKS % THREADS != 0 && q >= BCHUNKS) continue;
+                int outer, inner;
+                place(BLAY, q, TB::CHUNKS, 0, k0, &outer, &inner);
+                const bool up = EPI == kGate && outer >= HALF;
+                rb[i] = get(BLAY, up ? g.B[1] : B, g.ldb, n0 + outer - (up ? HALF : 0), inner, g.N);
+            }
+        };
+        auto at = [&](int LAY, const T* W, long ld, int outer, int inner) {
+            return LAY == kInner ? W + (long)outer * ld + inner : W + (long)inner * ld + outer;
+        };
+        if (inside && k0 + BK <= g.K)
+            all([&](int LAY, const T* W, long ld, int outer, int inner, int) { return whole_chunk(at(LAY, W, ld, outer, inner)); });
+        else if (pieces)
+            all([&](int LAY, const T* W, long ld, int outer, int inner, int outers) {
+                outer = min(outer, LAY == kInner ? outers - 1 : outers - VEC);
+                inner = min(inner, LAY == kInner ? g.K - VEC : g.K - 1);
+                return whole_chunk(at(LAY, W, ld, outer, inner));
+            });
+        else
+            all([&](int LAY, const T* W, long ld, int outer, int inner, int outers) {
+                const int left = LAY == kInner ? (outer < outers ? g.K - inner : 0) : (inner < g.K ? outers - outer : 0);
+                return edge_chunk(at(LAY, W, ld, outer, inner), left);
+            });
+    };
+    auto put = [&](int t, char* buf) {
+        const int k0 = t % tps * BK;
+        const bool fix = pieces && !(inside && k0 + BK <= g.K);
+        auto fixed = [&](int LAY, uint4 x, int outer, int inner, int outers) {
+            const int past = LAY == kInner ? inner - (g.K - VEC) : outer - (outers - VEC);      // elements of the piece past the end
+            if (past > 0) {
+                unsigned __int128 v;
+                __builtin_memcpy(&v, &x, 16);
+                v = past >= VEC ? 0 : v >> (past * (int)sizeof(T) * 8);
+                __builtin_memcpy(&x, &v, 16);
+            }
+            if (LAY == kOuter && inner >= g.K) x = make_uint4(0, 0, 0, 0);
+            return x;
+        };
+        if (fix) {
+#pragma unroll
+            for (int i = 0; i < APER; ++i) {
+                int outer, inner;
+                place(ALAY, tid + THREADS * i, TA::CHUNKS, m0, k0, &outer, &inner);
+                ra[i] = fixed(ALAY, ra[i], outer, inner, g.M);
+            }
+#pragma unroll
+            for (int i = 0; i < BPER; ++i) {
+                int outer, inner;
+                place(BLAY, tid + THREADS * i, TB::CHUNKS, 0, k0, &outer, &inner);
+                rb[i] = fixed(BLAY, rb[i], n0 + outer - (EPI == kGate && outer >= HALF ? HALF : 0), inner, g.N);
             }
         }
-    };
-    auto put = [&](char* buf) {
 #pragma unroll
-        for (int i = 0; i < TA::PER; ++i) {
-            const int q = tid + 256 * i, line = q / TA::CHUNKS;
-            if (TA::LINES * TA::CHUNKS % 256 != 0 && line >= TA::LINES) continue;
-            *reinterpret_cast<uint4*>(buf + line * TA::PITCH + q % TA::CHUNKS * 16) = ra[i];
+        for (int i = 0; i < APER; ++i) {
+            const int q = tid + THREADS * i;
+            if (ACHUNKS % THREADS != 0 && q >= ACHUNKS) continue;
+            *reinterpret_cast<uint4*>(buf + q / TA::CHUNKS * TA::PITCH + q % TA::CHUNKS * 16) = ra[i];
         }
 #pragma unroll
-        for (int i = 0; i < TB::PER; ++i) {
-            const int q = tid + 256 * i, line = q / TB::CHUNKS;
-            if (TB::LINES * TB::CHUNKS % 256 != 0 && line >= TB::LINES) continue;
-            *reinterpret_cast<uint4*>(buf + TA::BYTES + line * TB::PITCH + q % TB::CHUNKS * 16) = rb[i];
+        for (int i = 0; i < BPER; ++i) {
+            const int q = tid + THREADS * i;
+            if (BCHUNKS % THREADS != 0 && q >= BCHUNKS) continue;
+            *reinterpret_cast<uint4*>(buf + TA::BYTES + q / TB::CHUNKS * TB::PITCH + q % TB::CHUNKS * 16) = rb[i];
         }
     };
     // first column of the wave's j-th fragment in the tile; kGate: the first half of them from Wg, the others from Wu
@@ -261,7 +316,7 @@ __global__ __launch_bounds__(256) void gated_gemm_kernel(GemmArgs<T> g)
 
     if (t0 < t1) {
         load(t0);
-        put(lds[0]);
+        put(t0, lds[0]);
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
@@ -276,11 +331,13 @@ __global__ __launch_bounds__(256) void gated_gemm_kernel(GemmArgs<T> g)
             for (int j = 0; j < NT; ++j) b[j] = TB::frag(buf + TA::BYTES, column(j), step);
             // columns as the first operand: a lane's four results are neighbours in a row
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int k = 0; k < Mma<T>::TURNS; ++k)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = Mma<T>::mul(b[j], a[i], acc[i][j]);
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = Mma<T>::mul(b[j], a[i], acc[i][j], k);
         }
-        if (t + 1 < t1) put(lds[(t + 1 - t0) & 1]);
+        if (t + 1 < t1) put(t + 1, lds[(t + 1 - t0) & 1]);
         __syncthreads();
     }
 
