@@ -13,6 +13,8 @@
 #pragma once
 #include "da_layer_common.h"
 
+#include <type_traits>
+
 namespace daspmm {
 
 constexpr int kDistillBlock = 256;
@@ -23,7 +25,7 @@ struct Teacher {
     const void* index;
     const void* top;
     int index64, top_dtype;
-    float scale;                 // 1 / temperature
+    float scale;                 // log2(e) / temperature
 
     __device__ long cls(long at) const {
         return index64 ? static_cast<const int64_t*>(index)[at] : (long)static_cast<const int32_t*>(index)[at];
@@ -65,8 +67,8 @@ __device__ __forceinline__ float wave_max(float x, int lanes) {
     return x;
 }
 
-// exp((x - largest) / T)
-__device__ __forceinline__ float shifted_exp(float x, float largest, float scale) { return __expf((x - largest) * scale); }
+// exp((x - largest) / T); scale = log2(e) / T.  The difference comes first: scaled, large logits would lose it.
+__device__ __forceinline__ float shifted_exp(float x, float largest, float scale) { return exp2_hw((x - largest) * scale); }
 
 // ------------------------------------------------------------------------------------------
 // narrow rows: E accesses of V logits a lane.  BWD: a lane group's entries go through LDS, `best` slots of class and
@@ -81,6 +83,7 @@ __global__ __launch_bounds__(kDistillBlock) void distill_narrow_kernel(
     extern __shared__ Entry entries[];
     const int lane = threadIdx.x & (P - 1), per_block = kDistillBlock / P;
     Entry* mine = entries + (threadIdx.x / P) * te.best;
+    const float inv_t = 1.f / temperature;
     for (long row = (long)blockIdx.x * per_block + threadIdx.x / P; row < rows; row += (long)gridDim.x * per_block) {
         const T* __restrict__ zp = z + row * ldz;
         float x[E][V];
@@ -108,12 +111,12 @@ __global__ __launch_bounds__(kDistillBlock) void distill_narrow_kernel(
             for (long k = lane; k < te.best; k += P) {
                 const long c = te.cls(row * te.best + k);
                 if (!te.has(c)) continue;
-                const float t = (te.logit(row * te.best + k) - tmax) * te.scale;
-                const float p = __expf(t);
+                const float t = te.logit(row * te.best + k) - tmax;
+                const float p = exp2_hw(t * te.scale);
                 float zc[1];
                 load_floats<1>(zp + c, zc);
                 ps += p;
-                if (p != 0.f) a += p * (t - (zc[0] - m) * te.scale);
+                if (p != 0.f) a += p * ((t - (zc[0] - m)) * inv_t);
             }
             ps = wave_sum(ps, P);
             a = wave_sum(a, P);
@@ -202,25 +205,41 @@ template <int BLOCK> __device__ __forceinline__ float block_sum(float x, float* 
     return x;
 }
 
+// A thread's first entry, asked for before the row's logits
+struct FirstEntry {
+    long cls = -1;
+    float t = 0.f;
+    __device__ void load(long row, const Teacher& te) {
+        if (threadIdx.x < te.best) {
+            cls = te.cls(row * te.best + threadIdx.x);
+            t = te.logit(row * te.best + threadIdx.x);
+            if (!te.has(cls)) cls = -1;
+        }
+    }
+};
+
 // loss of a row from its largest logit and sum, by all threads of a block
 template <class T, int BLOCK>
-__device__ __forceinline__ void row_loss(long row, const Teacher& te, const T* __restrict__ zp, float m, float s,
-                                         float temperature, float* __restrict__ loss, float* __restrict__ stats, float* red)
+__device__ __forceinline__ void row_loss(long row, const Teacher& te, const FirstEntry& first, const T* __restrict__ zp, float m,
+                                         float s, float temperature, float* __restrict__ loss, float* __restrict__ stats, float* red)
 {
-    float tmax = -INFINITY;
-    for (long k = threadIdx.x; k < te.best; k += BLOCK)
+    float tmax = first.cls >= 0 ? first.t : -INFINITY;
+    for (long k = threadIdx.x + BLOCK; k < te.best; k += BLOCK)
         if (te.has(te.cls(row * te.best + k))) tmax = fmaxf(tmax, te.logit(row * te.best + k));
     tmax = block_max<BLOCK>(tmax, red);
+    const float inv_t = 1.f / temperature;
     float ps = 0.f, a = 0.f;
-    for (long k = threadIdx.x; k < te.best; k += BLOCK) {
-        const long c = te.cls(row * te.best + k);
-        if (!te.has(c)) continue;
-        const float t = (te.logit(row * te.best + k) - tmax) * te.scale;
-        const float p = __expf(t);
+    auto add = [&](long c, float logit) {
         float zc[1];
         load_floats<1>(zp + c, zc);
+        const float t = logit - tmax, p = exp2_hw(t * te.scale);
         ps += p;
-        if (p != 0.f) a += p * (t - (zc[0] - m) * te.scale);
+        if (p != 0.f) a += p * ((t - (zc[0] - m)) * inv_t);
+    };
+    if (first.cls >= 0) add(first.cls, first.t);
+    for (long k = threadIdx.x + BLOCK; k < te.best; k += BLOCK) {
+        const long c = te.cls(row * te.best + k);
+        if (te.has(c)) add(c, te.logit(row * te.best + k));
     }
     ps = block_sum<BLOCK>(ps, red);
     a = block_sum<BLOCK>(a, red);
@@ -230,6 +249,43 @@ __device__ __forceinline__ void row_loss(long row, const Teacher& te, const T* _
     }
 }
 
+// A thread's logits of a turn of a block, U accesses of V, as they come from memory.  The next turn's are asked for before
+// this one's are used: converted at once, they would be waited for.
+template <class T, int V, int U> struct Turn {
+    typedef typename std::conditional<sizeof(T) == 2, uint16_t, float>::type Raw;
+    typename Pack<Raw, V>::type x[U];
+
+    static __device__ __forceinline__ Raw none() {
+        if constexpr (sizeof(T) == 2) return 0xff80u;        // -inf
+        else return -INFINITY;
+    }
+    // from column c on; `whole`: the block's turn ends before `end`
+    __device__ __forceinline__ void load(const T* __restrict__ row, long c, long end, bool whole) {
+        const Raw* __restrict__ p = reinterpret_cast<const Raw*>(row);
+        if (whole) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const typename Pack<Raw, V>::type*>(p + c + (long)u * kWideBlock * V);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long at = c + (long)u * kWideBlock * V;
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[u][i] = none();
+                if (at + V <= end) x[u] = *reinterpret_cast<const typename Pack<Raw, V>::type*>(p + at);
+                else
+#pragma unroll
+                    for (int i = 0; i < V - 1; ++i)
+                        if (at + i < end) x[u][i] = p[at + i];
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int u, int i) const {
+        if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)x[u][i] << 16);
+        else return x[u][i];
+    }
+};
+constexpr int kWideTurns = 4, kWideForwardTurns = 2;          // forward the logits are wanted twice, as floats: 4 cost half of the waves
+
 // blockIdx.x: piece of `piece` columns; rows over blockIdx.y
 template <class T, int V>
 __global__ __launch_bounds__(kWideBlock) void distill_wide_kernel(long rows, long piece, Teacher te, const T* __restrict__ z,
@@ -237,32 +293,37 @@ __global__ __launch_bounds__(kWideBlock) void distill_wide_kernel(long rows, lon
                                                                   float* __restrict__ stats, float2* __restrict__ part)
 {
     __shared__ float red[kWideBlock / 64];
-    constexpr int U = 4;
+    constexpr int U = kWideForwardTurns;
+    constexpr long TURN = (long)U * kWideBlock * V;
     for (long row = blockIdx.y; row < rows; row += gridDim.y) {
         const T* __restrict__ zp = z + row * ldz;
         const long c0 = blockIdx.x * piece, c1 = min(c0 + piece, te.classes);
+        FirstEntry first;
+        if (gridDim.x == 1) first.load(row, te);
         float m = -INFINITY, s = 0.f;
-        for (long c = c0 + threadIdx.x * V; c < c1; c += U * kWideBlock * V) {
-            float x[U][V], top = m;
-#pragma unroll
-            for (int u = 0; u < U; ++u) load_logits<T, V>(zp, c + (long)u * kWideBlock * V, c1, x[u]);
+        Turn<T, V, U> next;
+        next.load(zp, c0 + threadIdx.x * V, c1, c0 + TURN <= c1);
+        for (long c = c0; c < c1; c += TURN) {
+            const Turn<T, V, U> now = next;
+            if (c + TURN < c1) next.load(zp, c + TURN + threadIdx.x * V, c1, c + 2 * TURN <= c1);
+            float top = m;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int i = 0; i < V; ++i) top = fmaxf(top, x[u][i]);
+                for (int i = 0; i < V; ++i) top = fmaxf(top, now.get(u, i));
             // nothing but -inf (or NaN) so far: taken relative to 0, where -inf adds nothing and NaN shows
             const float from = top == -INFINITY ? 0.f : top;
             s = m == -INFINITY ? s : s * shifted_exp(m, from, te.scale);
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int i = 0; i < V; ++i) s += shifted_exp(x[u][i], from, te.scale);
+                for (int i = 0; i < V; ++i) s += shifted_exp(now.get(u, i), from, te.scale);
             m = top;
         }
         const float top = block_max<kWideBlock>(m, red);
         if (top != -INFINITY) s = m == -INFINITY ? s : s * shifted_exp(m, top, te.scale);
         s = block_sum<kWideBlock>(s, red);
-        if (gridDim.x == 1) row_loss<T, kWideBlock>(row, te, zp, top, s, temperature, loss, stats, red);
+        if (gridDim.x == 1) row_loss<T, kWideBlock>(row, te, first, zp, top, s, temperature, loss, stats, red);
         else if (threadIdx.x == 0) part[row * gridDim.x + blockIdx.x] = make_float2(top, s);
         __syncthreads();
     }
@@ -275,12 +336,14 @@ __global__ __launch_bounds__(256) void distill_join_kernel(long rows, int pieces
 {
     __shared__ float red[4];
     for (long row = blockIdx.x; row < rows; row += gridDim.x) {
+        FirstEntry first;
+        first.load(row, te);
         float m = -INFINITY, s = 0.f;
         for (int k = 0; k < pieces; ++k) {                   // the same order for every thread
             const float2 p = part[row * pieces + k];
             join_max_sum(m, s, p.x, p.y, te.scale);
         }
-        row_loss<T, 256>(row, te, z + row * ldz, m, s, temperature, loss, stats, red);
+        row_loss<T, 256>(row, te, first, z + row * ldz, m, s, temperature, loss, stats, red);
         __syncthreads();
     }
 }
@@ -292,11 +355,14 @@ __global__ __launch_bounds__(kWideBlock) void distill_wide_grad_kernel(
 {
     __shared__ float red[kWideBlock / 64];
     __shared__ Entry entries[kDistillMaxBest];
-    constexpr int U = 4;
+    constexpr int U = kWideTurns;
+    constexpr long TURN = (long)U * kWideBlock * V;
     for (long row = blockIdx.y; row < rows; row += gridDim.y) {
         const T* __restrict__ zp = z + row * ldz;
         T* __restrict__ dp = dz + row * te.classes;
         const long c0 = blockIdx.x * piece, c1 = min(c0 + piece, te.classes);
+        Turn<T, V, U> next;
+        next.load(zp, c0 + threadIdx.x * V, c1, c0 + TURN <= c1);
         float tmax = -INFINITY, ps = 0.f;
         for (long k = threadIdx.x; k < te.best; k += kWideBlock)
             if (te.has(te.cls(row * te.best + k))) tmax = fmaxf(tmax, te.logit(row * te.best + k));
@@ -311,15 +377,16 @@ __global__ __launch_bounds__(kWideBlock) void distill_wide_grad_kernel(
         const float m = stats[2 * row], inv = stats[2 * row + 1];
         const bool none = tmax == -INFINITY;
         const float grad = none ? 0.f : dloss[row * dloss_stride] * temperature;
-        for (long c = c0 + threadIdx.x * V; c < c1; c += U * kWideBlock * V) {
-            float x[U][V];
-#pragma unroll
-            for (int u = 0; u < U; ++u) load_logits<T, V>(zp, c + (long)u * kWideBlock * V, c1, x[u]);
+        const float ginv = grad * inv;
+        for (long c = c0; c < c1; c += TURN) {
+            const Turn<T, V, U> now = next;
+            if (c + TURN < c1) next.load(zp, c + TURN + threadIdx.x * V, c1, c + 2 * TURN <= c1);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                float x[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[u][i] = none ? 0.f : grad * (shifted_exp(x[u][i], m, te.scale) * inv);
-                store_grads<T, V>(dp, c + (long)u * kWideBlock * V, c1, x[u]);
+                for (int i = 0; i < V; ++i) x[i] = none ? 0.f : ginv * shifted_exp(now.get(u, i), m, te.scale);
+                store_grads<T, V>(dp, c + threadIdx.x * V + (long)u * kWideBlock * V, c1, x);
             }
         }
         __syncthreads();                                     // the gradients of the entries' classes come over the others

@@ -417,7 +417,7 @@ void distill_forward(const DistillPlan& p, int64_t rows, const Teacher& te, cons
 }
 
 Teacher teacher(int64_t classes, int64_t best, const void* index, int index64, const void* top, int top_dtype, float temperature) {
-    return Teacher{classes, best, index, top, index64, top_dtype, 1.f / temperature};
+    return Teacher{classes, best, index, top, index64, top_dtype, (float)(1.4426950408889634 / (double)temperature)};
 }
 
 }  // namespace
