@@ -37,12 +37,15 @@ int pow2_at_least(int64_t x) {
 // Blocks of a launch: of 2^32 threads and more the high bits are lost
 constexpr int64_t kMaxBlocks = (1LL << 32) / 1024 - 1;
 
+// Rows that a thread of a team holds: twice as many cost half of the waves and more than they save
+constexpr int norm_held(int V) { return V >= 8 ? 2 : 4; }
+
 struct NormPlan {
     int V;                   // numbers of an access: divides a group
     bool each;               // every row is a sample and a group a few lanes' registers
     int P, E;
     int64_t each_grid;
-    int team, held;          // threads of a team (0: none), rows a thread holds
+    int team;                // threads of a team; 0: none
     TeamPlan tp;
     bool split;
     SplitPlan sp;
@@ -90,24 +93,30 @@ NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_
         }
     }
     if (!p.each) {
-        const int E = p.V >= 8 ? 4 : 8;
+        const int E = norm_held(p.V);
         const double mean = samples ? (double)rows / (double)samples : 0.0;
         auto tile = [&](int team) { return std::max<int64_t>(1, std::min<int64_t>(team / cgv, G)); };
         auto held = [&](int team) { return cgv > team ? 0 : (team / (tile(team) * cgv)) * (int64_t)E; };
-        for (int team : {64, 256, 1024}) {
-            if (cgv > team) continue;
-            if (team == 1024 || (ragged ? 2 * mean : mean) <= (double)held(team)) { p.team = team; break; }
+        // A wave or a block of 256 threads takes a sample that its registers hold, and some more that is read again: equal
+        // samples up to twice that, ragged ones up to 32768 numbers, since chunks are no longer than the shortest sample
+        // that is split and short ones are many blocks with nothing to do.  Longer samples are split.
+        // Blocks of 1024 threads take groups too wide for that, and equal samples that are too few to fill the chip, where
+        // one launch counts.  (2168 ragged samples of 285 rows x 64 bf16, forward and backward: kernels of 349 us with
+        // blocks of 1024 threads for up to 2048 rows, 274 split from 128 rows on, 227 from 512 on.)
+        const int64_t blocks = samples * ceil_div(G, tile(1024));
+        int64_t longest = 0;
+        if (cgv > 256) longest = cgv > 1024 ? 0 : 2 * held(1024);
+        else if (!ragged && blocks <= cus && length > 2 * held(256)) longest = held(1024);
+        else longest = std::max(2 * held(256), ragged ? 32768 / C : 0);
+        if (ragged || length <= longest) {
+            if (cgv <= 64 && (ragged ? 2 * mean : mean) <= (double)held(64)) p.team = 64;
+            else if (cgv <= 256 && (ragged || length <= 2 * held(256))) p.team = 256;
+            else if (cgv <= 1024) p.team = 1024;
         }
-        // A block takes up to a few times what its registers hold; longer samples are split.
-        const int64_t longest = (ragged ? 4 : 2) * held(1024);
-        if (!ragged && length > longest) p.team = 0;
         p.split = ragged ? rows > longest : length > longest;
         if (p.team) {
             const int64_t teams = p.team == 64 ? 4 : 1, cap = train ? cus * (p.team == 1024 ? 2 : 8) : 1 << 20;
             p.tp.GT = (int)tile(p.team);
-            // half as many registers where most samples need no more: two more blocks to a compute unit
-            // (and always in blocks of 1024 threads, which have 128 registers a thread)
-            p.held = p.team == 1024 || (ragged ? 1.5 * mean : mean) <= (double)held(p.team) / 2 ? E / 2 : E;
             p.tp.tiles = (int)ceil_div(G, p.tp.GT);
             p.tp.longest = longest;
             p.tp.blocks = std::min(ceil_div(samples, teams), cap);
@@ -189,18 +198,13 @@ void launch_first(const NormPlan& p, const NormShape& sh, const T* x, int64_t ld
                                stats, team_cols, table, part, cols);
     };
     const int64_t chunks = p.split ? p.sp.chunks : 0;
-    constexpr int E = V >= 8 ? 4 : 8;
-    auto held = [&](auto e) {
-        constexpr int H = decltype(e)::value;
-        if (p.team == 64 && chunks) go(norm_first_kernel<T, V, 64, H, true, BWD>, 256, p.tp, chunks);
-        else if (p.team == 64) go(norm_first_kernel<T, V, 64, H, false, BWD>, 256, p.tp, 0);
-        else if (chunks) go(norm_first_kernel<T, V, 256, H, true, BWD>, 256, p.tp, chunks);
-        else go(norm_first_kernel<T, V, 256, H, false, BWD>, 256, p.tp, 0);
-    };
-    if (p.team == 1024) go(norm_first_kernel<T, V, 1024, E / 2, false, BWD>, 1024, p.tp, 0);
+    constexpr int E = norm_held(V);
+    if (p.team == 1024) go(norm_first_kernel<T, V, 1024, E, false, BWD>, 1024, p.tp, 0);
     if (p.team == 1024 || !p.team) go(norm_first_kernel<T, V, 256, 0, true, BWD>, 256, TeamPlan{}, chunks);
-    else if (p.held == E / 2) held(std::integral_constant<int, E / 2>{});
-    else held(std::integral_constant<int, E>{});
+    else if (p.team == 64 && chunks) go(norm_first_kernel<T, V, 64, E, true, BWD>, 256, p.tp, chunks);
+    else if (p.team == 64) go(norm_first_kernel<T, V, 64, E, false, BWD>, 256, p.tp, 0);
+    else if (chunks) go(norm_first_kernel<T, V, 256, E, true, BWD>, 256, p.tp, chunks);
+    else go(norm_first_kernel<T, V, 256, E, false, BWD>, 256, p.tp, 0);
 }
 
 template <class T, int V>
