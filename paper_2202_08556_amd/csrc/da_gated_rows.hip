@@ -6,7 +6,8 @@
 // also dealt to `splits` blocks until the chip is full; their sums meet in gated_rows_join_kernel in a fixed order.
 // What is multiplied by the weights lies in LDS, R numbers (rows) to a line, so that one read serves them all.  a stays in
 // 32 bits between the two products: in bfloat16 it would be the larger part of the error.
-// One row of 4096 x 12288 bf16 (302 MB): see the table of the cases; per element two instructions and one more for each row.
+// One row of 4096 x 12288 bf16: 73 us for 302 MB (4.1 TB/s; a large copy 5.2); per element one instruction and one more for
+// each row, so that memory stays the bound up to eight rows.
 #pragma once
 #include "da_gated_kernels.hip"
 
@@ -26,16 +27,22 @@ template <class T> struct RowsArgs {
     int act;
 };
 
-template <class T, int V> __device__ __forceinline__ void load_line(const T* __restrict__ p, int left, float (&w)[V]) {
-    if (left >= V) load_floats<V>(p, w);
-    else
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float one[1] = {0.f};
-            if (i < left) load_floats<1>(p + i, one);
-            w[i] = one[0];
+// 16 bytes of a line, of which `left` elements are there, as they come from memory
+template <class T> struct LinePiece {
+    typename Mma<T>::Memory raw;
+    __device__ __forceinline__ void load(const T* __restrict__ p, int left) {
+        if (left >= Mma<T>::VEC) {
+            raw = *reinterpret_cast<const typename Mma<T>::Memory*>(p);
+        } else {
+            const uint4 v = edge_chunk(p, left);
+            __builtin_memcpy(&raw, &v, 16);
         }
-}
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)raw[i] << 16);
+        else return raw[i];
+    }
+};
 
 // What a finished sum becomes: columns n .. n + COUNT - 1 of row r, `left` of them there
 template <class T, int EPI, int COUNT>
@@ -74,19 +81,33 @@ __global__ __launch_bounds__(kRowsBlock) void gated_rows_kernel(RowsArgs<T> g, c
     const int n = (blockIdx.x * g.LN + ln) * V, left = g.N - n;
     const int k0 = blockIdx.y * g.per, k1 = min(k0 + g.per, g.K);
     float acc[S][R][V] = {};
-    auto add = [&](int line, const float (&w)[S][V]) {
+    auto add = [&](int line, const LinePiece<T> (&w)[S]) {
         float f[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) f[r] = factor[line][r];
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int i = 0; i < V; ++i) {
+                const float x = w[s].get(i);
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[s][r][i] += f[r] * w[s][i];
+                for (int r = 0; r < R; ++r) acc[s][r][i] += f[r] * x;
+            }
     };
     for (int base = k0; base < k1; base += kRowsLines) {
         const int lines = min(kRowsLines, k1 - base);
+        const T* __restrict__ p0 = g.W0 + (long)base * g.N + n;
+        const T* __restrict__ p1 = EPI == kGate ? g.W1 + (long)base * g.N + n : nullptr;
+        LinePiece<T> next[U][S];
+        auto load = [&](int from) {                          // lines past the last are the last one
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long at = (long)min(from + u * KG, lines - 1) * g.N;
+                next[u][0].load(p0 + at, left);
+                if constexpr (EPI == kGate) next[u][1].load(p1 + at, left);
+            }
+        };
+        load(kg);                                            // on their way while the factors are laid out
         __syncthreads();
         for (int q = tid; q < lines * R; q += kRowsBlock) {
             const int r = q / lines, line = q % lines;
@@ -95,25 +116,16 @@ __global__ __launch_bounds__(kRowsBlock) void gated_rows_kernel(RowsArgs<T> g, c
             factor[line][r] = one[0];
         }
         __syncthreads();
-        if (left <= 0) continue;
-        const T* __restrict__ p0 = g.W0 + (long)base * g.N + n;
-        const T* __restrict__ p1 = EPI == kGate ? g.W1 + (long)base * g.N + n : nullptr;
-        int line = kg;
-        for (; line + (U - 1) * KG < lines; line += U * KG) {
-            float w[U][S][V];
+        for (int line = kg; line < lines; line += U * KG) {
+            LinePiece<T> now[U][S];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                load_line<T, V>(p0 + (long)(line + u * KG) * g.N, left, w[u][0]);
-                if constexpr (EPI == kGate) load_line<T, V>(p1 + (long)(line + u * KG) * g.N, left, w[u][1]);
-            }
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int u = 0; u < U; ++u) add(line + u * KG, w[u]);
-        }
-        for (; line < lines; line += KG) {
-            float w[S][V];
-            load_line<T, V>(p0 + (long)line * g.N, left, w[0]);
-            if constexpr (EPI == kGate) load_line<T, V>(p1 + (long)line * g.N, left, w[1]);
-            add(line, w);
+                for (int s = 0; s < S; ++s) now[u][s] = next[u][s];
+            if (line + U * KG < lines) load(line + U * KG);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (line + u * KG < lines) add(line + u * KG, now[u]);
         }
     }
     // over the lines' threads, one row and weight at a time
