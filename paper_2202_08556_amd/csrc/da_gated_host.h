@@ -8,6 +8,7 @@
 #include "da_internal.h"
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 namespace daspmm {
@@ -17,7 +18,7 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
 
 // Tile of a product, and how its sum is cut.  A tile of 128 x 128 has the most products for what it reads; tiles of 64 x 64
-// are taken where the larger ones would leave most of the chip idle in their last turn (1531 x 602 out of 1187 float32: 60
+// are taken where the larger ones would leave much of the chip idle in their last turn (1531 x 602 out of 1187 float32: 60
 // large tiles, 240 small ones), and no more rows or columns than there are.  Where even these are fewer than the units, the
 // inner axis is cut, in parts of at least eight tiles of it (sixteen where it makes two parts at most).
 struct GemmPlan {
@@ -33,7 +34,7 @@ template <class T> GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, int segme
     p.BN = 128;
     if (p.BM == 128) {
         if (width <= 64 && epi != kGate) p.BN = 64;
-        else if (4 * ceil_div(tiles(128, 128), cus) > ceil_div(tiles(64, 64), cus)) p.BM = p.BN = 64;
+        else if (10 * ceil_div(tiles(128, 128), cus) > 3 * ceil_div(tiles(64, 64), cus)) p.BM = p.BN = 64;
     } else if (p.BM == 64 && tiles(64, 128) < cus) {
         p.BN = 64;
     }
@@ -69,9 +70,13 @@ void gemm(GemmArgs<T> g, int batches, float* part, hipStream_t s) {
             g.splits = 1;
             g.per = (int)ceil_div(g.K, STEP) * g.segments;
             auto kernel = gated_wide_kernel<ROWS, STEP, STAGES, ALAY, BLAY, EPI>;
-            static const hipError_t allowed =
-                hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
-            (void)allowed;
+            static std::atomic<uint64_t> allowed{0};         // devices that know how much LDS the kernel takes
+            int device = 0;
+            (void)hipGetDevice(&device);
+            const uint64_t bit = 1ull << (device & 63);
+            if (!(allowed.load(std::memory_order_relaxed) & bit) &&
+                hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) == hipSuccess)
+                allowed.fetch_or(bit, std::memory_order_relaxed);
             hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(g.M, ROWS) * ceil_div(width, kWideColumns)), 1, (unsigned)batches),
                                dim3(S::THREADS), S::LDS, s, g);
             return;

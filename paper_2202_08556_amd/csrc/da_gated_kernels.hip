@@ -112,12 +112,37 @@ template <class T> __device__ __forceinline__ uint4 edge_chunk(const T* p, int l
     return r;
 }
 
-// Results of a wave: MT x NT fragments from row m0 on, the j-th at column(j) of the tile that begins at column n0
-template <class T, int MT, int NT, int EPI, class F>
-__device__ __forceinline__ void gated_epilogue(const GemmArgs<T>& g, f32x4 (&acc)[MT][NT], int m0, int n0, int batch, F&& column)
+// Results of a wave, MT x NT fragments from row m0 on, leave by way of LDS (`mine`, the wave's own part), 16 rows at a time:
+// a lane's four neighbours in a row and the 16 rows of a fragment would be 64 bytes of each row at a time, and stores of
+// parts of lines ran at 2.9 TB/s; this way a store is whole lines.  kGate: the first half of the fragments are u, the
+// others v of the same columns.
+template <class T, int MT, int NT, int EPI>
+__device__ __forceinline__ void line_epilogue(const GemmArgs<T>& g, f32x4 (&acc)[MT][NT], char* mine, int m0, int n0, int batch)
 {
-    const int i16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
-    auto store4 = [&](auto* p, int left, const float (&x)[4]) {
+    constexpr int COLS = EPI == kGate ? NT * 8 : NT * 16, PITCH = (NT * 16 + 4) * 4;
+    constexpr int LANES = COLS / 4, ROWS = 64 / LANES, PASSES = 16 / ROWS;    // lanes of a row, rows at once
+    const int lane = threadIdx.x & 63, i16 = lane & 15, h = lane >> 4;
+    const int row0 = lane / LANES, col = lane % LANES * 4, n = n0 + col, left = g.N - n;
+    float u[2][PASSES][4], v[2][PASSES][4];                  // kGateGrad: of the next 16 rows and of these
+    auto load = [&](int i, int to) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int m = m0 + i * 16 + p * ROWS + row0;
+            if (m >= g.M || left <= 0) continue;
+            const long at = (long)m * g.N + n;
+            if (left >= 4) {
+                load_floats<4>(g.U + at, u[to][p]);
+                load_floats<4>(g.V + at, v[to][p]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    u[to][p][q] = q < left ? g.U[at + q] : 0.f;
+                    v[to][p][q] = q < left ? g.V[at + q] : 0.f;
+                }
+            }
+        }
+    };
+    auto store = [&](auto* p, const float (&x)[4]) {
         if (left >= 4) store_floats<4>(p, x);
         else
 #pragma unroll
@@ -126,62 +151,77 @@ __device__ __forceinline__ void gated_epilogue(const GemmArgs<T>& g, f32x4 (&acc
                 if (q < left) store_floats<1>(p + q, one);
             }
     };
-    constexpr int COLS = EPI == kGate ? NT / 2 : NT;
+    if constexpr (EPI == kGateGrad) load(0, 0);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        if constexpr (EPI == kGateGrad) {
+            if (i + 1 < MT) load(i + 1, (i + 1) & 1);
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4*>(mine + i16 * PITCH + (j * 16 + h * 4) * 4) = acc[i][j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");               // LDS serves a wave in order
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int row = p * ROWS + row0, m = m0 + i * 16 + row;
+            float x[4];
+            load_floats<4>(reinterpret_cast<const float*>(mine + row * PITCH) + col, x);
+            float w[4];
+            if constexpr (EPI == kGate) load_floats<4>(reinterpret_cast<const float*>(mine + row * PITCH) + COLS + col, w);
+            if (m >= g.M || left <= 0) continue;
+            const long at = (long)m * g.N + n;
+            if constexpr (EPI == kStore) {
+                store((batch ? g.C[1] : g.C[0]) + at, x);
+            } else if constexpr (EPI == kGate) {
+                if (g.U) {
+                    store(g.U + at, x);
+                    store(g.V + at, w);
+                }
+                act_values(g.act, x);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] *= w[q];
+                store(g.C[0] + at, x);
+            } else {
+                float (&uu)[4] = u[i & 1][p], (&vv)[4] = v[i & 1][p], slope[4];
+                act_both(g.act, uu, slope);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    vv[q] *= x[q] * slope[q];
+                    x[q] *= uu[q];
+                }
+                store(g.C[0] + at, vv);
+                store(g.C[1] + at, x);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// A part of a sum: MT x NT fragments of a wave from row m0 on, the j-th at column(j) of the tile that begins at column n0
+template <class T, int MT, int NT, int EPI, class F>
+__device__ __forceinline__ void part_epilogue(const GemmArgs<T>& g, f32x4 (&acc)[MT][NT], int m0, int n0, int batch, F&& column)
+{
+    const int i16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
+    const long width = EPI == kGate ? 2L * g.N : g.N;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int m = m0 + i * 16 + i16;
         if (m >= g.M) continue;
+        float* __restrict__ row = g.part + (((long)batch * g.splits + blockIdx.y) * g.M + m) * width;
 #pragma unroll
-        for (int j = 0; j < COLS; ++j) {
-            const int n = n0 + column(j) + 4 * h, left = g.N - n;
-            if (left <= 0) continue;
-            const long at = (long)m * g.N + n;
+        for (int j = 0; j < NT; ++j) {
+            const bool up = EPI == kGate && j >= NT / 2;
+            const int n = n0 + column(up ? j - NT / 2 : j) + 4 * h, left = g.N - n;
+            float* __restrict__ p = row + (up ? g.N : 0) + n;
             float x[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) x[q] = acc[i][j][q];
-            if (g.splits > 1) {
-                const long width = EPI == kGate ? 2L * g.N : g.N;
-                float* p = g.part + (((long)batch * g.splits + blockIdx.y) * g.M + m) * width + n;
-                store4(p, left, x);
-                if constexpr (EPI == kGate) {
-                    float v[4];
+            if (left >= 4) store_floats<4>(p, x);
+            else
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] = acc[i][j + NT / 2][q];
-                    store4(p + g.N, left, v);
-                }
-            } else if constexpr (EPI == kStore) {
-                store4((batch ? g.C[1] : g.C[0]) + at, left, x);
-            } else if constexpr (EPI == kGate) {
-                float v[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = acc[i][j + NT / 2][q];
-                if (g.U) {
-                    store4(g.U + at, left, x);
-                    store4(g.V + at, left, v);
-                }
-                act_values(g.act, x);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) x[q] *= v[q];
-                store4(g.C[0] + at, left, x);
-            } else {
-                float u[4] = {}, v[4] = {}, slope[4];
-                if (left >= 4) {
-                    load_floats<4>(g.U + at, u);
-                    load_floats<4>(g.V + at, v);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (q < left) { u[q] = g.U[at + q]; v[q] = g.V[at + q]; }
-                }
-                act_both(g.act, u, slope);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[q] *= x[q] * slope[q];
-                    x[q] *= u[q];
-                }
-                store4(g.C[0] + at, left, v);
-                store4(g.C[1] + at, left, x);
-            }
+                for (int q = 0; q < 4; ++q)
+                    if (q < left) p[q] = x[q];
         }
     }
 }
@@ -341,7 +381,13 @@ __global__ __launch_bounds__(64 * WM * WN) void gated_gemm_kernel(GemmArgs<T> g)
         __syncthreads();
     }
 
-    gated_epilogue<T, MT, NT, EPI>(g, acc, m0 + wm * MT * 16, n0, batch, column);
+    if (g.splits > 1) {
+        part_epilogue<T, MT, NT, EPI>(g, acc, m0 + wm * MT * 16, n0, batch, column);
+    } else {
+        constexpr int MINE = 16 * (NT * 16 + 4) * 4;         // 16 rows of a wave
+        static_assert(MINE * WM * WN <= sizeof(lds), "all waves' rows");
+        line_epilogue<T, MT, NT, EPI>(g, acc, lds[0] + wave * MINE, m0 + wm * MT * 16, n0 + column(0), batch);
+    }
 }
 
 // Sums the parts of a product and does what its epilogue would have done; a thread owns one number.

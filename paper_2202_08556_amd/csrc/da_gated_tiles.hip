@@ -100,92 +100,6 @@ template <int N> __device__ __forceinline__ void wait_for_loads() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
-// Results of a wave, MT x NT fragments from row m0 on, leave by way of LDS (`mine`, the wave's own part), 16 rows at a time:
-// a lane's four neighbours in a row and the 16 rows of a fragment would be 64 bytes of each row at a time, and stores of
-// parts of lines ran at 2.9 TB/s; this way a store is whole lines.  kGate: the first half of the fragments are u, the
-// others v of the same columns.
-template <int MT, int NT, int EPI>
-__device__ __forceinline__ void wide_epilogue(const GemmArgs<bf16>& g, f32x4 (&acc)[MT][NT], char* mine, int m0, int n0, int batch)
-{
-    constexpr int COLS = EPI == kGate ? NT * 8 : NT * 16, PITCH = (NT * 16 + 4) * 4;
-    constexpr int LANES = COLS / 4, ROWS = 64 / LANES, PASSES = 16 / ROWS;    // lanes of a row, rows at once
-    const int lane = threadIdx.x & 63, i16 = lane & 15, h = lane >> 4;
-    const int row0 = lane / LANES, col = lane % LANES * 4, n = n0 + col, left = g.N - n;
-    float u[2][PASSES][4], v[2][PASSES][4];                  // kGateGrad: of the next 16 rows and of these
-    auto load = [&](int i, int to) {
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int m = m0 + i * 16 + p * ROWS + row0;
-            if (m >= g.M || left <= 0) continue;
-            const long at = (long)m * g.N + n;
-            if (left >= 4) {
-                load_floats<4>(g.U + at, u[to][p]);
-                load_floats<4>(g.V + at, v[to][p]);
-            } else {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    u[to][p][q] = q < left ? g.U[at + q] : 0.f;
-                    v[to][p][q] = q < left ? g.V[at + q] : 0.f;
-                }
-            }
-        }
-    };
-    auto store = [&](auto* p, const float (&x)[4]) {
-        if (left >= 4) store_floats<4>(p, x);
-        else
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float one[1] = {x[q]};
-                if (q < left) store_floats<1>(p + q, one);
-            }
-    };
-    if constexpr (EPI == kGateGrad) load(0, 0);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        if constexpr (EPI == kGateGrad) {
-            if (i + 1 < MT) load(i + 1, (i + 1) & 1);
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4*>(mine + i16 * PITCH + (j * 16 + h * 4) * 4) = acc[i][j];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");               // LDS serves a wave in order
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int row = p * ROWS + row0, m = m0 + i * 16 + row;
-            float x[4];
-            load_floats<4>(reinterpret_cast<const float*>(mine + row * PITCH) + col, x);
-            float w[4];
-            if constexpr (EPI == kGate) load_floats<4>(reinterpret_cast<const float*>(mine + row * PITCH) + COLS + col, w);
-            if (m >= g.M || left <= 0) continue;
-            const long at = (long)m * g.N + n;
-            if constexpr (EPI == kStore) {
-                store((batch ? g.C[1] : g.C[0]) + at, x);
-            } else if constexpr (EPI == kGate) {
-                if (g.U) {
-                    store(g.U + at, x);
-                    store(g.V + at, w);
-                }
-                act_values(g.act, x);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) x[q] *= w[q];
-                store(g.C[0] + at, x);
-            } else {
-                float (&uu)[4] = u[i & 1][p], (&vv)[4] = v[i & 1][p], slope[4];
-                act_both(g.act, uu, slope);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    vv[q] *= x[q] * slope[q];
-                    x[q] *= uu[q];
-                }
-                store(g.C[0] + at, vv);
-                store(g.C[1] + at, x);
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
-}
-
 // A is one tile; B is one of 256 columns, or one of 128 of each of the two weights whose products the epilogue joins
 // (kGate, lines along the outer axis).
 // A wave has 128 x 64 results, or 64 x 128 (kGate: 64 x 64 of both), so that 64 columns of a row leave together.
@@ -310,7 +224,7 @@ __global__ __launch_bounds__(ROWS * 2) __attribute__((amdgpu_waves_per_eu(2, 2))
     __syncthreads();                                         // LDS is free
     constexpr int MINE = S::LDS / (THREADS / 64);
     static_assert(MINE >= 16 * (NT * 16 + 4) * 4, "16 rows of a wave");
-    wide_epilogue<MT, NT, EPI>(g, acc, lds + wave * MINE, m0 + wm * MT * 16, n0 + wn * (EPI == kGate ? NT * 8 : NT * 16), batch);
+    line_epilogue<bf16, MT, NT, EPI>(g, acc, lds + wave * MINE, m0 + wm * MT * 16, n0 + wn * (EPI == kGate ? NT * 8 : NT * 16), batch);
 }
 
 }  // namespace daspmm

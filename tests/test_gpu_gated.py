@@ -299,3 +299,33 @@ def test_large_products(T, d, h):
 @pytest.mark.parametrize("d,h,dout", [(1000, 2049, 77), (64, 100, 5000), (3, 7, 1), (2100, 64, 4096)])
 def test_few_rows(T, d, h, dout, dtype):
     run(*inputs(T, d, h, dout, dtype, seed=T + d))
+
+
+def test_large_products_in_a_graph_and_bad_numbers():
+    """The kernels for large products: captured and replayed on other numbers, twice bit for bit, NaN kept to its row."""
+    x, wg, wu, wd, dy = inputs(4096, 1024, 4096, 1024, torch.bfloat16, seed=11)
+    leaves = [t.requires_grad_(True) for t in (x, wg, wu, wd)]
+
+    def once():
+        y = layers.gated_feed_forward(*leaves)
+        return [y.detach(), *torch.autograd.grad(y, leaves, dy)]
+
+    first = once()
+    assert all(torch.equal(p, q) for p, q in zip(first, once()))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = once()
+    for k in range(3):
+        with torch.no_grad():
+            x.mul_(-0.5).add_(0.1 * k)
+        want = once()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), k
+    clean = layers.gated_feed_forward(*leaves).detach()
+    with torch.no_grad():
+        x[1234, 5] = float("nan")
+    y = layers.gated_feed_forward(*leaves).detach()
+    keep = torch.arange(4096, device="cuda") != 1234
+    assert torch.isnan(y[1234]).all() and torch.equal(y[keep], clean[keep])
