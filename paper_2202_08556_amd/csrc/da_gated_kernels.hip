@@ -8,6 +8,11 @@
 // everywhere but in the weights' gradients, the weights in products with their transposes) or lines of neighbouring
 // outer ones.  Both are copied to LDS line by line; the second kind is turned around on the way to the registers (for
 // bf16 by the transposing LDS read, for float by reading single numbers).
+//
+// Forward, 8192 x 2048 x 4096 float32: 126 TFLOP/s (the fp32 matrix cores give the general library 154 on large products);
+// 2000 x 512 x 2048 bf16, tiles of 128 x 128 and 64 x 64: 285.  A tile's next step waits in registers while this one is
+// multiplied; with one block to a compute unit its latency shows, with several they fill each other's gaps.  (Four waves of
+// 64 x 64 for a tile of 128 x 128 instead of eight of 32 x 64: 546 us instead of 521 for 100 003 x 64 x 256 float32, both ways.)
 #pragma once
 #include "da_layer_common.h"
 
