@@ -46,9 +46,32 @@ template <class T> GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, int segme
     return p;
 }
 
-template <class T> size_t part_bytes(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi) {
-    const GemmPlan p = gemm_plan<T>(M, N, K, segments, batches, epi);
-    return p.splits > 1 ? (size_t)batches * p.splits * M * N * (epi == kGate ? 2 : 1) * sizeof(float) : 0;
+// bfloat16, where the tiles' loads may be of whole pieces: 256 x 256 where there are enough tiles of it, otherwise 128 x 256,
+// two blocks to a compute unit, where these are enough (33558 x 216 x 984 forward: 134 us with the smaller tiles, 107 so).
+// Up to 128 rows the weights' stream is the bound: the inner axis is cut in parts of 512 positions and more until the chip
+// is full (79 x 2168 x 9560 forward: 102 and 66 us).  Cutting other products cost more than it gave (backward of 1024 x 1024 x
+// 4096: 200 and 248 us both ways).
+struct WidePlan {
+    int rows;                    // 256, 128; 0: not taken
+    int splits;
+};
+
+// few: the outer positions are rows of the input, not a weight's
+inline WidePlan wide_plan(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi, bool few) {
+    const int64_t width = epi == kGate ? 2 * N : N, cus = compute_units();
+    auto tiles = [&](int64_t rows) { return ceil_div(M, rows) * ceil_div(width, kWideColumns) * batches; };
+    if (tiles(256) >= cus) return WidePlan{256, 1};
+    const int64_t count = tiles(128);
+    if (count >= cus) return WidePlan{128, 1};
+    const int64_t splits = std::max<int64_t>(1, std::min(2 * cus / count, K * segments / 512));
+    return few && M > 16 && M <= 128 && count * splits >= cus ? WidePlan{128, (int)splits} : WidePlan{0, 1};
+}
+
+template <class T> size_t part_bytes(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi, bool few) {
+    if (M == 0 || N == 0) return 0;
+    int splits = gemm_plan<T>(M, N, K, segments, batches, epi).splits;
+    if constexpr (std::is_same_v<T, bf16>) splits = std::max(splits, wide_plan(M, N, K, segments, batches, epi, few).splits);
+    return splits > 1 ? (size_t)batches * splits * M * N * (epi == kGate ? 2 : 1) * sizeof(float) : 0;
 }
 
 // Whether the tiles of 256 x 256 take a product: their loads are of 16 bytes at addresses that are multiples of it
@@ -58,34 +81,45 @@ template <int ALAY, int BLAY> bool wide_takes(const GemmArgs<bf16>& g) {
            whole(g.B[0]) && whole(g.B[1]) && (ALAY == kInner || g.M % 8 == 0) && (BLAY == kInner || g.N % 8 == 0);
 }
 
+template <class T, int EPI> void join_parts(const GemmArgs<T>& g, int batches, hipStream_t s) {
+    if (g.splits == 1) return;
+    const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.M * g.N, 256), 16384);
+    hipLaunchKernelGGL((gated_join_kernel<T, EPI>), dim3((unsigned)blocks, 1, (unsigned)batches), dim3(256), 0, s, g);
+}
+
+template <int ROWS, int STEP, int STAGES, int ALAY, int BLAY, int EPI>
+void wide_gemm(GemmArgs<bf16> g, int batches, int splits, hipStream_t s) {
+    typedef WideShape<ROWS, STEP, STAGES> S;
+    const int64_t width = EPI == kGate ? 2 * (int64_t)g.N : g.N, inner = ceil_div(g.K, STEP) * g.segments;
+    g.per = (int)std::max<int64_t>(1, ceil_div(inner, splits));
+    g.splits = (int)std::max<int64_t>(1, ceil_div(inner, g.per));
+    auto kernel = gated_wide_kernel<ROWS, STEP, STAGES, ALAY, BLAY, EPI>;
+    static std::atomic<uint64_t> allowed{0};                 // devices that know how much LDS the kernel takes
+    int device = 0;
+    (void)hipGetDevice(&device);
+    const uint64_t bit = 1ull << (device & 63);
+    if (!(allowed.load(std::memory_order_relaxed) & bit) &&
+        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) == hipSuccess)
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(g.M, ROWS) * ceil_div(width, kWideColumns)), (unsigned)g.splits, (unsigned)batches),
+                       dim3(S::THREADS), S::LDS, s, g);
+    join_parts<bf16, EPI>(g, batches, s);
+}
+
 template <class T, int ALAY, int BLAY, int EPI>
 void gemm(GemmArgs<T> g, int batches, float* part, hipStream_t s) {
     if (g.M == 0 || g.N == 0) return;
+    g.part = part;
     if constexpr (std::is_same_v<T, bf16>) {
-        constexpr int ROWS = 256, STEP = 64, STAGES = 2;
-        const int64_t width = EPI == kGate ? 2 * (int64_t)g.N : g.N;
-        const int64_t tiles = ceil_div(g.M, ROWS) * ceil_div(width, kWideColumns) * batches;
-        if (tiles >= compute_units() && wide_takes<ALAY, BLAY>(g)) {
-            typedef WideShape<ROWS, STEP, STAGES> S;
-            g.splits = 1;
-            g.per = (int)ceil_div(g.K, STEP) * g.segments;
-            auto kernel = gated_wide_kernel<ROWS, STEP, STAGES, ALAY, BLAY, EPI>;
-            static std::atomic<uint64_t> allowed{0};         // devices that know how much LDS the kernel takes
-            int device = 0;
-            (void)hipGetDevice(&device);
-            const uint64_t bit = 1ull << (device & 63);
-            if (!(allowed.load(std::memory_order_relaxed) & bit) &&
-                hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) == hipSuccess)
-                allowed.fetch_or(bit, std::memory_order_relaxed);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(g.M, ROWS) * ceil_div(width, kWideColumns)), 1, (unsigned)batches),
-                               dim3(S::THREADS), S::LDS, s, g);
-            return;
+        const WidePlan w = wide_plan(g.M, g.N, g.K, g.segments, batches, EPI, ALAY == kInner);
+        if (w.rows && wide_takes<ALAY, BLAY>(g)) {
+            if (w.rows == 256) return wide_gemm<256, 64, 2, ALAY, BLAY, EPI>(g, batches, 1, s);
+            return wide_gemm<128, 32, 3, ALAY, BLAY, EPI>(g, batches, w.splits, s);
         }
     }
     const GemmPlan p = gemm_plan<T>(g.M, g.N, g.K, g.segments, batches, EPI);
     g.splits = p.splits;
     g.per = p.per;
-    g.part = part;
     const int64_t width = EPI == kGate ? 2 * (int64_t)g.N : g.N;
     const dim3 grid((unsigned)(ceil_div(g.M, p.BM) * ceil_div(width, p.BN)), (unsigned)p.splits, (unsigned)batches);
     auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, g); };
@@ -97,10 +131,7 @@ void gemm(GemmArgs<T> g, int batches, float* part, hipStream_t s) {
     if constexpr (EPI != kGate) {
         if (p.BM == 128 && p.BN == 64) go(gated_gemm_kernel<T, 2, 4, 4, 1, ALAY, BLAY, EPI>, 256);
     }
-    if (p.splits > 1) {
-        const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.M * g.N, 256), 16384);
-        hipLaunchKernelGGL((gated_join_kernel<T, EPI>), dim3((unsigned)blocks, 1, (unsigned)batches), dim3(256), 0, s, g);
-    }
+    join_parts<T, EPI>(g, batches, s);
 }
 
 // Few rows, forward
@@ -152,14 +183,14 @@ template <class T, class TX, int EPI> void rows_product(RowsArgs<T> g, const TX*
 
 template <class T> size_t gated_forward_bytes(const GatedShape& s) {
     if (s.rows <= kRowsMost) return rows_part_bytes<T>(s) + round16((size_t)(s.rows * s.h) * sizeof(float));
-    return std::max(part_bytes<T>(s.rows, s.h, s.d, 1, 1, kGate), part_bytes<T>(s.rows, s.dout, s.h, 1, 1, kStore));
+    return std::max(part_bytes<T>(s.rows, s.h, s.d, 1, 1, kGate, true), part_bytes<T>(s.rows, s.dout, s.h, 1, 1, kStore, true));
 }
 
 template <class T> size_t gated_backward_bytes(const GatedShape& s) {
-    size_t part = part_bytes<T>(s.rows, s.h, s.dout, 1, 1, kGateGrad);
-    part = std::max(part, part_bytes<T>(s.rows, s.d, s.h, 2, 1, kStore));
-    part = std::max(part, part_bytes<T>(s.d, s.h, s.rows, 1, 2, kStore));
-    part = std::max(part, part_bytes<T>(s.h, s.dout, s.rows, 1, 1, kStore));
+    size_t part = part_bytes<T>(s.rows, s.h, s.dout, 1, 1, kGateGrad, true);
+    part = std::max(part, part_bytes<T>(s.rows, s.d, s.h, 2, 1, kStore, true));
+    part = std::max(part, part_bytes<T>(s.d, s.h, s.rows, 1, 2, kStore, false));
+    part = std::max(part, part_bytes<T>(s.h, s.dout, s.rows, 1, 1, kStore, false));
     return 2 * round16((size_t)(s.rows * s.h) * sizeof(T)) + part;
 }
 

@@ -1,4 +1,5 @@
-// Large products of the gated feed-forward block in bfloat16: tiles of 256 x 256 of 8 waves.
+// Large products of the gated feed-forward block in bfloat16: tiles of 256 x 256 of 8 waves (and, where these are too few,
+// of 128 x 256 of 4, in steps of 32, three of them in LDS).
 //
 // The inner axis goes by in steps of 64, two of them in LDS (2 x 64 KB).  The data of a step goes from memory to LDS without
 // passing registers (16 bytes a lane, whole lines of memory), asked for a step before it is used, so that one barrier a
@@ -220,6 +221,10 @@ __global__ __launch_bounds__(ROWS * 2) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[i][j] = Mma<bf16>::mul(b[j], a[i], acc[i][j]);
         }
+    }
+    if (g.splits > 1) {
+        part_epilogue<bf16, MT, NT, EPI>(g, acc, m0 + wm * MT * 16, n0, batch, column);
+        return;
     }
     __syncthreads();                                         // LDS is free
     constexpr int MINE = S::LDS / (THREADS / 64);

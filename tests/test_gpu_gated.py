@@ -329,3 +329,12 @@ def test_large_products_in_a_graph_and_bad_numbers():
     y = layers.gated_feed_forward(*leaves).detach()
     keep = torch.arange(4096, device="cuda") != 1234
     assert torch.isnan(y[1234]).all() and torch.equal(y[keep], clean[keep])
+
+
+# bfloat16 tiles of 128 x 256: enough of them without 256 x 256, and few rows with the inner axis cut
+@pytest.mark.parametrize("T,d,h", [(20003, 216, 984), (79, 2168, 9560), (17, 1032, 8200), (128, 4096, 4104), (100, 3080, 5000)])
+def test_middle_products(T, d, h):
+    args = inputs(T, d, h, d, torch.bfloat16, seed=T)
+    first = run(*args)
+    again = run(*args)
+    assert all(torch.equal(first[k], again[k]) for k in first)
