@@ -1,14 +1,12 @@
 // The gated feed-forward block between its translation units: one for each type, and the C entry points.
 #pragma once
+#include "da_gated_plan.h"
+
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
 
 namespace daspmm {
-
-struct GatedShape {
-    int64_t rows, d, h, dout;
-};
 
 // Everything of one call; what a direction does not use is null.
 struct GatedCall {

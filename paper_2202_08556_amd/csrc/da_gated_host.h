@@ -1,10 +1,11 @@
-// Products of the gated feed-forward block: tiles, parts of the sums, launches.  Included by one translation unit for
+// Products of the gated feed-forward block: operands and launches (da_gated_plan.h cuts them).  Included by one translation unit for
 // each type.
 #pragma once
 #include "da_gated.h"
 #include "da_gated_kernels.hip"
 #include "da_gated_rows.hip"
 #include "da_gated_tiles.hip"
+#include "da_gated_plan.h"
 #include "da_internal.h"
 
 #include <algorithm>
@@ -13,66 +14,6 @@
 
 namespace daspmm {
 namespace {
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
-
-// Tile of a product, and how its sum is cut.  A tile of 128 x 128 has the most products for what it reads; tiles of 64 x 64
-// are taken where the larger ones would leave much of the chip idle in their last turn (1531 x 602 out of 1187 float32: 60
-// large tiles, 240 small ones), and no more rows or columns than there are.  Where even these are fewer than the units, the
-// inner axis is cut, in parts of at least eight tiles of it (sixteen where it makes two parts at most).
-struct GemmPlan {
-    int BM, BN;
-    int splits, per;
-};
-
-template <class T> GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi) {
-    GemmPlan p{};
-    const int64_t width = epi == kGate ? 2 * N : N, cus = compute_units();
-    auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(M, bm) * ceil_div(width, bn) * batches; };
-    p.BM = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    p.BN = 128;
-    if (p.BM == 128) {
-        if (width <= 64 && epi != kGate) p.BN = 64;
-        else if (10 * ceil_div(tiles(128, 128), cus) > 3 * ceil_div(tiles(64, 64), cus)) p.BM = p.BN = 64;
-    } else if (p.BM == 64 && tiles(64, 128) < cus) {
-        p.BN = 64;
-    }
-    const int64_t count = tiles(p.BM, p.BN), inner = ceil_div(K, kLineBytes / (int64_t)sizeof(T)) * segments;
-    int64_t splits = 1;
-    if (count <= cus) splits = std::min(2 * cus / std::max<int64_t>(count, 1), std::max<int64_t>(1, inner / (2 * count <= cus ? 8 : 16)));
-    p.per = (int)std::max<int64_t>(1, ceil_div(inner, std::max<int64_t>(splits, 1)));
-    p.splits = (int)std::max<int64_t>(1, ceil_div(inner, p.per));
-    return p;
-}
-
-// bfloat16, where the tiles' loads may be of whole pieces: 256 x 256 where there are enough tiles of it, otherwise 128 x 256,
-// two blocks to a compute unit, where these are enough (33558 x 216 x 984 forward: 134 us with the smaller tiles, 107 so).
-// Up to 128 rows the weights' stream is the bound: the inner axis is cut in parts of 512 positions and more until the chip
-// is full (79 x 2168 x 9560 forward: 102 and 66 us).  Cutting other products cost more than it gave (backward of 1024 x 1024 x
-// 4096: 200 and 248 us both ways).
-struct WidePlan {
-    int rows;                    // 256, 128; 0: not taken
-    int splits;
-};
-
-// few: the outer positions are rows of the input, not a weight's
-inline WidePlan wide_plan(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi, bool few) {
-    const int64_t width = epi == kGate ? 2 * N : N, cus = compute_units();
-    auto tiles = [&](int64_t rows) { return ceil_div(M, rows) * ceil_div(width, kWideColumns) * batches; };
-    if (tiles(256) >= cus) return WidePlan{256, 1};
-    const int64_t count = tiles(128);
-    if (count >= cus) return WidePlan{128, 1};
-    const int64_t splits = std::max<int64_t>(1, std::min(2 * cus / count, K * segments / 512));
-    return few && M > 16 && M <= 128 && count * splits >= cus ? WidePlan{128, (int)splits} : WidePlan{0, 1};
-}
-
-template <class T> size_t part_bytes(int64_t M, int64_t N, int64_t K, int segments, int batches, int epi, bool few) {
-    if (M == 0 || N == 0) return 0;
-    int splits = gemm_plan<T>(M, N, K, segments, batches, epi).splits;
-    if constexpr (std::is_same_v<T, bf16>) splits = std::max(splits, wide_plan(M, N, K, segments, batches, epi, few).splits);
-    return splits > 1 ? (size_t)batches * splits * M * N * (epi == kGate ? 2 : 1) * sizeof(float) : 0;
-}
 
 // Whether the tiles of 256 x 256 take a product: their loads are of 16 bytes at addresses that are multiples of it
 template <int ALAY, int BLAY> bool wide_takes(const GemmArgs<bf16>& g) {
@@ -106,18 +47,24 @@ void wide_gemm(GemmArgs<bf16> g, int batches, int splits, hipStream_t s) {
     join_parts<bf16, EPI>(g, batches, s);
 }
 
+// `part` holds what part_bytes() says of the product
 template <class T, int ALAY, int BLAY, int EPI>
-void gemm(GemmArgs<T> g, int batches, float* part, hipStream_t s) {
-    if (g.M == 0 || g.N == 0) return;
+void gemm(GemmArgs<T> g, const Product& product, float* part, hipStream_t s) {
+    if (product.M == 0 || product.N == 0) return;
+    const int batches = product.batches;
+    g.M = (int)product.M;
+    g.N = (int)product.N;
+    g.K = (int)product.K;
+    g.segments = product.segments;
     g.part = part;
     if constexpr (std::is_same_v<T, bf16>) {
-        const WidePlan w = wide_plan(g.M, g.N, g.K, g.segments, batches, EPI, ALAY == kInner);
+        const WidePlan w = wide_plan(product);
         if (w.rows && wide_takes<ALAY, BLAY>(g)) {
             if (w.rows == 256) return wide_gemm<256, 64, 2, ALAY, BLAY, EPI>(g, batches, 1, s);
             return wide_gemm<128, 32, 3, ALAY, BLAY, EPI>(g, batches, w.splits, s);
         }
     }
-    const GemmPlan p = gemm_plan<T>(g.M, g.N, g.K, g.segments, batches, EPI);
+    const GemmPlan p = gemm_plan(product, sizeof(T));
     g.splits = p.splits;
     g.per = p.per;
     const int64_t width = EPI == kGate ? 2 * (int64_t)g.N : g.N;
@@ -183,15 +130,11 @@ template <class T, class TX, int EPI> void rows_product(RowsArgs<T> g, const TX*
 
 template <class T> size_t gated_forward_bytes(const GatedShape& s) {
     if (s.rows <= kRowsMost) return rows_part_bytes<T>(s) + round16((size_t)(s.rows * s.h) * sizeof(float));
-    return std::max(part_bytes<T>(s.rows, s.h, s.d, 1, 1, kGate, true), part_bytes<T>(s.rows, s.dout, s.h, 1, 1, kStore, true));
+    return std::max(part_bytes(gate_product(s), sizeof(T)), part_bytes(down_product(s), sizeof(T)));
 }
 
 template <class T> size_t gated_backward_bytes(const GatedShape& s) {
-    size_t part = part_bytes<T>(s.rows, s.h, s.dout, 1, 1, kGateGrad, true);
-    part = std::max(part, part_bytes<T>(s.rows, s.d, s.h, 2, 1, kStore, true));
-    part = std::max(part, part_bytes<T>(s.d, s.h, s.rows, 1, 2, kStore, false));
-    part = std::max(part, part_bytes<T>(s.h, s.dout, s.rows, 1, 1, kStore, false));
-    return 2 * round16((size_t)(s.rows * s.h) * sizeof(T)) + part;
+    return 2 * round16((size_t)(s.rows * s.h) * sizeof(T)) + backward_part_bytes(s, sizeof(T));
 }
 
 template <class T> void gated_forward(const GatedCall& c) {
@@ -228,31 +171,23 @@ template <class T> void gated_forward(const GatedCall& c) {
     g.B[1] = static_cast<const T*>(c.wu);
     g.lda = c.ldx;
     g.ldb = h;
-    g.M = rows;
-    g.N = h;
-    g.K = d;
-    g.segments = 1;
     g.C[0] = static_cast<T*>(c.a);
     g.U = c.u;
     g.V = c.v;
     g.act = c.act;
-    gemm<T, kInner, kOuter, kGate>(g, 1, part, c.stream);
+    gemm<T, kInner, kOuter, kGate>(g, gate_product(c.s), part, c.stream);
 
     g = GemmArgs<T>{};
     g.A[0] = g.A[1] = static_cast<const T*>(c.a);
     g.B[0] = g.B[1] = static_cast<const T*>(c.wd);
     g.lda = h;
     g.ldb = dout;
-    g.M = rows;
-    g.N = dout;
-    g.K = h;
-    g.segments = 1;
     g.C[0] = static_cast<T*>(c.y);
-    gemm<T, kInner, kOuter, kStore>(g, 1, part, c.stream);
+    gemm<T, kInner, kOuter, kStore>(g, down_product(c.s), part, c.stream);
 }
 
 template <class T> void gated_backward(const GatedCall& c) {
-    const int rows = (int)c.s.rows, d = (int)c.s.d, h = (int)c.s.h, dout = (int)c.s.dout;
+    const int h = (int)c.s.h, dout = (int)c.s.dout;
     const size_t hidden = round16((size_t)(c.s.rows * c.s.h) * sizeof(T));
     T* du = reinterpret_cast<T*>(c.workspace);
     T* dv = reinterpret_cast<T*>(c.workspace + hidden);
@@ -263,16 +198,12 @@ template <class T> void gated_backward(const GatedCall& c) {
         g.B[0] = g.B[1] = static_cast<const T*>(c.wd);
         g.lda = c.ldy;
         g.ldb = dout;
-        g.M = rows;
-        g.N = h;
-        g.K = dout;
-        g.segments = 1;
         g.C[0] = du;
         g.C[1] = dv;
         g.U = c.u;
         g.V = c.v;
         g.act = c.act;
-        gemm<T, kInner, kInner, kGateGrad>(g, 1, part, c.stream);
+        gemm<T, kInner, kInner, kGateGrad>(g, hidden_grad_product(c.s), part, c.stream);
     }
     if (c.dx) {
         g = GemmArgs<T>{};
@@ -282,12 +213,8 @@ template <class T> void gated_backward(const GatedCall& c) {
         g.B[1] = static_cast<const T*>(c.wu);
         g.lda = h;
         g.ldb = h;
-        g.M = rows;
-        g.N = d;
-        g.K = h;
-        g.segments = 2;
         g.C[0] = static_cast<T*>(c.dx);
-        gemm<T, kInner, kInner, kStore>(g, 1, part, c.stream);
+        gemm<T, kInner, kInner, kStore>(g, input_grad_product(c.s), part, c.stream);
     }
     if (c.dwg || c.dwu) {
         const int first = c.dwg ? 0 : 1, batches = c.dwg && c.dwu ? 2 : 1;
@@ -299,13 +226,9 @@ template <class T> void gated_backward(const GatedCall& c) {
         g.B[1] = dv;
         g.lda = c.ldx;
         g.ldb = h;
-        g.M = d;
-        g.N = h;
-        g.K = rows;
-        g.segments = 1;
         g.C[0] = static_cast<T*>(to[first]);
         g.C[1] = static_cast<T*>(c.dwu);
-        gemm<T, kOuter, kOuter, kStore>(g, batches, part, c.stream);
+        gemm<T, kOuter, kOuter, kStore>(g, up_grad_product(c.s, batches), part, c.stream);
     }
     if (c.dwd) {
         g = GemmArgs<T>{};
@@ -313,12 +236,8 @@ template <class T> void gated_backward(const GatedCall& c) {
         g.B[0] = g.B[1] = static_cast<const T*>(c.dy);
         g.lda = h;
         g.ldb = c.ldy;
-        g.M = h;
-        g.N = dout;
-        g.K = rows;
-        g.segments = 1;
         g.C[0] = static_cast<T*>(c.dwd);
-        gemm<T, kOuter, kOuter, kStore>(g, 1, part, c.stream);
+        gemm<T, kOuter, kOuter, kStore>(g, down_grad_product(c.s), part, c.stream);
     }
 }
 

@@ -14,6 +14,7 @@
 // multiplied; with one block to a compute unit its latency shows, with several they fill each other's gaps.  (Four waves of
 // 64 x 64 for a tile of 128 x 128 instead of eight of 32 x 64: 546 us instead of 521 for 100 003 x 64 x 256 float32, both ways.)
 #pragma once
+#include "da_gated_plan.h"
 #include "da_layer_common.h"
 
 namespace daspmm {
@@ -23,7 +24,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 enum { kInner = 0, kOuter = 1 };             // what neighbours in memory
-enum { kStore = 0, kGate = 1, kGateGrad = 2 };
 
 // 16 bytes a lane are a fragment: 8 bf16, one instruction of 16 x 16 x 32, or 4 floats, four of 16 x 16 x 4 (element j
 // of all lanes is one instruction: any assignment of inner positions to instructions gives the same sum).
@@ -59,8 +59,6 @@ template <class T> struct GemmArgs {
     float* part;                 // splits > 1: [batch][split][M][N] sums, of u and v side by side for kGate
     int act;
 };
-
-constexpr int kLineBytes = 128;  // of the inner axis in a tile
 
 // One operand's tile: OUTER outer positions x kLineBytes of the inner axis
 template <class T, int LAY, int OUTER> struct Tile {

@@ -16,8 +16,6 @@
 
 namespace daspmm {
 
-constexpr int kWideColumns = 256;
-
 // Shape of a block: ROWS x 256 results, STAGES steps of STEP inner positions in LDS, a wave to every 8192 results
 template <int ROWS, int STEP, int STAGES> struct WideShape {
     static constexpr int THREADS = ROWS * 2, A_BYTES = ROWS * STEP * 2, B_BYTES = kWideColumns * STEP * 2;

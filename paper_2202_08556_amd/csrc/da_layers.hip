@@ -23,8 +23,6 @@ int launched(const char* where) {
 
 bool known_dtype(int d) { return d == DA_F32 || d == DA_BF16; }
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int pow2_at_least(int64_t x) {
     int p = 1;
     while (p < x) p <<= 1;

@@ -338,3 +338,18 @@ def test_middle_products(T, d, h):
     first = run(*args)
     again = run(*args)
     assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+# one of w_gate and w_up by itself where its product's sum is cut further than that of both together, and nothing else that
+# the backward pass computes needs as much scratch memory
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,d,h,dout", [(8192, 1024, 4096, 7), (1000, 216, 4096, 1), (20003, 768, 64, 768)])
+def test_one_weights_gradient_alone(T, d, h, dout, dtype):
+    print(f"gated, one gradient, {T}x{d}x{h}x{dout} {dtype}", flush=True)
+    x, wg, wu, wd, dy = inputs(T, d, h, dout, dtype, seed=T)
+    want = formula(x, wg, wu, wd, "silu", dy)
+    for which, name in ((1, "dwg"), (2, "dwu")):
+        leaves = [t.detach().requires_grad_(i == which) for i, t in enumerate((x, wg, wu, wd))]
+        g, = torch.autograd.grad(layers.gated_feed_forward(*leaves), [leaves[which]], dy)
+        torch.cuda.synchronize()
+        compare({name: g}, want, dtype, T)
