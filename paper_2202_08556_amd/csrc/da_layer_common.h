@@ -159,7 +159,7 @@ template <int N> __device__ __forceinline__ void act_slopes(int act, float (&z)[
     for (int i = 0; i < N; ++i) z[i] = slope[i];
 }
 
-__device__ __forceinline__ float wave_sum(float x, int lanes) {
+template <class S> __device__ __forceinline__ S wave_sum(S x, int lanes) {
     for (int d = 1; d < lanes; d <<= 1) x += __shfl_xor(x, d, 64);
     return x;
 }

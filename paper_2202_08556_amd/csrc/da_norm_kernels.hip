@@ -9,12 +9,18 @@
 //   each   a sample is one row: the numbers of one group are a few lanes' registers
 //   team   a sample (some of its groups) is one wave's or block's: read once where the registers hold it
 //   split  a sample is cut into chunks of rows, one block each: partial statistics, their sum, and a second pass
-// Statistics are held in 32 bits: as sums of squares about the mean where the data stays in registers, about the
-// first number of a chunk's column otherwise, joined by the formula for the variance of a union; never as the mean of
-// squares less the square of the mean, which loses everything where the mean is large.
+// Variance: where every row is a sample, sums of squares about the mean, both from registers.  Elsewhere one pass takes the
+// sums of c = x - s and of c^2, s the first number of the sample's or chunk's group, in 64 bits: s is one of the n numbers,
+// so sum c^2 exceeds the sum of squares about the mean by a factor of at most about n, however far s is from the others (a
+// first row of padding, a mean that is large), and the difference keeps all 24 bits.  In 32 bits it would lose them.  Chunks
+// are joined by the formula for the variance of a union, in 64 bits for the same reason.  The additions in 64 bits took a
+// first pass from 31 to 33 us (8000 samples of 23 rows x 96 float32), from 16 to 19 (30011 x 602 bf16, accesses of 4 bytes) and
+// nothing where memory is the bound (262144 x 256 float32).  All else is held in 32 bits.
 // All sums are taken in an order that follows from the sizes alone: results are the same from run to run.
 #pragma once
 #include "da_layer_common.h"
+
+#include <type_traits>
 
 namespace daspmm {
 
@@ -218,11 +224,11 @@ __global__ __launch_bounds__(kNormBlock) void norm_each_kernel(NormShape sh, int
 // columns, the others along the rows, E rows a thread in registers; rows beyond that are read again.
 // stats: mean and r of every sample and group, written forward and read backward.
 // Samples of more than `longest` rows are left to the split kernels.
-// 8000 samples of 23 rows x 96 float32: 31 us forward, 53 backward (4.3 and 3.8 TB/s): a sample's loads, its three barriers and
+// 8000 samples of 23 rows x 96 float32: 33 us forward, 53 backward (4.1 and 3.8 TB/s): a sample's loads, its three barriers and
 // its stores follow one another, other blocks fill the gaps.
 // ------------------------------------------------------------------------------------------
 // Sum of squares about the mean from b = sum c^2, a = sum c and a / n; NaN and infinities stay visible.
-__device__ __forceinline__ float variance(float b, float a, float m) { return fmaxf(b - a * m, 0.f) + (b - b); }
+__device__ __forceinline__ double variance(double b, double a, double m) { return fmax(b - a * m, 0.0) + (b - b); }
 
 template <int TEAM> __device__ __forceinline__ void team_sync() {
     if constexpr (TEAM == 64) {
@@ -246,10 +252,11 @@ __device__ __forceinline__ void norm_team(const NormShape& sh, const TeamPlan& t
                                           float* __restrict__ stats, float* __restrict__ part)
 {
     constexpr int BLOCK = TEAM < 256 ? 256 : TEAM, TEAMS = BLOCK / TEAM;
-    __shared__ float red_mem[TEAMS][2][TEAM], tot_mem[TEAMS][2][TEAM];
+    typedef typename std::conditional<BWD, float, double>::type Sum;
+    __shared__ Sum red_mem[TEAMS][2][TEAM], tot_mem[TEAMS][2][TEAM];
     const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM, GT = tp.GT;
-    float (&red)[2][TEAM] = red_mem[team];
-    float (&tot)[2][TEAM] = tot_mem[team];
+    Sum (&red)[2][TEAM] = red_mem[team];
+    Sum (&tot)[2][TEAM] = tot_mem[team];
     const int cgv = sh.cg / V, TX = GT * cgv, TY = TEAM / TX;
     const int tx = t % TX, ty = t / TX;
     const int g0 = tile * GT, gn = min(GT, sh.G - g0);
@@ -257,19 +264,19 @@ __device__ __forceinline__ void norm_team(const NormShape& sh, const TeamPlan& t
     const int col = g0 * sh.cg + tx * V, g = g0 + tx / cgv;
 
     // sums over a group's threads, for every thread of the group
-    auto join = [&](float& a, float& b) {
-        red[0][t] = on ? a : 0.f;
-        red[1][t] = on ? b : 0.f;
+    auto join = [&](Sum& a, Sum& b) {
+        red[0][t] = on ? a : 0;
+        red[1][t] = on ? b : 0;
         team_sync<TEAM>();
         if (t < TX) {
-            float p = 0.f, q = 0.f;
+            Sum p = 0, q = 0;
             for (int k = 0; k < TY; ++k) { p += red[0][t + k * TX]; q += red[1][t + k * TX]; }
             red[0][t] = p;
             red[1][t] = q;
         }
         team_sync<TEAM>();
         if (t < GT) {
-            float p = 0.f, q = 0.f;
+            Sum p = 0, q = 0;
             for (int k = 0; k < cgv; ++k) { p += red[0][t * cgv + k]; q += red[1][t * cgv + k]; }
             tot[0][t] = p;
             tot[1][t] = q;
@@ -305,14 +312,15 @@ __device__ __forceinline__ void norm_team(const NormShape& sh, const TeamPlan& t
         }
         const int rest = ty + TY * E;                        // first row that is not in registers
         if constexpr (!BWD) {
-            float a = 0.f, b = 0.f, shift = 0.f;
+            double a = 0.0, b = 0.0;
+            float shift = 0.f;
             if (on) {
                 float first[1];
                 load_floats<1>(x + r0 * ldx + (long)g * sh.cg, first);
                 shift = first[0];
                 auto add = [&](const float (&u)[V]) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) { const float c = u[i] - shift; a += c; b += c * c; }
+                    for (int i = 0; i < V; ++i) { const double c = u[i] - shift; a += c; b = fma(c, c, b); }
                 };
 #pragma unroll
                 for (int e = 0; e < E; ++e)
@@ -324,8 +332,11 @@ __device__ __forceinline__ void norm_team(const NormShape& sh, const TeamPlan& t
                 }
             }
             join(a, b);
-            const float m = a * inv, mean = shift + m;
-            const float r = __builtin_amdgcn_rsqf(variance(b, a, m) * inv + sh.eps);
+            double share = inv;                              // 1 / count in 32 bits, and a step of Newton's method
+            share *= 2.0 - share * ((double)n * (double)sh.cg);
+            const double m = a * share;
+            const float mean = shift + (float)m;
+            const float r = __builtin_amdgcn_rsqf((float)(variance(b, a, m) * share) + sh.eps);
             if (stats && on && ty == 0 && tx % cgv == 0) {
                 stats[(s * sh.G + g) * 2] = mean;
                 stats[(s * sh.G + g) * 2 + 1] = r;
@@ -552,7 +563,8 @@ __device__ __forceinline__ bool sample_to_join(const NormShape& sh, const SplitP
 }
 
 // Sums of two numbers over the threads of a block that share a group (gn == 1: over all), left in red[.][group]
-__device__ __forceinline__ void join_groups(float (&red)[2][kNormBlock], float a, float b, int TX, int TY, int cgv, int gn) {
+template <class Sum>
+__device__ __forceinline__ void join_groups(Sum (&red)[2][kNormBlock], Sum a, Sum b, int TX, int TY, int cgv, int gn) {
     const int t = threadIdx.x;
     __syncthreads();
     red[0][t] = a;
@@ -566,12 +578,12 @@ __device__ __forceinline__ void join_groups(float (&red)[2][kNormBlock], float a
     __syncthreads();
     const int width = gn == 1 ? TX : cgv;
     if (gn == 1 && t < 64) {                                 // up to 256 numbers: a wave
-        a = b = 0.f;
+        a = b = 0;
         for (int k = t; k < width; k += 64) { a += red[0][k]; b += red[1][k]; }
         a = wave_sum(a, 64);
         b = wave_sum(b, 64);
     } else if (gn > 1 && t < gn) {
-        a = b = 0.f;
+        a = b = 0;
         for (int k = 0; k < width; ++k) { a += red[0][t * width + k]; b += red[1][t * width + k]; }
     }
     __syncthreads();
@@ -586,7 +598,7 @@ template <class T, int V>
 __device__ __forceinline__ void norm_stats(const NormShape& sh, const SplitPlan& sp, int chunk, int tile, const T* __restrict__ x,
                                            long ldx, ChunkEntry* __restrict__ table, float2* __restrict__ part)
 {
-    __shared__ float red[2][kNormBlock];
+    __shared__ double red[2][kNormBlock];
     Segment seg[2];
     segments_of(sh, sp, chunk, seg, table, true);
     const ColumnTile ct = column_tile<V>(sh, sp, tile);
@@ -597,7 +609,8 @@ __device__ __forceinline__ void norm_stats(const NormShape& sh, const SplitPlan&
     for (int q = 0; q < 2; ++q) {
         if (seg[q].s < 0) continue;
         const long r0 = seg[q].r0, r1 = seg[q].r1;
-        float a = 0.f, b = 0.f, shift = 0.f;
+        double a = 0.0, b = 0.0;
+        float shift = 0.f;
         if (on) {
             const T* __restrict__ xp = x + (long)vec * V;
             const int from = ct.gn == 1 ? ct.vec0 : vec / cgv * cgv;
@@ -606,7 +619,7 @@ __device__ __forceinline__ void norm_stats(const NormShape& sh, const SplitPlan&
             shift = one[0];
             auto add = [&](const float (&u)[V]) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) { const float c = u[i] - shift; a += c; b += c * c; }
+                for (int i = 0; i < V; ++i) { const double c = u[i] - shift; a += c; b = fma(c, c, b); }
             };
             constexpr int U = 8;
             long row = r0 + ty;
@@ -629,9 +642,9 @@ __device__ __forceinline__ void norm_stats(const NormShape& sh, const SplitPlan&
         if (t < ct.gn) {
             float one[1];
             load_floats<1>(x + r0 * ldx + ((long)ct.vec0 + (long)t * cgv) * V, one);
-            const float count = (float)(r1 - r0) * (float)(width * V), m = red[0][t] / count;
+            const double m = red[0][t] / ((double)(r1 - r0) * (double)(width * V));
             const long at = sp.pieces == 1 ? ct.g0 + t : tile;
-            part[at * sp.slots + seg[q].slot] = make_float2(one[0] + m, variance(red[1][t], red[0][t], m));
+            part[at * sp.slots + seg[q].slot] = make_float2(one[0] + (float)m, (float)variance(red[1][t], red[0][t], m));
         }
     }
 }
@@ -666,23 +679,22 @@ __global__ __launch_bounds__(kJoinBlock) void norm_join_kernel(NormShape sh, Spl
     if (!sample_to_join(sh, sp, blockIdx.x, table, &s, &p)) return;
     const int g = blockIdx.y * kJoinGroups + (threadIdx.x >> 6), lane = threadIdx.x & 63, pieces = sp.pieces, cgv = sh.cg / V;
     if (g >= sh.G) return;
-    const float total = (float)(p.r1 - p.r0) * (float)sh.cg;
-    float a = 0.f, b = 0.f;
-    // relative to the first chunk's mean, which the others are near
+    const double total = (double)(p.r1 - p.r0) * (double)sh.cg;
+    double a = 0.0, b = 0.0;
+    // relative to the first part's mean, which may be that of a single row
     const float origin = part[(long)g * pieces * sp.slots + p.slot(0)].x;
     for_parts(sh, sp, p, g, part, [&](float2 v, int piece, int c) {
         const int width = pieces == 1 ? cgv : min(sp.TX, cgv - piece * sp.TX);
-        const float d = v.x - origin, n = (float)p.rows(c) * (float)(width * V);
+        const double d = (double)v.x - origin, n = (double)p.rows(c) * (double)(width * V);
         a += d * n;
         b += v.y + d * d * n;
     });
     a = wave_sum(a, 64);
     b = wave_sum(b, 64);
-    const float m = a / total, mean = origin + m;
-    b = variance(b, a, m);
     if (lane == 0) {
-        stats[(s * sh.G + g) * 2] = mean;
-        stats[(s * sh.G + g) * 2 + 1] = 1.f / sqrtf(b / total + sh.eps);
+        const double m = a / total;
+        stats[(s * sh.G + g) * 2] = origin + (float)m;
+        stats[(s * sh.G + g) * 2 + 1] = 1.f / sqrtf((float)(variance(b, a, m) / total) + sh.eps);
     }
 }
 

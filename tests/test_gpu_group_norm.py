@@ -382,3 +382,37 @@ def test_long_samples_that_share_a_chunk(lens):
     for C, G in ((24, 3), (8, 8)):
         x, w, b, dy = inputs((sum(lens), C), torch.float32, seed=len(lens))
         run(x, G, w, b, "gelu", offsets, dy=dy)
+
+
+def outlying(shape, level, first, seed):
+    """Numbers of deviation 1 around a level; the first row of the tensor is something else throughout."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    C = shape[-1]
+    x = torch.randn(*shape, generator=g, device="cuda") + level
+    x.view(-1, C)[0] = first
+    w = 1 + 0.2 * torch.randn(C, generator=g, device="cuda")
+    b = 0.2 * torch.randn(C, generator=g, device="cuda")
+    return x, w, b, torch.randn(*shape, generator=g, device="cuda")
+
+
+# one wave, blocks of 256 and of 1024 threads, chunks, groups cut into pieces
+@pytest.mark.parametrize("shape", [(3, 23, 64, 4), (2, 900, 16, 1), (300, 100, 16, 2), (2, 8, 2304, 1), (2, 1500, 48, 6), (1, 20000, 32, 2),
+                                   (1, 4000, 8, 1), (1, 600, 4104, 1)], ids=str)
+@pytest.mark.parametrize("level,first", [(0.0, 30.0), (0.0, 1000.0), (100.0, 0.0), (1000.0, 0.0)])
+def test_a_first_row_unlike_the_others(shape, level, first):
+    """A node without neighbours or a row of padding in front: sums about a sample's first number alone lose the variance."""
+    x, w, b, dy = outlying(shape[:3], level, first, seed=14)
+    run(x, shape[3], w, b, "silu", dy=dy)
+
+
+# a long sample's first part is all of a chunk, one row of it, or a few
+@pytest.mark.parametrize("before", [0, 1, 4090, 4094, 4095, 4096])
+@pytest.mark.parametrize("level,first", [(0.0, 1000.0), (1000.0, 0.0)])
+def test_a_first_row_unlike_the_others_in_ragged_samples(before, level, first):
+    for C, G, dtype in ((8, 2, torch.float32), (8, 1, torch.bfloat16), (96, 8, torch.float32)):
+        lens = [before, 9000 if C == 8 else 2000, 0, 300]
+        offsets = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+        x, w, b, dy = outlying((sum(lens), C), level, first, seed=15)
+        x[before] = first                                    # of the long sample
+        x[-300] = first
+        run(x.to(dtype), G, w, b, "silu", offsets, dy=dy.to(dtype))
