@@ -66,8 +66,9 @@ int da_group_norm_backward(int dtype, int64_t rows, int64_t samples, const int32
  *   loss[r] = temperature^2 sum_k p_k (log p_k - log q[class_k])
  *   dz[r,j] = dloss[r] temperature (q_j - sum of p_k over the entries k of class j)
  *
- * A row without entries, or with none above -inf, has loss 0 and gradient 0.  An entry with p_k = 0 (a logit of -inf
- * beside others) adds nothing.  Several entries of one class count as they stand.
+ * A row without entries, or all of whose entries are -inf, has loss 0 and gradient 0.  An entry with p_k = 0 (a logit of
+ * -inf beside others) adds nothing.  An entry of NaN makes its row's loss NaN, and the gradient of its entries' classes.
+ * Several entries of one class count as they stand.
  *
  *   z         rows x classes of dtype, ldz >= classes; dz dense
  *   index     rows x best, int32 or (index64 != 0) int64, dense

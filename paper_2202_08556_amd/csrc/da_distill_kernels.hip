@@ -64,8 +64,11 @@ template <class T, int V> __device__ __forceinline__ void store_grads(T* __restr
     }
 }
 
+// The larger one; NaN if one is.  A teacher's NaN would otherwise be a missing entry.
+__device__ __forceinline__ float larger(float x, float o) { return o > x || o != o ? o : x; }
+
 __device__ __forceinline__ float wave_max(float x, int lanes) {
-    for (int d = 1; d < lanes; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+    for (int d = 1; d < lanes; d <<= 1) x = larger(x, __shfl_xor(x, d, 64));
     return x;
 }
 
@@ -94,7 +97,7 @@ __global__ __launch_bounds__(kDistillBlock) void distill_narrow_kernel(
         // the teacher's entries
         float tmax = -INFINITY;
         for (long k = lane; k < te.best; k += P)
-            if (te.has(te.cls(row * te.best + k))) tmax = fmaxf(tmax, te.logit(row * te.best + k));
+            if (te.has(te.cls(row * te.best + k))) tmax = larger(tmax, te.logit(row * te.best + k));
         tmax = wave_max(tmax, P);
         if constexpr (!BWD) {
             float m = -INFINITY, s = 0.f;
@@ -194,7 +197,7 @@ template <int BLOCK> __device__ __forceinline__ float block_max(float x, float* 
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
     __syncthreads();
     x = red[0];
-    for (int w = 1; w < BLOCK / 64; ++w) x = fmaxf(x, red[w]);
+    for (int w = 1; w < BLOCK / 64; ++w) x = larger(x, red[w]);
     return x;
 }
 template <int BLOCK> __device__ __forceinline__ float block_sum(float x, float* red) {
@@ -227,7 +230,7 @@ __device__ __forceinline__ void row_loss(long row, const Teacher& te, const Firs
 {
     float tmax = first.cls >= 0 ? first.t : -INFINITY;
     for (long k = threadIdx.x + BLOCK; k < te.best; k += BLOCK)
-        if (te.has(te.cls(row * te.best + k))) tmax = fmaxf(tmax, te.logit(row * te.best + k));
+        if (te.has(te.cls(row * te.best + k))) tmax = larger(tmax, te.logit(row * te.best + k));
     tmax = block_max<BLOCK>(tmax, red);
     const float inv_t = 1.f / temperature;
     float ps = 0.f, a = 0.f;
@@ -367,7 +370,7 @@ __global__ __launch_bounds__(kWideBlock) void distill_wide_grad_kernel(
         next.load(zp, c0 + threadIdx.x * V, c1, c0 + TURN <= c1);
         float tmax = -INFINITY, ps = 0.f;
         for (long k = threadIdx.x; k < te.best; k += kWideBlock)
-            if (te.has(te.cls(row * te.best + k))) tmax = fmaxf(tmax, te.logit(row * te.best + k));
+            if (te.has(te.cls(row * te.best + k))) tmax = larger(tmax, te.logit(row * te.best + k));
         tmax = block_max<kWideBlock>(tmax, red);
         for (long k = threadIdx.x; k < te.best; k += kWideBlock) {
             const long c = te.cls(row * te.best + k);

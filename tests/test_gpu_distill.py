@@ -292,3 +292,34 @@ def test_refusals():
     g, = torch.autograd.grad(f(z, index, top), z, create_graph=True)
     with pytest.raises(RuntimeError, match="differentiated again"):
         g.sum().backward()
+
+
+@pytest.mark.parametrize("best", [1, 4, 700])
+@pytest.mark.parametrize("V", [41, 700, 3001, 90001])
+def test_a_teacher_that_is_no_number_shows(V, best):
+    """A row with an entry whose logit is NaN has a NaN loss and NaN gradients of its entries' classes, whether it has other
+    entries or not; a missing entry's NaN is not looked at."""
+    best = min(best, V)
+    z, index, top = inputs(6, V, best, torch.float32, seed=12, missing=0.0, empty=0.0)
+    index[4, 1:] = -1
+    index[3, 0] = -1
+    index[5] = -1
+    want = run(z, index, top)
+    bad = top.clone()
+    bad[1] = float("nan")                                    # nothing else there
+    bad[2, -1] = float("nan")                                # one of some
+    bad[3, 0] = bad[5, 0] = float("nan")                     # missing
+    bad[4, 1:] = -math.inf
+    bad[4, 0] = float("nan")                                 # beside missing ones
+    z.requires_grad_(True)
+    loss = layers.distill_loss(z, index, bad, 1.0, "none")
+    dz, = torch.autograd.grad(loss, z, torch.ones_like(loss))
+    assert torch.isnan(loss[[1, 2, 4]]).all()
+    for r in (1, 2, 4):
+        entries = torch.zeros(V, dtype=torch.bool, device="cuda")
+        entries[index[r][index[r] >= 0].long()] = True
+        assert torch.isnan(dz[r, entries]).all() and torch.isfinite(dz[r, ~entries]).all()
+    keep = [0, 5] if best == 1 else [0, 3, 5]
+    assert torch.equal(loss[keep], want[0][keep]) and torch.isfinite(dz[keep]).all()
+    if best == 1:
+        assert loss[3] == 0 and not dz[3].any()
