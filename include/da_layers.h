@@ -76,7 +76,7 @@ int da_group_norm_backward(int dtype, int64_t rows, int64_t samples, const int32
  *   stats     float32[rows x 2], written by the forward call (a row's largest logit and 1 / the sum of exp((z - largest) /
  *             temperature)) and read backward; may be NULL where no gradient is needed
  *   loss, dloss   float32[rows]; dloss_stride 0 takes dloss[0] for every row
- * Limits: rows < 2^31, classes < 2^31 - 2^16, best <= 1024.
+ * Without classes every entry is missing.  Limits: rows < 2^31, classes < 2^31 - 2^16, best <= 1024.
  */
 int da_distill_workspace(int64_t rows, int64_t classes, size_t *bytes /* host, out */);
 int da_distill(int dtype, int64_t rows, int64_t classes, int64_t best, const void *z, int64_t ldz, const void *index,

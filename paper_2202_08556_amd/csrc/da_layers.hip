@@ -372,7 +372,7 @@ DistillPlan distill_plan(int dtype, int64_t rows, int64_t classes, int64_t best)
     const int64_t want = 8 * compute_units();
     p.pieces = std::clamp<int64_t>(ceil_div(want, std::max<int64_t>(rows, 1)), 1, std::max<int64_t>(1, classes / 8192));
     const int64_t turn = 4 * kWideBlock * V;
-    p.piece = ceil_div(ceil_div(classes, p.pieces), turn) * turn;
+    p.piece = std::max<int64_t>(1, ceil_div(ceil_div(classes, p.pieces), turn)) * turn;       // no classes: nothing in one piece
     p.pieces = std::max<int64_t>(1, ceil_div(classes, p.piece));
     return p;
 }

@@ -323,3 +323,14 @@ def test_a_teacher_that_is_no_number_shows(V, best):
     assert torch.equal(loss[keep], want[0][keep]) and torch.isfinite(dz[keep]).all()
     if best == 1:
         assert loss[3] == 0 and not dz[3].any()
+
+
+@pytest.mark.parametrize("best", [0, 1, 5, 1024])
+@pytest.mark.parametrize("shape", [(3,), (0,), (2, 3), ()], ids=str)
+def test_no_classes(shape, best):
+    """Every entry is missing: loss 0."""
+    z = torch.empty((*shape, 0), device="cuda", requires_grad=True)
+    index = torch.zeros((*shape, best), dtype=torch.int32, device="cuda")
+    loss = layers.distill_loss(z, index, torch.ones((*shape, best), device="cuda"), 2.0, "none")
+    dz, = torch.autograd.grad(loss, z, torch.ones_like(loss))
+    assert loss.shape == shape and not loss.any() and dz.shape == z.shape

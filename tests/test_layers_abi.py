@@ -100,3 +100,19 @@ def test_python_refuses_what_is_not_on_the_gpu():
                  lambda: layers.distill_loss(x, torch.zeros(4, 2, dtype=torch.int32), x[:, :2])):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("rows", [0, 1, 3, 10 ** 6])
+@pytest.mark.parametrize("classes", [0, 1, 41, 8192, 65537, 2 ** 31 - 2 ** 16 - 1])
+def test_distill_workspace_of_any_size(rows, classes):
+    assert lib().da_distill_workspace(i64(rows), i64(classes), OUT[0]) == da.DA_OK
+    pieces = SIZES[0].value // (8 * rows) if rows else 0
+    assert pieces * 8192 <= max(classes, 8192)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("best", [0, 5, 1024])
+def test_distill_of_no_rows_and_no_classes(dtype, best):
+    assert distill(dtype=dtype, rows=0, classes=0, best=best, ldz=0, z=None, index=None, top=None, loss=None) == da.DA_OK
+    assert lib().da_distill_backward(dtype, i64(3), i64(0), i64(best), None, i64(0), P, 0, P, 0, f32(1.0), None, None, i64(1), None,
+                                     None) == da.DA_OK
