@@ -32,8 +32,13 @@ int pow2_at_least(int64_t x) {
 // ------------------------------------------------------------------------------------------
 // group norm
 // ------------------------------------------------------------------------------------------
-// Blocks of a launch: of 2^32 threads and more the high bits are lost
+// Blocks of a launch: of 2^32 threads and more the high bits are lost.  What takes more is launched in pieces.
 constexpr int64_t kMaxBlocks = (1LL << 32) / 1024 - 1;
+
+// launch(first, count) for `all` things, `most` at a time
+template <class F> void in_pieces(int64_t all, int64_t most, F&& launch) {
+    for (int64_t first = 0; first < all; first += most) launch(first, std::min(most, all - first));
+}
 
 // Rows that a thread of a team holds: twice as many cost half of the waves and more than they save
 constexpr int norm_held(int V) { return V >= 8 ? 2 : 4; }
@@ -48,7 +53,6 @@ struct NormPlan {
     bool split;
     SplitPlan sp;
     int64_t slots;
-    bool fits;               // the chunks are few enough to be counted in 32 bits
     // memory
     size_t stats;            // floats
     int64_t col_rows;        // rows of 2 C sums: the first pass's blocks, then the chunks
@@ -69,7 +73,6 @@ int norm_check(int dtype, int64_t rows, int64_t samples, int64_t channels, int64
 // Which kernels a shape takes.  train: statistics are kept and the backward pass is planned, too.
 NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_t C, int64_t G, bool train) {
     NormPlan p{};
-    p.fits = true;
     const int64_t cg = C / G, length = ragged || samples == 0 ? 0 : rows / samples;
     const int most = dtype == DA_F32 ? 4 : 8;
     p.V = 1;
@@ -117,7 +120,7 @@ NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_
             p.tp.GT = (int)tile(p.team);
             p.tp.tiles = (int)ceil_div(G, p.tp.GT);
             p.tp.longest = longest;
-            p.tp.blocks = std::min(ceil_div(samples, teams), cap);
+            p.tp.blocks = std::min({ceil_div(samples, teams), cap, kMaxBlocks / p.tp.tiles});
             first_rows = p.tp.blocks;
         }
         if (p.split) {
@@ -145,9 +148,8 @@ NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_
                 each = ceil_div(length, p.sp.per);
                 chunks = p.slots = samples * each;
             }
-            p.fits = chunks <= kMaxBlocks;
-            p.sp.each = (int)std::min(each, kMaxBlocks);
-            p.sp.chunks = (int)std::min(chunks, kMaxBlocks);
+            p.sp.each = (int)each;
+            p.sp.chunks = (int)chunks;                       // no more than rows
             p.sp.slots = p.slots;
         }
     }
@@ -189,11 +191,15 @@ void launch_each(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx
 template <class T, int V, bool BWD>
 void launch_first(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, const T* dy, int64_t ldy, T* out, float* stats,
                   float* team_cols, ChunkEntry* table, float2* part, float* cols, hipStream_t s) {
-    auto go = [&](auto kernel, int block, const TeamPlan& tp, int64_t chunks) {
+    auto launch = [&](auto kernel, int block, const TeamPlan& tp, int64_t from, int64_t chunks) {
         const int64_t blocks = tp.blocks * tp.tiles + chunks * p.sp.tiles;
         if (blocks)
-            hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(block), 0, s, sh, tp, p.sp, x, (long)ldx, dy, (long)ldy, out,
+            hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(block), 0, s, sh, tp, p.sp, (int)from, x, (long)ldx, dy, (long)ldy, out,
                                stats, team_cols, table, part, cols);
+    };
+    auto go = [&](auto kernel, int block, const TeamPlan& tp, int64_t chunks) {
+        if (!chunks) return launch(kernel, block, tp, 0, 0);
+        in_pieces(chunks, kMaxBlocks / p.sp.tiles, [&](int64_t from, int64_t count) { launch(kernel, block, from ? TeamPlan{} : tp, from, count); });
     };
     const int64_t chunks = p.split ? p.sp.chunks : 0;
     constexpr int E = norm_held(V);
@@ -205,6 +211,16 @@ void launch_first(const NormPlan& p, const NormShape& sh, const T* x, int64_t ld
     else go(norm_first_kernel<T, V, 256, E, false, BWD>, 256, p.tp, 0);
 }
 
+// The last chunks first: the kernel counts down from the last of its own
+template <class T, int V, bool BWD>
+void launch_apply(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, const T* dy, int64_t ldy, const float* stats,
+                  const float* means, ChunkEntry* table, T* out, hipStream_t s) {
+    in_pieces(p.sp.chunks, kMaxBlocks, [&](int64_t done, int64_t count) {
+        hipLaunchKernelGGL((norm_apply_kernel<T, V, BWD>), dim3((unsigned)count, (unsigned)p.sp.tiles), dim3(kNormBlock), 0, s, sh, p.sp,
+                           (int)(p.sp.chunks - 1 - done), x, (long)ldx, dy, (long)ldy, stats, means, table, out);
+    });
+}
+
 template <class T, int V>
 void norm_forward(const NormPlan& p, const NormShape& sh, const T* x, int64_t ldx, T* y, float* stats, char* ws, hipStream_t s) {
     const T* none = nullptr;
@@ -213,11 +229,11 @@ void norm_forward(const NormPlan& p, const NormShape& sh, const T* x, int64_t ld
     ChunkEntry* table = reinterpret_cast<ChunkEntry*>(ws + p.table_at);
     launch_first<T, V, false>(p, sh, x, ldx, none, 0, y, stats, nullptr, table, part, nullptr, s);
     if (!p.split) return;
-    const int64_t joins = sh.offsets ? p.sp.chunks : sh.samples;
-    hipLaunchKernelGGL((norm_join_kernel<V>), dim3((unsigned)joins, (unsigned)ceil_div(sh.G, kJoinGroups)), dim3(kJoinBlock), 0, s, sh, p.sp,
-                       table, part, stats);
-    hipLaunchKernelGGL((norm_apply_kernel<T, V, false>), dim3((unsigned)p.sp.chunks, (unsigned)p.sp.tiles), dim3(kNormBlock), 0, s, sh,
-                       p.sp, x, (long)ldx, none, 0L, stats, static_cast<const float*>(nullptr), table, y);
+    in_pieces(sh.offsets ? p.sp.chunks : sh.samples, kMaxBlocks, [&](int64_t from, int64_t joins) {
+        hipLaunchKernelGGL((norm_join_kernel<V>), dim3((unsigned)joins, (unsigned)ceil_div(sh.G, kJoinGroups)), dim3(kJoinBlock), 0, s, sh, p.sp,
+                           (int)from, table, part, stats);
+    });
+    launch_apply<T, V, false>(p, sh, x, ldx, none, 0, stats, nullptr, table, y, s);
 }
 
 template <class T, int V>
@@ -230,13 +246,17 @@ void norm_backward(const NormPlan& p, const NormShape& sh, const T* x, int64_t l
     if (p.each) launch_each<T, V, true>(p, sh, x, ldx, dy, ldy, dx, cols, s);
     else launch_first<T, V, true>(p, sh, x, ldx, dy, ldy, dx, const_cast<float*>(stats), cols, table, part, cols + p.tp.blocks * 2 * sh.C,
                                   s);
-    const int64_t joins = !p.split ? 0 : (sh.offsets ? p.sp.chunks : sh.samples) * ceil_div(sh.G, kJoinGroups), sums = dw || db ? ceil_div(2 * sh.C, 16) : 0;
-    if (joins + sums)
-        hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)(joins + sums)), dim3(kJoinBlock), 0, s, sh, p.sp, (int)joins, table, part, means,
-                           cols, (long)p.col_rows, dw, db);
-    if (p.split)
-        hipLaunchKernelGGL((norm_apply_kernel<T, V, true>), dim3((unsigned)p.sp.chunks, (unsigned)p.sp.tiles), dim3(kNormBlock), 0, s,
-                           sh, p.sp, x, (long)ldx, dy, (long)ldy, stats, means, table, dx);
+    // a join is of kJoinGroups groups of a sample; the sums are part of the first launch
+    const int64_t each = ceil_div(sh.G, kJoinGroups), joins = !p.split ? 0 : sh.offsets ? p.sp.chunks : sh.samples, sums = dw || db ? ceil_div(2 * sh.C, 16) : 0;
+    auto join = [&](int64_t from, int64_t count) {
+        const int64_t more = from ? 0 : sums;
+        if (count + more)
+            hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)(count * each + more)), dim3(kJoinBlock), 0, s, sh, p.sp, (int)from,
+                               (int)(count * each), table, part, means, cols, (long)p.col_rows, dw, db);
+    };
+    if (joins) in_pieces(joins, (kMaxBlocks - sums) / each, join);
+    else join(0, 0);
+    if (p.split) launch_apply<T, V, true>(p, sh, x, ldx, dy, ldy, stats, means, table, dx, s);
 }
 
 template <class F> void with_type_and_width(int dtype, int V, F&& f) {
@@ -266,10 +286,6 @@ int norm_shape(int dtype, int64_t rows, int64_t samples, const int32_t* offsets,
     *sh = NormShape{rows, samples, offsets, samples ? rows / samples : 0, (int)channels, (int)groups, (int)(channels / groups), eps,
                     act, param_dtype, w, b};
     return DA_OK;
-}
-
-bool norm_fits(const NormPlan& p, int64_t groups) {
-    return p.fits && p.sp.chunks * std::max<int64_t>(groups, p.sp.tiles) <= kMaxBlocks && p.tp.blocks * p.tp.tiles <= kMaxBlocks;
 }
 
 int workspace_error() {
@@ -304,7 +320,6 @@ extern "C" int da_group_norm(int dtype, int64_t rows, int64_t samples, const int
     if (!y) return fail(DA_ERR_INVALID_ARG, "null y");
     const NormPlan p = norm_plan(dtype, rows, samples, offsets != nullptr, channels, groups, stats != nullptr);
     if (p.forward && (!workspace || workspace_bytes < p.forward || !aligned16(workspace))) return workspace_error();
-    if (!norm_fits(p, groups)) return fail(DA_ERR_UNSUPPORTED, "size too large");
     char* ws = static_cast<char*>(workspace);
     float* kept = stats ? stats : p.stats ? reinterpret_cast<float*>(ws + p.forward - p.stats * sizeof(float)) : nullptr;
     with_type_and_width(dtype, p.V, [&](auto t, auto v) {
@@ -326,12 +341,10 @@ extern "C" int da_group_norm_backward(int dtype, int64_t rows, int64_t samples, 
     if (ldy < channels) return fail(DA_ERR_INVALID_ARG, "leading dimension smaller than the extent it strides over");
     if (rows > 0 && (!dy || !dx)) return fail(DA_ERR_INVALID_ARG, "null dy or dx");
     NormPlan p{};
-    p.V = 1;
-    p.fits = true;                                           // no rows: dw and db are sums of nothing
+    p.V = 1;                                                 // no rows: dw and db are sums of nothing
     if (rows > 0) p = norm_plan(dtype, rows, samples, offsets != nullptr, channels, groups, true);
     if (p.stats && !stats) return fail(DA_ERR_INVALID_ARG, "null stats");
     if (p.backward && (!workspace || workspace_bytes < p.backward || !aligned16(workspace))) return workspace_error();
-    if (!norm_fits(p, groups)) return fail(DA_ERR_UNSUPPORTED, "size too large");
     with_type_and_width(dtype, p.V, [&](auto t, auto v) {
         using T = decltype(t);
         norm_backward<T, decltype(v)::value>(p, sh, static_cast<const T*>(x), ldx, static_cast<const T*>(dy), ldy, stats,

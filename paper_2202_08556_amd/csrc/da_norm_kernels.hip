@@ -501,7 +501,7 @@ __device__ __forceinline__ void segments_of(const NormShape& sh, const SplitPlan
     out[0].s = out[1].s = -1;
     if (!sh.offsets) {
         const int s = c / sp.each;
-        const long r0 = s * sh.length + c % sp.each * sp.per;
+        const long r0 = s * sh.length + (long)(c % sp.each) * sp.per;
         out[0] = Segment{s, r0, min(r0 + sp.per, (s + 1) * sh.length), c};
         return;
     }
@@ -518,7 +518,7 @@ __device__ __forceinline__ void segments_of(const NormShape& sh, const SplitPlan
         long r0, r1;
         sh.range(s, &r0, &r1);
         if (r1 - r0 > sp.longest && r0 < e && r1 > a && (q ? s != out[0].s : r0 <= a))
-            out[q] = Segment{s, max(r0, a), min(r1, e), sp.per == 1 ? c : 2 * c + q};
+            out[q] = Segment{s, max(r0, a), min(r1, e), sp.per == 1 ? (long)c : 2L * c + q};
     }
     if (threadIdx.x == 0) {                                  // by all column tiles alike
         table[c].seg[0] = out[0];
@@ -532,7 +532,7 @@ struct Parts {
     long r0, r1, per;
     bool ragged, late;           // late: begins inside its first chunk
 
-    __device__ long slot(int k) const { return !ragged || per == 1 ? first + k : 2 * (first + k) + (k == 0 && late ? 1 : 0); }
+    __device__ long slot(int k) const { return !ragged || per == 1 ? first + k : 2L * (first + k) + (k == 0 && late ? 1 : 0); }
     __device__ long rows(int k) const {
         if (!ragged) return min(per, r1 - r0 - k * per);
         const long a = (first + k) * per;
@@ -671,12 +671,12 @@ __device__ __forceinline__ void for_parts(const NormShape& sh, const SplitPlan& 
 
 // Joins the parts of a sample and group by the formula for the variance of a union; a wave owns a group
 template <int V>
-__global__ __launch_bounds__(kJoinBlock) void norm_join_kernel(NormShape sh, SplitPlan sp, const ChunkEntry* __restrict__ table,
+__global__ __launch_bounds__(kJoinBlock) void norm_join_kernel(NormShape sh, SplitPlan sp, int from, const ChunkEntry* __restrict__ table,
                                                                const float2* __restrict__ part, float* __restrict__ stats)
 {
     long s;
     Parts p;
-    if (!sample_to_join(sh, sp, blockIdx.x, table, &s, &p)) return;
+    if (!sample_to_join(sh, sp, from + blockIdx.x, table, &s, &p)) return;
     const int g = blockIdx.y * kJoinGroups + (threadIdx.x >> 6), lane = threadIdx.x & 63, pieces = sp.pieces, cgv = sh.cg / V;
     if (g >= sh.G) return;
     const double total = (double)(p.r1 - p.r0) * (double)sh.cg;
@@ -701,14 +701,14 @@ __global__ __launch_bounds__(kJoinBlock) void norm_join_kernel(NormShape sh, Spl
 // y of a chunk; BWD: dx, with the means of e and e xh of every sample and group in `means`.  The last chunks first: they
 // are the ones that the pass before has left in the caches.
 template <class T, int V, bool BWD>
-__global__ __launch_bounds__(kNormBlock) void norm_apply_kernel(NormShape sh, SplitPlan sp, const T* __restrict__ x, long ldx,
+__global__ __launch_bounds__(kNormBlock) void norm_apply_kernel(NormShape sh, SplitPlan sp, int last, const T* __restrict__ x, long ldx,
                                                                 const T* __restrict__ dy, long ldy,
                                                                 const float* __restrict__ stats,
                                                                 const float* __restrict__ means, ChunkEntry* __restrict__ table,
                                                                 T* __restrict__ out)
 {
     Segment seg[2];
-    segments_of(sh, sp, sp.chunks - 1 - blockIdx.x, seg, table, false);
+    segments_of(sh, sp, last - blockIdx.x, seg, table, false);
     const ColumnTile ct = column_tile<V>(sh, sp, blockIdx.y);
     const int TX = sp.TX, TY = kNormBlock / TX, tx = threadIdx.x % TX, ty = threadIdx.x / TX;
     if ((seg[0].s < 0 && seg[1].s < 0) || ty >= TY || tx >= ct.width) return;
@@ -857,7 +857,7 @@ __device__ __forceinline__ void norm_grad_stats(const NormShape& sh, const Split
 // sample.  Equal samples are all of one kind; their launches hold registers for that kind only.
 template <class T, int V, int TEAM, int E, bool CHUNKS, bool BWD>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_first_kernel(
-    NormShape sh, TeamPlan tp, SplitPlan sp, const T* __restrict__ x, long ldx, const T* __restrict__ dy, long ldy,
+    NormShape sh, TeamPlan tp, SplitPlan sp, int from, const T* __restrict__ x, long ldx, const T* __restrict__ dy, long ldy,
     T* __restrict__ out, float* __restrict__ stats, float* __restrict__ team_cols, ChunkEntry* __restrict__ table,
     float2* __restrict__ part, float* __restrict__ cols)
 {
@@ -866,15 +866,15 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_first_kernel(
         if constexpr (E > 0)
             norm_team<T, V, TEAM, E, BWD>(sh, tp, blockIdx.x / tp.tiles, blockIdx.x % tp.tiles, x, ldx, dy, ldy, out, stats, team_cols);
     } else if constexpr (CHUNKS) {
-        const unsigned k = blockIdx.x - teams, chunk = k / sp.tiles, tile = k % sp.tiles;
+        const unsigned k = blockIdx.x - teams, chunk = from + k / sp.tiles, tile = k % sp.tiles;
         if constexpr (BWD) norm_grad_stats<T, V>(sh, sp, chunk, tile, x, ldx, dy, ldy, stats, table, part, cols);
         else norm_stats<T, V>(sh, sp, chunk, tile, x, ldx, table, part);
     }
 }
 
 // Second pass backward: the means of e and e xh of every split sample and group (first `joins` blocks, kJoinGroups groups
-// to a block), and dw, db from `rows` rows of 2 C sums, 16 columns to a block.
-__global__ __launch_bounds__(kJoinBlock) void norm_grad_join_kernel(NormShape sh, SplitPlan sp, int joins,
+// to a block, from the from-th on), and dw, db from `rows` rows of 2 C sums, 16 columns to a block.
+__global__ __launch_bounds__(kJoinBlock) void norm_grad_join_kernel(NormShape sh, SplitPlan sp, int from, int joins,
                                                                     const ChunkEntry* __restrict__ table, const float2* __restrict__ part, float* __restrict__ means,
                                                                     const float* __restrict__ cols, long rows, void* dw, void* db)
 {
@@ -884,7 +884,7 @@ __global__ __launch_bounds__(kJoinBlock) void norm_grad_join_kernel(NormShape sh
         const int blocks = (sh.G + kJoinGroups - 1) / kJoinGroups;
         long s;
         Parts p;
-        if (!sample_to_join(sh, sp, blockIdx.x / blocks, table, &s, &p)) return;
+        if (!sample_to_join(sh, sp, from + blockIdx.x / blocks, table, &s, &p)) return;
         const int g = (int)(blockIdx.x % blocks) * kJoinGroups + (t >> 6);
         if (g >= sh.G) return;
         float a = 0.f, b = 0.f;

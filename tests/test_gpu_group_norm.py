@@ -416,3 +416,76 @@ def test_a_first_row_unlike_the_others_in_ragged_samples(before, level, first):
         x[before] = first                                    # of the long sample
         x[-300] = first
         run(x.to(dtype), G, w, b, "silu", offsets, dy=dy.to(dtype))
+
+
+@pytest.mark.parametrize("L,C,G", [(8192, 2048, 2048), (100, 65535, 65535), (500, 32768, 16384)])
+def test_one_sample_of_many_groups(L, C, G):
+    x, w, b, dy = inputs((1, L, C), torch.float32, seed=16)
+    run(x, G, w, b, "silu", dy=dy)
+
+
+def test_ragged_samples_of_many_groups():
+    lens = [60, 1, 0, 5000, 17]
+    offsets = torch.tensor([0] + lens).cumsum(0).to(torch.int32).cuda()
+    x, w, b, dy = inputs((sum(lens), 16384), torch.float32, seed=17)
+    run(x, 16384, w, b, None, offsets, dy=dy)
+
+
+def test_a_large_graph_of_one_channel_to_a_group():
+    """4.3 million rows of 256 channels, statistics of every channel by itself: the last channels against the same channels as
+    a narrower input and against 64 bits."""
+    rows, C = 4300000, 256
+    g = torch.Generator(device="cuda").manual_seed(18)
+    x = torch.randn((rows, C), generator=g, device="cuda", dtype=torch.bfloat16)
+    x.requires_grad_(True)
+    y = layers.group_norm(x, C)
+    tail = x.detach()[:, -2:].double()
+    want = (tail - tail.mean(0)) / (tail.var(0, correction=0) + 1e-5).sqrt()
+    # as in check(): numbers of size 6 at most, deviation 1
+    err = (y.detach()[:, -2:].double() - want).abs()
+    assert (err <= 2.0 ** -8 * want.abs() + E * (K * 6 + (K + 8) * want.abs())).all()
+    dy = torch.randn((rows, C), generator=g, device="cuda", dtype=torch.bfloat16)
+    dx, = torch.autograd.grad(y, x, dy)
+    e = dy[:, -2:].double()
+    r = 1 / (tail.var(0, correction=0) + 1e-5).sqrt()
+    full = r * (e - e.mean(0) - want * (e * want).mean(0))
+    err = (dx[:, -2:].double() - full).abs()
+    assert (err <= 2.0 ** -8 * full.abs() + 8 * K * E * (6 + want.abs())).all()
+
+
+def test_many_short_samples_of_many_tiles():
+    """More samples than a launch has blocks for when their channels take several: the same results as for the last few alone."""
+    B, C, G = 4200000, 315, 105
+    x = torch.zeros((B, 2, C), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(19)
+    for part in (x[:100], x[-100:]):
+        part.copy_(torch.randn(100, 2, C, generator=g, device="cuda"))
+    with torch.no_grad():
+        y = layers.group_norm(x, G, activation="silu")
+        for part, got in ((x[:100], y[:100]), (x[-100:], y[-100:])):
+            assert torch.equal(got, layers.group_norm(part, G, activation="silu"))
+        assert not y[100:-100].any()
+
+
+def test_more_chunks_than_a_launch_has_blocks():
+    """Ragged samples of a group too wide for a block, a chunk to a row: the last sample, which a later launch joins and
+    writes, against the same sample alone."""
+    rows, C, tail = 4300000, 1025, 500
+    g = torch.Generator(device="cuda").manual_seed(21)
+    x = torch.zeros((rows, C), dtype=torch.bfloat16, device="cuda")
+    dy = torch.zeros_like(x)
+    x[-tail:] = torch.randn(tail, C, generator=g, device="cuda").to(torch.bfloat16)
+    dy[-tail:] = torch.randn(tail, C, generator=g, device="cuda").to(torch.bfloat16)
+    w = 1 + 0.2 * torch.randn(C, generator=g, device="cuda")
+
+    def once(x, dy, offsets):
+        x.requires_grad_(True)
+        w.requires_grad_(True)
+        y = layers.group_norm(x, 1, w, activation="silu", offsets=torch.tensor(offsets, dtype=torch.int32, device="cuda"))
+        return y.detach(), *torch.autograd.grad(y, (x, w), dy)
+
+    y, dx, dw = once(x, dy, [0, rows - tail, rows])
+    want = once(x.detach()[-tail:].clone(), dy[-tail:], [0, tail])
+    assert torch.equal(y[-tail:], want[0]) and torch.equal(dx[-tail:], want[1])
+    assert torch.allclose(dw, want[2], rtol=1e-4, atol=1e-3)  # rows in another order
+    assert not y[:1000].any() and not y[rows // 2:rows // 2 + 1000].any() and not dx[:1000].any()
