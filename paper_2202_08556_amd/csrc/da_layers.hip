@@ -87,10 +87,11 @@ NormPlan norm_plan(int dtype, int64_t rows, int64_t samples, bool ragged, int64_
             p.each = true;
             p.E = E;
             p.P = pow2_at_least(ceil_div(cgv, E));
+            // A lane group that goes on to other rows keeps its group where the launch's lane groups are a multiple of G;
+            // where every one of them has a row at most, no more are launched than there are.
             const int64_t per_block = kNormBlock / p.P, m = G / std::gcd(G, per_block);
-            const int64_t need = ceil_div(rows * G, per_block), cap = std::max<int64_t>(m, cus * 8 / m * m);
-            p.each_grid = std::min(cap, ceil_div(need, m) * m);
-            first_rows = p.each_grid;
+            p.each_grid = std::min(ceil_div(rows * G, per_block), std::max<int64_t>(m, cus * 8 / m * m));
+            first_rows = per_block > G ? p.each_grid : std::min(rows, p.each_grid * per_block / G);
         }
     }
     if (!p.each) {

@@ -56,8 +56,10 @@ struct NormShape {
 
 // ------------------------------------------------------------------------------------------
 // each: P lanes hold the cg numbers of one row and group, E accesses of V numbers a lane.  The lane groups of a
-// launch are a multiple of G, so that a lane keeps its columns (parameters and their gradients in registers) from
-// row to row.  BWD: statistics are taken again from the registers; part receives this block's sums of dw and db.
+// launch are a multiple of G (or have a row each), so that a lane keeps its columns (parameters and their gradients in
+// registers) from row to row.  BWD: statistics are taken again from the registers; part receives sums of dw and db: a row of
+// 2 C for every block, or, where a block has no group twice, for every lane group of a group.  (A row for every block would be
+// 64 MB for one row of 8008 numbers in 1001 groups.)
 // 262144 rows of 128 bf16 in groups of 32 with gelu: 37 us forward, 59 backward (3.6 and 3.4 TB/s; a copy 5.2).  The vector
 // instructions, some 27 and 45 a number, take as long as the bytes.
 // ------------------------------------------------------------------------------------------
@@ -197,6 +199,19 @@ __global__ __launch_bounds__(kNormBlock) void norm_each_kernel(NormShape sh, int
         }
     }
     if constexpr (BWD) {
+        if (per_block <= sh.G) {                             // the same for all
+            const long slot = first / sh.G;                  // lane group of its group; those without a row are past the last slot
+            if (slot < min(sh.rows, step)) {
+                float* __restrict__ to = part + slot * 2 * sh.C + col;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if (!on[e]) continue;
+                    store_floats<V>(to + P * e * V, aw[e]);
+                    store_floats<V>(to + sh.C + P * e * V, ab[e]);
+                }
+            }
+            return;
+        }
         // [lane group][position in the group], once for dw and once for db
         const int width = P * E * V;
 #pragma unroll

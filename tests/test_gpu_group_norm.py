@@ -489,3 +489,16 @@ def test_more_chunks_than_a_launch_has_blocks():
     assert torch.equal(y[-tail:], want[0]) and torch.equal(dx[-tail:], want[1])
     assert torch.allclose(dw, want[2], rtol=1e-4, atol=1e-3)  # rows in another order
     assert not y[:1000].any() and not y[rows // 2:rows // 2 + 1000].any() and not dx[:1000].any()
+
+
+# many groups, few rows: lane groups of a block that are no multiple or divisor of the groups
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,C,G", [(1, 8008, 1001), (3, 8008, 1001), (300, 8008, 1001), (700, 4097, 4097), (1, 65528, 8191), (40, 65535, 65535),
+                                      (5000, 771, 257), (9000, 129, 129)])
+def test_rows_of_many_groups(rows, C, G, dtype):
+    x, w, b, dy = inputs((rows, 1, C), dtype, seed=rows)
+    if C == G:                                               # a number by itself is its mean
+        y, dx, _, _ = run(x, G, w, b, None, dy=dy)
+        assert not dx.any()
+    else:
+        run(x, G, w, b, "silu", dy=dy)

@@ -116,3 +116,12 @@ def test_distill_of_no_rows_and_no_classes(dtype, best):
     assert distill(dtype=dtype, rows=0, classes=0, best=best, ldz=0, z=None, index=None, top=None, loss=None) == da.DA_OK
     assert lib().da_distill_backward(dtype, i64(3), i64(0), i64(best), None, i64(0), P, 0, P, 0, f32(1.0), None, None, i64(1), None,
                                      None) == da.DA_OK
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,channels,groups", [(1, 8008, 1001), (1, 65528, 8191), (3, 65535, 65535), (100, 8008, 1001), (10 ** 6, 65535, 65535),
+                                                  (10 ** 6, 983025, 65535)])
+def test_group_norm_workspace_of_rows_of_many_groups(rows, channels, groups, dtype):
+    """Sums of dw and db: two numbers of 32 bits for every number of x at most, and no more than 1 GB."""
+    assert norm_sizes(dtype=dtype, rows=rows, samples=rows, channels=channels, groups=groups) == da.DA_OK
+    assert 0 < SIZES[2].value <= min(8 * rows * channels + 16, 2 ** 30)
