@@ -151,15 +151,16 @@ variable_list norm_backward(const Tensor& dy, const Tensor& x, const Tensor& wei
 }
 
 struct GroupNormBackward : torch::autograd::Node {
-    SavedVariable x, w, b;
+    SavedVariable x, w, b, offsets;
     Tensor stats;
-    NormArgs args;
+    NormArgs args;               // without offsets
 
     void release_variables() override {
         std::lock_guard<std::mutex> lk(mutex_);
         x.reset_data();
         w.reset_data();
         b.reset_data();
+        offsets.reset_data();
         stats.reset();
     }
     variable_list apply(variable_list&& grads) override {
@@ -168,17 +169,19 @@ struct GroupNormBackward : torch::autograd::Node {
     variable_list gradients(const variable_list& grads) {
         if (!grads[0].defined()) return variable_list(3);
         Tensor X, W, B, S;
+        NormArgs a = args;
         {
             std::lock_guard<std::mutex> lk(mutex_);
             X = x.unpack();
             W = w.unpack();
             B = b.unpack();
+            a.offsets = offsets.unpack();
             S = stats;
         }
         variable_list result;
         {
             at::AutoDispatchBelowADInplaceOrView below;
-            result = norm_backward(grads[0], X, W, B, S, args, W.defined() && task_should_compute_output(1),
+            result = norm_backward(grads[0], X, W, B, S, a, W.defined() && task_should_compute_output(1),
                                    B.defined() && task_should_compute_output(2));
         }
         if (!task_should_compute_output(0)) result[0] = Tensor();
@@ -205,7 +208,8 @@ Tensor group_norm(const Tensor& x, int64_t groups, const std::optional<Tensor>& 
     }
     if (train) {
         auto node = std::shared_ptr<GroupNormBackward>(new GroupNormBackward(), torch::autograd::deleteNode);
-        node->args = a;
+        node->args = NormArgs{a.groups, a.eps, a.act, Tensor()};
+        node->offsets = SavedVariable(a.offsets, false);
         node->stats = out.second;
         node->x = SavedVariable(x, false);
         node->w = SavedVariable(w, false);

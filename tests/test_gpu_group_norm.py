@@ -502,3 +502,14 @@ def test_rows_of_many_groups(rows, C, G, dtype):
         assert not dx.any()
     else:
         run(x, G, w, b, "silu", dy=dy)
+
+
+def test_changed_offsets_are_noticed():
+    """A batch's offsets refilled in place before its backward pass."""
+    x, w, b, dy = inputs((40, 24), torch.float32, seed=20)
+    offsets = torch.tensor([0, 3, 3, 40], dtype=torch.int32, device="cuda")
+    x.requires_grad_(True)
+    y = layers.group_norm(x, 3, w, b, offsets=offsets)
+    offsets[1] = 30
+    with pytest.raises(RuntimeError, match="modified"):
+        torch.autograd.grad(y, x, dy)
