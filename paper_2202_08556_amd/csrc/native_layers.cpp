@@ -151,8 +151,7 @@ variable_list norm_backward(const Tensor& dy, const Tensor& x, const Tensor& wei
 }
 
 struct GroupNormBackward : torch::autograd::Node {
-    SavedVariable x, w, b, offsets;
-    Tensor stats;
+    SavedVariable x, w, b, offsets, stats;
     NormArgs args;               // without offsets
 
     void release_variables() override {
@@ -161,7 +160,7 @@ struct GroupNormBackward : torch::autograd::Node {
         w.reset_data();
         b.reset_data();
         offsets.reset_data();
-        stats.reset();
+        stats.reset_data();
     }
     variable_list apply(variable_list&& grads) override {
         return in_backward([&] { return gradients(grads); });
@@ -176,7 +175,7 @@ struct GroupNormBackward : torch::autograd::Node {
             W = w.unpack();
             B = b.unpack();
             a.offsets = offsets.unpack();
-            S = stats;
+            S = stats.unpack();
         }
         variable_list result;
         {
@@ -210,7 +209,7 @@ Tensor group_norm(const Tensor& x, int64_t groups, const std::optional<Tensor>& 
         auto node = std::shared_ptr<GroupNormBackward>(new GroupNormBackward(), torch::autograd::deleteNode);
         node->args = NormArgs{a.groups, a.eps, a.act, Tensor()};
         node->offsets = SavedVariable(a.offsets, false);
-        node->stats = out.second;
+        node->stats = SavedVariable(out.second, false);
         node->x = SavedVariable(x, false);
         node->w = SavedVariable(w, false);
         node->b = SavedVariable(b, false);
@@ -283,8 +282,7 @@ Tensor distill_backward(const Tensor& dloss, const Tensor& z, const Tensor& stat
 
 struct DistillBackward : torch::autograd::Node {
     SavedVariable z;
-    SavedVariable index, top;
-    Tensor stats;
+    SavedVariable index, top, stats;
     double temperature = 1.0;
 
     void release_variables() override {
@@ -292,7 +290,7 @@ struct DistillBackward : torch::autograd::Node {
         z.reset_data();
         index.reset_data();
         top.reset_data();
-        stats.reset();
+        stats.reset_data();
     }
     variable_list apply(variable_list&& grads) override {
         return in_backward([&] { return gradients(grads); });
@@ -305,7 +303,7 @@ struct DistillBackward : torch::autograd::Node {
             std::lock_guard<std::mutex> lk(mutex_);
             Z = z.unpack();
             a = DistillArgs{index.unpack(), top.unpack(), temperature};
-            S = stats;
+            S = stats.unpack();
         }
         variable_list result(1);
         {
@@ -333,7 +331,7 @@ Tensor distill(const Tensor& z, const Tensor& index, const Tensor& top, double t
     if (train) {
         auto node = std::shared_ptr<DistillBackward>(new DistillBackward(), torch::autograd::deleteNode);
         node->temperature = temperature;
-        node->stats = out.second;
+        node->stats = SavedVariable(out.second, false);
         node->z = SavedVariable(z, false);
         node->index = SavedVariable(a.index, false);
         node->top = SavedVariable(a.top, false);
@@ -434,7 +432,7 @@ variable_list gated_backward(const Tensor& dy, const Tensor& x, const Weights& w
 
 struct GatedBackward : torch::autograd::Node {
     SavedVariable x, gate, up, down;
-    GatedKept kept;
+    SavedVariable u, v, a;       // the largest: hooks for saved tensors see them, too
     int act = 0;
 
     void release_variables() override {
@@ -443,7 +441,9 @@ struct GatedBackward : torch::autograd::Node {
         gate.reset_data();
         up.reset_data();
         down.reset_data();
-        kept = GatedKept{};
+        u.reset_data();
+        v.reset_data();
+        a.reset_data();
     }
     variable_list apply(variable_list&& grads) override {
         return in_backward([&] { return gradients(grads); });
@@ -457,7 +457,7 @@ struct GatedBackward : torch::autograd::Node {
             std::lock_guard<std::mutex> lk(mutex_);
             X = x.unpack();
             w = Weights{gate.unpack(), up.unpack(), down.unpack()};
-            k = kept;
+            k = GatedKept{u.unpack(), v.unpack(), a.unpack()};
         }
         std::array<bool, 4> need;
         for (int i = 0; i < 4; ++i) need[i] = task_should_compute_output(i);
@@ -483,7 +483,9 @@ Tensor gated(const Tensor& x, const Tensor& gate, const Tensor& up, const Tensor
     if (train) {
         auto node = std::shared_ptr<GatedBackward>(new GatedBackward(), torch::autograd::deleteNode);
         node->act = act;
-        node->kept = std::move(kept);
+        node->u = SavedVariable(kept.u, false);
+        node->v = SavedVariable(kept.v, false);
+        node->a = SavedVariable(kept.a, false);
         node->x = SavedVariable(x, false);
         node->gate = SavedVariable(gate, false);
         node->up = SavedVariable(up, false);

@@ -81,3 +81,45 @@ def test_changed_operands_are_noticed():
         leaves[3].mul_(2)
     with pytest.raises(RuntimeError, match="modified"):
         y.sum().backward()
+
+
+@pytest.mark.parametrize("name,kept", [("group_norm", 40 * 24 + 2 * 24 + 4 + 3 * 3 * 2), ("gated", 40 * 24 + 3 * 24 * 56 + 3 * 40 * 56),
+                                       ("distill", 40 * 41 + 2 * 40 * 5 + 2 * 40)])
+def test_hooks_see_all_that_is_kept(name, kept):
+    """What waits for the backward pass goes through the hooks for saved tensors and nothing stays beside them: offloaded and
+    brought back, the same results.  kept: operands and statistics; operands, u, v and a."""
+    operands, f = calls()[name]
+    want = run(operands, f)
+    packed = []
+
+    def pack(t):
+        packed.append(t.numel())
+        return t.detach().cpu()
+
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.cuda()):
+        got = run(operands, f)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    assert sum(packed) == kept
+
+
+def test_recomputation_keeps_nothing_of_the_block():
+    """The gated block's hidden numbers (u, v, a: 20 MB each) are not held between forward and backward under checkpoint."""
+    from torch.utils.checkpoint import checkpoint
+    x, wg, wu, wd = (torch.randn(s, device="cuda").requires_grad_(True) for s in ((5000, 16), (16, 1024), (16, 1024), (1024, 16)))
+    layers.gated_feed_forward(x, wg, wu, wd).sum().backward()
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    y = checkpoint(layers.gated_feed_forward, x, wg, wu, wd, use_reentrant=False)
+    assert torch.cuda.memory_allocated() - before < 5000 * 1024 * 4
+    y.sum().backward()
+
+
+@pytest.mark.parametrize("name", ["group_norm", "gated", "distill"])
+def test_function_transforms_and_forward_mode_are_refused(name):
+    operands, f = calls()[name]
+    with pytest.raises(RuntimeError):
+        torch.func.vmap(lambda x: f(x, *operands[1:]))(operands[0].expand(2, *operands[0].shape))
+    with torch.autograd.forward_ad.dual_level():
+        x = torch.autograd.forward_ad.make_dual(operands[0], torch.ones_like(operands[0]))
+        with pytest.raises(RuntimeError):
+            f(x, *operands[1:])
