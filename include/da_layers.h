@@ -102,8 +102,8 @@ int da_distill_backward(int dtype, int64_t rows, int64_t classes, int64_t best, 
  *             rows are multiplied by the vector units forward, with an a of 32 bits).
  *   dx, dw_*  dense; any of them may be NULL and is then not computed
  *
- * Sums are held in 32 bits.  float32 is multiplied as it is (fp32 matrix cores).  All sizes up to 2^30, and fewer than 2^24
- * tiles of a result (DA_ERR_UNSUPPORTED beyond).
+ * Sums are held in 32 bits.  float32 is multiplied as it is (fp32 matrix cores).  All sizes up to 2^30, and fewer than
+ * 2^23 tiles of 128 x 128 of a result, 2^24 where smaller ones are taken (DA_ERR_UNSUPPORTED beyond).
  */
 int da_gated_workspace(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout, size_t *forward_bytes,
                        size_t *backward_bytes /* host, out */);

@@ -86,6 +86,25 @@ inline WidePlan wide_plan(const Product& g) {
     return g.few && g.M > 16 && g.M <= 128 && count * splits >= cus ? WidePlan{128, (int)splits} : WidePlan{0, 1};
 }
 
+// Threads side by side in a launch of a product, whichever kernels take it
+inline int64_t launch_threads(const Product& g, int size) {
+    if (g.M == 0 || g.N == 0) return 0;
+    const int64_t width = g.epi == kGate ? 2 * g.N : g.N;
+    const GemmPlan p = gemm_plan(g, size);
+    const int64_t threads = ceil_div(g.M, p.BM) * ceil_div(width, p.BN) * (p.BM == 128 && p.BN == 128 ? 512 : 256);
+    const WidePlan w = size == 2 ? wide_plan(g) : WidePlan{0, 1};
+    return w.rows ? std::max(threads, ceil_div(g.M, w.rows) * ceil_div(width, kWideColumns) * 2 * w.rows) : threads;
+}
+
+// Whether every launch can be counted: of 2^32 threads and more the high bits are lost
+inline bool gated_fits(const GatedShape& s, int size) {
+    if (std::max({s.rows, s.d, s.h, s.dout}) <= 1 << 17) return true;    // 2^11 x 2^12 tiles at most, of 256 threads
+    for (const Product& g : {gate_product(s), down_product(s), hidden_grad_product(s), input_grad_product(s), up_grad_product(s, 1),
+                             up_grad_product(s, 2), down_grad_product(s)})
+        if (launch_threads(g, size) >= 1LL << 32) return false;
+    return true;
+}
+
 // Scratch of a product: its parts, whichever kernels take it
 inline size_t part_bytes(const Product& g, int size) {
     if (g.M == 0 || g.N == 0) return 0;

@@ -507,16 +507,13 @@ extern "C" int da_distill_backward(int dtype, int64_t rows, int64_t classes, int
 namespace {
 
 constexpr int64_t kGatedMax = 1 << 30;                      // the kernels count rows and columns, and those past the end, in 32 bits
-constexpr int64_t kGatedMaxTiles = 1 << 24;                 // of 2^32 threads and more the high bits are lost
 
 int gated_check(int dtype, int64_t rows, int64_t d, int64_t h, int64_t dout) {
     if (!known_dtype(dtype)) return fail(DA_ERR_UNSUPPORTED, "dtype is neither DA_F32 nor DA_BF16");
     if (rows < 0 || d < 0 || h < 0 || dout < 0) return fail(DA_ERR_INVALID_ARG, "negative size");
     const int64_t most = std::max({rows, d, h, dout});
     if (most > kGatedMax) return fail(DA_ERR_UNSUPPORTED, "size too large");
-    const int64_t n = std::max({d, 2 * h, dout});
-    if (ceil_div(std::max(rows, h), 128) * ceil_div(n, 64) >= kGatedMaxTiles || ceil_div(d, 128) * ceil_div(h, 64) >= kGatedMaxTiles)
-        return fail(DA_ERR_UNSUPPORTED, "size too large");
+    if (!gated_fits(GatedShape{rows, d, h, dout}, dtype == DA_F32 ? 4 : 2)) return fail(DA_ERR_UNSUPPORTED, "size too large");
     return DA_OK;
 }
 

@@ -88,3 +88,55 @@ def test_workspace_of_one_weights_gradient(dtype):
     assert lib.da_gated_workspace(dtype, *map(ctypes.c_int64, (rows, d, h, dout)), ctypes.byref(forward), ctypes.byref(backward)) == 0
     hidden = 2 * rows * h * (4 if dtype == 0 else 2)
     assert backward.value - hidden >= 2 * d * h * 4
+
+
+THREADS = r"""
+#include "da_gated_plan.h"
+#include <cstdio>
+#include <cstdlib>
+namespace daspmm { int compute_units() noexcept { return 256; } }
+using namespace daspmm;
+
+static int64_t threads(const Product& g, int size) {
+    if (g.M == 0 || g.N == 0) return 0;
+    const int64_t width = g.epi == kGate ? 2 * g.N : g.N;
+    const GemmPlan p = gemm_plan(g, size);
+    int64_t most = ceil_div(g.M, p.BM) * ceil_div(width, p.BN) * (p.BM == 128 && p.BN == 128 ? 512 : 256);
+    const WidePlan w = wide_plan(g);
+    if (size == 2 && w.rows) most = std::max(most, ceil_div(g.M, w.rows) * ceil_div(width, kWideColumns) * 2 * w.rows);
+    return most;
+}
+
+int main(int argc, char** argv) {
+    for (int i = 1; i + 3 < argc; i += 4) {
+        const GatedShape s{std::atoll(argv[i]), std::atoll(argv[i + 1]), std::atoll(argv[i + 2]), std::atoll(argv[i + 3])};
+        for (int size : {4, 2})
+            for (const Product& g : {gate_product(s), down_product(s), hidden_grad_product(s), input_grad_product(s), up_grad_product(s, 1),
+                                     up_grad_product(s, 2), down_grad_product(s)})
+                if (threads(g, size) >= 1LL << 32) {
+                    std::printf("rows %ld d %ld h %ld dout %ld: %ld threads side by side\n", (long)s.rows, (long)s.d, (long)s.h, (long)s.dout,
+                                (long)threads(g, size));
+                    return 1;
+                }
+    }
+    return 0;
+}
+"""
+
+
+def test_accepted_sizes_are_no_more_threads_than_a_launch_counts(tmp_path):
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no g++")
+    source, program = tmp_path / "threads.cpp", tmp_path / "threads"
+    source.write_text(THREADS)
+    subprocess.run([gxx, "-O1", "-std=c++17", "-Wall", "-Werror", "-I" + CSRC, str(source), "-o", str(program)], check=True)
+    lib = ctypes.CDLL(os.path.join(ROOT, "paper_2202_08556_amd", "libdaspmm.so"))
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    sizes = (1, 9, 32, 33, 64, 65, 129, 2 ** 20, 2 ** 24, 2 ** 29, 2 ** 29 + 1, 2 ** 30 - 128, 2 ** 30 - 63, 2 ** 30)
+    accepted = [s for s in ((r, d, h, o) for r in sizes for d in sizes for h in sizes for o in sizes)
+                if lib.da_gated_workspace(0, *map(ctypes.c_int64, s), ctypes.byref(a), ctypes.byref(b)) == 0]
+    assert (2 ** 30 - 128, 1, 1, 1) in accepted and len(accepted) > 1000
+    for i in range(0, len(accepted), 2000):
+        res = subprocess.run([str(program), *(str(n) for s in accepted[i:i + 2000] for n in s)], stdout=subprocess.PIPE, text=True)
+        assert res.returncode == 0, res.stdout
