@@ -334,3 +334,33 @@ def test_no_classes(shape, best):
     loss = layers.distill_loss(z, index, torch.ones((*shape, best), device="cuda"), 2.0, "none")
     dz, = torch.autograd.grad(loss, z, torch.ones_like(loss))
     assert loss.shape == shape and not loss.any() and dz.shape == z.shape
+
+
+@pytest.mark.parametrize("reduction", ["sum", "mean"])
+@pytest.mark.parametrize("R,V", [(3, 41), (300000, 3), (5000001, 1)])
+def test_reductions_in_a_graph(R, V, reduction):
+    """The loss of all rows in a graph, replayed between eager work on inputs that change."""
+    g = torch.Generator(device="cuda").manual_seed(13)
+    z = (2 * torch.randn(R, V, generator=g, device="cuda")).requires_grad_(True)
+    index = torch.randint(0, V, (R, 2), generator=g, device="cuda", dtype=torch.int32)
+    top = torch.randn(R, 2, generator=g, device="cuda")
+
+    def once():
+        loss = layers.distill_loss(z, index, top, 1.5, reduction)
+        return loss.detach(), torch.autograd.grad(loss, z)[0]
+
+    once()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = once()
+    for k in range(5):
+        with torch.no_grad():
+            z.mul_(-0.7).add_(0.2 * k)
+        want = once()
+        rows = layers.distill_loss(z.detach(), index, top, 1.5, "none")
+        share = R if reduction == "mean" else 1
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), k
+        assert abs(float(out[0]) - float(rows.double().sum()) / share) <= K * E * float(rows.double().abs().sum()) / share
