@@ -10,8 +10,8 @@
 //   narrow rows  P lanes hold a row in registers
 //   wide rows    one block walks a row with a running maximum and sum; few rows are cut into pieces, a block each,
 //                joined by distill_join_kernel
-// 262144 x 41 float32 with 8 entries: 20 us forward, 36 backward (3 TB/s: rows of 164 bytes, a sixth of the bytes are entries).
-// 2048 x 65536 bf16: 78 us forward, 110 backward (3.5 and 4.9 TB/s; a copy 5.2).
+// 262144 x 41 float32 with 8 entries: 20 us forward, 37 backward (3 TB/s: rows of 164 bytes, a sixth of the bytes are entries).
+// 2048 x 65536 bf16: 79 us forward, 109 backward (3.4 and 4.9 TB/s; a copy 5.2).
 #pragma once
 #include "da_layer_common.h"
 

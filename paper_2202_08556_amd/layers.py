@@ -52,7 +52,7 @@ def group_norm(x: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
     x (..., L, C): every sample is L rows of C channels: (nodes, C) is one graph, (nodes, 1, C) normalises every node
     by itself.  With offsets, int32[samples + 1] on the device, x is (rows, C) and sample s is its rows offsets[s] up to
     offsets[s + 1]: a batch of graphs, empty ones allowed.  offsets are trusted to be well formed (from 0 to rows,
-    non-decreasing), like the row pointers of a matrix.
+    non-decreasing), like the row pointers of a matrix, and left as they are until the backward pass.
     weight, bias: C numbers, float32 or bfloat16 whatever the type of x.  activation: None, "relu", "silu", "gelu", "sigmoid"."""
     act, eps, groups = _activation(activation), float(eps), int(groups)
     if _native.layers_take(x, weight, bias, offsets):
@@ -95,7 +95,7 @@ def gated_feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor
                        activation: str | None = "silu") -> torch.Tensor:
     """(act(x . w_gate) * (x . w_up)) . w_down for x (..., d), w_gate and w_up (d, h), w_down (h, d_out), all float32 or all
     bfloat16.  activation as for group_norm.  For the backward pass both projections are kept in float32 and their gated
-    product in the type of x."""
+    product in the type of x.  Weights whose rows are not dense (a transposed one, say) are copied at every call."""
     act = _activation(activation)
     if _native.layers_take(x, w_gate, w_up, w_down):
         return _native.gated(x, w_gate, w_up, w_down, act)
