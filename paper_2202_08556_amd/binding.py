@@ -40,6 +40,12 @@ DA_ACT_NONE, DA_ACT_RELU, DA_ACT_SILU, DA_ACT_GELU, DA_ACT_SIGMOID = range(5)
 LAYER_EXPORTS = ("da_group_norm_sizes", "da_group_norm", "da_group_norm_backward", "da_distill_workspace", "da_distill",
                  "da_distill_backward", "da_gated_workspace", "da_gated", "da_gated_backward")
 
+# include/da_training.h; called through the extension module
+DA_LOSS_ROWS, DA_LOSS_SUM, DA_LOSS_MEAN = range(3)
+TRAINING_EXPORTS = ("da_rms_norm_workspace", "da_rms_norm", "da_rms_norm_e4m3", "da_rms_norm_backward",
+                    "da_linear_cross_entropy_sizes", "da_linear_cross_entropy", "da_linear_cross_entropy_backward",
+                    "da_orthogonalise_workspace", "da_orthogonalise")
+
 
 class da_features(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("nnz", ctypes.c_int64),

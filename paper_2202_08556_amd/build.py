@@ -11,7 +11,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdaspmm.so")
-SOURCES = ["da_spmm_api.hip", "da_layers.hip", "da_gated_f32.hip", "da_gated_bf16.hip", "da_spmm_select.cpp"]
+SOURCES = ["da_spmm_api.hip", "da_layers.hip", "da_gated_f32.hip", "da_gated_bf16.hip", "da_rms.hip", "da_cross_entropy.hip",
+           "da_orthogonal.hip", "da_spmm_select.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
     # packed fp32 arithmetic stays off for all device code
@@ -76,7 +77,8 @@ def build_native(verbose: bool = False) -> str:
            "-isystem", os.path.join(rocm, "include"), "-DTORCH_EXTENSION_NAME=_native",
            "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"],
            "-isystem", os.path.join(tdir, "include"), "-isystem", os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
-           os.path.join(CSRC, "native.cpp"), os.path.join(CSRC, "native_layers.cpp"), "-o", tmp,
+           os.path.join(CSRC, "native.cpp"), os.path.join(CSRC, "native_layers.cpp"),
+           os.path.join(CSRC, "native_training.cpp"), "-o", tmp,
            "-L" + PKG, "-ldaspmm", "-L" + os.path.join(tdir, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
            "-ltorch_hip", "-lc10", "-lc10_hip", "-lamdhip64", "-L" + os.path.join(rocm, "lib"), "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(tdir, "lib")]
     if verbose:

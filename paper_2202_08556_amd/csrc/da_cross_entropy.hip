@@ -1,0 +1,773 @@
+// Cross entropy of a linear layer on the matrix cores, by pieces of the classes, without keeping logits:
+//   z = x w + b,  loss = log sum exp z - z_target;   dz = g (exp(z - log sum exp) - 1 at the target),
+//   dx = dz w^T,  dw = x^T dz,  db = sum of dz over the rows
+//
+// Forward, a tile of z leaves as the maximum and the sum of exponentials of each of its rows in 64 (or fewer) columns; these are
+// joined by rows.  Backward, z is computed again a piece of the classes at a time, and leaves as dz, which the other two
+// products read: eight operations for each of rows x d x classes instead of six, and no logits in memory.
+// Rows that have a target are gathered first (x is packed for the products anyway), and the products stop at their number,
+// which only the device knows: rows without one cost nothing and may hold anything.
+#include "da_training.h"
+
+#include "da_planes_host.h"
+#include "da_spmm.h"
+
+#include <type_traits>
+
+namespace daspmm {
+namespace {
+
+constexpr int64_t kCeMost = 1 << 22, kCeRowsMost = 1 << 26;
+constexpr int kChunks = 1024;                // of the rows, most
+constexpr int kJoinBlocks = 1024;
+constexpr int64_t kPieceBytes = 512LL << 20;
+constexpr float kLog2e = 1.44269504088896f;
+
+template <class T> using PlaneOf = std::conditional_t<std::is_same_v<T, float>, Halves, One>;
+
+// What a backward pass reads, and how far the arrays behind it are from its start
+struct CeStats {
+    int *count, *index, *target;             // rows that have a target: how many, which, and which class
+    int* place;                              // of every row in that list; -1: not there
+    float* lse;
+};
+size_t stats_bytes(int64_t rows) { return 16 + 4 * round16((size_t)rows * 4); }
+CeStats ce_stats(void* p, int64_t rows) {
+    char* c = static_cast<char*>(p);
+    const size_t n = round16((size_t)rows * 4);
+    auto ints = [&](size_t at) { return reinterpret_cast<int*>(c + at); };
+    return {ints(0), ints(16), ints(16 + n), ints(16 + 2 * n), reinterpret_cast<float*>(c + 16 + 3 * n)};
+}
+
+// Largest magnitudes of x, w and dz's factors, as bits; scale: the power of two that takes them to 2^14 .. 2^15
+enum { kMaxX = 0, kMaxW = 1, kMaxG = 2, kMaxes = 4 };
+struct Scale {
+    float by, inv;
+};
+__device__ __forceinline__ Scale scale_of(uint32_t bits) {
+    const float most = __uint_as_float(bits);
+    int e = 0;
+    if (most > 0.f) (void)frexpf(most, &e);                  // most < 2^e
+    else e = 15;
+    const int k = min(126, max(-126, 15 - e));
+    return {ldexpf(1.f, k), ldexpf(1.f, -k)};
+}
+template <class P> __device__ __forceinline__ Scale scale_at(const uint32_t* maxes, int which) {
+    if constexpr (P::N == 1) return {1.f, 1.f};
+    return scale_of(maxes[which]);
+}
+
+__device__ __forceinline__ long target_of(const void* t, int wide, long r) {
+    return wide ? static_cast<const int64_t*>(t)[r] : (long)static_cast<const int32_t*>(t)[r];
+}
+
+__global__ void ce_zero_kernel(uint32_t* p, int n) {
+    if ((int)threadIdx.x < n) p[threadIdx.x] = 0;
+}
+
+// Rows of a chunk that have a target
+__global__ __launch_bounds__(256) void ce_count_kernel(const void* __restrict__ target, int wide, long rows, long classes, long chunk,
+                                                       int* __restrict__ counts)
+{
+    __shared__ int red[4];
+    const long r0 = blockIdx.x * chunk, r1 = min(r0 + chunk, rows);
+    int n = 0;
+    for (long r = r0 + threadIdx.x; r < r1; r += 256) {
+        const long t = target_of(target, wide, r);
+        n += t >= 0 && t < classes;
+    }
+    n = wave_sum(n, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) counts[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
+// Lists them in order; the others' losses are 0.  counts: of the chunks, where there are several
+__global__ __launch_bounds__(256) void ce_index_kernel(const void* __restrict__ target, int wide, long rows, long classes, long chunk,
+                                                       const int* __restrict__ counts, CeStats st, float* __restrict__ loss,
+                                                       uint32_t* __restrict__ maxes)
+{
+    __shared__ int red[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int before = 0;
+    if (counts) {
+        for (int k = tid; k < (int)blockIdx.x; k += 256) before += counts[k];
+        before = wave_sum(before, 64);
+        if (lane == 0) red[wave] = before;
+        __syncthreads();
+        before = red[0] + red[1] + red[2] + red[3];
+    }
+    if (blockIdx.x == 0 && tid < kMaxes) maxes[tid] = 0;
+    const long r0 = blockIdx.x * chunk, r1 = min(r0 + chunk, rows);
+    for (long r = r0 + tid; r - tid < r1; r += 256) {
+        const long t = r < r1 ? target_of(target, wide, r) : -1;
+        const bool has = t >= 0 && t < classes;
+        const uint64_t mask = __ballot(has);
+        __syncthreads();                                     // the counts before have been read
+        if (lane == 0) red[wave] = __popcll(mask);
+        __syncthreads();
+        int at = before;
+        for (int k = 0; k < wave; ++k) at += red[k];
+        if (has) {
+            at += __popcll(mask & ((1ull << lane) - 1));
+            st.index[at] = (int)r;
+            st.target[at] = (int)t;
+            st.place[r] = at;
+        } else if (r < r1) {
+            st.place[r] = -1;
+            if (loss) loss[r] = 0.f;
+        }
+        before += red[0] + red[1] + red[2] + red[3];
+    }
+    if (r1 == rows && tid == 0) *st.count = before;
+}
+
+__device__ __forceinline__ void keep_largest(float most, uint32_t* to) {
+    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+    // the order of these does not show
+    if ((threadIdx.x & 63) == 0 && most > 0.f) atomicMax(to, __float_as_uint(most));
+}
+__device__ __forceinline__ float magnitude(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.f;                   // infinities and NaN have no part in a scale
+}
+
+// Largest finite magnitudes: blockIdx.y 0 of the rows of x that count, 1 of w
+__global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x, long ldx, CeStats st, long d, const float* __restrict__ w,
+                                                     long numbers, uint32_t* __restrict__ maxes)
+{
+    float most = 0.f;
+    if (blockIdx.y == 0) {
+        const int count = *st.count, lane = threadIdx.x & 63;
+        for (long m = (long)blockIdx.x * 4 + (threadIdx.x >> 6); m < count; m += (long)gridDim.x * 4) {
+            const float* __restrict__ row = x + (long)st.index[m] * ldx;
+            long c = lane * 4;
+            for (; c + 4 <= d; c += 256) {
+                float v[4];
+                load_floats<4>(row + c, v);
+                most = fmaxf(fmaxf(most, fmaxf(magnitude(v[0]), magnitude(v[1]))), fmaxf(magnitude(v[2]), magnitude(v[3])));
+            }
+            for (; c < d; ++c) most = fmaxf(most, magnitude(row[c]));
+        }
+    } else {
+        const long step = (long)gridDim.x * 1024;
+        for (long c = ((long)blockIdx.x * 256 + threadIdx.x) * 4; c < numbers; c += step) {
+            if (c + 4 <= numbers) {
+                float v[4];
+                load_floats<4>(w + c, v);
+                most = fmaxf(fmaxf(most, fmaxf(magnitude(v[0]), magnitude(v[1]))), fmaxf(magnitude(v[2]), magnitude(v[3])));
+            } else {
+                for (long i = c; i < numbers; ++i) most = fmaxf(most, magnitude(w[i]));
+            }
+        }
+    }
+    keep_largest(most, maxes + (blockIdx.y == 0 ? kMaxX : kMaxW));
+}
+
+// Packs `lines` lines of n numbers (index: those of a list, of which *count are there, and zeros up to the next multiple of 64),
+// 8 numbers at a time; lines and their ends are padded with zeros.
+template <class T, class P>
+__global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ from, long ld, long lines, int n, const int* __restrict__ index,
+                                                      const int* __restrict__ count, const uint32_t* __restrict__ maxes, int which,
+                                                      uint16_t* __restrict__ to, long ldt)
+{
+    const Scale s = scale_at<P>(maxes, which);
+    const int pieces = (int)(padded(n) / 8);
+    const long there = index ? *count : lines, all = padded(there) * pieces;
+    for (long k = (long)blockIdx.x * 256 + threadIdx.x; k < all; k += (long)gridDim.x * 256) {
+        const long line = k / pieces;
+        const int at = (int)(k % pieces) * 8;
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        if (line < there) {
+            const T* __restrict__ p = from + (index ? (long)index[line] : line) * ld + at;
+            if (at + 8 <= n) {
+                load_floats<8>(p, x);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (at + i < n) {
+                        float one[1];
+                        load_floats<1>(p + i, one);
+                        x[i] = one[0];
+                    }
+            }
+        }
+        if constexpr (P::N == 2)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= s.by;
+        put_values<P, 8>(to + line * ldt, at, x);
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// Epilogues
+// ------------------------------------------------------------------------------------------
+template <class P> struct Logits {
+    const uint32_t* maxes;
+    const void* bias;
+    int bias_type;
+    int classes;
+    CeStats st;
+    // the scales leave one after the other: their product may not be a float
+    __device__ __forceinline__ float logit(float x, int n, const Scale& sx, const Scale& sw) const {
+        if constexpr (P::N == 2) x = x * sx.inv * sw.inv;
+        return bias ? x + load_param(bias, bias_type, n) : x;
+    }
+};
+
+// A row's maximum and sum of exponentials in the columns of a wave
+template <class P> struct SumsOut : Logits<P> {
+    static constexpr bool kSymmetric = false, kWhole = true;
+    float2* part;                // [row][slot]
+    int slots;
+    float* at_target;            // [row]
+    template <int MT, int NT> __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int slot) const {
+        const int i16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4, count = *this->st.count;
+        const Scale sx = scale_at<P>(this->maxes, kMaxX), sw = scale_at<P>(this->maxes, kMaxW);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int m = mw + i * 16 + i16;
+            const int t = m < count ? this->st.target[m] : -1;
+            float z[NT][4], most = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = nw + j * 16 + 4 * h + q;
+                    z[j][q] = n < this->classes ? this->logit(acc[i][j][q], n, sx, sw) : -INFINITY;
+                    most = fmaxf(most, z[j][q]);
+                    if (n == t) at_target[m] = z[j][q];
+                }
+            most = fmaxf(most, __shfl_xor(most, 16, 64));
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            const float from = most == -INFINITY ? 0.f : most;
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum += exp2_hw((z[j][q] - from) * kLog2e);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (h == 0 && m < count) part[(long)m * slots + slot] = make_float2(most, sum);
+        }
+    }
+};
+
+// dz of a piece of the classes that begins at `first`; rows behind the last one are 0
+template <class P> struct GradOut : Logits<P> {
+    static constexpr bool kSymmetric = false, kWhole = false;
+    const float* g;
+    int first;
+    uint16_t* dz;
+    long ldz;
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool, int) const {
+        const int count = *this->st.count;
+        if (m < count) {
+            const Scale sx = scale_at<P>(this->maxes, kMaxX), sw = scale_at<P>(this->maxes, kMaxW);
+            const float lse = this->st.lse[m];
+            const int t = this->st.target[m] - first;
+            const float by = g[m] * scale_at<P>(this->maxes, kMaxG).by;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (first + n + q < this->classes) {
+                    const float p = exp2_hw((this->logit(x[q], first + n + q, sx, sw) - lse) * kLog2e);
+                    x[q] = by * (n + q == t ? p - 1.f : p);
+                } else {
+                    x[q] = 0.f;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = 0.f;
+        }
+        put_values<P, 4>(dz + (long)m * ldz, n, x);
+    }
+};
+
+template <class T> __device__ __forceinline__ void store_row(T* p, int left, const float (&x)[4]) {
+    if (left >= 4) {
+        store_floats<4>(p, x);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            const float one[1] = {x[q]};
+            if (q < left) store_floats<1>(p + q, one);
+        }
+    }
+}
+
+// dx, or what the pieces so far give of it
+template <class T, class P> struct InputOut {
+    static constexpr bool kSymmetric = false, kWhole = false;
+    const uint32_t* maxes;
+    CeStats st;
+    const float* before;         // dense rows x ldb, packed rows
+    float* after;                // where not null: the sum goes here instead of to dx
+    long ldb;
+    T* dx;
+    int d;
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool, int) const {
+        if (m >= *st.count || n >= d) return;
+        const Scale sg = scale_at<P>(maxes, kMaxG), sw = scale_at<P>(maxes, kMaxW);
+        if constexpr (P::N == 2)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = x[q] * sw.inv * sg.inv;
+        if (before) {
+            float u[4];
+            load_floats<4>(before + (long)m * ldb + n, u);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] += u[q];
+        }
+        if (after) store_floats<4>(after + (long)m * ldb + n, x);
+        else store_row(dx + (long)st.index[m] * d + n, d - n, x);
+    }
+};
+
+template <class T, class P> struct WeightOut {
+    static constexpr bool kSymmetric = false, kWhole = false;
+    const uint32_t* maxes;
+    T* dw;                       // of the piece
+    long ldw;
+    int d, classes;              // of the piece
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool, int) const {
+        if (m >= d || n >= classes) return;
+        const Scale sg = scale_at<P>(maxes, kMaxG), sx = scale_at<P>(maxes, kMaxX);
+        if constexpr (P::N == 2)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = x[q] * sx.inv * sg.inv;
+        store_row(dw + (long)m * ldw + n, classes - n, x);
+    }
+};
+
+// ------------------------------------------------------------------------------------------
+// Rows
+// ------------------------------------------------------------------------------------------
+// log sum exp and loss of the rows, P lanes to one; with sums, those of the blocks' losses
+__global__ __launch_bounds__(256) void ce_join_kernel(CeStats st, const float2* __restrict__ part, int slots, int P,
+                                                      const float* __restrict__ at_target, float* __restrict__ loss, double* __restrict__ sums)
+{
+    __shared__ double red[4];
+    const int lane = threadIdx.x & (P - 1), count = *st.count, teams = 256 / P;
+    double total = 0.0;
+    for (long m = (long)blockIdx.x * teams + threadIdx.x / P; m < count; m += (long)gridDim.x * teams) {
+        const float2* __restrict__ p = part + m * slots;
+        float most = -INFINITY, sum = 0.f;
+        for (int k = lane; k < slots; k += P) most = fmaxf(most, p[k].x);
+        for (int d = 1; d < P; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+        const float from = most == -INFINITY ? 0.f : most;
+        for (int k = lane; k < slots; k += P) sum += p[k].y * exp2_hw((p[k].x - from) * kLog2e);
+        sum = wave_sum(sum, P);
+        const float lse = most + logf(sum), l = lse - at_target[m];
+        if (lane == 0) {
+            st.lse[m] = lse;
+            if (loss) loss[st.index[m]] = l;
+            total += l;
+        }
+    }
+    if (!sums) return;
+    total = wave_sum(total, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) sums[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+__global__ __launch_bounds__(256) void ce_total_kernel(CeStats st, const double* __restrict__ sums, int blocks, int mean, float* loss)
+{
+    __shared__ double red[4];
+    double s = 0.0;
+    for (int k = threadIdx.x; k < blocks; k += 256) s += sums[k];
+    s = wave_sum(s, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = (red[0] + red[1]) + (red[2] + red[3]);
+        *loss = (float)(mean ? s / max(1, *st.count) : s);
+    }
+}
+
+// The factor of each row's gradient, and the largest of them
+__global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, long rows, const float* __restrict__ dloss, long stride, int reduction,
+                                                        float* __restrict__ g, uint32_t* __restrict__ maxes)
+{
+    const int count = *st.count;
+    float most = 0.f;
+    for (long m = (long)blockIdx.x * 256 + threadIdx.x; m < count; m += (long)gridDim.x * 256) {
+        const float v = reduction == DA_LOSS_ROWS ? dloss[st.index[m] * stride] : reduction == DA_LOSS_MEAN ? dloss[0] / (float)count : dloss[0];
+        g[m] = v;
+        most = fmaxf(most, magnitude(v));
+    }
+    keep_largest(most, maxes + kMaxG);
+}
+// Rows of dx without a target
+template <class T>
+__global__ __launch_bounds__(256) void ce_rest_kernel(CeStats st, long rows, int d, T* __restrict__ dx)
+{
+    const int lane = threadIdx.x & 63;
+    for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (long)gridDim.x * 4) {
+        if (st.place[r] >= 0) continue;
+        for (int k = lane * 4; k < d; k += 256) {
+            const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+            store_row(dx + r * d + k, d - k, zero);
+        }
+    }
+}
+
+// db: sums of dz's columns over parts of the rows, then over the parts
+template <class P>
+__global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t* __restrict__ dz, long ldz, int Nb, long per, float* __restrict__ part)
+{
+    __shared__ f32x4 red[4][64];
+    const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4, k = threadIdx.x >> 6;
+    const long r0 = blockIdx.y * per, r1 = min(r0 + per, (long)*st.count);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (n < Nb)
+        for (long m = r0 + k; m < r1; m += 4) {
+            float x[4];
+            get_values<P, 4>(dz + m * ldz, n, x);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s[q] += x[q];
+        }
+    red[k][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (k == 0 && n < Nb) {
+        const int l = threadIdx.x;
+        *reinterpret_cast<f32x4*>(part + (long)blockIdx.y * Nb + n) = (red[0][l] + red[1][l]) + (red[2][l] + red[3][l]);
+    }
+}
+template <class P>
+__global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restrict__ part, int parts, int Nb, int classes,
+                                                           const uint32_t* __restrict__ maxes, void* db, int type, int first)
+{
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= classes) return;
+    float s[4] = {};
+    int k = 0;
+    for (; k + 4 <= parts; k += 4)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] += part[(long)(k + u) * Nb + n];
+    for (; k < parts; ++k) s[0] += part[(long)k * Nb + n];
+    store_param(db, type, first + n, ((s[0] + s[1]) + (s[2] + s[3])) * scale_at<P>(maxes, kMaxG).inv);
+}
+
+// ------------------------------------------------------------------------------------------
+// Host
+// ------------------------------------------------------------------------------------------
+int fail(int code, const char* text) { return set_error(code, text); }
+int launched(const char* where) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? DA_OK : set_hip_error(e, where);
+}
+
+struct CeShape {
+    int64_t rows, d, V;
+};
+
+struct CePlan {
+    int64_t Ma, D, Vb;           // rows, d and classes, padded
+    int64_t chunk, chunks;       // of the rows
+    PlanePlan logits;
+    int slots;
+    int64_t piece;               // classes of a piece, a multiple of 64 where there are several
+    int bias_parts;
+    size_t counts_at, sums_at, target_at, x_at, w_at, part_at, forward;          // bytes
+    size_t g_at, dz_at, dx_at, bias_at, sum_at, backward;
+};
+
+int wave_columns(const PlanePlan& p) { return p.shape == 0 ? PlaneLarge::WN : p.shape == 1 ? PlaneMiddle::WN : PlaneSmall::WN; }
+
+struct PiecePlan {
+    PlanePlan logits, input, weight;
+};
+PiecePlan piece_plan(const CePlan& p, int64_t width, int step) {
+    const int64_t Vb = padded(width);
+    return {plane_plan(p.Ma, Vb, p.D / step, 1, false, false), plane_plan(p.Ma, p.D, Vb / step, 1, false, true),
+            plane_plan(p.D, Vb, p.Ma / step, 1, false, true)};
+}
+
+CePlan ce_plan(int dtype, const CeShape& s) {
+    CePlan p{};
+    const int N = dtype == DA_F32 ? 2 : 1, step = N == 2 ? Halves::STEP : One::STEP;
+    p.Ma = padded(s.rows);
+    p.D = padded(s.d);
+    p.Vb = padded(s.V);
+    p.chunk = std::max<int64_t>(2048, ceil_div(ceil_div(s.rows, kChunks), 256) * 256);
+    p.chunks = std::max<int64_t>(1, ceil_div(s.rows, p.chunk));
+    p.logits = plane_plan(p.Ma, p.Vb, p.D / step, 1, false, false);
+    p.slots = p.logits.tiles_n * wave_columns(p.logits);
+    size_t at = 16;                                          // the largest magnitudes
+    auto take = [&](size_t bytes) {
+        const size_t from = at;
+        at += round16(bytes);
+        return from;
+    };
+    p.x_at = take((size_t)p.Ma * p.D * 2 * N);
+    p.w_at = take((size_t)p.D * p.Vb * 2 * N);
+    const size_t both = at;
+    p.counts_at = take((size_t)p.chunks * 4);
+    p.sums_at = take(kJoinBlocks * sizeof(double));
+    p.target_at = take((size_t)p.Ma * 4);
+    p.part_at = take((size_t)p.Ma * p.slots * sizeof(float2));
+    p.forward = at;
+
+    at = both;
+    p.g_at = take((size_t)p.Ma * 4);
+    p.piece = std::max<int64_t>(1024, kPieceBytes / std::max<int64_t>(1, p.Ma * 2 * N) / 256 * 256);
+    if (p.piece >= s.V) p.piece = std::max<int64_t>(s.V, 1);
+    const int64_t Pb = padded(p.piece);
+    p.dz_at = take((size_t)p.Ma * Pb * 2 * N);
+    p.dx_at = take(p.piece < s.V ? (size_t)p.Ma * p.D * 4 : 0);
+    p.bias_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(s.rows, 64), std::max<int64_t>(1, 1024 / ceil_div(Pb, 256))));
+    p.bias_at = take((size_t)p.bias_parts * Pb * 4);
+    size_t sums = 0;
+    for (const int64_t width : {p.piece, s.V % p.piece})
+        if (width > 0) {
+            const PiecePlan q = piece_plan(p, width, step);
+            sums = std::max({sums, plane_part_bytes(q.input, p.Ma, p.D, 1), plane_part_bytes(q.weight, p.D, padded(width), 1)});
+        }
+    p.sum_at = take(sums);
+    p.backward = at;
+    return p;
+}
+
+int ce_check(int dtype, int64_t rows, int64_t d, int64_t classes) {
+    if (dtype != DA_F32 && dtype != DA_BF16) return fail(DA_ERR_UNSUPPORTED, "dtype is neither DA_F32 nor DA_BF16");
+    if (rows < 0 || d < 0 || classes < 0) return fail(DA_ERR_INVALID_ARG, "negative size");
+    if (rows > kCeRowsMost || d > kCeMost || classes > kCeMost) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    // a launch's threads are counted in 32 bits: tiles of 256 x 256 where there are many, and 512 threads to one
+    const int64_t m = ceil_div(rows, 256), n = ceil_div(d, 256), v = ceil_div(classes, 256);
+    if (std::max({m * v, m * n, n * v}) >= 1 << 23) return fail(DA_ERR_UNSUPPORTED, "size too large");
+    return DA_OK;
+}
+
+struct CeCall {
+    CeShape s;
+    CePlan p;
+    const void *x, *w, *b;
+    int64_t ldx;
+    int param_dtype;
+    CeStats st;
+    char* ws;
+    hipStream_t stream;
+};
+
+template <class T> const uint16_t* pack_operands(const CeCall& c, long* ldw) {
+    typedef PlaneOf<T> P;
+    uint32_t* maxes = reinterpret_cast<uint32_t*>(c.ws);
+    const T* x = static_cast<const T*>(c.x);
+    const T* w = static_cast<const T*>(c.w);
+    if constexpr (P::N == 2) {
+        const int64_t most = std::max(ceil_div(c.s.rows, 4), ceil_div(c.s.d * c.s.V, 4096));
+        hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 2048)), 2), dim3(256), 0, c.stream, x,
+                           (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V), maxes);
+    }
+    auto pack = [&](const T* from, long ld, long lines, int n, const int* index, int which, size_t to) {
+        const int64_t blocks = std::min<int64_t>(ceil_div(padded(lines) * (padded(n) / 8), 256), 8192);
+        if (blocks)
+            hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)blocks), dim3(256), 0, c.stream, from, ld, lines, n, index, c.st.count, maxes,
+                               which, reinterpret_cast<uint16_t*>(c.ws + to), (long)(padded(n) * P::N));
+    };
+    pack(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, kMaxX, c.p.x_at);
+    // a weight of whole pads is read where it is
+    if (P::N == 1 && c.s.d % kPad == 0 && c.s.V % kPad == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0) {
+        *ldw = c.s.V;
+        return reinterpret_cast<const uint16_t*>(w);
+    }
+    pack(w, c.s.V, c.s.d, (int)c.s.V, nullptr, kMaxW, c.p.w_at);
+    *ldw = c.p.Vb * P::N;
+    return reinterpret_cast<const uint16_t*>(c.ws + c.p.w_at);
+}
+
+template <class P> void fill(Logits<P>& l, const CeCall& c) {
+    l.maxes = reinterpret_cast<const uint32_t*>(c.ws);
+    l.bias = c.b;
+    l.bias_type = c.param_dtype;
+    l.classes = (int)c.s.V;
+    l.st = c.st;
+}
+
+// Operands of the logits' product of the classes from `first` on
+template <class P> PlaneArgs logits_args(const CeCall& c, const uint16_t* w, long ldw, int64_t first, int64_t width) {
+    PlaneArgs g{};
+    g.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
+    g.lda = c.p.D * P::N;
+    g.B = w + first * P::N;
+    g.ldb = ldw;
+    g.Ma = (int)c.p.Ma;
+    g.Nb = (int)padded(width);
+    g.K = (int)c.p.D;
+    g.rows = c.st.count;
+    return g;
+}
+
+template <class T>
+void ce_forward(const CeCall& c, const void* target, int target64, int reduction, float* loss) {
+    typedef PlaneOf<T> P;
+    int* counts = reinterpret_cast<int*>(c.ws + c.p.counts_at);
+    const bool several = c.p.chunks > 1;
+    if (several)
+        hipLaunchKernelGGL(ce_count_kernel, dim3((unsigned)c.p.chunks), dim3(256), 0, c.stream, target, target64, (long)c.s.rows, (long)c.s.V,
+                           (long)c.p.chunk, counts);
+    float* rows = reduction == DA_LOSS_ROWS ? loss : nullptr;
+    hipLaunchKernelGGL(ce_index_kernel, dim3((unsigned)c.p.chunks), dim3(256), 0, c.stream, target, target64, (long)c.s.rows, (long)c.s.V,
+                       (long)c.p.chunk, several ? counts : nullptr, c.st, rows, reinterpret_cast<uint32_t*>(c.ws));
+    long ldw = 0;
+    const uint16_t* w = pack_operands<T>(c, &ldw);
+    SumsOut<P> out{};
+    fill(out, c);
+    out.part = reinterpret_cast<float2*>(c.ws + c.p.part_at);
+    out.slots = c.p.slots;
+    out.at_target = reinterpret_cast<float*>(c.ws + c.p.target_at);
+    plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, 0, c.s.V), out, c.p.logits, 1, nullptr, c.stream);
+    int lanes = 1;
+    while (lanes < 64 && lanes < c.p.slots) lanes *= 2;
+    double* sums = reduction == DA_LOSS_ROWS ? nullptr : reinterpret_cast<double*>(c.ws + c.p.sums_at);
+    const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256 / lanes), kJoinBlocks));
+    hipLaunchKernelGGL(ce_join_kernel, dim3(blocks), dim3(256), 0, c.stream, c.st, out.part, c.p.slots, lanes, out.at_target, rows, sums);
+    if (sums) hipLaunchKernelGGL(ce_total_kernel, dim3(1), dim3(256), 0, c.stream, c.st, sums, blocks, (int)(reduction == DA_LOSS_MEAN), loss);
+}
+
+template <class T>
+void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, T* dx, T* dw, void* db) {
+    typedef PlaneOf<T> P;
+    uint32_t* maxes = reinterpret_cast<uint32_t*>(c.ws);
+    float* g = reinterpret_cast<float*>(c.ws + c.p.g_at);
+    hipLaunchKernelGGL(ce_zero_kernel, dim3(1), dim3(64), 0, c.stream, maxes, (int)kMaxes);
+    hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 1024))), dim3(256), 0,
+                       c.stream, c.st, (long)c.s.rows, dloss, (long)stride, reduction, g, maxes);
+    if (dx && c.s.d > 0 && c.s.rows > 0)
+        hipLaunchKernelGGL((ce_rest_kernel<T>), dim3((unsigned)std::min<int64_t>(ceil_div(c.s.rows, 4), 4096)), dim3(256), 0, c.stream, c.st,
+                           (long)c.s.rows, (int)c.s.d, dx);
+    if (c.s.V == 0) return;
+    long ldw = 0;
+    const uint16_t* w = pack_operands<T>(c, &ldw);
+    uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + c.p.dz_at);
+    float* acc = reinterpret_cast<float*>(c.ws + c.p.dx_at);
+    float* part = reinterpret_cast<float*>(c.ws + c.p.sum_at);
+    float* bias = reinterpret_cast<float*>(c.ws + c.p.bias_at);
+    for (int64_t first = 0; first < c.s.V; first += c.p.piece) {
+        const int64_t width = std::min(c.p.piece, c.s.V - first), Vb = padded(width);
+        const PiecePlan q = piece_plan(c.p, width, P::STEP);
+        const long ldz = Vb * P::N;
+        GradOut<P> grad{};
+        fill(grad, c);
+        grad.g = g;
+        grad.first = (int)first;
+        grad.dz = dz;
+        grad.ldz = ldz;
+        plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, first, width), grad, q.logits, 1, nullptr, c.stream);
+        if (dx && c.s.d > 0) {
+            PlaneArgs a{};
+            a.A = dz;
+            a.lda = ldz;
+            a.B = w + first * P::N;
+            a.ldb = ldw;
+            a.Ma = (int)c.p.Ma;
+            a.Nb = (int)c.p.D;
+            a.K = (int)Vb;
+            a.rows = c.st.count;
+            InputOut<T, P> out{};
+            out.maxes = maxes;
+            out.st = c.st;
+            out.before = first > 0 ? acc : nullptr;
+            out.after = first + width < c.s.V ? acc : nullptr;
+            out.ldb = c.p.D;
+            out.dx = dx;
+            out.d = (int)c.s.d;
+            plane_product<P, kAlong, kAlong, kBoundM>(a, out, q.input, 1, part, c.stream);
+        }
+        if (dw && c.s.d > 0) {
+            PlaneArgs a{};
+            a.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
+            a.lda = c.p.D * P::N;
+            a.B = dz;
+            a.ldb = ldz;
+            a.Ma = (int)c.p.D;
+            a.Nb = (int)Vb;
+            a.K = (int)c.p.Ma;
+            a.rows = c.st.count;
+            const WeightOut<T, P> out{maxes, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
+            plane_product<P, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, c.stream);
+        }
+        if (db) {
+            const int64_t per = ceil_div(c.s.rows, c.p.bias_parts);
+            hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, ldz,
+                               (int)Vb, (long)per, bias);
+            hipLaunchKernelGGL((ce_bias_join_kernel<P>), dim3((unsigned)ceil_div(width, 256)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
+                               (int)width, maxes, db, c.param_dtype, (int)first);
+        }
+    }
+}
+
+int ce_call(int dtype, int64_t rows, int64_t d, int64_t classes, const void* x, int64_t ldx, const void* w, const void* b, int param_dtype,
+            int reduction, const void* stats, void* workspace, size_t workspace_bytes, bool backward, void* stream, CeCall* c) {
+    const int st = ce_check(dtype, rows, d, classes);
+    if (st != DA_OK) return st;
+    if (b && param_dtype != DA_F32 && param_dtype != DA_BF16) return fail(DA_ERR_UNSUPPORTED, "param_dtype is neither DA_F32 nor DA_BF16");
+    if (reduction != DA_LOSS_ROWS && reduction != DA_LOSS_SUM && reduction != DA_LOSS_MEAN) return fail(DA_ERR_INVALID_ARG, "unknown reduction");
+    if (ldx < d) return fail(DA_ERR_INVALID_ARG, "leading dimension smaller than the extent it strides over");
+    if ((rows > 0 && d > 0 && !x) || (d > 0 && classes > 0 && !w)) return fail(DA_ERR_INVALID_ARG, "null x or w");
+    if (!stats || reinterpret_cast<uintptr_t>(stats) % 16 != 0) return fail(DA_ERR_INVALID_ARG, "stats missing or misaligned");
+    c->s = CeShape{rows, d, classes};
+    c->p = ce_plan(dtype, c->s);
+    if (!workspace || workspace_bytes < (backward ? c->p.backward : c->p.forward) || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
+        return fail(DA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than reported");
+    c->x = x;
+    c->w = w;
+    c->b = b;
+    c->ldx = ldx;
+    c->param_dtype = param_dtype;
+    c->st = ce_stats(const_cast<void*>(stats), rows);
+    c->ws = static_cast<char*>(workspace);
+    c->stream = (hipStream_t)stream;
+    return DA_OK;
+}
+
+}  // namespace
+}  // namespace daspmm
+
+using namespace daspmm;
+
+extern "C" int da_linear_cross_entropy_sizes(int dtype, int64_t rows, int64_t d, int64_t classes, size_t* stats, size_t* forward_bytes,
+                                             size_t* backward_bytes)
+{
+    if (!stats || !forward_bytes || !backward_bytes) return fail(DA_ERR_INVALID_ARG, "null output");
+    const int st = ce_check(dtype, rows, d, classes);
+    if (st != DA_OK) return st;
+    const CePlan p = ce_plan(dtype, CeShape{rows, d, classes});
+    *stats = stats_bytes(rows);
+    *forward_bytes = p.forward;
+    *backward_bytes = p.backward;
+    return DA_OK;
+}
+
+extern "C" int da_linear_cross_entropy(int dtype, int64_t rows, int64_t d, int64_t classes, const void* x, int64_t ldx, const void* w,
+                                       const void* b, int param_dtype, const void* target, int target64, int reduction, float* loss,
+                                       void* stats, void* workspace, size_t workspace_bytes, void* stream)
+{
+    CeCall c{};
+    const int st = ce_call(dtype, rows, d, classes, x, ldx, w, b, param_dtype, reduction, stats, workspace, workspace_bytes, false, stream, &c);
+    if (st != DA_OK) return st;
+    if (rows > 0 && !target) return fail(DA_ERR_INVALID_ARG, "null target");
+    if (!loss && (rows > 0 || reduction != DA_LOSS_ROWS)) return fail(DA_ERR_INVALID_ARG, "null loss");
+    if (dtype == DA_F32) ce_forward<float>(c, target, target64, reduction, loss);
+    else ce_forward<bf16>(c, target, target64, reduction, loss);
+    return launched("da_linear_cross_entropy launch");
+}
+
+extern "C" int da_linear_cross_entropy_backward(int dtype, int64_t rows, int64_t d, int64_t classes, const void* x, int64_t ldx,
+                                                const void* w, const void* b, int param_dtype, int reduction, const void* stats,
+                                                const float* dloss, int64_t dloss_stride, void* dx, void* dw, void* db, void* workspace,
+                                                size_t workspace_bytes, void* stream)
+{
+    CeCall c{};
+    const int st = ce_call(dtype, rows, d, classes, x, ldx, w, b, param_dtype, reduction, stats, workspace, workspace_bytes, true, stream, &c);
+    if (st != DA_OK) return st;
+    if (dloss_stride < 0) return fail(DA_ERR_INVALID_ARG, "negative stride");
+    if (!dloss && (rows > 0 || reduction != DA_LOSS_ROWS)) return fail(DA_ERR_INVALID_ARG, "null dloss");
+    if (db && param_dtype != DA_F32 && param_dtype != DA_BF16) return fail(DA_ERR_UNSUPPORTED, "param_dtype is neither DA_F32 nor DA_BF16");
+    if (!dx && !dw && !db) return DA_OK;
+    if (dtype == DA_F32) ce_backward<float>(c, reduction, dloss, dloss_stride, static_cast<float*>(dx), static_cast<float*>(dw), db);
+    else ce_backward<bf16>(c, reduction, dloss, dloss_stride, static_cast<bf16*>(dx), static_cast<bf16*>(dw), db);
+    return launched("da_linear_cross_entropy_backward launch");
+}

@@ -1,0 +1,363 @@
+// Matrices as the matrix cores take them: packed in 16-bit numbers, padded with zeros to multiples of 64 both ways, and
+// products of them whose epilogues are those of the operators that use them.
+//
+// A number is one bf16 (One), or the sum of two fp16 (Halves): the nearest fp16 and what that leaves.  A pair has 22 bits;
+// the arrays are scaled by a power of two so that the largest number is below 2^15, and the second half of numbers 2^18
+// times less begins to lose bits, 2^-25 of the scale.  The product of two pairs is three instructions of 16-bit numbers
+// (the fourth, of both second halves, is below the 22 bits) in place of one of 32-bit numbers at a sixteenth of the rate.
+//
+// Pairs lie in groups of 32: 32 first halves and 32 second ones along a line, so that 64 bytes of either are 128 in one
+// place.
+#pragma once
+#include "da_gated_plan.h"
+#include "da_layer_common.h"
+
+namespace daspmm {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+enum { kAlong = 0, kAcross = 1 };            // a line of memory goes along the inner axis, or across it
+
+constexpr int kPad = 64;
+__host__ __device__ inline long padded(long n) { return (n + kPad - 1) / kPad * kPad; }
+
+struct One {
+    static constexpr int N = 1, STEP = 64;   // numbers of a value, inner positions of a step
+    typedef bf16x8 Frag;
+    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+struct Halves {
+    static constexpr int N = 2, STEP = 32;
+    typedef f16x8 Frag;
+    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+// V neighbouring values of a packed line from position `at` (a multiple of V) on
+template <class P, int V> __device__ __forceinline__ void put_values(uint16_t* line, long at, const float (&x)[V]) {
+    typedef uint16_t Bits __attribute__((ext_vector_type(V)));
+    if constexpr (P::N == 1) {
+        Bits b;
+#pragma unroll
+        for (int i = 0; i < V; ++i) b[i] = __builtin_bit_cast(uint16_t, (bf16)x[i]);
+        *reinterpret_cast<Bits*>(line + at) = b;
+    } else {
+        Bits first, second;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const _Float16 h = (_Float16)x[i];
+            const float rest = x[i] - (float)h;              // exact; of an infinity: none
+            first[i] = __builtin_bit_cast(uint16_t, h);
+            second[i] = __builtin_bit_cast(uint16_t, (_Float16)(rest == rest ? rest : 0.f));
+        }
+        uint16_t* p = line + at / 32 * 64 + at % 32;
+        *reinterpret_cast<Bits*>(p) = first;
+        *reinterpret_cast<Bits*>(p + 32) = second;
+    }
+}
+template <class P, int V> __device__ __forceinline__ void get_values(const uint16_t* line, long at, float (&x)[V]) {
+    typedef uint16_t Bits __attribute__((ext_vector_type(V)));
+    if constexpr (P::N == 1) {
+        const Bits b = *reinterpret_cast<const Bits*>(line + at);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = __uint_as_float((uint32_t)b[i] << 16);
+    } else {
+        const uint16_t* p = line + at / 32 * 64 + at % 32;
+        const Bits first = *reinterpret_cast<const Bits*>(p), second = *reinterpret_cast<const Bits*>(p + 32);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)first[i]) + (float)__builtin_bit_cast(_Float16, (uint16_t)second[i]);
+    }
+}
+
+// One operand's part of a step in LDS: OUTER x STEP values, lines of 128 bytes (along) or of OUTER values (across).
+// A 16-byte piece of a line goes to a place chosen by an exclusive or with bits of the line's number, so that the lanes that
+// are served together read from different banks; memory is read through the same permutation, since the lanes of a load
+// write to LDS side by side.
+template <class P, int LAY, int OUTER> struct PlaneTile {
+    static constexpr int LINE = LAY == kAlong ? 64 : OUTER * P::N;           // numbers
+    static constexpr int BYTES = OUTER * 128;
+    // piece q in LDS order: which line, and which numbers of it
+    static __device__ __forceinline__ void piece(int q, int* line, int* at) {
+        if constexpr (LAY == kAlong) {
+            *line = q / 8;
+            *at = ((q & 7) ^ turn(*line)) * 8;
+        } else {
+            const int p = q % (LINE / 8);
+            *line = q / (LINE / 8);
+            *at = (((p >> 1) ^ twist(*line)) * 2 + (p & 1)) * 8;
+        }
+    }
+    static __device__ __forceinline__ int turn(int line) { return line >> 1 & 7; }
+    static __device__ __forceinline__ int twist(int line) { return ((line & 3) | ((line >> 3) & 3) << 2) & (LINE / 16 - 1); }
+
+    // the lane's part of the fragment of outer positions o .. o + 15; s: inner positions 32 s and on, or which half
+    static __device__ __forceinline__ typename P::Frag frag(const char* lds, int o, int s) {
+        const int i = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
+        if constexpr (LAY == kAlong) {
+            const int line = o + i;
+            return *reinterpret_cast<const typename P::Frag*>(lds + line * 128 + ((4 * s + h) ^ turn(line)) * 16);
+        } else {
+            typedef __attribute__((address_space(3))) s16x4* Lds;
+            union { s16x4 half[2]; typename P::Frag all; } f;
+            const int pair = P::N == 1 ? o / 16 : o / 32 * 4 + s * 2 + (o / 16 & 1);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int line = (P::N == 1 ? s * 32 : 0) + h * 8 + n * 4 + i / 4;
+                f.half[n] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + line * (LINE * 2) + (pair ^ twist(line)) * 32 + (i & 3) * 8));
+            }
+            return f.all;
+        }
+    }
+};
+
+// Operands of a product: lines of A go along or across the inner axis, lda numbers apart; Ma and Nb are the padded outer extents,
+// K the padded inner one.
+struct PlaneArgs {
+    const uint16_t *A, *B;
+    long lda, ldb;
+    long batch_a, batch_b;       // numbers from one batch to the next
+    int Ma, Nb, K;
+    int tiles_m, tiles_n;
+    const int* rows;             // where not null: so many of the outer positions of A (kBoundM), or of the inner ones (kBoundK), are there
+    int splits, per;             // parts of the sum, steps of one
+    float* part;                 // splits > 1: [batch][split][Ma][Nb]
+};
+enum { kBoundNone = 0, kBoundM = 1, kBoundK = 2 };
+
+// 16 bytes a lane from base + offset to LDS: byte `to` of it and on, lane by lane.  Written out because the compiler, which
+// knows the builtin of this instruction, waits for all of them before every transposing read; the waits are in the loop.
+// Nothing else in these kernels uses m0.
+__device__ __forceinline__ void line_to_lds(const char* base, unsigned offset, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+// the same for all lanes, for the compiler's knowledge
+__device__ __forceinline__ const char* same_for_all(const char* p) {
+    const uint64_t v = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (const char*)((uint64_t)hi << 32 | lo);
+}
+template <int N> __device__ __forceinline__ void wait_for_lines() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+// Tile of a block: blocks go to the 8 dies of the chip in turn; a die takes neighbouring tiles, four rows of tiles at a time,
+// so that what its blocks read at the same time is shared in its cache.
+__device__ __forceinline__ void plane_tile(int block, int tiles_m, int tiles_n, int* bm, int* bn) {
+    const int tiles = tiles_m * tiles_n, die = block & 7, k = block >> 3;
+    const int at = die * (tiles / 8) + min(die, tiles & 7) + k;
+    constexpr int GROUP = 4;
+    const int group = at / (GROUP * tiles_n), first = group * GROUP, size = min(GROUP, tiles_m - first);
+    const int in = at - group * GROUP * tiles_n;
+    *bm = first + in % size;
+    *bn = in / size;
+}
+// ... of a symmetric result: tiles with bm <= bn
+__device__ __forceinline__ void half_tile(int block, int tiles, int* bm, int* bn) {
+    int m = 0;
+    while (block >= tiles - m) {
+        block -= tiles - m;
+        ++m;
+    }
+    *bm = m;
+    *bn = m + block;
+}
+
+// BM x BN results to a block of WM x WN waves, STAGES steps in LDS, asked for STAGES - 1 steps ahead.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_> struct PlaneShape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
+    static constexpr int THREADS = 64 * WM * WN, MT = BM / 16 / WM, NT = BN / 16 / WN;
+    static constexpr int STAGE = (BM + BN) * 128, LDS = STAGES * STAGE;
+    static constexpr int A_PIECES = BM * 8 / THREADS, B_PIECES = BN * 8 / THREADS, LOADS = A_PIECES + B_PIECES;
+    static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0, "every thread asks for as many pieces");
+    static constexpr int PITCH = (NT * 16 + 4) * 4, MINE = 16 * PITCH;       // 16 rows of a wave on their way out
+    static_assert(MINE * WM * WN <= LDS, "all waves' rows");
+    static constexpr int OCCUPANCY = LDS > 80 * 1024 ? THREADS / 256 : 2 * THREADS / 256;
+};
+
+// E: the epilogue.  E::kSymmetric: only tiles on and above the diagonal.  epi.rows(...) gets a tile's fragments if E::kWhole,
+// otherwise epi.four(m, n, x, tile is below its mirror image, batch) four neighbouring results at a time, after their sums are whole.
+template <class P, class S, int ALAY, int BLAY, int BOUND, class E>
+__global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::OCCUPANCY, S::OCCUPANCY))) void plane_kernel(PlaneArgs g, E epi)
+{
+    typedef PlaneTile<P, ALAY, S::BM> TA;
+    typedef PlaneTile<P, BLAY, S::BN> TB;
+    constexpr int MT = S::MT, NT = S::NT, THREADS = S::THREADS, STEP = P::STEP;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / S::WN, wn = wave % S::WN;
+    int bm, bn;
+    if constexpr (E::kSymmetric) half_tile(blockIdx.x, g.tiles_m, &bm, &bn);
+    else plane_tile(blockIdx.x, g.tiles_m, g.tiles_n, &bm, &bn);
+    const int m0 = bm * S::BM, n0 = bn * S::BN, batch = blockIdx.z;
+    int steps = g.K / STEP;
+    if constexpr (BOUND == kBoundM) {
+        if (m0 >= *g.rows) return;
+    } else if constexpr (BOUND == kBoundK) {
+        steps = min(steps, (*g.rows + STEP - 1) / STEP);
+    }
+    const int t0 = blockIdx.y * g.per, t1 = min(t0 + g.per, steps);
+    const char* const A = (const char*)(g.A + batch * g.batch_a);
+    const char* const B = (const char*)(g.B + batch * g.batch_b);
+
+    const unsigned lds_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    // bytes from a step's first number to the thread's pieces; outer positions past the end are any: their results are not stored
+    unsigned aoff[S::A_PIECES], boff[S::B_PIECES];
+#pragma unroll
+    for (int i = 0; i < S::A_PIECES; ++i) {
+        int line, at;
+        TA::piece(tid + THREADS * i, &line, &at);
+        if constexpr (ALAY == kAlong) line = min(line, g.Ma - 1 - m0);
+        else at = min(at, (g.Ma - m0) * P::N - 8);
+        aoff[i] = (unsigned)((long)line * g.lda + at) * 2;
+    }
+#pragma unroll
+    for (int i = 0; i < S::B_PIECES; ++i) {
+        int line, at;
+        TB::piece(tid + THREADS * i, &line, &at);
+        if constexpr (BLAY == kAlong) line = min(line, g.Nb - 1 - n0);
+        else at = min(at, (g.Nb - n0) * P::N - 8);
+        boff[i] = (unsigned)((long)line * g.ldb + at) * 2;
+    }
+    auto fetch = [&](int t, int stage) {
+        const long k0 = (long)t * STEP;
+        const char* a = same_for_all(A + (ALAY == kAlong ? (long)m0 * g.lda + k0 * P::N : k0 * g.lda + (long)m0 * P::N) * 2);
+        const char* b = same_for_all(B + (BLAY == kAlong ? (long)n0 * g.ldb + k0 * P::N : k0 * g.ldb + (long)n0 * P::N) * 2);
+        const unsigned to = lds_at + stage * S::STAGE + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < S::A_PIECES; ++i) line_to_lds(a, aoff[i], to + i * THREADS * 16);
+#pragma unroll
+        for (int i = 0; i < S::B_PIECES; ++i) line_to_lds(b, boff[i], to + TA::BYTES + i * THREADS * 16);
+    };
+
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    constexpr int AHEAD = S::STAGES - 1;
+    static_assert(AHEAD >= 1 && AHEAD <= 3, "waits below");
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s)
+        if (t0 + s < t1) fetch(t0 + s, s);
+    int stage = 0, filled = AHEAD;
+    for (int t = t0; t < t1; ++t) {
+        const int left = t1 - 1 - t;
+        // the steps after this one may still be on their way
+        if (AHEAD == 3 && left >= 2) wait_for_lines<2 * S::LOADS>();
+        else if (AHEAD >= 2 && left >= 1) wait_for_lines<S::LOADS>();
+        else wait_for_lines<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (left >= AHEAD) {
+            fetch(t + AHEAD, filled);
+            filled = filled + 1 == S::STAGES ? 0 : filled + 1;
+        }
+        const char* buf = lds + stage * S::STAGE;
+        stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+        auto afrag = [&](int i, int s) { return TA::frag(buf, (wm * MT + i) * 16, s); };
+        auto bfrag = [&](int j, int s) { return TB::frag(buf + TA::BYTES, (wn * NT + j) * 16, s); };
+        typename P::Frag a[MT], b[NT];
+        // columns as the first operand: a lane's four results are neighbours in a row
+        auto all = [&](typename P::Frag (&x)[MT], typename P::Frag (&y)[NT]) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(y[j], x[i], acc[i][j]);
+        };
+        if constexpr (P::N == 1) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) b[j] = bfrag(j, s);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) a[i] = afrag(i, s);
+                __builtin_amdgcn_sched_barrier(0);           // all reads are on their way before the first product
+                all(a, b);
+            }
+        } else {
+            typename P::Frag c[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[j] = bfrag(j, 0);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[i] = afrag(i, 0);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) c[j] = bfrag(j, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            all(a, b);
+            all(a, c);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const typename P::Frag second = afrag(i, 1);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(b[j], second, acc[i][j]);
+            }
+        }
+    }
+    const int mw = m0 + wm * MT * 16, nw = n0 + wn * NT * 16, lane = tid & 63, i16 = lane & 15, h = lane >> 4;
+    if constexpr (E::kWhole) {
+        epi.template tile<MT, NT>(acc, mw, nw, bn * S::WN + wn);
+    } else {
+        if (g.splits > 1) {
+            float* __restrict__ part = g.part + (long)(batch * g.splits + blockIdx.y) * g.Ma * g.Nb;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const int m = mw + i * 16 + i16, n = nw + j * 16 + 4 * h;
+                    if (m < g.Ma && n < g.Nb) *reinterpret_cast<f32x4*>(part + (long)m * g.Nb + n) = acc[i][j];
+                }
+            return;
+        }
+        __syncthreads();                                     // LDS is free
+        // Results leave by way of LDS, 16 rows of the wave at a time, so that a store is whole lines
+        constexpr int LANES = NT * 4, ROWS = 64 / LANES;
+        char* const mine = lds + wave * S::MINE;
+        const int row0 = lane / LANES, col = lane % LANES * 4, n = nw + col;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4*>(mine + i16 * S::PITCH + (j * 16 + h * 4) * 4) = acc[i][j];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");           // LDS serves a wave in order
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int p = 0; p < 16 / ROWS; ++p) {
+                const int row = p * ROWS + row0, m = mw + i * 16 + row;
+                float x[4];
+                load_floats<4>(reinterpret_cast<const float*>(mine + row * S::PITCH) + col, x);
+                if (m < g.Ma && n < g.Nb) epi.four(m, n, x, E::kSymmetric && bm != bn, batch);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
+// Sums the parts of a product, four neighbouring results to a thread, in one order.
+template <int BM, int BN, class E> __global__ __launch_bounds__(256) void plane_join_kernel(PlaneArgs g, E epi)
+{
+    const long fours = g.Nb / 4, total = (long)g.Ma * fours, plane = (long)g.Ma * g.Nb;
+    const int batch = blockIdx.z;
+    for (long at = (long)blockIdx.x * 256 + threadIdx.x; at < total; at += (long)gridDim.x * 256) {
+        const int m = (int)(at / fours), n = (int)(at % fours) * 4;
+        if (E::kSymmetric && m / BM > n / BN) continue;
+        const float* __restrict__ p = g.part + (long)batch * g.splits * plane + (long)m * g.Nb + n;
+        f32x4 s[4] = {};
+        int k = 0;
+        for (; k + 4 <= g.splits; k += 4)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[u] += *reinterpret_cast<const f32x4*>(p + (k + u) * plane);
+        for (; k < g.splits; ++k) s[0] += *reinterpret_cast<const f32x4*>(p + k * plane);
+        const f32x4 t = (s[0] + s[1]) + (s[2] + s[3]);
+        float x[4] = {t[0], t[1], t[2], t[3]};
+        epi.four(m, n, x, E::kSymmetric && m / BM != n / BN, batch);
+    }
+}
+
+}  // namespace daspmm

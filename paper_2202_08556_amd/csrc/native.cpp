@@ -636,6 +636,7 @@ PyMODINIT_FUNC PyInit__native(void) {
         auto mod = py::reinterpret_borrow<py::module_>(m);
         bind_graphs(mod);
         bind_layers(mod);
+        bind_training(mod);
     } catch (const std::exception& e) {
         Py_DECREF(m);
         PyErr_SetString(PyExc_ImportError, e.what());

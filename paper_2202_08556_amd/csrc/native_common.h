@@ -99,5 +99,6 @@ inline bool ordinary(py::handle x) { return THPVariable_CheckExact(x.ptr()) && o
 inline bool wants_grad(const Tensor& t) { return t.defined() && t.requires_grad(); }
 
 void bind_layers(py::module_& mod);
+void bind_training(py::module_& mod);
 
 }  // namespace da_native

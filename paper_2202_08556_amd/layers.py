@@ -1,9 +1,10 @@
-"""Layers that stand between the aggregations of a model of node features: group norm with an activation, a gated
-feed-forward block and the loss of a distillation from a teacher's best classes, each forward and backward in
-hand-written kernels (include/da_layers.h).
+"""Layers that stand between the aggregations of a model of node features: group norm with an activation, root-mean-square
+norm with the residual's addition, a gated feed-forward block, the loss of a distillation from a teacher's best classes and
+the cross entropy of a linear layer, each forward and backward in hand-written kernels (include/da_layers.h,
+include/da_training.h).
 
-float32 and bfloat16.  Each is one operation forward and one backward, in C++ (csrc/native_layers.cpp); this module
-only checks and marshals arguments, and there is no fallback when the HIP library is missing (importing ``binding``
+float32 and bfloat16.  Each is one operation forward and one backward, in C++ (csrc/native_layers.cpp, csrc/native_training.cpp); this
+module only checks and marshals arguments, and there is no fallback when the HIP library is missing (importing ``binding``
 raises).  Work is enqueued on the current stream of the operands' device; the calls can be captured in a HIP graph.
 Gradients cannot be differentiated again (asking for that raises).
 """
@@ -74,6 +75,75 @@ class GroupNorm(torch.nn.Module):
 
     def forward(self, x: torch.Tensor, offsets: torch.Tensor | None = None) -> torch.Tensor:
         return group_norm(x, self.groups, self.weight, self.bias, self.eps, self.activation, offsets)
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        y, total = _native.rms_norm_forward(x, weight, residual, eps)
+        ctx.save_for_backward(x if total is None else total, weight)
+        ctx.eps = eps
+        ctx.set_materialize_grads(False)
+        return y, total
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dsum):
+        if dy is None and dsum is None:
+            return None, None, None, None
+        s, weight = ctx.saved_tensors
+        dx, dw = _native.rms_norm_backward(dy, dsum, s, weight, ctx.eps)
+        return dx, dw, dx if ctx.needs_input_grad[2] else None, None
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor | None = None, residual: torch.Tensor | None = None, eps: float = 1e-6):
+    """weight s / sqrt(mean(s^2) + eps) of the rows (the last axis) of s = x + residual.
+
+    With a residual (of the shape and type of x) the result is (y, s): s is what the next residual is, rounded to the type of
+    x, and its gradient joins that of y.  Without one the result is y and s is x.  weight: C numbers, float32 or bfloat16 whatever
+    the type of x."""
+    eps = float(eps)
+    if _native.layers_take(x, weight, residual):
+        y, total = _native.rms_norm(x, weight, residual, eps)
+    else:
+        y, total = _RmsNorm.apply(x, weight, residual, eps)
+    return y if residual is None else (y, total)
+
+
+class RMSNorm(torch.nn.Module):
+    """rms_norm with its weight; forward takes the residual."""
+
+    def __init__(self, channels: int, eps: float = 1e-6, affine: bool = True):
+        super().__init__()
+        self.eps = eps
+        self.weight = torch.nn.Parameter(torch.ones(channels)) if affine else None
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        return rms_norm(x, self.weight, residual, self.eps)
+
+
+class _RmsNormE4m3(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        return _native.rms_norm_e4m3(x, weight, residual, eps)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("rms_norm_e4m3 has no gradient")
+
+
+def rms_norm_e4m3(x: torch.Tensor, weight: torch.Tensor | None = None, residual: torch.Tensor | None = None, eps: float = 1e-6):
+    """rms_norm for serving, its result in 8 bits: (q, scale), or (q, scale, s) with a residual.  y = q scale[..., None] with q in
+    torch.float8_e4m3fn and scale = max |y| / 448 of each row in float32 (0 for a row of zeros, whose q is 0).  Not
+    differentiable: call it without gradients."""
+    eps = float(eps)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, residual)):
+        raise ValueError("rms_norm_e4m3 has no gradient: call it under torch.no_grad()")
+    if _native.layers_take(x, weight, residual):
+        q, scale, total = _native.rms_norm_e4m3(x, weight, residual, eps)
+    else:
+        q, scale, total = _RmsNormE4m3.apply(x, weight, residual, eps)
+    return (q, scale) if residual is None else (q, scale, total)
 
 
 class _Gated(torch.autograd.Function):
@@ -153,3 +223,39 @@ def distill_loss(logits: torch.Tensor, top_index: torch.Tensor, top_logits: torc
     else:
         loss = _Distill.apply(logits, top_index, top_logits, temperature)
     return loss if reduction == "none" else loss.sum() if reduction == "sum" else loss.mean()
+
+
+REDUCTIONS = {"none": da.DA_LOSS_ROWS, "sum": da.DA_LOSS_SUM, "mean": da.DA_LOSS_MEAN}
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, target, reduction):
+        loss, stats = _native.linear_cross_entropy_forward(x, weight, bias, target, reduction)
+        ctx.save_for_backward(x, weight, bias, stats)
+        ctx.reduction = reduction
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        x, weight, bias, stats = ctx.saved_tensors
+        return *_native.linear_cross_entropy_backward(dloss, x, weight, bias, stats, ctx.reduction), None, None
+
+
+def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, bias: torch.Tensor | None = None,
+                         reduction: str = "mean") -> torch.Tensor:
+    """Cross entropy of the logits x . weight + bias against a target class a row; the logits are never in memory.
+
+    x (..., d), weight (d, classes), both float32 or both bfloat16; bias: a number a class, float32 or bfloat16.  target
+    (...), int32 or int64: a row whose target is outside 0 .. classes - 1 (-1 or -100, say) has none; it adds nothing to the loss
+    and gets no gradient, whatever its x holds.  The loss is float32; reduction "none" gives one a row (0 without a target),
+    "sum" their sum, "mean" that over the number of rows with a target (0 where there is none).  A weight whose rows are not
+    dense (a transposed one, say) is copied at every call."""
+    try:
+        kind = REDUCTIONS[reduction]
+    except (KeyError, TypeError):
+        raise ValueError(f"reduction must be 'none', 'sum' or 'mean', not {reduction!r}") from None
+    if _native.layers_take(x, weight, target, bias):
+        return _native.linear_cross_entropy(x, weight, bias, target, kind)
+    return _LinearCrossEntropy.apply(x, weight, bias, target, kind)
