@@ -122,10 +122,16 @@ __global__ __launch_bounds__(256) void ce_index_kernel(const void* __restrict__ 
     if (r1 == rows && tid == 0) *st.count = before;
 }
 
+// The largest of a block's; the order of the blocks does not show
 __device__ __forceinline__ void keep_largest(float most, uint32_t* to) {
+    __shared__ float red[4];
     for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
-    // the order of these does not show
-    if ((threadIdx.x & 63) == 0 && most > 0.f) atomicMax(to, __float_as_uint(most));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        most = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        if (most > 0.f) atomicMax(to, __float_as_uint(most));
+    }
 }
 __device__ __forceinline__ float magnitude(float x) {
     const float a = fabsf(x);
@@ -439,15 +445,23 @@ template <class P>
 __global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restrict__ part, int parts, int Nb, int classes,
                                                            const uint32_t* __restrict__ maxes, void* db, int type, int first)
 {
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= classes) return;
+    __shared__ float red[16][17];
+    const int n = blockIdx.x * 16 + (threadIdx.x & 15), k0 = threadIdx.x >> 4;
     float s[4] = {};
-    int k = 0;
-    for (; k + 4 <= parts; k += 4)
+    if (n < classes) {
+        int k = k0;
+        for (; k + 48 < parts; k += 64)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) s[u] += part[(long)(k + u) * Nb + n];
-    for (; k < parts; ++k) s[0] += part[(long)k * Nb + n];
-    store_param(db, type, first + n, ((s[0] + s[1]) + (s[2] + s[3])) * scale_at<P>(maxes, kMaxG).inv);
+            for (int u = 0; u < 4; ++u) s[u] += part[(long)(k + u * 16) * Nb + n];
+        for (; k < parts; k += 16) s[0] += part[(long)k * Nb + n];
+    }
+    red[k0][threadIdx.x & 15] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    if (threadIdx.x < 16 && n < classes) {
+        float t = 0.f;
+        for (int i = 0; i < 16; ++i) t += red[i][threadIdx.x];
+        store_param(db, type, first + n, t * scale_at<P>(maxes, kMaxG).inv);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -481,8 +495,8 @@ struct PiecePlan {
 };
 PiecePlan piece_plan(const CePlan& p, int64_t width, int step) {
     const int64_t Vb = padded(width);
-    return {plane_plan(p.Ma, Vb, p.D / step, 1, false, false), plane_plan(p.Ma, p.D, Vb / step, 1, false, true),
-            plane_plan(p.D, Vb, p.Ma / step, 1, false, true)};
+    return {plane_plan(p.Ma, Vb, p.D / step, 1, false, false, step == Halves::STEP), plane_plan(p.Ma, p.D, Vb / step, 1, false, true, step == Halves::STEP),
+            plane_plan(p.D, Vb, p.Ma / step, 1, false, true, step == Halves::STEP)};
 }
 
 CePlan ce_plan(int dtype, const CeShape& s) {
@@ -493,7 +507,7 @@ CePlan ce_plan(int dtype, const CeShape& s) {
     p.Vb = padded(s.V);
     p.chunk = std::max<int64_t>(2048, ceil_div(ceil_div(s.rows, kChunks), 256) * 256);
     p.chunks = std::max<int64_t>(1, ceil_div(s.rows, p.chunk));
-    p.logits = plane_plan(p.Ma, p.Vb, p.D / step, 1, false, false);
+    p.logits = plane_plan(p.Ma, p.Vb, p.D / step, 1, false, false, step == Halves::STEP);
     p.slots = p.logits.tiles_n * wave_columns(p.logits);
     size_t at = 16;                                          // the largest magnitudes
     auto take = [&](size_t bytes) {
@@ -558,7 +572,7 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, long* ldw) {
     const T* w = static_cast<const T*>(c.w);
     if constexpr (P::N == 2) {
         const int64_t most = std::max(ceil_div(c.s.rows, 4), ceil_div(c.s.d * c.s.V, 4096));
-        hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 2048)), 2), dim3(256), 0, c.stream, x,
+        hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 512)), 2), dim3(256), 0, c.stream, x,
                            (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V), maxes);
     }
     auto pack = [&](const T* from, long ld, long lines, int n, const int* index, int which, size_t to) {
@@ -633,7 +647,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
     uint32_t* maxes = reinterpret_cast<uint32_t*>(c.ws);
     float* g = reinterpret_cast<float*>(c.ws + c.p.g_at);
     hipLaunchKernelGGL(ce_zero_kernel, dim3(1), dim3(64), 0, c.stream, maxes, (int)kMaxes);
-    hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 1024))), dim3(256), 0,
+    hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 256))), dim3(256), 0,
                        c.stream, c.st, (long)c.s.rows, dloss, (long)stride, reduction, g, maxes);
     if (dx && c.s.d > 0 && c.s.rows > 0)
         hipLaunchKernelGGL((ce_rest_kernel<T>), dim3((unsigned)std::min<int64_t>(ceil_div(c.s.rows, 4), 4096)), dim3(256), 0, c.stream, c.st,
@@ -693,7 +707,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             const int64_t per = ceil_div(c.s.rows, c.p.bias_parts);
             hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, ldz,
                                (int)Vb, (long)per, bias);
-            hipLaunchKernelGGL((ce_bias_join_kernel<P>), dim3((unsigned)ceil_div(width, 256)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
+            hipLaunchKernelGGL((ce_bias_join_kernel<P>), dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
                                (int)width, maxes, db, c.param_dtype, (int)first);
         }
     }

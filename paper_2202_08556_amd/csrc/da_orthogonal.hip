@@ -17,7 +17,7 @@
 namespace daspmm {
 namespace {
 
-constexpr int kNormParts = 64;               // of the norm's sum to a matrix
+constexpr int kNormParts = 512;              // of the norm's sum to a matrix
 constexpr int kOrthMost = 1 << 17;
 
 // Sums of squares in 64 bits: the squares of floats neither overflow nor vanish there
@@ -27,13 +27,16 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(const T* __restrict__ g,
 {
     __shared__ double red[4];
     const T* __restrict__ p = g + blockIdx.y * stride;
-    const long per = (rows + gridDim.x - 1) / gridDim.x, r0 = blockIdx.x * per, r1 = min(r0 + per, rows);
-    double s = 0.0;
-    // a wave goes down a row; waves take rows in turn, or all four share one that is long
+    // pieces of 1024 columns of a row, a wave's turn each, dealt to all waves of the matrix
+    const long across = (cols + 1023) / 1024, all = rows * across, step = (long)gridDim.x * 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (long r = r0 + wave; r < r1; r += 4) {
+    double s = 0.0;
+    for (long k = (long)blockIdx.x * 4 + wave; k < all; k += step) {
+        const long r = k / across, c0 = k % across * 1024;
         const T* __restrict__ row = p + r * ldg;
-        for (long c = lane * 4; c < cols; c += 256) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const long c = c0 + e * 256 + lane * 4;
             float x[4] = {0.f, 0.f, 0.f, 0.f};
             if (c + 4 <= cols) {
                 load_floats<4>(row + c, x);
@@ -246,12 +249,12 @@ OrthPlan orth_plan(int64_t batch, int64_t rows, int64_t cols) {
     p.n = std::max(rows, cols);
     p.Ma = padded(p.m);
     p.Nb = padded(p.n);
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(kNormParts, ceil_div(rows, 16)));
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(kNormParts, ceil_div(rows * cols, 8192)));
     p.parts_bytes = (size_t)batch * p.parts * sizeof(double);
     const int64_t step = Halves::STEP;
-    p.gram = plane_plan(p.Ma, p.Ma, p.Nb / step, batch, true, true);
-    p.poly = plane_plan(p.Ma, p.Ma, p.Ma / step, batch, true, true);
-    p.step = plane_plan(p.Ma, p.Nb, p.Ma / step, batch, false, true);
+    p.gram = plane_plan(p.Ma, p.Ma, p.Nb / step, batch, true, true, 1);
+    p.poly = plane_plan(p.Ma, p.Ma, p.Ma / step, batch, true, true, 1);
+    p.step = plane_plan(p.Ma, p.Nb, p.Ma / step, batch, false, true, 1);
     p.X = (size_t)batch * p.Ma * p.Nb * 4;
     p.A = (size_t)batch * p.Ma * p.Ma * 4;
     p.part = std::max({plane_part_bytes(p.gram, p.Ma, p.Ma, batch), plane_part_bytes(p.poly, p.Ma, p.Ma, batch),

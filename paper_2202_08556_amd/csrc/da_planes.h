@@ -339,24 +339,27 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
     }
 }
 
-// Sums the parts of a product, four neighbouring results to a thread, in one order.
-template <int BM, int BN, class E> __global__ __launch_bounds__(256) void plane_join_kernel(PlaneArgs g, E epi)
+// Sums the parts of a product in one order, four neighbouring results to `lanes` lanes.
+template <int BM, int BN, class E> __global__ __launch_bounds__(256) void plane_join_kernel(PlaneArgs g, int lanes, E epi)
 {
     const long fours = g.Nb / 4, total = (long)g.Ma * fours, plane = (long)g.Ma * g.Nb;
-    const int batch = blockIdx.z;
-    for (long at = (long)blockIdx.x * 256 + threadIdx.x; at < total; at += (long)gridDim.x * 256) {
+    const int batch = blockIdx.z, lane = threadIdx.x & (lanes - 1);
+    for (long at = ((long)blockIdx.x * 256 + threadIdx.x) / lanes; at < total; at += (long)gridDim.x * 256 / lanes) {
         const int m = (int)(at / fours), n = (int)(at % fours) * 4;
         if (E::kSymmetric && m / BM > n / BN) continue;
         const float* __restrict__ p = g.part + (long)batch * g.splits * plane + (long)m * g.Nb + n;
         f32x4 s[4] = {};
-        int k = 0;
-        for (; k + 4 <= g.splits; k += 4)
+        int k = lane;
+        for (; k + 3 * lanes < g.splits; k += 4 * lanes)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) s[u] += *reinterpret_cast<const f32x4*>(p + (k + u) * plane);
-        for (; k < g.splits; ++k) s[0] += *reinterpret_cast<const f32x4*>(p + k * plane);
-        const f32x4 t = (s[0] + s[1]) + (s[2] + s[3]);
+            for (int u = 0; u < 4; ++u) s[u] += *reinterpret_cast<const f32x4*>(p + (long)(k + u * lanes) * plane);
+        for (; k < g.splits; k += lanes) s[0] += *reinterpret_cast<const f32x4*>(p + (long)k * plane);
+        f32x4 t = (s[0] + s[1]) + (s[2] + s[3]);
+        for (int d = 1; d < lanes; d <<= 1)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) t[q] += __shfl_xor(t[q], d, 64);
         float x[4] = {t[0], t[1], t[2], t[3]};
-        epi.four(m, n, x, E::kSymmetric && m / BM != n / BN, batch);
+        if (lane == 0) epi.four(m, n, x, E::kSymmetric && m / BM != n / BN, batch);
     }
 }
 

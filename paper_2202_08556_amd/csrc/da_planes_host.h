@@ -20,27 +20,43 @@ struct PlanePlan {
     int splits, per;
 };
 
-// The largest tiles of which there is one for every unit; fewer than two of the smallest to a unit: the inner axis is cut, in
-// parts of at least eight steps.
-inline PlanePlan plane_plan(int64_t Ma, int64_t Nb, int64_t steps, int64_t batches, bool symmetric, bool may_split) {
-    PlanePlan p{};
+// What tiles of a size cost, in us, as measured: a step of a block that has its unit for itself and of one that shares it (two to
+// a unit), and what a block needs beside its steps.
+struct PlaneCost {
+    int64_t side;
+    double alone, shared, more;
+};
+constexpr PlaneCost kPlaneCost[2][3] = {{{256, 1.65, 1.65, 8.0}, {128, 0.55, 0.9, 5.0}, {64, 0.15, 0.25, 3.0}},          // One
+                                        {{256, 2.4, 2.4, 8.0}, {128, 0.8, 1.3, 5.0}, {64, 0.17, 0.35, 3.0}}};          // Halves
+
+// The tile, and the number of parts of the inner axis, whose turns on the chip take the least time: large tiles read least for what
+// they compute, small ones and parts keep all units busy, and parts pass through memory once more (4 TB/s and a launch).
+inline PlanePlan plane_plan(int64_t Ma, int64_t Nb, int64_t steps, int64_t batches, bool symmetric, bool may_split, int halves) {
+    PlanePlan best{};
     const int64_t cus = compute_units();
-    auto set = [&](int shape, int64_t bm, int64_t bn) {
+    double least = 0.0;
+    for (int shape = 0; shape < 3; ++shape) {
+        const PlaneCost& c = kPlaneCost[halves][shape];
+        PlanePlan p{};
         p.shape = shape;
-        p.tiles_m = (int)ceil_div(Ma, bm);
-        p.tiles_n = (int)ceil_div(Nb, bn);
+        p.tiles_m = (int)ceil_div(Ma, c.side);
+        p.tiles_n = (int)ceil_div(Nb, c.side);
         p.tiles = symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
-        return p.tiles * batches >= cus;
-    };
-    if (!set(0, 256, 256) && !set(1, 128, 128)) set(2, 64, 64);
-    p.splits = 1;
-    p.per = (int)std::max<int64_t>(steps, 1);
-    if (may_split && p.tiles * batches < cus) {
-        const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(2 * cus / std::max<int64_t>(1, p.tiles * batches), steps / 8));
-        p.per = (int)std::max<int64_t>(1, ceil_div(steps, splits));
-        p.splits = (int)std::max<int64_t>(1, ceil_div(steps, p.per));
+        const double parts = (double)batches * Ma * Nb * 8.0 / 4e6 * (symmetric ? 0.5 : 1.0);
+        for (int64_t splits = 1; splits <= 1024 && (splits == 1 || (may_split && steps / splits >= 4)); splits += std::max<int64_t>(1, splits / 2)) {
+            const int64_t per = std::max<int64_t>(1, ceil_div(steps, splits)), real = std::max<int64_t>(1, ceil_div(steps, per));
+            const int64_t blocks = p.tiles * batches * real, slots = shape == 0 ? cus : 2 * cus;
+            const double turn = (double)per * (blocks > cus ? c.shared : c.alone) + c.more;
+            const double time = (double)ceil_div(std::max<int64_t>(blocks, 1), slots) * turn + (real > 1 ? 4.0 + parts * (double)real : 0.0);
+            if ((shape == 0 && splits == 1) || time < least) {
+                least = time;
+                best = p;
+                best.splits = (int)real;
+                best.per = (int)per;
+            }
+        }
     }
-    return p;
+    return best;
 }
 inline size_t plane_part_bytes(const PlanePlan& p, int64_t Ma, int64_t Nb, int64_t batches) {
     return p.splits > 1 ? (size_t)batches * p.splits * Ma * Nb * sizeof(float) : 0;
@@ -59,8 +75,9 @@ void plane_launch(const PlaneArgs& g, const E& epi, const PlanePlan& p, int batc
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles, (unsigned)p.splits, (unsigned)batches), dim3(S::THREADS), S::LDS, s, g, epi);
     if constexpr (!E::kWhole) {
         if (p.splits > 1) {
-            const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.Ma * g.Nb / 4, 256), 8192);
-            hipLaunchKernelGGL((plane_join_kernel<S::BM, S::BN, E>), dim3((unsigned)blocks, 1, (unsigned)batches), dim3(256), 0, s, g, epi);
+            const int lanes = p.splits >= 64 ? 16 : p.splits >= 16 ? 4 : 1;
+            const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.Ma * g.Nb / 4 * lanes, 256), 8192);
+            hipLaunchKernelGGL((plane_join_kernel<S::BM, S::BN, E>), dim3((unsigned)blocks, 1, (unsigned)batches), dim3(256), 0, s, g, lanes, epi);
         }
     }
 }

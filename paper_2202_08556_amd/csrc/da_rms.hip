@@ -95,6 +95,12 @@ __device__ __forceinline__ void team_join(float (&x)[COUNT], int P, int waves, f
 }
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 
+// Squares of numbers this large or small are no floats any more: the row is taken times 2^-70 or 2^60 then (1 otherwise)
+__device__ __forceinline__ float other_scale(float sum, float inv, float eps) {
+    if (!(sum < 1e38f)) return 0x1p-70f;
+    return sum * inv + eps < 1e-24f && sum > 0.f || (sum == 0.f && eps < 1e-24f) ? 0x1p60f : 1.f;
+}
+
 // Rounded to the nearest number of e4m3, ties to even; |x| <= 448 but for a scale that lost digits below 2^-126
 __device__ __forceinline__ float in_e4m3(float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; }
 template <int V> __device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float (&x)[V]) {
@@ -124,7 +130,7 @@ __global__ __launch_bounds__(kRmsMost) void rms_kernel(RmsArgs<T> a, int P)
     __shared__ float lds[1][kRmsMost / 64];
     const int waves = P > 64 ? P / 64 : 1, lane = threadIdx.x & (P - 1), teams = blockDim.x / P;
     constexpr int N = E ? E : 1;
-    const float inv = 1.f / (float)a.C;
+    const float inv = a.C ? 1.f / (float)a.C : 0.f;
     float w[N][V];
     if constexpr (E > 0)
 #pragma unroll
@@ -146,10 +152,16 @@ __global__ __launch_bounds__(kRmsMost) void rms_kernel(RmsArgs<T> a, int P)
                     for (int i = 0; i < V; ++i) v[i] = (float)(bf16)v[i];
             }
         };
-        float v[N][V], ss[1] = {0.f};
+        float v[N][V], ss[1] = {0.f}, k = 1.f;
         auto count = [&](float (&p)[V]) {
 #pragma unroll
             for (int i = 0; i < V; ++i) ss[0] += p[i] * p[i];
+        };
+        // E == 0: the row again, as this thread wrote it where there is a residual
+        auto again = [&](int c, float (&p)[V]) {
+            load_some<V>((res ? (const T*)sum : x) + c, a.C - c, p);
+#pragma unroll
+            for (int i = 0; i < V; ++i) p[i] *= k;
         };
         if constexpr (E > 0) {
 #pragma unroll
@@ -167,28 +179,45 @@ __global__ __launch_bounds__(kRmsMost) void rms_kernel(RmsArgs<T> a, int P)
             }
         }
         team_join<1>(ss, P, waves, lds, add);
-        const float r = 1.f / sqrtf(ss[0] * inv + a.eps);
-        auto scaled = [&](int c, float (&p)[V], float (&u)[V]) {             // y
+        k = other_scale(ss[0], inv, a.eps);
+        if (k != 1.f) {
+            ss[0] = 0.f;
+            if constexpr (E > 0) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[e][i] *= k;
+                    count(v[e]);
+                }
+            } else {
+                for (int c = lane * V; c < a.C; c += P * V) {
+                    again(c, v[0]);
+                    count(v[0]);
+                }
+            }
+            team_join<1>(ss, P, waves, lds, add);
+        }
+        const float r = 1.f / sqrtf(ss[0] * inv + a.eps * k * k);
+        auto scaled = [&](float (&p)[V], float (&u)[V]) {                    // y
 #pragma unroll
             for (int i = 0; i < V; ++i) p[i] = p[i] * r * u[i];
         };
-        // E == 0: the row again, as this thread wrote it where there is a residual
-        auto again = [&](int c, float (&p)[V], float (&u)[V]) {
-            load_some<V>((res ? (const T*)sum : x) + c, a.C - c, p);
-            load_weights<V>(a.w, a.w_type, c, a.C - c, u);
-            scaled(c, p, u);
+        auto result = [&](int c) {                           // E == 0
+            again(c, v[0]);
+            load_weights<V>(a.w, a.w_type, c, a.C - c, w[0]);
+            scaled(v[0], w[0]);
         };
         if constexpr (!EIGHT) {
             T* __restrict__ y = a.y + row * a.C;
             if constexpr (E > 0) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    scaled(0, v[e], w[e]);
+                    scaled(v[e], w[e]);
                     store_some<V>(y + (lane + e * P) * V, a.C - (lane + e * P) * V, v[e]);
                 }
             } else {
                 for (int c = lane * V; c < a.C; c += P * V) {
-                    again(c, v[0], w[0]);
+                    result(c);
                     store_some<V>(y + c, a.C - c, v[0]);
                 }
             }
@@ -198,13 +227,13 @@ __global__ __launch_bounds__(kRmsMost) void rms_kernel(RmsArgs<T> a, int P)
             if constexpr (E > 0) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    scaled(0, v[e], w[e]);
+                    scaled(v[e], w[e]);
 #pragma unroll
                     for (int i = 0; i < V; ++i) most[0] = larger(most[0], fabsf(v[e][i]));
                 }
             } else {
                 for (int c = lane * V; c < a.C; c += P * V) {
-                    again(c, v[0], w[0]);
+                    result(c);
 #pragma unroll
                     for (int i = 0; i < V; ++i) most[0] = larger(most[0], fabsf(v[0][i]));
                 }
@@ -221,7 +250,7 @@ __global__ __launch_bounds__(kRmsMost) void rms_kernel(RmsArgs<T> a, int P)
                 }
             } else {
                 for (int c = lane * V; c < a.C; c += P * V) {
-                    again(c, v[0], w[0]);
+                    result(c);
 #pragma unroll
                     for (int i = 0; i < V; ++i) v[0][i] /= by;
                     store_e4m3<V>(q + c, a.C - c, v[0]);
@@ -239,7 +268,7 @@ __global__ __launch_bounds__(kRmsMost) void rms_grad_kernel(RmsArgs<T> a, int P)
     extern __shared__ float columns[];       // teams of less than a wave to a block: [threads][E V], their parts of dw
     const int waves = P > 64 ? P / 64 : 1, lane = threadIdx.x & (P - 1), teams = blockDim.x / P;
     constexpr int N = E ? E : 1;
-    const float inv = 1.f / (float)a.C;
+    const float inv = a.C ? 1.f / (float)a.C : 0.f;
     float w[N][V], dw[N][V];
     float* __restrict__ mine = a.part ? a.part + (long)blockIdx.x * a.C : nullptr;
     if constexpr (E > 0)
@@ -261,12 +290,25 @@ __global__ __launch_bounds__(kRmsMost) void rms_grad_kernel(RmsArgs<T> a, int P)
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[i] = 0.f;
         };
-        float v[N][V], g[N][V], d[N][V], sums[2] = {0.f, 0.f};
-        auto count = [&](const float (&p)[V], const float (&u)[V], const float (&k)[V]) {
+        float v[N][V], g[N][V], d[N][V], sums[2] = {0.f, 0.f}, k = 1.f;
+        auto count = [&](float (&p)[V], const float (&u)[V], const float (&f)[V]) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 sums[0] += p[i] * p[i];
-                sums[1] += p[i] * (u[i] * k[i]);
+                sums[1] += p[i] * (u[i] * f[i]);
+            }
+        };
+        auto scaled = [&](float (&p)[V]) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) p[i] *= k;
+        };
+        auto walk = [&] {                                    // E == 0
+            for (int c = lane * V; c < a.C; c += P * V) {
+                get(s, c, v[0]);
+                get(dy, c, g[0]);
+                load_weights<V>(a.w, a.w_type, c, a.C - c, w[0]);
+                scaled(v[0]);
+                count(v[0], g[0], w[0]);
             }
         };
         if constexpr (E > 0) {
@@ -279,20 +321,29 @@ __global__ __launch_bounds__(kRmsMost) void rms_grad_kernel(RmsArgs<T> a, int P)
 #pragma unroll
             for (int e = 0; e < E; ++e) count(v[e], g[e], w[e]);
         } else {
-            for (int c = lane * V; c < a.C; c += P * V) {
-                get(s, c, v[0]);
-                get(dy, c, g[0]);
-                load_weights<V>(a.w, a.w_type, c, a.C - c, w[0]);
-                count(v[0], g[0], w[0]);
-            }
+            walk();
         }
         team_join<2>(sums, P, waves, lds, add);
-        const float r = 1.f / sqrtf(sums[0] * inv + a.eps), m = sums[1] * r * inv;
-        auto finish = [&](int c, float (&p)[V], float (&u)[V], float (&k)[V], float (&plus)[V], float (&t)[V]) {
+        k = other_scale(sums[0], inv, a.eps);
+        if (k != 1.f) {
+            sums[0] = sums[1] = 0.f;
+            if constexpr (E > 0) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    scaled(v[e]);
+                    count(v[e], g[e], w[e]);
+                }
+            } else {
+                walk();
+            }
+            team_join<2>(sums, P, waves, lds, add);
+        }
+        const float r = 1.f / sqrtf(sums[0] * inv + a.eps * k * k), m = sums[1] * r * inv, rk = r * k;
+        auto finish = [&](int c, float (&p)[V], float (&u)[V], float (&f)[V], float (&plus)[V], float (&t)[V]) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float xh = p[i] * r;
-                p[i] = r * (u[i] * k[i] - xh * m) + plus[i];
+                p[i] = rk * (u[i] * f[i] - xh * m) + plus[i];
                 t[i] += u[i] * xh;
             }
             if (dx) store_some<V>(dx + c, a.C - c, p);
@@ -306,6 +357,7 @@ __global__ __launch_bounds__(kRmsMost) void rms_grad_kernel(RmsArgs<T> a, int P)
                 get(dy, c, g[0]);
                 get(more, c, d[0]);
                 load_weights<V>(a.w, a.w_type, c, a.C - c, w[0]);
+                scaled(v[0]);
                 if (first || !mine)
 #pragma unroll
                     for (int i = 0; i < V; ++i) dw[0][i] = 0.f;

@@ -1,0 +1,303 @@
+"""linear_cross_entropy against its formula in 64 bits, forward and backward.
+
+Tolerances, with e = 2^-24 and u half a step of a result's type.  A logit's sum over d products is off by A = (d / 16 + 16) e of
+the sum of their magnitudes.  float32 operands are pairs of halves: each is off by 2^-22 and the product of the second halves
+is left out, 2^-20 together, and numbers far below the largest of their array by 2^-39 of it.  With D the largest error of a
+row's logits, the loss is off by 2 D + (K + 4 |lse|) e, K = 64 + classes / 1024; a probability p by P = 2 D + (K + 4 |z - lse|) e of it;
+dz by |g| (p P + 4 e (p + [target])) and its rounding (bfloat16: 2^-8 of it; halves: 2^-22 and 2^-39 of the largest g).  dx, dw and db
+are off by what dz's errors add up to, A as above of their own sums, and u."""
+import pytest
+import torch
+
+from paper_2202_08556_amd import layers
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+U = {torch.float32: E, torch.bfloat16: 2.0 ** -8}
+
+
+def make(rows, d, V, dtype, bias=True, share=1.0, seed=0, device="cuda"):
+    g = torch.Generator(device="cuda").manual_seed(seed + rows + 3 * d + 7 * V)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")          # noqa: E731
+    x, w = r(rows, d).to(dtype), (2 * d ** -0.5 * r(d, V)).to(dtype)
+    b = (0.3 * r(V)).to(dtype) if bias else None
+    t = torch.randint(0, max(V, 1), (rows,), generator=g, device="cuda")
+    t = torch.where(torch.rand(rows, generator=g, device="cuda") < share, t, -1)
+    return x, w, b, t, torch.rand(rows, generator=g, device="cuda") + 0.1
+
+
+def formula(x, w, b, t, g, dtype, device):
+    """Results and their tolerances in 64 bits; g: factors of the rows."""
+    f = lambda a: a.detach().to(device).double()                         # noqa: E731
+    V, d = w.shape[1], w.shape[0]
+    has = (t >= 0) & (t < V)
+    keep = has.nonzero()[:, 0].to(device)
+    X, W, g, t = f(x)[keep], f(w), f(g)[keep], t.to(device)[keep]
+    halves = dtype == torch.float32
+    A = (d / 16 + 16) * E + (2.0 ** -20 if halves else 0)
+    z = torch.mm(X, W) + (f(b) if b is not None else 0)
+    dz_err = A * torch.mm(X.abs(), W.abs()) + 2 * E * z.abs().masked_fill(z.isinf(), 0)
+    if halves and X.numel() and W.numel():
+        dz_err += 2.0 ** -38 * d * X.abs().max() * W.abs().max()
+    D = dz_err.amax(1, keepdim=True)
+    K = 64 + V / 1024
+    lse = z.logsumexp(1, keepdim=True)
+    zt = z.gather(1, t[:, None])
+    loss, tol = (lse - zt)[:, 0], (2 * D + (K + 4 * lse.abs()) * E)[:, 0]
+    p = (z - lse).exp()
+    away = (z - lse).abs().masked_fill(z.isinf(), 0)
+    one = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
+    dz = g[:, None] * (p - one)
+    t_dz = g[:, None].abs() * (p * (2 * D + (K + 4 * away) * E) + 4 * E * (p + one)) + dz.abs() * (2.0 ** -22 if halves else 2.0 ** -8)
+    if halves and g.numel():
+        t_dz += 2.0 ** -39 * g.abs().max()
+    extra = 2.0 ** -20 if halves else 0.0
+    rows = x.shape[0]
+    dx, t_dx = torch.mm(dz, W.t()), torch.mm(t_dz, W.abs().t()) + ((V / 16 + 16) * E + extra) * torch.mm(dz.abs(), W.abs().t())
+    dw, t_dw = torch.mm(X.t(), dz), torch.mm(X.abs().t(), t_dz) + ((rows / 16 + 80) * E + extra) * torch.mm(X.abs().t(), dz.abs())
+    if halves and g.numel() and W.numel():
+        t_dx += 2.0 ** -38 * V * g.abs().max() * W.abs().max()
+        t_dw += 2.0 ** -38 * rows * g.abs().max() * X.abs().max()
+    db, t_db = dz.sum(0), t_dz.sum(0) + (rows / 16 + 80) * E * dz.abs().sum(0)
+    place = lambda v: torch.zeros(rows, *v.shape[1:], dtype=v.dtype, device=device).index_copy(0, keep, v)       # noqa: E731
+    return dict(loss=(place(loss), place(tol)), dx=(place(dx), place(t_dx)), dw=(dw, t_dw), db=(db, t_db))
+
+
+def near(got, want, tol, u, name):
+    got = got.detach().to(want.device).double()
+    assert got.shape == want.shape, name
+    off = (got - want).abs()
+    ok = off <= tol * (1 + u) + want.abs() * u + 2.0 ** -126
+    assert ok.all(), (name, float((off / (tol + want.abs() * u + 2.0 ** -126)).max()))
+
+
+def check(x, w, b, t, g, device="cpu", reduction="none"):
+    dt = x.dtype
+    leaves = [v.detach().requires_grad_(True) for v in (x, w, b) if v is not None]
+    B = leaves[2] if b is not None else None
+    loss = layers.linear_cross_entropy(leaves[0], leaves[1], t, bias=B, reduction=reduction)
+    rows, V = x.shape[0], w.shape[1]
+    count = max(1, int(((t >= 0) & (t < V)).sum()))
+    if reduction == "none":
+        assert loss.shape == t.shape
+        grads, factors = torch.autograd.grad(loss, leaves, g), g
+    else:
+        assert loss.shape == ()
+        grads = torch.autograd.grad(loss, leaves, g[0])
+        factors = g[0].double().expand(rows) / (count if reduction == "mean" else 1)
+    assert loss.dtype == torch.float32
+    torch.cuda.synchronize()
+    want = formula(x, w, b, t, factors, dt, device)
+    if reduction == "none":
+        near(loss, *want["loss"], E, "loss")
+        assert not loss.detach().cpu()[(t.cpu() < 0) | (t.cpu() >= V)].any()
+    else:
+        by = count if reduction == "mean" else 1
+        near(loss, want["loss"][0].sum() / by, want["loss"][1].sum() / by, 2 * E, "loss")
+    near(grads[0], *want["dx"], U[dt], "dx")
+    near(grads[1], *want["dw"], U[dt], "dw")
+    if b is not None:
+        near(grads[2], *want["db"], U[b.dtype], "db")
+    return loss, grads
+
+
+SIZES = [(1, 1, 1), (1, 16, 4), (3, 5, 2), (2, 64, 1), (61, 64, 41), (64, 64, 64), (65, 70, 129), (130, 33, 300), (257, 96, 1000), (300, 128, 257),
+         (1000, 24, 70), (5000, 16, 41), (40, 300, 5000), (1, 602, 9973), (700, 1, 33), (2100, 64, 2100), (16, 2000, 64), (4099, 40, 4100)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("rows,d,V", SIZES)
+def test_forward_and_backward(rows, d, V, dtype):
+    x, w, b, t, g = make(rows, d, V, dtype)
+    check(x, w, b, t, g)
+
+
+@pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("rows,d,V,share", [(61, 64, 41, 0.5), (3000, 20, 41, 0.1), (5000, 16, 300, 0.5), (200, 48, 900, 0.3), (50, 32, 41, 0.0),
+                                            (2049, 8, 10, 0.7)])
+def test_rows_without_a_target(rows, d, V, share, dtype, reduction):
+    x, w, b, t, g = make(rows, d, V, dtype, bias=V != 300, share=share)
+    t = torch.where((t < 0) & (torch.arange(rows, device="cuda") % 3 == 0), V + 5, t)      # beyond the classes: none either
+    if reduction == "mean":
+        t = t.to(torch.int32)
+    without = (t < 0) | (t >= V)
+    bad = x.clone()
+    bad[without] = float("nan")                              # what they hold does not matter
+    bad[without & (torch.arange(rows, device="cuda") % 2 == 0)] = float("inf")
+    loss, grads = check(x, w, b, t, g, reduction=reduction)
+    leaves = [v.detach().requires_grad_(True) for v in (bad, w, b) if v is not None]
+    again = layers.linear_cross_entropy(leaves[0], leaves[1], t, bias=leaves[2] if b is not None else None, reduction=reduction)
+    g2 = torch.autograd.grad(again, leaves, g if reduction == "none" else g[0])
+    assert torch.equal(again, loss) and all(torch.equal(p, q) for p, q in zip(g2, grads))
+    assert not grads[0][without].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_many_rows_and_pieces(dtype):
+    """More rows than one piece of the classes has room for: dx is summed over pieces."""
+    rows, V = (140000, 1100) if dtype == torch.float32 else (280000, 1100)
+    x, w, b, t, g = make(rows, 8, V, dtype)
+    check(x, w, b, t, g, device="cuda", reduction="mean")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_strides_types_and_axes(dtype):
+    x, w, b, t, g = make(60, 50, 45, dtype)
+    wide = torch.randn(60, 120, device="cuda").to(dtype)
+    check(wide[:, 5:55], w, b, t, g)                         # rows 120 apart at odd addresses
+    check(wide[:, 5:55], w.t().contiguous().t(), b, t, g)    # a transposed weight
+    check(x, w, b.float() if dtype == torch.bfloat16 else b.bfloat16(), t, g)
+    check(x, w, b, torch.stack([t, t], 1)[:, 0], g)          # targets that are not neighbours
+    leaf = x.view(3, 20, 50).detach().requires_grad_(True)
+    loss = layers.linear_cross_entropy(leaf, w, t.view(3, 20), bias=b, reduction="none")
+    assert loss.shape == (3, 20) and torch.equal(loss.flatten(), layers.linear_cross_entropy(x, w, t, bias=b, reduction="none"))
+    one, = torch.autograd.grad(loss.sum(), leaf)             # one number for all rows
+    leaf2 = x.detach().requires_grad_(True)
+    two, = torch.autograd.grad(layers.linear_cross_entropy(leaf2, w, t, bias=b, reduction="none"), leaf2, torch.ones(60, device="cuda"))
+    assert torch.equal(one.view(60, 50), two)
+    single = layers.linear_cross_entropy(x[3], w, t[3], bias=b, reduction="none")
+    assert single.shape == ()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_masked_classes(dtype):
+    """A bias of -inf, or of the type's lowest value, takes a class out; one that leaves only the target gives loss 0."""
+    x, w, b, t, g = make(70, 24, 90, dtype)
+    t = t % 40
+    for low in (float("-inf"), torch.finfo(dtype).min):
+        masked = b.clone()
+        masked[40:] = low
+        leaf = [v.detach().requires_grad_(True) for v in (x, w, masked)]
+        loss = layers.linear_cross_entropy(leaf[0], leaf[1], t, bias=leaf[2], reduction="none")
+        grads = torch.autograd.grad(loss, leaf, g)
+        few = [v.detach().requires_grad_(True) for v in (x, w[:, :40].contiguous(), b[:40])]
+        want = layers.linear_cross_entropy(few[0], few[1], t, bias=few[2], reduction="none")
+        ref = torch.autograd.grad(want, few, g)
+        # the same numbers but for the order of sums and, in float32, the scale of w: 2^-19 of the loss's terms
+        assert torch.allclose(loss, want, rtol=2.0 ** -18, atol=2.0 ** -18)
+        assert torch.allclose(grads[0].float(), ref[0].float(), rtol=2.0 ** -6, atol=2.0 ** -12)
+        assert not grads[1][:, 40:].any() and not grads[2][40:].any()
+        assert torch.allclose(grads[1][:, :40].float(), ref[1].float(), rtol=2.0 ** -6, atol=2.0 ** -8)
+    masked = torch.full_like(b, float("-inf"))
+    masked[7] = 0
+    assert torch.equal(layers.linear_cross_entropy(x, w, torch.full_like(t, 7), bias=masked, reduction="none"), torch.zeros(70, device="cuda"))
+    assert (layers.linear_cross_entropy(x, w, torch.full_like(t, 8), bias=masked, reduction="none") == float("inf")).all()
+
+
+def test_bad_rows_stay_by_themselves():
+    x, w, b, t, g = make(100, 32, 60, torch.float32)
+    want = layers.linear_cross_entropy(x, w, t, bias=b, reduction="none")
+    x[13, 3], x[40, 0] = float("nan"), float("inf")
+    got = layers.linear_cross_entropy(x, w, t, bias=b, reduction="none")
+    rest = torch.ones(100, dtype=torch.bool, device="cuda")
+    rest[13] = rest[40] = False
+    assert torch.equal(got[rest], want[rest]) and not torch.isfinite(got[~rest]).any()
+
+
+def test_wide_ranges():
+    """Rows and classes of very different size in float32: halves keep 2^-39 of the largest."""
+    x, w, b, t, g = make(64, 32, 48, torch.float32)
+    x *= torch.logspace(-6, 1, 64, device="cuda")[:, None]
+    w *= torch.logspace(-4, 0, 48, device="cuda")
+    check(x, w, b, t, g * torch.logspace(-5, 0, 64, device="cuda"))
+    check(x * 1e-20, w * 1e20, b, t, g)
+    check(x * 0, w, b, t, g)
+
+
+def test_differences():
+    """The gradient along a direction is what the loss changes by: central differences in steps of 2^-6 are off by the third
+    derivative's 2^-13 and 2^-15 of the losses (float32)."""
+    x, w, b, t, g = make(20, 24, 30, torch.float32, share=0.8)
+    f = lambda *a: (layers.linear_cross_entropy(a[0], a[1], t, bias=a[2], reduction="none") * g).double().sum()       # noqa: E731
+    leaves = [v.clone().requires_grad_(True) for v in (x, w, b)]
+    grads = torch.autograd.grad(f(*leaves), leaves)
+    for i, v in enumerate((x, w, b)):
+        dirn = torch.randn_like(v) / v.numel() ** 0.5
+        h = 2.0 ** -6
+        p, m = ([a + s * h * dirn if k == i else a for k, a in enumerate((x, w, b))] for s in (1, -1))
+        slope = float((f(*p) - f(*m)) / (2 * h))
+        assert abs(slope - float((grads[i] * dirn).double().sum())) <= float(g.sum()) * 2.0 ** -9
+
+
+def test_only_what_is_asked_for():
+    x, w, b, t, g = make(64, 32, 41, torch.float32)
+    for need in ((True, False, False), (False, True, False), (False, False, True)):
+        leaves = [v.clone().requires_grad_(n) for v, n in zip((x, w, b), need)]
+        layers.linear_cross_entropy(leaves[0], leaves[1], t, bias=leaves[2]).backward()
+        assert [v.grad is not None for v in leaves] == list(need)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_graph_with_other_targets(dtype):
+    """A captured step, replayed on other inputs and other numbers of labelled rows."""
+    x, w, b, t, g = make(3000, 64, 300, dtype, share=0.5)
+    X, W, B = (v.clone().requires_grad_(True) for v in (x, w, b))
+
+    def step():
+        loss = layers.linear_cross_entropy(X, W, t, bias=B)
+        return (loss, *torch.autograd.grad(loss, (X, W, B)))
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for share in (1.0, 0.2, 0.0, 0.6):
+        x, _, _, t2, _ = make(3000, 64, 300, dtype, share=share, seed=int(10 * share) + 1)
+        with torch.no_grad():
+            X.copy_(x)
+        t.copy_(t2)
+        graph.replay()
+        torch.cuda.synchronize()
+        mine = [v.clone() for v in got]
+        assert all(torch.equal(p, q) for p, q in zip(mine, step())), share
+
+
+def test_runs_are_alike():
+    x, w, b, t, g = make(3000, 40, 700, torch.float32, share=0.7)
+    first = check(x, w, b, t, g, device="cuda")
+    again = check(x, w, b, t, g, device="cuda")
+    assert torch.equal(first[0], again[0]) and all(torch.equal(p, q) for p, q in zip(first[1], again[1]))
+
+
+def test_empty():
+    for rows, d, V in ((0, 8, 5), (4, 0, 5), (4, 8, 0), (0, 0, 0)):
+        x, w = torch.zeros(rows, d, device="cuda", requires_grad=True), torch.zeros(d, V, device="cuda", requires_grad=True)
+        b = torch.zeros(V, device="cuda", requires_grad=True)
+        t = torch.zeros(rows, dtype=torch.long, device="cuda")
+        for reduction in ("none", "mean", "sum"):
+            loss = layers.linear_cross_entropy(x, w, t, bias=b, reduction=reduction)
+            dx, dw, db = torch.autograd.grad(loss.sum(), (x, w, b))
+            want = 5 ** 0.5 * 0 + torch.log(torch.tensor(5.0)) if (rows, d, V) == (4, 0, 5) else torch.tensor(0.0)
+            if reduction == "mean":
+                assert torch.allclose(loss.cpu(), want)
+            assert not dx.any() and not dw.any() and (db.any() == ((rows, V) == (4, 5)))
+
+
+def test_refusals():
+    x, w, b, t, g = make(8, 16, 5, torch.float32)
+    L = layers.linear_cross_entropy
+    for bad in ((x, w.t(), t), (x, w, t[:4]), (x[:, :8], w, t), (x.cpu(), w, t), (x, w.cpu(), t), (x, w, t.cpu()), (x, w[0], t)):
+        with pytest.raises(ValueError):
+            L(*bad)
+    for bad in ((x.half(), w.half(), t), (x.bfloat16(), w, t), (x, w, t.float()), (x, w, t.to(torch.int16))):
+        with pytest.raises(TypeError):
+            L(*bad)
+    with pytest.raises(ValueError):
+        L(x, w, t, bias=b[:2])
+    with pytest.raises(ValueError):
+        L(x, w, t, reduction="max")
+    x.requires_grad_(True)
+    dx, = torch.autograd.grad(L(x, w, t), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(dx.sum(), x)
+    w2 = w.clone().requires_grad_(True)
+    loss = L(x, w2, t)
+    with torch.no_grad():
+        w2.mul_(2.0)
+    with pytest.raises(RuntimeError):
+        loss.backward()
