@@ -9,6 +9,7 @@
 // which only the device knows: rows without one cost nothing and may hold anything.
 #include "da_training.h"
 
+#include "da_ce_narrow.h"
 #include "da_planes_host.h"
 #include "da_spmm.h"
 
@@ -216,10 +217,46 @@ template <class P> struct Logits {
     int bias_type;
     int classes;
     CeStats st;
-    // the scales leave one after the other: their product may not be a float
-    __device__ __forceinline__ float logit(float x, int n, const Scale& sx, const Scale& sw) const {
-        if constexpr (P::N == 2) x = x * sx.inv * sw.inv;
-        return bias ? x + load_param(bias, bias_type, n) : x;
+    // A wave's logits from its sums: columns nw + 16 j + 4 h and on of row i16 of each 16 (the scales leave one after the other: their
+    // product may not be a float); -inf behind the last class
+    template <int NT> struct Columns {
+        Scale sx, sw;
+        float bias[NT][4];
+        bool inside;
+    };
+    template <int NT> __device__ __forceinline__ Columns<NT> columns(int nw) const {
+        Columns<NT> c;
+        c.sx = scale_at<P>(maxes, kMaxX);
+        c.sw = scale_at<P>(maxes, kMaxW);
+        c.inside = nw + NT * 16 <= classes;
+        const int n = nw + 4 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) c.bias[j][q] = bias && n + j * 16 + q < classes ? load_param(bias, bias_type, n + j * 16 + q) : 0.f;
+        return c;
+    }
+    template <int NT> __device__ __forceinline__ void logits(const f32x4 (&acc)[NT], const Columns<NT>& c, int nw, float (&z)[NT][4]) const {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                z[j][q] = acc[j][q];
+                if constexpr (P::N == 2) z[j][q] = z[j][q] * c.sx.inv * c.sw.inv;
+            }
+        if (bias)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) z[j][q] += c.bias[j][q];
+        if (!c.inside) {
+            const int n = nw + 4 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (n + j * 16 + q >= classes) z[j][q] = -INFINITY;
+        }
     }
 };
 
@@ -229,23 +266,28 @@ template <class P> struct SumsOut : Logits<P> {
     float2* part;                // [row][slot]
     int slots;
     float* at_target;            // [row]
-    template <int MT, int NT> __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int slot) const {
+    template <int MT, int NT>
+    __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int slot, char*, int, int) const {
         const int i16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4, count = *this->st.count;
-        const Scale sx = scale_at<P>(this->maxes, kMaxX), sw = scale_at<P>(this->maxes, kMaxW);
+        const auto c = this->template columns<NT>(nw);
+        int t[MT];                                           // of the row, from the lane's first column on
+#pragma unroll
+        for (int i = 0; i < MT; ++i) t[i] = (mw + i * 16 + i16 < count ? this->st.target[mw + i * 16 + i16] : -0x40000000) - nw - 4 * h;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int m = mw + i * 16 + i16;
-            const int t = m < count ? this->st.target[m] : -1;
             float z[NT][4], most = -INFINITY;
+            this->logits(acc[i], c, nw, z);
+            if (__any(t[i] >= 0 && t[i] < NT * 16))
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (t[i] == j * 16 + q) at_target[m] = z[j][q];
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = nw + j * 16 + 4 * h + q;
-                    z[j][q] = n < this->classes ? this->logit(acc[i][j][q], n, sx, sw) : -INFINITY;
-                    most = fmaxf(most, z[j][q]);
-                    if (n == t) at_target[m] = z[j][q];
-                }
+                for (int q = 0; q < 4; ++q) most = fmaxf(most, z[j][q]);
             most = fmaxf(most, __shfl_xor(most, 16, 64));
             most = fmaxf(most, __shfl_xor(most, 32, 64));
             const float from = most == -INFINITY ? 0.f : most;
@@ -263,32 +305,60 @@ template <class P> struct SumsOut : Logits<P> {
 
 // dz of a piece of the classes that begins at `first`; rows behind the last one are 0
 template <class P> struct GradOut : Logits<P> {
-    static constexpr bool kSymmetric = false, kWhole = false;
+    static constexpr bool kSymmetric = false, kWhole = true;
     const float* g;
     int first;
     uint16_t* dz;
     long ldz;
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool, int) const {
-        const int count = *this->st.count;
-        if (m < count) {
-            const Scale sx = scale_at<P>(this->maxes, kMaxX), sw = scale_at<P>(this->maxes, kMaxW);
-            const float lse = this->st.lse[m];
-            const int t = this->st.target[m] - first;
-            const float by = g[m] * scale_at<P>(this->maxes, kMaxG).by;
+    // 16 rows at a time: a lane makes its numbers of one row, packed as they are in memory, and they leave by way of LDS in whole lines
+    template <int MT, int NT>
+    __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int, char* lds, int Ma, int Nb) const {
+        constexpr int BYTES = NT * 32 * P::N, PITCH = BYTES + 16, CHUNKS = BYTES / 16;
+        const int lane = threadIdx.x & 63, i16 = lane & 15, h = lane >> 4, count = *this->st.count, n0 = first + nw;
+        const auto c = this->template columns<NT>(n0);
+        const float up = scale_at<P>(this->maxes, kMaxG).by;
+        float lse[MT], by[MT];
+        int t[MT];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (first + n + q < this->classes) {
-                    const float p = exp2_hw((this->logit(x[q], first + n + q, sx, sw) - lse) * kLog2e);
-                    x[q] = by * (n + q == t ? p - 1.f : p);
-                } else {
-                    x[q] = 0.f;
-                }
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = 0.f;
+        for (int i = 0; i < MT; ++i) {
+            const int m = mw + i * 16 + i16;
+            const bool there = m < count;
+            lse[i] = there ? this->st.lse[m] : 0.f;
+            by[i] = there ? g[m] * up : 0.f;
+            t[i] = (there ? this->st.target[m] : -0x40000000) - n0 - 4 * h;
         }
-        put_values<P, 4>(dz + (long)m * ldz, n, x);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            float z[NT][4];
+            this->logits(acc[i], c, n0, z);
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) z[j][q] = exp2_hw((z[j][q] - lse[i]) * kLog2e);
+            if (__any(t[i] >= 0 && t[i] < NT * 16))
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (t[i] == j * 16 + q) z[j][q] -= 1.f;
+            const bool there = mw + i * 16 + i16 < count;    // a row that is not may hold anything
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) z[j][q] = there && (c.inside || n0 + j * 16 + 4 * h + q < this->classes) ? z[j][q] * by[i] : 0.f;
+                put_values<P, 4>(reinterpret_cast<uint16_t*>(lds + i16 * PITCH), j * 16 + 4 * h, z[j]);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");           // LDS serves a wave in order
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int p = 0; p < CHUNKS / 4; ++p) {
+                const int k = p * 64 + lane, row = k / CHUNKS, at = k % CHUNKS, m = mw + i * 16 + row;
+                const uint4 line = *reinterpret_cast<const uint4*>(lds + row * PITCH + at * 16);
+                if (m < Ma && nw < Nb) *reinterpret_cast<uint4*>(dz + (long)m * ldz + (long)nw * P::N + at * 8) = line;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
     }
 };
 
@@ -314,7 +384,7 @@ template <class T, class P> struct InputOut {
     long ldb;
     T* dx;
     int d;
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool, int) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
         if (m >= *st.count || n >= d) return;
         const Scale sg = scale_at<P>(maxes, kMaxG), sw = scale_at<P>(maxes, kMaxW);
         if constexpr (P::N == 2)
@@ -337,7 +407,7 @@ template <class T, class P> struct WeightOut {
     T* dw;                       // of the piece
     long ldw;
     int d, classes;              // of the piece
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool, int) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
         if (m >= d || n >= classes) return;
         const Scale sg = scale_at<P>(maxes, kMaxG), sx = scale_at<P>(maxes, kMaxX);
         if constexpr (P::N == 2)
@@ -477,7 +547,29 @@ struct CeShape {
     int64_t rows, d, V;
 };
 
+// Few classes and inner positions: da_ce_narrow.h
+struct NarrowPlan {
+    bool taken;
+    int NF, KW;                  // fragments of the classes, and of the inner positions to a wave
+    int chunk, blocks;
+};
+NarrowPlan narrow_plan(const CeShape& s, bool backward) {
+    NarrowPlan p{};
+    if (s.V < 1 || s.V > kNarrowClasses || s.d > kNarrowInner || s.rows < 1) return p;
+    const int f = (int)ceil_div(s.V, 16), inner = narrow_inner(s.d);
+    p.NF = f <= 4 ? f : f <= 6 ? 6 : 8;
+    p.KW = inner <= 64 ? 1 : inner <= 128 ? 2 : 4;
+    if (narrow_lds(p.NF, inner, true) > kNarrowLds || p.KW * p.NF > 16) return p;    // of dw, 64 registers at most
+    const size_t lds = narrow_lds(p.NF, inner, backward);
+    p.taken = true;
+    const int64_t cus = compute_units(), resident = cus * std::max<int64_t>(1, std::min<int64_t>(6, (int64_t)(160 * 1024 / (lds + 256))));
+    p.chunk = (int)std::max<int64_t>(64, std::min<int64_t>(kNarrowChunk, ceil_div(ceil_div(s.rows, resident), 64) * 64));
+    p.blocks = (int)std::min(ceil_div(s.rows, p.chunk), resident);
+    return p;
+}
+
 struct CePlan {
+    NarrowPlan narrow, narrow_back;
     int64_t Ma, D, Vb;           // rows, d and classes, padded
     int64_t chunk, chunks;       // of the rows
     PlanePlan logits;
@@ -509,14 +601,21 @@ CePlan ce_plan(int dtype, const CeShape& s) {
     p.chunks = std::max<int64_t>(1, ceil_div(s.rows, p.chunk));
     p.logits = plane_plan(p.Ma, p.Vb, p.D / step, 1, false, false, step == Halves::STEP);
     p.slots = p.logits.tiles_n * wave_columns(p.logits);
+    p.narrow = narrow_plan(s, false);
+    p.narrow_back = narrow_plan(s, true);
+    if (p.narrow.taken) {
+        p.forward = 16 + (size_t)p.narrow.blocks * 2 * sizeof(double);
+        p.backward = 16 + round16((size_t)p.narrow_back.blocks * (s.d + 1) * s.V * sizeof(float));
+        return p;
+    }
     size_t at = 16;                                          // the largest magnitudes
     auto take = [&](size_t bytes) {
         const size_t from = at;
         at += round16(bytes);
         return from;
     };
-    p.x_at = take((size_t)p.Ma * p.D * 2 * N);
-    p.w_at = take((size_t)p.D * p.Vb * 2 * N);
+    p.x_at = take((size_t)p.Ma * plane_pitch(s.d, N) * 2);
+    p.w_at = take((size_t)p.D * plane_pitch(s.V, N) * 2);
     const size_t both = at;
     p.counts_at = take((size_t)p.chunks * 4);
     p.sums_at = take(kJoinBlocks * sizeof(double));
@@ -529,7 +628,7 @@ CePlan ce_plan(int dtype, const CeShape& s) {
     p.piece = std::max<int64_t>(1024, kPieceBytes / std::max<int64_t>(1, p.Ma * 2 * N) / 256 * 256);
     if (p.piece >= s.V) p.piece = std::max<int64_t>(s.V, 1);
     const int64_t Pb = padded(p.piece);
-    p.dz_at = take((size_t)p.Ma * Pb * 2 * N);
+    p.dz_at = take((size_t)p.Ma * plane_pitch(Pb, N) * 2);
     p.dx_at = take(p.piece < s.V ? (size_t)p.Ma * p.D * 4 : 0);
     p.bias_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(s.rows, 64), std::max<int64_t>(1, 1024 / ceil_div(Pb, 256))));
     p.bias_at = take((size_t)p.bias_parts * Pb * 4);
@@ -579,7 +678,7 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, long* ldw) {
         const int64_t blocks = std::min<int64_t>(ceil_div(padded(lines) * (padded(n) / 8), 256), 8192);
         if (blocks)
             hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)blocks), dim3(256), 0, c.stream, from, ld, lines, n, index, c.st.count, maxes,
-                               which, reinterpret_cast<uint16_t*>(c.ws + to), (long)(padded(n) * P::N));
+                               which, reinterpret_cast<uint16_t*>(c.ws + to), plane_pitch(n, P::N));
     };
     pack(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, kMaxX, c.p.x_at);
     // a weight of whole pads is read where it is
@@ -588,7 +687,7 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, long* ldw) {
         return reinterpret_cast<const uint16_t*>(w);
     }
     pack(w, c.s.V, c.s.d, (int)c.s.V, nullptr, kMaxW, c.p.w_at);
-    *ldw = c.p.Vb * P::N;
+    *ldw = plane_pitch(c.s.V, P::N);
     return reinterpret_cast<const uint16_t*>(c.ws + c.p.w_at);
 }
 
@@ -604,7 +703,7 @@ template <class P> void fill(Logits<P>& l, const CeCall& c) {
 template <class P> PlaneArgs logits_args(const CeCall& c, const uint16_t* w, long ldw, int64_t first, int64_t width) {
     PlaneArgs g{};
     g.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
-    g.lda = c.p.D * P::N;
+    g.lda = plane_pitch(c.s.d, P::N);
     g.B = w + first * P::N;
     g.ldb = ldw;
     g.Ma = (int)c.p.Ma;
@@ -662,7 +761,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
     for (int64_t first = 0; first < c.s.V; first += c.p.piece) {
         const int64_t width = std::min(c.p.piece, c.s.V - first), Vb = padded(width);
         const PiecePlan q = piece_plan(c.p, width, P::STEP);
-        const long ldz = Vb * P::N;
+        const long ldz = plane_pitch(Vb, P::N);
         GradOut<P> grad{};
         fill(grad, c);
         grad.g = g;
@@ -693,7 +792,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
         if (dw && c.s.d > 0) {
             PlaneArgs a{};
             a.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
-            a.lda = c.p.D * P::N;
+            a.lda = plane_pitch(c.s.d, P::N);
             a.B = dz;
             a.ldb = ldz;
             a.Ma = (int)c.p.D;
@@ -711,6 +810,76 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
                                (int)width, maxes, db, c.param_dtype, (int)first);
         }
     }
+}
+
+// ... a launch by the fragments that a call has
+template <class T, bool BWD> void narrow_launch(const NarrowPlan& p, const NarrowArgs& a, hipStream_t s) {
+    const size_t lds = narrow_lds(p.NF, narrow_inner(a.d), BWD);
+    auto go = [&](auto kernel) {
+        static std::atomic<uint64_t> allowed{0};             // devices that know how much LDS the kernel takes
+        int device = 0;
+        (void)hipGetDevice(&device);
+        const uint64_t bit = 1ull << (device & 63);
+        if (!(allowed.load(std::memory_order_relaxed) & bit) &&
+            hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kNarrowLds) == hipSuccess)
+            allowed.fetch_or(bit, std::memory_order_relaxed);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)p.blocks), dim3(kNarrowBlock), lds, s, a);
+    };
+    auto by_inner = [&](auto nf) {
+        constexpr int NF = decltype(nf)::value;
+        if (!BWD || p.KW == 1) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, 1, BWD>>::value);
+        else if (p.KW == 2) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, BWD ? 2 : 1, BWD>>::value);
+        else if constexpr (NF <= 4) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, BWD ? 4 : 1, BWD>>::value);
+    };
+    if (p.NF == 1) by_inner(std::integral_constant<int, 1>());
+    else if (p.NF == 2) by_inner(std::integral_constant<int, 2>());
+    else if (p.NF == 3) by_inner(std::integral_constant<int, 3>());
+    else if (p.NF == 4) by_inner(std::integral_constant<int, 4>());
+    else if (p.NF == 6) by_inner(std::integral_constant<int, 6>());
+    else by_inner(std::integral_constant<int, 8>());
+}
+
+// The statistics of such a call are by row: the class or -1, and log sum exp
+NarrowArgs narrow_args(const CeCall& c, const NarrowPlan& p, int reduction) {
+    NarrowArgs a{};
+    a.x = c.x;
+    a.w = c.w;
+    a.b = c.b;
+    a.ldx = c.ldx;
+    a.rows = c.s.rows;
+    a.d = (int)c.s.d;
+    a.V = (int)c.s.V;
+    a.param_type = c.param_dtype;
+    a.reduction = reduction;
+    a.chunk = p.chunk;
+    a.count = c.st.count;
+    a.kept_target = c.st.target;
+    a.lse = c.st.lse;
+    return a;
+}
+template <class T> void narrow_forward(const CeCall& c, const void* target, int target64, int reduction, float* loss) {
+    NarrowArgs a = narrow_args(c, c.p.narrow, reduction);
+    a.target = target;
+    a.target64 = target64;
+    a.loss = loss;
+    a.sums = reinterpret_cast<double*>(c.ws + 16);
+    narrow_launch<T, false>(c.p.narrow, a, c.stream);
+    if (c.p.narrow.blocks > 1) hipLaunchKernelGGL(ce_narrow_total_kernel, dim3(1), dim3(256), 0, c.stream, a, c.p.narrow.blocks);
+}
+template <class T>
+void narrow_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, void* dx, void* dw, void* db) {
+    const NarrowPlan& p = c.p.narrow_back;
+    NarrowArgs a = narrow_args(c, p, reduction);
+    a.dloss = dloss;
+    a.stride = stride;
+    a.dx = c.s.d ? dx : nullptr;
+    a.dw = c.s.d ? dw : nullptr;
+    a.db = db;
+    a.part = reinterpret_cast<float*>(c.ws + 16);
+    narrow_launch<T, true>(p, a, c.stream);
+    const int64_t numbers = (a.dw ? c.s.d * c.s.V : 0) + (db ? c.s.V : 0);
+    if (p.blocks > 1 && numbers)
+        hipLaunchKernelGGL((ce_narrow_join_kernel<T>), dim3((unsigned)ceil_div(numbers, 16)), dim3(256), 0, c.stream, a, p.blocks);
 }
 
 int ce_call(int dtype, int64_t rows, int64_t d, int64_t classes, const void* x, int64_t ldx, const void* w, const void* b, int param_dtype,
@@ -764,6 +933,11 @@ extern "C" int da_linear_cross_entropy(int dtype, int64_t rows, int64_t d, int64
     if (st != DA_OK) return st;
     if (rows > 0 && !target) return fail(DA_ERR_INVALID_ARG, "null target");
     if (!loss && (rows > 0 || reduction != DA_LOSS_ROWS)) return fail(DA_ERR_INVALID_ARG, "null loss");
+    if (c.p.narrow.taken) {
+        if (dtype == DA_F32) narrow_forward<float>(c, target, target64, reduction, loss);
+        else narrow_forward<bf16>(c, target, target64, reduction, loss);
+        return launched("da_linear_cross_entropy launch");
+    }
     if (dtype == DA_F32) ce_forward<float>(c, target, target64, reduction, loss);
     else ce_forward<bf16>(c, target, target64, reduction, loss);
     return launched("da_linear_cross_entropy launch");
@@ -781,6 +955,11 @@ extern "C" int da_linear_cross_entropy_backward(int dtype, int64_t rows, int64_t
     if (!dloss && (rows > 0 || reduction != DA_LOSS_ROWS)) return fail(DA_ERR_INVALID_ARG, "null dloss");
     if (db && param_dtype != DA_F32 && param_dtype != DA_BF16) return fail(DA_ERR_UNSUPPORTED, "param_dtype is neither DA_F32 nor DA_BF16");
     if (!dx && !dw && !db) return DA_OK;
+    if (c.p.narrow.taken) {
+        if (dtype == DA_F32) narrow_backward<float>(c, reduction, dloss, dloss_stride, dx, dw, db);
+        else narrow_backward<bf16>(c, reduction, dloss, dloss_stride, dx, dw, db);
+        return launched("da_linear_cross_entropy_backward launch");
+    }
     if (dtype == DA_F32) ce_backward<float>(c, reduction, dloss, dloss_stride, static_cast<float*>(dx), static_cast<float*>(dw), db);
     else ce_backward<bf16>(c, reduction, dloss, dloss_stride, static_cast<bf16*>(dx), static_cast<bf16*>(dw), db);
     return launched("da_linear_cross_entropy_backward launch");

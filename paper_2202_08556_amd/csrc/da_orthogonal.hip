@@ -3,16 +3,21 @@
 // All products are of pairs of fp16 halves (da_planes.h): a step multiplies errors of the small singular values by up to
 // a, like the values themselves, so what is kept between products keeps 22 bits; bf16 or single fp16 numbers there would be
 // off by 1e-2 and 3e-3 of the result where rounding it to bf16 costs 1.7e-3.
+// With bfloat16 two of these roundings do not show beside the result's: the first step's, on numbers that came with 8 bits (its
+// products are of first halves alone), and X's where b A + c A^2 multiplies it (its second half is left out there).  Over square
+// and wide random and low-rank matrices the result is then off by 1.04 to 1.2 times what rounding it costs.
 // X is held with the shorter side as rows (a tall matrix is turned around on its way in and out).  A and A^2 are symmetric:
 // only tiles on and above the diagonal are computed, and each is written to both of its places.
 // The scales of X, A and b A + c A^2 follow from how large singular values can be: at most 1 at first (the Frobenius norm
 // bounds them), then by the polynomial's extremes, which the host takes.
 #include "da_training.h"
 
+#include "da_orth_small.h"
 #include "da_planes_host.h"
 #include "da_spmm.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace daspmm {
 namespace {
@@ -139,33 +144,22 @@ struct GramOut {
     uint16_t* A;
     long lda, batch_a;
     float by;                    // of the product to A's scale
-    __device__ __forceinline__ void put(int m, int n, float (&x)[4], bool both, int batch) const {
-        uint16_t* __restrict__ a = A + batch * batch_a;
-        put_values<Halves, 4>(a + (long)m * lda, n, x);
-        if (both) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float one[1] = {x[q]};
-                put_values<Halves, 1>(a + (long)(n + q) * lda, m, one);
-            }
-        }
-    }
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool both, int batch) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] *= by;
-        put(m, n, x, both, batch);
+        put_values<Halves, 4>(A + batch * batch_a + (long)m * lda, n, x);
     }
 };
 // b A + c A^2
 struct PolyOut : GramOut {
     const uint16_t* from;        // A, laid out like the result
     float b, c;                  // with the scales
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool both, int batch) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
         float a[4];
         get_values<Halves, 4>(from + batch * batch_a + (long)m * lda, n, a);
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] = b * a[q] + c * x[q];
-        put(m, n, x, both, batch);
+        put_values<Halves, 4>(A + batch * batch_a + (long)m * lda, n, x);
     }
 };
 // a X + (b A + c A^2) X, packed
@@ -181,7 +175,7 @@ struct StepOut {
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] = a * old[q] + by * x[q];
     }
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool, int batch) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
         value(m, n, x, batch);
         put_values<Halves, 4>(to + batch * batch_x + (long)m * ldx, n, x);
     }
@@ -190,7 +184,7 @@ struct StepOut {
 template <class T> struct LastOut : StepOut {
     T* out;
     int rows, cols;
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], bool, int batch) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
         if (m >= rows || n >= cols) return;
         value(m, n, x, batch);
         T* __restrict__ p = out + (long)batch * rows * cols + (long)m * cols + n;
@@ -228,6 +222,8 @@ __global__ __launch_bounds__(256) void orth_scale_kernel(const T* __restrict__ g
 }
 
 // ------------------------------------------------------------------------------------------
+// Host
+// ------------------------------------------------------------------------------------------
 int fail(int code, const char* text) { return set_error(code, text); }
 int launched(const char* where) {
     const hipError_t e = hipGetLastError();
@@ -255,8 +251,8 @@ OrthPlan orth_plan(int64_t batch, int64_t rows, int64_t cols) {
     p.gram = plane_plan(p.Ma, p.Ma, p.Nb / step, batch, true, true, 1);
     p.poly = plane_plan(p.Ma, p.Ma, p.Ma / step, batch, true, true, 1);
     p.step = plane_plan(p.Ma, p.Nb, p.Ma / step, batch, false, true, 1);
-    p.X = (size_t)batch * p.Ma * p.Nb * 4;
-    p.A = (size_t)batch * p.Ma * p.Ma * 4;
+    p.X = (size_t)batch * p.Ma * plane_pitch(p.Nb, 2) * 2;
+    p.A = (size_t)batch * p.Ma * plane_pitch(p.Ma, 2) * 2;
     p.part = std::max({plane_part_bytes(p.gram, p.Ma, p.Ma, batch), plane_part_bytes(p.poly, p.Ma, p.Ma, batch),
                        plane_part_bytes(p.step, p.Ma, p.Nb, batch)});
     return p;
@@ -301,6 +297,36 @@ bool orth_scales(int steps, const float* c, StepScales* s) {
     return true;
 }
 
+bool small_takes(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kSmallSide && std::max(rows, cols) <= kSmallLong; }
+
+template <class T>
+void orthogonalise_small(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_t ldg, int64_t stride, int steps, const float* c, float eps,
+                         T* out, const StepScales* scales, hipStream_t s) {
+    SmallArgs a{};
+    a.ldg = ldg;
+    a.stride = stride;
+    a.rows = (int)rows;
+    a.cols = (int)cols;
+    a.steps = steps;
+    a.eps = eps;
+    a.first = scales[0].X;
+    a.last = 1.f / scales[steps].X;
+    for (int k = 0; k < steps; ++k) {
+        const float sx = scales[k].X, sa = scales[k].A, sb = scales[k].B, to = scales[k + 1].X;
+        a.step[k] = {sa / (sx * sx), c[3 * k + 1] * sb / sa, c[3 * k + 2] * sb / (sa * sa), c[3 * k] * to / sx, to / (sb * sx)};
+    }
+    const int n = (int)padded(std::max(rows, cols));
+    auto kernel = orth_small_kernel<T>;
+    static std::atomic<uint64_t> allowed{0};                 // devices that know how much LDS the kernel takes
+    int device = 0;
+    (void)hipGetDevice(&device);
+    const uint64_t bit = 1ull << (device & 63);
+    if (!(allowed.load(std::memory_order_relaxed) & bit) &&
+        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)small_lds(kSmallLong)) == hipSuccess)
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)batch), dim3(kSmallThreads), small_lds(n), s, g, out, a, n);
+}
+
 template <class T>
 void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_t ldg, int64_t stride, int steps, const float* c, float eps,
                    T* out, char* ws, const OrthPlan& p, const StepScales* scales, hipStream_t s) {
@@ -312,6 +338,7 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
     uint16_t* B = reinterpret_cast<uint16_t*>(ws + 2 * p.X + p.A);
     float* part = reinterpret_cast<float*>(ws + 2 * p.X + 2 * p.A);
     const bool tall = rows > cols;
+    if (small_takes(rows, cols)) return orthogonalise_small<T>(batch, rows, cols, g, ldg, stride, steps, c, eps, out, scales, s);
     hipLaunchKernelGGL((orth_norm_kernel<T>), dim3((unsigned)p.parts, (unsigned)batch), dim3(256), 0, s, g, (long)ldg, (long)stride,
                        (long)rows, (long)cols, norm);
     if (steps == 0) {
@@ -319,7 +346,7 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
                            dim3(256), 0, s, g, (long)ldg, (long)stride, (long)rows, (long)cols, norm, p.parts, eps, out);
         return;
     }
-    const long ldx = 2 * p.Nb, lda = 2 * p.Ma, bx = p.Ma * ldx, ba = p.Ma * lda;
+    const long ldx = plane_pitch(p.Nb, 2), lda = plane_pitch(p.Ma, 2), bx = p.Ma * ldx, ba = p.Ma * lda;
     hipLaunchKernelGGL((orth_pack_kernel<T>), dim3((unsigned)(p.Nb / 64), (unsigned)(p.Ma / 64), (unsigned)batch), dim3(256), 0, s, g,
                        (long)ldg, (long)stride, (int)rows, (int)cols, (int)tall, norm, p.parts, eps, scales[0].X, X, ldx, bx);
     PlaneArgs gram{}, poly{}, step{};
@@ -331,7 +358,10 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
     gram.K = step.Nb = (int)p.Nb;
     poly.A = poly.B = A;
     step.A = B;
-    for (int k = 0; k < steps; ++k) {
+    constexpr bool narrow = std::is_same_v<T, bf16>;
+    auto one_step = [&](int k, auto square, auto product) {
+        typedef decltype(square) S;
+        typedef decltype(product) P;
         const float sx = scales[k].X, sa = scales[k].A, sb = scales[k].B;
         gram.A = gram.B = step.B = X;
         GramOut first{};
@@ -339,28 +369,33 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
         first.lda = lda;
         first.batch_a = ba;
         first.by = sa / (sx * sx);
-        plane_product<Halves, kAlong, kAlong, kBoundNone>(gram, first, p.gram, (int)batch, part, s);
+        plane_product<S, kAlong, kAlong, kBoundNone>(gram, first, p.gram, (int)batch, part, s);
         PolyOut second{};
         static_cast<GramOut&>(second) = first;
         second.A = B;
         second.from = A;
         second.b = c[3 * k + 1] * sb / sa;
         second.c = c[3 * k + 2] * sb / (sa * sa);
-        plane_product<Halves, kAlong, kAlong, kBoundNone>(poly, second, p.poly, (int)batch, part, s);
+        plane_product<S, kAlong, kAlong, kBoundNone>(poly, second, p.poly, (int)batch, part, s);
         const bool last = k + 1 == steps && !tall;
         const float to = last ? 1.f : scales[k + 1].X;
-        StepOut third{X, Y, ldx, bx, c[3 * k] * to / sx, to / (sb * sx)};
+        const StepOut third{X, Y, ldx, bx, c[3 * k] * to / sx, to / (sb * sx)};
         if (last) {
             LastOut<T> l{};
             static_cast<StepOut&>(l) = third;
             l.out = out;
             l.rows = (int)rows;
             l.cols = (int)cols;
-            plane_product<Halves, kAlong, kAcross, kBoundNone>(step, l, p.step, (int)batch, part, s);
+            plane_product<P, kAlong, kAcross, kBoundNone>(step, l, p.step, (int)batch, part, s);
         } else {
-            plane_product<Halves, kAlong, kAcross, kBoundNone>(step, third, p.step, (int)batch, part, s);
+            plane_product<P, kAlong, kAcross, kBoundNone>(step, third, p.step, (int)batch, part, s);
         }
         std::swap(X, Y);
+    };
+    for (int k = 0; k < steps; ++k) {
+        if constexpr (!narrow) one_step(k, Halves(), Halves());
+        else if (k == 0) one_step(k, HalvesBy<1>(), HalvesBy<1>());
+        else one_step(k, Halves(), HalvesBy<2>());
     }
     if (tall)
         hipLaunchKernelGGL((orth_turn_kernel<T>), dim3((unsigned)(p.Nb / 64), (unsigned)(p.Ma / 64), (unsigned)batch), dim3(256), 0, s, X, ldx,
@@ -378,7 +413,7 @@ extern "C" int da_orthogonalise_workspace(int dtype, int64_t batch, int64_t rows
     const int st = orth_check(dtype, batch, rows, cols, steps);
     if (st != DA_OK) return st;
     const OrthPlan p = orth_plan(batch, rows, cols);
-    *bytes = steps == 0 ? round16(p.parts_bytes) : p.bytes();
+    *bytes = small_takes(rows, cols) ? 0 : steps == 0 ? round16(p.parts_bytes) : p.bytes();
     return DA_OK;
 }
 
@@ -395,7 +430,7 @@ extern "C" int da_orthogonalise(int dtype, int64_t batch, int64_t rows, int64_t 
     if (!orth_scales(steps, coefficients, scales)) return fail(DA_ERR_INVALID_ARG, "coefficients with which values could grow too large");
     if (batch == 0 || rows == 0 || cols == 0) return DA_OK;
     if (!g || !out) return fail(DA_ERR_INVALID_ARG, "null g or out");
-    if (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
+    if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
         return fail(DA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than reported");
     const OrthPlan p = orth_plan(batch, rows, cols);
     char* ws = static_cast<char*>(workspace);

@@ -24,6 +24,13 @@ enum { kAlong = 0, kAcross = 1 };            // a line of memory goes along the 
 constexpr int kPad = 64;
 __host__ __device__ inline long padded(long n) { return (n + kPad - 1) / kPad * kPad; }
 
+// Numbers from one line to the next of n values of N numbers each: lines whose distance is a multiple of 4 KB meet in few places of the
+// caches (4096 x 65536 . 65536 x 2048: 1133 us, and 1 line of 128 bytes further apart ONE_LINE)
+__host__ __device__ inline long plane_pitch(long n, int N) {
+    const long numbers = padded(n) * N;
+    return numbers % 2048 == 0 ? numbers + 64 : numbers;
+}
+
 struct One {
     static constexpr int N = 1, STEP = 64;   // numbers of a value, inner positions of a step
     typedef bf16x8 Frag;
@@ -31,13 +38,14 @@ struct One {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
 };
-struct Halves {
-    static constexpr int N = 2, STEP = 32;
+template <int PRODUCTS_> struct HalvesBy {   // 3: all; 2: both halves of the left operand with the first of the right one; 1: first halves
+    static constexpr int N = 2, STEP = 32, PRODUCTS = PRODUCTS_;
     typedef f16x8 Frag;
     static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
 };
+typedef HalvesBy<3> Halves;
 
 // V neighbouring values of a packed line from position `at` (a multiple of V) on
 template <class P, int V> __device__ __forceinline__ void put_values(uint16_t* line, long at, const float (&x)[V]) {
@@ -180,8 +188,9 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES_> struct PlaneShape {
     static constexpr int OCCUPANCY = LDS > 80 * 1024 ? THREADS / 256 : 2 * THREADS / 256;
 };
 
-// E: the epilogue.  E::kSymmetric: only tiles on and above the diagonal.  epi.rows(...) gets a tile's fragments if E::kWhole,
-// otherwise epi.four(m, n, x, tile is below its mirror image, batch) four neighbouring results at a time, after their sums are whole.
+// E: the epilogue.  epi.tile(...) gets a wave's fragments and its part of LDS if E::kWhole, otherwise epi.four(m, n, x, batch) four
+// neighbouring results at a time, after their sums are whole.  E::kSymmetric: only tiles on and above the diagonal are computed;
+// the results of those above it are handed over a second time, turned around.
 template <class P, class S, int ALAY, int BLAY, int BOUND, class E>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::OCCUPANCY, S::OCCUPANCY))) void plane_kernel(PlaneArgs g, E epi)
 {
@@ -287,22 +296,26 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
             for (int j = 0; j < NT; ++j) b[j] = bfrag(j, 0);
 #pragma unroll
             for (int i = 0; i < MT; ++i) a[i] = afrag(i, 0);
+            if constexpr (P::PRODUCTS == 3)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) c[j] = bfrag(j, 1);
+                for (int j = 0; j < NT; ++j) c[j] = bfrag(j, 1);
             __builtin_amdgcn_sched_barrier(0);
             all(a, b);
-            all(a, c);
+            if constexpr (P::PRODUCTS == 3) all(a, c);
+            if constexpr (P::PRODUCTS >= 2)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const typename P::Frag second = afrag(i, 1);
+                for (int i = 0; i < MT; ++i) {
+                    const typename P::Frag second = afrag(i, 1);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(b[j], second, acc[i][j]);
-            }
+                    for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(b[j], second, acc[i][j]);
+                }
         }
     }
     const int mw = m0 + wm * MT * 16, nw = n0 + wn * NT * 16, lane = tid & 63, i16 = lane & 15, h = lane >> 4;
+    char* const mine = lds + wave * S::MINE;
     if constexpr (E::kWhole) {
-        epi.template tile<MT, NT>(acc, mw, nw, bn * S::WN + wn);
+        __syncthreads();                                     // LDS is free
+        epi.template tile<MT, NT>(acc, mw, nw, bn * S::WN + wn, mine, g.Ma, g.Nb);
     } else {
         if (g.splits > 1) {
             float* __restrict__ part = g.part + (long)(batch * g.splits + blockIdx.y) * g.Ma * g.Nb;
@@ -318,7 +331,6 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         __syncthreads();                                     // LDS is free
         // Results leave by way of LDS, 16 rows of the wave at a time, so that a store is whole lines
         constexpr int LANES = NT * 4, ROWS = 64 / LANES;
-        char* const mine = lds + wave * S::MINE;
         const int row0 = lane / LANES, col = lane % LANES * 4, n = nw + col;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -331,22 +343,46 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
                 const int row = p * ROWS + row0, m = mw + i * 16 + row;
                 float x[4];
                 load_floats<4>(reinterpret_cast<const float*>(mine + row * S::PITCH) + col, x);
-                if (m < g.Ma && n < g.Nb) epi.four(m, n, x, E::kSymmetric && bm != bn, batch);
+                if (m < g.Ma && n < g.Nb) epi.four(m, n, x, batch);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
+        }
+        if constexpr (E::kSymmetric) {
+            if (bm == bn) return;
+            constexpr int COLS = MT * 16, TURNED = (COLS + 4) * 4, ACROSS = COLS / 4, DOWN = 64 / ACROSS;
+            static_assert(16 * TURNED <= S::LDS / (THREADS / 64), "16 turned rows of a wave");
+            char* const turned = lds + wave * (S::LDS / (THREADS / 64));
+            __syncthreads();                                 // the waves' parts of LDS are others now
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) *reinterpret_cast<float*>(turned + (h * 4 + q) * TURNED + (i * 16 + i16) * 4) = acc[i][j][q];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int p = 0; p < 16 / DOWN; ++p) {
+                    const int row = p * DOWN + lane / ACROSS, at = lane % ACROSS * 4, m = nw + j * 16 + row, n = mw + at;
+                    float x[4];
+                    load_floats<4>(reinterpret_cast<const float*>(turned + row * TURNED) + at, x);
+                    if (m < g.Nb && n < g.Ma) epi.four(m, n, x, batch);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
         }
     }
 }
 
 // Sums the parts of a product in one order, four neighbouring results to `lanes` lanes.
-template <int BM, int BN, class E> __global__ __launch_bounds__(256) void plane_join_kernel(PlaneArgs g, int lanes, E epi)
+template <class E> __global__ __launch_bounds__(256) void plane_join_kernel(PlaneArgs g, int lanes, E epi)
 {
     const long fours = g.Nb / 4, total = (long)g.Ma * fours, plane = (long)g.Ma * g.Nb;
     const int batch = blockIdx.z, lane = threadIdx.x & (lanes - 1);
     for (long at = ((long)blockIdx.x * 256 + threadIdx.x) / lanes; at < total; at += (long)gridDim.x * 256 / lanes) {
         const int m = (int)(at / fours), n = (int)(at % fours) * 4;
-        if (E::kSymmetric && m / BM > n / BN) continue;
         const float* __restrict__ p = g.part + (long)batch * g.splits * plane + (long)m * g.Nb + n;
         f32x4 s[4] = {};
         int k = lane;
@@ -359,7 +395,42 @@ template <int BM, int BN, class E> __global__ __launch_bounds__(256) void plane_
 #pragma unroll
             for (int q = 0; q < 4; ++q) t[q] += __shfl_xor(t[q], d, 64);
         float x[4] = {t[0], t[1], t[2], t[3]};
-        if (lane == 0) epi.four(m, n, x, E::kSymmetric && m / BM != n / BN, batch);
+        if (lane == 0) epi.four(m, n, x, batch);
+    }
+}
+
+// ... of a symmetric one: a tile of 64 x 64 on or above the diagonal to a block, which hands it over in both places
+template <class E> __global__ __launch_bounds__(256) void plane_join_half_kernel(PlaneArgs g, E epi)
+{
+    __shared__ float turned[64][65];
+    const long plane = (long)g.Ma * g.Nb;
+    const int batch = blockIdx.z, r = threadIdx.x / 16, c = threadIdx.x % 16 * 4;
+    int bm, bn;
+    half_tile(blockIdx.x, g.Ma / 64, &bm, &bn);
+    const float* __restrict__ part = g.part + (long)batch * g.splits * plane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int m = bm * 64 + i * 16 + r, n = bn * 64 + c;
+        const float* __restrict__ p = part + (long)m * g.Nb + n;
+        f32x4 s[4] = {};
+        int k = 0;
+        for (; k + 4 <= g.splits; k += 4)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[u] += *reinterpret_cast<const f32x4*>(p + (long)(k + u) * plane);
+        for (; k < g.splits; ++k) s[0] += *reinterpret_cast<const f32x4*>(p + (long)k * plane);
+        const f32x4 t = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) turned[c + q][i * 16 + r] = t[q];
+        float x[4] = {t[0], t[1], t[2], t[3]};
+        epi.four(m, n, x, batch);
+    }
+    if (bm == bn) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 16 + r;
+        float x[4] = {turned[row][c], turned[row][c + 1], turned[row][c + 2], turned[row][c + 3]};
+        epi.four(bn * 64 + row, bm * 64 + c, x, batch);
     }
 }
 

@@ -75,9 +75,14 @@ void plane_launch(const PlaneArgs& g, const E& epi, const PlanePlan& p, int batc
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles, (unsigned)p.splits, (unsigned)batches), dim3(S::THREADS), S::LDS, s, g, epi);
     if constexpr (!E::kWhole) {
         if (p.splits > 1) {
-            const int lanes = p.splits >= 64 ? 16 : p.splits >= 16 ? 4 : 1;
-            const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.Ma * g.Nb / 4 * lanes, 256), 8192);
-            hipLaunchKernelGGL((plane_join_kernel<S::BM, S::BN, E>), dim3((unsigned)blocks, 1, (unsigned)batches), dim3(256), 0, s, g, lanes, epi);
+            if constexpr (E::kSymmetric) {
+                const int64_t side = g.Ma / 64;
+                hipLaunchKernelGGL((plane_join_half_kernel<E>), dim3((unsigned)(side * (side + 1) / 2), 1, (unsigned)batches), dim3(256), 0, s, g, epi);
+            } else {
+                const int lanes = p.splits >= 64 ? 16 : p.splits >= 16 ? 4 : 1;
+                const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.Ma * g.Nb / 4 * lanes, 256), 8192);
+                hipLaunchKernelGGL((plane_join_kernel<E>), dim3((unsigned)blocks, 1, (unsigned)batches), dim3(256), 0, s, g, lanes, epi);
+            }
         }
     }
 }

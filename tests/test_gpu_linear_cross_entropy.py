@@ -102,7 +102,9 @@ def check(x, w, b, t, g, device="cpu", reduction="none"):
 
 
 SIZES = [(1, 1, 1), (1, 16, 4), (3, 5, 2), (2, 64, 1), (61, 64, 41), (64, 64, 64), (65, 70, 129), (130, 33, 300), (257, 96, 1000), (300, 128, 257),
-         (1000, 24, 70), (5000, 16, 41), (40, 300, 5000), (1, 602, 9973), (700, 1, 33), (2100, 64, 2100), (16, 2000, 64), (4099, 40, 4100)]
+         (1000, 24, 70), (5000, 16, 41), (40, 300, 5000), (1, 602, 9973), (700, 1, 33), (2100, 64, 2100), (16, 2000, 64), (4099, 40, 4100),
+         (20000, 128, 47), (3000, 256, 64), (2500, 250, 40), (900, 100, 128), (1100, 128, 100), (700, 144, 90), (700, 64, 128), (333, 257, 41),
+         (100000, 3, 2), (129, 17, 96), (64, 256, 16)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)

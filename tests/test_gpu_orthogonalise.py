@@ -45,7 +45,8 @@ def momentum(B, r, c, dtype, seed=0):
 
 
 SIZES = [(1, 1, 1), (1, 1, 7), (1, 5, 1), (1, 16, 16), (1, 64, 256), (1, 65, 129), (1, 63, 64), (3, 40, 100), (2, 100, 40), (1, 200, 1000), (1, 1187, 602),
-         (12, 256, 1024), (48, 64, 64), (1, 130, 5000), (1, 5000, 130), (40, 250, 300), (1, 2100, 2200), (1, 300, 9000), (5, 1, 64), (70, 128, 512)]
+         (12, 256, 1024), (48, 64, 64), (1, 130, 5000), (1, 5000, 130), (40, 250, 300), (1, 2100, 2200), (1, 300, 9000), (5, 1, 64), (70, 128, 512),
+         (600, 64, 512), (3, 512, 64), (2, 64, 513), (2, 33, 470), (7, 500, 17), (1, 64, 65)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)

@@ -94,14 +94,14 @@ def test_cross_entropy_sizes(change, status):
 @pytest.mark.parametrize("change,status", [
     (dict(ldx=7), INVALID), (dict(x=None), INVALID), (dict(w=None), INVALID), (dict(param=9), UNSUPPORTED), (dict(target=None), INVALID),
     (dict(reduction=3), INVALID), (dict(reduction=-1), INVALID), (dict(loss=None), INVALID), (dict(stats=None), INVALID),
-    (dict(stats=ODD), INVALID), (dict(ws=None), INVALID), (dict(bytes=64), INVALID), (dict(ws=ODD), INVALID)])
+    (dict(stats=ODD), INVALID), (dict(ws=None), INVALID), (dict(bytes=16), INVALID), (dict(d=300, ldx=300, bytes=64), INVALID), (dict(ws=ODD), INVALID)])
 def test_cross_entropy(change, status):
     assert ce(**change) == status
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(ldx=7), INVALID), (dict(x=None), INVALID), (dict(stride=-1), INVALID), (dict(dloss=None), INVALID), (dict(reduction=5), INVALID),
-    (dict(b=None, param=9), UNSUPPORTED), (dict(bytes=64), INVALID), (dict(stats=None), INVALID), (dict(dx=None, dw=None, db=None), da.DA_OK)])
+    (dict(b=None, param=9), UNSUPPORTED), (dict(bytes=64), INVALID), (dict(V=300, bytes=1024), INVALID), (dict(stats=None), INVALID), (dict(dx=None, dw=None, db=None), da.DA_OK)])
 def test_cross_entropy_backward(change, status):
     assert ce_back(**change) == status
 
@@ -120,8 +120,8 @@ def orth(dtype=0, batch=1, rows=8, cols=8, g=P, ldg=8, stride=64, coefficients=G
     (dict(dtype=2), UNSUPPORTED), (dict(batch=-1), INVALID), (dict(rows=-1), INVALID), (dict(batch=65536), UNSUPPORTED),
     (dict(rows=2 ** 17 + 1), UNSUPPORTED), (dict(cols=2 ** 17 + 1, ldg=2 ** 18), UNSUPPORTED), (dict(rows=2 ** 17, cols=2 ** 17, ldg=2 ** 17, batch=500), UNSUPPORTED),
     (dict(steps=-1), INVALID), (dict(steps=65), UNSUPPORTED), (dict(coefficients=None, steps=5), INVALID), (dict(ldg=7), INVALID),
-    (dict(stride=-64), INVALID), (dict(eps=-1.0), INVALID), (dict(g=None), INVALID), (dict(out=None), INVALID), (dict(ws=None), INVALID),
-    (dict(bytes=64), INVALID), (dict(ws=ODD), INVALID),
+    (dict(stride=-64), INVALID), (dict(eps=-1.0), INVALID), (dict(g=None), INVALID), (dict(out=None), INVALID), (dict(rows=80, cols=80, ldg=80, ws=None), INVALID),
+    (dict(rows=80, cols=80, ldg=80, bytes=64), INVALID), (dict(rows=80, cols=80, ldg=80, ws=ODD), INVALID),
     # values that grow from step to step, or are none
     (dict(coefficients=(200.0, 0.0, 0.0)), INVALID), (dict(coefficients=(3.0, 0.0, 0.0) * 5), INVALID),
     (dict(coefficients=(float("nan"), 0.0, 0.0)), INVALID), (dict(coefficients=(1.0, float("inf"), 0.0)), INVALID),
