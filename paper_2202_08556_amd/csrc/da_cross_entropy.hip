@@ -62,8 +62,9 @@ __device__ __forceinline__ long target_of(const void* t, int wide, long r) {
     return wide ? static_cast<const int64_t*>(t)[r] : (long)static_cast<const int32_t*>(t)[r];
 }
 
-__global__ void ce_zero_kernel(uint32_t* p, int n) {
-    if ((int)threadIdx.x < n) p[threadIdx.x] = 0;
+__global__ void ce_zero_kernel(uint32_t* maxes, int* arrived) {
+    if (threadIdx.x < kMaxes) maxes[threadIdx.x] = 0;
+    for (int k = threadIdx.x; k < kMostParted; k += 256) arrived[k] = 0;
 }
 
 // Rows of a chunk that have a target
@@ -577,10 +578,10 @@ struct CePlan {
     int64_t piece;               // classes of a piece, a multiple of 64 where there are several
     int bias_parts;
     size_t counts_at, sums_at, target_at, x_at, w_at, part_at, forward;          // bytes
-    size_t g_at, dz_at, dx_at, bias_at, sum_at, backward;
+    size_t g_at, arrived_at, dz_at, dx_at, bias_at, sum_at, backward;
 };
 
-int wave_columns(const PlanePlan& p) { return p.shape == 0 ? PlaneLarge::WN : p.shape == 1 ? PlaneMiddle::WN : PlaneSmall::WN; }
+int wave_columns(const PlanePlan& p) { return p.shape == 0 ? PlaneLarge::WN : PlaneSmall::WN; }
 
 struct PiecePlan {
     PlanePlan logits, input, weight;
@@ -625,6 +626,7 @@ CePlan ce_plan(int dtype, const CeShape& s) {
 
     at = both;
     p.g_at = take((size_t)p.Ma * 4);
+    p.arrived_at = take(kMostParted * sizeof(int));
     p.piece = std::max<int64_t>(1024, kPieceBytes / std::max<int64_t>(1, p.Ma * 2 * N) / 256 * 256);
     if (p.piece >= s.V) p.piece = std::max<int64_t>(s.V, 1);
     const int64_t Pb = padded(p.piece);
@@ -636,7 +638,7 @@ CePlan ce_plan(int dtype, const CeShape& s) {
     for (const int64_t width : {p.piece, s.V % p.piece})
         if (width > 0) {
             const PiecePlan q = piece_plan(p, width, step);
-            sums = std::max({sums, plane_part_bytes(q.input, p.Ma, p.D, 1), plane_part_bytes(q.weight, p.D, padded(width), 1)});
+            sums = std::max({sums, plane_part_bytes(q.input, 1), plane_part_bytes(q.weight, 1)});
         }
     p.sum_at = take(sums);
     p.backward = at;
@@ -731,7 +733,7 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
     out.part = reinterpret_cast<float2*>(c.ws + c.p.part_at);
     out.slots = c.p.slots;
     out.at_target = reinterpret_cast<float*>(c.ws + c.p.target_at);
-    plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, 0, c.s.V), out, c.p.logits, 1, nullptr, c.stream);
+    plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, 0, c.s.V), out, c.p.logits, 1, nullptr, nullptr, c.stream);
     int lanes = 1;
     while (lanes < 64 && lanes < c.p.slots) lanes *= 2;
     double* sums = reduction == DA_LOSS_ROWS ? nullptr : reinterpret_cast<double*>(c.ws + c.p.sums_at);
@@ -745,7 +747,8 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
     typedef PlaneOf<T> P;
     uint32_t* maxes = reinterpret_cast<uint32_t*>(c.ws);
     float* g = reinterpret_cast<float*>(c.ws + c.p.g_at);
-    hipLaunchKernelGGL(ce_zero_kernel, dim3(1), dim3(64), 0, c.stream, maxes, (int)kMaxes);
+    int* arrived = reinterpret_cast<int*>(c.ws + c.p.arrived_at);
+    hipLaunchKernelGGL(ce_zero_kernel, dim3(1), dim3(256), 0, c.stream, maxes, arrived);
     hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 256))), dim3(256), 0,
                        c.stream, c.st, (long)c.s.rows, dloss, (long)stride, reduction, g, maxes);
     if (dx && c.s.d > 0 && c.s.rows > 0)
@@ -768,7 +771,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
         grad.first = (int)first;
         grad.dz = dz;
         grad.ldz = ldz;
-        plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, first, width), grad, q.logits, 1, nullptr, c.stream);
+        plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, first, width), grad, q.logits, 1, nullptr, nullptr, c.stream);
         if (dx && c.s.d > 0) {
             PlaneArgs a{};
             a.A = dz;
@@ -787,7 +790,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             out.ldb = c.p.D;
             out.dx = dx;
             out.d = (int)c.s.d;
-            plane_product<P, kAlong, kAlong, kBoundM>(a, out, q.input, 1, part, c.stream);
+            plane_product<P, kAlong, kAlong, kBoundM>(a, out, q.input, 1, part, arrived, c.stream);
         }
         if (dw && c.s.d > 0) {
             PlaneArgs a{};
@@ -800,7 +803,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             a.K = (int)c.p.Ma;
             a.rows = c.st.count;
             const WeightOut<T, P> out{maxes, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
-            plane_product<P, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, c.stream);
+            plane_product<P, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, arrived, c.stream);
         }
         if (db) {
             const int64_t per = ceil_div(c.s.rows, c.p.bias_parts);

@@ -28,10 +28,12 @@ constexpr int kOrthMost = 1 << 17;
 // Sums of squares in 64 bits: the squares of floats neither overflow nor vanish there
 template <class T>
 __global__ __launch_bounds__(256) void orth_norm_kernel(const T* __restrict__ g, long ldg, long stride, long rows, long cols,
-                                                        double* __restrict__ part)
+                                                        double* __restrict__ part, int* __restrict__ arrived)
 {
     __shared__ double red[4];
     const T* __restrict__ p = g + blockIdx.y * stride;
+    if (arrived && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int k = threadIdx.x; k < kMostParted; k += 256) arrived[k] = 0;
     // pieces of 1024 columns of a row, a wave's turn each, dealt to all waves of the matrix
     const long across = (cols + 1023) / 1024, all = rows * across, step = (long)gridDim.x * 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -235,7 +237,7 @@ struct OrthPlan {
     int parts;                   // of a norm
     PlanePlan gram, poly, step;
     size_t X, A, part;           // bytes
-    size_t bytes() const { return round16((size_t)parts_bytes) + 2 * X + 2 * A + part; }
+    size_t bytes() const { return round16((size_t)parts_bytes) + kMostParted * sizeof(int) + 2 * X + 2 * A + part; }
     size_t parts_bytes;
 };
 
@@ -253,8 +255,7 @@ OrthPlan orth_plan(int64_t batch, int64_t rows, int64_t cols) {
     p.step = plane_plan(p.Ma, p.Nb, p.Ma / step, batch, false, true, 1);
     p.X = (size_t)batch * p.Ma * plane_pitch(p.Nb, 2) * 2;
     p.A = (size_t)batch * p.Ma * plane_pitch(p.Ma, 2) * 2;
-    p.part = std::max({plane_part_bytes(p.gram, p.Ma, p.Ma, batch), plane_part_bytes(p.poly, p.Ma, p.Ma, batch),
-                       plane_part_bytes(p.step, p.Ma, p.Nb, batch)});
+    p.part = std::max({plane_part_bytes(p.gram, batch), plane_part_bytes(p.poly, batch), plane_part_bytes(p.step, batch)});
     return p;
 }
 
@@ -332,6 +333,8 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
                    T* out, char* ws, const OrthPlan& p, const StepScales* scales, hipStream_t s) {
     double* norm = reinterpret_cast<double*>(ws);
     ws += round16(p.parts_bytes);
+    int* arrived = steps ? reinterpret_cast<int*>(ws) : nullptr;
+    ws += kMostParted * sizeof(int);
     uint16_t* X = reinterpret_cast<uint16_t*>(ws);
     uint16_t* Y = reinterpret_cast<uint16_t*>(ws + p.X);
     uint16_t* A = reinterpret_cast<uint16_t*>(ws + 2 * p.X);
@@ -340,7 +343,7 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
     const bool tall = rows > cols;
     if (small_takes(rows, cols)) return orthogonalise_small<T>(batch, rows, cols, g, ldg, stride, steps, c, eps, out, scales, s);
     hipLaunchKernelGGL((orth_norm_kernel<T>), dim3((unsigned)p.parts, (unsigned)batch), dim3(256), 0, s, g, (long)ldg, (long)stride,
-                       (long)rows, (long)cols, norm);
+                       (long)rows, (long)cols, norm, arrived);
     if (steps == 0) {
         hipLaunchKernelGGL((orth_scale_kernel<T>), dim3((unsigned)std::min<int64_t>(ceil_div(rows * cols, 256), 2048), (unsigned)batch),
                            dim3(256), 0, s, g, (long)ldg, (long)stride, (long)rows, (long)cols, norm, p.parts, eps, out);
@@ -369,14 +372,14 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
         first.lda = lda;
         first.batch_a = ba;
         first.by = sa / (sx * sx);
-        plane_product<S, kAlong, kAlong, kBoundNone>(gram, first, p.gram, (int)batch, part, s);
+        plane_product<S, kAlong, kAlong, kBoundNone>(gram, first, p.gram, (int)batch, part, arrived, s);
         PolyOut second{};
         static_cast<GramOut&>(second) = first;
         second.A = B;
         second.from = A;
         second.b = c[3 * k + 1] * sb / sa;
         second.c = c[3 * k + 2] * sb / (sa * sa);
-        plane_product<S, kAlong, kAlong, kBoundNone>(poly, second, p.poly, (int)batch, part, s);
+        plane_product<S, kAlong, kAlong, kBoundNone>(poly, second, p.poly, (int)batch, part, arrived, s);
         const bool last = k + 1 == steps && !tall;
         const float to = last ? 1.f : scales[k + 1].X;
         const StepOut third{X, Y, ldx, bx, c[3 * k] * to / sx, to / (sb * sx)};
@@ -386,9 +389,9 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
             l.out = out;
             l.rows = (int)rows;
             l.cols = (int)cols;
-            plane_product<P, kAlong, kAcross, kBoundNone>(step, l, p.step, (int)batch, part, s);
+            plane_product<P, kAlong, kAcross, kBoundNone>(step, l, p.step, (int)batch, part, arrived, s);
         } else {
-            plane_product<P, kAlong, kAcross, kBoundNone>(step, third, p.step, (int)batch, part, s);
+            plane_product<P, kAlong, kAcross, kBoundNone>(step, third, p.step, (int)batch, part, arrived, s);
         }
         std::swap(X, Y);
     };

@@ -134,8 +134,10 @@ struct PlaneArgs {
     int tiles_m, tiles_n;
     const int* rows;             // where not null: so many of the outer positions of A (kBoundM), or of the inner ones (kBoundK), are there
     int splits, per;             // parts of the sum, steps of one
-    float* part;                 // splits > 1: [batch][split][Ma][Nb]
+    float* part;                 // splits > 1: [batch][tile][split], a tile's sums as its waves hold them
+    int* arrived;                // ... [batch][tile], 0: how many of a tile's parts are there
 };
+constexpr int kMostParted = 1024;            // tiles whose sums are in parts
 enum { kBoundNone = 0, kBoundM = 1, kBoundK = 2 };
 
 // 16 bytes a lane from base + offset to LDS: byte `to` of it and on, lane by lane.  Written out because the compiler, which
@@ -152,6 +154,13 @@ __device__ __forceinline__ const char* same_for_all(const char* p) {
 }
 template <int N> __device__ __forceinline__ void wait_for_lines() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+// All but the loads of the last `left` steps, MOST at most
+template <int LOADS, int MOST> __device__ __forceinline__ void wait_for_steps(int left) {
+    if constexpr (MOST == 0) wait_for_lines<0>();
+    else if (left >= MOST) wait_for_lines<MOST * LOADS>();
+    else wait_for_steps<LOADS, MOST - 1>(left);
 }
 
 // Tile of a block: blocks go to the 8 dies of the chip in turn; a die takes neighbouring tiles, four rows of tiles at a time,
@@ -251,7 +260,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     constexpr int AHEAD = S::STAGES - 1;
-    static_assert(AHEAD >= 1 && AHEAD <= 3, "waits below");
+    static_assert(AHEAD >= 1 && AHEAD <= 7 && (AHEAD - 1) * S::LOADS <= 63, "waits below");
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s)
         if (t0 + s < t1) fetch(t0 + s, s);
@@ -259,9 +268,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
     for (int t = t0; t < t1; ++t) {
         const int left = t1 - 1 - t;
         // the steps after this one may still be on their way
-        if (AHEAD == 3 && left >= 2) wait_for_lines<2 * S::LOADS>();
-        else if (AHEAD >= 2 && left >= 1) wait_for_lines<S::LOADS>();
-        else wait_for_lines<0>();
+        wait_for_steps<S::LOADS, AHEAD - 1>(left);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (left >= AHEAD) {
@@ -317,16 +324,48 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         __syncthreads();                                     // LDS is free
         epi.template tile<MT, NT>(acc, mw, nw, bn * S::WN + wn, mine, g.Ma, g.Nb);
     } else {
+        // The block that comes last adds a tile's parts, in their order: nobody waits for another.  Parts pass between blocks of
+        // different dies, whose caches do not know of each other: they are written and read at the chip's scope (a fence of that
+        // scope writes back all that a die's cache holds: 80 us in place of 5).
         if (g.splits > 1) {
-            float* __restrict__ part = g.part + (long)(batch * g.splits + blockIdx.y) * g.Ma * g.Nb;
+            constexpr int PART = S::BM * S::BN / 2, MINE = MT * NT * 128;    // pairs of floats, of a tile and of a wave
+            const long tile = (long)batch * gridDim.x + blockIdx.x;
+            uint64_t* const part = reinterpret_cast<uint64_t*>(g.part) + tile * g.splits * PART + wave * MINE + lane;
+            uint64_t* const to = part + (long)blockIdx.y * PART;
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const int m = mw + i * 16 + i16, n = nw + j * 16 + 4 * h;
-                    if (m < g.Ma && n < g.Nb) *reinterpret_cast<f32x4*>(part + (long)m * g.Nb + n) = acc[i][j];
-                }
-            return;
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        __hip_atomic_store(to + ((i * NT + j) * 2 + q) * 64,
+                                           (uint64_t)__float_as_uint(acc[i][j][2 * q]) | (uint64_t)__float_as_uint(acc[i][j][2 * q + 1]) << 32,
+                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // this wave's are there
+            __syncthreads();
+            int* const last = reinterpret_cast<int*>(lds);
+            if (tid == 0) {
+                *last = __hip_atomic_fetch_add(g.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == g.splits - 1;
+                if (*last) __hip_atomic_store(g.arrived + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next product
+            }
+            __syncthreads();
+            if (!*last) return;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < g.splits; ++k)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const uint64_t v = __hip_atomic_load(part + (long)k * PART + ((i * NT + j) * 2 + q) * 64, __ATOMIC_RELAXED,
+                                                                 __HIP_MEMORY_SCOPE_AGENT);
+                            acc[i][j][2 * q] += __uint_as_float((uint32_t)v);
+                            acc[i][j][2 * q + 1] += __uint_as_float((uint32_t)(v >> 32));
+                        }
         }
         __syncthreads();                                     // LDS is free
         // Results leave by way of LDS, 16 rows of the wave at a time, so that a store is whole lines
@@ -373,64 +412,6 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
                 __builtin_amdgcn_wave_barrier();
             }
         }
-    }
-}
-
-// Sums the parts of a product in one order, four neighbouring results to `lanes` lanes.
-template <class E> __global__ __launch_bounds__(256) void plane_join_kernel(PlaneArgs g, int lanes, E epi)
-{
-    const long fours = g.Nb / 4, total = (long)g.Ma * fours, plane = (long)g.Ma * g.Nb;
-    const int batch = blockIdx.z, lane = threadIdx.x & (lanes - 1);
-    for (long at = ((long)blockIdx.x * 256 + threadIdx.x) / lanes; at < total; at += (long)gridDim.x * 256 / lanes) {
-        const int m = (int)(at / fours), n = (int)(at % fours) * 4;
-        const float* __restrict__ p = g.part + (long)batch * g.splits * plane + (long)m * g.Nb + n;
-        f32x4 s[4] = {};
-        int k = lane;
-        for (; k + 3 * lanes < g.splits; k += 4 * lanes)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) s[u] += *reinterpret_cast<const f32x4*>(p + (long)(k + u * lanes) * plane);
-        for (; k < g.splits; k += lanes) s[0] += *reinterpret_cast<const f32x4*>(p + (long)k * plane);
-        f32x4 t = (s[0] + s[1]) + (s[2] + s[3]);
-        for (int d = 1; d < lanes; d <<= 1)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) t[q] += __shfl_xor(t[q], d, 64);
-        float x[4] = {t[0], t[1], t[2], t[3]};
-        if (lane == 0) epi.four(m, n, x, batch);
-    }
-}
-
-// ... of a symmetric one: a tile of 64 x 64 on or above the diagonal to a block, which hands it over in both places
-template <class E> __global__ __launch_bounds__(256) void plane_join_half_kernel(PlaneArgs g, E epi)
-{
-    __shared__ float turned[64][65];
-    const long plane = (long)g.Ma * g.Nb;
-    const int batch = blockIdx.z, r = threadIdx.x / 16, c = threadIdx.x % 16 * 4;
-    int bm, bn;
-    half_tile(blockIdx.x, g.Ma / 64, &bm, &bn);
-    const float* __restrict__ part = g.part + (long)batch * g.splits * plane;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = bm * 64 + i * 16 + r, n = bn * 64 + c;
-        const float* __restrict__ p = part + (long)m * g.Nb + n;
-        f32x4 s[4] = {};
-        int k = 0;
-        for (; k + 4 <= g.splits; k += 4)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) s[u] += *reinterpret_cast<const f32x4*>(p + (long)(k + u) * plane);
-        for (; k < g.splits; ++k) s[0] += *reinterpret_cast<const f32x4*>(p + (long)k * plane);
-        const f32x4 t = (s[0] + s[1]) + (s[2] + s[3]);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) turned[c + q][i * 16 + r] = t[q];
-        float x[4] = {t[0], t[1], t[2], t[3]};
-        epi.four(m, n, x, batch);
-    }
-    if (bm == bn) return;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = i * 16 + r;
-        float x[4] = {turned[row][c], turned[row][c + 1], turned[row][c + 2], turned[row][c + 3]};
-        epi.four(bn * 64 + row, bm * 64 + c, x, batch);
     }
 }
 

@@ -26,11 +26,11 @@ struct PlaneCost {
     int64_t side;
     double alone, shared, more;
 };
-constexpr PlaneCost kPlaneCost[2][3] = {{{256, 1.65, 1.65, 8.0}, {128, 0.55, 0.9, 5.0}, {64, 0.15, 0.25, 3.0}},          // One
-                                        {{256, 2.4, 2.4, 8.0}, {128, 0.8, 1.3, 5.0}, {64, 0.17, 0.35, 3.0}}};          // Halves
+constexpr PlaneCost kPlaneCost[2][3] = {{{256, 1.65, 1.65, 8.0}, {128, 0.6, 0.9, 6.0}, {64, 0.25, 0.3, 5.0}},          // One
+                                        {{256, 2.4, 2.4, 8.0}, {128, 0.9, 1.3, 6.0}, {64, 0.3, 0.4, 5.0}}};          // Halves
 
 // The tile, and the number of parts of the inner axis, whose turns on the chip take the least time: large tiles read least for what
-// they compute, small ones and parts keep all units busy, and parts pass through memory once more (4 TB/s and a launch).
+// they compute, small ones and parts keep all units busy, and a tile's parts go to memory and are read by one block (about 60 KB/us).
 inline PlanePlan plane_plan(int64_t Ma, int64_t Nb, int64_t steps, int64_t batches, bool symmetric, bool may_split, int halves) {
     PlanePlan best{};
     const int64_t cus = compute_units();
@@ -42,12 +42,13 @@ inline PlanePlan plane_plan(int64_t Ma, int64_t Nb, int64_t steps, int64_t batch
         p.tiles_m = (int)ceil_div(Ma, c.side);
         p.tiles_n = (int)ceil_div(Nb, c.side);
         p.tiles = symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
-        const double parts = (double)batches * Ma * Nb * 8.0 / 4e6 * (symmetric ? 0.5 : 1.0);
-        for (int64_t splits = 1; splits <= 1024 && (splits == 1 || (may_split && steps / splits >= 4)); splits += std::max<int64_t>(1, splits / 2)) {
+        const bool parts = may_split && p.tiles * batches <= kMostParted;
+        for (int64_t splits = 1; splits <= 1024 && (splits == 1 || (parts && steps / splits >= 4)); splits += std::max<int64_t>(1, splits / 2)) {
             const int64_t per = std::max<int64_t>(1, ceil_div(steps, splits)), real = std::max<int64_t>(1, ceil_div(steps, per));
             const int64_t blocks = p.tiles * batches * real, slots = shape == 0 ? cus : 2 * cus;
             const double turn = (double)per * (blocks > cus ? c.shared : c.alone) + c.more;
-            const double time = (double)ceil_div(std::max<int64_t>(blocks, 1), slots) * turn + (real > 1 ? 4.0 + parts * (double)real : 0.0);
+            const double join = real > 1 ? 3.0 + (double)(real + 1) * (double)(c.side * c.side) * 4.0 / 6e4 : 0.0;
+            const double time = (double)ceil_div(std::max<int64_t>(blocks, 1), slots) * turn + join;
             if ((shape == 0 && splits == 1) || time < least) {
                 least = time;
                 best = p;
@@ -58,8 +59,9 @@ inline PlanePlan plane_plan(int64_t Ma, int64_t Nb, int64_t steps, int64_t batch
     }
     return best;
 }
-inline size_t plane_part_bytes(const PlanePlan& p, int64_t Ma, int64_t Nb, int64_t batches) {
-    return p.splits > 1 ? (size_t)batches * p.splits * Ma * Nb * sizeof(float) : 0;
+inline size_t plane_part_bytes(const PlanePlan& p, int64_t batches) {
+    const size_t side = kPlaneCost[0][p.shape].side;
+    return p.splits > 1 ? (size_t)batches * p.tiles * p.splits * side * side * sizeof(float) : 0;
 }
 
 template <class P, class S, int ALAY, int BLAY, int BOUND, class E>
@@ -73,29 +75,18 @@ void plane_launch(const PlaneArgs& g, const E& epi, const PlanePlan& p, int batc
         hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) == hipSuccess)
         allowed.fetch_or(bit, std::memory_order_relaxed);
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles, (unsigned)p.splits, (unsigned)batches), dim3(S::THREADS), S::LDS, s, g, epi);
-    if constexpr (!E::kWhole) {
-        if (p.splits > 1) {
-            if constexpr (E::kSymmetric) {
-                const int64_t side = g.Ma / 64;
-                hipLaunchKernelGGL((plane_join_half_kernel<E>), dim3((unsigned)(side * (side + 1) / 2), 1, (unsigned)batches), dim3(256), 0, s, g, epi);
-            } else {
-                const int lanes = p.splits >= 64 ? 16 : p.splits >= 16 ? 4 : 1;
-                const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)g.Ma * g.Nb / 4 * lanes, 256), 8192);
-                hipLaunchKernelGGL((plane_join_kernel<E>), dim3((unsigned)blocks, 1, (unsigned)batches), dim3(256), 0, s, g, lanes, epi);
-            }
-        }
-    }
 }
 
-// `p` is plane_plan's for the same sizes; `part` holds plane_part_bytes.
+// `p` is plane_plan's for the same sizes; `part` holds plane_part_bytes, `arrived` kMostParted numbers that are 0 and are left so.
 template <class P, int ALAY, int BLAY, int BOUND, class E>
-void plane_product(PlaneArgs g, const E& epi, const PlanePlan& p, int batches, float* part, hipStream_t s) {
+void plane_product(PlaneArgs g, const E& epi, const PlanePlan& p, int batches, float* part, int* arrived, hipStream_t s) {
     if (p.tiles == 0 || batches == 0) return;
     g.tiles_m = p.tiles_m;
     g.tiles_n = p.tiles_n;
     g.splits = p.splits;
     g.per = p.per;
     g.part = part;
+    g.arrived = arrived;
     if (p.shape == 0) plane_launch<P, PlaneLarge, ALAY, BLAY, BOUND, E>(g, epi, p, batches, s);
     else if (p.shape == 1) plane_launch<P, PlaneMiddle, ALAY, BLAY, BOUND, E>(g, epi, p, batches, s);
     else plane_launch<P, PlaneSmall, ALAY, BLAY, BOUND, E>(g, epi, p, batches, s);
