@@ -310,7 +310,7 @@ template <class P> struct GradOut : Logits<P> {
     const float* g;
     int first;
     uint16_t* dz;
-    long ldz;
+    long ldz, gz;
     // 16 rows at a time: a lane makes its numbers of one row, packed as they are in memory, and they leave by way of LDS in whole lines
     template <int MT, int NT>
     __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int, char* lds, int Ma, int Nb) const {
@@ -353,9 +353,9 @@ template <class P> struct GradOut : Logits<P> {
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int p = 0; p < CHUNKS / 4; ++p) {
-                const int k = p * 64 + lane, row = k / CHUNKS, at = k % CHUNKS, m = mw + i * 16 + row;
+                const int k = p * 64 + lane, row = k / CHUNKS, at = k % CHUNKS, m = mw + i * 16 + row, n = nw * P::N + at * 8;
                 const uint4 line = *reinterpret_cast<const uint4*>(lds + row * PITCH + at * 16);
-                if (m < Ma && nw < Nb) *reinterpret_cast<uint4*>(dz + (long)m * ldz + (long)nw * P::N + at * 8) = line;
+                if (m < Ma && nw < Nb) *reinterpret_cast<uint4*>(dz + (long)m * ldz + n / 64 * gz + n % 64) = line;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(256) void ce_rest_kernel(CeStats st, long rows, int
 
 // db: sums of dz's columns over parts of the rows, then over the parts
 template <class P>
-__global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t* __restrict__ dz, long ldz, int Nb, long per, float* __restrict__ part)
+__global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t* __restrict__ dz, long ldz, long gz, int Nb, long per, float* __restrict__ part)
 {
     __shared__ f32x4 red[4][64];
     const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4, k = threadIdx.x >> 6;
@@ -501,7 +501,7 @@ __global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t
     if (n < Nb)
         for (long m = r0 + k; m < r1; m += 4) {
             float x[4];
-            get_values<P, 4>(dz + m * ldz, n, x);
+            get_values<P, 4>(dz + m * ldz + n * P::N / 64 * gz, n % (64 / P::N), x);
 #pragma unroll
             for (int q = 0; q < 4; ++q) s[q] += x[q];
         }
@@ -630,7 +630,7 @@ CePlan ce_plan(int dtype, const CeShape& s) {
     p.piece = std::max<int64_t>(1024, kPieceBytes / std::max<int64_t>(1, p.Ma * 2 * N) / 256 * 256);
     if (p.piece >= s.V) p.piece = std::max<int64_t>(s.V, 1);
     const int64_t Pb = padded(p.piece);
-    p.dz_at = take((size_t)p.Ma * plane_pitch(Pb, N) * 2);
+    p.dz_at = take((size_t)p.Ma * Pb * 2 * N);
     p.dx_at = take(p.piece < s.V ? (size_t)p.Ma * p.D * 4 : 0);
     p.bias_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(s.rows, 64), std::max<int64_t>(1, 1024 / ceil_div(Pb, 256))));
     p.bias_at = take((size_t)p.bias_parts * Pb * 4);
@@ -706,6 +706,7 @@ template <class P> PlaneArgs logits_args(const CeCall& c, const uint16_t* w, lon
     PlaneArgs g{};
     g.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
     g.lda = plane_pitch(c.s.d, P::N);
+    g.ga = g.gb = 64;
     g.B = w + first * P::N;
     g.ldb = ldw;
     g.Ma = (int)c.p.Ma;
@@ -764,18 +765,24 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
     for (int64_t first = 0; first < c.s.V; first += c.p.piece) {
         const int64_t width = std::min(c.p.piece, c.s.V - first), Vb = padded(width);
         const PiecePlan q = piece_plan(c.p, width, P::STEP);
-        const long ldz = plane_pitch(Vb, P::N);
+        // dz lies in panels of 64 numbers of all rows: what a step reads of it is in one place.  (The distance of a panel's numbers has to
+        // be within 32 bits.)
+        const bool panels = c.p.Ma <= 1 << 21;
+        const long ldz = panels ? 64 : Vb * P::N, gz = panels ? c.p.Ma * 64 : 64;
         GradOut<P> grad{};
         fill(grad, c);
         grad.g = g;
         grad.first = (int)first;
         grad.dz = dz;
         grad.ldz = ldz;
+        grad.gz = gz;
         plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, first, width), grad, q.logits, 1, nullptr, nullptr, c.stream);
         if (dx && c.s.d > 0) {
             PlaneArgs a{};
             a.A = dz;
             a.lda = ldz;
+            a.ga = gz;
+            a.gb = 64;
             a.B = w + first * P::N;
             a.ldb = ldw;
             a.Ma = (int)c.p.Ma;
@@ -798,6 +805,8 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             a.lda = plane_pitch(c.s.d, P::N);
             a.B = dz;
             a.ldb = ldz;
+            a.ga = 64;
+            a.gb = gz;
             a.Ma = (int)c.p.D;
             a.Nb = (int)Vb;
             a.K = (int)c.p.Ma;
@@ -807,7 +816,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
         }
         if (db) {
             const int64_t per = ceil_div(c.s.rows, c.p.bias_parts);
-            hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, ldz,
+            hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, ldz, gz,
                                (int)Vb, (long)per, bias);
             hipLaunchKernelGGL((ce_bias_join_kernel<P>), dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
                                (int)width, maxes, db, c.param_dtype, (int)first);

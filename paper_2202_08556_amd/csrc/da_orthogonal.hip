@@ -354,6 +354,7 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
                        (long)ldg, (long)stride, (int)rows, (int)cols, (int)tall, norm, p.parts, eps, scales[0].X, X, ldx, bx);
     PlaneArgs gram{}, poly{}, step{};
     gram.lda = gram.ldb = step.ldb = ldx;
+    gram.ga = gram.gb = poly.ga = poly.gb = step.ga = step.gb = 64;
     gram.batch_a = gram.batch_b = step.batch_b = bx;
     poly.lda = poly.ldb = step.lda = lda;
     poly.batch_a = poly.batch_b = step.batch_a = ba;

@@ -32,7 +32,7 @@ __host__ __device__ inline long plane_pitch(long n, int N) {
 }
 
 struct One {
-    static constexpr int N = 1, STEP = 64;   // numbers of a value, inner positions of a step
+    static constexpr int N = 1, STEP = 64, PRODUCTS = 1;     // numbers of a value, inner positions of a step
     typedef bf16x8 Frag;
     static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -124,11 +124,11 @@ template <class P, int LAY, int OUTER> struct PlaneTile {
     }
 };
 
-// Operands of a product: lines of A go along or across the inner axis, lda numbers apart; Ma and Nb are the padded outer extents,
-// K the padded inner one.
+// Operands of a product: lines of A go along or across the inner axis, lda numbers apart, and the next 64 numbers of a line are
+// ga numbers further on (64, or all lines of a panel of 64); Ma and Nb are the padded outer extents, K the padded inner one.
 struct PlaneArgs {
     const uint16_t *A, *B;
-    long lda, ldb;
+    long lda, ldb, ga, gb;
     long batch_a, batch_b;       // numbers from one batch to the next
     int Ma, Nb, K;
     int tiles_m, tiles_n;
@@ -186,7 +186,8 @@ __device__ __forceinline__ void half_tile(int block, int tiles, int* bm, int* bn
 }
 
 // BM x BN results to a block of WM x WN waves, STAGES steps in LDS, asked for STAGES - 1 steps ahead.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_> struct PlaneShape {
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PIPED_> struct PlaneShape {
+    static constexpr bool PIPED = PIPED_;        // two steps' fragments in registers
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     static constexpr int THREADS = 64 * WM * WN, MT = BM / 16 / WM, NT = BN / 16 / WN;
     static constexpr int STAGE = (BM + BN) * 128, LDS = STAGES * STAGE;
@@ -232,7 +233,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         TA::piece(tid + THREADS * i, &line, &at);
         if constexpr (ALAY == kAlong) line = min(line, g.Ma - 1 - m0);
         else at = min(at, (g.Ma - m0) * P::N - 8);
-        aoff[i] = (unsigned)((long)line * g.lda + at) * 2;
+        aoff[i] = (unsigned)((long)line * g.lda + at / 64 * g.ga + at % 64) * 2;
     }
 #pragma unroll
     for (int i = 0; i < S::B_PIECES; ++i) {
@@ -240,12 +241,13 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         TB::piece(tid + THREADS * i, &line, &at);
         if constexpr (BLAY == kAlong) line = min(line, g.Nb - 1 - n0);
         else at = min(at, (g.Nb - n0) * P::N - 8);
-        boff[i] = (unsigned)((long)line * g.ldb + at) * 2;
+        boff[i] = (unsigned)((long)line * g.ldb + at / 64 * g.gb + at % 64) * 2;
     }
     auto fetch = [&](int t, int stage) {
+        static_assert(STEP * P::N == 64 && S::BM * P::N % 64 == 0 && S::BN * P::N % 64 == 0, "whole groups");
         const long k0 = (long)t * STEP;
-        const char* a = same_for_all(A + (ALAY == kAlong ? (long)m0 * g.lda + k0 * P::N : k0 * g.lda + (long)m0 * P::N) * 2);
-        const char* b = same_for_all(B + (BLAY == kAlong ? (long)n0 * g.ldb + k0 * P::N : k0 * g.ldb + (long)n0 * P::N) * 2);
+        const char* a = same_for_all(A + (ALAY == kAlong ? (long)m0 * g.lda + t * g.ga : k0 * g.lda + (long)(m0 * P::N / 64) * g.ga) * 2);
+        const char* b = same_for_all(B + (BLAY == kAlong ? (long)n0 * g.ldb + t * g.gb : k0 * g.ldb + (long)(n0 * P::N / 64) * g.gb) * 2);
         const unsigned to = lds_at + stage * S::STAGE + wave * 1024;
 #pragma unroll
         for (int i = 0; i < S::A_PIECES; ++i) line_to_lds(a, aoff[i], to + i * THREADS * 16);
@@ -259,63 +261,119 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    constexpr int AHEAD = S::STAGES - 1;
-    static_assert(AHEAD >= 1 && AHEAD <= 7 && (AHEAD - 1) * S::LOADS <= 63, "waits below");
+    typedef typename P::Frag Frag;
+    // The fragments of a step: s is inner positions 32 s and on, or which half
+    auto afrag = [&](const char* buf, int i, int s) { return TA::frag(buf, (wm * MT + i) * 16, s); };
+    auto bfrag = [&](const char* buf, int j, int s) { return TB::frag(buf + TA::BYTES, (wn * NT + j) * 16, s); };
+    // columns as the first operand: a lane's four results are neighbours in a row
+    auto all = [&](Frag (&x)[MT], Frag (&y)[NT]) {
 #pragma unroll
-    for (int s = 0; s < AHEAD; ++s)
-        if (t0 + s < t1) fetch(t0 + s, s);
-    int stage = 0, filled = AHEAD;
-    for (int t = t0; t < t1; ++t) {
-        const int left = t1 - 1 - t;
-        // the steps after this one may still be on their way
-        wait_for_steps<S::LOADS, AHEAD - 1>(left);
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (left >= AHEAD) {
-            fetch(t + AHEAD, filled);
-            filled = filled + 1 == S::STAGES ? 0 : filled + 1;
-        }
-        const char* buf = lds + stage * S::STAGE;
-        stage = stage + 1 == S::STAGES ? 0 : stage + 1;
-        auto afrag = [&](int i, int s) { return TA::frag(buf, (wm * MT + i) * 16, s); };
-        auto bfrag = [&](int j, int s) { return TB::frag(buf + TA::BYTES, (wn * NT + j) * 16, s); };
-        typename P::Frag a[MT], b[NT];
-        // columns as the first operand: a lane's four results are neighbours in a row
-        auto all = [&](typename P::Frag (&x)[MT], typename P::Frag (&y)[NT]) {
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(y[j], x[i], acc[i][j]);
+            for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(y[j], x[i], acc[i][j]);
+    };
+    const int steps_here = max(0, t1 - t0);
+    if constexpr (S::PIPED) {
+        // Fragments of the next step are read while those of this one are multiplied, so a step's place in LDS is free a step earlier.
+        struct Step {
+            Frag a[2][MT], b[2][NT];
         };
-        if constexpr (P::N == 1) {
+        auto read = [&](const char* buf, Step& f) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
+                if (P::N == 1 || s == 0 || P::PRODUCTS == 3)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) b[j] = bfrag(j, s);
+                    for (int j = 0; j < NT; ++j) f.b[s][j] = bfrag(buf, j, s);
+                if (P::N == 1 || s == 0 || P::PRODUCTS >= 2)
 #pragma unroll
-                for (int i = 0; i < MT; ++i) a[i] = afrag(i, s);
-                __builtin_amdgcn_sched_barrier(0);           // all reads are on their way before the first product
-                all(a, b);
+                    for (int i = 0; i < MT; ++i) f.a[s][i] = afrag(buf, i, s);
             }
-        } else {
-            typename P::Frag c[NT];
+        };
+        auto multiply = [&](Step& f) {
+            all(f.a[0], f.b[0]);
+            if constexpr (P::N == 1) {
+                all(f.a[1], f.b[1]);
+            } else {
+                if constexpr (P::PRODUCTS == 3) all(f.a[0], f.b[1]);
+                if constexpr (P::PRODUCTS >= 2) all(f.a[1], f.b[0]);
+            }
+        };
+        constexpr int STAGES = S::STAGES;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) b[j] = bfrag(j, 0);
+        for (int s = 0; s < STAGES; ++s)
+            if (s < steps_here) fetch(t0 + s, s);
+        Step one, two;
+        int stage = 0;                                       // of step t
+        auto next = [&](int at) { return at + 1 == STAGES ? 0 : at + 1; };
+        if (steps_here > 0) {
+            wait_for_steps<S::LOADS, STAGES - 1>(steps_here - 1);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            read(lds, one);
+        }
+        auto turn = [&](int t, Step& now, Step& then) {
+            if (t + 1 < steps_here) {
+                // the steps after the next may still be on their way; this step's fragments are in registers, everybody's behind the barrier
+                wait_for_steps<S::LOADS, STAGES - 2>(steps_here - 2 - t);
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                if (t + STAGES < steps_here) fetch(t0 + t + STAGES, stage);
+                stage = next(stage);
+                read(lds + stage * S::STAGE, then);
+            }
+            multiply(now);
+        };
+        for (int t = 0; t < steps_here; t += 2) {
+            turn(t, one, two);
+            if (t + 1 < steps_here) turn(t + 1, two, one);
+        }
+    } else {
+        constexpr int AHEAD = S::STAGES - 1;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) a[i] = afrag(i, 0);
-            if constexpr (P::PRODUCTS == 3)
+        for (int s = 0; s < AHEAD; ++s)
+            if (s < steps_here) fetch(t0 + s, s);
+        int stage = 0, filled = AHEAD;
+        for (int t = 0; t < steps_here; ++t) {
+            const int left = steps_here - 1 - t;
+            wait_for_steps<S::LOADS, AHEAD - 1>(left);       // the steps after this one may still be on their way
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (left >= AHEAD) {
+                fetch(t0 + t + AHEAD, filled);
+                filled = filled + 1 == S::STAGES ? 0 : filled + 1;
+            }
+            const char* buf = lds + stage * S::STAGE;
+            stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+            Frag a[MT], b[NT], c[NT];
+            if constexpr (P::N == 1) {
 #pragma unroll
-                for (int j = 0; j < NT; ++j) c[j] = bfrag(j, 1);
-            __builtin_amdgcn_sched_barrier(0);
-            all(a, b);
-            if constexpr (P::PRODUCTS == 3) all(a, c);
-            if constexpr (P::PRODUCTS >= 2)
+                for (int s = 0; s < 2; ++s) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const typename P::Frag second = afrag(i, 1);
+                    for (int j = 0; j < NT; ++j) b[j] = bfrag(buf, j, s);
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(b[j], second, acc[i][j]);
+                    for (int i = 0; i < MT; ++i) a[i] = afrag(buf, i, s);
+                    __builtin_amdgcn_sched_barrier(0);       // all reads are on their way before the first product
+                    all(a, b);
                 }
+            } else {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) b[j] = bfrag(buf, j, 0);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) a[i] = afrag(buf, i, 0);
+                if constexpr (P::PRODUCTS == 3)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) c[j] = bfrag(buf, j, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                all(a, b);
+                if constexpr (P::PRODUCTS == 3) all(a, c);
+                if constexpr (P::PRODUCTS >= 2)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        const Frag second = afrag(buf, i, 1);
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(b[j], second, acc[i][j]);
+                    }
+            }
         }
     }
     const int mw = m0 + wm * MT * 16, nw = n0 + wn * NT * 16, lane = tid & 63, i16 = lane & 15, h = lane >> 4;

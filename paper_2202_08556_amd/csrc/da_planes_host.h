@@ -9,9 +9,9 @@
 namespace daspmm {
 namespace {
 
-typedef PlaneShape<256, 256, 2, 4, 2> PlaneLarge;
-typedef PlaneShape<128, 128, 2, 2, 2> PlaneMiddle;
-typedef PlaneShape<64, 64, 2, 2, 4> PlaneSmall;
+typedef PlaneShape<256, 256, 2, 4, 2, false> PlaneLarge;
+typedef PlaneShape<128, 128, 2, 2, 2, true> PlaneMiddle;
+typedef PlaneShape<64, 64, 2, 2, 4, true> PlaneSmall;
 
 struct PlanePlan {
     int shape;                   // 0 large, 1 middle, 2 small
