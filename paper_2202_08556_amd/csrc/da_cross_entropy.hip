@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x
 template <class T, class P>
 __global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ from, long ld, long lines, int n, const int* __restrict__ index,
                                                       const int* __restrict__ count, const uint32_t* __restrict__ maxes, int which,
-                                                      uint16_t* __restrict__ to, long ldt)
+                                                      uint16_t* __restrict__ to, Packed lt)
 {
     const Scale s = scale_at<P>(maxes, which);
     const int pieces = (int)(padded(n) / 8);
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ from
         if constexpr (P::N == 2)
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] *= s.by;
-        put_values<P, 8>(to + line * ldt, at, x);
+        put_values<P, 8>(to + place<P>(lt, line, at), x);
     }
 }
 
@@ -310,7 +310,7 @@ template <class P> struct GradOut : Logits<P> {
     const float* g;
     int first;
     uint16_t* dz;
-    long ldz, gz;
+    Packed lz;
     // 16 rows at a time: a lane makes its numbers of one row, packed as they are in memory, and they leave by way of LDS in whole lines
     template <int MT, int NT>
     __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int, char* lds, int Ma, int Nb) const {
@@ -347,7 +347,7 @@ template <class P> struct GradOut : Logits<P> {
             for (int j = 0; j < NT; ++j) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) z[j][q] = there && (c.inside || n0 + j * 16 + 4 * h + q < this->classes) ? z[j][q] * by[i] : 0.f;
-                put_values<P, 4>(reinterpret_cast<uint16_t*>(lds + i16 * PITCH), j * 16 + 4 * h, z[j]);
+                put_values<P, 4>(in_line<P>(reinterpret_cast<uint16_t*>(lds + i16 * PITCH), j * 16 + 4 * h), z[j]);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");           // LDS serves a wave in order
             __builtin_amdgcn_wave_barrier();
@@ -355,7 +355,7 @@ template <class P> struct GradOut : Logits<P> {
             for (int p = 0; p < CHUNKS / 4; ++p) {
                 const int k = p * 64 + lane, row = k / CHUNKS, at = k % CHUNKS, m = mw + i * 16 + row, n = nw * P::N + at * 8;
                 const uint4 line = *reinterpret_cast<const uint4*>(lds + row * PITCH + at * 16);
-                if (m < Ma && nw < Nb) *reinterpret_cast<uint4*>(dz + (long)m * ldz + n / 64 * gz + n % 64) = line;
+                if (m < Ma && nw < Nb) *reinterpret_cast<uint4*>(dz + (long)m * lz.line + n / 64 * lz.group + n % 64) = line;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(256) void ce_rest_kernel(CeStats st, long rows, int
 
 // db: sums of dz's columns over parts of the rows, then over the parts
 template <class P>
-__global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t* __restrict__ dz, long ldz, long gz, int Nb, long per, float* __restrict__ part)
+__global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t* __restrict__ dz, Packed lz, int Nb, long per, float* __restrict__ part)
 {
     __shared__ f32x4 red[4][64];
     const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4, k = threadIdx.x >> 6;
@@ -501,7 +501,7 @@ __global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t
     if (n < Nb)
         for (long m = r0 + k; m < r1; m += 4) {
             float x[4];
-            get_values<P, 4>(dz + m * ldz + n * P::N / 64 * gz, n % (64 / P::N), x);
+            get_values<P, 4>(dz + place<P>(lz, m, n), x);
 #pragma unroll
             for (int q = 0; q < 4; ++q) s[q] += x[q];
         }
@@ -615,8 +615,8 @@ CePlan ce_plan(int dtype, const CeShape& s) {
         at += round16(bytes);
         return from;
     };
-    p.x_at = take((size_t)p.Ma * plane_pitch(s.d, N) * 2);
-    p.w_at = take((size_t)p.D * plane_pitch(s.V, N) * 2);
+    p.x_at = take((size_t)p.Ma * p.D * 2 * N);
+    p.w_at = take((size_t)p.D * p.Vb * 2 * N);
     const size_t both = at;
     p.counts_at = take((size_t)p.chunks * 4);
     p.sums_at = take(kJoinBlocks * sizeof(double));
@@ -666,7 +666,7 @@ struct CeCall {
     hipStream_t stream;
 };
 
-template <class T> const uint16_t* pack_operands(const CeCall& c, long* ldw) {
+template <class T> const uint16_t* pack_operands(const CeCall& c, Packed* lw) {
     typedef PlaneOf<T> P;
     uint32_t* maxes = reinterpret_cast<uint32_t*>(c.ws);
     const T* x = static_cast<const T*>(c.x);
@@ -680,16 +680,16 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, long* ldw) {
         const int64_t blocks = std::min<int64_t>(ceil_div(padded(lines) * (padded(n) / 8), 256), 8192);
         if (blocks)
             hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)blocks), dim3(256), 0, c.stream, from, ld, lines, n, index, c.st.count, maxes,
-                               which, reinterpret_cast<uint16_t*>(c.ws + to), plane_pitch(n, P::N));
+                               which, reinterpret_cast<uint16_t*>(c.ws + to), packed(padded(lines), n, P::N));
     };
     pack(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, kMaxX, c.p.x_at);
     // a weight of whole pads is read where it is
     if (P::N == 1 && c.s.d % kPad == 0 && c.s.V % kPad == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0) {
-        *ldw = c.s.V;
+        *lw = packed_lines(c.s.V);
         return reinterpret_cast<const uint16_t*>(w);
     }
     pack(w, c.s.V, c.s.d, (int)c.s.V, nullptr, kMaxW, c.p.w_at);
-    *ldw = plane_pitch(c.s.V, P::N);
+    *lw = packed(c.p.D, c.s.V, P::N);
     return reinterpret_cast<const uint16_t*>(c.ws + c.p.w_at);
 }
 
@@ -702,13 +702,12 @@ template <class P> void fill(Logits<P>& l, const CeCall& c) {
 }
 
 // Operands of the logits' product of the classes from `first` on
-template <class P> PlaneArgs logits_args(const CeCall& c, const uint16_t* w, long ldw, int64_t first, int64_t width) {
+template <class P> PlaneArgs logits_args(const CeCall& c, const uint16_t* w, const Packed& lw, int64_t first, int64_t width) {
     PlaneArgs g{};
     g.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
-    g.lda = plane_pitch(c.s.d, P::N);
-    g.ga = g.gb = 64;
-    g.B = w + first * P::N;
-    g.ldb = ldw;
+    g.a = packed(c.p.Ma, c.s.d, P::N);
+    g.B = w + place<P>(lw, 0, first);
+    g.b = lw;
     g.Ma = (int)c.p.Ma;
     g.Nb = (int)padded(width);
     g.K = (int)c.p.D;
@@ -727,14 +726,14 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
     float* rows = reduction == DA_LOSS_ROWS ? loss : nullptr;
     hipLaunchKernelGGL(ce_index_kernel, dim3((unsigned)c.p.chunks), dim3(256), 0, c.stream, target, target64, (long)c.s.rows, (long)c.s.V,
                        (long)c.p.chunk, several ? counts : nullptr, c.st, rows, reinterpret_cast<uint32_t*>(c.ws));
-    long ldw = 0;
-    const uint16_t* w = pack_operands<T>(c, &ldw);
+    Packed lw{};
+    const uint16_t* w = pack_operands<T>(c, &lw);
     SumsOut<P> out{};
     fill(out, c);
     out.part = reinterpret_cast<float2*>(c.ws + c.p.part_at);
     out.slots = c.p.slots;
     out.at_target = reinterpret_cast<float*>(c.ws + c.p.target_at);
-    plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, 0, c.s.V), out, c.p.logits, 1, nullptr, nullptr, c.stream);
+    plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, lw, 0, c.s.V), out, c.p.logits, 1, nullptr, nullptr, c.stream);
     int lanes = 1;
     while (lanes < 64 && lanes < c.p.slots) lanes *= 2;
     double* sums = reduction == DA_LOSS_ROWS ? nullptr : reinterpret_cast<double*>(c.ws + c.p.sums_at);
@@ -756,8 +755,8 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
         hipLaunchKernelGGL((ce_rest_kernel<T>), dim3((unsigned)std::min<int64_t>(ceil_div(c.s.rows, 4), 4096)), dim3(256), 0, c.stream, c.st,
                            (long)c.s.rows, (int)c.s.d, dx);
     if (c.s.V == 0) return;
-    long ldw = 0;
-    const uint16_t* w = pack_operands<T>(c, &ldw);
+    Packed lw{};
+    const uint16_t* w = pack_operands<T>(c, &lw);
     uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + c.p.dz_at);
     float* acc = reinterpret_cast<float*>(c.ws + c.p.dx_at);
     float* part = reinterpret_cast<float*>(c.ws + c.p.sum_at);
@@ -765,26 +764,20 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
     for (int64_t first = 0; first < c.s.V; first += c.p.piece) {
         const int64_t width = std::min(c.p.piece, c.s.V - first), Vb = padded(width);
         const PiecePlan q = piece_plan(c.p, width, P::STEP);
-        // dz lies in panels of 64 numbers of all rows: what a step reads of it is in one place.  (The distance of a panel's numbers has to
-        // be within 32 bits.)
-        const bool panels = c.p.Ma <= 1 << 21;
-        const long ldz = panels ? 64 : Vb * P::N, gz = panels ? c.p.Ma * 64 : 64;
+        const Packed lz = packed(c.p.Ma, width, P::N);
         GradOut<P> grad{};
         fill(grad, c);
         grad.g = g;
         grad.first = (int)first;
         grad.dz = dz;
-        grad.ldz = ldz;
-        grad.gz = gz;
-        plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, ldw, first, width), grad, q.logits, 1, nullptr, nullptr, c.stream);
+        grad.lz = lz;
+        plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, lw, first, width), grad, q.logits, 1, nullptr, nullptr, c.stream);
         if (dx && c.s.d > 0) {
             PlaneArgs a{};
             a.A = dz;
-            a.lda = ldz;
-            a.ga = gz;
-            a.gb = 64;
-            a.B = w + first * P::N;
-            a.ldb = ldw;
+            a.a = lz;
+            a.B = w + place<P>(lw, 0, first);
+            a.b = lw;
             a.Ma = (int)c.p.Ma;
             a.Nb = (int)c.p.D;
             a.K = (int)Vb;
@@ -802,11 +795,9 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
         if (dw && c.s.d > 0) {
             PlaneArgs a{};
             a.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
-            a.lda = plane_pitch(c.s.d, P::N);
+            a.a = packed(c.p.Ma, c.s.d, P::N);
             a.B = dz;
-            a.ldb = ldz;
-            a.ga = 64;
-            a.gb = gz;
+            a.b = lz;
             a.Ma = (int)c.p.D;
             a.Nb = (int)Vb;
             a.K = (int)c.p.Ma;
@@ -816,7 +807,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
         }
         if (db) {
             const int64_t per = ceil_div(c.s.rows, c.p.bias_parts);
-            hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, ldz, gz,
+            hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, lz,
                                (int)Vb, (long)per, bias);
             hipLaunchKernelGGL((ce_bias_join_kernel<P>), dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
                                (int)width, maxes, db, c.param_dtype, (int)first);

@@ -99,10 +99,10 @@ __global__ __launch_bounds__(kSmallThreads) void orth_small_kernel(const T* __re
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float one[1] = {y[i]};
-                if (c + i < a.cols) put_values<Halves, 1>(reinterpret_cast<uint16_t*>(X + (c + i) * PX), r, one);
+                if (c + i < a.cols) put_values<Halves, 1>(in_line<Halves>(reinterpret_cast<uint16_t*>(X + (c + i) * PX), r), one);
             }
         } else {
-            put_values<Halves, 4>(reinterpret_cast<uint16_t*>(X + r * PX), c, y);
+            put_values<Halves, 4>(in_line<Halves>(reinterpret_cast<uint16_t*>(X + r * PX), c), y);
         }
     });
     __syncthreads();
@@ -130,21 +130,21 @@ __global__ __launch_bounds__(kSmallThreads) void orth_small_kernel(const T* __re
         }
         return acc[0] + (acc[1] + acc[2]);
     };
-    uint16_t* const line = reinterpret_cast<uint16_t*>(A + (m + i16) * PA);
+    uint16_t* const mine = in_line<Halves>(reinterpret_cast<uint16_t*>(A + (m + i16) * PA), j + 4 * h);
     for (int k = 0; k < a.steps; ++k) {
         const SmallStep& t = a.step[k];
         f32x4 acc = square(X, PX, n);
         float v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = t.gram * acc[q];
-        put_values<Halves, 4>(line, j + 4 * h, v);
+        put_values<Halves, 4>(mine, v);
         __syncthreads();
         acc = square(A, PA, kSmallSide);
-        get_values<Halves, 4>(line, j + 4 * h, v);
+        get_values<Halves, 4>(mine, v);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = t.poly_b * v[q] + t.poly_c * acc[q];
         __syncthreads();                                     // A has been read
-        put_values<Halves, 4>(line, j + 4 * h, v);
+        put_values<Halves, 4>(mine, v);
         __syncthreads();
         f16x8 b[4][2][2];                                    // rows, inner positions, halves
 #pragma unroll
@@ -167,12 +167,12 @@ __global__ __launch_bounds__(kSmallThreads) void orth_small_kernel(const T* __re
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                uint16_t* const to = reinterpret_cast<uint16_t*>(X + (r * 16 + i16) * PX);
+                uint16_t* const to = in_line<Halves>(reinterpret_cast<uint16_t*>(X + (r * 16 + i16) * PX), c + 4 * h);
                 float x[4];
-                get_values<Halves, 4>(to, c + 4 * h, x);
+                get_values<Halves, 4>(to, x);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) x[q] = t.a * x[q] + t.by * sum[r][q];
-                put_values<Halves, 4>(to, c + 4 * h, x);
+                put_values<Halves, 4>(to, x);
             }
         }
         __syncthreads();
@@ -184,11 +184,11 @@ __global__ __launch_bounds__(kSmallThreads) void orth_small_kernel(const T* __re
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float one[1];
-                get_values<Halves, 1>(reinterpret_cast<const uint16_t*>(X + (c + i) * PX), r, one);      // lines up to 63 are there
+                get_values<Halves, 1>(in_line<Halves>(reinterpret_cast<const uint16_t*>(X + (c + i) * PX), r), one);      // lines up to 63 are there
                 y[i] = one[0];
             }
         } else {
-            get_values<Halves, 4>(reinterpret_cast<const uint16_t*>(X + r * PX), c, y);
+            get_values<Halves, 4>(in_line<Halves>(reinterpret_cast<const uint16_t*>(X + r * PX), c), y);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] *= a.last;

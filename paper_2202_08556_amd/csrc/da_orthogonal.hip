@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(const T* __restrict__ g,
 template <class T>
 __global__ __launch_bounds__(256) void orth_pack_kernel(const T* __restrict__ g, long ldg, long stride, int rows, int cols, int tall,
                                                         const double* __restrict__ part, int parts, float eps, float scale,
-                                                        uint16_t* __restrict__ X, long ldx, long batch_x)
+                                                        uint16_t* __restrict__ X, Packed lx, long batch_x)
 {
     __shared__ float tile[64][65];
     __shared__ double by;
@@ -112,13 +112,13 @@ __global__ __launch_bounds__(256) void orth_pack_kernel(const T* __restrict__ g,
         float x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = tall ? tile[at + i][line] : tile[line][at + i];
-        put_values<Halves, 4>(out + (long)(blockIdx.y * 64 + line) * ldx, blockIdx.x * 64 + at, x);
+        put_values<Halves, 4>(out + place<Halves>(lx, blockIdx.y * 64 + line, blockIdx.x * 64 + at), x);
     }
 }
 
 // The result of a tall matrix: X^T / scale
 template <class T>
-__global__ __launch_bounds__(256) void orth_turn_kernel(const uint16_t* __restrict__ X, long ldx, long batch_x, int rows, int cols, float inv,
+__global__ __launch_bounds__(256) void orth_turn_kernel(const uint16_t* __restrict__ X, Packed lx, long batch_x, int rows, int cols, float inv,
                                                         T* __restrict__ out)
 {
     __shared__ float tile[64][65];
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256) void orth_turn_kernel(const uint16_t* __restri
     for (int k = tid; k < 1024; k += 256) {
         const int line = k / 16, at = k % 16 * 4;
         float x[4];
-        get_values<Halves, 4>(in + (long)(blockIdx.y * 64 + line) * ldx, blockIdx.x * 64 + at, x);
+        get_values<Halves, 4>(in + place<Halves>(lx, blockIdx.y * 64 + line, blockIdx.x * 64 + at), x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) tile[line][at + i] = x[i] * inv;
     }
@@ -144,12 +144,13 @@ __global__ __launch_bounds__(256) void orth_turn_kernel(const uint16_t* __restri
 struct GramOut {
     static constexpr bool kSymmetric = true, kWhole = false;
     uint16_t* A;
-    long lda, batch_a;
+    Packed la;
+    long batch_a;
     float by;                    // of the product to A's scale
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] *= by;
-        put_values<Halves, 4>(A + batch * batch_a + (long)m * lda, n, x);
+        put_values<Halves, 4>(A + batch * batch_a + place<Halves>(la, m, n), x);
     }
 };
 // b A + c A^2
@@ -158,10 +159,10 @@ struct PolyOut : GramOut {
     float b, c;                  // with the scales
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
         float a[4];
-        get_values<Halves, 4>(from + batch * batch_a + (long)m * lda, n, a);
+        get_values<Halves, 4>(from + batch * batch_a + place<Halves>(la, m, n), a);
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] = b * a[q] + c * x[q];
-        put_values<Halves, 4>(A + batch * batch_a + (long)m * lda, n, x);
+        put_values<Halves, 4>(A + batch * batch_a + place<Halves>(la, m, n), x);
     }
 };
 // a X + (b A + c A^2) X, packed
@@ -169,17 +170,18 @@ struct StepOut {
     static constexpr bool kSymmetric = false, kWhole = false;
     const uint16_t* from;
     uint16_t* to;
-    long ldx, batch_x;
+    Packed lx;
+    long batch_x;
     float a, by;                 // with the scales
     __device__ __forceinline__ void value(int m, int n, float (&x)[4], int batch) const {
         float old[4];
-        get_values<Halves, 4>(from + batch * batch_x + (long)m * ldx, n, old);
+        get_values<Halves, 4>(from + batch * batch_x + place<Halves>(lx, m, n), old);
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] = a * old[q] + by * x[q];
     }
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
         value(m, n, x, batch);
-        put_values<Halves, 4>(to + batch * batch_x + (long)m * ldx, n, x);
+        put_values<Halves, 4>(to + batch * batch_x + place<Halves>(lx, m, n), x);
     }
 };
 // ... as the result
@@ -253,8 +255,8 @@ OrthPlan orth_plan(int64_t batch, int64_t rows, int64_t cols) {
     p.gram = plane_plan(p.Ma, p.Ma, p.Nb / step, batch, true, true, 1);
     p.poly = plane_plan(p.Ma, p.Ma, p.Ma / step, batch, true, true, 1);
     p.step = plane_plan(p.Ma, p.Nb, p.Ma / step, batch, false, true, 1);
-    p.X = (size_t)batch * p.Ma * plane_pitch(p.Nb, 2) * 2;
-    p.A = (size_t)batch * p.Ma * plane_pitch(p.Ma, 2) * 2;
+    p.X = (size_t)batch * p.Ma * p.Nb * 4;
+    p.A = (size_t)batch * p.Ma * p.Ma * 4;
     p.part = std::max({plane_part_bytes(p.gram, batch), plane_part_bytes(p.poly, batch), plane_part_bytes(p.step, batch)});
     return p;
 }
@@ -349,14 +351,14 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
                            dim3(256), 0, s, g, (long)ldg, (long)stride, (long)rows, (long)cols, norm, p.parts, eps, out);
         return;
     }
-    const long ldx = plane_pitch(p.Nb, 2), lda = plane_pitch(p.Ma, 2), bx = p.Ma * ldx, ba = p.Ma * lda;
+    const Packed lx = packed(p.Ma, p.Nb, 2), la = packed(p.Ma, p.Ma, 2);
+    const long bx = p.Ma * p.Nb * 2, ba = p.Ma * p.Ma * 2;
     hipLaunchKernelGGL((orth_pack_kernel<T>), dim3((unsigned)(p.Nb / 64), (unsigned)(p.Ma / 64), (unsigned)batch), dim3(256), 0, s, g,
-                       (long)ldg, (long)stride, (int)rows, (int)cols, (int)tall, norm, p.parts, eps, scales[0].X, X, ldx, bx);
+                       (long)ldg, (long)stride, (int)rows, (int)cols, (int)tall, norm, p.parts, eps, scales[0].X, X, lx, bx);
     PlaneArgs gram{}, poly{}, step{};
-    gram.lda = gram.ldb = step.ldb = ldx;
-    gram.ga = gram.gb = poly.ga = poly.gb = step.ga = step.gb = 64;
+    gram.a = gram.b = step.b = lx;
     gram.batch_a = gram.batch_b = step.batch_b = bx;
-    poly.lda = poly.ldb = step.lda = lda;
+    poly.a = poly.b = step.a = la;
     poly.batch_a = poly.batch_b = step.batch_a = ba;
     gram.Ma = gram.Nb = poly.Ma = poly.Nb = poly.K = step.Ma = step.K = (int)p.Ma;
     gram.K = step.Nb = (int)p.Nb;
@@ -370,7 +372,7 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
         gram.A = gram.B = step.B = X;
         GramOut first{};
         first.A = A;
-        first.lda = lda;
+        first.la = la;
         first.batch_a = ba;
         first.by = sa / (sx * sx);
         plane_product<S, kAlong, kAlong, kBoundNone>(gram, first, p.gram, (int)batch, part, arrived, s);
@@ -383,7 +385,7 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
         plane_product<S, kAlong, kAlong, kBoundNone>(poly, second, p.poly, (int)batch, part, arrived, s);
         const bool last = k + 1 == steps && !tall;
         const float to = last ? 1.f : scales[k + 1].X;
-        const StepOut third{X, Y, ldx, bx, c[3 * k] * to / sx, to / (sb * sx)};
+        const StepOut third{X, Y, lx, bx, c[3 * k] * to / sx, to / (sb * sx)};
         if (last) {
             LastOut<T> l{};
             static_cast<StepOut&>(l) = third;
@@ -402,7 +404,7 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
         else one_step(k, Halves(), HalvesBy<2>());
     }
     if (tall)
-        hipLaunchKernelGGL((orth_turn_kernel<T>), dim3((unsigned)(p.Nb / 64), (unsigned)(p.Ma / 64), (unsigned)batch), dim3(256), 0, s, X, ldx,
+        hipLaunchKernelGGL((orth_turn_kernel<T>), dim3((unsigned)(p.Nb / 64), (unsigned)(p.Ma / 64), (unsigned)batch), dim3(256), 0, s, X, lx,
                            bx, (int)rows, (int)cols, 1.f / scales[steps].X, out);
 }
 

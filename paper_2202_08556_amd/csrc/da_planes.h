@@ -24,11 +24,16 @@ enum { kAlong = 0, kAcross = 1 };            // a line of memory goes along the 
 constexpr int kPad = 64;
 __host__ __device__ inline long padded(long n) { return (n + kPad - 1) / kPad * kPad; }
 
-// Numbers from one line to the next of n values of N numbers each: lines whose distance is a multiple of 4 KB meet in few places of the
-// caches (4096 x 65536 . 65536 x 2048: 1133 us, and 1 line of 128 bytes further apart ONE_LINE)
-__host__ __device__ inline long plane_pitch(long n, int N) {
-    const long numbers = padded(n) * N;
-    return numbers % 2048 == 0 ? numbers + 64 : numbers;
+// Where a packed matrix' numbers are: from a line to the next, and from 64 numbers of a line to the next 64.  Panels of 64 numbers of
+// all lines have what a step reads along the lines in one place (4096 x 65536 . 65536 x 2048 bf16, lines of the first operand
+// 128 KB apart and in panels: 1149 and 885 us).  The distance of a tile's numbers has to be within 32 bits: more than 2^21 lines lie
+// one after the other.
+struct Packed {
+    long line, group;
+};
+__host__ __device__ inline Packed packed_lines(long numbers) { return {numbers, 64}; }
+__host__ __device__ inline Packed packed(long lines, long n, int N) {
+    return lines <= 1 << 21 ? Packed{64, lines * 64} : packed_lines(padded(n) * N);
 }
 
 struct One {
@@ -47,14 +52,20 @@ template <int PRODUCTS_> struct HalvesBy {   // 3: all; 2: both halves of the le
 };
 typedef HalvesBy<3> Halves;
 
-// V neighbouring values of a packed line from position `at` (a multiple of V) on
-template <class P, int V> __device__ __forceinline__ void put_values(uint16_t* line, long at, const float (&x)[V]) {
+// Value `at` of a packed line
+template <class P> __host__ __device__ __forceinline__ long place(const Packed& l, long line, long at) {
+    return line * l.line + at / (64 / P::N) * l.group + at % (64 / P::N);
+}
+template <class P, class T> __device__ __forceinline__ T* in_line(T* line, long at) { return line + at / (64 / P::N) * 64 + at % (64 / P::N); }
+
+// V neighbouring values whose place is a multiple of V
+template <class P, int V> __device__ __forceinline__ void put_values(uint16_t* to, const float (&x)[V]) {
     typedef uint16_t Bits __attribute__((ext_vector_type(V)));
     if constexpr (P::N == 1) {
         Bits b;
 #pragma unroll
         for (int i = 0; i < V; ++i) b[i] = __builtin_bit_cast(uint16_t, (bf16)x[i]);
-        *reinterpret_cast<Bits*>(line + at) = b;
+        *reinterpret_cast<Bits*>(to) = b;
     } else {
         Bits first, second;
 #pragma unroll
@@ -64,20 +75,18 @@ template <class P, int V> __device__ __forceinline__ void put_values(uint16_t* l
             first[i] = __builtin_bit_cast(uint16_t, h);
             second[i] = __builtin_bit_cast(uint16_t, (_Float16)(rest == rest ? rest : 0.f));
         }
-        uint16_t* p = line + at / 32 * 64 + at % 32;
-        *reinterpret_cast<Bits*>(p) = first;
-        *reinterpret_cast<Bits*>(p + 32) = second;
+        *reinterpret_cast<Bits*>(to) = first;
+        *reinterpret_cast<Bits*>(to + 32) = second;
     }
 }
-template <class P, int V> __device__ __forceinline__ void get_values(const uint16_t* line, long at, float (&x)[V]) {
+template <class P, int V> __device__ __forceinline__ void get_values(const uint16_t* from, float (&x)[V]) {
     typedef uint16_t Bits __attribute__((ext_vector_type(V)));
     if constexpr (P::N == 1) {
-        const Bits b = *reinterpret_cast<const Bits*>(line + at);
+        const Bits b = *reinterpret_cast<const Bits*>(from);
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = __uint_as_float((uint32_t)b[i] << 16);
     } else {
-        const uint16_t* p = line + at / 32 * 64 + at % 32;
-        const Bits first = *reinterpret_cast<const Bits*>(p), second = *reinterpret_cast<const Bits*>(p + 32);
+        const Bits first = *reinterpret_cast<const Bits*>(from), second = *reinterpret_cast<const Bits*>(from + 32);
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)first[i]) + (float)__builtin_bit_cast(_Float16, (uint16_t)second[i]);
     }
@@ -124,11 +133,11 @@ template <class P, int LAY, int OUTER> struct PlaneTile {
     }
 };
 
-// Operands of a product: lines of A go along or across the inner axis, lda numbers apart, and the next 64 numbers of a line are
-// ga numbers further on (64, or all lines of a panel of 64); Ma and Nb are the padded outer extents, K the padded inner one.
+// Operands of a product: lines of A and B go along or across the inner axis; Ma and Nb are the padded outer extents, K the padded
+// inner one.
 struct PlaneArgs {
     const uint16_t *A, *B;
-    long lda, ldb, ga, gb;
+    Packed a, b;
     long batch_a, batch_b;       // numbers from one batch to the next
     int Ma, Nb, K;
     int tiles_m, tiles_n;
@@ -233,7 +242,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         TA::piece(tid + THREADS * i, &line, &at);
         if constexpr (ALAY == kAlong) line = min(line, g.Ma - 1 - m0);
         else at = min(at, (g.Ma - m0) * P::N - 8);
-        aoff[i] = (unsigned)((long)line * g.lda + at / 64 * g.ga + at % 64) * 2;
+        aoff[i] = (unsigned)((long)line * g.a.line + at / 64 * g.a.group + at % 64) * 2;
     }
 #pragma unroll
     for (int i = 0; i < S::B_PIECES; ++i) {
@@ -241,13 +250,13 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         TB::piece(tid + THREADS * i, &line, &at);
         if constexpr (BLAY == kAlong) line = min(line, g.Nb - 1 - n0);
         else at = min(at, (g.Nb - n0) * P::N - 8);
-        boff[i] = (unsigned)((long)line * g.ldb + at / 64 * g.gb + at % 64) * 2;
+        boff[i] = (unsigned)((long)line * g.b.line + at / 64 * g.b.group + at % 64) * 2;
     }
     auto fetch = [&](int t, int stage) {
         static_assert(STEP * P::N == 64 && S::BM * P::N % 64 == 0 && S::BN * P::N % 64 == 0, "whole groups");
         const long k0 = (long)t * STEP;
-        const char* a = same_for_all(A + (ALAY == kAlong ? (long)m0 * g.lda + t * g.ga : k0 * g.lda + (long)(m0 * P::N / 64) * g.ga) * 2);
-        const char* b = same_for_all(B + (BLAY == kAlong ? (long)n0 * g.ldb + t * g.gb : k0 * g.ldb + (long)(n0 * P::N / 64) * g.gb) * 2);
+        const char* a = same_for_all(A + (ALAY == kAlong ? (long)m0 * g.a.line + t * g.a.group : k0 * g.a.line + (long)(m0 * P::N / 64) * g.a.group) * 2);
+        const char* b = same_for_all(B + (BLAY == kAlong ? (long)n0 * g.b.line + t * g.b.group : k0 * g.b.line + (long)(n0 * P::N / 64) * g.b.group) * 2);
         const unsigned to = lds_at + stage * S::STAGE + wave * 1024;
 #pragma unroll
         for (int i = 0; i < S::A_PIECES; ++i) line_to_lds(a, aoff[i], to + i * THREADS * 16);
