@@ -41,7 +41,7 @@ CeStats ce_stats(void* p, int64_t rows) {
 }
 
 // Largest magnitudes of x, w and dz's factors, as bits; scale: the power of two that takes them to 2^14 .. 2^15
-enum { kMaxX = 0, kMaxW = 1, kMaxG = 2, kMaxes = 4 };
+enum { kMaxX = 0, kMaxW = 1, kMaxG = 2, kArrived = 3, kMaxes = 4 };      // kArrived: a count of blocks
 struct Scale {
     float by, inv;
 };
@@ -58,13 +58,25 @@ template <class P> __device__ __forceinline__ Scale scale_at(const uint32_t* max
     return scale_of(maxes[which]);
 }
 
-__device__ __forceinline__ long target_of(const void* t, int wide, long r) {
-    return wide ? static_cast<const int64_t*>(t)[r] : (long)static_cast<const int32_t*>(t)[r];
+// The gradient of the loss: of the rows, g, or one factor for all of them
+struct Upstream {
+    const float *dloss, *g;
+    int reduction;
+    const int* count;
+    __device__ __forceinline__ float all() const { return reduction == DA_LOSS_MEAN ? dloss[0] / (float)max(1, *count) : dloss[0]; }
+    __device__ __forceinline__ float row(int m) const { return reduction == DA_LOSS_ROWS ? g[m] : all(); }
+};
+__device__ __forceinline__ float magnitude(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.f;                   // infinities and NaN have no part in a scale
+}
+template <class P> __device__ __forceinline__ Scale scale_of_gradient(const uint32_t* maxes, const Upstream& u) {
+    if constexpr (P::N == 1) return {1.f, 1.f};
+    return scale_of(u.reduction == DA_LOSS_ROWS ? maxes[kMaxG] : __float_as_uint(magnitude(u.all())));
 }
 
-__global__ void ce_zero_kernel(uint32_t* maxes, int* arrived) {
-    if (threadIdx.x < kMaxes) maxes[threadIdx.x] = 0;
-    for (int k = threadIdx.x; k < kMostParted; k += 256) arrived[k] = 0;
+__device__ __forceinline__ long target_of(const void* t, int wide, long r) {
+    return wide ? static_cast<const int64_t*>(t)[r] : (long)static_cast<const int32_t*>(t)[r];
 }
 
 // Rows of a chunk that have a target
@@ -135,11 +147,6 @@ __device__ __forceinline__ void keep_largest(float most, uint32_t* to) {
         if (most > 0.f) atomicMax(to, __float_as_uint(most));
     }
 }
-__device__ __forceinline__ float magnitude(float x) {
-    const float a = fabsf(x);
-    return a <= 3.402823466e38f ? a : 0.f;                   // infinities and NaN have no part in a scale
-}
-
 // Largest finite magnitudes: blockIdx.y 0 of the rows of x that count, 1 of w
 __global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x, long ldx, CeStats st, long d, const float* __restrict__ w,
                                                      long numbers, uint32_t* __restrict__ maxes)
@@ -172,16 +179,23 @@ __global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x
     keep_largest(most, maxes + (blockIdx.y == 0 ? kMaxX : kMaxW));
 }
 
-// Packs `lines` lines of n numbers (index: those of a list, of which *count are there, and zeros up to the next multiple of 64),
-// 8 numbers at a time; lines and their ends are padded with zeros.
+// Packs lines of numbers, 8 numbers at a time; lines and their ends are padded with zeros.
+template <class T> struct PackJob {
+    const T* from;
+    long ld, lines;
+    int n;
+    const int *index, *count;    // not null: *count lines of a list, and zeros up to the next multiple of 64
+    int which;
+    uint16_t* to;
+    Packed layout;
+};
 template <class T, class P>
-__global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ from, long ld, long lines, int n, const int* __restrict__ index,
-                                                      const int* __restrict__ count, const uint32_t* __restrict__ maxes, int which,
-                                                      uint16_t* __restrict__ to, Packed lt)
+__global__ __launch_bounds__(256) void ce_pack_kernel(PackJob<T> x, PackJob<T> w, const uint32_t* __restrict__ maxes)
 {
-    const Scale s = scale_at<P>(maxes, which);
-    const int pieces = (int)(padded(n) / 8);
-    const long there = index ? *count : lines, all = padded(there) * pieces;
+    const PackJob<T>& j = blockIdx.y ? w : x;
+    const Scale s = scale_at<P>(maxes, j.which);
+    const int pieces = (int)(padded(j.n) / 8);
+    const long there = j.index ? *j.count : j.lines, all = padded(there) * pieces;
     for (long k = (long)blockIdx.x * 256 + threadIdx.x; k < all; k += (long)gridDim.x * 256) {
         const long line = k / pieces;
         const int at = (int)(k % pieces) * 8;
@@ -189,13 +203,13 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ from
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = 0.f;
         if (line < there) {
-            const T* __restrict__ p = from + (index ? (long)index[line] : line) * ld + at;
-            if (at + 8 <= n) {
+            const T* __restrict__ p = j.from + (j.index ? (long)j.index[line] : line) * j.ld + at;
+            if (at + 8 <= j.n) {
                 load_floats<8>(p, x);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (at + i < n) {
+                    if (at + i < j.n) {
                         float one[1];
                         load_floats<1>(p + i, one);
                         x[i] = one[0];
@@ -205,7 +219,7 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ from
         if constexpr (P::N == 2)
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] *= s.by;
-        put_values<P, 8>(to + place<P>(lt, line, at), x);
+        put_values<P, 8>(j.to + place<P>(j.layout, line, at), x);
     }
 }
 
@@ -307,7 +321,7 @@ template <class P> struct SumsOut : Logits<P> {
 // dz of a piece of the classes that begins at `first`; rows behind the last one are 0
 template <class P> struct GradOut : Logits<P> {
     static constexpr bool kSymmetric = false, kWhole = true;
-    const float* g;
+    Upstream u;
     int first;
     uint16_t* dz;
     Packed lz;
@@ -317,7 +331,7 @@ template <class P> struct GradOut : Logits<P> {
         constexpr int BYTES = NT * 32 * P::N, PITCH = BYTES + 16, CHUNKS = BYTES / 16;
         const int lane = threadIdx.x & 63, i16 = lane & 15, h = lane >> 4, count = *this->st.count, n0 = first + nw;
         const auto c = this->template columns<NT>(n0);
-        const float up = scale_at<P>(this->maxes, kMaxG).by;
+        const float up = scale_of_gradient<P>(this->maxes, u).by;
         float lse[MT], by[MT];
         int t[MT];
 #pragma unroll
@@ -325,7 +339,7 @@ template <class P> struct GradOut : Logits<P> {
             const int m = mw + i * 16 + i16;
             const bool there = m < count;
             lse[i] = there ? this->st.lse[m] : 0.f;
-            by[i] = there ? g[m] * up : 0.f;
+            by[i] = there ? u.row(m) * up : 0.f;
             t[i] = (there ? this->st.target[m] : -0x40000000) - n0 - 4 * h;
         }
 #pragma unroll
@@ -379,6 +393,7 @@ template <class T> __device__ __forceinline__ void store_row(T* p, int left, con
 template <class T, class P> struct InputOut {
     static constexpr bool kSymmetric = false, kWhole = false;
     const uint32_t* maxes;
+    Upstream u;
     CeStats st;
     const float* before;         // dense rows x ldb, packed rows
     float* after;                // where not null: the sum goes here instead of to dx
@@ -387,7 +402,7 @@ template <class T, class P> struct InputOut {
     int d;
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
         if (m >= *st.count || n >= d) return;
-        const Scale sg = scale_at<P>(maxes, kMaxG), sw = scale_at<P>(maxes, kMaxW);
+        const Scale sg = scale_of_gradient<P>(maxes, u), sw = scale_at<P>(maxes, kMaxW);
         if constexpr (P::N == 2)
 #pragma unroll
             for (int q = 0; q < 4; ++q) x[q] = x[q] * sw.inv * sg.inv;
@@ -405,12 +420,13 @@ template <class T, class P> struct InputOut {
 template <class T, class P> struct WeightOut {
     static constexpr bool kSymmetric = false, kWhole = false;
     const uint32_t* maxes;
+    Upstream u;
     T* dw;                       // of the piece
     long ldw;
     int d, classes;              // of the piece
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
         if (m >= d || n >= classes) return;
-        const Scale sg = scale_at<P>(maxes, kMaxG), sx = scale_at<P>(maxes, kMaxX);
+        const Scale sg = scale_of_gradient<P>(maxes, u), sx = scale_at<P>(maxes, kMaxX);
         if constexpr (P::N == 2)
 #pragma unroll
             for (int q = 0; q < 4; ++q) x[q] = x[q] * sx.inv * sg.inv;
@@ -421,9 +437,10 @@ template <class T, class P> struct WeightOut {
 // ------------------------------------------------------------------------------------------
 // Rows
 // ------------------------------------------------------------------------------------------
-// log sum exp and loss of the rows, P lanes to one; with sums, those of the blocks' losses
+// log sum exp and loss of the rows, P lanes to one; with sums, the loss of all of them
 __global__ __launch_bounds__(256) void ce_join_kernel(CeStats st, const float2* __restrict__ part, int slots, int P,
-                                                      const float* __restrict__ at_target, float* __restrict__ loss, double* __restrict__ sums)
+                                                      const float* __restrict__ at_target, float* __restrict__ loss, uint64_t* __restrict__ sums,
+                                                      uint32_t* __restrict__ arrived, int mean, float* __restrict__ loss_all)
 {
     __shared__ double red[4];
     const int lane = threadIdx.x & (P - 1), count = *st.count, teams = 256 / P;
@@ -444,42 +461,53 @@ __global__ __launch_bounds__(256) void ce_join_kernel(CeStats st, const float2* 
         }
     }
     if (!sums) return;
-    total = wave_sum(total, 64);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = total;
-    __syncthreads();
-    if (threadIdx.x == 0) sums[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
-}
-__global__ __launch_bounds__(256) void ce_total_kernel(CeStats st, const double* __restrict__ sums, int blocks, int mean, float* loss)
-{
-    __shared__ double red[4];
-    double s = 0.0;
-    for (int k = threadIdx.x; k < blocks; k += 256) s += sums[k];
-    s = wave_sum(s, 64);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-    __syncthreads();
+    // the block that comes last adds the blocks' sums, in their order
+    auto block_sum = [&](double v) {
+        v = wave_sum(v, 64);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        return (red[0] + red[1]) + (red[2] + red[3]);
+    };
+    total = block_sum(total);
+    __shared__ int last;
     if (threadIdx.x == 0) {
-        s = (red[0] + red[1]) + (red[2] + red[3]);
-        *loss = (float)(mean ? s / max(1, *st.count) : s);
+        __hip_atomic_store(sums + blockIdx.x, __builtin_bit_cast(uint64_t, total), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
     }
+    __syncthreads();
+    if (!last) return;
+    total = 0.0;
+    for (int k = threadIdx.x; k < (int)gridDim.x; k += 256)
+        total += __builtin_bit_cast(double, __hip_atomic_load(sums + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    total = block_sum(total);
+    if (threadIdx.x == 0) *loss_all = (float)(mean ? total / max(1, count) : total);
 }
 
-// The factor of each row's gradient, and the largest of them
-__global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, long rows, const float* __restrict__ dloss, long stride, int reduction,
-                                                        float* __restrict__ g, uint32_t* __restrict__ maxes)
+// The factors of the rows' gradients, and the largest of them
+__global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, const float* __restrict__ dloss, long stride, float* __restrict__ g,
+                                                        uint32_t* __restrict__ maxes)
 {
     const int count = *st.count;
     float most = 0.f;
     for (long m = (long)blockIdx.x * 256 + threadIdx.x; m < count; m += (long)gridDim.x * 256) {
-        const float v = reduction == DA_LOSS_ROWS ? dloss[st.index[m] * stride] : reduction == DA_LOSS_MEAN ? dloss[0] / (float)count : dloss[0];
+        const float v = dloss[st.index[m] * stride];
         g[m] = v;
         most = fmaxf(most, magnitude(v));
     }
     keep_largest(most, maxes + kMaxG);
 }
-// Rows of dx without a target
+// What a backward pass begins with: no magnitudes and no parts yet, and 0 in the rows of dx without a target
 template <class T>
-__global__ __launch_bounds__(256) void ce_rest_kernel(CeStats st, long rows, int d, T* __restrict__ dx)
+__global__ __launch_bounds__(256) void ce_begin_kernel(CeStats st, long rows, int d, T* __restrict__ dx, uint32_t* __restrict__ maxes,
+                                                       int* __restrict__ arrived)
 {
+    if (blockIdx.x == 0) {
+        if (threadIdx.x < kMaxes) maxes[threadIdx.x] = 0;
+        for (int k = threadIdx.x; k < kMostParted; k += 256) arrived[k] = 0;
+    }
+    if (!dx) return;
     const int lane = threadIdx.x & 63;
     for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (long)gridDim.x * 4) {
         if (st.place[r] >= 0) continue;
@@ -514,7 +542,7 @@ __global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t
 }
 template <class P>
 __global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restrict__ part, int parts, int Nb, int classes,
-                                                           const uint32_t* __restrict__ maxes, void* db, int type, int first)
+                                                           const uint32_t* __restrict__ maxes, Upstream u, void* db, int type, int first)
 {
     __shared__ float red[16][17];
     const int n = blockIdx.x * 16 + (threadIdx.x & 15), k0 = threadIdx.x >> 4;
@@ -531,7 +559,7 @@ __global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restri
     if (threadIdx.x < 16 && n < classes) {
         float t = 0.f;
         for (int i = 0; i < 16; ++i) t += red[i][threadIdx.x];
-        store_param(db, type, first + n, t * scale_at<P>(maxes, kMaxG).inv);
+        store_param(db, type, first + n, t * scale_of_gradient<P>(maxes, u).inv);
     }
 }
 
@@ -569,6 +597,16 @@ NarrowPlan narrow_plan(const CeShape& s, bool backward) {
     return p;
 }
 
+struct PiecePlan {
+    PlanePlan logits, input, weight;
+};
+PiecePlan piece_plan(int64_t Ma, int64_t D, int64_t width, int step) {
+    const int64_t Vb = padded(width);
+    const int halves = step == Halves::STEP;
+    return {plane_plan(Ma, Vb, D / step, 1, false, false, halves), plane_plan(Ma, D, Vb / step, 1, false, true, halves),
+            plane_plan(D, Vb, Ma / step, 1, false, true, halves)};
+}
+
 struct CePlan {
     NarrowPlan narrow, narrow_back;
     int64_t Ma, D, Vb;           // rows, d and classes, padded
@@ -576,6 +614,7 @@ struct CePlan {
     PlanePlan logits;
     int slots;
     int64_t piece;               // classes of a piece, a multiple of 64 where there are several
+    PiecePlan whole, rest;       // products of a whole piece and of the last one
     int bias_parts;
     size_t counts_at, sums_at, target_at, x_at, w_at, part_at, forward;          // bytes
     size_t g_at, arrived_at, dz_at, dx_at, bias_at, sum_at, backward;
@@ -583,16 +622,7 @@ struct CePlan {
 
 int wave_columns(const PlanePlan& p) { return p.shape == 0 ? PlaneLarge::WN : PlaneSmall::WN; }
 
-struct PiecePlan {
-    PlanePlan logits, input, weight;
-};
-PiecePlan piece_plan(const CePlan& p, int64_t width, int step) {
-    const int64_t Vb = padded(width);
-    return {plane_plan(p.Ma, Vb, p.D / step, 1, false, false, step == Halves::STEP), plane_plan(p.Ma, p.D, Vb / step, 1, false, true, step == Halves::STEP),
-            plane_plan(p.D, Vb, p.Ma / step, 1, false, true, step == Halves::STEP)};
-}
-
-CePlan ce_plan(int dtype, const CeShape& s) {
+CePlan make_ce_plan(int dtype, const CeShape& s) {
     CePlan p{};
     const int N = dtype == DA_F32 ? 2 : 1, step = N == 2 ? Halves::STEP : One::STEP;
     p.Ma = padded(s.rows);
@@ -635,14 +665,30 @@ CePlan ce_plan(int dtype, const CeShape& s) {
     p.bias_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(s.rows, 64), std::max<int64_t>(1, 1024 / ceil_div(Pb, 256))));
     p.bias_at = take((size_t)p.bias_parts * Pb * 4);
     size_t sums = 0;
-    for (const int64_t width : {p.piece, s.V % p.piece})
-        if (width > 0) {
-            const PiecePlan q = piece_plan(p, width, step);
-            sums = std::max({sums, plane_part_bytes(q.input, 1), plane_part_bytes(q.weight, 1)});
-        }
+    p.whole = piece_plan(p.Ma, p.D, p.piece, step);
+    p.rest = s.V % p.piece ? piece_plan(p.Ma, p.D, s.V % p.piece, step) : p.whole;
+    for (const PiecePlan& q : {p.whole, p.rest}) sums = std::max({sums, plane_part_bytes(q.input, 1), plane_part_bytes(q.weight, 1)});
     p.sum_at = take(sums);
     p.backward = at;
     return p;
+}
+
+// A call asks for its plan twice, and a program for the same one in every step
+const CePlan& ce_plan(int dtype, const CeShape& s) {
+    struct Last {
+        int dtype = -1, units = 0;
+        CeShape s{};
+        CePlan p{};
+    };
+    thread_local Last last;
+    const int units = compute_units();
+    if (last.dtype != dtype || last.units != units || last.s.rows != s.rows || last.s.d != s.d || last.s.V != s.V) {
+        last.p = make_ce_plan(dtype, s);
+        last.s = s;
+        last.units = units;
+        last.dtype = dtype;
+    }
+    return last.p;
 }
 
 int ce_check(int dtype, int64_t rows, int64_t d, int64_t classes) {
@@ -676,21 +722,18 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, Packed* lw) {
         hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 512)), 2), dim3(256), 0, c.stream, x,
                            (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V), maxes);
     }
-    auto pack = [&](const T* from, long ld, long lines, int n, const int* index, int which, size_t to) {
-        const int64_t blocks = std::min<int64_t>(ceil_div(padded(lines) * (padded(n) / 8), 256), 8192);
-        if (blocks)
-            hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)blocks), dim3(256), 0, c.stream, from, ld, lines, n, index, c.st.count, maxes,
-                               which, reinterpret_cast<uint16_t*>(c.ws + to), packed(padded(lines), n, P::N));
+    auto job = [&](const T* from, long ld, long lines, int n, const int* index, int which, size_t to) {
+        return PackJob<T>{from, ld, lines, n, index, c.st.count, which, reinterpret_cast<uint16_t*>(c.ws + to), packed(padded(lines), n, P::N)};
     };
-    pack(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, kMaxX, c.p.x_at);
+    const PackJob<T> jx = job(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, kMaxX, c.p.x_at), jw = job(w, c.s.V, c.s.d, (int)c.s.V, nullptr, kMaxW, c.p.w_at);
     // a weight of whole pads is read where it is
-    if (P::N == 1 && c.s.d % kPad == 0 && c.s.V % kPad == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0) {
-        *lw = packed_lines(c.s.V);
-        return reinterpret_cast<const uint16_t*>(w);
-    }
-    pack(w, c.s.V, c.s.d, (int)c.s.V, nullptr, kMaxW, c.p.w_at);
-    *lw = packed(c.p.D, c.s.V, P::N);
-    return reinterpret_cast<const uint16_t*>(c.ws + c.p.w_at);
+    const bool direct = P::N == 1 && c.s.d % kPad == 0 && c.s.V % kPad == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
+    const int64_t eights = std::max(c.p.Ma * (c.p.D / 8), direct ? 0 : c.p.D * (c.p.Vb / 8));
+    if (eights)
+        hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::min<int64_t>(ceil_div(eights, 256), 8192), direct ? 1 : 2), dim3(256), 0,
+                           c.stream, jx, jw, maxes);
+    *lw = direct ? packed_lines(c.s.V) : jw.layout;
+    return direct ? reinterpret_cast<const uint16_t*>(w) : jw.to;
 }
 
 template <class P> void fill(Logits<P>& l, const CeCall& c) {
@@ -736,10 +779,10 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
     plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, lw, 0, c.s.V), out, c.p.logits, 1, nullptr, nullptr, c.stream);
     int lanes = 1;
     while (lanes < 64 && lanes < c.p.slots) lanes *= 2;
-    double* sums = reduction == DA_LOSS_ROWS ? nullptr : reinterpret_cast<double*>(c.ws + c.p.sums_at);
+    uint64_t* sums = reduction == DA_LOSS_ROWS ? nullptr : reinterpret_cast<uint64_t*>(c.ws + c.p.sums_at);
     const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256 / lanes), kJoinBlocks));
-    hipLaunchKernelGGL(ce_join_kernel, dim3(blocks), dim3(256), 0, c.stream, c.st, out.part, c.p.slots, lanes, out.at_target, rows, sums);
-    if (sums) hipLaunchKernelGGL(ce_total_kernel, dim3(1), dim3(256), 0, c.stream, c.st, sums, blocks, (int)(reduction == DA_LOSS_MEAN), loss);
+    hipLaunchKernelGGL(ce_join_kernel, dim3(blocks), dim3(256), 0, c.stream, c.st, out.part, c.p.slots, lanes, out.at_target, rows, sums,
+                       reinterpret_cast<uint32_t*>(c.ws) + kArrived, (int)(reduction == DA_LOSS_MEAN), loss);
 }
 
 template <class T>
@@ -748,12 +791,13 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
     uint32_t* maxes = reinterpret_cast<uint32_t*>(c.ws);
     float* g = reinterpret_cast<float*>(c.ws + c.p.g_at);
     int* arrived = reinterpret_cast<int*>(c.ws + c.p.arrived_at);
-    hipLaunchKernelGGL(ce_zero_kernel, dim3(1), dim3(256), 0, c.stream, maxes, arrived);
-    hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 256))), dim3(256), 0,
-                       c.stream, c.st, (long)c.s.rows, dloss, (long)stride, reduction, g, maxes);
-    if (dx && c.s.d > 0 && c.s.rows > 0)
-        hipLaunchKernelGGL((ce_rest_kernel<T>), dim3((unsigned)std::min<int64_t>(ceil_div(c.s.rows, 4), 4096)), dim3(256), 0, c.stream, c.st,
-                           (long)c.s.rows, (int)c.s.d, dx);
+    const Upstream u{dloss, g, reduction, c.st.count};
+    if (c.s.d == 0) dx = dw = nullptr;
+    hipLaunchKernelGGL((ce_begin_kernel<T>), dim3((unsigned)(dx ? std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 4), 4096)) : 1)), dim3(256), 0,
+                       c.stream, c.st, (long)c.s.rows, (int)c.s.d, dx, maxes, arrived);
+    if (reduction == DA_LOSS_ROWS)
+        hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 256))), dim3(256), 0,
+                           c.stream, c.st, dloss, (long)stride, g, maxes);
     if (c.s.V == 0) return;
     Packed lw{};
     const uint16_t* w = pack_operands<T>(c, &lw);
@@ -763,16 +807,16 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
     float* bias = reinterpret_cast<float*>(c.ws + c.p.bias_at);
     for (int64_t first = 0; first < c.s.V; first += c.p.piece) {
         const int64_t width = std::min(c.p.piece, c.s.V - first), Vb = padded(width);
-        const PiecePlan q = piece_plan(c.p, width, P::STEP);
+        const PiecePlan& q = width == c.p.piece ? c.p.whole : c.p.rest;
         const Packed lz = packed(c.p.Ma, width, P::N);
         GradOut<P> grad{};
         fill(grad, c);
-        grad.g = g;
+        grad.u = u;
         grad.first = (int)first;
         grad.dz = dz;
         grad.lz = lz;
         plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, lw, first, width), grad, q.logits, 1, nullptr, nullptr, c.stream);
-        if (dx && c.s.d > 0) {
+        if (dx) {
             PlaneArgs a{};
             a.A = dz;
             a.a = lz;
@@ -784,6 +828,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             a.rows = c.st.count;
             InputOut<T, P> out{};
             out.maxes = maxes;
+            out.u = u;
             out.st = c.st;
             out.before = first > 0 ? acc : nullptr;
             out.after = first + width < c.s.V ? acc : nullptr;
@@ -792,7 +837,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             out.d = (int)c.s.d;
             plane_product<P, kAlong, kAlong, kBoundM>(a, out, q.input, 1, part, arrived, c.stream);
         }
-        if (dw && c.s.d > 0) {
+        if (dw) {
             PlaneArgs a{};
             a.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
             a.a = packed(c.p.Ma, c.s.d, P::N);
@@ -802,7 +847,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             a.Nb = (int)Vb;
             a.K = (int)c.p.Ma;
             a.rows = c.st.count;
-            const WeightOut<T, P> out{maxes, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
+            const WeightOut<T, P> out{maxes, u, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
             plane_product<P, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, arrived, c.stream);
         }
         if (db) {
@@ -810,7 +855,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, lz,
                                (int)Vb, (long)per, bias);
             hipLaunchKernelGGL((ce_bias_join_kernel<P>), dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
-                               (int)width, maxes, db, c.param_dtype, (int)first);
+                               (int)width, maxes, u, db, c.param_dtype, (int)first);
         }
     }
 }
@@ -920,7 +965,7 @@ extern "C" int da_linear_cross_entropy_sizes(int dtype, int64_t rows, int64_t d,
     if (!stats || !forward_bytes || !backward_bytes) return fail(DA_ERR_INVALID_ARG, "null output");
     const int st = ce_check(dtype, rows, d, classes);
     if (st != DA_OK) return st;
-    const CePlan p = ce_plan(dtype, CeShape{rows, d, classes});
+    const CePlan& p = ce_plan(dtype, CeShape{rows, d, classes});
     *stats = stats_bytes(rows);
     *forward_bytes = p.forward;
     *backward_bytes = p.backward;

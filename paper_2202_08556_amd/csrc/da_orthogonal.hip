@@ -243,7 +243,7 @@ struct OrthPlan {
     size_t parts_bytes;
 };
 
-OrthPlan orth_plan(int64_t batch, int64_t rows, int64_t cols) {
+OrthPlan make_orth_plan(int64_t batch, int64_t rows, int64_t cols) {
     OrthPlan p{};
     p.m = std::min(rows, cols);
     p.n = std::max(rows, cols);
@@ -259,6 +259,25 @@ OrthPlan orth_plan(int64_t batch, int64_t rows, int64_t cols) {
     p.A = (size_t)batch * p.Ma * p.Ma * 4;
     p.part = std::max({plane_part_bytes(p.gram, batch), plane_part_bytes(p.poly, batch), plane_part_bytes(p.step, batch)});
     return p;
+}
+
+// A call asks for its plan twice, and a program for the same one in every step
+const OrthPlan& orth_plan(int64_t batch, int64_t rows, int64_t cols) {
+    struct Last {
+        int units = 0;
+        int64_t batch = -1, rows = 0, cols = 0;
+        OrthPlan p{};
+    };
+    thread_local Last last;
+    const int units = compute_units();
+    if (last.units != units || last.batch != batch || last.rows != rows || last.cols != cols) {
+        last.p = make_orth_plan(batch, rows, cols);
+        last.batch = batch;
+        last.rows = rows;
+        last.cols = cols;
+        last.units = units;
+    }
+    return last.p;
 }
 
 int orth_check(int dtype, int64_t batch, int64_t rows, int64_t cols, int steps) {
@@ -418,8 +437,12 @@ extern "C" int da_orthogonalise_workspace(int dtype, int64_t batch, int64_t rows
     if (!bytes) return fail(DA_ERR_INVALID_ARG, "null output");
     const int st = orth_check(dtype, batch, rows, cols, steps);
     if (st != DA_OK) return st;
-    const OrthPlan p = orth_plan(batch, rows, cols);
-    *bytes = small_takes(rows, cols) ? 0 : steps == 0 ? round16(p.parts_bytes) : p.bytes();
+    if (small_takes(rows, cols)) {
+        *bytes = 0;
+        return DA_OK;
+    }
+    const OrthPlan& p = orth_plan(batch, rows, cols);
+    *bytes = steps == 0 ? round16(p.parts_bytes) : p.bytes();
     return DA_OK;
 }
 
@@ -438,7 +461,7 @@ extern "C" int da_orthogonalise(int dtype, int64_t batch, int64_t rows, int64_t 
     if (!g || !out) return fail(DA_ERR_INVALID_ARG, "null g or out");
     if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
         return fail(DA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than reported");
-    const OrthPlan p = orth_plan(batch, rows, cols);
+    const OrthPlan p = small_takes(rows, cols) ? OrthPlan{} : orth_plan(batch, rows, cols);
     char* ws = static_cast<char*>(workspace);
     if (dtype == DA_F32)
         orthogonalise<float>(batch, rows, cols, static_cast<const float*>(g), ldg, stride, steps, coefficients, eps, static_cast<float*>(out), ws, p,
