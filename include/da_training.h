@@ -57,7 +57,7 @@ int da_rms_norm_backward(int dtype, int64_t rows, int64_t channels, const void *
  *   loss      float32[rows] (DA_LOSS_ROWS), or one number: the sum over the rows, or that over the number of rows with a
  *             target (DA_LOSS_MEAN; 0 where there is none)
  *   stats     written by the forward call and read by the backward call on the same arguments (which rows have a target,
- *             and their log sum exp); da_linear_cross_entropy_sizes says how many bytes
+ *             their log sum exp, the magnitudes of x and w), 16-byte aligned; da_linear_cross_entropy_sizes says how many bytes
  *   dloss     float32, like loss; dloss_stride (DA_LOSS_ROWS) 0 takes dloss[0] for every row
  *   dx, dw, db   dense, of the types of x, w and b; any of them may be NULL and is then not computed
  *

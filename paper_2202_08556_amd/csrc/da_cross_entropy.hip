@@ -26,22 +26,25 @@ constexpr float kLog2e = 1.44269504088896f;
 
 template <class T> using PlaneOf = std::conditional_t<std::is_same_v<T, float>, Halves, One>;
 
-// What a backward pass reads, and how far the arrays behind it are from its start
+// What a backward pass reads
 struct CeStats {
     int *count, *index, *target;             // rows that have a target: how many, which, and which class
     int* place;                              // of every row in that list; -1: not there
     float* lse;
+    uint32_t* maxes;                         // kMaxX and so on
 };
-size_t stats_bytes(int64_t rows) { return 16 + 4 * round16((size_t)rows * 4); }
+constexpr size_t kStatsHead = 32;
+size_t stats_bytes(int64_t rows) { return kStatsHead + 4 * round16((size_t)rows * 4); }
 CeStats ce_stats(void* p, int64_t rows) {
     char* c = static_cast<char*>(p);
     const size_t n = round16((size_t)rows * 4);
     auto ints = [&](size_t at) { return reinterpret_cast<int*>(c + at); };
-    return {ints(0), ints(16), ints(16 + n), ints(16 + 2 * n), reinterpret_cast<float*>(c + 16 + 3 * n)};
+    return {ints(0), ints(kStatsHead), ints(kStatsHead + n), ints(kStatsHead + 2 * n), reinterpret_cast<float*>(c + kStatsHead + 3 * n),
+            reinterpret_cast<uint32_t*>(c + 16)};
 }
 
-// Largest magnitudes of x, w and dz's factors, as bits; scale: the power of two that takes them to 2^14 .. 2^15
-enum { kMaxX = 0, kMaxW = 1, kMaxG = 2, kArrived = 3, kMaxes = 4 };      // kArrived: a count of blocks
+// Largest magnitudes of x and w, as bits, and a count of blocks; scale: the power of two that takes them to 2^14 .. 2^15
+enum { kMaxX = 0, kMaxW = 1, kArrived = 2, kMaxes = 4 };
 struct Scale {
     float by, inv;
 };
@@ -61,6 +64,7 @@ template <class P> __device__ __forceinline__ Scale scale_at(const uint32_t* max
 // The gradient of the loss: of the rows, g, or one factor for all of them
 struct Upstream {
     const float *dloss, *g;
+    const uint32_t* largest;     // of the rows' factors
     int reduction;
     const int* count;
     __device__ __forceinline__ float all() const { return reduction == DA_LOSS_MEAN ? dloss[0] / (float)max(1, *count) : dloss[0]; }
@@ -70,9 +74,9 @@ __device__ __forceinline__ float magnitude(float x) {
     const float a = fabsf(x);
     return a <= 3.402823466e38f ? a : 0.f;                   // infinities and NaN have no part in a scale
 }
-template <class P> __device__ __forceinline__ Scale scale_of_gradient(const uint32_t* maxes, const Upstream& u) {
+template <class P> __device__ __forceinline__ Scale scale_of_gradient(const Upstream& u) {
     if constexpr (P::N == 1) return {1.f, 1.f};
-    return scale_of(u.reduction == DA_LOSS_ROWS ? maxes[kMaxG] : __float_as_uint(magnitude(u.all())));
+    return scale_of(u.reduction == DA_LOSS_ROWS ? *u.largest : __float_as_uint(magnitude(u.all())));
 }
 
 __device__ __forceinline__ long target_of(const void* t, int wide, long r) {
@@ -98,8 +102,7 @@ __global__ __launch_bounds__(256) void ce_count_kernel(const void* __restrict__ 
 
 // Lists them in order; the others' losses are 0.  counts: of the chunks, where there are several
 __global__ __launch_bounds__(256) void ce_index_kernel(const void* __restrict__ target, int wide, long rows, long classes, long chunk,
-                                                       const int* __restrict__ counts, CeStats st, float* __restrict__ loss,
-                                                       uint32_t* __restrict__ maxes)
+                                                       const int* __restrict__ counts, CeStats st, float* __restrict__ loss)
 {
     __shared__ int red[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(256) void ce_index_kernel(const void* __restrict__ 
         __syncthreads();
         before = red[0] + red[1] + red[2] + red[3];
     }
-    if (blockIdx.x == 0 && tid < kMaxes) maxes[tid] = 0;
+    if (blockIdx.x == 0 && tid < kMaxes) st.maxes[tid] = 0;
     const long r0 = blockIdx.x * chunk, r1 = min(r0 + chunk, rows);
     for (long r = r0 + tid; r - tid < r1; r += 256) {
         const long t = r < r1 ? target_of(target, wide, r) : -1;
@@ -149,7 +152,7 @@ __device__ __forceinline__ void keep_largest(float most, uint32_t* to) {
 }
 // Largest finite magnitudes: blockIdx.y 0 of the rows of x that count, 1 of w
 __global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x, long ldx, CeStats st, long d, const float* __restrict__ w,
-                                                     long numbers, uint32_t* __restrict__ maxes)
+                                                     long numbers)
 {
     float most = 0.f;
     if (blockIdx.y == 0) {
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x
             }
         }
     }
-    keep_largest(most, maxes + (blockIdx.y == 0 ? kMaxX : kMaxW));
+    keep_largest(most, st.maxes + (blockIdx.y == 0 ? kMaxX : kMaxW));
 }
 
 // Packs lines of numbers, 8 numbers at a time; lines and their ends are padded with zeros.
@@ -227,7 +230,6 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(PackJob<T> x, PackJob<T> w
 // Epilogues
 // ------------------------------------------------------------------------------------------
 template <class P> struct Logits {
-    const uint32_t* maxes;
     const void* bias;
     int bias_type;
     int classes;
@@ -241,8 +243,8 @@ template <class P> struct Logits {
     };
     template <int NT> __device__ __forceinline__ Columns<NT> columns(int nw) const {
         Columns<NT> c;
-        c.sx = scale_at<P>(maxes, kMaxX);
-        c.sw = scale_at<P>(maxes, kMaxW);
+        c.sx = scale_at<P>(st.maxes, kMaxX);
+        c.sw = scale_at<P>(st.maxes, kMaxW);
         c.inside = nw + NT * 16 <= classes;
         const int n = nw + 4 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
@@ -331,7 +333,7 @@ template <class P> struct GradOut : Logits<P> {
         constexpr int BYTES = NT * 32 * P::N, PITCH = BYTES + 16, CHUNKS = BYTES / 16;
         const int lane = threadIdx.x & 63, i16 = lane & 15, h = lane >> 4, count = *this->st.count, n0 = first + nw;
         const auto c = this->template columns<NT>(n0);
-        const float up = scale_of_gradient<P>(this->maxes, u).by;
+        const float up = scale_of_gradient<P>(u).by;
         float lse[MT], by[MT];
         int t[MT];
 #pragma unroll
@@ -392,7 +394,6 @@ template <class T> __device__ __forceinline__ void store_row(T* p, int left, con
 // dx, or what the pieces so far give of it
 template <class T, class P> struct InputOut {
     static constexpr bool kSymmetric = false, kWhole = false;
-    const uint32_t* maxes;
     Upstream u;
     CeStats st;
     const float* before;         // dense rows x ldb, packed rows
@@ -402,7 +403,7 @@ template <class T, class P> struct InputOut {
     int d;
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
         if (m >= *st.count || n >= d) return;
-        const Scale sg = scale_of_gradient<P>(maxes, u), sw = scale_at<P>(maxes, kMaxW);
+        const Scale sg = scale_of_gradient<P>(u), sw = scale_at<P>(st.maxes, kMaxW);
         if constexpr (P::N == 2)
 #pragma unroll
             for (int q = 0; q < 4; ++q) x[q] = x[q] * sw.inv * sg.inv;
@@ -426,7 +427,7 @@ template <class T, class P> struct WeightOut {
     int d, classes;              // of the piece
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
         if (m >= d || n >= classes) return;
-        const Scale sg = scale_of_gradient<P>(maxes, u), sx = scale_at<P>(maxes, kMaxX);
+        const Scale sg = scale_of_gradient<P>(u), sx = scale_at<P>(maxes, kMaxX);
         if constexpr (P::N == 2)
 #pragma unroll
             for (int q = 0; q < 4; ++q) x[q] = x[q] * sx.inv * sg.inv;
@@ -487,7 +488,7 @@ __global__ __launch_bounds__(256) void ce_join_kernel(CeStats st, const float2* 
 
 // The factors of the rows' gradients, and the largest of them
 __global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, const float* __restrict__ dloss, long stride, float* __restrict__ g,
-                                                        uint32_t* __restrict__ maxes)
+                                                        uint32_t* __restrict__ largest)
 {
     const int count = *st.count;
     float most = 0.f;
@@ -496,15 +497,15 @@ __global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, const float*
         g[m] = v;
         most = fmaxf(most, magnitude(v));
     }
-    keep_largest(most, maxes + kMaxG);
+    keep_largest(most, largest);
 }
-// What a backward pass begins with: no magnitudes and no parts yet, and 0 in the rows of dx without a target
+// What a backward pass begins with: no magnitude and no parts yet, and 0 in the rows of dx without a target
 template <class T>
-__global__ __launch_bounds__(256) void ce_begin_kernel(CeStats st, long rows, int d, T* __restrict__ dx, uint32_t* __restrict__ maxes,
+__global__ __launch_bounds__(256) void ce_begin_kernel(CeStats st, long rows, int d, T* __restrict__ dx, uint32_t* __restrict__ largest,
                                                        int* __restrict__ arrived)
 {
     if (blockIdx.x == 0) {
-        if (threadIdx.x < kMaxes) maxes[threadIdx.x] = 0;
+        if (threadIdx.x == 0) *largest = 0;
         for (int k = threadIdx.x; k < kMostParted; k += 256) arrived[k] = 0;
     }
     if (!dx) return;
@@ -542,7 +543,7 @@ __global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t
 }
 template <class P>
 __global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restrict__ part, int parts, int Nb, int classes,
-                                                           const uint32_t* __restrict__ maxes, Upstream u, void* db, int type, int first)
+                                                           Upstream u, void* db, int type, int first)
 {
     __shared__ float red[16][17];
     const int n = blockIdx.x * 16 + (threadIdx.x & 15), k0 = threadIdx.x >> 4;
@@ -559,7 +560,7 @@ __global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restri
     if (threadIdx.x < 16 && n < classes) {
         float t = 0.f;
         for (int i = 0; i < 16; ++i) t += red[i][threadIdx.x];
-        store_param(db, type, first + n, t * scale_of_gradient<P>(maxes, u).inv);
+        store_param(db, type, first + n, t * scale_of_gradient<P>(u).inv);
     }
 }
 
@@ -639,7 +640,7 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
         p.backward = 16 + round16((size_t)p.narrow_back.blocks * (s.d + 1) * s.V * sizeof(float));
         return p;
     }
-    size_t at = 16;                                          // the largest magnitudes
+    size_t at = 16;                                          // the largest factor of a row
     auto take = [&](size_t bytes) {
         const size_t from = at;
         at += round16(bytes);
@@ -712,15 +713,16 @@ struct CeCall {
     hipStream_t stream;
 };
 
-template <class T> const uint16_t* pack_operands(const CeCall& c, Packed* lw) {
+template <class T> const uint16_t* pack_operands(const CeCall& c, bool forward, Packed* lw) {
     typedef PlaneOf<T> P;
-    uint32_t* maxes = reinterpret_cast<uint32_t*>(c.ws);
     const T* x = static_cast<const T*>(c.x);
     const T* w = static_cast<const T*>(c.w);
     if constexpr (P::N == 2) {
-        const int64_t most = std::max(ceil_div(c.s.rows, 4), ceil_div(c.s.d * c.s.V, 4096));
-        hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 512)), 2), dim3(256), 0, c.stream, x,
-                           (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V), maxes);
+        if (forward) {                                       // kept for the backward pass
+            const int64_t most = std::max(ceil_div(c.s.rows, 4), ceil_div(c.s.d * c.s.V, 4096));
+            hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 512)), 2), dim3(256), 0, c.stream, x,
+                               (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V));
+        }
     }
     auto job = [&](const T* from, long ld, long lines, int n, const int* index, int which, size_t to) {
         return PackJob<T>{from, ld, lines, n, index, c.st.count, which, reinterpret_cast<uint16_t*>(c.ws + to), packed(padded(lines), n, P::N)};
@@ -731,13 +733,12 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, Packed* lw) {
     const int64_t eights = std::max(c.p.Ma * (c.p.D / 8), direct ? 0 : c.p.D * (c.p.Vb / 8));
     if (eights)
         hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::min<int64_t>(ceil_div(eights, 256), 8192), direct ? 1 : 2), dim3(256), 0,
-                           c.stream, jx, jw, maxes);
+                           c.stream, jx, jw, c.st.maxes);
     *lw = direct ? packed_lines(c.s.V) : jw.layout;
     return direct ? reinterpret_cast<const uint16_t*>(w) : jw.to;
 }
 
 template <class P> void fill(Logits<P>& l, const CeCall& c) {
-    l.maxes = reinterpret_cast<const uint32_t*>(c.ws);
     l.bias = c.b;
     l.bias_type = c.param_dtype;
     l.classes = (int)c.s.V;
@@ -768,9 +769,9 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
                            (long)c.p.chunk, counts);
     float* rows = reduction == DA_LOSS_ROWS ? loss : nullptr;
     hipLaunchKernelGGL(ce_index_kernel, dim3((unsigned)c.p.chunks), dim3(256), 0, c.stream, target, target64, (long)c.s.rows, (long)c.s.V,
-                       (long)c.p.chunk, several ? counts : nullptr, c.st, rows, reinterpret_cast<uint32_t*>(c.ws));
+                       (long)c.p.chunk, several ? counts : nullptr, c.st, rows);
     Packed lw{};
-    const uint16_t* w = pack_operands<T>(c, &lw);
+    const uint16_t* w = pack_operands<T>(c, true, &lw);
     SumsOut<P> out{};
     fill(out, c);
     out.part = reinterpret_cast<float2*>(c.ws + c.p.part_at);
@@ -782,25 +783,25 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
     uint64_t* sums = reduction == DA_LOSS_ROWS ? nullptr : reinterpret_cast<uint64_t*>(c.ws + c.p.sums_at);
     const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256 / lanes), kJoinBlocks));
     hipLaunchKernelGGL(ce_join_kernel, dim3(blocks), dim3(256), 0, c.stream, c.st, out.part, c.p.slots, lanes, out.at_target, rows, sums,
-                       reinterpret_cast<uint32_t*>(c.ws) + kArrived, (int)(reduction == DA_LOSS_MEAN), loss);
+                       c.st.maxes + kArrived, (int)(reduction == DA_LOSS_MEAN), loss);
 }
 
 template <class T>
 void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, T* dx, T* dw, void* db) {
     typedef PlaneOf<T> P;
-    uint32_t* maxes = reinterpret_cast<uint32_t*>(c.ws);
+    uint32_t* largest = reinterpret_cast<uint32_t*>(c.ws);
     float* g = reinterpret_cast<float*>(c.ws + c.p.g_at);
     int* arrived = reinterpret_cast<int*>(c.ws + c.p.arrived_at);
-    const Upstream u{dloss, g, reduction, c.st.count};
+    const Upstream u{dloss, g, largest, reduction, c.st.count};
     if (c.s.d == 0) dx = dw = nullptr;
     hipLaunchKernelGGL((ce_begin_kernel<T>), dim3((unsigned)(dx ? std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 4), 4096)) : 1)), dim3(256), 0,
-                       c.stream, c.st, (long)c.s.rows, (int)c.s.d, dx, maxes, arrived);
+                       c.stream, c.st, (long)c.s.rows, (int)c.s.d, dx, largest, arrived);
     if (reduction == DA_LOSS_ROWS)
         hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 256))), dim3(256), 0,
-                           c.stream, c.st, dloss, (long)stride, g, maxes);
+                           c.stream, c.st, dloss, (long)stride, g, largest);
     if (c.s.V == 0) return;
     Packed lw{};
-    const uint16_t* w = pack_operands<T>(c, &lw);
+    const uint16_t* w = pack_operands<T>(c, false, &lw);
     uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + c.p.dz_at);
     float* acc = reinterpret_cast<float*>(c.ws + c.p.dx_at);
     float* part = reinterpret_cast<float*>(c.ws + c.p.sum_at);
@@ -827,7 +828,6 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             a.K = (int)Vb;
             a.rows = c.st.count;
             InputOut<T, P> out{};
-            out.maxes = maxes;
             out.u = u;
             out.st = c.st;
             out.before = first > 0 ? acc : nullptr;
@@ -847,7 +847,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             a.Nb = (int)Vb;
             a.K = (int)c.p.Ma;
             a.rows = c.st.count;
-            const WeightOut<T, P> out{maxes, u, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
+            const WeightOut<T, P> out{c.st.maxes, u, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
             plane_product<P, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, arrived, c.stream);
         }
         if (db) {
@@ -855,7 +855,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, lz,
                                (int)Vb, (long)per, bias);
             hipLaunchKernelGGL((ce_bias_join_kernel<P>), dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
-                               (int)width, maxes, u, db, c.param_dtype, (int)first);
+                               (int)width, u, db, c.param_dtype, (int)first);
         }
     }
 }
