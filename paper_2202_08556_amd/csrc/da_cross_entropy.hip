@@ -9,6 +9,7 @@
 // which only the device knows: rows without one cost nothing and may hold anything.
 #include "da_training.h"
 
+#include "da_ce_few.h"
 #include "da_ce_narrow.h"
 #include "da_planes_host.h"
 #include "da_spmm.h"
@@ -598,6 +599,27 @@ NarrowPlan narrow_plan(const CeShape& s, bool backward) {
     return p;
 }
 
+// Few rows: da_ce_few.h
+struct FewPlan {
+    bool taken;
+    int splits, per, across;     // of the lines forward; parts of the classes backward
+    int64_t columns, blocks;     // blocks along the classes of the logits and of their sums
+};
+FewPlan few_plan(const CeShape& s, int size) {
+    FewPlan p{};
+    if (s.rows < 1 || s.rows > kFewRows || s.d < 1 || s.V < 1) return p;
+    p.taken = true;
+    const int64_t cus = compute_units();
+    p.columns = ceil_div(s.V, 64 * 16 / size);
+    p.blocks = ceil_div(s.V, kFewBlock);
+    // four blocks to a unit, no fewer than 32 lines to one
+    const int64_t splits = std::max<int64_t>(1, std::min(ceil_div(4 * cus, p.columns), s.d / 32));
+    p.per = (int)ceil_div(s.d, splits);
+    p.splits = (int)ceil_div(s.d, p.per);
+    p.across = (int)std::max<int64_t>(1, std::min(ceil_div(2 * cus, ceil_div(s.d, kFewDown)), ceil_div(s.V, 4 * kFewBlock)));
+    return p;
+}
+
 struct PiecePlan {
     PlanePlan logits, input, weight;
 };
@@ -610,6 +632,8 @@ PiecePlan piece_plan(int64_t Ma, int64_t D, int64_t width, int step) {
 
 struct CePlan {
     NarrowPlan narrow, narrow_back;
+    FewPlan few;
+    size_t few_sums, few_target, few_dz, few_dx;             // bytes
     int64_t Ma, D, Vb;           // rows, d and classes, padded
     int64_t chunk, chunks;       // of the rows
     PlanePlan logits;
@@ -640,12 +664,25 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
         p.backward = 16 + round16((size_t)p.narrow_back.blocks * (s.d + 1) * s.V * sizeof(float));
         return p;
     }
-    size_t at = 16;                                          // the largest factor of a row
+    size_t at = 16;                                          // the largest factor of a row, or a count
     auto take = [&](size_t bytes) {
         const size_t from = at;
         at += round16(bytes);
         return from;
     };
+    p.few = few_plan(s, dtype == DA_F32 ? 4 : 2);
+    if (p.few.taken) {
+        (void)take((size_t)p.few.splits * s.rows * p.Vb * 4);
+        const size_t both = at;
+        p.few_sums = take((size_t)s.rows * p.few.blocks * sizeof(float2));
+        p.few_target = take((size_t)s.rows * 4);
+        p.forward = at;
+        at = both;
+        p.few_dz = take((size_t)s.rows * p.Vb * 4);
+        p.few_dx = take(p.few.across > 1 ? (size_t)p.few.across * s.rows * s.d * 4 : 0);
+        p.backward = at;
+        return p;
+    }
     p.x_at = take((size_t)p.Ma * p.D * 2 * N);
     p.w_at = take((size_t)p.D * p.Vb * 2 * N);
     const size_t both = at;
@@ -930,6 +967,72 @@ void narrow_backward(const CeCall& c, int reduction, const float* dloss, int64_t
         hipLaunchKernelGGL((ce_narrow_join_kernel<T>), dim3((unsigned)ceil_div(numbers, 16)), dim3(256), 0, c.stream, a, p.blocks);
 }
 
+// ... by the rows that registers are held for
+template <class T, class F> void by_rows(int64_t rows, F&& go) {
+    if (rows == 1) go(std::integral_constant<int, 1>());
+    else if (rows == 2) go(std::integral_constant<int, 2>());
+    else if (rows <= 4) go(std::integral_constant<int, 4>());
+    else if (rows <= 8) go(std::integral_constant<int, 8>());
+    else go(std::integral_constant<int, 16>());
+}
+FewArgs few_args(const CeCall& c, int reduction) {
+    FewArgs a{};
+    a.x = c.x;
+    a.w = c.w;
+    a.b = c.b;
+    a.ldx = c.ldx;
+    a.V = c.s.V;
+    a.Vp = c.p.Vb;
+    a.rows = (int)c.s.rows;
+    a.d = (int)c.s.d;
+    a.param_type = c.param_dtype;
+    a.reduction = reduction;
+    a.splits = c.p.few.splits;
+    a.per = c.p.few.per;
+    a.part = reinterpret_cast<float*>(c.ws + 16);
+    a.arrived = reinterpret_cast<uint32_t*>(c.ws);
+    a.count = c.st.count;
+    a.kept_target = c.st.target;
+    a.lse = c.st.lse;
+    return a;
+}
+template <class T> void few_forward(const CeCall& c, const void* target, int target64, int reduction, float* loss) {
+    FewArgs a = few_args(c, reduction);
+    a.target = target;
+    a.target64 = target64;
+    a.loss = loss;
+    a.sums = reinterpret_cast<float2*>(c.ws + c.p.few_sums);
+    a.at_target = reinterpret_cast<float*>(c.ws + c.p.few_target);
+    by_rows<T>(c.s.rows, [&](auto r) {
+        hipLaunchKernelGGL((ce_few_logits_kernel<T, decltype(r)::value, false>), dim3((unsigned)c.p.few.columns, (unsigned)a.splits), dim3(kFewBlock), 0,
+                           c.stream, a);
+    });
+    hipLaunchKernelGGL(ce_few_sums_kernel, dim3((unsigned)c.p.few.blocks, (unsigned)a.rows), dim3(kFewBlock), 0, c.stream, a);
+}
+template <class T> void few_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, void* dx, void* dw, void* db) {
+    FewArgs a = few_args(c, reduction);
+    a.dloss = dloss;
+    a.stride = stride;
+    a.dx = dx;
+    a.dw = dw;
+    a.db = db;
+    a.dz = reinterpret_cast<float*>(c.ws + c.p.few_dz);
+    a.dx_part = reinterpret_cast<float*>(c.ws + c.p.few_dx);
+    by_rows<T>(c.s.rows, [&](auto r) {
+        hipLaunchKernelGGL((ce_few_logits_kernel<T, decltype(r)::value, true>), dim3((unsigned)c.p.few.columns, (unsigned)a.splits), dim3(kFewBlock), 0,
+                           c.stream, a);
+    });
+    hipLaunchKernelGGL(ce_few_grad_kernel, dim3((unsigned)ceil_div(a.Vp, kFewBlock)), dim3(kFewBlock), 0, c.stream, a);
+    if (!dx && !dw) return;
+    by_rows<T>(c.s.rows, [&](auto r) {
+        hipLaunchKernelGGL((ce_few_products_kernel<T, decltype(r)::value>), dim3((unsigned)ceil_div(c.s.d, kFewDown), (unsigned)c.p.few.across),
+                           dim3(kFewBlock), 0, c.stream, a);
+    });
+    if (dx && c.p.few.across > 1)
+        hipLaunchKernelGGL((ce_few_join_kernel<T>), dim3((unsigned)ceil_div((int64_t)a.rows * a.d, kFewBlock)), dim3(kFewBlock), 0, c.stream, a,
+                           c.p.few.across);
+}
+
 int ce_call(int dtype, int64_t rows, int64_t d, int64_t classes, const void* x, int64_t ldx, const void* w, const void* b, int param_dtype,
             int reduction, const void* stats, void* workspace, size_t workspace_bytes, bool backward, void* stream, CeCall* c) {
     const int st = ce_check(dtype, rows, d, classes);
@@ -986,6 +1089,11 @@ extern "C" int da_linear_cross_entropy(int dtype, int64_t rows, int64_t d, int64
         else narrow_forward<bf16>(c, target, target64, reduction, loss);
         return launched("da_linear_cross_entropy launch");
     }
+    if (c.p.few.taken) {
+        if (dtype == DA_F32) few_forward<float>(c, target, target64, reduction, loss);
+        else few_forward<bf16>(c, target, target64, reduction, loss);
+        return launched("da_linear_cross_entropy launch");
+    }
     if (dtype == DA_F32) ce_forward<float>(c, target, target64, reduction, loss);
     else ce_forward<bf16>(c, target, target64, reduction, loss);
     return launched("da_linear_cross_entropy launch");
@@ -1006,6 +1114,11 @@ extern "C" int da_linear_cross_entropy_backward(int dtype, int64_t rows, int64_t
     if (c.p.narrow.taken) {
         if (dtype == DA_F32) narrow_backward<float>(c, reduction, dloss, dloss_stride, dx, dw, db);
         else narrow_backward<bf16>(c, reduction, dloss, dloss_stride, dx, dw, db);
+        return launched("da_linear_cross_entropy_backward launch");
+    }
+    if (c.p.few.taken) {
+        if (dtype == DA_F32) few_backward<float>(c, reduction, dloss, dloss_stride, dx, dw, db);
+        else few_backward<bf16>(c, reduction, dloss, dloss_stride, dx, dw, db);
         return launched("da_linear_cross_entropy_backward launch");
     }
     if (dtype == DA_F32) ce_backward<float>(c, reduction, dloss, dloss_stride, static_cast<float*>(dx), static_cast<float*>(dw), db);
