@@ -62,14 +62,15 @@ template <class P> __device__ __forceinline__ Scale scale_at(const uint32_t* max
     return scale_of(maxes[which]);
 }
 
-// The gradient of the loss: of the rows, g, or one factor for all of them
+// The gradient of the loss: of the rows, or one factor for all of them
 struct Upstream {
-    const float *dloss, *g;
+    const float* dloss;
+    long stride;
     const uint32_t* largest;     // of the rows' factors
     int reduction;
-    const int* count;
+    const int *count, *index;
     __device__ __forceinline__ float all() const { return reduction == DA_LOSS_MEAN ? dloss[0] / (float)max(1, *count) : dloss[0]; }
-    __device__ __forceinline__ float row(int m) const { return reduction == DA_LOSS_ROWS ? g[m] : all(); }
+    __device__ __forceinline__ float row(int m) const { return reduction == DA_LOSS_ROWS ? dloss[index[m] * stride] : all(); }
 };
 __device__ __forceinline__ float magnitude(float x) {
     const float a = fabsf(x);
@@ -183,6 +184,18 @@ __global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x
     keep_largest(most, st.maxes + (blockIdx.y == 0 ? kMaxX : kMaxW));
 }
 
+template <class T> __device__ __forceinline__ void store_row(T* p, int left, const float (&x)[4]) {
+    if (left >= 4) {
+        store_floats<4>(p, x);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            const float one[1] = {x[q]};
+            if (q < left) store_floats<1>(p + q, one);
+        }
+    }
+}
+
 // Packs lines of numbers, 8 numbers at a time; lines and their ends are padded with zeros.
 template <class T> struct PackJob {
     const T* from;
@@ -193,11 +206,35 @@ template <class T> struct PackJob {
     uint16_t* to;
     Packed layout;
 };
+// What a backward pass begins with beside that: no magnitude and no parts yet, and 0 in the rows of dx without a target
+template <class T> struct BeginJob {
+    long rows;
+    int d;
+    T* dx;
+    uint32_t* largest;
+    int* arrived;                // null: forward
+    __device__ __forceinline__ void run(const CeStats& st) const {
+        if (blockIdx.x == 0) {
+            if (threadIdx.x == 0) *largest = 0;
+            for (int k = threadIdx.x; k < kMostParted; k += 256) arrived[k] = 0;
+        }
+        if (!dx) return;
+        const int lane = threadIdx.x & 63;
+        for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (long)gridDim.x * 4) {
+            if (st.place[r] >= 0) continue;
+            for (int k = lane * 4; k < d; k += 256) {
+                const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+                store_row(dx + r * d + k, d - k, zero);
+            }
+        }
+    }
+};
 template <class T, class P>
-__global__ __launch_bounds__(256) void ce_pack_kernel(PackJob<T> x, PackJob<T> w, const uint32_t* __restrict__ maxes)
+__global__ __launch_bounds__(256) void ce_pack_kernel(CeStats st, PackJob<T> x, PackJob<T> w, BeginJob<T> begin)
 {
+    if (blockIdx.y == 2) return begin.run(st);
     const PackJob<T>& j = blockIdx.y ? w : x;
-    const Scale s = scale_at<P>(maxes, j.which);
+    const Scale s = scale_at<P>(st.maxes, j.which);
     const int pieces = (int)(padded(j.n) / 8);
     const long there = j.index ? *j.count : j.lines, all = padded(there) * pieces;
     for (long k = (long)blockIdx.x * 256 + threadIdx.x; k < all; k += (long)gridDim.x * 256) {
@@ -380,18 +417,6 @@ template <class P> struct GradOut : Logits<P> {
     }
 };
 
-template <class T> __device__ __forceinline__ void store_row(T* p, int left, const float (&x)[4]) {
-    if (left >= 4) {
-        store_floats<4>(p, x);
-    } else {
-#pragma unroll
-        for (int q = 0; q < 3; ++q) {
-            const float one[1] = {x[q]};
-            if (q < left) store_floats<1>(p + q, one);
-        }
-    }
-}
-
 // dx, or what the pieces so far give of it
 template <class T, class P> struct InputOut {
     static constexpr bool kSymmetric = false, kWhole = false;
@@ -487,37 +512,13 @@ __global__ __launch_bounds__(256) void ce_join_kernel(CeStats st, const float2* 
     if (threadIdx.x == 0) *loss_all = (float)(mean ? total / max(1, count) : total);
 }
 
-// The factors of the rows' gradients, and the largest of them
-__global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, const float* __restrict__ dloss, long stride, float* __restrict__ g,
-                                                        uint32_t* __restrict__ largest)
+// The largest factor of a row
+__global__ __launch_bounds__(256) void ce_factor_kernel(Upstream u, uint32_t* __restrict__ largest)
 {
-    const int count = *st.count;
+    const int count = *u.count;
     float most = 0.f;
-    for (long m = (long)blockIdx.x * 256 + threadIdx.x; m < count; m += (long)gridDim.x * 256) {
-        const float v = dloss[st.index[m] * stride];
-        g[m] = v;
-        most = fmaxf(most, magnitude(v));
-    }
+    for (long m = (long)blockIdx.x * 256 + threadIdx.x; m < count; m += (long)gridDim.x * 256) most = fmaxf(most, magnitude(u.row((int)m)));
     keep_largest(most, largest);
-}
-// What a backward pass begins with: no magnitude and no parts yet, and 0 in the rows of dx without a target
-template <class T>
-__global__ __launch_bounds__(256) void ce_begin_kernel(CeStats st, long rows, int d, T* __restrict__ dx, uint32_t* __restrict__ largest,
-                                                       int* __restrict__ arrived)
-{
-    if (blockIdx.x == 0) {
-        if (threadIdx.x == 0) *largest = 0;
-        for (int k = threadIdx.x; k < kMostParted; k += 256) arrived[k] = 0;
-    }
-    if (!dx) return;
-    const int lane = threadIdx.x & 63;
-    for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (long)gridDim.x * 4) {
-        if (st.place[r] >= 0) continue;
-        for (int k = lane * 4; k < d; k += 256) {
-            const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-            store_row(dx + r * d + k, d - k, zero);
-        }
-    }
 }
 
 // db: sums of dz's columns over parts of the rows, then over the parts
@@ -642,7 +643,7 @@ struct CePlan {
     PiecePlan whole, rest;       // products of a whole piece and of the last one
     int bias_parts;
     size_t counts_at, sums_at, target_at, x_at, w_at, part_at, forward;          // bytes
-    size_t g_at, arrived_at, dz_at, dx_at, bias_at, sum_at, backward;
+    size_t arrived_at, dz_at, dx_at, bias_at, sum_at, backward;
 };
 
 int wave_columns(const PlanePlan& p) { return p.shape == 0 ? PlaneLarge::WN : PlaneSmall::WN; }
@@ -693,7 +694,6 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
     p.forward = at;
 
     at = both;
-    p.g_at = take((size_t)p.Ma * 4);
     p.arrived_at = take(kMostParted * sizeof(int));
     p.piece = std::max<int64_t>(1024, kPieceBytes / std::max<int64_t>(1, p.Ma * 2 * N) / 256 * 256);
     if (p.piece >= s.V) p.piece = std::max<int64_t>(s.V, 1);
@@ -750,12 +750,12 @@ struct CeCall {
     hipStream_t stream;
 };
 
-template <class T> const uint16_t* pack_operands(const CeCall& c, bool forward, Packed* lw) {
+template <class T> const uint16_t* pack_operands(const CeCall& c, const BeginJob<T>& begin, Packed* lw) {
     typedef PlaneOf<T> P;
     const T* x = static_cast<const T*>(c.x);
     const T* w = static_cast<const T*>(c.w);
     if constexpr (P::N == 2) {
-        if (forward) {                                       // kept for the backward pass
+        if (!begin.arrived) {                                // kept for the backward pass
             const int64_t most = std::max(ceil_div(c.s.rows, 4), ceil_div(c.s.d * c.s.V, 4096));
             hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 512)), 2), dim3(256), 0, c.stream, x,
                                (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V));
@@ -768,9 +768,11 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, bool forward, 
     // a weight of whole pads is read where it is
     const bool direct = P::N == 1 && c.s.d % kPad == 0 && c.s.V % kPad == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
     const int64_t eights = std::max(c.p.Ma * (c.p.D / 8), direct ? 0 : c.p.D * (c.p.Vb / 8));
-    if (eights)
-        hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::min<int64_t>(ceil_div(eights, 256), 8192), direct ? 1 : 2), dim3(256), 0,
-                           c.stream, jx, jw, c.st.maxes);
+    PackJob<T> jw_here = jw;
+    if (direct) jw_here.lines = jw_here.n = 0;
+    if (eights || begin.arrived)
+        hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(eights, 256), 8192)), begin.arrived ? 3 : direct ? 1 : 2),
+                           dim3(256), 0, c.stream, c.st, jx, jw_here, begin);
     *lw = direct ? packed_lines(c.s.V) : jw.layout;
     return direct ? reinterpret_cast<const uint16_t*>(w) : jw.to;
 }
@@ -808,7 +810,7 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
     hipLaunchKernelGGL(ce_index_kernel, dim3((unsigned)c.p.chunks), dim3(256), 0, c.stream, target, target64, (long)c.s.rows, (long)c.s.V,
                        (long)c.p.chunk, several ? counts : nullptr, c.st, rows);
     Packed lw{};
-    const uint16_t* w = pack_operands<T>(c, true, &lw);
+    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{}, &lw);
     SumsOut<P> out{};
     fill(out, c);
     out.part = reinterpret_cast<float2*>(c.ws + c.p.part_at);
@@ -827,18 +829,15 @@ template <class T>
 void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, T* dx, T* dw, void* db) {
     typedef PlaneOf<T> P;
     uint32_t* largest = reinterpret_cast<uint32_t*>(c.ws);
-    float* g = reinterpret_cast<float*>(c.ws + c.p.g_at);
     int* arrived = reinterpret_cast<int*>(c.ws + c.p.arrived_at);
-    const Upstream u{dloss, g, largest, reduction, c.st.count};
+    const Upstream u{dloss, (long)stride, largest, reduction, c.st.count, c.st.index};
     if (c.s.d == 0) dx = dw = nullptr;
-    hipLaunchKernelGGL((ce_begin_kernel<T>), dim3((unsigned)(dx ? std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 4), 4096)) : 1)), dim3(256), 0,
-                       c.stream, c.st, (long)c.s.rows, (int)c.s.d, dx, largest, arrived);
-    if (reduction == DA_LOSS_ROWS)
-        hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 256))), dim3(256), 0,
-                           c.stream, c.st, dloss, (long)stride, g, largest);
-    if (c.s.V == 0) return;
     Packed lw{};
-    const uint16_t* w = pack_operands<T>(c, false, &lw);
+    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{(long)c.s.rows, (int)c.s.d, dx, largest, arrived}, &lw);
+    if (c.s.V == 0) return;
+    if (P::N == 2 && reduction == DA_LOSS_ROWS)              // whose scale dz takes
+        hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 256))), dim3(256), 0,
+                           c.stream, u, largest);
     uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + c.p.dz_at);
     float* acc = reinterpret_cast<float*>(c.ws + c.p.dx_at);
     float* part = reinterpret_cast<float*>(c.ws + c.p.sum_at);
