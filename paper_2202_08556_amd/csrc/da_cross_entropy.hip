@@ -149,7 +149,8 @@ __device__ __forceinline__ void keep_largest(float most, uint32_t* to) {
     __syncthreads();
     if (threadIdx.x == 0) {
         most = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-        if (most > 0.f) atomicMax(to, __float_as_uint(most));
+        // most blocks find a larger one there
+        if (__float_as_uint(most) > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, __float_as_uint(most));
     }
 }
 // Largest finite magnitudes: blockIdx.y 0 of the rows of x that count, 1 of w
@@ -235,11 +236,13 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(CeStats st, PackJob<T> x, 
     if (blockIdx.y == 2) return begin.run(st);
     const PackJob<T>& j = blockIdx.y ? w : x;
     const Scale s = scale_at<P>(st.maxes, j.which);
-    const int pieces = (int)(padded(j.n) / 8);
-    const long there = j.index ? *j.count : j.lines, all = padded(there) * pieces;
-    for (long k = (long)blockIdx.x * 256 + threadIdx.x; k < all; k += (long)gridDim.x * 256) {
-        const long line = k / pieces;
-        const int at = (int)(k % pieces) * 8;
+    // 16 lines x 128 numbers at a time, four lines to a wave: whole lines of memory on both sides
+    const int n = (int)padded(j.n), across = (n + 127) / 128;
+    const long there = j.index ? *j.count : j.lines, tiles = (padded(there) / 16) * across;
+    for (long k = blockIdx.x; k < tiles; k += gridDim.x) {
+        const long line = k / across * 16 + threadIdx.x / 16;
+        const int at = (int)(k % across) * 128 + threadIdx.x % 16 * 8;
+        if (at >= n) continue;
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = 0.f;
@@ -757,7 +760,7 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, const BeginJob
     if constexpr (P::N == 2) {
         if (!begin.arrived) {                                // kept for the backward pass
             const int64_t most = std::max(ceil_div(c.s.rows, 4), ceil_div(c.s.d * c.s.V, 4096));
-            hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 512)), 2), dim3(256), 0, c.stream, x,
+            hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 1024)), 2), dim3(256), 0, c.stream, x,
                                (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V));
         }
     }
@@ -767,11 +770,11 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, const BeginJob
     const PackJob<T> jx = job(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, kMaxX, c.p.x_at), jw = job(w, c.s.V, c.s.d, (int)c.s.V, nullptr, kMaxW, c.p.w_at);
     // a weight of whole pads is read where it is
     const bool direct = P::N == 1 && c.s.d % kPad == 0 && c.s.V % kPad == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
-    const int64_t eights = std::max(c.p.Ma * (c.p.D / 8), direct ? 0 : c.p.D * (c.p.Vb / 8));
+    const int64_t tiles = std::max(c.p.Ma / 16 * ceil_div(c.p.D, 128), direct ? 0 : c.p.D / 16 * ceil_div(c.p.Vb, 128));
     PackJob<T> jw_here = jw;
     if (direct) jw_here.lines = jw_here.n = 0;
-    if (eights || begin.arrived)
-        hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(eights, 256), 8192)), begin.arrived ? 3 : direct ? 1 : 2),
+    if (tiles || begin.arrived)
+        hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(tiles, 8192)), begin.arrived ? 3 : direct ? 1 : 2),
                            dim3(256), 0, c.stream, c.st, jx, jw_here, begin);
     *lw = direct ? packed_lines(c.s.V) : jw.layout;
     return direct ? reinterpret_cast<const uint16_t*>(w) : jw.to;
