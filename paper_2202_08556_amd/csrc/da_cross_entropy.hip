@@ -11,6 +11,7 @@
 
 #include "da_ce_few.h"
 #include "da_ce_narrow.h"
+#include "da_ce_tall.h"
 #include "da_planes_host.h"
 #include "da_spmm.h"
 
@@ -603,6 +604,28 @@ NarrowPlan narrow_plan(const CeShape& s, bool backward) {
     return p;
 }
 
+// Few classes and more inner positions: da_ce_tall.h
+struct TallPlan {
+    bool taken;
+    int NF, chunk, blocks;       // of the rows
+    int parts;                   // of the rows of dw
+    int64_t per;
+};
+TallPlan tall_plan(const CeShape& s) {
+    TallPlan p{};
+    if (s.V < 1 || s.V > kTallClasses || s.rows <= kFewRows || s.d < 1) return p;
+    p.taken = true;
+    p.NF = (int)ceil_div(s.V, 16);
+    const int64_t cus = compute_units(), resident = 2 * cus;
+    p.chunk = (int)std::max<int64_t>(kTallRows, std::min<int64_t>(kNarrowChunk, ceil_div(ceil_div(s.rows, resident), kTallRows) * kTallRows));
+    p.blocks = (int)std::min(ceil_div(s.rows, p.chunk), resident);
+    // three blocks to a unit, no fewer than 256 rows to one
+    const int64_t parts = std::max<int64_t>(1, std::min(ceil_div(3 * cus, ceil_div(s.d, 64)), ceil_div(s.rows, 256)));
+    p.per = ceil_div(ceil_div(s.rows, parts), 64) * 64;
+    p.parts = (int)ceil_div(s.rows, p.per);
+    return p;
+}
+
 // Few rows: da_ce_few.h
 struct FewPlan {
     bool taken;
@@ -637,6 +660,8 @@ PiecePlan piece_plan(int64_t Ma, int64_t D, int64_t width, int step) {
 struct CePlan {
     NarrowPlan narrow, narrow_back;
     FewPlan few;
+    TallPlan tall;
+    size_t tall_part;
     size_t few_sums, few_target, few_dz, few_dx;             // bytes
     int64_t Ma, D, Vb;           // rows, d and classes, padded
     int64_t chunk, chunks;       // of the rows
@@ -666,6 +691,13 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
     if (p.narrow.taken) {
         p.forward = 16 + (size_t)p.narrow.blocks * 2 * sizeof(double);
         p.backward = 16 + round16((size_t)p.narrow_back.blocks * (s.d + 1) * s.V * sizeof(float));
+        return p;
+    }
+    p.tall = tall_plan(s);
+    if (p.tall.taken) {
+        p.forward = 16 + (size_t)p.tall.blocks * 2 * sizeof(double);
+        p.tall_part = 16 + round16((size_t)s.rows * p.tall.NF * 16 * 4);
+        p.backward = p.tall_part + round16((size_t)p.tall.parts * (s.d + 1) * s.V * 4);
         return p;
     }
     size_t at = 16;                                          // the largest factor of a row, or a count
@@ -969,6 +1001,53 @@ void narrow_backward(const CeCall& c, int reduction, const float* dloss, int64_t
         hipLaunchKernelGGL((ce_narrow_join_kernel<T>), dim3((unsigned)ceil_div(numbers, 16)), dim3(256), 0, c.stream, a, p.blocks);
 }
 
+template <class F> void by_fragments(int NF, F&& go) {
+    if (NF == 1) go(std::integral_constant<int, 1>());
+    else if (NF == 2) go(std::integral_constant<int, 2>());
+    else if (NF == 3) go(std::integral_constant<int, 3>());
+    else go(std::integral_constant<int, 4>());
+}
+TallArgs tall_args(const CeCall& c, int reduction) {
+    NarrowPlan p{};
+    p.chunk = c.p.tall.chunk;
+    TallArgs a{};
+    static_cast<NarrowArgs&>(a) = narrow_args(c, p, reduction);
+    return a;
+}
+template <class T> void tall_forward(const CeCall& c, const void* target, int target64, int reduction, float* loss) {
+    TallArgs a = tall_args(c, reduction);
+    a.target = target;
+    a.target64 = target64;
+    a.loss = loss;
+    a.sums = reinterpret_cast<double*>(c.ws + 16);
+    by_fragments(c.p.tall.NF, [&](auto nf) {
+        hipLaunchKernelGGL((ce_tall_kernel<T, decltype(nf)::value, false>), dim3((unsigned)c.p.tall.blocks), dim3(kNarrowBlock), 0, c.stream, a);
+    });
+    if (c.p.tall.blocks > 1) hipLaunchKernelGGL(ce_narrow_total_kernel, dim3(1), dim3(256), 0, c.stream, static_cast<const NarrowArgs&>(a), c.p.tall.blocks);
+}
+template <class T> void tall_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, void* dx, void* dw, void* db) {
+    const TallPlan& p = c.p.tall;
+    TallArgs a = tall_args(c, reduction);
+    a.dloss = dloss;
+    a.stride = stride;
+    a.dx = dx;
+    a.dw = dw;
+    a.db = db;
+    a.dz = reinterpret_cast<float*>(c.ws + 16);
+    a.part = reinterpret_cast<float*>(c.ws + c.p.tall_part);
+    a.per = p.per;
+    by_fragments(p.NF, [&](auto nf) {
+        hipLaunchKernelGGL((ce_tall_kernel<T, decltype(nf)::value, true>), dim3((unsigned)p.blocks), dim3(kNarrowBlock), 0, c.stream, a);
+        if (dw || db)
+            hipLaunchKernelGGL((ce_tall_weight_kernel<T, decltype(nf)::value>), dim3((unsigned)(dw ? ceil_div(c.s.d, 64) : 1), (unsigned)p.parts),
+                               dim3(kNarrowBlock), 0, c.stream, a);
+    });
+    const int64_t numbers = (dw ? c.s.d * c.s.V : 0) + (db ? c.s.V : 0);
+    if (numbers)
+        hipLaunchKernelGGL((ce_narrow_join_kernel<T>), dim3((unsigned)ceil_div(numbers, 16)), dim3(256), 0, c.stream, static_cast<const NarrowArgs&>(a),
+                           p.parts);
+}
+
 // ... by the rows that registers are held for
 template <class T, class F> void by_rows(int64_t rows, F&& go) {
     if (rows == 1) go(std::integral_constant<int, 1>());
@@ -1091,6 +1170,11 @@ extern "C" int da_linear_cross_entropy(int dtype, int64_t rows, int64_t d, int64
         else narrow_forward<bf16>(c, target, target64, reduction, loss);
         return launched("da_linear_cross_entropy launch");
     }
+    if (c.p.tall.taken) {
+        if (dtype == DA_F32) tall_forward<float>(c, target, target64, reduction, loss);
+        else tall_forward<bf16>(c, target, target64, reduction, loss);
+        return launched("da_linear_cross_entropy launch");
+    }
     if (c.p.few.taken) {
         if (dtype == DA_F32) few_forward<float>(c, target, target64, reduction, loss);
         else few_forward<bf16>(c, target, target64, reduction, loss);
@@ -1116,6 +1200,11 @@ extern "C" int da_linear_cross_entropy_backward(int dtype, int64_t rows, int64_t
     if (c.p.narrow.taken) {
         if (dtype == DA_F32) narrow_backward<float>(c, reduction, dloss, dloss_stride, dx, dw, db);
         else narrow_backward<bf16>(c, reduction, dloss, dloss_stride, dx, dw, db);
+        return launched("da_linear_cross_entropy_backward launch");
+    }
+    if (c.p.tall.taken) {
+        if (dtype == DA_F32) tall_backward<float>(c, reduction, dloss, dloss_stride, dx, dw, db);
+        else tall_backward<bf16>(c, reduction, dloss, dloss_stride, dx, dw, db);
         return launched("da_linear_cross_entropy_backward launch");
     }
     if (c.p.few.taken) {

@@ -105,7 +105,8 @@ SIZES = [(1, 1, 1), (1, 16, 4), (3, 5, 2), (2, 64, 1), (61, 64, 41), (64, 64, 64
          (1000, 24, 70), (5000, 16, 41), (40, 300, 5000), (1, 602, 9973), (700, 1, 33), (2100, 64, 2100), (16, 2000, 64), (4099, 40, 4100),
          (20000, 128, 47), (3000, 256, 64), (2500, 250, 40), (900, 100, 128), (1100, 128, 100), (700, 144, 90), (700, 64, 128), (333, 257, 41),
          (100000, 3, 2), (129, 17, 96), (64, 256, 16),
-         (1, 1, 300), (1, 4096, 1000), (2, 33, 2049), (3, 1208, 1583), (7, 500, 777), (16, 300, 130), (16, 20, 20011), (17, 300, 130), (9, 2000, 7)]
+         (1, 1, 300), (1, 4096, 1000), (2, 33, 2049), (3, 1208, 1583), (7, 500, 777), (16, 300, 130), (16, 20, 20011), (17, 300, 130), (9, 2000, 7),
+         (17, 300, 1), (100, 257, 41), (1000, 700, 10), (5000, 333, 64), (300, 2000, 33), (129, 1025, 48), (40000, 260, 3), (500, 260, 65)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
@@ -119,7 +120,7 @@ def test_forward_and_backward(rows, d, V, dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
 @pytest.mark.parametrize("rows,d,V,share", [(61, 64, 41, 0.5), (3000, 20, 41, 0.1), (5000, 16, 300, 0.5), (200, 48, 900, 0.3), (50, 32, 41, 0.0),
                                             (2049, 8, 10, 0.7), (11, 40, 900, 0.6), (16, 300, 41, 0.3),
-                                            (2, 64, 500, 0.0)])
+                                            (2, 64, 500, 0.0), (3000, 300, 20, 0.4), (40, 270, 9, 0.0), (257, 400, 60, 0.9)])
 def test_rows_without_a_target(rows, d, V, share, dtype, reduction):
     x, w, b, t, g = make(rows, d, V, dtype, bias=V != 300, share=share)
     t = torch.where((t < 0) & (torch.arange(rows, device="cuda") % 3 == 0), V + 5, t)      # beyond the classes: none either
