@@ -37,7 +37,8 @@ def orthogonalise(update: torch.Tensor, steps: int = 5, coefficients=COEFFICIENT
     steps, eps = int(steps), float(eps)
     if steps < 0:
         raise ValueError("steps must not be negative")
-    triples = [coefficients] * steps if not hasattr(coefficients[0], "__len__") else list(coefficients)
+    coefficients = list(coefficients)
+    triples = coefficients if not coefficients or hasattr(coefficients[0], "__len__") else [coefficients] * steps
     if len(triples) != steps or any(len(t) != 3 for t in triples):
         raise ValueError("coefficients must be (a, b, c), or one such triple a step")
     if torch.is_grad_enabled() and update.requires_grad:

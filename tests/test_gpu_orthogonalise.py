@@ -80,6 +80,7 @@ def test_coefficients_and_steps():
     g = momentum(2, 60, 100, torch.float32)
     check(g, steps=0)
     check(g.transpose(1, 2), steps=0)
+    assert torch.equal(optim.orthogonalise(g, steps=0, coefficients=[]), optim.orthogonalise(g, steps=0))
     check(g, steps=1)
     check(g, steps=8, coefficients=(1.5, -0.5, 0.0))
     check(g, steps=3, coefficients=[(4.0, -6.0, 3.0), (3.0, -3.2, 1.2), (1.9, -1.3, 0.4)])
