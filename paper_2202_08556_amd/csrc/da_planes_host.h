@@ -27,8 +27,8 @@ struct PlaneCost {
     double few, one, two, more;
 };
 constexpr PlaneCost kPlaneCost[2][3] = {
-    {{256, 1.2, 1.65, 1.65, 12.0}, {128, 0.55, 0.7, 0.9, 6.0}, {64, 0.24, 0.28, 0.32, 4.0}},         // One
-    {{256, 1.65, 2.35, 2.35, 13.0}, {128, 0.72, 0.95, 1.2, 6.0}, {64, 0.28, 0.32, 0.36, 4.0}}};      // Halves
+    {{256, 1.2, 1.65, 1.65, 12.0}, {128, 0.55, 0.7, 0.9, 8.0}, {64, 0.24, 0.28, 0.32, 4.0}},         // One
+    {{256, 1.65, 2.35, 2.35, 13.0}, {128, 0.72, 0.95, 1.2, 8.0}, {64, 0.28, 0.32, 0.36, 4.0}}};      // Halves
 
 // The tile, and the number of parts of the inner axis, whose turns on the chip take the least time: large tiles read least for what
 // they compute, small ones and parts keep all units busy, and a tile's parts go to memory and are read by one block (22 KB/us).
