@@ -4,7 +4,9 @@ the paper's three-loop model (Sec. 3, Table 1) plus data-aware algorithm selecti
 Sub-modules
   generators  seeded synthetic inputs (pure numpy; shared by tests, oracle checks and benchmarks)
   binding     thin ctypes marshalling over the C-ABI library libdaspmm.so (HIP kernels)
-  layers      group norm with an activation, gated feed-forward block, distillation loss (HIP kernels)
+  layers      group norm with an activation, RMS norm with a residual, gated feed-forward block, distillation loss, cross
+              entropy of a linear layer (HIP kernels)
+  optim       orthogonalised updates of weights (HIP kernels)
   build       compiles the HIP library (and the C oracle used by the tests) in-tree
 
 Importing the package does not load the HIP library; importing ``binding`` does, and raises if

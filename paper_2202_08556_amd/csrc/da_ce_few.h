@@ -1,6 +1,7 @@
 // Cross entropy of a linear layer for up to 16 rows (single tokens): every number of the weight is read for a handful of products, so
 // memory bounds it and the vector units do the arithmetic, in 32 bits for both types.  Packing the weight for the matrix cores would
-// read and write it once more than the products themselves (3 rows of 1208 x 11583 float32, forward: 67 us).
+// read and write it once more than the products themselves (3 rows of 1208 x 11583 float32, forward: 67 us,
+// so 22; the weight's 56 MB are 11 of them).
 //
 // Logits: a lane owns 16 bytes of a line of the weight and goes down the lines, four waves of a block and the blocks of a column of
 // the grid share them; the parts of the sums pass through memory.  Backward, a block owns four lines of the weight and of its gradient:

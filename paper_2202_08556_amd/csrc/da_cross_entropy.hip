@@ -7,6 +7,8 @@
 // products read: eight operations for each of rows x d x classes instead of six, and no logits in memory.
 // Rows that have a target are gathered first (x is packed for the products anyway), and the products stop at their number,
 // which only the device knows: rows without one cost nothing and may hold anything.
+// 4096 x 2048 x 65536 bf16, forward and backward: 3745 us, 1180 TFLOP/s; the four products 890 to 1020 each, the more the larger
+// their epilogues.
 #include "da_training.h"
 
 #include "da_ce_few.h"

@@ -4,6 +4,8 @@
 //
 // A wave of the 16 owns a fragment of A and of b A + c A^2, which takes A's place, and every sixteenth 16 columns of X,
 // which it replaces after reading them: only the two small matrices have to be waited for.
+// 64 x 64, 64 x 256 and 64 x 512 float32, five steps: 18, 35 and 58 us; a step of 64 x 256 is 5.4, 1.4 of it at the matrix cores' rate of
+// one unit.  (Blocks of 32 x 32 of A to a wave, with a quarter of the inner axis each, read half as much from LDS and took as long.)
 #pragma once
 #include "da_planes.h"
 
