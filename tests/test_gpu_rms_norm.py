@@ -187,6 +187,26 @@ def test_graph_and_streams():
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
 
 
+@pytest.mark.parametrize("rows,C", [(530000, 4096), (140000, 16400)])
+def test_many_numbers(rows, C):
+    """Offsets beyond 32 bits: the last rows are what they are by themselves."""
+    x = torch.empty(rows, C, device="cuda", dtype=torch.bfloat16).normal_()
+    w = torch.randn(C, device="cuda")
+    X = x.detach().requires_grad_(True)
+    y, s = layers.rms_norm(X, w, residual=x)
+    dx, = torch.autograd.grad((y, s), X, (x, x))
+    few = x[-100:].clone().requires_grad_(True)
+    y1, s1 = layers.rms_norm(few, w, residual=x[-100:])
+    dx1, = torch.autograd.grad((y1, s1), few, (x[-100:], x[-100:]))
+    # one row may be dealt to another number of lanes: the sum of squares in another order, and one rounding to bfloat16 more or less
+    for a, b in ((y, y1), (s, s1), (dx, dx1)):
+        assert torch.allclose(a[-100:].float(), b.float(), rtol=2.0 ** -7, atol=2.0 ** -9)
+    with torch.no_grad():
+        q, scale = layers.rms_norm_e4m3(x, w)
+        q1, scale1 = layers.rms_norm_e4m3(x[-100:], w)
+    assert torch.allclose(scale[-100:], scale1, rtol=1e-5) and torch.allclose(q[-100:].float(), q1.float(), rtol=0.13, atol=2.0 ** -8)
+
+
 def test_refusals():
     x, res, w, dy, _ = make(8, 16, torch.float32)
     with pytest.raises(ValueError):
