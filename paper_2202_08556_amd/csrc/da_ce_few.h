@@ -1,4 +1,4 @@
-// Cross entropy of a linear layer for up to 16 rows (single tokens): every number of the weight is read for a handful of products, so
+// Cross entropy of a linear layer for up to 4 rows (single tokens): every number of the weight is read for a handful of products, so
 // memory bounds it and the vector units do the arithmetic, in 32 bits for both types.  Packing the weight for the matrix cores would
 // read and write it once more than the products themselves (3 rows of 1208 x 11583 float32, forward: 67 us,
 // so 22; the weight's 56 MB are 11 of them).
@@ -11,7 +11,9 @@
 
 namespace daspmm {
 
-constexpr int kFewRows = 16, kFewBlock = 256, kFewLines = 256, kFewDown = 4;    // rows; threads; lines whose factors are in LDS; lines of a block backward
+constexpr int kFewRows = 4, kSomeRows = 64;  // here, and of da_ce_some.h
+constexpr int kFewBlock = 256, kFewLines = 256, kFewDown = 4;        // threads; lines whose factors are in LDS; lines of a block backward
+constexpr int kFewApart = 32;                // counts lie in lines of their own
 
 struct FewArgs {
     const void *x, *w, *b, *target;
@@ -19,9 +21,11 @@ struct FewArgs {
     int rows, d, param_type, target64, reduction;
     int splits, per;             // of the lines, lines of one
     float* part;                 // [split][row][Vp]
-    float2* sums;                // [row][block of 256 classes]
+    float2* sums;                // [row][block]
+    int each;                    // classes of a thread in that
     float* at_target;            // [row]
-    uint32_t* arrived;
+    uint32_t* arrived;           // [kSomeRows + 1][kFewApart]: blocks of a row, rows
+    double* losses;              // [row]
     int* count;
     int* kept_target;            // [row]: the class, or -1
     float *lse, *loss;
@@ -45,7 +49,7 @@ template <class T, int R, bool BWD> __global__ __launch_bounds__(kFewBlock) void
     __shared__ __attribute__((aligned(16))) float factor[kFewLines][R];
     __shared__ float others[3][64][V * AT_ONCE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (!BWD && blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *a.arrived = 0;
+    if (!BWD && blockIdx.x == 0 && blockIdx.y == 0 && tid <= kSomeRows) a.arrived[tid * kFewApart] = 0;
     const long n = ((long)blockIdx.x * 64 + lane) * V;
     const long left = a.V - n;
     const int k0 = blockIdx.y * a.per, k1 = min(k0 + a.per, a.d);
@@ -135,73 +139,91 @@ __device__ __forceinline__ float few_logit(const FewArgs& a, int r, long v) {
     return a.b ? z + load_param(a.b, a.param_type, v) : z;
 }
 
-// Maxima and sums of 256 classes of a row; the block that comes last makes the losses of them
+// Maxima and sums of 256 x each classes of a row; the block that comes last at a row makes its loss of them, the last of those their sum
 __global__ __launch_bounds__(kFewBlock) void ce_few_sums_kernel(FewArgs a)
 {
     __shared__ float red[4];
     __shared__ int last;
-    __shared__ double losses[kFewRows];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.y, t = few_target(a, r, false);
-    const long v = (long)blockIdx.x * kFewBlock + tid;
+    auto largest = [&](float x) {
+        for (int d = 1; d < 64; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+        if (lane == 0) red[wave] = x;
+        __syncthreads();
+        x = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        __syncthreads();
+        return x;
+    };
+    auto total = [&](float x) {
+        x = wave_sum(x, 64);
+        if (lane == 0) red[wave] = x;
+        __syncthreads();
+        x = (red[0] + red[1]) + (red[2] + red[3]);
+        __syncthreads();
+        return x;
+    };
+    auto comes_last = [&](uint32_t* count, uint32_t of) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // what this wave has stored is there
+        __syncthreads();
+        if (tid == 0) last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
+        __syncthreads();
+        return last;
+    };
+    uint64_t* const sums = reinterpret_cast<uint64_t*>(a.sums + (long)r * gridDim.x);
+    auto above = [](float m) { return m == -INFINITY ? 0.f : m; };
     if (t >= 0) {
-        const float z = v < a.V ? few_logit(a, r, v) : -INFINITY;
-        if (v == t) __hip_atomic_store(a.at_target + r, z, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        float most = z;
-        for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
-        if (lane == 0) red[wave] = most;
-        __syncthreads();
-        most = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-        const float from = most == -INFINITY ? 0.f : most;
-        const float sum = wave_sum(exp2_hw((z - from) * 1.44269504088896f), 64);
-        __syncthreads();
-        if (lane == 0) red[wave] = sum;
-        __syncthreads();
-        if (tid == 0) {
-            const float total = (red[0] + red[1]) + (red[2] + red[3]);
-            __hip_atomic_store(reinterpret_cast<uint64_t*>(a.sums + (long)r * gridDim.x + blockIdx.x),
-                               (uint64_t)__float_as_uint(most) | (uint64_t)__float_as_uint(total) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wave's are there
-    __syncthreads();
-    if (tid == 0) last = __hip_atomic_fetch_add(a.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x * gridDim.y - 1;
-    __syncthreads();
-    if (!last) return;
-    for (int k = wave; k < a.rows; k += 4) {                 // a row to a wave
-        const int target = few_target(a, k, false);
-        double loss = 0.0;
-        if (target >= 0) {
-            const uint64_t* __restrict__ p = reinterpret_cast<const uint64_t*>(a.sums + (long)k * gridDim.x);
-            auto get = [&](int c) { return __hip_atomic_load(p + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-            float most = -INFINITY, sum = 0.f;
-            for (int c = lane; c < (int)gridDim.x; c += 64) most = fmaxf(most, __uint_as_float((uint32_t)get(c)));
-            for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
-            const float from = most == -INFINITY ? 0.f : most;
-            for (int c = lane; c < (int)gridDim.x; c += 64) {
-                const uint64_t e = get(c);
-                sum += __uint_as_float((uint32_t)(e >> 32)) * exp2_hw((__uint_as_float((uint32_t)e) - from) * 1.44269504088896f);
+        constexpr int U = 4;
+        float own = -INFINITY, own_sum = 0.f;                // of the thread's
+        for (int i = 0; i < a.each; i += U) {
+            float z[U], m = own;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long v = ((long)blockIdx.x * a.each + i + u) * kFewBlock + tid;
+                z[u] = i + u < a.each && v < a.V ? few_logit(a, r, v) : -INFINITY;
+                if (i + u < a.each && v == t) __hip_atomic_store(a.at_target + r, z[u], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                m = fmaxf(m, z[u]);
             }
-            sum = wave_sum(sum, 64);
-            const float lse = most + logf(sum);
-            loss = lse - __hip_atomic_load(a.at_target + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (lane == 0) a.lse[k] = lse;
+            own_sum *= exp2_hw((own - above(m)) * 1.44269504088896f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) own_sum += exp2_hw((z[u] - above(m)) * 1.44269504088896f);
+            own = m;
         }
-        if (lane == 0) {
-            a.kept_target[k] = target;
-            losses[k] = loss;
-            if (a.reduction == DA_LOSS_ROWS) a.loss[k] = (float)loss;
-        }
+        const float most = largest(own);
+        const float sum = total(own_sum * exp2_hw((own - above(most)) * 1.44269504088896f));
+        if (tid == 0)
+            __hip_atomic_store(sums + blockIdx.x, (uint64_t)__float_as_uint(most) | (uint64_t)__float_as_uint(sum) << 32, __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
     }
-    __syncthreads();
-    if (tid == 0) {
-        double total = 0.0;
-        int many = 0;
-        for (int k = 0; k < a.rows; ++k) {
-            total += losses[k];
-            many += few_target(a, k, false) >= 0;
+    if (!comes_last(a.arrived + r * kFewApart, gridDim.x)) return;
+    double loss = 0.0;
+    if (t >= 0) {
+        auto get = [&](int c) { return __hip_atomic_load(sums + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+        float most = -INFINITY, sum = 0.f;
+        for (int c = tid; c < (int)gridDim.x; c += kFewBlock) most = fmaxf(most, __uint_as_float((uint32_t)get(c)));
+        most = largest(most);
+        const float from = above(most);
+        for (int c = tid; c < (int)gridDim.x; c += kFewBlock) {
+            const uint64_t e = get(c);
+            sum += __uint_as_float((uint32_t)(e >> 32)) * exp2_hw((__uint_as_float((uint32_t)e) - from) * 1.44269504088896f);
         }
+        const float lse = most + logf(total(sum));
+        loss = lse - __hip_atomic_load(a.at_target + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (tid == 0) a.lse[r] = lse;
+    }
+    if (tid == 0) {
+        a.kept_target[r] = t;
+        if (a.reduction == DA_LOSS_ROWS) a.loss[r] = (float)loss;
+        __hip_atomic_store(reinterpret_cast<uint64_t*>(a.losses) + r, (uint64_t)__double_as_longlong(loss), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (!comes_last(a.arrived + kSomeRows * kFewApart, a.rows) || wave > 0) return;
+    static_assert(kSomeRows == 64, "a row to a lane");
+    double all = lane < a.rows ? __longlong_as_double((long long)__hip_atomic_load(reinterpret_cast<uint64_t*>(a.losses) + lane, __ATOMIC_RELAXED,
+                                                                                  __HIP_MEMORY_SCOPE_AGENT))
+                               : 0.0;
+    for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d, 64);
+    const int many = __popcll(__ballot(few_target(a, lane, false) >= 0));
+    if (lane == 0) {
         *a.count = many;
-        if (a.reduction != DA_LOSS_ROWS) *a.loss = (float)(a.reduction == DA_LOSS_MEAN ? total / max(1, many) : total);
+        if (a.reduction != DA_LOSS_ROWS) *a.loss = (float)(a.reduction == DA_LOSS_MEAN ? all / max(1, many) : all);
     }
 }
 

@@ -13,6 +13,7 @@
 
 #include "da_ce_few.h"
 #include "da_ce_narrow.h"
+#include "da_ce_some.h"
 #include "da_ce_tall.h"
 #include "da_planes_host.h"
 #include "da_spmm.h"
@@ -615,7 +616,7 @@ struct TallPlan {
 };
 TallPlan tall_plan(const CeShape& s) {
     TallPlan p{};
-    if (s.V < 1 || s.V > kTallClasses || s.rows <= kFewRows || s.d < 1) return p;
+    if (s.V < 1 || s.V > kTallClasses || s.rows <= 16 || s.d < 1) return p;
     p.taken = true;
     p.NF = (int)ceil_div(s.V, 16);
     const int64_t cus = compute_units(), resident = 2 * cus;
@@ -628,19 +629,42 @@ TallPlan tall_plan(const CeShape& s) {
     return p;
 }
 
-// Few rows: da_ce_few.h
+// Few rows: da_ce_few.h, and da_ce_some.h
 struct FewPlan {
     bool taken;
     int splits, per, across;     // of the lines forward; parts of the classes backward
+    int each;                    // classes of a thread in their sums
     int64_t columns, blocks;     // blocks along the classes of the logits and of their sums
 };
+// In how many parts `steps` of each of so many blocks are taken: the turns on the chip that take least, 4 steps to begin and end a block
+int64_t some_parts(int64_t blocks, int64_t steps, int64_t slots) {
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t parts = 1; parts <= std::min<int64_t>(1024, steps); ++parts) {
+        const int64_t time = ceil_div(blocks * parts, slots) * (ceil_div(steps, parts) + 4);
+        if (time < least) {
+            least = time;
+            best = parts;
+        }
+    }
+    return best;
+}
 FewPlan few_plan(const CeShape& s, int size) {
     FewPlan p{};
-    if (s.rows < 1 || s.rows > kFewRows || s.d < 1 || s.V < 1) return p;
+    if (s.rows < 1 || s.rows > (size == 4 ? some_rows<float> : some_rows<bf16>) || s.d < 1 || s.V < 1) return p;
     p.taken = true;
     const int64_t cus = compute_units();
+    p.each = (int)std::min<int64_t>(16, ceil_div(s.rows * ceil_div(s.V, kFewBlock), 4 * cus));
+    p.blocks = ceil_div(s.V, (int64_t)kFewBlock * p.each);
+    if (s.rows > kFewRows) {
+        const int RF = (int)ceil_div(s.rows, 16);
+        p.columns = ceil_div(s.V, kSomeStep);
+        p.splits = (int)some_parts(p.columns, ceil_div(s.d, 64), some_logit_blocks(RF) * cus);
+        p.per = (int)(ceil_div(ceil_div(s.d, 64), p.splits) * 64);
+        p.splits = (int)ceil_div(s.d, p.per);
+        p.across = (int)some_parts(ceil_div(s.d, 64), ceil_div(s.V, kSomeStep), some_blocks(RF) * cus);
+        return p;
+    }
     p.columns = ceil_div(s.V, 64 * 16 / size);
-    p.blocks = ceil_div(s.V, kFewBlock);
     // four blocks to a unit, no fewer than 32 lines to one
     const int64_t splits = std::max<int64_t>(1, std::min(ceil_div(4 * cus, p.columns), s.d / 32));
     p.per = (int)ceil_div(s.d, splits);
@@ -664,7 +688,7 @@ struct CePlan {
     FewPlan few;
     TallPlan tall;
     size_t tall_part;
-    size_t few_sums, few_target, few_dz, few_dx;             // bytes
+    size_t few_arrived, few_losses, few_sums, few_target, few_dz, few_dx;        // bytes
     int64_t Ma, D, Vb;           // rows, d and classes, padded
     int64_t chunk, chunks;       // of the rows
     PlanePlan logits;
@@ -712,6 +736,8 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
     if (p.few.taken) {
         (void)take((size_t)p.few.splits * s.rows * p.Vb * 4);
         const size_t both = at;
+        p.few_arrived = take((kSomeRows + 1) * kFewApart * 4);
+        p.few_losses = take(kSomeRows * sizeof(double));
         p.few_sums = take((size_t)s.rows * p.few.blocks * sizeof(float2));
         p.few_target = take((size_t)s.rows * 4);
         p.forward = at;
@@ -1054,9 +1080,7 @@ template <class T> void tall_backward(const CeCall& c, int reduction, const floa
 template <class T, class F> void by_rows(int64_t rows, F&& go) {
     if (rows == 1) go(std::integral_constant<int, 1>());
     else if (rows == 2) go(std::integral_constant<int, 2>());
-    else if (rows <= 4) go(std::integral_constant<int, 4>());
-    else if (rows <= 8) go(std::integral_constant<int, 8>());
-    else go(std::integral_constant<int, 16>());
+    else go(std::integral_constant<int, 4>());
 }
 FewArgs few_args(const CeCall& c, int reduction) {
     FewArgs a{};
@@ -1073,23 +1097,36 @@ FewArgs few_args(const CeCall& c, int reduction) {
     a.splits = c.p.few.splits;
     a.per = c.p.few.per;
     a.part = reinterpret_cast<float*>(c.ws + 16);
-    a.arrived = reinterpret_cast<uint32_t*>(c.ws);
     a.count = c.st.count;
     a.kept_target = c.st.target;
     a.lse = c.st.lse;
     return a;
+}
+template <class T, class G> void by_some(int rows, const G& go) {
+    if (some_rows<T> == 16 || rows <= 16) go(std::integral_constant<int, 1>());
+    else if constexpr (some_rows<T> > 16) {
+        if (rows <= 32) go(std::integral_constant<int, 2>());
+        else if (rows <= 48) go(std::integral_constant<int, 3>());
+        else go(std::integral_constant<int, 4>());
+    }
+}
+template <class T, bool BWD> void few_logits(const CeCall& c, const FewArgs& a) {
+    const dim3 grid((unsigned)c.p.few.columns, (unsigned)a.splits), block(kFewBlock);
+    if (a.rows > kFewRows)
+        by_some<T>(a.rows, [&](auto f) { hipLaunchKernelGGL((ce_some_logits_kernel<T, decltype(f)::value, BWD>), grid, block, 0, c.stream, a); });
+    else by_rows<T>(c.s.rows, [&](auto r) { hipLaunchKernelGGL((ce_few_logits_kernel<T, decltype(r)::value, BWD>), grid, block, 0, c.stream, a); });
 }
 template <class T> void few_forward(const CeCall& c, const void* target, int target64, int reduction, float* loss) {
     FewArgs a = few_args(c, reduction);
     a.target = target;
     a.target64 = target64;
     a.loss = loss;
+    a.each = c.p.few.each;
+    a.arrived = reinterpret_cast<uint32_t*>(c.ws + c.p.few_arrived);
+    a.losses = reinterpret_cast<double*>(c.ws + c.p.few_losses);
     a.sums = reinterpret_cast<float2*>(c.ws + c.p.few_sums);
     a.at_target = reinterpret_cast<float*>(c.ws + c.p.few_target);
-    by_rows<T>(c.s.rows, [&](auto r) {
-        hipLaunchKernelGGL((ce_few_logits_kernel<T, decltype(r)::value, false>), dim3((unsigned)c.p.few.columns, (unsigned)a.splits), dim3(kFewBlock), 0,
-                           c.stream, a);
-    });
+    few_logits<T, false>(c, a);
     hipLaunchKernelGGL(ce_few_sums_kernel, dim3((unsigned)c.p.few.blocks, (unsigned)a.rows), dim3(kFewBlock), 0, c.stream, a);
 }
 template <class T> void few_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, void* dx, void* dw, void* db) {
@@ -1101,16 +1138,21 @@ template <class T> void few_backward(const CeCall& c, int reduction, const float
     a.db = db;
     a.dz = reinterpret_cast<float*>(c.ws + c.p.few_dz);
     a.dx_part = reinterpret_cast<float*>(c.ws + c.p.few_dx);
-    by_rows<T>(c.s.rows, [&](auto r) {
-        hipLaunchKernelGGL((ce_few_logits_kernel<T, decltype(r)::value, true>), dim3((unsigned)c.p.few.columns, (unsigned)a.splits), dim3(kFewBlock), 0,
-                           c.stream, a);
-    });
-    hipLaunchKernelGGL(ce_few_grad_kernel, dim3((unsigned)ceil_div(a.Vp, kFewBlock)), dim3(kFewBlock), 0, c.stream, a);
-    if (!dx && !dw) return;
-    by_rows<T>(c.s.rows, [&](auto r) {
-        hipLaunchKernelGGL((ce_few_products_kernel<T, decltype(r)::value>), dim3((unsigned)ceil_div(c.s.d, kFewDown), (unsigned)c.p.few.across),
-                           dim3(kFewBlock), 0, c.stream, a);
-    });
+    few_logits<T, true>(c, a);
+    if (a.rows > kFewRows) {
+        hipLaunchKernelGGL(ce_some_grad_kernel, dim3((unsigned)ceil_div(a.Vp, kFewBlock), (unsigned)a.rows), dim3(kFewBlock), 0, c.stream, a);
+        by_some<T>(a.rows, [&](auto f) {
+            hipLaunchKernelGGL((ce_some_products_kernel<T, decltype(f)::value>), dim3((unsigned)(dx || dw ? ceil_div(c.s.d, 64) : 1), (unsigned)c.p.few.across),
+                               dim3(kFewBlock), 0, c.stream, a);
+        });
+    } else {
+        hipLaunchKernelGGL(ce_few_grad_kernel, dim3((unsigned)ceil_div(a.Vp, kFewBlock)), dim3(kFewBlock), 0, c.stream, a);
+        if (!dx && !dw) return;
+        by_rows<T>(c.s.rows, [&](auto r) {
+            hipLaunchKernelGGL((ce_few_products_kernel<T, decltype(r)::value>), dim3((unsigned)ceil_div(c.s.d, kFewDown), (unsigned)c.p.few.across),
+                               dim3(kFewBlock), 0, c.stream, a);
+        });
+    }
     if (dx && c.p.few.across > 1)
         hipLaunchKernelGGL((ce_few_join_kernel<T>), dim3((unsigned)ceil_div((int64_t)a.rows * a.d, kFewBlock)), dim3(kFewBlock), 0, c.stream, a,
                            c.p.few.across);

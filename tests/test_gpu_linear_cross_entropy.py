@@ -139,6 +139,30 @@ def test_rows_without_a_target(rows, d, V, share, dtype, reduction):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("rows,d,V", [(4, 70, 1000), (5, 1, 65), (5, 4097, 66), (8, 63, 20011), (15, 65, 4096), (16, 1000, 130), (17, 66, 65), (31, 129, 2050),
+                                      (32, 64, 64000), (33, 250, 257), (47, 2000, 100), (48, 15, 5003), (49, 17, 67), (63, 777, 3001), (64, 128, 129),
+                                      (64, 4100, 515), (65, 100, 1000)])
+def test_some_rows(rows, d, V, dtype):
+    x, w, b, t, g = make(rows, d, V, dtype, share=0.8)
+    check(x, w, b, t, g)
+    check(x, w, None, t, g, reduction="mean")
+    without = (t < 0) | (t >= V)
+    bad = torch.cat([x, x], 1)[:, d // 2:d // 2 + d]         # rows 2 d apart
+    bad[without] = float("nan")
+    loss, grads = check(x.clone(), w, b, t, g, reduction="sum")
+    wide = torch.full((rows, 2 * d + 1), float("nan"), device="cuda", dtype=dtype)
+    wide[:, 1:d + 1] = torch.where(without[:, None], bad, x)
+    leaves = [v.detach().requires_grad_(True) for v in (wide[:, 1:d + 1], w, b)]
+    again = layers.linear_cross_entropy(leaves[0], leaves[1], t, bias=leaves[2], reduction="sum")
+    g2 = torch.autograd.grad(again, leaves, g[0])
+    assert torch.equal(again, loss) and all(torch.equal(p, q) for p, q in zip(g2, grads))
+    for i, leaf in enumerate((x, w, b)):                     # one gradient alone is the same
+        one = [v.detach().requires_grad_(k == i) for k, v in enumerate((x, w, b))]
+        alone = layers.linear_cross_entropy(one[0], one[1], t, bias=one[2], reduction="sum")
+        assert torch.equal(torch.autograd.grad(alone, one[i], g[0])[0], grads[i])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
 def test_many_rows_and_pieces(dtype):
     """More rows than one piece of the classes has room for: dx is summed over pieces."""
     rows, V = (140000, 1100) if dtype == torch.float32 else (280000, 1100)

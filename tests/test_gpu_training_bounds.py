@@ -85,6 +85,13 @@ def test_cross_entropy(seed):
     check(r)
 
 
+@pytest.mark.parametrize("seed", range(30))
+def test_cross_entropy_of_some_rows(seed, monkeypatch):
+    """... of 1 to 70 rows of a large weight."""
+    monkeypatch.setitem(globals(), "ce_shape", lambda rng: (rng.randint(1, 70), rng.choice([rng.randint(1, 64), rng.randint(257, 2000)]), rng.randint(65, 5000)))
+    test_cross_entropy(seed)
+
+
 @pytest.mark.parametrize("seed", range(25))
 def test_orthogonalise(seed):
     rng = random.Random(seed)
