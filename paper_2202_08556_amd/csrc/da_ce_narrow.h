@@ -67,18 +67,26 @@ __global__ __launch_bounds__(kNarrowBlock) void ce_narrow_kernel(NarrowArgs a)
     __shared__ double totals[4][2];
     const int inner = (a.d + 15) / 16 * 16, PK = narrow_pitch(inner), PV = narrow_pitch(NF * 16);
     float* const w = room;                                   // [class][inner position]
-    int* const list = reinterpret_cast<int*>(w + NF * 16 * PK);              // rows of the chunk that have a target; their classes from bit 16 on
+    int* const list = reinterpret_cast<int*>(w + NF * 16 * PK);              // rows of the chunk that have a target, their classes from bit 16 on; the others from the end
     float* const xs = reinterpret_cast<float*>(list + kNarrowChunk);     // [row][inner position]
     float* const ds = xs + kNarrowRows * PK;                 // [row][class]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i16 = lane & 15, h = lane >> 4;
     const T* __restrict__ W = static_cast<const T*>(a.w);
     const T* __restrict__ X = static_cast<const T*>(a.x);
 
-    for (int k = tid; k < inner * NF * 16; k += kNarrowBlock) {
-        const int p = k / (NF * 16), n = k % (NF * 16);
-        float one[1] = {0.f};
-        if (p < a.d && n < a.V) load_floats<1>(W + (long)p * a.V + n, one);
-        w[n * PK + p] = one[0];
+    constexpr int W_AT_ONCE = 8;
+    for (int k0 = tid; k0 < inner * NF * 16; k0 += W_AT_ONCE * kNarrowBlock) {
+        float one[W_AT_ONCE][1];
+#pragma unroll
+        for (int u = 0; u < W_AT_ONCE; ++u) {                // what is not there is some other number until it is put down
+            const int k = k0 + u * kNarrowBlock, p = k / (NF * 16), n = k % (NF * 16);
+            load_floats<1>(W + (long)min(p, a.d - 1) * a.V + min(n, a.V - 1), one[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < W_AT_ONCE; ++u) {
+            const int k = k0 + u * kNarrowBlock, p = k / (NF * 16), n = k % (NF * 16);
+            if (p < inner) w[n * PK + p] = p < a.d && n < a.V ? one[u][0] : 0.f;
+        }
     }
     float bias[NF][4];
 #pragma unroll
@@ -124,21 +132,25 @@ __global__ __launch_bounds__(kNarrowBlock) void ce_narrow_kernel(NarrowArgs a)
             __syncthreads();
             int at = n;
             for (int v = 0; v < wave; ++v) at += counts[v];
-            if (t >= 0) {
-                at += __popcll(mask & ((1ull << lane) - 1));
-                list[at] = (k + tid) | (int)t << 16;
-            }
+            at += __popcll(mask & ((1ull << lane) - 1));     // rows before this one that have a target; of k + tid
+            if (t >= 0) list[at] = (k + tid) | (int)t << 16;
+            else if (k + tid < here) list[kNarrowChunk - 1 - (k + tid - at)] = k + tid;
             n += counts[0] + counts[1] + counts[2] + counts[3];
             __syncthreads();
         }
         many += n;
         if constexpr (BWD) {
             if (a.dx)                                        // rows without a target
-                for (int k = wave; k < here; k += 4) {
-                    if (kept[first + k] >= 0) continue;
-                    T* __restrict__ p = static_cast<T*>(a.dx) + (first + k) * a.d;
-                    const float zero[1] = {0.f};
-                    for (int c = lane; c < a.d; c += 64) store_floats<1>(p + c, zero);
+                for (int k = wave; k < here - n; k += 4) {
+                    T* __restrict__ p = static_cast<T*>(a.dx) + (first + list[kNarrowChunk - 1 - k]) * a.d;
+                    const float zero[4] = {0.f, 0.f, 0.f, 0.f}, one[1] = {0.f};
+                    for (int c = 4 * lane; c < a.d; c += 256) {
+                        if (c + 4 <= a.d) {
+                            store_floats<4>(p + c, zero);
+                        } else {
+                            for (int q = c; q < a.d; ++q) store_floats<1>(p + q, one);
+                        }
+                    }
                 }
         }
         for (int g0 = 0; g0 < n; g0 += kNarrowRows) {
@@ -146,17 +158,30 @@ __global__ __launch_bounds__(kNarrowBlock) void ce_narrow_kernel(NarrowArgs a)
             const bool there = mine < n;
             const int entry = there ? list[mine] : -0x10000, t = entry >> 16;
             const long row = first + (entry & 0xffff);
-            const T* __restrict__ x = X + row * a.ldx;
+            const T* __restrict__ x = X + (there ? row : first) * a.ldx;
             f32x4 z[NF];
 #pragma unroll
             for (int j = 0; j < NF; ++j) z[j] = f32x4{0.f, 0.f, 0.f, 0.f};
             constexpr int AT_ONCE = 8;
             for (int k0 = 0; k0 < inner; k0 += 16 * AT_ONCE) {
                 f32x4 xf[AT_ONCE];
+                if (a.d == inner && k0 + 16 * AT_ONCE <= inner) {            // all at once, with nothing to decide by lane
 #pragma unroll
-                for (int u = 0; u < AT_ONCE; ++u) {
-                    const int c = k0 + u * 16 + 4 * h;
-                    xf[u] = narrow_four(x + c, there ? a.d - c : 0);
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        float v[4];
+                        load_floats<4>(x + k0 + u * 16 + 4 * h, v);
+                        xf[u] = f32x4{v[0], v[1], v[2], v[3]};
+                    }
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) xf[u][q] = there ? xf[u][q] : 0.f;
+                } else {
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        const int c = k0 + u * 16 + 4 * h;
+                        xf[u] = narrow_four(x + c, there ? a.d - c : 0);
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < AT_ONCE; ++u) {
