@@ -6,7 +6,7 @@
 // multiplies its rows, as they come from memory, with the weight in LDS, and has the rows' logits whole.  Backward it does so again,
 // and the lanes that hold dz hold it as the operand of dz w^T; dz and x go to LDS for x^T dz, of which each wave owns some inner
 // positions over all of the block's rows.  The blocks' parts of dw and db are added in one order.
-// 262144 x 128 x 41 float32, half of the rows labelled: 39 us forward and 105 backward (by the packed products 340 and 490).
+// 262144 x 128 x 41 float32, half of the rows labelled: 34 us forward and 86 backward (by the packed products 340 and 490).
 #pragma once
 #include "da_layer_common.h"
 

@@ -84,18 +84,25 @@ __global__ __launch_bounds__(kNarrowBlock) void ce_tall_kernel(TallArgs a)
             __syncthreads();
             int at = n;
             for (int v = 0; v < wave; ++v) at += counts[v];
-            if (t >= 0) list[at + __popcll(mask & ((1ull << lane) - 1))] = (k + tid) | (int)t << 16;
+            at += __popcll(mask & ((1ull << lane) - 1));     // rows before this one that have a target; of k + tid
+            if (t >= 0) list[at] = (k + tid) | (int)t << 16;
+            else if (k + tid < here) list[kNarrowChunk - 1 - (k + tid - at)] = k + tid;      // the others from the end
             n += counts[0] + counts[1] + counts[2] + counts[3];
             __syncthreads();
         }
         many += n;
         if constexpr (BWD) {
             if (a.dx)                                        // rows without a target
-                for (int k = wave; k < here; k += 4) {
-                    if (kept[first + k] >= 0) continue;
-                    T* __restrict__ p = static_cast<T*>(a.dx) + (first + k) * a.d;
-                    const float zero[1] = {0.f};
-                    for (int c = lane; c < a.d; c += 64) store_floats<1>(p + c, zero);
+                for (int k = wave; k < here - n; k += 4) {
+                    T* __restrict__ p = static_cast<T*>(a.dx) + (first + list[kNarrowChunk - 1 - k]) * a.d;
+                    const float zero[4] = {0.f, 0.f, 0.f, 0.f}, one[1] = {0.f};
+                    for (int c = 4 * lane; c < a.d; c += 256) {
+                        if (c + 4 <= a.d) {
+                            store_floats<4>(p + c, zero);
+                        } else {
+                            for (int q = c; q < a.d; ++q) store_floats<1>(p + q, one);
+                        }
+                    }
                 }
         }
         for (int g0 = 0; g0 < n; g0 += kTallRows) {
