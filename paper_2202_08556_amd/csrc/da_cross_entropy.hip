@@ -639,7 +639,7 @@ struct FewPlan {
 // In how many parts `steps` of each of so many blocks are taken: the turns on the chip that take least, 4 steps to begin and end a block
 int64_t some_parts(int64_t blocks, int64_t steps, int64_t slots) {
     int64_t best = 1, least = INT64_MAX;
-    for (int64_t parts = 1; parts <= std::min<int64_t>(1024, steps); ++parts) {
+    for (int64_t parts = 1; parts <= std::min<int64_t>(1024, steps); parts += std::max<int64_t>(1, parts / 8)) {
         const int64_t time = ceil_div(blocks * parts, slots) * (ceil_div(steps, parts) + 4);
         if (time < least) {
             least = time;
