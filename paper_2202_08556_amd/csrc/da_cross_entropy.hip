@@ -962,21 +962,16 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
 // ... a launch by the fragments that a call has
 template <class T, bool BWD> void narrow_launch(const NarrowPlan& p, const NarrowArgs& a, hipStream_t s) {
     const size_t lds = narrow_lds(p.NF, narrow_inner(a.d), BWD);
-    auto go = [&](auto kernel) {
-        static std::atomic<uint64_t> allowed{0};             // devices that know how much LDS the kernel takes
-        int device = 0;
-        (void)hipGetDevice(&device);
-        const uint64_t bit = 1ull << (device & 63);
-        if (!(allowed.load(std::memory_order_relaxed) & bit) &&
-            hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kNarrowLds) == hipSuccess)
-            allowed.fetch_or(bit, std::memory_order_relaxed);
+    auto go = [&](auto k) {
+        constexpr auto kernel = decltype(k)::value;
+        allow_lds<kernel>(kNarrowLds);
         hipLaunchKernelGGL(kernel, dim3((unsigned)p.blocks), dim3(kNarrowBlock), lds, s, a);
     };
     auto by_inner = [&](auto nf) {
         constexpr int NF = decltype(nf)::value;
-        if (!BWD || p.KW == 1) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, 1, BWD>>::value);
-        else if (p.KW == 2) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, BWD ? 2 : 1, BWD>>::value);
-        else if constexpr (NF <= 4) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, BWD ? 4 : 1, BWD>>::value);
+        if (!BWD || p.KW == 1) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, 1, BWD>>());
+        else if (p.KW == 2) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, BWD ? 2 : 1, BWD>>());
+        else if constexpr (NF <= 4) go(std::integral_constant<void (*)(NarrowArgs), ce_narrow_kernel<T, NF, BWD ? 4 : 1, BWD>>());
     };
     if (p.NF == 1) by_inner(std::integral_constant<int, 1>());
     else if (p.NF == 2) by_inner(std::integral_constant<int, 2>());

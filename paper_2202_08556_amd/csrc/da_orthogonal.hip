@@ -340,14 +340,8 @@ void orthogonalise_small(int64_t batch, int64_t rows, int64_t cols, const T* g, 
         a.step[k] = {sa / (sx * sx), c[3 * k + 1] * sb / sa, c[3 * k + 2] * sb / (sa * sa), c[3 * k] * to / sx, to / (sb * sx)};
     }
     const int n = (int)padded(std::max(rows, cols));
-    auto kernel = orth_small_kernel<T>;
-    static std::atomic<uint64_t> allowed{0};                 // devices that know how much LDS the kernel takes
-    int device = 0;
-    (void)hipGetDevice(&device);
-    const uint64_t bit = 1ull << (device & 63);
-    if (!(allowed.load(std::memory_order_relaxed) & bit) &&
-        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)small_lds(kSmallLong)) == hipSuccess)
-        allowed.fetch_or(bit, std::memory_order_relaxed);
+    constexpr auto kernel = orth_small_kernel<T>;
+    allow_lds<kernel>((int)small_lds(kSmallLong));
     hipLaunchKernelGGL(kernel, dim3((unsigned)batch), dim3(kSmallThreads), small_lds(n), s, g, out, a, n);
 }
 

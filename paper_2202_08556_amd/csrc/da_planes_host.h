@@ -4,7 +4,6 @@
 #include "da_planes.h"
 
 #include <algorithm>
-#include <atomic>
 
 namespace daspmm {
 namespace {
@@ -69,14 +68,8 @@ inline size_t plane_part_bytes(const PlanePlan& p, int64_t batches) {
 
 template <class P, class S, int ALAY, int BLAY, int BOUND, class E>
 void plane_launch(const PlaneArgs& g, const E& epi, const PlanePlan& p, int batches, hipStream_t s) {
-    auto kernel = plane_kernel<P, S, ALAY, BLAY, BOUND, E>;
-    static std::atomic<uint64_t> allowed{0};                 // devices that know how much LDS the kernel takes
-    int device = 0;
-    (void)hipGetDevice(&device);
-    const uint64_t bit = 1ull << (device & 63);
-    if (!(allowed.load(std::memory_order_relaxed) & bit) &&
-        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) == hipSuccess)
-        allowed.fetch_or(bit, std::memory_order_relaxed);
+    constexpr auto kernel = plane_kernel<P, S, ALAY, BLAY, BOUND, E>;
+    allow_lds<kernel>(S::LDS);
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles, (unsigned)p.splits, (unsigned)batches), dim3(S::THREADS), S::LDS, s, g, epi);
 }
 
