@@ -112,7 +112,7 @@ def optimizers(model: NodeClassifier, lr: float = 0.02) -> list[torch.optim.Opti
     """Orthogonalised updates for the blocks' matrices, Adam for everything else."""
     matrices = [p for p in model.blocks.parameters() if p.dim() == 2]
     ids = {id(p) for p in matrices}
-    return [OrthogonalMomentum(matrices, lr=lr), torch.optim.Adam([p for p in model.parameters() if id(p) not in ids], lr=3e-3)]
+    return [OrthogonalMomentum(matrices, lr=lr, out_axis=-1), torch.optim.Adam([p for p in model.parameters() if id(p) not in ids], lr=3e-3)]
 
 
 def label_step(model: NodeClassifier, optimizers: list[torch.optim.Optimizer], graph: SparseGraph, X: torch.Tensor, offsets: torch.Tensor,

@@ -50,22 +50,35 @@ def orthogonalise(update: torch.Tensor, steps: int = 5, coefficients=COEFFICIENT
 
 
 class OrthogonalMomentum(torch.optim.Optimizer):
-    """p <- (1 - lr weight_decay) p - lr max(1, rows / columns)^(1/2) orthogonalise(momentum of the gradient), for weights
+    """p <- (1 - lr weight_decay) p - lr max(1, outputs / inputs)^(1/2) orthogonalise(momentum of the gradient), for weights
     that are matrices (the last two axes); other parameters belong to another optimizer.  Weights of one shape and type are
-    orthogonalised in one call."""
+    orthogonalised in one call.
+
+    out_axis says which axis of a weight goes along its layer's outputs: -2, the rows, as in torch.nn.Linear, or -1 for weights
+    (in, out) like those of GraphConv, GatedFeedForward and linear_cross_entropy.  It can differ by parameter group."""
 
     def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
-                 steps: int = 5, coefficients=COEFFICIENTS, eps: float = 1e-7):
+                 steps: int = 5, coefficients=COEFFICIENTS, eps: float = 1e-7, out_axis: int = -2):
         if lr < 0.0 or not 0.0 <= momentum < 1.0 or weight_decay < 0.0:
             raise ValueError("lr and weight_decay must not be negative, momentum in [0, 1)")
         super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps,
-                                      coefficients=coefficients, eps=eps))
+                                      coefficients=coefficients, eps=eps, out_axis=out_axis))
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        for group in self.param_groups:                      # saved before there was a choice
+            group.setdefault("out_axis", -2)
 
     def add_param_group(self, group):
         super().add_param_group(group)
+        wrong = None
         if any(p.dim() < 2 for p in self.param_groups[-1]["params"]):
+            wrong = "OrthogonalMomentum takes matrices; give vectors and numbers to another optimizer"
+        elif self.param_groups[-1]["out_axis"] not in (-1, -2):
+            wrong = "out_axis must be -2 (weights (out, in)) or -1 (weights (in, out))"
+        if wrong:
             self.param_groups.pop()
-            raise ValueError("OrthogonalMomentum takes matrices; give vectors and numbers to another optimizer")
+            raise ValueError(wrong)
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -87,7 +100,8 @@ class OrthogonalMomentum(torch.optim.Optimizer):
             for (shape, _, _), pairs in alike.items():
                 many = torch.stack([u for _, u in pairs]) if len(pairs) > 1 else pairs[0][1].unsqueeze(0)
                 turned = orthogonalise(many, group["steps"], group["coefficients"], group["eps"])
-                size = group["lr"] * max(1.0, shape[-2] / shape[-1]) ** 0.5 if shape[-1] else 0.0
+                outputs, inputs = shape[group["out_axis"]], shape[-3 - group["out_axis"]]
+                size = group["lr"] * max(1.0, outputs / inputs) ** 0.5 if inputs else 0.0
                 for (p, _), t in zip(pairs, turned):
                     if group["weight_decay"]:
                         p.mul_(1.0 - group["lr"] * group["weight_decay"])

@@ -1,0 +1,65 @@
+"""OrthogonalMomentum without a GPU: what it does around the orthogonalised update, with another operation in its place."""
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2202_08556_amd import optim
+from paper_2202_08556_amd.node_classifier import NodeClassifier, optimizers
+
+README = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")
+
+
+@pytest.fixture
+def as_it_is(monkeypatch):
+    """orthogonalise hands its update back; what it was given is kept."""
+    given = []
+
+    def same(update, *_):
+        given.append(update)
+        return update.clone()
+
+    monkeypatch.setattr(optim, "orthogonalise", same)
+    return given
+
+
+def step(shape, **kw):
+    p = torch.nn.Parameter(torch.zeros(shape))
+    p.grad = torch.ones(shape)
+    optim.OrthogonalMomentum([p], lr=1.0, momentum=0.0, nesterov=False, **kw).step()
+    return float(-p.detach().flatten()[0])
+
+
+def test_factor_by_the_axis_of_the_outputs(as_it_is):
+    """max(1, outputs / inputs)^(1/2), for weights (out, in) and (in, out)."""
+    assert step((8, 2)) == 2.0 and step((2, 8)) == 1.0 and step((3, 8, 2)) == 2.0
+    assert step((8, 2), out_axis=-1) == 1.0 and step((2, 8), out_axis=-1) == 2.0 and step((3, 2, 8), out_axis=-1) == 2.0
+    for bad in (0, 1, -3, None):
+        with pytest.raises(ValueError):
+            step((2, 8), out_axis=bad)
+
+
+def test_factor_of_the_framework_s_own_weights(as_it_is):
+    """A layer that widens takes the larger step, one that narrows does not: their weights are (in, out)."""
+    model = NodeClassifier(4, 8, 3)
+    before = {n: p.detach().clone() for n, p in model.named_parameters()}
+    for p in model.parameters():
+        p.grad = torch.ones_like(p)
+    optimizers(model, lr=1.0)[0].step()
+    moved = {n: float((before[n] - p.detach()).flatten()[0]) for n, p in model.named_parameters() if p.dim() == 2 and "blocks" in n}
+    update = 1.0 + 0.95                                      # gradient 1 and the momentum's share of it
+    for name, by in (("w_up", 2.0), ("w_gate", 2.0), ("w_down", 1.0), ("conv.weight", 1.0)):
+        got = [v for n, v in moved.items() if n.endswith(name)]
+        assert len(got) == 2 and all(abs(v - by * update) < 1e-5 for v in got), (name, got)
+
+
+def test_states_saved_without_the_choice(as_it_is):
+    p = torch.nn.Parameter(torch.zeros(2, 8))
+    opt = optim.OrthogonalMomentum([p], lr=1.0)
+    saved = opt.state_dict()
+    del saved["param_groups"][0]["out_axis"]
+    opt.load_state_dict(saved)
+    p.grad = torch.ones(2, 8)
+    opt.step()
+    assert opt.param_groups[0]["out_axis"] == -2 and float(-p.detach()[0, 0]) == pytest.approx(1.95)
