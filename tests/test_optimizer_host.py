@@ -63,3 +63,11 @@ def test_states_saved_without_the_choice(as_it_is):
     p.grad = torch.ones(2, 8)
     opt.step()
     assert opt.param_groups[0]["out_axis"] == -2 and float(-p.detach()[0, 0]) == pytest.approx(1.95)
+
+
+def test_the_readme_s_optimizer():
+    """The line of README.md runs as it is written, on a model with vectors among its blocks' parameters."""
+    line, = re.findall(r"^step = (optim\..*?)(?:  +#.*)?$", open(README).read(), flags=re.M)
+    model = NodeClassifier(4, 8, 3, norm="rms")
+    step = eval(line, {"optim": optim, "model": model})
+    assert all(p.dim() == 2 for g in step.param_groups for p in g["params"]) and step.param_groups[0]["out_axis"] == -1
