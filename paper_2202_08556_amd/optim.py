@@ -55,7 +55,9 @@ class OrthogonalMomentum(torch.optim.Optimizer):
     orthogonalised in one call.
 
     out_axis says which axis of a weight goes along its layer's outputs: -2, the rows, as in torch.nn.Linear, or -1 for weights
-    (in, out) like those of GraphConv, GatedFeedForward and linear_cross_entropy.  It can differ by parameter group."""
+    (in, out) like those of GraphConv, GatedFeedForward and linear_cross_entropy.  It can differ by parameter group.
+
+    The momentum is held in float32 whatever the weight's type, and rounded to that once for what is orthogonalised."""
 
     def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
                  steps: int = 5, coefficients=COEFFICIENTS, eps: float = 1e-7, out_axis: int = -2):
@@ -68,6 +70,15 @@ class OrthogonalMomentum(torch.optim.Optimizer):
         super().__setstate__(state)
         for group in self.param_groups:                      # saved before there was a choice
             group.setdefault("out_axis", -2)
+
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)
+        # torch rounds a state to the type of its parameter
+        ids = [i for group in state_dict["param_groups"] for i in group["params"]]
+        for i, p in zip(ids, [p for group in self.param_groups for p in group["params"]]):
+            kept = state_dict["state"].get(i, {}).get("momentum")
+            if kept is not None:
+                self.state[p]["momentum"] = kept.detach().to(p.device, torch.float32, copy=True)
 
     def add_param_group(self, group):
         super().add_param_group(group)
@@ -93,9 +104,9 @@ class OrthogonalMomentum(torch.optim.Optimizer):
                     continue
                 state = self.state[p]
                 if "momentum" not in state:
-                    state["momentum"] = torch.zeros_like(p)
+                    state["momentum"] = torch.zeros_like(p, dtype=torch.float32)
                 m = state["momentum"].mul_(group["momentum"]).add_(p.grad)
-                update = p.grad.add(m, alpha=group["momentum"]) if group["nesterov"] else m
+                update = (p.grad.add(m, alpha=group["momentum"]) if group["nesterov"] else m).to(p.dtype)
                 alike.setdefault((p.shape, p.dtype, p.device), []).append((p, update))
             for (shape, _, _), pairs in alike.items():
                 many = torch.stack([u for _, u in pairs]) if len(pairs) > 1 else pairs[0][1].unsqueeze(0)

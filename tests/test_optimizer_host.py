@@ -71,3 +71,24 @@ def test_the_readme_s_optimizer():
     model = NodeClassifier(4, 8, 3, norm="rms")
     step = eval(line, {"optim": optim, "model": model})
     assert all(p.dim() == 2 for g in step.param_groups for p in g["params"]) and step.param_groups[0]["out_axis"] == -1
+
+
+def test_momentum_is_held_in_32_bits(as_it_is):
+    """bfloat16 weights: 200 steps of one gradient bring a momentum of 0.99 to (1 - 0.99^200) / 0.01 times it, off by no more than
+    a rounding to 32 bits a step; what is orthogonalised has the weight's type and one rounding.  Also after saving and loading."""
+    p = torch.nn.Parameter(torch.zeros(2, 8, dtype=torch.bfloat16))
+    opt = optim.OrthogonalMomentum([p], lr=1e-3, momentum=0.99, nesterov=False)
+    g = torch.linspace(0.5, 1.5, 16).view(2, 8).to(torch.bfloat16)
+    for k in range(200):
+        if k == 100:
+            other = torch.nn.Parameter(p.detach().clone())
+            again = optim.OrthogonalMomentum([other], lr=1e-3, momentum=0.99, nesterov=False)
+            again.load_state_dict(opt.state_dict())
+            p, opt = other, again
+        p.grad = g.clone()
+        opt.step()
+    want = g.double() * (1 - 0.99 ** 200) / 0.01
+    held = opt.state[p]["momentum"]
+    assert held.dtype == torch.float32 and ((held.double() - want).abs() <= 200 * 2.0 ** -24 * want).all()
+    last = as_it_is[-1]
+    assert last.dtype == torch.bfloat16 and ((last[0].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -16) * want).all()
