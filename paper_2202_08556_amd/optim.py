@@ -14,6 +14,7 @@ from . import binding as da  # noqa: F401  (loads the library)
 
 # a, b, c of X <- a X + (b A + c A^2) X, A = X X^T: singular values between 0.01 and 1 come to 0.7 .. 1.2 in five steps
 COEFFICIENTS = (3.4445, -4.775, 2.0315)
+MATRICES = 65535                             # that a call takes
 
 
 class _Orthogonalise(torch.autograd.Function):
@@ -52,7 +53,7 @@ def orthogonalise(update: torch.Tensor, steps: int = 5, coefficients=COEFFICIENT
 class OrthogonalMomentum(torch.optim.Optimizer):
     """p <- (1 - lr weight_decay) p - lr max(1, outputs / inputs)^(1/2) orthogonalise(momentum of the gradient), for weights
     that are matrices (the last two axes); other parameters belong to another optimizer.  Weights of one shape and type are
-    orthogonalised in one call.
+    orthogonalised in one call, 65535 matrices at most.
 
     out_axis says which axis of a weight goes along its layer's outputs: -2, the rows, as in torch.nn.Linear, or -1 for weights
     (in, out) like those of GraphConv, GatedFeedForward and linear_cross_entropy.  It can differ by parameter group.
@@ -109,8 +110,12 @@ class OrthogonalMomentum(torch.optim.Optimizer):
                 update = (p.grad.add(m, alpha=group["momentum"]) if group["nesterov"] else m).to(p.dtype)
                 alike.setdefault((p.shape, p.dtype, p.device), []).append((p, update))
             for (shape, _, _), pairs in alike.items():
-                many = torch.stack([u for _, u in pairs]) if len(pairs) > 1 else pairs[0][1].unsqueeze(0)
-                turned = orthogonalise(many, group["steps"], group["coefficients"], group["eps"])
+                most = max(1, MATRICES // max(1, shape[:-2].numel()))
+                turned = []
+                for k in range(0, len(pairs), most):
+                    some = [u for _, u in pairs[k:k + most]]
+                    many = torch.stack(some) if len(some) > 1 else some[0].unsqueeze(0)
+                    turned += orthogonalise(many, group["steps"], group["coefficients"], group["eps"])
                 outputs, inputs = shape[group["out_axis"]], shape[-3 - group["out_axis"]]
                 size = group["lr"] * max(1.0, outputs / inputs) ** 0.5 if inputs else 0.0
                 for (p, _), t in zip(pairs, turned):

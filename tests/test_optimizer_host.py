@@ -92,3 +92,13 @@ def test_momentum_is_held_in_32_bits(as_it_is):
     assert held.dtype == torch.float32 and ((held.double() - want).abs() <= 200 * 2.0 ** -24 * want).all()
     last = as_it_is[-1]
     assert last.dtype == torch.bfloat16 and ((last[0].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -16) * want).all()
+
+
+def test_more_matrices_than_a_call_takes(as_it_is):
+    """Weights of one shape go in as few calls as take 65535 matrices at most each."""
+    params = [torch.nn.Parameter(torch.zeros(30000, 1, 2)) for _ in range(5)]
+    for i, p in enumerate(params):
+        p.grad = torch.full_like(p, float(i + 1))
+    optim.OrthogonalMomentum(params, lr=1.0, momentum=0.0, nesterov=False).step()
+    assert [u.shape[0] * u.shape[1] for u in as_it_is] == [60000, 60000, 30000]
+    assert all((p.detach() == -(i + 1.0)).all() for i, p in enumerate(params))
