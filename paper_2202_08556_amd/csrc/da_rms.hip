@@ -96,9 +96,10 @@ __device__ __forceinline__ void team_join(float (&x)[COUNT], int P, int waves, f
 }
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 
-// Squares of numbers this large or small are no floats any more: the row is taken times 2^-70 or 2^60 then (1 otherwise)
+// Squares of numbers this large or small are no floats any more: the row is taken times 2^-76 or 2^60 then (1 otherwise).  2^20 squares of
+// numbers below 2^(128 - 76) are below 2^124, and the largest of a row whose squares come to 1e38 is 2^53 at least.
 __device__ __forceinline__ float other_scale(float sum, float inv, float eps) {
-    if (!(sum < 1e38f)) return 0x1p-70f;
+    if (!(sum < 1e38f)) return 0x1p-76f;
     return sum * inv + eps < 1e-24f && sum > 0.f || (sum == 0.f && eps < 1e-24f) ? 0x1p60f : 1.f;
 }
 
