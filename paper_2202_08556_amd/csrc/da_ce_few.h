@@ -339,7 +339,8 @@ template <class T, int R> __global__ __launch_bounds__(kFewBlock) void ce_few_pr
     for (int i = tid; i < K * R; i += kFewBlock) {
         const int k = k0 + i / R, r = i % R;
         if (k >= a.d || r >= a.rows) continue;
-        const float one[1] = {(sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i])};
+        // without a target 0, also where the weight holds infinities
+        const float one[1] = {a.kept_target[r] >= 0 ? (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]) : 0.f};
         if (gridDim.y > 1) a.dx_part[((long)blockIdx.y * a.rows + r) * a.d + k] = one[0];
         else store_floats<1>(static_cast<T*>(a.dx) + (long)r * a.d + k, one);
     }

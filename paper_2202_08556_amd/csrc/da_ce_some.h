@@ -243,8 +243,9 @@ template <class T, int RF> __global__ __launch_bounds__(kFewBlock, some_blocks(R
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int r = f * 16 + 4 * h + q;
-            const float one[1] = {(dx[f][0][q] + dx[f][1][q]) + (dx[f][2][q] + dx[f][3][q])};
             if (r >= a.rows) break;
+            // without a target 0, also where the weight holds infinities
+            const float one[1] = {a.kept_target[r] >= 0 ? (dx[f][0][q] + dx[f][1][q]) + (dx[f][2][q] + dx[f][3][q]) : 0.f};
             if (gridDim.y > 1) a.dx_part[((long)blockIdx.y * a.rows + r) * a.d + k + i16] = one[0];
             else store_floats<1>(static_cast<T*>(a.dx) + (long)r * a.d + k + i16, one);
         }

@@ -161,6 +161,23 @@ def test_bad_rows_stay_by_themselves(way, dtype):
 
 @EACH
 @TYPES
+def test_infinite_weights(way, dtype):
+    """Rows without a target get no gradient whatever the weight holds."""
+    x, w, b, t, g = make(way, dtype)
+    t[: (x.shape[0] + 1) // 2] = -1
+    w = w.clone()
+    w[5, 7], w[6, 40] = float("inf"), float("nan")
+    takes(way, x, w, b, t, g)
+    loss, dx, dw, db = run(x, w, b, t, g)
+    assert not loss[t < 0].any() and not dx[t < 0].any()
+    assert torch.isnan(loss[t >= 0]).all() and torch.isnan(dx[t >= 0]).any(1).all()
+    t[:] = -1
+    loss, dx, dw, db = run(x, w, b, t, g)
+    assert not loss.any() and not dx.any() and not dw.any() and not db.any()
+
+
+@EACH
+@TYPES
 def test_strides_types_and_axes(way, dtype):
     x, w, b, t, g = make(way, dtype, share=0.9)
     rows, d = x.shape
