@@ -61,9 +61,12 @@ int da_rms_norm_backward(int dtype, int64_t rows, int64_t channels, const void *
  *   dloss     float32, like loss; dloss_stride (DA_LOSS_ROWS) 0 takes dloss[0] for every row
  *   dx, dw, db   dense, of the types of x, w and b; any of them may be NULL and is then not computed
  *
- * The backward call computes the logits again.  float32 is multiplied as pairs of 16-bit halves (22 bits of a number below
- * 2^18 times less than the largest of its array; others are off by 2^-40 of that), sums are held in 32 bits; with bfloat16
- * dz is rounded, since it is an operand of the matrix cores.  Limits: rows <= 2^26, d, classes <= 2^22, and fewer than 2^23
+ * The backward call computes the logits again; sums are held in 32 bits.  Up to 128 classes of up to 256 inner positions (with
+ * many of both: up to 64 classes), and up to 64 rows (bfloat16: 16), the products are of 32-bit numbers for both types.  Beyond that operands are
+ * packed for the 16-bit matrix cores.  With bfloat16 dz is rounded then; float32 is multiplied as pairs of halves, 22 bits of a
+ * number, fewer of small ones: those of a row of x are off by up to 2^-35 of the row's largest, those of dz by 2^-40 of the row's factor, those of w by
+ * 2^-40 of the largest of all.  Loss and dx of a row do not depend on other rows; to dw a row adds with an error of up to 2^-37 of
+ * the largest product of any row's largest x and its factor.  Limits: rows <= 2^26, d, classes <= 2^22, and fewer than 2^23
  * tiles of 256 x 256 of any of the products' results (DA_ERR_UNSUPPORTED beyond).
  */
 enum { DA_LOSS_ROWS = 0, DA_LOSS_SUM = 1, DA_LOSS_MEAN = 2 };

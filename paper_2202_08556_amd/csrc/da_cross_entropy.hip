@@ -7,6 +7,8 @@
 // products read: eight operations for each of rows x d x classes instead of six, and no logits in memory.
 // Rows that have a target are gathered first (x is packed for the products anyway), and the products stop at their number,
 // which only the device knows: rows without one cost nothing and may hold anything.
+// The scales by row cost 1 to 3 % (float32, 4096 x 1024 x 8192: 775 and 778 us, rows far apart 765 and 795), and a packing of x where the rows' factors
+// differ (100000 x 700 x 130: 959 and 1114).
 // 4096 x 2048 x 65536 bf16, forward and backward: 3745 us, 1180 TFLOP/s; the four products 890 to 1020 each, the more the larger
 // their epilogues.
 #include "da_training.h"
@@ -36,53 +38,84 @@ struct CeStats {
     int *count, *index, *target;             // rows that have a target: how many, which, and which class
     int* place;                              // of every row in that list; -1: not there
     float* lse;
+    int* shift;                              // packed float32: that of a row of x in the list by itself
     uint32_t* maxes;                         // kMaxX and so on
 };
 constexpr size_t kStatsHead = 32;
-size_t stats_bytes(int64_t rows) { return kStatsHead + 4 * round16((size_t)rows * 4); }
+size_t stats_bytes(int64_t rows, bool shifts) { return kStatsHead + (shifts ? 5 : 4) * round16((size_t)rows * 4); }
 CeStats ce_stats(void* p, int64_t rows) {
     char* c = static_cast<char*>(p);
     const size_t n = round16((size_t)rows * 4);
     auto ints = [&](size_t at) { return reinterpret_cast<int*>(c + at); };
     return {ints(0), ints(kStatsHead), ints(kStatsHead + n), ints(kStatsHead + 2 * n), reinterpret_cast<float*>(c + kStatsHead + 3 * n),
-            reinterpret_cast<uint32_t*>(c + 16)};
+            ints(kStatsHead + 4 * n), reinterpret_cast<uint32_t*>(c + 16)};
 }
 
-// Largest magnitudes of x and w, as bits, and a count of blocks; scale: the power of two that takes them to 2^14 .. 2^15
-enum { kMaxX = 0, kMaxW = 1, kArrived = 2, kMaxes = 4 };
-struct Scale {
-    float by, inv;
-};
-__device__ __forceinline__ Scale scale_of(uint32_t bits) {
+// Numbers leave for the packed halves times a power of two that takes the largest to 2^14 .. 2^15; `shift` is its exponent.  w has one.  A
+// row of x has that of the whole x, or its own where it is more than 2^kNear times smaller, and a row of dz that of its factor: what
+// a row's results are off by does not depend on other rows.
+// Of x and w: the largest magnitude as bits, and that of the rows' own shifts; and a count of blocks.
+enum { kMaxX = 0, kMaxW = 1, kArrived = 2, kRowX = 3, kMaxes = 4 };
+constexpr int kNear = 4, kNoShift = -1000, kShiftBias = 512;     // kNoShift: a row of zeros
+__device__ __forceinline__ int shift_of(uint32_t bits) {
     const float most = __uint_as_float(bits);
-    int e = 0;
+    int e = 15;
     if (most > 0.f) (void)frexpf(most, &e);                  // most < 2^e
-    else e = 15;
-    const int k = min(126, max(-126, 15 - e));
-    return {ldexpf(1.f, k), ldexpf(1.f, -k)};
+    return 15 - e;
 }
-template <class P> __device__ __forceinline__ Scale scale_at(const uint32_t* maxes, int which) {
-    if constexpr (P::N == 1) return {1.f, 1.f};
-    return scale_of(maxes[which]);
+__device__ __forceinline__ float magnitude(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.f;                   // infinities and NaN have no part in a scale
+}
+__device__ __forceinline__ int shift_of_row(const CeStats& st, int m) {
+    const int own = st.shift[m], all = shift_of(st.maxes[kMaxX]);
+    return own > all + kNear ? own : all;
+}
+// whether a row of x has its own
+__device__ __forceinline__ bool rows_differ(const CeStats& st) {
+    return (int)st.maxes[kRowX] - kShiftBias > shift_of(st.maxes[kMaxX]) + kNear;
 }
 
 // The gradient of the loss: of the rows, or one factor for all of them
 struct Upstream {
     const float* dloss;
     long stride;
-    const uint32_t* largest;     // of the rows' factors
     int reduction;
     const int *count, *index;
     __device__ __forceinline__ float all() const { return reduction == DA_LOSS_MEAN ? dloss[0] / (float)max(1, *count) : dloss[0]; }
     __device__ __forceinline__ float row(int m) const { return reduction == DA_LOSS_ROWS ? dloss[index[m] * stride] : all(); }
+    // of a row of dz; which numbers it takes to 2^14 .. 2^15 follows from the factor alone, since dz is at most that
+    __device__ __forceinline__ int shift(float factor) const { return shift_of(__float_as_uint(magnitude(factor))); }
 };
-__device__ __forceinline__ float magnitude(float x) {
-    const float a = fabsf(x);
-    return a <= 3.402823466e38f ? a : 0.f;                   // infinities and NaN have no part in a scale
+
+// dw adds rows, so x and dz of a row have to come times the same power of two together, 2^sum: where rows of x or of dz have shifts of
+// their own, x is packed a second time, times what dz lacks.  sum is the smallest of a row's two shifts together: the row
+// that adds most has all its bits, the others theirs from 2^-38 of its numbers on.
+struct Joint {
+    int sum, differ;
+};
+struct FactorPart {
+    int sum, least, most;        // of some rows: the smallest sum of shifts, the smallest and the largest shift of dz
+};
+__device__ __forceinline__ FactorPart joined(const FactorPart& a, const FactorPart& b) {
+    return {min(a.sum, b.sum), min(a.least, b.least), max(a.most, b.most)};
 }
-template <class P> __device__ __forceinline__ Scale scale_of_gradient(const Upstream& u) {
-    if constexpr (P::N == 1) return {1.f, 1.f};
-    return scale_of(u.reduction == DA_LOSS_ROWS ? *u.largest : __float_as_uint(magnitude(u.all())));
+__device__ __forceinline__ FactorPart no_rows() { return {1 << 20, 1 << 20, -(1 << 20)}; }
+// all 256 threads' in every thread
+__device__ __forceinline__ FactorPart block_joined(FactorPart p) {
+    __shared__ FactorPart red[4];
+    for (int d = 1; d < 64; d <<= 1) p = joined(p, {__shfl_xor(p.sum, d, 64), __shfl_xor(p.least, d, 64), __shfl_xor(p.most, d, 64)});
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = p;
+    __syncthreads();
+    return joined(joined(red[0], red[1]), joined(red[2], red[3]));
+}
+constexpr int kFactorParts = 256;
+__device__ __forceinline__ Joint joint_of(const CeStats& st, const Upstream& u, const FactorPart* part, int parts) {
+    if (u.reduction != DA_LOSS_ROWS) return {shift_of(st.maxes[kMaxX]) + u.shift(u.all()), rows_differ(st)};
+    const FactorPart p = block_joined((int)threadIdx.x < parts ? part[threadIdx.x] : no_rows());
+    if (p.least > p.most) return {0, 0};
+    const bool differ = rows_differ(st) || p.least != p.most;
+    return {differ ? p.sum : shift_of(st.maxes[kMaxX]) + p.least, differ};
 }
 
 __device__ __forceinline__ long target_of(const void* t, int wide, long r) {
@@ -146,45 +179,56 @@ __global__ __launch_bounds__(256) void ce_index_kernel(const void* __restrict__ 
 }
 
 // The largest of a block's; the order of the blocks does not show
-__device__ __forceinline__ void keep_largest(float most, uint32_t* to) {
-    __shared__ float red[4];
-    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+__device__ __forceinline__ void keep_largest(uint32_t most, uint32_t* to) {
+    __shared__ uint32_t red[4];
+    for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d, 64));
+    __syncthreads();                                         // those of a call before have been read
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = most;
     __syncthreads();
     if (threadIdx.x == 0) {
-        most = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        most = max(max(red[0], red[1]), max(red[2], red[3]));
         // most blocks find a larger one there
-        if (__float_as_uint(most) > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, __float_as_uint(most));
+        if (most > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, most);
     }
 }
-// Largest finite magnitudes: blockIdx.y 0 of the rows of x that count, 1 of w
+// Largest finite magnitudes: blockIdx.y 0 of the rows of x that count, and their shifts, 1 of w
 __global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x, long ldx, CeStats st, long d, const float* __restrict__ w,
                                                      long numbers)
 {
-    float most = 0.f;
+    uint32_t most = 0;                                       // of floats that are not negative bits are in order
     if (blockIdx.y == 0) {
         const int count = *st.count, lane = threadIdx.x & 63;
+        uint32_t far = 0;
         for (long m = (long)blockIdx.x * 4 + (threadIdx.x >> 6); m < count; m += (long)gridDim.x * 4) {
             const float* __restrict__ row = x + (long)st.index[m] * ldx;
+            float here = 0.f;
             long c = lane * 4;
             for (; c + 4 <= d; c += 256) {
                 float v[4];
                 load_floats<4>(row + c, v);
-                most = fmaxf(fmaxf(most, fmaxf(magnitude(v[0]), magnitude(v[1]))), fmaxf(magnitude(v[2]), magnitude(v[3])));
+                here = fmaxf(fmaxf(here, fmaxf(magnitude(v[0]), magnitude(v[1]))), fmaxf(magnitude(v[2]), magnitude(v[3])));
             }
-            for (; c < d; ++c) most = fmaxf(most, magnitude(row[c]));
+            for (; c < d; ++c) here = fmaxf(here, magnitude(row[c]));
+            for (int k = 1; k < 64; k <<= 1) here = fmaxf(here, __shfl_xor(here, k, 64));
+            const int shift = shift_of(__float_as_uint(here));
+            if (lane == 0) st.shift[m] = here > 0.f ? shift : kNoShift;
+            if (here > 0.f) far = max(far, (uint32_t)(shift + kShiftBias));
+            most = max(most, __float_as_uint(here));
         }
+        keep_largest(far, st.maxes + kRowX);
     } else {
+        float here = 0.f;
         const long step = (long)gridDim.x * 1024;
         for (long c = ((long)blockIdx.x * 256 + threadIdx.x) * 4; c < numbers; c += step) {
             if (c + 4 <= numbers) {
                 float v[4];
                 load_floats<4>(w + c, v);
-                most = fmaxf(fmaxf(most, fmaxf(magnitude(v[0]), magnitude(v[1]))), fmaxf(magnitude(v[2]), magnitude(v[3])));
+                here = fmaxf(fmaxf(here, fmaxf(magnitude(v[0]), magnitude(v[1]))), fmaxf(magnitude(v[2]), magnitude(v[3])));
             } else {
-                for (long i = c; i < numbers; ++i) most = fmaxf(most, magnitude(w[i]));
+                for (long i = c; i < numbers; ++i) here = fmaxf(here, magnitude(w[i]));
             }
         }
+        most = __float_as_uint(here);
     }
     keep_largest(most, st.maxes + (blockIdx.y == 0 ? kMaxX : kMaxW));
 }
@@ -207,22 +251,18 @@ template <class T> struct PackJob {
     long ld, lines;
     int n;
     const int *index, *count;    // not null: *count lines of a list, and zeros up to the next multiple of 64
-    int which;
     uint16_t* to;
     Packed layout;
 };
-// What a backward pass begins with beside that: no magnitude and no parts yet, and 0 in the rows of dx without a target
+// What a backward pass begins with beside that: no parts yet, and 0 in the rows of dx without a target
 template <class T> struct BeginJob {
     long rows;
     int d;
     T* dx;
-    uint32_t* largest;
     int* arrived;                // null: forward
     __device__ __forceinline__ void run(const CeStats& st) const {
-        if (blockIdx.x == 0) {
-            if (threadIdx.x == 0) *largest = 0;
+        if (blockIdx.x == 0)
             for (int k = threadIdx.x; k < kMostParted; k += 256) arrived[k] = 0;
-        }
         if (!dx) return;
         const int lane = threadIdx.x & 63;
         for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (long)gridDim.x * 4) {
@@ -234,12 +274,29 @@ template <class T> struct BeginJob {
         }
     }
 };
+// ... and, packed float32, x for dw
+struct JointJob {
+    Upstream u;
+    const FactorPart* part;
+    int parts;
+    Joint* joint;
+    uint16_t* to;
+};
+// blockIdx.y 0: x, 1: w, 2: begin, 3: x for dw
 template <class T, class P>
-__global__ __launch_bounds__(256) void ce_pack_kernel(CeStats st, PackJob<T> x, PackJob<T> w, BeginJob<T> begin)
+__global__ __launch_bounds__(256) void ce_pack_kernel(CeStats st, PackJob<T> x, PackJob<T> w, BeginJob<T> begin, JointJob again)
 {
     if (blockIdx.y == 2) return begin.run(st);
-    const PackJob<T>& j = blockIdx.y ? w : x;
-    const Scale s = scale_at<P>(st.maxes, j.which);
+    Joint joint{};
+    PackJob<T> j = blockIdx.y == 1 ? w : x;
+    if constexpr (P::N == 2) {
+        if (blockIdx.y == 3) {
+            joint = joint_of(st, again.u, again.part, again.parts);
+            if (blockIdx.x == 0 && threadIdx.x == 0) *again.joint = joint;
+            if (!joint.differ) return;
+            j.to = again.to;
+        }
+    }
     // 16 lines x 128 numbers at a time, four lines to a wave: whole lines of memory on both sides
     const int n = (int)padded(j.n), across = (n + 127) / 128;
     const long there = j.index ? *j.count : j.lines, tiles = (padded(there) / 16) * across;
@@ -263,10 +320,15 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(CeStats st, PackJob<T> x, 
                         x[i] = one[0];
                     }
             }
-        }
-        if constexpr (P::N == 2)
+            if constexpr (P::N == 2) {
+                // a row that adds nothing to dw, its factor 0 or none, is not in the joint sum: no more than its own shift
+                const int by = blockIdx.y == 1   ? shift_of(st.maxes[kMaxW])
+                               : blockIdx.y == 0 ? shift_of_row(st, (int)line)
+                                                 : min(joint.sum - again.u.shift(again.u.row((int)line)), max(st.shift[line], shift_of(st.maxes[kMaxX])));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= s.by;
+                for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i], by);
+            }
+        }
         put_values<P, 8>(j.to + place<P>(j.layout, line, at), x);
     }
 }
@@ -279,17 +341,16 @@ template <class P> struct Logits {
     int bias_type;
     int classes;
     CeStats st;
-    // A wave's logits from its sums: columns nw + 16 j + 4 h and on of row i16 of each 16 (the scales leave one after the other: their
-    // product may not be a float); -inf behind the last class
+    // A wave's logits from its sums: columns nw + 16 j + 4 h and on of row i16 of each 16 (both scales leave as one exponent: neither
+    // they nor their product need be floats); -inf behind the last class
     template <int NT> struct Columns {
-        Scale sx, sw;
+        int shift;                                           // of w
         float bias[NT][4];
         bool inside;
     };
     template <int NT> __device__ __forceinline__ Columns<NT> columns(int nw) const {
         Columns<NT> c;
-        c.sx = scale_at<P>(st.maxes, kMaxX);
-        c.sw = scale_at<P>(st.maxes, kMaxW);
+        c.shift = P::N == 2 ? shift_of(st.maxes[kMaxW]) : 0;
         c.inside = nw + NT * 16 <= classes;
         const int n = nw + 4 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
@@ -298,13 +359,15 @@ template <class P> struct Logits {
             for (int q = 0; q < 4; ++q) c.bias[j][q] = bias && n + j * 16 + q < classes ? load_param(bias, bias_type, n + j * 16 + q) : 0.f;
         return c;
     }
-    template <int NT> __device__ __forceinline__ void logits(const f32x4 (&acc)[NT], const Columns<NT>& c, int nw, float (&z)[NT][4]) const {
+    // shift: of the row of x
+    template <int NT>
+    __device__ __forceinline__ void logits(const f32x4 (&acc)[NT], const Columns<NT>& c, int shift, int nw, float (&z)[NT][4]) const {
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 z[j][q] = acc[j][q];
-                if constexpr (P::N == 2) z[j][q] = z[j][q] * c.sx.inv * c.sw.inv;
+                if constexpr (P::N == 2) z[j][q] = ldexpf(z[j][q], -(shift + c.shift));
             }
         if (bias)
 #pragma unroll
@@ -332,14 +395,18 @@ template <class P> struct SumsOut : Logits<P> {
     __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int slot, char*, int, int) const {
         const int i16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4, count = *this->st.count;
         const auto c = this->template columns<NT>(nw);
-        int t[MT];                                           // of the row, from the lane's first column on
+        int t[MT], shift[MT];                                // of the row; the target from the lane's first column on
 #pragma unroll
-        for (int i = 0; i < MT; ++i) t[i] = (mw + i * 16 + i16 < count ? this->st.target[mw + i * 16 + i16] : -0x40000000) - nw - 4 * h;
+        for (int i = 0; i < MT; ++i) {
+            const int m = mw + i * 16 + i16;
+            t[i] = (m < count ? this->st.target[m] : -0x40000000) - nw - 4 * h;
+            shift[i] = P::N == 2 && m < count ? shift_of_row(this->st, m) : 0;
+        }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int m = mw + i * 16 + i16;
             float z[NT][4], most = -INFINITY;
-            this->logits(acc[i], c, nw, z);
+            this->logits(acc[i], c, shift[i], nw, z);
             if (__any(t[i] >= 0 && t[i] < NT * 16))
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
@@ -378,21 +445,22 @@ template <class P> struct GradOut : Logits<P> {
         constexpr int BYTES = NT * 32 * P::N, PITCH = BYTES + 16, CHUNKS = BYTES / 16;
         const int lane = threadIdx.x & 63, i16 = lane & 15, h = lane >> 4, count = *this->st.count, n0 = first + nw;
         const auto c = this->template columns<NT>(n0);
-        const float up = scale_of_gradient<P>(u).by;
         float lse[MT], by[MT];
-        int t[MT];
+        int t[MT], shift[MT];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int m = mw + i * 16 + i16;
             const bool there = m < count;
             lse[i] = there ? this->st.lse[m] : 0.f;
-            by[i] = there ? u.row(m) * up : 0.f;
+            by[i] = there ? u.row(m) : 0.f;
+            if constexpr (P::N == 2) by[i] = ldexpf(by[i], u.shift(by[i]));
+            shift[i] = P::N == 2 && there ? shift_of_row(this->st, m) : 0;
             t[i] = (there ? this->st.target[m] : -0x40000000) - n0 - 4 * h;
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             float z[NT][4];
-            this->logits(acc[i], c, n0, z);
+            this->logits(acc[i], c, shift[i], n0, z);
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -436,10 +504,11 @@ template <class T, class P> struct InputOut {
     int d;
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
         if (m >= *st.count || n >= d) return;
-        const Scale sg = scale_of_gradient<P>(u), sw = scale_at<P>(st.maxes, kMaxW);
-        if constexpr (P::N == 2)
+        if constexpr (P::N == 2) {
+            const int down = -(shift_of(st.maxes[kMaxW]) + u.shift(u.row(m)));
 #pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = x[q] * sw.inv * sg.inv;
+            for (int q = 0; q < 4; ++q) x[q] = ldexpf(x[q], down);
+        }
         if (before) {
             float u[4];
             load_floats<4>(before + (long)m * ldb + n, u);
@@ -453,17 +522,17 @@ template <class T, class P> struct InputOut {
 
 template <class T, class P> struct WeightOut {
     static constexpr bool kSymmetric = false, kWhole = false;
-    const uint32_t* maxes;
-    Upstream u;
+    const Joint* joint;
     T* dw;                       // of the piece
     long ldw;
     int d, classes;              // of the piece
     __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
         if (m >= d || n >= classes) return;
-        const Scale sg = scale_of_gradient<P>(u), sx = scale_at<P>(maxes, kMaxX);
-        if constexpr (P::N == 2)
+        if constexpr (P::N == 2) {
+            const int down = -joint->sum;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = x[q] * sx.inv * sg.inv;
+            for (int q = 0; q < 4; ++q) x[q] = ldexpf(x[q], down);
+        }
         store_row(dw + (long)m * ldw + n, classes - n, x);
     }
 };
@@ -519,18 +588,24 @@ __global__ __launch_bounds__(256) void ce_join_kernel(CeStats st, const float2* 
     if (threadIdx.x == 0) *loss_all = (float)(mean ? total / max(1, count) : total);
 }
 
-// The largest factor of a row
-__global__ __launch_bounds__(256) void ce_factor_kernel(Upstream u, uint32_t* __restrict__ largest)
+// The rows' shifts that dw has to bring together, by parts of the rows
+__global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, Upstream u, FactorPart* __restrict__ part)
 {
     const int count = *u.count;
-    float most = 0.f;
-    for (long m = (long)blockIdx.x * 256 + threadIdx.x; m < count; m += (long)gridDim.x * 256) most = fmaxf(most, magnitude(u.row((int)m)));
-    keep_largest(most, largest);
+    FactorPart p = no_rows();
+    for (long m = (long)blockIdx.x * 256 + threadIdx.x; m < count; m += (long)gridDim.x * 256) {
+        const float g = magnitude(u.row((int)m));
+        const int own = st.shift[m], t = u.shift(g);
+        if (g > 0.f && own != kNoShift) p = joined(p, {own + t, t, t});
+    }
+    p = block_joined(p);
+    if (threadIdx.x == 0) part[blockIdx.x] = p;
 }
 
 // db: sums of dz's columns over parts of the rows, then over the parts
 template <class P>
-__global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t* __restrict__ dz, Packed lz, int Nb, long per, float* __restrict__ part)
+__global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, Upstream u, const uint16_t* __restrict__ dz, Packed lz, int Nb, long per,
+                                                      float* __restrict__ part)
 {
     __shared__ f32x4 red[4][64];
     const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4, k = threadIdx.x >> 6;
@@ -540,8 +615,9 @@ __global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t
         for (long m = r0 + k; m < r1; m += 4) {
             float x[4];
             get_values<P, 4>(dz + place<P>(lz, m, n), x);
+            const int down = P::N == 2 ? -u.shift(u.row((int)m)) : 0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s[q] += x[q];
+            for (int q = 0; q < 4; ++q) s[q] += P::N == 2 ? ldexpf(x[q], down) : x[q];
         }
     red[k][threadIdx.x & 63] = s;
     __syncthreads();
@@ -550,9 +626,8 @@ __global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, const uint16_t
         *reinterpret_cast<f32x4*>(part + (long)blockIdx.y * Nb + n) = (red[0][l] + red[1][l]) + (red[2][l] + red[3][l]);
     }
 }
-template <class P>
-__global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restrict__ part, int parts, int Nb, int classes,
-                                                           Upstream u, void* db, int type, int first)
+__global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restrict__ part, int parts, int Nb, int classes, void* db, int type,
+                                                           int first)
 {
     __shared__ float red[16][17];
     const int n = blockIdx.x * 16 + (threadIdx.x & 15), k0 = threadIdx.x >> 4;
@@ -569,7 +644,7 @@ __global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restri
     if (threadIdx.x < 16 && n < classes) {
         float t = 0.f;
         for (int i = 0; i < 16; ++i) t += red[i][threadIdx.x];
-        store_param(db, type, first + n, t * scale_of_gradient<P>(u).inv);
+        store_param(db, type, first + n, t);
     }
 }
 
@@ -697,13 +772,16 @@ struct CePlan {
     PiecePlan whole, rest;       // products of a whole piece and of the last one
     int bias_parts;
     size_t counts_at, sums_at, target_at, x_at, w_at, part_at, forward;          // bytes
-    size_t arrived_at, dz_at, dx_at, bias_at, sum_at, backward;
+    size_t arrived_at, dz_at, dx_at, bias_at, sum_at, again_at, factor_at, backward;
+    bool shifts() const { return !narrow.taken && !tall.taken && !few.taken && halves; }
+    bool halves;
 };
 
 int wave_columns(const PlanePlan& p) { return p.shape == 0 ? PlaneLarge::WN : PlaneSmall::WN; }
 
 CePlan make_ce_plan(int dtype, const CeShape& s) {
     CePlan p{};
+    p.halves = dtype == DA_F32;
     const int N = dtype == DA_F32 ? 2 : 1, step = N == 2 ? Halves::STEP : One::STEP;
     p.Ma = padded(s.rows);
     p.D = padded(s.d);
@@ -726,7 +804,7 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
         p.backward = p.tall_part + round16((size_t)p.tall.parts * (s.d + 1) * s.V * 4);
         return p;
     }
-    size_t at = 16;                                          // the largest factor of a row, or a count
+    size_t at = 16;                                          // Joint, or a count
     auto take = [&](size_t bytes) {
         const size_t from = at;
         at += round16(bytes);
@@ -770,6 +848,8 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
     p.rest = s.V % p.piece ? piece_plan(p.Ma, p.D, s.V % p.piece, step) : p.whole;
     for (const PiecePlan& q : {p.whole, p.rest}) sums = std::max({sums, plane_part_bytes(q.input, 1), plane_part_bytes(q.weight, 1)});
     p.sum_at = take(sums);
+    p.again_at = take(N == 2 ? (size_t)p.Ma * p.D * 2 * N : 0);
+    p.factor_at = take(N == 2 ? kFactorParts * sizeof(FactorPart) : 0);
     p.backward = at;
     return p;
 }
@@ -813,7 +893,7 @@ struct CeCall {
     hipStream_t stream;
 };
 
-template <class T> const uint16_t* pack_operands(const CeCall& c, const BeginJob<T>& begin, Packed* lw) {
+template <class T> const uint16_t* pack_operands(const CeCall& c, const BeginJob<T>& begin, const JointJob& again, Packed* lw) {
     typedef PlaneOf<T> P;
     const T* x = static_cast<const T*>(c.x);
     const T* w = static_cast<const T*>(c.w);
@@ -824,18 +904,18 @@ template <class T> const uint16_t* pack_operands(const CeCall& c, const BeginJob
                                (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V));
         }
     }
-    auto job = [&](const T* from, long ld, long lines, int n, const int* index, int which, size_t to) {
-        return PackJob<T>{from, ld, lines, n, index, c.st.count, which, reinterpret_cast<uint16_t*>(c.ws + to), packed(padded(lines), n, P::N)};
+    auto job = [&](const T* from, long ld, long lines, int n, const int* index, size_t to) {
+        return PackJob<T>{from, ld, lines, n, index, c.st.count, reinterpret_cast<uint16_t*>(c.ws + to), packed(padded(lines), n, P::N)};
     };
-    const PackJob<T> jx = job(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, kMaxX, c.p.x_at), jw = job(w, c.s.V, c.s.d, (int)c.s.V, nullptr, kMaxW, c.p.w_at);
+    const PackJob<T> jx = job(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, c.p.x_at), jw = job(w, c.s.V, c.s.d, (int)c.s.V, nullptr, c.p.w_at);
     // a weight of whole pads is read where it is
     const bool direct = P::N == 1 && c.s.d % kPad == 0 && c.s.V % kPad == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
     const int64_t tiles = std::max(c.p.Ma / 16 * ceil_div(c.p.D, 128), direct ? 0 : c.p.D / 16 * ceil_div(c.p.Vb, 128));
     PackJob<T> jw_here = jw;
     if (direct) jw_here.lines = jw_here.n = 0;
     if (tiles || begin.arrived)
-        hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(tiles, 8192)), begin.arrived ? 3 : direct ? 1 : 2),
-                           dim3(256), 0, c.stream, c.st, jx, jw_here, begin);
+        hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(tiles, 8192)), again.to ? 4 : begin.arrived ? 3 : direct ? 1 : 2),
+                           dim3(256), 0, c.stream, c.st, jx, jw_here, begin, again);
     *lw = direct ? packed_lines(c.s.V) : jw.layout;
     return direct ? reinterpret_cast<const uint16_t*>(w) : jw.to;
 }
@@ -873,7 +953,7 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
     hipLaunchKernelGGL(ce_index_kernel, dim3((unsigned)c.p.chunks), dim3(256), 0, c.stream, target, target64, (long)c.s.rows, (long)c.s.V,
                        (long)c.p.chunk, several ? counts : nullptr, c.st, rows);
     Packed lw{};
-    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{}, &lw);
+    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{}, JointJob{}, &lw);
     SumsOut<P> out{};
     fill(out, c);
     out.part = reinterpret_cast<float2*>(c.ws + c.p.part_at);
@@ -891,16 +971,20 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
 template <class T>
 void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, T* dx, T* dw, void* db) {
     typedef PlaneOf<T> P;
-    uint32_t* largest = reinterpret_cast<uint32_t*>(c.ws);
     int* arrived = reinterpret_cast<int*>(c.ws + c.p.arrived_at);
-    const Upstream u{dloss, (long)stride, largest, reduction, c.st.count, c.st.index};
+    Joint* joint = reinterpret_cast<Joint*>(c.ws);
+    const Upstream u{dloss, (long)stride, reduction, c.st.count, c.st.index};
     if (c.s.d == 0) dx = dw = nullptr;
+    JointJob again{};
+    if (P::N == 2 && dw && c.s.V > 0) {
+        FactorPart* factors = reinterpret_cast<FactorPart*>(c.ws + c.p.factor_at);
+        again = JointJob{u, factors, (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), kFactorParts)), joint,
+                         reinterpret_cast<uint16_t*>(c.ws + c.p.again_at)};
+        if (reduction == DA_LOSS_ROWS) hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)again.parts), dim3(256), 0, c.stream, c.st, u, factors);
+    }
     Packed lw{};
-    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{(long)c.s.rows, (int)c.s.d, dx, largest, arrived}, &lw);
+    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{(long)c.s.rows, (int)c.s.d, dx, arrived}, again, &lw);
     if (c.s.V == 0) return;
-    if (P::N == 2 && reduction == DA_LOSS_ROWS)              // whose scale dz takes
-        hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), 256))), dim3(256), 0,
-                           c.stream, u, largest);
     uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + c.p.dz_at);
     float* acc = reinterpret_cast<float*>(c.ws + c.p.dx_at);
     float* part = reinterpret_cast<float*>(c.ws + c.p.sum_at);
@@ -946,15 +1030,17 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             a.Nb = (int)Vb;
             a.K = (int)c.p.Ma;
             a.rows = c.st.count;
-            const WeightOut<T, P> out{c.st.maxes, u, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
+            a.other = again.to ? &joint->differ : nullptr;
+            a.A_other = again.to;
+            const WeightOut<T, P> out{joint, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
             plane_product<P, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, arrived, c.stream);
         }
         if (db) {
             const int64_t per = ceil_div(c.s.rows, c.p.bias_parts);
-            hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, dz, lz,
+            hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, u, dz, lz,
                                (int)Vb, (long)per, bias);
-            hipLaunchKernelGGL((ce_bias_join_kernel<P>), dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
-                               (int)width, u, db, c.param_dtype, (int)first);
+            hipLaunchKernelGGL(ce_bias_join_kernel, dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
+                               (int)width, db, c.param_dtype, (int)first);
         }
     }
 }
@@ -1189,7 +1275,7 @@ extern "C" int da_linear_cross_entropy_sizes(int dtype, int64_t rows, int64_t d,
     const int st = ce_check(dtype, rows, d, classes);
     if (st != DA_OK) return st;
     const CePlan& p = ce_plan(dtype, CeShape{rows, d, classes});
-    *stats = stats_bytes(rows);
+    *stats = stats_bytes(rows, p.shifts());
     *forward_bytes = p.forward;
     *backward_bytes = p.backward;
     return DA_OK;

@@ -2,7 +2,7 @@
 // products of them whose epilogues are those of the operators that use them.
 //
 // A number is one bf16 (One), or the sum of two fp16 (Halves): the nearest fp16 and what that leaves.  A pair has 22 bits;
-// the arrays are scaled by a power of two so that the largest number is below 2^15, and the second half of numbers 2^18
+// they come times a power of two, for an array or for each of its rows, that takes the largest below 2^15, and the second half of numbers 2^18
 // times less begins to lose bits, 2^-25 of the scale.  The product of two pairs is three instructions of 16-bit numbers
 // (the fourth, of both second halves, is below the 22 bits) in place of one of 32-bit numbers at a sixteenth of the rate.
 //
@@ -146,6 +146,8 @@ struct PlaneArgs {
     int Ma, Nb, K;
     int tiles_m, tiles_n;
     const int* rows;             // where not null: so many of the outer positions of A (kBoundM), or of the inner ones (kBoundK), are there
+    const int* other;            // kBoundK, where not null and not 0: the first operand is A_other
+    const uint16_t* A_other;
     int splits, per;             // parts of the sum, steps of one
     float* part;                 // splits > 1: [batch][tile][split], a tile's sums as its waves hold them
     int* arrived;                // ... [batch][tile], 0: how many of a tile's parts are there
@@ -234,7 +236,11 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         steps = min(steps, (*g.rows + STEP - 1) / STEP);
     }
     const int t0 = blockIdx.y * g.per, t1 = min(t0 + g.per, steps);
-    const char* const A = (const char*)(g.A + batch * g.batch_a);
+    const uint16_t* first = g.A;
+    if constexpr (BOUND == kBoundK) {
+        if (g.other && *g.other) first = g.A_other;
+    }
+    const char* const A = (const char*)(first + batch * g.batch_a);
     const char* const B = (const char*)(g.B + batch * g.batch_b);
 
     const unsigned lds_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;

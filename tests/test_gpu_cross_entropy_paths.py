@@ -177,6 +177,60 @@ def test_infinite_weights(way, dtype):
 
 
 @EACH
+def test_rows_of_very_different_size(way):
+    """float32: what a row's loss and gradient are off by does not depend on other rows."""
+    x, w, b, t, g = make(way, F32)
+    rows = x.shape[0]
+    size = torch.logspace(-6, 1, rows, device="cuda")
+    takes(way, x * size[:, None], w, b, t, g)
+    check(x * size[:, None], w, b, t, g * torch.logspace(-5, 0, rows, device="cuda"))
+    for k in (1e8, 1e12, 1e25):                              # one number, and one row's factor, far beyond the others
+        y, f = x.clone(), g.clone()
+        y[0, 0] = k
+        check(y, w, b, t, g)
+        f[rows // 2] = k
+        check(x, w, b, t, f)
+        check(y, w, b, t, f / k)
+    check(x, w, b, t, g * torch.logspace(-20, 0, rows, device="cuda"))
+    check(x * torch.logspace(-20, 0, rows, device="cuda")[:, None], w, b, t, g * torch.logspace(0, -20, rows, device="cuda"))
+    f = g.clone()
+    f[::2] = 0.0
+    check(x, w, b, t, f)
+    check(x, w, b, t, f * 0)
+    y = x.clone()
+    y[1::2] = 0.0
+    check(y, w, b, t, g)
+
+
+@EACH
+def test_weights_of_very_different_size(way):
+    """float32: the weight has one scale, and numbers of it keep 2^-39 of the largest."""
+    x, w, b, t, g = make(way, F32)
+    V = w.shape[1]
+    check(x, w * torch.logspace(-4, 0, V, device="cuda"), b, t, g)
+    for k in (1e-20, 1e20, 1e-35, 1e33):                     # logits as they were, between numbers that are far from 1
+        check(x * k, w / k, b, t, g)
+    check(x * 0, w, b, t, g)
+    check(x, w * 0, b, t, g)
+
+
+@EACH
+@pytest.mark.parametrize("reduction", ["sum", "mean"])
+def test_rows_of_very_different_size_reduced(way, reduction):
+    x, w, b, t, g = make(way, F32, share=0.7)
+    rows = x.shape[0]
+    t[0] = 3
+    x = x * torch.logspace(6, -8, rows, device="cuda")[:, None]
+    takes(way, x, w, b, t, g, reduction=reduction)
+    got = run(x, w, b, t, g, reduction=reduction)
+    count = int((t >= 0).sum()) if reduction == "mean" else 1
+    want = formula(x, w, b, t, (g[0] / count).expand(rows))
+    assert abs(float(got[0]) - float(want[0][0].sum()) / count) <= float(want[0][1].sum()) / count + 4 * E * abs(float(got[0]))
+    for name, a, (ref, tol, u) in zip(("dx", "dw", "db"), got[1:], want[1:]):
+        assert ((a.cpu().double() - ref).abs() <= tol * (1 + u) + ref.abs() * (u + 2 * E) + 2.0 ** -126).all(), name
+
+
+@EACH
 @TYPES
 def test_strides_types_and_axes(way, dtype):
     x, w, b, t, g = make(way, dtype, share=0.9)
