@@ -86,9 +86,8 @@ int da_linear_cross_entropy_backward(int dtype, int64_t rows, int64_t d, int64_t
  *
  *   X = g / (|g| + eps)  (Frobenius norm),   then for each step's (a, b, c):   A = X X^T,  X <- a X + (b A + c A^2) X
  *
- * (for rows > cols of the transposed matrix).  Products are of pairs of 16-bit halves with 22 bits; with bfloat16 those of the
- * first step have 11 bits, and so has X in the last product of the others (the result is off by up to 1.2 times what rounding
- * it costs).  Sums are held in 32 bits, the norm's in 64.
+ * (for rows > cols of the transposed matrix).  Products are of pairs of 16-bit halves with 22 bits for both types; sums are held in 32
+ * bits, the norm's in 64.  bfloat16 is rounded to once, at the end.
  *
  *   g         of dtype; neighbouring columns, rows ldg, matrices `stride` numbers apart
  *   coefficients   host, 3 steps numbers.  Those with which singular values could grow beyond 128 or b x + c x^2 beyond 2^12

@@ -2,13 +2,12 @@
 //
 // All products are of pairs of fp16 halves (da_planes.h): a step multiplies errors of the small singular values by up to
 // a, like the values themselves, so what is kept between products keeps 22 bits; bf16 or single fp16 numbers there would be
-// off by 1e-2 and 3e-3 of the result where rounding it to bf16 costs 1.7e-3.
-// With bfloat16 two of these roundings do not show beside the result's: the first step's, on numbers that came with 8 bits (its
-// products are of first halves alone), and X's where b A + c A^2 multiplies it (its second half is left out there).  Over square
-// and wide random and low-rank matrices the result is then off by 1.04 to 1.2 times what rounding it costs.
+// off by 1e-2 and 3e-3 of the result where rounding it to bf16 costs 1.7e-3.  That holds for bfloat16, too, from the first step on: with first
+// halves there, and X's alone in its product with b A + c A^2, random matrices came out within 1.2 times the rounding, but those of
+// numbers of one magnitude, whose roundings are all alike, off by up to 5e-3.
 // X is held with the shorter side as rows (a tall matrix is turned around on its way in and out).  A and A^2 are symmetric:
 // only tiles on and above the diagonal are computed, and each is written to both of its places.
-// 2048 x 8192 bf16, five steps: 1351 us; a step's products 105, 53 and 137.  1187 x 602 float32: 175, of which a kernel's start, its
+// 2048 x 8192 bf16, five steps: 1600 us; a step's products 105, 53 and 160.  1187 x 602 float32: 175, of which a kernel's start, its
 // first loads from what another die's cache wrote, and its end are some 5 of each launch's 11.
 // The scales of X, A and b A + c A^2 follow from how large singular values can be: at most 1 at first (the Frobenius norm
 // bounds them), then by the polynomial's extremes, which the host takes.
@@ -19,7 +18,6 @@
 #include "da_spmm.h"
 
 #include <cmath>
-#include <type_traits>
 
 namespace daspmm {
 namespace {
@@ -379,10 +377,7 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
     gram.K = step.Nb = (int)p.Nb;
     poly.A = poly.B = A;
     step.A = B;
-    constexpr bool narrow = std::is_same_v<T, bf16>;
-    auto one_step = [&](int k, auto square, auto product) {
-        typedef decltype(square) S;
-        typedef decltype(product) P;
+    for (int k = 0; k < steps; ++k) {
         const float sx = scales[k].X, sa = scales[k].A, sb = scales[k].B;
         gram.A = gram.B = step.B = X;
         GramOut first{};
@@ -390,14 +385,14 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
         first.la = la;
         first.batch_a = ba;
         first.by = sa / (sx * sx);
-        plane_product<S, kAlong, kAlong, kBoundNone>(gram, first, p.gram, (int)batch, part, arrived, s);
+        plane_product<Halves, kAlong, kAlong, kBoundNone>(gram, first, p.gram, (int)batch, part, arrived, s);
         PolyOut second{};
         static_cast<GramOut&>(second) = first;
         second.A = B;
         second.from = A;
         second.b = c[3 * k + 1] * sb / sa;
         second.c = c[3 * k + 2] * sb / (sa * sa);
-        plane_product<S, kAlong, kAlong, kBoundNone>(poly, second, p.poly, (int)batch, part, arrived, s);
+        plane_product<Halves, kAlong, kAlong, kBoundNone>(poly, second, p.poly, (int)batch, part, arrived, s);
         const bool last = k + 1 == steps && !tall;
         const float to = last ? 1.f : scales[k + 1].X;
         const StepOut third{X, Y, lx, bx, c[3 * k] * to / sx, to / (sb * sx)};
@@ -407,16 +402,11 @@ void orthogonalise(int64_t batch, int64_t rows, int64_t cols, const T* g, int64_
             l.out = out;
             l.rows = (int)rows;
             l.cols = (int)cols;
-            plane_product<P, kAlong, kAcross, kBoundNone>(step, l, p.step, (int)batch, part, arrived, s);
+            plane_product<Halves, kAlong, kAcross, kBoundNone>(step, l, p.step, (int)batch, part, arrived, s);
         } else {
-            plane_product<P, kAlong, kAcross, kBoundNone>(step, third, p.step, (int)batch, part, arrived, s);
+            plane_product<Halves, kAlong, kAcross, kBoundNone>(step, third, p.step, (int)batch, part, arrived, s);
         }
         std::swap(X, Y);
-    };
-    for (int k = 0; k < steps; ++k) {
-        if constexpr (!narrow) one_step(k, Halves(), Halves());
-        else if (k == 0) one_step(k, HalvesBy<1>(), HalvesBy<1>());
-        else one_step(k, Halves(), HalvesBy<2>());
     }
     if (tall)
         hipLaunchKernelGGL((orth_turn_kernel<T>), dim3((unsigned)(p.Nb / 64), (unsigned)(p.Ma / 64), (unsigned)batch), dim3(256), 0, s, X, lx,

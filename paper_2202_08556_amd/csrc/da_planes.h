@@ -41,20 +41,19 @@ __host__ __device__ inline Packed packed(long lines, long n, int N) {
 }
 
 struct One {
-    static constexpr int N = 1, STEP = 64, PRODUCTS = 1;     // numbers of a value, inner positions of a step
+    static constexpr int N = 1, STEP = 64;                   // numbers of a value, inner positions of a step
     typedef bf16x8 Frag;
     static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
 };
-template <int PRODUCTS_> struct HalvesBy {   // 3: all; 2: both halves of the left operand with the first of the right one; 1: first halves
-    static constexpr int N = 2, STEP = 32, PRODUCTS = PRODUCTS_;
+struct Halves {
+    static constexpr int N = 2, STEP = 32;
     typedef f16x8 Frag;
     static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
 };
-typedef HalvesBy<3> Halves;
 
 // Value `at` of a packed line
 template <class P> __host__ __device__ __forceinline__ long place(const Packed& l, long line, long at) {
@@ -300,12 +299,10 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         auto read = [&](const char* buf, Step& f) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                if (P::N == 1 || s == 0 || P::PRODUCTS == 3)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) f.b[s][j] = bfrag(buf, j, s);
-                if (P::N == 1 || s == 0 || P::PRODUCTS >= 2)
+                for (int j = 0; j < NT; ++j) f.b[s][j] = bfrag(buf, j, s);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) f.a[s][i] = afrag(buf, i, s);
+                for (int i = 0; i < MT; ++i) f.a[s][i] = afrag(buf, i, s);
             }
         };
         auto multiply = [&](Step& f) {
@@ -313,8 +310,8 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
             if constexpr (P::N == 1) {
                 all(f.a[1], f.b[1]);
             } else {
-                if constexpr (P::PRODUCTS == 3) all(f.a[0], f.b[1]);
-                if constexpr (P::PRODUCTS >= 2) all(f.a[1], f.b[0]);
+                all(f.a[0], f.b[1]);
+                all(f.a[1], f.b[0]);
             }
         };
         constexpr int STAGES = S::STAGES;
@@ -379,19 +376,17 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
                 for (int j = 0; j < NT; ++j) b[j] = bfrag(buf, j, 0);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) a[i] = afrag(buf, i, 0);
-                if constexpr (P::PRODUCTS == 3)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) c[j] = bfrag(buf, j, 1);
+                for (int j = 0; j < NT; ++j) c[j] = bfrag(buf, j, 1);
                 __builtin_amdgcn_sched_barrier(0);
                 all(a, b);
-                if constexpr (P::PRODUCTS == 3) all(a, c);
-                if constexpr (P::PRODUCTS >= 2)
+                all(a, c);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const Frag second = afrag(buf, i, 1);
+                for (int i = 0; i < MT; ++i) {
+                    const Frag second = afrag(buf, i, 1);
 #pragma unroll
-                        for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(b[j], second, acc[i][j]);
-                    }
+                    for (int j = 0; j < NT; ++j) acc[i][j] = P::mul(b[j], second, acc[i][j]);
+                }
             }
         }
     }

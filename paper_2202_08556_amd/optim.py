@@ -33,8 +33,8 @@ def orthogonalise(update: torch.Tensor, steps: int = 5, coefficients=COEFFICIENT
     """Newton-Schulz steps X <- a X + (b A + c A^2) X, A = X X^T, from X = update / (|update| + eps) (Frobenius norm).
 
     update (..., rows, columns): each matrix by itself, the like weights of several layers at once; what is stacked costs less
-    than one after the other.  coefficients: (a, b, c), or one such triple a step.  The products have 22 bits, with bfloat16 fewer
-    where the result's rounding is larger (da_training.h).  Not differentiable: call it without gradients."""
+    than one after the other.  coefficients: (a, b, c), or one such triple a step.  The products have 22 bits; a bfloat16
+    result is rounded once, at the end.  Not differentiable: call it without gradients."""
     steps, eps = int(steps), float(eps)
     if steps < 0:
         raise ValueError("steps must not be negative")
