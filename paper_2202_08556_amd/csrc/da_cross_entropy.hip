@@ -7,6 +7,7 @@
 // products read: eight operations for each of rows x d x classes instead of six, and no logits in memory.
 // Rows that have a target are gathered first (x is packed for the products anyway), and the products stop at their number,
 // which only the device knows: rows without one cost nothing and may hold anything.
+// db is summed where dz is made, before it is rounded as an operand.
 // The scales by row cost 1 to 3 % (float32, 4096 x 1024 x 8192: 775 and 778 us, rows far apart 765 and 795), and a packing of x where the rows' factors
 // differ (100000 x 700 x 130: 959 and 1114).
 // 4096 x 2048 x 65536 bf16, forward and backward: 3745 us, 1180 TFLOP/s; the four products 890 to 1020 each, the more the larger
@@ -439,6 +440,7 @@ template <class P> struct GradOut : Logits<P> {
     int first;
     uint16_t* dz;
     Packed lz;
+    float* sums;                 // not null: [rows of a wave, one after the other][Nb], what they add to db, in 32 bits
     // 16 rows at a time: a lane makes its numbers of one row, packed as they are in memory, and they leave by way of LDS in whole lines
     template <int MT, int NT>
     __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int, char* lds, int Ma, int Nb) const {
@@ -457,6 +459,9 @@ template <class P> struct GradOut : Logits<P> {
             shift[i] = P::N == 2 && there ? shift_of_row(this->st, m) : 0;
             t[i] = (there ? this->st.target[m] : -0x40000000) - n0 - 4 * h;
         }
+        f32x4 sum[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             float z[NT][4];
@@ -472,6 +477,13 @@ template <class P> struct GradOut : Logits<P> {
                     for (int q = 0; q < 4; ++q)
                         if (t[i] == j * 16 + q) z[j][q] -= 1.f;
             const bool there = mw + i * 16 + i16 < count;    // a row that is not may hold anything
+            if (sums) {
+                const float g = there ? u.row(mw + i * 16 + i16) : 0.f;
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) sum[j][q] += there ? z[j][q] * g : 0.f;
+            }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
 #pragma unroll
@@ -489,8 +501,17 @@ template <class P> struct GradOut : Logits<P> {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
+        if (!sums || mw >= Ma || nw >= Nb) return;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[j][q] = wave_sum(sum[j][q], 16);
+            if (i16 == 0) *reinterpret_cast<f32x4*>(sums + (long)(mw / (MT * 16)) * Nb + nw + j * 16 + 4 * h) = sum[j];
+        }
     }
 };
+// rows of a wave of its tiles
+constexpr int grad_rows(int shape) { return shape == 0 ? PlaneLarge::MT * 16 : shape == 1 ? PlaneMiddle::MT * 16 : PlaneSmall::MT * 16; }
 
 // dx, or what the pieces so far give of it
 template <class T, class P> struct InputOut {
@@ -602,35 +623,12 @@ __global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, Upstream u, 
     if (threadIdx.x == 0) part[blockIdx.x] = p;
 }
 
-// db: sums of dz's columns over parts of the rows, then over the parts
-template <class P>
-__global__ __launch_bounds__(256) void ce_bias_kernel(CeStats st, Upstream u, const uint16_t* __restrict__ dz, Packed lz, int Nb, long per,
-                                                      float* __restrict__ part)
-{
-    __shared__ f32x4 red[4][64];
-    const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4, k = threadIdx.x >> 6;
-    const long r0 = blockIdx.y * per, r1 = min(r0 + per, (long)*st.count);
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (n < Nb)
-        for (long m = r0 + k; m < r1; m += 4) {
-            float x[4];
-            get_values<P, 4>(dz + place<P>(lz, m, n), x);
-            const int down = P::N == 2 ? -u.shift(u.row((int)m)) : 0;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) s[q] += P::N == 2 ? ldexpf(x[q], down) : x[q];
-        }
-    red[k][threadIdx.x & 63] = s;
-    __syncthreads();
-    if (k == 0 && n < Nb) {
-        const int l = threadIdx.x;
-        *reinterpret_cast<f32x4*>(part + (long)blockIdx.y * Nb + n) = (red[0][l] + red[1][l]) + (red[2][l] + red[3][l]);
-    }
-}
-__global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restrict__ part, int parts, int Nb, int classes, void* db, int type,
-                                                           int first)
+// db: what the waves' rows add, `per` rows each
+__global__ __launch_bounds__(256) void ce_bias_join_kernel(const float* __restrict__ part, const int* __restrict__ count, int per, int Nb,
+                                                           int classes, void* db, int type, int first)
 {
     __shared__ float red[16][17];
-    const int n = blockIdx.x * 16 + (threadIdx.x & 15), k0 = threadIdx.x >> 4;
+    const int parts = (*count + per - 1) / per, n = blockIdx.x * 16 + (threadIdx.x & 15), k0 = threadIdx.x >> 4;
     float s[4] = {};
     if (n < classes) {
         int k = k0;
@@ -770,7 +768,6 @@ struct CePlan {
     int slots;
     int64_t piece;               // classes of a piece, a multiple of 64 where there are several
     PiecePlan whole, rest;       // products of a whole piece and of the last one
-    int bias_parts;
     size_t counts_at, sums_at, target_at, x_at, w_at, part_at, forward;          // bytes
     size_t arrived_at, dz_at, dx_at, bias_at, sum_at, again_at, factor_at, backward;
     bool shifts() const { return !narrow.taken && !tall.taken && !few.taken && halves; }
@@ -841,11 +838,10 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
     const int64_t Pb = padded(p.piece);
     p.dz_at = take((size_t)p.Ma * Pb * 2 * N);
     p.dx_at = take(p.piece < s.V ? (size_t)p.Ma * p.D * 4 : 0);
-    p.bias_parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(s.rows, 64), std::max<int64_t>(1, 1024 / ceil_div(Pb, 256))));
-    p.bias_at = take((size_t)p.bias_parts * Pb * 4);
     size_t sums = 0;
     p.whole = piece_plan(p.Ma, p.D, p.piece, step);
     p.rest = s.V % p.piece ? piece_plan(p.Ma, p.D, s.V % p.piece, step) : p.whole;
+    p.bias_at = take((size_t)ceil_div(p.Ma, std::min(grad_rows(p.whole.logits.shape), grad_rows(p.rest.logits.shape))) * Pb * 4);
     for (const PiecePlan& q : {p.whole, p.rest}) sums = std::max({sums, plane_part_bytes(q.input, 1), plane_part_bytes(q.weight, 1)});
     p.sum_at = take(sums);
     p.again_at = take(N == 2 ? (size_t)p.Ma * p.D * 2 * N : 0);
@@ -999,6 +995,7 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
         grad.first = (int)first;
         grad.dz = dz;
         grad.lz = lz;
+        grad.sums = db ? bias : nullptr;
         plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, lw, first, width), grad, q.logits, 1, nullptr, nullptr, c.stream);
         if (dx) {
             PlaneArgs a{};
@@ -1036,11 +1033,8 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             plane_product<P, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, arrived, c.stream);
         }
         if (db) {
-            const int64_t per = ceil_div(c.s.rows, c.p.bias_parts);
-            hipLaunchKernelGGL((ce_bias_kernel<P>), dim3((unsigned)ceil_div(Vb, 256), (unsigned)c.p.bias_parts), dim3(256), 0, c.stream, c.st, u, dz, lz,
-                               (int)Vb, (long)per, bias);
-            hipLaunchKernelGGL(ce_bias_join_kernel, dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.p.bias_parts, (int)Vb,
-                               (int)width, db, c.param_dtype, (int)first);
+            hipLaunchKernelGGL(ce_bias_join_kernel, dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.st.count,
+                               grad_rows(q.logits.shape), (int)Vb, (int)width, db, c.param_dtype, (int)first);
         }
     }
 }

@@ -82,7 +82,8 @@ def formula(x, w, b, t, g):
     # an error e of a logit is a factor exp(e) of p; and p, computed or not, is between 0 and 1, but for the rounding of z - lse where
     # z is the largest logit and lse above it: whatever the logits are off by, p is off by 1 and a little at most
     t_p = torch.nan_to_num(p * torch.expm1(2 * D + (K + 4 * away) * E), nan=1.0, posinf=1.0).clamp(max=1.0) + 2.0 ** -20 * p
-    t_dz = gm * (t_p + 4 * E * (p + one)) + dz.abs() * (2.0 ** -22 if halves else 2.0 ** -8)
+    t_sum = gm * (t_p + 4 * E * (p + one))                   # db adds what has not been rounded as an operand
+    t_dz = t_sum + dz.abs() * (2.0 ** -22 if halves else 2.0 ** -8)
     if halves:
         t_dz = t_dz + 2.0 ** -39 * gm
     dx, t_dx = torch.mm(dz, W.t()), torch.mm(t_dz, W.abs().t()) + ((V / 16 + 16) * E + extra) * torch.mm(dz.abs(), W.abs().t())
@@ -90,7 +91,7 @@ def formula(x, w, b, t, g):
     if halves:
         t_dx = t_dx + 2.0 ** -38 * V * gm * wm
         t_dw = t_dw + 2.0 ** -37 * rows * (xm * gm).max()
-    db, t_db = dz.sum(0), t_dz.sum(0) + (rows / 16 + 80) * E * dz.abs().sum(0)
+    db, t_db = dz.sum(0), t_sum.sum(0) + (rows / 16 + 80) * E * dz.abs().sum(0)
     place = lambda v: torch.zeros(rows, *v.shape[1:], dtype=v.dtype).index_copy(0, keep, v)             # noqa: E731
     return [(place(loss), place(t_loss), E), (place(dx), place(t_dx), U[dtype]), (dw, t_dw, U[dtype])] + \
         ([(db, t_db, U[b.dtype])] if b is not None else [])
@@ -112,6 +113,20 @@ def test_plain(way, dtype):
     args = make(way, dtype, share=0.8)
     takes(way, *args)
     check(*args)
+
+
+@EACH
+@pytest.mark.parametrize("reduction", ["none", "sum"])
+def test_bias_in_32_bits_beside_bfloat16(way, reduction):
+    """The gradient of a float32 bias is a sum in 32 bits of numbers in 32 bits, also where dz is rounded for the other products."""
+    x, w, b, t, g = make(way, BF16, share=0.8)
+    b = b.float()
+    if reduction == "none":
+        check(x, w, b, t, g)
+        return
+    db = run(x, w, b, t, g, reduction="sum")[3]
+    want, tol, u = formula(x, w, b, t, g[0].expand(x.shape[0]))[3]
+    assert u == E and ((db.cpu().double() - want).abs() <= tol * (1 + u) + want.abs() * 2 * E).all()
 
 
 @EACH
