@@ -13,8 +13,8 @@
 // Pairs lie in groups of 32: 32 first halves and 32 second ones along a line, so that 64 bytes of either are 128 in one
 // place.
 #pragma once
-#include "da_gated_plan.h"
 #include "da_layer_common.h"
+#include "da_planes_plan.h"
 
 namespace daspmm {
 
@@ -151,12 +151,12 @@ struct PlaneArgs {
     float* part;                 // splits > 1: [batch][tile][split], a tile's sums as its waves hold them
     int* arrived;                // ... [batch][tile], 0: how many of a tile's parts are there
 };
-constexpr int kMostParted = 1024;            // tiles whose sums are in parts
 enum { kBoundNone = 0, kBoundM = 1, kBoundK = 2 };
 
 // 16 bytes a lane from base + offset to LDS: byte `to` of it and on, lane by lane.  Written out because the compiler, which
 // knows the builtin of this instruction, waits for all of them before every transposing read; the waits are in the loop.
-// Nothing else in these kernels uses m0.
+// m0 is a reserved register: the compiler keeps nothing in it from one instruction to another, sets it before each use of its own, and
+// takes no clobber of it.
 __device__ __forceinline__ void line_to_lds(const char* base, unsigned offset, unsigned to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }

@@ -1,4 +1,4 @@
-// Products of packed matrices: how one is cut into tiles and parts, and its launch.
+// Products of packed matrices: their launch.
 #pragma once
 #include "da_internal.h"
 #include "da_planes.h"
@@ -12,62 +12,9 @@ typedef PlaneShape<256, 256, 2, 4, 2, false> PlaneLarge;
 typedef PlaneShape<128, 128, 2, 2, 2, true> PlaneMiddle;
 typedef PlaneShape<64, 64, 2, 2, 4, true> PlaneSmall;
 
-struct PlanePlan {
-    int shape;                   // 0 large, 1 middle, 2 small
-    int tiles_m, tiles_n;
-    int64_t tiles;               // of a batch
-    int splits, per;
-};
-
-// What tiles of a size cost, in us, as measured on products of 200 to 8192: a step of a block where at most half of the units have one,
-// where each has at most one, and where they have two (the large tiles: one after the other), and what a block needs beside its steps.
-struct PlaneCost {
-    int64_t side;
-    double few, one, two, more;
-};
-constexpr PlaneCost kPlaneCost[2][3] = {
-    {{256, 1.2, 1.65, 1.65, 12.0}, {128, 0.55, 0.7, 0.9, 6.0}, {64, 0.24, 0.28, 0.32, 4.0}},         // One
-    {{256, 1.65, 2.35, 2.35, 13.0}, {128, 0.72, 0.95, 1.2, 6.0}, {64, 0.28, 0.32, 0.36, 4.0}}};      // Halves
-
-// The tile, and the number of parts of the inner axis, whose turns on the chip take the least time: large tiles read least for what
-// they compute, small ones and parts keep all units busy, and a tile's parts go to memory and are read by one block (22 KB/us).
-// Blocks of 128 x 128 whose results are pairs, read and written by their epilogue (all of pairs but the logits), need 2 us more: with and without them 12
-// updates of 256 x 1024 take 196 and 217 us, and logits of 4096 x 407 x 856 in bfloat16 38 and 33, of 6633 x 253 x 1287 in float32 78 and 75.
-// 1024 x 4096 times its transpose, one after the other in tiles of 256, 128 and 64 with the best number of parts: 131, 34 and 27 us;
-// 2048 x 2048 . 2048 x 8192: 159, 175 and 240.
-inline PlanePlan plane_plan(int64_t Ma, int64_t Nb, int64_t steps, int64_t batches, bool symmetric, bool may_split, int halves) {
-    PlanePlan best{};
-    const int64_t cus = compute_units();
-    double least = 0.0;
-    for (int shape = 0; shape < 3; ++shape) {
-        const PlaneCost& c = kPlaneCost[halves][shape];
-        PlanePlan p{};
-        p.shape = shape;
-        p.tiles_m = (int)ceil_div(Ma, c.side);
-        p.tiles_n = (int)ceil_div(Nb, c.side);
-        p.tiles = symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
-        const bool parts = may_split && p.tiles * batches <= kMostParted;
-        for (int64_t splits = 1; splits <= 1024 && (splits == 1 || (parts && steps / splits >= 4)); splits += std::max<int64_t>(1, splits / 2)) {
-            const int64_t per = std::max<int64_t>(1, ceil_div(steps, splits)), real = std::max<int64_t>(1, ceil_div(steps, per));
-            const int64_t blocks = p.tiles * batches * real, slots = shape == 0 ? cus : 2 * cus;
-            const double more = c.more + (shape == 1 && halves && may_split ? 2.0 : 0.0);
-            const double turn = (double)per * (blocks > cus ? c.two : 2 * blocks > cus ? c.one : c.few) + more;
-            const double join = real > 1 ? 2.0 + (double)(real * c.side * c.side * 4) / 22e3 : 0.0;
-            const double time = (double)ceil_div(std::max<int64_t>(blocks, 1), slots) * turn + join;
-            if ((shape == 0 && splits == 1) || time < least) {
-                least = time;
-                best = p;
-                best.splits = (int)real;
-                best.per = (int)per;
-            }
-        }
-    }
-    return best;
-}
-inline size_t plane_part_bytes(const PlanePlan& p, int64_t batches) {
-    const size_t side = kPlaneCost[0][p.shape].side;
-    return p.splits > 1 ? (size_t)batches * p.tiles * p.splits * side * side * sizeof(float) : 0;
-}
+static_assert(PlaneLarge::THREADS == kPlaneCost[0][0].threads && PlaneMiddle::THREADS == kPlaneCost[0][1].threads &&
+              PlaneSmall::THREADS == kPlaneCost[0][2].threads && PlaneLarge::BM == kPlaneCost[0][0].side &&
+              PlaneMiddle::BM == kPlaneCost[0][1].side && PlaneSmall::BM == kPlaneCost[0][2].side, "the tiles that are planned with");
 
 template <class P, class S, int ALAY, int BLAY, int BOUND, class E>
 void plane_launch(const PlaneArgs& g, const E& epi, const PlanePlan& p, int batches, hipStream_t s) {
