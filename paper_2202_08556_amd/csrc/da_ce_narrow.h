@@ -373,25 +373,33 @@ template <class T> __global__ __launch_bounds__(256) void ce_narrow_join_kernel(
 {
     __shared__ float red[16][17];
     const long all = (long)(a.d + 1) * a.V, from = a.dw ? 0 : (long)a.d * a.V;
-    const long c = from + (long)blockIdx.x * 16 + (threadIdx.x & 15);
     const int k0 = threadIdx.x >> 4;
-    const bool take = c < (long)a.d * a.V || (c < all && a.db);
-    float s[4] = {};
-    if (take) {
-        int k = k0;
-        for (; k + 48 < blocks; k += 64)
+    for (long c0 = from + (long)blockIdx.x * 16; c0 < all; c0 += (long)gridDim.x * 16) {
+        const long c = c0 + (threadIdx.x & 15);
+        const bool take = c < (long)a.d * a.V || (c < all && a.db);
+        float s[4] = {};
+        if (take) {
+            int k = k0;
+            for (; k + 48 < blocks; k += 64)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) s[u] += a.part[(k + u * 16) * all + c];
-        for (; k < blocks; k += 16) s[0] += a.part[k * all + c];
+                for (int u = 0; u < 4; ++u) s[u] += a.part[(k + u * 16) * all + c];
+            for (; k < blocks; k += 16) s[0] += a.part[k * all + c];
+        }
+        red[k0][threadIdx.x & 15] = (s[0] + s[1]) + (s[2] + s[3]);
+        __syncthreads();
+        if (threadIdx.x < 16 && take) {
+            float one[1] = {0.f};
+            for (int i = 0; i < 16; ++i) one[0] += red[i][threadIdx.x];
+            if (c < (long)a.d * a.V) store_floats<1>(static_cast<T*>(a.dw) + c, one);
+            else store_param(a.db, a.param_type, c - (long)a.d * a.V, one[0]);
+        }
+        __syncthreads();                                     // before the next numbers
     }
-    red[k0][threadIdx.x & 15] = (s[0] + s[1]) + (s[2] + s[3]);
-    __syncthreads();
-    if (threadIdx.x < 16 && take) {
-        float one[1] = {0.f};
-        for (int i = 0; i < 16; ++i) one[0] += red[i][threadIdx.x];
-        if (c < (long)a.d * a.V) store_floats<1>(static_cast<T*>(a.dw) + c, one);
-        else store_param(a.db, a.param_type, c - (long)a.d * a.V, one[0]);
-    }
+}
+// blocks of it; a launch has fewer than 2^32 threads
+inline unsigned narrow_join_blocks(int64_t numbers) {
+    const int64_t most = 1 << 20, blocks = (numbers + 15) / 16;
+    return (unsigned)(blocks < most ? blocks : most);
 }
 
 }  // namespace daspmm

@@ -1101,7 +1101,7 @@ void narrow_backward(const CeCall& c, int reduction, const float* dloss, int64_t
     narrow_launch<T, true>(p, a, c.stream);
     const int64_t numbers = (a.dw ? c.s.d * c.s.V : 0) + (db ? c.s.V : 0);
     if (p.blocks > 1 && numbers)
-        hipLaunchKernelGGL((ce_narrow_join_kernel<T>), dim3((unsigned)ceil_div(numbers, 16)), dim3(256), 0, c.stream, a, p.blocks);
+        hipLaunchKernelGGL((ce_narrow_join_kernel<T>), dim3(narrow_join_blocks(numbers)), dim3(256), 0, c.stream, a, p.blocks);
 }
 
 template <class F> void by_fragments(int NF, F&& go) {
@@ -1147,7 +1147,7 @@ template <class T> void tall_backward(const CeCall& c, int reduction, const floa
     });
     const int64_t numbers = (dw ? c.s.d * c.s.V : 0) + (db ? c.s.V : 0);
     if (numbers)
-        hipLaunchKernelGGL((ce_narrow_join_kernel<T>), dim3((unsigned)ceil_div(numbers, 16)), dim3(256), 0, c.stream, static_cast<const NarrowArgs&>(a),
+        hipLaunchKernelGGL((ce_narrow_join_kernel<T>), dim3(narrow_join_blocks(numbers)), dim3(256), 0, c.stream, static_cast<const NarrowArgs&>(a),
                            p.parts);
 }
 
