@@ -45,9 +45,9 @@ __device__ __forceinline__ int few_target(const FewArgs& a, int r, bool backward
 
 template <class T, int R, bool BWD> __global__ __launch_bounds__(kFewBlock) void ce_few_logits_kernel(FewArgs a)
 {
-    constexpr int V = 16 / sizeof(T), U = 4, AT_ONCE = R < 4 ? R : 4;
+    constexpr int V = 16 / sizeof(T), U = 4;
     __shared__ __attribute__((aligned(16))) float factor[kFewLines][R];
-    __shared__ float others[3][64][V * AT_ONCE];
+    __shared__ float others[3][64][V * R];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (!BWD && blockIdx.x == 0 && blockIdx.y == 0 && tid <= kSomeRows) a.arrived[tid * kFewApart] = 0;
     const long n = ((long)blockIdx.x * 64 + lane) * V;
@@ -103,26 +103,21 @@ template <class T, int R, bool BWD> __global__ __launch_bounds__(kFewBlock) void
             add(l, w);
         }
     }
+    if (wave > 0)
 #pragma unroll
-    for (int r0 = 0; r0 < R; r0 += AT_ONCE) {
-        __syncthreads();
-        if (wave > 0)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int r = 0; r < AT_ONCE; ++r)
+            for (int i = 0; i < V; ++i) others[wave - 1][lane][r * V + i] = acc[r][i];
+    __syncthreads();
+    if (wave == 0 && n < a.Vp)
 #pragma unroll
-                for (int i = 0; i < V; ++i) others[wave - 1][lane][r * V + i] = acc[r0 + r][i];
-        __syncthreads();
-        if (wave == 0 && n < a.Vp)
+        for (int r = 0; r < R; ++r) {
+            if (r >= a.rows) break;
+            float s[V];
 #pragma unroll
-            for (int r = 0; r < AT_ONCE; ++r) {
-                if (r0 + r >= a.rows) break;
-                float s[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    s[i] = (acc[r0 + r][i] + others[0][lane][r * V + i]) + (others[1][lane][r * V + i] + others[2][lane][r * V + i]);
-                store_floats<V>(a.part + ((long)blockIdx.y * a.rows + r0 + r) * a.Vp + n, s);
-            }
-    }
+            for (int i = 0; i < V; ++i) s[i] = (acc[r][i] + others[0][lane][r * V + i]) + (others[1][lane][r * V + i] + others[2][lane][r * V + i]);
+            store_floats<V>(a.part + ((long)blockIdx.y * a.rows + r) * a.Vp + n, s);
+        }
 }
 
 // A logit from its parts

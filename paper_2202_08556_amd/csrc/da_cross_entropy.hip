@@ -1152,7 +1152,7 @@ template <class T> void tall_backward(const CeCall& c, int reduction, const floa
 }
 
 // ... by the rows that registers are held for
-template <class T, class F> void by_rows(int64_t rows, F&& go) {
+template <class F> void by_rows(int64_t rows, F&& go) {
     if (rows == 1) go(std::integral_constant<int, 1>());
     else if (rows == 2) go(std::integral_constant<int, 2>());
     else go(std::integral_constant<int, 4>());
@@ -1189,7 +1189,7 @@ template <class T, bool BWD> void few_logits(const CeCall& c, const FewArgs& a) 
     const dim3 grid((unsigned)c.p.few.columns, (unsigned)a.splits), block(kFewBlock);
     if (a.rows > kFewRows)
         by_some<T>(a.rows, [&](auto f) { hipLaunchKernelGGL((ce_some_logits_kernel<T, decltype(f)::value, BWD>), grid, block, 0, c.stream, a); });
-    else by_rows<T>(c.s.rows, [&](auto r) { hipLaunchKernelGGL((ce_few_logits_kernel<T, decltype(r)::value, BWD>), grid, block, 0, c.stream, a); });
+    else by_rows(c.s.rows, [&](auto r) { hipLaunchKernelGGL((ce_few_logits_kernel<T, decltype(r)::value, BWD>), grid, block, 0, c.stream, a); });
 }
 template <class T> void few_forward(const CeCall& c, const void* target, int target64, int reduction, float* loss) {
     FewArgs a = few_args(c, reduction);
@@ -1223,7 +1223,7 @@ template <class T> void few_backward(const CeCall& c, int reduction, const float
     } else {
         hipLaunchKernelGGL(ce_few_grad_kernel, dim3((unsigned)ceil_div(a.Vp, kFewBlock)), dim3(kFewBlock), 0, c.stream, a);
         if (!dx && !dw) return;
-        by_rows<T>(c.s.rows, [&](auto r) {
+        by_rows(c.s.rows, [&](auto r) {
             hipLaunchKernelGGL((ce_few_products_kernel<T, decltype(r)::value>), dim3((unsigned)ceil_div(c.s.d, kFewDown), (unsigned)c.p.few.across),
                                dim3(kFewBlock), 0, c.stream, a);
         });
