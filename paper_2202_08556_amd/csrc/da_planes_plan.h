@@ -25,8 +25,9 @@ constexpr PlaneCost kPlaneCost[2][3] = {
 
 // The tile, and the number of parts of the inner axis, whose turns on the chip take the least time: large tiles read least for what
 // they compute, small ones and parts keep all units busy, and a tile's parts go to memory and are read by one block (22 KB/us).
-// Blocks of 128 x 128 whose results are pairs, read and written by their epilogue (all of pairs but the logits), need 2 us more: with and without them 12
-// updates of 256 x 1024 take 196 and 217 us, and logits of 4096 x 407 x 856 in bfloat16 38 and 33, of 6633 x 253 x 1287 in float32 78 and 75.
+// Blocks of 128 x 128 whose results leave (all but those of logits, whose sums may not be cut) need 2 us more: with and without them 12 updates of 256 x
+// 1024 take 196 and 217 us and dx of 1000000 x 32 x 200 in bfloat16 186 and 271; but logits of 4096 x 407 x 856 in bfloat16 38 and 33, of 6633 x 253 x
+// 1287 in float32 78 and 75.
 // 1024 x 4096 times its transpose, one after the other in tiles of 256, 128 and 64 with the best number of parts: 131, 34 and 27 us;
 // 2048 x 2048 . 2048 x 8192: 159, 175 and 240.
 inline PlanePlan plane_plan(int64_t Ma, int64_t Nb, int64_t steps, int64_t batches, bool symmetric, bool may_split, int halves) {
@@ -46,7 +47,7 @@ inline PlanePlan plane_plan(int64_t Ma, int64_t Nb, int64_t steps, int64_t batch
         for (int64_t splits = 1; splits <= 1024 && (splits == 1 || (parts && steps / splits >= 4)); splits += std::max<int64_t>(1, splits / 2)) {
             const int64_t per = std::max<int64_t>(1, ceil_div(steps, splits)), real = std::max<int64_t>(1, ceil_div(steps, per));
             const int64_t blocks = p.tiles * batches * real, slots = shape == 0 ? cus : 2 * cus;
-            const double more = c.more + (shape == 1 && halves && may_split ? 2.0 : 0.0);
+            const double more = c.more + (shape == 1 && may_split ? 2.0 : 0.0);
             const double turn = (double)per * (blocks > cus ? c.two : 2 * blocks > cus ? c.one : c.few) + more;
             const double join = real > 1 ? 2.0 + (double)(real * c.side * c.side * 4) / 22e3 : 0.0;
             const double time = (double)ceil_div(std::max<int64_t>(blocks, 1), slots) * turn + join;
