@@ -63,9 +63,9 @@ int da_rms_norm_backward(int dtype, int64_t rows, int64_t channels, const void *
  *
  * The backward call computes the logits again; sums are held in 32 bits.  Up to 128 classes of up to 256 inner positions (with
  * many of both: up to 64 classes), and up to 64 rows (bfloat16: 16), the products are of 32-bit numbers for both types.  Beyond that operands are
- * packed for the 16-bit matrix cores.  With bfloat16 dz is rounded for dx and dw then (not for db); float32 is multiplied as pairs of halves, 22 bits of a
+ * packed for the 16-bit matrix cores.  With bfloat16 dz has the 11 bits of fp16 for dx and dw then; float32 is multiplied as pairs of halves, 22 bits of a
  * number, fewer of small ones: those of a row of x are off by up to 2^-35 of the row's largest, those of dz by 2^-40 of the row's factor, those of w by
- * 2^-40 of the largest of all.  Loss and dx of a row do not depend on other rows; to dw a row adds with an error of up to 2^-37 of
+ * 2^-40 of the largest of all (bfloat16: of its line, where a number is less than 2^32 times smaller it is exact).  Loss and dx of a row do not depend on other rows; to dw a row adds with an error of up to 2^-37 of
  * the largest product of any row's largest x and its factor.  Limits: rows <= 2^26, d, classes <= 2^22, and fewer than 2^23
  * tiles of 256 x 256 of any of the products' results (DA_ERR_UNSUPPORTED beyond).
  */

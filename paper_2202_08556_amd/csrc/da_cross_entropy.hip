@@ -10,8 +10,8 @@
 // db is summed where dz is made, before it is rounded as an operand.
 // The scales by row cost 1 to 3 % (float32, 4096 x 1024 x 8192: 775 and 778 us, rows far apart 765 and 795), and a packing of x where the rows' factors
 // differ (100000 x 700 x 130: 959 and 1114).
-// 4096 x 2048 x 65536 bf16, forward and backward: 3745 us, 1180 TFLOP/s; the four products 890 to 1020 each, the more the larger
-// their epilogues.
+// 4096 x 2048 x 65536 bf16, forward and backward: 3940 us, 1120 TFLOP/s; the four products 860 to 1000 each, the more the larger
+// their epilogues, w's largest numbers 46 and its packing 120.
 #include "da_training.h"
 
 #include "da_ce_few.h"
@@ -32,7 +32,10 @@ constexpr int kJoinBlocks = 1024;
 constexpr int64_t kPieceBytes = 512LL << 20;
 constexpr float kLog2e = 1.44269504088896f;
 
+// Numbers that the logits are products of, and those of dz and what it is multiplied with: bfloat16 there as fp16, which holds its 8 bits and 11
+// of dz (with dz in bfloat16 dw was off by up to 1.5 times what rounding it costs).
 template <class T> using PlaneOf = std::conditional_t<std::is_same_v<T, float>, Halves, One>;
+template <class T> using GradOf = std::conditional_t<std::is_same_v<T, float>, Halves, Half>;
 
 // What a backward pass reads
 struct CeStats {
@@ -52,9 +55,9 @@ CeStats ce_stats(void* p, int64_t rows) {
             ints(kStatsHead + 4 * n), reinterpret_cast<uint32_t*>(c + 16)};
 }
 
-// Numbers leave for the packed halves times a power of two that takes the largest to 2^14 .. 2^15; `shift` is its exponent.  w has one.  A
-// row of x has that of the whole x, or its own where it is more than 2^kNear times smaller, and a row of dz that of its factor: what
-// a row's results are off by does not depend on other rows.
+// Numbers leave for fp16 times a power of two that takes the largest to 2^14 .. 2^15; `shift` is its exponent.  A row of x has that of the
+// whole x, or its own where it is more than 2^kNear times smaller, and a row of dz that of its factor: what a row's results are off by
+// does not depend on other rows.  w has one (float32), or one for each line, which goes along dx (bfloat16).
 // Of x and w: the largest magnitude as bits, and that of the rows' own shifts; and a count of blocks.
 enum { kMaxX = 0, kMaxW = 1, kArrived = 2, kRowX = 3, kMaxes = 4 };
 constexpr int kNear = 4, kNoShift = -1000, kShiftBias = 512;     // kNoShift: a row of zeros
@@ -68,13 +71,108 @@ __device__ __forceinline__ float magnitude(float x) {
     const float a = fabsf(x);
     return a <= 3.402823466e38f ? a : 0.f;                   // infinities and NaN have no part in a scale
 }
-__device__ __forceinline__ int shift_of_row(const CeStats& st, int m) {
-    const int own = st.shift[m], all = shift_of(st.maxes[kMaxX]);
+__device__ __forceinline__ int shift_of_row(const CeStats& st, int m, uint32_t largest) {
+    const int own = st.shift[m], all = shift_of(largest);
     return own > all + kNear ? own : all;
+}
+__device__ __forceinline__ int shift_of_row(const CeStats& st, int m) { return shift_of_row(st, m, st.maxes[kMaxX]); }
+// While they are taken the three maxima have kSpread places each, in lines of their own: a thousand blocks that end together and all go to one
+// place take 20 us for that
+constexpr int kSpread = 16, kApart = 32;
+__device__ __forceinline__ uint32_t* spread_at(uint32_t* spread, int which, int block) {
+    return spread + ((which == kRowX ? 2 : which) * kSpread + block % kSpread) * kApart;
+}
+__device__ __forceinline__ uint32_t spread_most(uint32_t* spread, int which) {           // in all lanes
+    uint32_t most = *spread_at(spread, which, threadIdx.x);
+    for (int d = 1; d < kSpread; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d, 64));
+    return most;
 }
 // whether a row of x has its own
 __device__ __forceinline__ bool rows_differ(const CeStats& st) {
     return (int)st.maxes[kRowX] - kShiftBias > shift_of(st.maxes[kMaxX]) + kNear;
+}
+// lanes to a row of n numbers of so many bytes
+__host__ __device__ inline int row_lanes(long n, int size) {
+    int lanes = 1;
+    while (lanes < 64 && lanes * 16 < n * size) lanes *= 2;
+    return lanes;
+}
+// The largest finite magnitude of a row or line, in all lanes of its team; `lane` of `lanes`, at most a wave
+template <class T> __device__ __forceinline__ float most_of(const T* __restrict__ p, long n, int lane, int lanes) {
+    constexpr int V = 16 / sizeof(T), U = 4;
+    float most = 0.f;
+    long c = lane * V;
+    for (; c + (U - 1) * lanes * V + V <= n; c += U * lanes * V) {
+        float v[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_floats<V>(p + c + u * lanes * V, v[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < V; ++i) most = fmaxf(most, magnitude(v[u][i]));
+    }
+    for (; c < n; c += lanes * V) {
+        if (c + V <= n) {
+            float v[V];
+            load_floats<V>(p + c, v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) most = fmaxf(most, magnitude(v[i]));
+        } else {
+            for (long i = c; i < n; ++i) {
+                float one[1];
+                load_floats<1>(p + i, one);
+                most = fmaxf(most, magnitude(one[0]));
+            }
+        }
+    }
+    for (int k = 1; k < lanes; k <<= 1) most = fmaxf(most, __shfl_xor(most, k, 64));
+    return most;
+}
+// ... of several rows at once, whose loads are on their way together
+constexpr int kAtOnce = 4;
+template <class T>
+__device__ __forceinline__ void most_of_rows(const T* const (&p)[kAtOnce], long n, int lane, int lanes, float (&most)[kAtOnce]) {
+    constexpr int V = 16 / sizeof(T);
+#pragma unroll
+    for (int r = 0; r < kAtOnce; ++r) most[r] = 0.f;
+    for (long c = lane * V; c < n; c += lanes * V) {
+        if (c + V <= n) {
+            float v[kAtOnce][V];
+#pragma unroll
+            for (int r = 0; r < kAtOnce; ++r) load_floats<V>(p[r] + c, v[r]);
+#pragma unroll
+            for (int r = 0; r < kAtOnce; ++r)
+#pragma unroll
+                for (int i = 0; i < V; ++i) most[r] = fmaxf(most[r], magnitude(v[r][i]));
+        } else {
+            for (long i = c; i < n; ++i)
+#pragma unroll
+                for (int r = 0; r < kAtOnce; ++r) {
+                    float one[1];
+                    load_floats<1>(p[r] + i, one);
+                    most[r] = fmaxf(most[r], magnitude(one[0]));
+                }
+        }
+    }
+    for (int k = 1; k < lanes; k <<= 1)
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r) most[r] = fmaxf(most[r], __shfl_xor(most[r], k, 64));
+}
+// The listed rows of x, a few at once to a team of lanes: f(row, its largest magnitude, whether the lane is the team's first)
+template <class T, class F>
+__device__ __forceinline__ void each_row_most(const T* __restrict__ x, long ldx, const int* __restrict__ index, int count, long d, int blocks, F&& f) {
+    const int lanes = row_lanes(d, sizeof(T)), lane = threadIdx.x & (lanes - 1), teams = 256 / lanes;
+    const long step = (long)blocks * teams;
+    for (long m = (long)blockIdx.x * teams + threadIdx.x / lanes; m < count; m += kAtOnce * step) {
+        const T* p[kAtOnce];
+        float most[kAtOnce];
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r) p[r] = x + (long)index[m + r * step < count ? m + r * step : m] * ldx;
+        most_of_rows(p, d, lane, lanes, most);
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r)
+            if (m + r * step < count) f((int)(m + r * step), most[r], lane == 0);
+    }
 }
 
 // The gradient of the loss: of the rows, or one factor for all of them
@@ -89,9 +187,9 @@ struct Upstream {
     __device__ __forceinline__ int shift(float factor) const { return shift_of(__float_as_uint(magnitude(factor))); }
 };
 
-// dw adds rows, so x and dz of a row have to come times the same power of two together, 2^sum: where rows of x or of dz have shifts of
-// their own, x is packed a second time, times what dz lacks.  sum is the smallest of a row's two shifts together: the row
-// that adds most has all its bits, the others theirs from 2^-38 of its numbers on.
+// dw adds rows, so x and dz of a row have to come times the same power of two together, 2^sum: x is packed for it times what dz lacks, a second
+// time in float32, and there only where rows of x or of dz have shifts of their own.  sum is the smallest of a row's two shifts
+// together: the row that adds most has all its bits, the others theirs from 2^-38 of its numbers on.
 struct Joint {
     int sum, differ;
 };
@@ -110,12 +208,14 @@ __device__ __forceinline__ FactorPart block_joined(FactorPart p) {
     __syncthreads();
     return joined(joined(red[0], red[1]), joined(red[2], red[3]));
 }
-constexpr int kFactorParts = 256;
-__device__ __forceinline__ Joint joint_of(const CeStats& st, const Upstream& u, const FactorPart* part, int parts) {
-    if (u.reduction != DA_LOSS_ROWS) return {shift_of(st.maxes[kMaxX]) + u.shift(u.all()), rows_differ(st)};
-    const FactorPart p = block_joined((int)threadIdx.x < parts ? part[threadIdx.x] : no_rows());
-    if (p.least > p.most) return {0, 0};
-    const bool differ = rows_differ(st) || p.least != p.most;
+constexpr int kFactorParts = 1024, kLongLine = 2048;
+template <class Q> __device__ __forceinline__ Joint joint_of(const CeStats& st, const Upstream& u, const FactorPart* part, int parts) {
+    if (Q::N == 2 && u.reduction != DA_LOSS_ROWS) return {shift_of(st.maxes[kMaxX]) + u.shift(u.all()), rows_differ(st)};
+    FactorPart p = no_rows();
+    for (int k = threadIdx.x; k < parts; k += 256) p = joined(p, part[k]);
+    p = block_joined(p);
+    if (p.least > p.most) return {0, Q::N == 1};
+    const bool differ = Q::N == 1 || rows_differ(st) || p.least != p.most;
     return {differ ? p.sum : shift_of(st.maxes[kMaxX]) + p.least, differ};
 }
 
@@ -142,7 +242,8 @@ __global__ __launch_bounds__(256) void ce_count_kernel(const void* __restrict__ 
 
 // Lists them in order; the others' losses are 0.  counts: of the chunks, where there are several
 __global__ __launch_bounds__(256) void ce_index_kernel(const void* __restrict__ target, int wide, long rows, long classes, long chunk,
-                                                       const int* __restrict__ counts, CeStats st, float* __restrict__ loss)
+                                                       const int* __restrict__ counts, CeStats st, uint32_t* __restrict__ spread,
+                                                       float* __restrict__ loss)
 {
     __shared__ int red[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -155,6 +256,7 @@ __global__ __launch_bounds__(256) void ce_index_kernel(const void* __restrict__ 
         before = red[0] + red[1] + red[2] + red[3];
     }
     if (blockIdx.x == 0 && tid < kMaxes) st.maxes[tid] = 0;
+    if (blockIdx.x == 0 && tid < 3 * kSpread) spread[tid * kApart] = 0;
     const long r0 = blockIdx.x * chunk, r1 = min(r0 + chunk, rows);
     for (long r = r0 + tid; r - tid < r1; r += 256) {
         const long t = r < r1 ? target_of(target, wide, r) : -1;
@@ -192,46 +294,41 @@ __device__ __forceinline__ void keep_largest(uint32_t most, uint32_t* to) {
         if (most > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, most);
     }
 }
+// 4096 x 1024 x 8192: 16 us; 100000 x 700: 56.
 // Largest finite magnitudes: blockIdx.y 0 of the rows of x that count, and their shifts, 1 of w
 __global__ __launch_bounds__(256) void ce_max_kernel(const float* __restrict__ x, long ldx, CeStats st, long d, const float* __restrict__ w,
-                                                     long numbers)
+                                                     long numbers, uint32_t* __restrict__ spread)
 {
     uint32_t most = 0;                                       // of floats that are not negative bits are in order
     if (blockIdx.y == 0) {
-        const int count = *st.count, lane = threadIdx.x & 63;
+        if ((long)blockIdx.x * (256 / row_lanes(d, 4)) >= *st.count) return;
         uint32_t far = 0;
-        for (long m = (long)blockIdx.x * 4 + (threadIdx.x >> 6); m < count; m += (long)gridDim.x * 4) {
-            const float* __restrict__ row = x + (long)st.index[m] * ldx;
-            float here = 0.f;
-            long c = lane * 4;
-            for (; c + 4 <= d; c += 256) {
-                float v[4];
-                load_floats<4>(row + c, v);
-                here = fmaxf(fmaxf(here, fmaxf(magnitude(v[0]), magnitude(v[1]))), fmaxf(magnitude(v[2]), magnitude(v[3])));
-            }
-            for (; c < d; ++c) here = fmaxf(here, magnitude(row[c]));
-            for (int k = 1; k < 64; k <<= 1) here = fmaxf(here, __shfl_xor(here, k, 64));
+        each_row_most(x, ldx, st.index, *st.count, d, gridDim.x, [&](int m, float here, bool first) {
             const int shift = shift_of(__float_as_uint(here));
-            if (lane == 0) st.shift[m] = here > 0.f ? shift : kNoShift;
+            if (first) st.shift[m] = here > 0.f ? shift : kNoShift;
             if (here > 0.f) far = max(far, (uint32_t)(shift + kShiftBias));
             most = max(most, __float_as_uint(here));
-        }
-        keep_largest(far, st.maxes + kRowX);
+        });
+        keep_largest(far, spread_at(spread, kRowX, blockIdx.x));
     } else {
-        float here = 0.f;
+        constexpr int U = 4;                                 // pieces of the whole grid on their way
         const long step = (long)gridDim.x * 1024;
-        for (long c = ((long)blockIdx.x * 256 + threadIdx.x) * 4; c < numbers; c += step) {
-            if (c + 4 <= numbers) {
-                float v[4];
-                load_floats<4>(w + c, v);
-                here = fmaxf(fmaxf(here, fmaxf(magnitude(v[0]), magnitude(v[1]))), fmaxf(magnitude(v[2]), magnitude(v[3])));
-            } else {
-                for (long i = c; i < numbers; ++i) here = fmaxf(here, magnitude(w[i]));
-            }
+        float here = 0.f;
+        long c = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
+        for (; c + (U - 1) * step + 4 <= numbers; c += U * step) {
+            float v[U][4];
+#pragma unroll
+            for (int u = 0; u < U; ++u) load_floats<4>(w + c + u * step, v[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) here = fmaxf(here, magnitude(v[u][i]));
         }
+        for (; c < numbers; c += step)
+            for (long i = c; i < min(c + 4, numbers); ++i) here = fmaxf(here, magnitude(w[i]));
         most = __float_as_uint(here);
     }
-    keep_largest(most, st.maxes + (blockIdx.y == 0 ? kMaxX : kMaxW));
+    keep_largest(most, spread_at(spread, blockIdx.y == 0 ? kMaxX : kMaxW, blockIdx.x));
 }
 
 template <class T> __device__ __forceinline__ void store_row(T* p, int left, const float (&x)[4]) {
@@ -249,7 +346,7 @@ template <class T> __device__ __forceinline__ void store_row(T* p, int left, con
 // Packs lines of numbers, 8 numbers at a time; lines and their ends are padded with zeros.
 template <class T> struct PackJob {
     const T* from;
-    long ld, lines;
+    long ld, whole, lines;       // lines that there are, and of them to pack
     int n;
     const int *index, *count;    // not null: *count lines of a list, and zeros up to the next multiple of 64
     uint16_t* to;
@@ -275,28 +372,50 @@ template <class T> struct BeginJob {
         }
     }
 };
-// ... and, packed float32, x for dw
+// ... and x for dw, and bfloat16's w for dx, both in the numbers of dz; `to` null: not wanted
 struct JointJob {
     Upstream u;
     const FactorPart* part;
     int parts;
+    const int* shift;            // of the rows of x by themselves
     Joint* joint;
     uint16_t* to;
 };
-// blockIdx.y 0: x, 1: w, 2: begin, 3: x for dw
-template <class T, class P>
-__global__ __launch_bounds__(256) void ce_pack_kernel(CeStats st, PackJob<T> x, PackJob<T> w, BeginJob<T> begin, JointJob again)
+struct LinesJob {
+    const int* shift;            // of the lines of w
+    uint16_t* to;
+};
+// blockIdx.y 0: x, 1: w, 2: begin, 3: x for dw, 4: w for dx
+template <class T, class P, class Q>
+__global__ __launch_bounds__(256) void ce_pack_kernel(CeStats st, uint32_t* __restrict__ spread, PackJob<T> x, PackJob<T> w, BeginJob<T> begin,
+                                                      JointJob again, LinesJob lines)
 {
     if (blockIdx.y == 2) return begin.run(st);
-    Joint joint{};
-    PackJob<T> j = blockIdx.y == 1 ? w : x;
+    uint32_t largest = 0;                                    // of x, or of w
     if constexpr (P::N == 2) {
-        if (blockIdx.y == 3) {
-            joint = joint_of(st, again.u, again.part, again.parts);
-            if (blockIdx.x == 0 && threadIdx.x == 0) *again.joint = joint;
-            if (!joint.differ) return;
-            j.to = again.to;
+        if (spread) {                                        // forward: for the kernels after this one, too
+            largest = spread_most(spread, blockIdx.y == 1 ? kMaxW : kMaxX);
+            const uint32_t row = spread_most(spread, kRowX);
+            if (blockIdx.x == 0 && threadIdx.x == 0) {
+                st.maxes[blockIdx.y == 1 ? kMaxW : kMaxX] = largest;
+                if (blockIdx.y == 0) st.maxes[kRowX] = row;
+            }
+        } else {
+            largest = st.maxes[blockIdx.y == 1 ? kMaxW : kMaxX];
         }
+    }
+    Joint joint{};
+    PackJob<T> j = blockIdx.y == 1 || blockIdx.y == 4 ? w : x;
+    if (blockIdx.y == 4) {
+        j.lines = j.whole;
+        j.to = lines.to;
+    }
+    if (blockIdx.y == 3) {
+        if (!again.to) return;
+        joint = joint_of<Q>(st, again.u, again.part, again.parts);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *again.joint = joint;
+        if (!joint.differ) return;
+        j.to = again.to;
     }
     // 16 lines x 128 numbers at a time, four lines to a wave: whole lines of memory on both sides
     const int n = (int)padded(j.n), across = (n + 127) / 128;
@@ -321,16 +440,26 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(CeStats st, PackJob<T> x, 
                         x[i] = one[0];
                     }
             }
-            if constexpr (P::N == 2) {
+            if (P::N == 2 && blockIdx.y < 3) {
+                const int by = blockIdx.y == 1 ? shift_of(largest) : shift_of_row(st, (int)line, largest);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i], by);
+            }
+            if (blockIdx.y == 3) {
                 // a row that adds nothing to dw, its factor 0 or none, is not in the joint sum: no more than its own shift
-                const int by = blockIdx.y == 1   ? shift_of(st.maxes[kMaxW])
-                               : blockIdx.y == 0 ? shift_of_row(st, (int)line)
-                                                 : min(joint.sum - again.u.shift(again.u.row((int)line)), max(st.shift[line], shift_of(st.maxes[kMaxX])));
+                const int own = again.shift[line], by = own == kNoShift ? 0 : min(joint.sum - again.u.shift(again.u.row((int)line)), own);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i], by);
             }
         }
-        put_values<P, 8>(j.to + place<P>(j.layout, line, at), x);
+        if (P::N == 1 && blockIdx.y == 4 && line < there) {
+            const int by = lines.shift[line];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i], by);
+        }
+        uint16_t* const to = j.to + place<P>(j.layout, line, at);
+        if (blockIdx.y >= 3) put_values<Q, 8>(to, x);
+        else put_values<P, 8>(to, x);
     }
 }
 
@@ -434,28 +563,33 @@ template <class P> struct SumsOut : Logits<P> {
 };
 
 // dz of a piece of the classes that begins at `first`; rows behind the last one are 0
-template <class P> struct GradOut : Logits<P> {
+template <class P, class Q, bool BIAS> struct GradOut : Logits<P> {
     static constexpr bool kSymmetric = false, kWhole = true;
     Upstream u;
     int first;
     uint16_t* dz;
     Packed lz;
-    float* sums;                 // not null: [rows of a wave, one after the other][Nb], what they add to db, in 32 bits
+    int* up;                     // what a row of dz comes times, for dx; by the first columns' waves
+    float* sums;                 // BIAS: [rows of a wave, one after the other][Nb], what they add to db, in 32 bits
     // 16 rows at a time: a lane makes its numbers of one row, packed as they are in memory, and they leave by way of LDS in whole lines
     template <int MT, int NT>
     __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], int mw, int nw, int, char* lds, int Ma, int Nb) const {
         constexpr int BYTES = NT * 32 * P::N, PITCH = BYTES + 16, CHUNKS = BYTES / 16;
         const int lane = threadIdx.x & 63, i16 = lane & 15, h = lane >> 4, count = *this->st.count, n0 = first + nw;
         const auto c = this->template columns<NT>(n0);
-        float lse[MT], by[MT];
+        float lse[MT], by[MT], g[MT];
         int t[MT], shift[MT];
+        const bool each = u.reduction == DA_LOSS_ROWS;
+        const float all = each ? 0.f : u.all();
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int m = mw + i * 16 + i16;
             const bool there = m < count;
             lse[i] = there ? this->st.lse[m] : 0.f;
-            by[i] = there ? u.row(m) : 0.f;
-            if constexpr (P::N == 2) by[i] = ldexpf(by[i], u.shift(by[i]));
+            g[i] = there ? each ? u.row(m) : all : 0.f;
+            const int s = u.shift(g[i]);
+            by[i] = ldexpf(g[i], s);
+            if (there && h == 0 && n0 == 0) up[m] = s;
             shift[i] = P::N == 2 && there ? shift_of_row(this->st, m) : 0;
             t[i] = (there ? this->st.target[m] : -0x40000000) - n0 - 4 * h;
         }
@@ -477,18 +611,16 @@ template <class P> struct GradOut : Logits<P> {
                     for (int q = 0; q < 4; ++q)
                         if (t[i] == j * 16 + q) z[j][q] -= 1.f;
             const bool there = mw + i * 16 + i16 < count;    // a row that is not may hold anything
-            if (sums) {
-                const float g = there ? u.row(mw + i * 16 + i16) : 0.f;
+            if constexpr (BIAS)
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) sum[j][q] += there ? z[j][q] * g : 0.f;
-            }
+                    for (int q = 0; q < 4; ++q) sum[j][q] += there ? z[j][q] * g[i] : 0.f;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) z[j][q] = there && (c.inside || n0 + j * 16 + 4 * h + q < this->classes) ? z[j][q] * by[i] : 0.f;
-                put_values<P, 4>(in_line<P>(reinterpret_cast<uint16_t*>(lds + i16 * PITCH), j * 16 + 4 * h), z[j]);
+                put_values<Q, 4>(in_line<Q>(reinterpret_cast<uint16_t*>(lds + i16 * PITCH), j * 16 + 4 * h), z[j]);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");           // LDS serves a wave in order
             __builtin_amdgcn_wave_barrier();
@@ -501,7 +633,7 @@ template <class P> struct GradOut : Logits<P> {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
-        if (!sums || mw >= Ma || nw >= Nb) return;
+        if (!BIAS || mw >= Ma || nw >= Nb) return;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
 #pragma unroll
@@ -514,22 +646,33 @@ template <class P> struct GradOut : Logits<P> {
 constexpr int grad_rows(int shape) { return shape == 0 ? PlaneLarge::MT * 16 : shape == 1 ? PlaneMiddle::MT * 16 : PlaneSmall::MT * 16; }
 
 // dx, or what the pieces so far give of it
-template <class T, class P> struct InputOut {
+template <class T, class Q> struct InputOut {
     static constexpr bool kSymmetric = false, kWhole = false;
-    Upstream u;
     CeStats st;
+    const int* shift;            // of dz's rows
     const float* before;         // dense rows x ldb, packed rows
     float* after;                // where not null: the sum goes here instead of to dx
     long ldb;
     T* dx;
     int d;
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
-        if (m >= *st.count || n >= d) return;
-        if constexpr (P::N == 2) {
-            const int down = -(shift_of(st.maxes[kMaxW]) + u.shift(u.row(m)));
-#pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = ldexpf(x[q], down);
+    const int* lines;            // bfloat16: shifts of w's
+    struct Column {
+        int count, down[4];
+    };
+    __device__ __forceinline__ Column column(int n) const {
+        if constexpr (Q::N == 2) {
+            const int w = -shift_of(st.maxes[kMaxW]);
+            return {*st.count, {w, w, w, w}};
+        } else {
+            const int4 w = n < d ? *reinterpret_cast<const int4*>(lines + n) : make_int4(0, 0, 0, 0);
+            return {*st.count, {-w.x, -w.y, -w.z, -w.w}};
         }
+    }
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int, const Column& c) const {
+        if (m >= c.count || n >= d) return;
+        const int up = shift[m];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] = ldexpf(x[q], c.down[q] - up);
         if (before) {
             float u[4];
             load_floats<4>(before + (long)m * ldb + n, u);
@@ -541,19 +684,17 @@ template <class T, class P> struct InputOut {
     }
 };
 
-template <class T, class P> struct WeightOut {
+template <class T> struct WeightOut {
     static constexpr bool kSymmetric = false, kWhole = false;
     const Joint* joint;
     T* dw;                       // of the piece
     long ldw;
     int d, classes;              // of the piece
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int) const {
+    __device__ __forceinline__ int column(int) const { return -joint->sum; }
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int, int down) const {
         if (m >= d || n >= classes) return;
-        if constexpr (P::N == 2) {
-            const int down = -joint->sum;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = ldexpf(x[q], down);
-        }
+        for (int q = 0; q < 4; ++q) x[q] = ldexpf(x[q], down);
         store_row(dw + (long)m * ldw + n, classes - n, x);
     }
 };
@@ -609,15 +750,46 @@ __global__ __launch_bounds__(256) void ce_join_kernel(CeStats st, const float2* 
     if (threadIdx.x == 0) *loss_all = (float)(mean ? total / max(1, count) : total);
 }
 
-// The rows' shifts that dw has to bring together, by parts of the rows
-__global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, Upstream u, FactorPart* __restrict__ part)
+// What dz and x have to bring together for dw, by parts of the rows; with bfloat16 the shifts of x's rows are taken first, and beside them
+// (blockIdx.y 1) those of w's lines, a line to a wave or, if it is long, to a block
+template <class T>
+__global__ __launch_bounds__(256) void ce_factor_kernel(CeStats st, Upstream u, const T* __restrict__ x, long ldx, int d, int* __restrict__ shift,
+                                                        FactorPart* __restrict__ part, int parts, const T* __restrict__ w, int classes,
+                                                        int* __restrict__ lines)
 {
+    if (blockIdx.y == 1) {
+        __shared__ float red[4];
+        const bool block = classes > kLongLine;
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, teams = block ? 1 : 4;
+        const long per = block ? (classes + 31) / 32 * 8 : classes, c0 = block ? wave * per : 0;             // a wave's quarter of a line
+        for (long line = (long)blockIdx.x * teams + (block ? 0 : wave); line < d; line += (long)gridDim.x * teams) {
+            float most = most_of(w + line * classes + c0, max(0l, min(per, classes - c0)), lane, 64);
+            if (block) {
+                __syncthreads();                             // those of the line before have been read
+                if (lane == 0) red[wave] = most;
+                __syncthreads();
+                most = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+            }
+            if (lane == 0 && (!block || wave == 0)) lines[line] = shift_of(__float_as_uint(most));
+        }
+        return;
+    }
+    if ((int)blockIdx.x >= parts) return;
     const int count = *u.count;
     FactorPart p = no_rows();
-    for (long m = (long)blockIdx.x * 256 + threadIdx.x; m < count; m += (long)gridDim.x * 256) {
-        const float g = magnitude(u.row((int)m));
-        const int own = st.shift[m], t = u.shift(g);
+    auto add = [&](int m, int own) {
+        const float g = magnitude(u.row(m));
+        const int t = u.shift(g);
         if (g > 0.f && own != kNoShift) p = joined(p, {own + t, t, t});
+    };
+    if constexpr (sizeof(T) == 4) {
+        for (long m = (long)blockIdx.x * 256 + threadIdx.x; m < count; m += (long)parts * 256) add((int)m, shift[m]);
+    } else {
+        each_row_most(x, ldx, st.index, count, d, parts, [&](int m, float here, bool first) {
+            const int own = here > 0.f ? shift_of(__float_as_uint(here)) : kNoShift;
+            if (first) shift[m] = own;
+            add(m, own);
+        });
     }
     p = block_joined(p);
     if (threadIdx.x == 0) part[blockIdx.x] = p;
@@ -768,8 +940,8 @@ struct CePlan {
     int slots;
     int64_t piece;               // classes of a piece, a multiple of 64 where there are several
     PiecePlan whole, rest;       // products of a whole piece and of the last one
-    size_t counts_at, sums_at, target_at, x_at, w_at, part_at, forward;          // bytes
-    size_t arrived_at, dz_at, dx_at, bias_at, sum_at, again_at, factor_at, backward;
+    size_t spread_at, counts_at, sums_at, target_at, x_at, w_at, part_at, forward;          // bytes
+    size_t arrived_at, dz_at, dx_at, bias_at, sum_at, again_at, factor_at, shift_at, wide_at, lines_at, up_at, backward;
     bool shifts() const { return !narrow.taken && !tall.taken && !few.taken && halves; }
     bool halves;
 };
@@ -825,6 +997,7 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
     p.x_at = take((size_t)p.Ma * p.D * 2 * N);
     p.w_at = take((size_t)p.D * p.Vb * 2 * N);
     const size_t both = at;
+    p.spread_at = take(3 * kSpread * kApart * 4);
     p.counts_at = take((size_t)p.chunks * 4);
     p.sums_at = take(kJoinBlocks * sizeof(double));
     p.target_at = take((size_t)p.Ma * 4);
@@ -844,8 +1017,12 @@ CePlan make_ce_plan(int dtype, const CeShape& s) {
     p.bias_at = take((size_t)ceil_div(p.Ma, std::min(grad_rows(p.whole.logits.shape), grad_rows(p.rest.logits.shape))) * Pb * 4);
     for (const PiecePlan& q : {p.whole, p.rest}) sums = std::max({sums, plane_part_bytes(q.input, 1), plane_part_bytes(q.weight, 1)});
     p.sum_at = take(sums);
-    p.again_at = take(N == 2 ? (size_t)p.Ma * p.D * 2 * N : 0);
-    p.factor_at = take(N == 2 ? kFactorParts * sizeof(FactorPart) : 0);
+    p.again_at = take((size_t)p.Ma * p.D * 2 * N);
+    p.factor_at = take(kFactorParts * sizeof(FactorPart));
+    p.shift_at = take(N == 1 ? (size_t)s.rows * 4 : 0);
+    p.up_at = take((size_t)s.rows * 4);
+    p.wide_at = take(N == 1 ? (size_t)p.D * p.Vb * 2 : 0);
+    p.lines_at = take(N == 1 ? (size_t)p.D * 4 : 0);
     p.backward = at;
     return p;
 }
@@ -889,29 +1066,32 @@ struct CeCall {
     hipStream_t stream;
 };
 
-template <class T> const uint16_t* pack_operands(const CeCall& c, const BeginJob<T>& begin, const JointJob& again, Packed* lw) {
+template <class T>
+const uint16_t* pack_operands(const CeCall& c, const BeginJob<T>& begin, const JointJob& again, const LinesJob& lines, Packed* lw) {
     typedef PlaneOf<T> P;
     const T* x = static_cast<const T*>(c.x);
     const T* w = static_cast<const T*>(c.w);
+    uint32_t* const spread = begin.arrived ? nullptr : reinterpret_cast<uint32_t*>(c.ws + c.p.spread_at);
     if constexpr (P::N == 2) {
         if (!begin.arrived) {                                // kept for the backward pass
             const int64_t most = std::max(ceil_div(c.s.rows, 4), ceil_div(c.s.d * c.s.V, 4096));
             hipLaunchKernelGGL(ce_max_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 1024)), 2), dim3(256), 0, c.stream, x,
-                               (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V));
+                               (long)c.ldx, c.st, (long)c.s.d, w, (long)(c.s.d * c.s.V), spread);
         }
     }
     auto job = [&](const T* from, long ld, long lines, int n, const int* index, size_t to) {
-        return PackJob<T>{from, ld, lines, n, index, c.st.count, reinterpret_cast<uint16_t*>(c.ws + to), packed(padded(lines), n, P::N)};
+        return PackJob<T>{from, ld, lines, lines, n, index, c.st.count, reinterpret_cast<uint16_t*>(c.ws + to), packed(padded(lines), n, P::N)};
     };
     const PackJob<T> jx = job(x, c.ldx, c.s.rows, (int)c.s.d, c.st.index, c.p.x_at), jw = job(w, c.s.V, c.s.d, (int)c.s.V, nullptr, c.p.w_at);
     // a weight of whole pads is read where it is
     const bool direct = P::N == 1 && c.s.d % kPad == 0 && c.s.V % kPad == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
-    const int64_t tiles = std::max(c.p.Ma / 16 * ceil_div(c.p.D, 128), direct ? 0 : c.p.D / 16 * ceil_div(c.p.Vb, 128));
+    const int64_t tiles = std::max(c.p.Ma / 16 * ceil_div(c.p.D, 128), direct && !lines.to ? 0 : c.p.D / 16 * ceil_div(c.p.Vb, 128));
     PackJob<T> jw_here = jw;
-    if (direct) jw_here.lines = jw_here.n = 0;
+    if (direct) jw_here.lines = 0;
     if (tiles || begin.arrived)
-        hipLaunchKernelGGL((ce_pack_kernel<T, P>), dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(tiles, 8192)), again.to ? 4 : begin.arrived ? 3 : direct ? 1 : 2),
-                           dim3(256), 0, c.stream, c.st, jx, jw_here, begin, again);
+        hipLaunchKernelGGL((ce_pack_kernel<T, P, GradOf<T>>),
+                           dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(tiles, 8192)), lines.to ? 5 : again.to ? 4 : begin.arrived ? 3 : direct ? 1 : 2),
+                           dim3(256), 0, c.stream, c.st, spread, jx, jw_here, begin, again, lines);
     *lw = direct ? packed_lines(c.s.V) : jw.layout;
     return direct ? reinterpret_cast<const uint16_t*>(w) : jw.to;
 }
@@ -947,9 +1127,10 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
                            (long)c.p.chunk, counts);
     float* rows = reduction == DA_LOSS_ROWS ? loss : nullptr;
     hipLaunchKernelGGL(ce_index_kernel, dim3((unsigned)c.p.chunks), dim3(256), 0, c.stream, target, target64, (long)c.s.rows, (long)c.s.V,
-                       (long)c.p.chunk, several ? counts : nullptr, c.st, rows);
+                       (long)c.p.chunk, several ? counts : nullptr, c.st,
+                       reinterpret_cast<uint32_t*>(c.ws + c.p.spread_at), rows);
     Packed lw{};
-    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{}, JointJob{}, &lw);
+    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{}, JointJob{}, LinesJob{}, &lw);
     SumsOut<P> out{};
     fill(out, c);
     out.part = reinterpret_cast<float2*>(c.ws + c.p.part_at);
@@ -967,19 +1148,28 @@ void ce_forward(const CeCall& c, const void* target, int target64, int reduction
 template <class T>
 void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t stride, T* dx, T* dw, void* db) {
     typedef PlaneOf<T> P;
+    typedef GradOf<T> Q;
     int* arrived = reinterpret_cast<int*>(c.ws + c.p.arrived_at);
     Joint* joint = reinterpret_cast<Joint*>(c.ws);
     const Upstream u{dloss, (long)stride, reduction, c.st.count, c.st.index};
     if (c.s.d == 0) dx = dw = nullptr;
     JointJob again{};
-    if (P::N == 2 && dw && c.s.V > 0) {
-        FactorPart* factors = reinterpret_cast<FactorPart*>(c.ws + c.p.factor_at);
-        again = JointJob{u, factors, (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, 256), kFactorParts)), joint,
-                         reinterpret_cast<uint16_t*>(c.ws + c.p.again_at)};
-        if (reduction == DA_LOSS_ROWS) hipLaunchKernelGGL(ce_factor_kernel, dim3((unsigned)again.parts), dim3(256), 0, c.stream, c.st, u, factors);
+    LinesJob lines{};
+    FactorPart* factors = reinterpret_cast<FactorPart*>(c.ws + c.p.factor_at);
+    int* shift = P::N == 2 ? c.st.shift : reinterpret_cast<int*>(c.ws + c.p.shift_at);
+    int* line_shift = reinterpret_cast<int*>(c.ws + c.p.lines_at);
+    const int64_t at_once = P::N == 2 ? 256 : 256 / row_lanes(c.s.d, sizeof(T)) * kAtOnce;
+    const int parts = dw ? (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(c.s.rows, at_once), kFactorParts)) : 0;
+    if (dw && c.s.V > 0) again = JointJob{u, factors, parts, shift, joint, reinterpret_cast<uint16_t*>(c.ws + c.p.again_at)};
+    if (P::N == 1 && dx && c.s.V > 0) lines = LinesJob{line_shift, reinterpret_cast<uint16_t*>(c.ws + c.p.wide_at)};
+    if ((again.to || lines.to) && (P::N == 1 || reduction == DA_LOSS_ROWS)) {
+        const int64_t line_blocks = lines.to ? std::min<int64_t>(ceil_div(c.s.d, c.s.V > kLongLine ? 1 : 4), 4096) : 0;
+        hipLaunchKernelGGL((ce_factor_kernel<T>), dim3((unsigned)std::max<int64_t>(parts, line_blocks), lines.to ? 2 : 1), dim3(256), 0, c.stream, c.st,
+                           u, static_cast<const T*>(c.x), (long)c.ldx, (int)c.s.d, shift, factors, parts, static_cast<const T*>(c.w), (int)c.s.V,
+                           line_shift);
     }
     Packed lw{};
-    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{(long)c.s.rows, (int)c.s.d, dx, arrived}, again, &lw);
+    const uint16_t* w = pack_operands<T>(c, BeginJob<T>{(long)c.s.rows, (int)c.s.d, dx, arrived}, again, lines, &lw);
     if (c.s.V == 0) return;
     uint16_t* dz = reinterpret_cast<uint16_t*>(c.ws + c.p.dz_at);
     float* acc = reinterpret_cast<float*>(c.ws + c.p.dx_at);
@@ -989,37 +1179,44 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
         const int64_t width = std::min(c.p.piece, c.s.V - first), Vb = padded(width);
         const PiecePlan& q = width == c.p.piece ? c.p.whole : c.p.rest;
         const Packed lz = packed(c.p.Ma, width, P::N);
-        GradOut<P> grad{};
-        fill(grad, c);
-        grad.u = u;
-        grad.first = (int)first;
-        grad.dz = dz;
-        grad.lz = lz;
-        grad.sums = db ? bias : nullptr;
-        plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, lw, first, width), grad, q.logits, 1, nullptr, nullptr, c.stream);
+        int* const up = reinterpret_cast<int*>(c.ws + c.p.up_at);
+        auto gradient = [&](auto out) {
+            fill(out, c);
+            out.u = u;
+            out.first = (int)first;
+            out.dz = dz;
+            out.lz = lz;
+            out.up = up;
+            out.sums = bias;
+            plane_product<P, kAlong, kAcross, kBoundM>(logits_args<P>(c, w, lw, first, width), out, q.logits, 1, nullptr, nullptr, c.stream);
+        };
+        if (db) gradient(GradOut<P, Q, true>{});
+        else gradient(GradOut<P, Q, false>{});
         if (dx) {
             PlaneArgs a{};
             a.A = dz;
             a.a = lz;
-            a.B = w + place<P>(lw, 0, first);
-            a.b = lw;
+            const Packed lb = P::N == 2 ? lw : packed(c.p.D, c.s.V, 1);
+            a.B = (P::N == 2 ? w : lines.to) + place<Q>(lb, 0, first);
+            a.b = lb;
             a.Ma = (int)c.p.Ma;
             a.Nb = (int)c.p.D;
             a.K = (int)Vb;
             a.rows = c.st.count;
-            InputOut<T, P> out{};
-            out.u = u;
+            InputOut<T, Q> out{};
             out.st = c.st;
+            out.shift = up;
             out.before = first > 0 ? acc : nullptr;
             out.after = first + width < c.s.V ? acc : nullptr;
             out.ldb = c.p.D;
             out.dx = dx;
             out.d = (int)c.s.d;
-            plane_product<P, kAlong, kAlong, kBoundM>(a, out, q.input, 1, part, arrived, c.stream);
+            out.lines = line_shift;
+            plane_product<Q, kAlong, kAlong, kBoundM>(a, out, q.input, 1, part, arrived, c.stream);
         }
         if (dw) {
             PlaneArgs a{};
-            a.A = reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at);
+            a.A = P::N == 2 ? reinterpret_cast<const uint16_t*>(c.ws + c.p.x_at) : again.to;
             a.a = packed(c.p.Ma, c.s.d, P::N);
             a.B = dz;
             a.b = lz;
@@ -1027,10 +1224,10 @@ void ce_backward(const CeCall& c, int reduction, const float* dloss, int64_t str
             a.Nb = (int)Vb;
             a.K = (int)c.p.Ma;
             a.rows = c.st.count;
-            a.other = again.to ? &joint->differ : nullptr;
+            a.other = P::N == 2 ? &joint->differ : nullptr;
             a.A_other = again.to;
-            const WeightOut<T, P> out{joint, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
-            plane_product<P, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, arrived, c.stream);
+            const WeightOut<T> out{joint, dw + first, (long)c.s.V, (int)c.s.d, (int)width};
+            plane_product<Q, kAcross, kAcross, kBoundK>(a, out, q.weight, 1, part, arrived, c.stream);
         }
         if (db) {
             hipLaunchKernelGGL(ce_bias_join_kernel, dim3((unsigned)ceil_div(width, 16)), dim3(256), 0, c.stream, bias, c.st.count,

@@ -147,7 +147,8 @@ struct GramOut {
     Packed la;
     long batch_a;
     float by;                    // of the product to A's scale
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
+    __device__ __forceinline__ NoColumn column(int) const { return {}; }
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch, NoColumn) const {
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] *= by;
         put_values<Halves, 4>(A + batch * batch_a + place<Halves>(la, m, n), x);
@@ -157,7 +158,7 @@ struct GramOut {
 struct PolyOut : GramOut {
     const uint16_t* from;        // A, laid out like the result
     float b, c;                  // with the scales
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch, NoColumn) const {
         float a[4];
         get_values<Halves, 4>(from + batch * batch_a + place<Halves>(la, m, n), a);
 #pragma unroll
@@ -173,13 +174,14 @@ struct StepOut {
     Packed lx;
     long batch_x;
     float a, by;                 // with the scales
+    __device__ __forceinline__ NoColumn column(int) const { return {}; }
     __device__ __forceinline__ void value(int m, int n, float (&x)[4], int batch) const {
         float old[4];
         get_values<Halves, 4>(from + batch * batch_x + place<Halves>(lx, m, n), old);
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q] = a * old[q] + by * x[q];
     }
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch, NoColumn) const {
         value(m, n, x, batch);
         put_values<Halves, 4>(to + batch * batch_x + place<Halves>(lx, m, n), x);
     }
@@ -188,7 +190,7 @@ struct StepOut {
 template <class T> struct LastOut : StepOut {
     T* out;
     int rows, cols;
-    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch) const {
+    __device__ __forceinline__ void four(int m, int n, float (&x)[4], int batch, NoColumn) const {
         if (m >= rows || n >= cols) return;
         value(m, n, x, batch);
         T* __restrict__ p = out + (long)batch * rows * cols + (long)m * cols + n;

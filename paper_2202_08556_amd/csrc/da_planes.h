@@ -1,7 +1,7 @@
 // Matrices as the matrix cores take them: packed in 16-bit numbers, padded with zeros to multiples of 64 both ways, and
 // products of them whose epilogues are those of the operators that use them.
 //
-// A number is one bf16 (One), or the sum of two fp16 (Halves): the nearest fp16 and what that leaves.  A pair has 22 bits;
+// A number is one bf16 (One), one fp16 (Half), or the sum of two fp16 (Halves): the nearest fp16 and what that leaves.  A pair has 22 bits;
 // they come times a power of two, for an array or for each of its rows, that takes the largest below 2^15, and the second half of numbers 2^18
 // times less begins to lose bits, 2^-25 of the scale.  The product of two pairs is three instructions of 16-bit numbers
 // (the fourth, of both second halves, is below the 22 bits) in place of one of 32-bit numbers at a sixteenth of the rate.
@@ -43,13 +43,23 @@ __host__ __device__ inline Packed packed(long lines, long n, int N) {
 struct One {
     static constexpr int N = 1, STEP = 64;                   // numbers of a value, inner positions of a step
     typedef bf16x8 Frag;
+    typedef bf16 Number;
     static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+struct Half {
+    static constexpr int N = 1, STEP = 64;
+    typedef f16x8 Frag;
+    typedef _Float16 Number;
+    static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
 };
 struct Halves {
     static constexpr int N = 2, STEP = 32;
     typedef f16x8 Frag;
+    typedef _Float16 Number;
     static __device__ __forceinline__ f32x4 mul(const Frag& a, const Frag& b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
@@ -67,7 +77,7 @@ template <class P, int V> __device__ __forceinline__ void put_values(uint16_t* t
     if constexpr (P::N == 1) {
         Bits b;
 #pragma unroll
-        for (int i = 0; i < V; ++i) b[i] = __builtin_bit_cast(uint16_t, (bf16)x[i]);
+        for (int i = 0; i < V; ++i) b[i] = __builtin_bit_cast(uint16_t, (typename P::Number)x[i]);
         *reinterpret_cast<Bits*>(to) = b;
     } else {
         Bits first, second;
@@ -83,16 +93,11 @@ template <class P, int V> __device__ __forceinline__ void put_values(uint16_t* t
     }
 }
 template <class P, int V> __device__ __forceinline__ void get_values(const uint16_t* from, float (&x)[V]) {
+    static_assert(P::N == 2, "pairs");
     typedef uint16_t Bits __attribute__((ext_vector_type(V)));
-    if constexpr (P::N == 1) {
-        const Bits b = *reinterpret_cast<const Bits*>(from);
+    const Bits first = *reinterpret_cast<const Bits*>(from), second = *reinterpret_cast<const Bits*>(from + 32);
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = __uint_as_float((uint32_t)b[i] << 16);
-    } else {
-        const Bits first = *reinterpret_cast<const Bits*>(from), second = *reinterpret_cast<const Bits*>(from + 32);
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)first[i]) + (float)__builtin_bit_cast(_Float16, (uint16_t)second[i]);
-    }
+    for (int i = 0; i < V; ++i) x[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)first[i]) + (float)__builtin_bit_cast(_Float16, (uint16_t)second[i]);
 }
 
 // One operand's part of a step in LDS: OUTER x STEP values, lines of 128 bytes (along) or of OUTER values (across).
@@ -199,6 +204,8 @@ __device__ __forceinline__ void half_tile(int block, int tiles, int* bm, int* bn
     *bn = m + block;
 }
 
+struct NoColumn {};                          // of an epilogue that asks for nothing
+
 // BM x BN results to a block of WM x WN waves, STAGES steps in LDS, asked for STAGES - 1 steps ahead.
 template <int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PIPED_> struct PlaneShape {
     static constexpr bool PIPED = PIPED_;        // two steps' fragments in registers
@@ -212,8 +219,8 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PIPED_> struct P
     static constexpr int OCCUPANCY = LDS > 80 * 1024 ? THREADS / 256 : 2 * THREADS / 256;
 };
 
-// E: the epilogue.  epi.tile(...) gets a wave's fragments and its part of LDS if E::kWhole, otherwise epi.four(m, n, x, batch) four
-// neighbouring results at a time, after their sums are whole.  E::kSymmetric: only tiles on and above the diagonal are computed;
+// E: the epilogue.  epi.tile(...) gets a wave's fragments and its part of LDS if E::kWhole, otherwise epi.four(m, n, x, batch, column) four
+// neighbouring results at a time, after their sums are whole; column is epi.column(n), asked for once for all of a lane's rows.  E::kSymmetric: only tiles on and above the diagonal are computed;
 // the results of those above it are handed over a second time, turned around.
 template <class P, class S, int ALAY, int BLAY, int BOUND, class E>
 __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::OCCUPANCY, S::OCCUPANCY))) void plane_kernel(PlaneArgs g, E epi)
@@ -443,6 +450,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
         // Results leave by way of LDS, 16 rows of the wave at a time, so that a store is whole lines
         constexpr int LANES = NT * 4, ROWS = 64 / LANES;
         const int row0 = lane / LANES, col = lane % LANES * 4, n = nw + col;
+        const auto column = epi.column(n);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
@@ -454,7 +462,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
                 const int row = p * ROWS + row0, m = mw + i * 16 + row;
                 float x[4];
                 load_floats<4>(reinterpret_cast<const float*>(mine + row * S::PITCH) + col, x);
-                if (m < g.Ma && n < g.Nb) epi.four(m, n, x, batch);
+                if (m < g.Ma && n < g.Nb) epi.four(m, n, x, batch, column);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -478,7 +486,7 @@ __global__ __launch_bounds__(S::THREADS) __attribute__((amdgpu_waves_per_eu(S::O
                     const int row = p * DOWN + lane / ACROSS, at = lane % ACROSS * 4, m = nw + j * 16 + row, n = mw + at;
                     float x[4];
                     load_floats<4>(reinterpret_cast<const float*>(turned + row * TURNED) + at, x);
-                    if (m < g.Nb && n < g.Ma) epi.four(m, n, x, batch);
+                    if (m < g.Nb && n < g.Ma) epi.four(m, n, x, batch, epi.column(n));
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();

@@ -253,7 +253,7 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Te
     "sum" their sum, "mean" that over the number of rows with a target (0 where there is none).  A weight whose rows are not
     dense (a transposed one, say) is copied at every call, forward and backward.
 
-    Large products run on the 16-bit matrix cores: with bfloat16 the gradient of the logits is rounded to it, and float32 has 22 bits
+    Large products run on the 16-bit matrix cores: the gradient of the logits has 11 bits there with bfloat16, and float32 has 22 bits
     of a number, fewer of those far smaller than the largest of their row of x (2^-35 of it), than their row's
     gradient (2^-40) or than the largest of the weight (2^-40).  Rows do not depend on each other's size (include/da_training.h)."""
     try:

@@ -2,7 +2,7 @@
 partial gradients, graphs.  Each test says which kernels the call launches, so that sizes cannot move to another way unseen.
 
 Tolerances as in the tests of the formula, but for each row by itself: what its results are off by follows from its own numbers, its
-own factor and the weight, never from other rows.  Pairs of halves keep 2^-35 of a row's largest x (2^-36 and a bit for the
+own factor and the weight, never from other rows.  With bfloat16 dz has the 11 bits of fp16 for dx and dw.  Pairs of halves keep 2^-35 of a row's largest x (2^-36 and a bit for the
 row's scale), 2^-39 of its factor for dz, 2^-39 of the largest w; a row adds to dw with an error of 2^-37 of the largest product of
 a row's x and its factor."""
 import pytest
@@ -83,14 +83,11 @@ def formula(x, w, b, t, g):
     # z is the largest logit and lse above it: whatever the logits are off by, p is off by 1 and a little at most
     t_p = torch.nan_to_num(p * torch.expm1(2 * D + (K + 4 * away) * E), nan=1.0, posinf=1.0).clamp(max=1.0) + 2.0 ** -20 * p
     t_sum = gm * (t_p + 4 * E * (p + one))                   # db adds what has not been rounded as an operand
-    t_dz = t_sum + dz.abs() * (2.0 ** -22 if halves else 2.0 ** -8)
-    if halves:
-        t_dz = t_dz + 2.0 ** -39 * gm
+    t_dz = t_sum + dz.abs() * (2.0 ** -22 if halves else 2.0 ** -11) + 2.0 ** -39 * gm         # pairs, or one fp16 number
     dx, t_dx = torch.mm(dz, W.t()), torch.mm(t_dz, W.abs().t()) + ((V / 16 + 16) * E + extra) * torch.mm(dz.abs(), W.abs().t())
     dw, t_dw = torch.mm(X.t(), dz), torch.mm(X.abs().t(), t_dz) + ((rows / 16 + 80) * E + extra) * torch.mm(X.abs().t(), dz.abs())
-    if halves:
-        t_dx = t_dx + 2.0 ** -38 * V * gm * wm
-        t_dw = t_dw + 2.0 ** -37 * rows * (xm * gm).max()
+    t_dx = t_dx + 2.0 ** -38 * V * gm * wm                   # the weight's numbers far below the largest, or those of its line
+    t_dw = t_dw + 2.0 ** -37 * rows * (xm * gm).max()
     db, t_db = dz.sum(0), t_sum.sum(0) + (rows / 16 + 80) * E * dz.abs().sum(0)
     place = lambda v: torch.zeros(rows, *v.shape[1:], dtype=v.dtype).index_copy(0, keep, v)             # noqa: E731
     return [(place(loss), place(t_loss), E), (place(dx), place(t_dx), U[dtype]), (dw, t_dw, U[dtype])] + \
