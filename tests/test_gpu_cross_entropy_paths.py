@@ -189,11 +189,12 @@ def test_infinite_weights(way, dtype):
 
 
 @EACH
-def test_rows_of_very_different_size(way):
-    """float32: what a row's loss and gradient are off by does not depend on other rows."""
-    x, w, b, t, g = make(way, F32)
+@TYPES
+def test_rows_of_very_different_size(way, dtype):
+    """What a row's loss and gradient are off by does not depend on other rows."""
+    x, w, b, t, g = make(way, dtype)
     rows = x.shape[0]
-    size = torch.logspace(-6, 1, rows, device="cuda")
+    size = torch.logspace(-6, 1, rows, device="cuda").to(dtype)
     takes(way, x * size[:, None], w, b, t, g)
     check(x * size[:, None], w, b, t, g * torch.logspace(-5, 0, rows, device="cuda"))
     for k in (1e8, 1e12, 1e25):                              # one number, and one row's factor, far beyond the others
@@ -204,7 +205,7 @@ def test_rows_of_very_different_size(way):
         check(x, w, b, t, f)
         check(y, w, b, t, f / k)
     check(x, w, b, t, g * torch.logspace(-20, 0, rows, device="cuda"))
-    check(x * torch.logspace(-20, 0, rows, device="cuda")[:, None], w, b, t, g * torch.logspace(0, -20, rows, device="cuda"))
+    check(x * torch.logspace(-20, 0, rows, device="cuda")[:, None].to(dtype), w, b, t, g * torch.logspace(0, -20, rows, device="cuda"))
     f = g.clone()
     f[::2] = 0.0
     check(x, w, b, t, f)
@@ -215,11 +216,13 @@ def test_rows_of_very_different_size(way):
 
 
 @EACH
-def test_weights_of_very_different_size(way):
-    """float32: the weight has one scale, and numbers of it keep 2^-39 of the largest."""
-    x, w, b, t, g = make(way, F32)
-    V = w.shape[1]
-    check(x, w * torch.logspace(-4, 0, V, device="cuda"), b, t, g)
+@TYPES
+def test_weights_of_very_different_size(way, dtype):
+    """The weight has one scale, or one for each line with bfloat16, and numbers of it keep 2^-39 of the largest under one."""
+    x, w, b, t, g = make(way, dtype)
+    d, V = w.shape
+    check(x, w * torch.logspace(-4, 0, V, device="cuda").to(dtype), b, t, g)
+    check(x, w * torch.logspace(-4, 0, d, device="cuda").to(dtype)[:, None], b, t, g)
     for k in (1e-20, 1e20, 1e-35, 1e33):                     # logits as they were, between numbers that are far from 1
         check(x * k, w / k, b, t, g)
     check(x * 0, w, b, t, g)
@@ -227,12 +230,13 @@ def test_weights_of_very_different_size(way):
 
 
 @EACH
+@TYPES
 @pytest.mark.parametrize("reduction", ["sum", "mean"])
-def test_rows_of_very_different_size_reduced(way, reduction):
-    x, w, b, t, g = make(way, F32, share=0.7)
+def test_rows_of_very_different_size_reduced(way, dtype, reduction):
+    x, w, b, t, g = make(way, dtype, share=0.7)
     rows = x.shape[0]
     t[0] = 3
-    x = x * torch.logspace(6, -8, rows, device="cuda")[:, None]
+    x = x * torch.logspace(6, -8, rows, device="cuda")[:, None].to(dtype)
     takes(way, x, w, b, t, g, reduction=reduction)
     got = run(x, w, b, t, g, reduction=reduction)
     count = int((t >= 0).sum()) if reduction == "mean" else 1
