@@ -1,8 +1,9 @@
-// Cross entropy of a linear layer for 5 to 64 rows of float32, or 5 to 16 of bfloat16: the weight is still what has to be read, and
+// Cross entropy of a linear layer for 5 to 64 rows of float32, or 5 to 32 of bfloat16: the weight is still what has to be read, and
 // packing it reads and writes it once more than a product does.  The fp32 matrix cores take it as it comes; with 64 rows they are as
 // busy as memory (16 x 16 x 4 products for every 16 rows of 64 bytes).  Forward and backward by rows, against packing the weight:
-//   4096 x 32000 float32   5: 464   32: 510   64: 707   65, packed: 1368 us      1000 x 100000   5: 363   32: 447   64: 653   65: 1046
-//   ... bfloat16           5: 270   16: 282   17, packed: 285; 17 here: 403                      5: 278   16: 296   17: 427, here 386
+//   4096 x 32000 float32   5: 464   32: 510   64: 680   65, packed: 1340 us      1000 x 100000   5: 363   32: 447   64: 653   65: 1046
+//   ... bfloat16           5: 270   16: 280   32: 403   33, packed: 460; 40 here: 520            5: 278   16: 293   32: 403   33: 583, 40 here 502
+// 64 rows of float32 are what the registers hold; packing would be the better way from some 140 on.
 // The logits of 64 rows take 177 us of the matrix cores' 109, the other products 400 of 218.
 //
 // Logits: a block of four waves has 64 classes, a wave every fourth 16 of its lines; a lane loads 16 bytes of four lines, which are the
@@ -14,7 +15,7 @@
 
 namespace daspmm {
 
-template <class T> constexpr int some_rows = sizeof(T) == 4 ? kSomeRows : 16;
+template <class T> constexpr int some_rows = sizeof(T) == 4 ? kSomeRows : 32;
 constexpr int kSomeStep = 64, kSomePitch = kSomeStep + 4;      // classes of a step
 
 // Blocks to a unit whose registers there have to be, backward and for logits

@@ -4,12 +4,11 @@
 //
 // Forward, a tile of z leaves as the maximum and the sum of exponentials of each of its rows in 64 (or fewer) columns; these are
 // joined by rows.  Backward, z is computed again a piece of the classes at a time, and leaves as dz, which the other two
-// products read: eight operations for each of rows x d x classes instead of six, and no logits in memory.
+// products read: eight operations for each of rows x d x classes instead of six, and nothing of the logits' size is kept.
 // Rows that have a target are gathered first (x is packed for the products anyway), and the products stop at their number,
 // which only the device knows: rows without one cost nothing and may hold anything.
 // db is summed where dz is made, before it is rounded as an operand.
-// The scales by row cost 1 to 3 % (float32, 4096 x 1024 x 8192: 775 and 778 us, rows far apart 765 and 795), and a packing of x where the rows' factors
-// differ (100000 x 700 x 130: 959 and 1114).
+// Where float32 rows differ in size or factor x is packed twice (100000 x 700 x 130: 955 us with one factor, 1080 with one for each row).
 // 4096 x 2048 x 65536 bf16, forward and backward: 3940 us, 1120 TFLOP/s; the four products 860 to 1000 each, the more the larger
 // their epilogues, w's largest numbers 46 and its packing 120.
 #include "da_training.h"
@@ -1375,10 +1374,10 @@ FewArgs few_args(const CeCall& c, int reduction) {
     return a;
 }
 template <class T, class G> void by_some(int rows, const G& go) {
-    if (some_rows<T> == 16 || rows <= 16) go(std::integral_constant<int, 1>());
-    else if constexpr (some_rows<T> > 16) {
-        if (rows <= 32) go(std::integral_constant<int, 2>());
-        else if (rows <= 48) go(std::integral_constant<int, 3>());
+    if (rows <= 16) return go(std::integral_constant<int, 1>());
+    if (some_rows<T> == 32 || rows <= 32) return go(std::integral_constant<int, 2>());
+    if constexpr (some_rows<T> > 32) {
+        if (rows <= 48) go(std::integral_constant<int, 3>());
         else go(std::integral_constant<int, 4>());
     }
 }

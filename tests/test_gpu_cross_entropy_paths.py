@@ -23,6 +23,7 @@ WAYS = {
     "tall": ((100, 300, 60), "ce_tall_weight_kernel"),
     "few": ((3, 32, 700), "ce_few_products_kernel"),
     "some": ((15, 32, 700), "ce_some_products_kernel"),
+    "some_more": ((31, 32, 700), "ce_some_products_kernel"),
     "packed": ((200, 32, 700), "plane_kernel"),
     "packed_wide": ((300, 200, 2100), "plane_kernel"),       # several tiles both ways
 }
