@@ -7,7 +7,7 @@
 // numbers of one magnitude, whose roundings are all alike, off by up to 5e-3.
 // X is held with the shorter side as rows (a tall matrix is turned around on its way in and out).  A and A^2 are symmetric:
 // only tiles on and above the diagonal are computed, and each is written to both of its places.
-// 2048 x 8192 bf16, five steps: 1600 us; a step's products 105, 53 and 160.  1187 x 602 float32: 175, of which a kernel's start, its
+// 2048 x 8192 bf16, five steps: 1600 us; a step's products 106, 51 and 174.  1187 x 602 float32: 175, of which a kernel's start, its
 // first loads from what another die's cache wrote, and its end are some 5 of each launch's 11.
 // The scales of X, A and b A + c A^2 follow from how large singular values can be: at most 1 at first (the Frobenius norm
 // bounds them), then by the polynomial's extremes, which the host takes.

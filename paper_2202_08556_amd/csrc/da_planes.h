@@ -6,7 +6,7 @@
 // times less begins to lose bits, 2^-25 of the scale.  The product of two pairs is three instructions of 16-bit numbers
 // (the fourth, of both second halves, is below the 22 bits) in place of one of 32-bit numbers at a sixteenth of the rate.
 //
-// Rates: bf16, 4096 x 65536 . 65536 x 2048 1240 TFLOP/s, pairs, 2048 x 2048 . 2048 x 8192 430 (1290 of single products); the general
+// Rates: bf16, 4096 x 65536 . 65536 x 2048 1240 TFLOP/s, fp16 1270, pairs, 2048 x 2048 . 2048 x 8192 400 (1190 of single products); the general
 // library's 8192^3 in bf16 1276, in float32 154.  Tiles of 256 x 256 have one block to a unit, whose LDS holds two steps of 64 KB; those
 // of 128 and 64 have two, and read the next step's fragments while they multiply this one's.
 //

@@ -245,7 +245,9 @@ class _LinearCrossEntropy(torch.autograd.Function):
 
 def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, bias: torch.Tensor | None = None,
                          reduction: str = "mean") -> torch.Tensor:
-    """Cross entropy of the logits x . weight + bias against a target class a row; the logits are never in memory.
+    """Cross entropy of the logits x . weight + bias against a target class a row.  Nothing of the logits' size is kept for the
+    backward pass; a call holds packed copies of x and the weight and a piece of the logits' gradient of up to 512 MB (1024 classes, if that
+    is more), or, up to 64 rows, the logits themselves.
 
     x (..., d), weight (d, classes), both float32 or both bfloat16; bias: a number a class, float32 or bfloat16.  target
     (...), int32 or int64: a row whose target is outside 0 .. classes - 1 (-1 or -100, say) has none; it adds nothing to the loss
