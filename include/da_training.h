@@ -61,14 +61,19 @@ int da_rms_norm_backward(int dtype, int64_t rows, int64_t channels, const void *
  *   dloss     float32, like loss; dloss_stride (DA_LOSS_ROWS) 0 takes dloss[0] for every row
  *   dx, dw, db   dense, of the types of x, w and b; any of them may be NULL and is then not computed
  *
- * The backward call computes the logits again, a piece of the classes at a time: workspaces hold x and w packed and dz of a piece, up to
- * 512 MB or 1024 classes (up to 64 rows: all logits and dz, in 32 bits).  Sums are held in 32 bits.  Up to 128 classes of up to 256 inner positions (with
- * many of both: up to 64 classes), and up to 64 rows (bfloat16: 32), the products are of 32-bit numbers for both types.  Beyond that operands are
- * packed for the 16-bit matrix cores.  With bfloat16 dz has the 11 bits of fp16 for dx and dw then; float32 is multiplied as pairs of halves, 22 bits of a
- * number, fewer of small ones: those of a row of x are off by up to 2^-35 of the row's largest, those of dz by 2^-40 of the row's factor, those of w by
- * 2^-40 of the largest of all (bfloat16: of its line, where a number is less than 2^32 times smaller it is exact).  Loss and dx of a row do not depend on other rows; to dw a row adds with an error of up to 2^-37 of
- * the largest product of any row's largest x and its factor.  Limits: rows <= 2^26, d, classes <= 2^22, and fewer than 2^23
- * tiles of 256 x 256 of any of the products' results (DA_ERR_UNSUPPORTED beyond).
+ * The backward call computes the logits again, a piece of the classes at a time: workspaces hold x and w packed and dz of a
+ * piece, up to 512 MB or 1024 classes (for few rows: all logits and dz, in 32 bits).  Sums are held in 32 bits.
+ *
+ * Products are of 32-bit numbers for both types up to 128 classes of up to 256 inner positions (with many of both: up to 64
+ * classes), and up to 64 rows (bfloat16: 32).  Beyond that operands are packed for the 16-bit matrix cores:
+ *   bfloat16   dz has the 11 bits of fp16 for dx and dw; x and w are exact
+ *   float32    is multiplied as pairs of fp16, 22 bits of a number
+ * Small numbers have fewer bits: those of a row of x are off by up to 2^-35 of the row's largest (float32), those of dz by 2^-40
+ * of the row's factor, those of w by 2^-40 of the largest of all (bfloat16: of its line).  Loss and dx of a row do not depend on
+ * other rows; to dw a row adds with an error of up to 2^-37 of the largest product of any row's largest x and its factor.
+ *
+ * Limits: rows <= 2^26, d, classes <= 2^22, and fewer than 2^23 tiles of 256 x 256 of any of the products' results
+ * (DA_ERR_UNSUPPORTED beyond).
  */
 enum { DA_LOSS_ROWS = 0, DA_LOSS_SUM = 1, DA_LOSS_MEAN = 2 };
 int da_linear_cross_entropy_sizes(int dtype, int64_t rows, int64_t d, int64_t classes, size_t *stats_bytes, size_t *forward_bytes,
