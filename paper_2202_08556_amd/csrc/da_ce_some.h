@@ -3,6 +3,7 @@
 // busy as memory (16 x 16 x 4 products for every 16 rows of 64 bytes).  Forward and backward by rows, against packing the weight:
 //   4096 x 32000 float32   5: 464   32: 510   64: 680   65, packed: 1340 us      1000 x 100000   5: 363   32: 447   64: 653   65: 1046
 //   ... bfloat16           5: 270   16: 280   32: 403   33, packed: 460; 40 here: 520            5: 278   16: 293   32: 403   33: 583, 40 here 502
+// (forward and backward; forward alone, whose weight needs no packing where its sizes are whole, 32 rows of bfloat16 take 96 here and 60 packed).
 // 64 rows of float32 are what the registers hold; packing would be the better way from some 140 on.
 // The logits of 64 rows take 177 us of the matrix cores' 109, the other products 400 of 218.
 //
